@@ -1,4 +1,4 @@
-"""ctypes binding of the C-ABI library (``include/tcu_scan.h``): same names, argument
+"""ctypes binding of the C-ABI library (``include/tcu_scan.h``, ``include/tcu_lm.h``): same names, argument
 marshalling only.  Every step of the scan runs in the library's CUDA kernels; PyTorch is
 used by callers for device memory and streams.  There is no fallback: if the compiled
 library is missing, importing this module raises.
@@ -7,6 +7,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libtcu_scan.so")
@@ -15,6 +16,7 @@ TCU_OK, TCU_ERR_INVALID_ARG, TCU_ERR_UNSUPPORTED, TCU_ERR_WORKSPACE, TCU_ERR_CUD
 TCU_SCAN_NOALLOC_MAX_ELEMENTS = 1 << 26
 TCU_I8_I32, TCU_F16_F32, TCU_BF16_F32 = range(3)
 DTYPES = {"i8": TCU_I8_I32, "f16": TCU_F16_F32, "bf16": TCU_BF16_F32}
+TCU_F32, TCU_F16, TCU_BF16 = range(3)
 
 if not os.path.exists(LIB_PATH):
     raise ImportError(
@@ -87,6 +89,21 @@ _lib.tcu_widen_copy.argtypes = [_vp, _vp, _sz, _int, _vp]
 _lib.tcu_widen_copy.restype = _int
 _lib.tcu_scan_last_stats.argtypes = [ctypes.POINTER(TcuScanStats)]
 _lib.tcu_scan_last_stats.restype = _int
+_f32, _u64 = ctypes.c_float, ctypes.c_uint64
+_lib.tcu_linattn_workspace_bytes.argtypes = []
+_lib.tcu_linattn_workspace_bytes.restype = _sz
+_lib.tcu_linattn_forward.argtypes = [ctypes.c_char_p, _vp, _sz, _vp]
+_lib.tcu_linattn_forward.restype = _int
+_lib.tcu_linattn_backward.argtypes = [ctypes.c_char_p, _vp, _sz, _vp]
+_lib.tcu_linattn_backward.restype = _int
+_lib.tcu_linattn_step.argtypes = [ctypes.c_char_p, _vp]
+_lib.tcu_linattn_step.restype = _int
+_lib.tcu_embedding_forward.argtypes = [_vp, _int, _sz, _vp, _sz, _sz, _sz, _int, _f32, _vp, _vp]
+_lib.tcu_embedding_forward.restype = _int
+_lib.tcu_embedding_workspace_bytes.argtypes = [_sz, _sz, _sz]
+_lib.tcu_embedding_workspace_bytes.restype = _sz
+_lib.tcu_embedding_backward.argtypes = [_vp, _int, _vp, _int, _sz, _sz, _sz, _f32, _int, _vp, _int, _vp, _sz, _vp]
+_lib.tcu_embedding_backward.restype = _int
 _lib.tcu_status_string.argtypes = [_int]
 _lib.tcu_status_string.restype = ctypes.c_char_p
 
@@ -203,6 +220,51 @@ def tcu_sort_u32(d_keys_in, d_keys_out, n: int, d_tmp, tmp_bytes: int, d_ws, ws_
 
 def tcu_widen_copy(d_in, d_out, n: int, dt: int, stream=0) -> int:
     return _lib.tcu_widen_copy(_p(d_in), _p(d_out), n, dt, stream)
+
+
+# tcu_linattn_t, packed as bytes (a call costs less this way than through a ctypes.Structure of nested structures): every
+# member is naturally aligned, a token array is (pointer, stride_batch, stride_token, stride_head)
+_LINATTN = struct.Struct("=IIQQIIIfQQQQ" + "Qqqq" * 4 + "QQ" + "Qqqq" * 4 + "QQ")
+NO_TOKENS = (0, 0, 0, 0)
+
+
+def tcu_linattn_args(dtype: int, batch: int, tokens: int, heads: int, dk: int, dv: int, scale: float, d_log_decay: int, q, k, v, o=NO_TOKENS, *,
+                     d_offsets: int = 0, d_slots: int = 0, pool_slots: int = 0, d_state_in: int = 0, d_state_out: int = 0, d_o=NO_TOKENS,
+                     d_q=NO_TOKENS, d_k=NO_TOKENS, d_v=NO_TOKENS, d_dstate_out: int = 0, d_dstate_in: int = 0) -> bytes:
+    """The argument structure of the linear-attention calls; pointers are integers (0 for NULL)."""
+    return _LINATTN.pack(_LINATTN.size, dtype, batch, tokens, heads, dk, dv, scale, d_log_decay, d_offsets, d_slots, pool_slots,
+                         *q, *k, *v, *o, d_state_in, d_state_out, *d_o, *d_q, *d_k, *d_v, d_dstate_out, d_dstate_in)
+
+
+def tcu_linattn_workspace_bytes() -> int:
+    return int(_lib.tcu_linattn_workspace_bytes())
+
+
+def tcu_linattn_forward(args: bytes, d_ws, ws_bytes: int, stream=0) -> int:
+    return _lib.tcu_linattn_forward(args, _p(d_ws), ws_bytes, stream)
+
+
+def tcu_linattn_backward(args: bytes, d_ws, ws_bytes: int, stream=0) -> int:
+    return _lib.tcu_linattn_backward(args, _p(d_ws), ws_bytes, stream)
+
+
+def tcu_linattn_step(args: bytes, stream=0) -> int:
+    return _lib.tcu_linattn_step(args, stream)
+
+
+def tcu_embedding_forward(d_ids, id_bytes: int, n: int, d_table, rows: int, d: int, table_stride: int, dtype: int, scale: float, d_out,
+                          stream=0) -> int:
+    return _lib.tcu_embedding_forward(_p(d_ids), id_bytes, n, _p(d_table), rows, d, table_stride, dtype, scale, _p(d_out), stream)
+
+
+def tcu_embedding_workspace_bytes(n: int, rows: int, d: int) -> int:
+    return int(_lib.tcu_embedding_workspace_bytes(n, rows, d))
+
+
+def tcu_embedding_backward(d_out, dtype: int, d_ids, id_bytes: int, n: int, rows: int, d: int, scale: float, accumulate: int, d_table,
+                           table_dtype: int, d_ws, ws_bytes: int, stream=0) -> int:
+    return _lib.tcu_embedding_backward(_p(d_out), dtype, _p(d_ids), id_bytes, n, rows, d, scale, int(accumulate), _p(d_table), table_dtype,
+                                       _p(d_ws), ws_bytes, stream)
 
 
 def tcu_scan_last_stats() -> dict:

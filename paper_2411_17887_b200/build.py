@@ -10,8 +10,10 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "libtcu_scan.so")
-SOURCES = [os.path.join(HERE, "csrc", "tcu_scan.cu")]
-DEPENDS = SOURCES + [os.path.join(HERE, "csrc", "tcu_scan_kernel.cuh"), os.path.join(ROOT, "include", "tcu_scan.h")]
+SOURCES = [os.path.join(HERE, "csrc", name) for name in ("tcu_scan.cu", "tcu_lm.cu")]
+DEPENDS = SOURCES + [os.path.join(HERE, "csrc", name) for name in ("tcu_scan_kernel.cuh", "tcu_split.cuh", "tcu_linattn_kernel.cuh",
+                                                                   "tcu_embedding_kernel.cuh")]
+DEPENDS += [os.path.join(ROOT, "include", name) for name in ("tcu_scan.h", "tcu_lm.h")]
 
 
 PROFILE_LIB = os.path.join(HERE, "libtcu_scan_profile.so")   # the debug build with per-role wait counters
@@ -19,7 +21,7 @@ PROFILE_LIB = os.path.join(HERE, "libtcu_scan_profile.so")   # the debug build w
 
 def nvcc_command(out: str, verbose: bool = False, profile: bool = False):
     cmd = ["nvcc", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-           "-shared", "-Xcompiler", "-fPIC", "-I", os.path.join(ROOT, "include"), "-o", out] + SOURCES
+           "--threads", "0", "-shared", "-Xcompiler", "-fPIC", "-I", os.path.join(ROOT, "include"), "-o", out] + SOURCES
     if verbose:
         cmd[1:1] = ["-Xptxas", "-v"]
     if profile:
