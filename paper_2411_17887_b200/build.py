@@ -11,8 +11,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "libtcu_scan.so")
 SOURCES = [os.path.join(HERE, "csrc", name) for name in ("tcu_scan.cu", "tcu_lm.cu")]
-DEPENDS = SOURCES + [os.path.join(HERE, "csrc", name) for name in ("tcu_scan_kernel.cuh", "tcu_split.cuh", "tcu_linattn_kernel.cuh",
-                                                                   "tcu_embedding_kernel.cuh")]
+DEPENDS = SOURCES + [os.path.join(HERE, "csrc", name) for name in ("tcu_ptx.cuh", "tcu_scan_kernel.cuh", "tcu_split.cuh", "tcu_linattn_kernel.cuh", "tcu_embedding_kernel.cuh")]
 DEPENDS += [os.path.join(ROOT, "include", name) for name in ("tcu_scan.h", "tcu_lm.h")]
 
 

@@ -1,9 +1,12 @@
 // Host side of the C ABI declared in include/tcu_lm.h: argument checks, launches.
 #include "tcu_lm.h"
 
+#include <cuda.h>
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <initializer_list>
+#include <mutex>
 
 #include "tcu_embedding_kernel.cuh"
 #include "tcu_linattn_kernel.cuh"
@@ -51,6 +54,11 @@ tcu_status_t check_tokens(const tcu_tokens_t &x, bool packed, uint64_t batch, ui
 
 MixTokens view(const tcu_tokens_t &x) { return {x.ptr, x.stride_batch, x.stride_token, x.stride_head}; }
 
+// where a workspace keeps its status word: the header of a scan workspace, which tcu_scan_device_status reads
+struct WsStatus {
+    uint32_t epoch, done, error;
+};
+
 // What forward and backward share.  `empty` is set when there is nothing to walk (states may still have to be written).
 tcu_status_t check_linattn(const tcu_linattn_t *a, const void *d_ws, size_t ws_bytes) {
     if (!has_struct(a)) return TCU_ERR_INVALID_ARG;
@@ -69,22 +77,128 @@ tcu_status_t check_linattn(const tcu_linattn_t *a, const void *d_ws, size_t ws_b
     return TCU_OK;
 }
 
-tcu_status_t run_mix(const tcu_linattn_t *a, const MixParams &p, cudaStream_t stream) {
-    const uint32_t most = a->dk > a->dv ? a->dk : a->dv;
-    const dim3 grid(uint32_t(a->batch) * a->heads * p.jobs, (most + kMixCols - 1) / kMixCols);
-    if (a->type == TCU_F16) tcu_linattn_mix_kernel<__half><<<grid, 128, 0, stream>>>(p);
-    else tcu_linattn_mix_kernel<__nv_bfloat16><<<grid, 128, 0, stream>>>(p);
-    return launched();
+typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                  const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiledFn encode_fn() {
+    static std::once_flag once;
+    static EncodeTiledFn fn = nullptr;
+    std::call_once(once, [] {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess)
+            fn = reinterpret_cast<EncodeTiledFn>(p);
+    });
+    return fn;
 }
 
-MixParams mix_params(const tcu_linattn_t *a) {
-    MixParams p = {};
+// (feature, token, head, sequence) view, tiles of 64 features x 128 tokens; features past the width and tokens past the end read as
+// zero and are not written.  An axis along which the array repeats has an extent of 1 in the map.
+bool encode_tokens(CUtensorMap *map, const tcu_linattn_t *a, const tcu_tokens_t &x, uint32_t width) {
+    const bool packed = a->d_offsets != nullptr;
+    const uint64_t nb = packed || x.stride_batch == 0 ? 1 : a->batch, nh = x.stride_head == 0 ? 1 : a->heads;
+    const cuuint64_t dims[4] = {width, a->tokens, nh, nb};
+    auto bytes = [](uint64_t extent, int64_t stride) { return extent > 1 ? cuuint64_t(stride) * 2 : cuuint64_t(16); };   // (not used when the extent is 1)
+    const cuuint64_t strides[3] = {bytes(a->tokens, x.stride_token), bytes(nh, x.stride_head), bytes(nb, x.stride_batch)};
+    const cuuint32_t box[4] = {64, kGroup, 1, 1}, step[4] = {1, 1, 1, 1};
+    return encode_fn()(map, a->type == TCU_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, x.ptr, dims, strides, box, step,
+                       CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                       CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+int sm_count() {
+    static std::atomic<int> cached{0};
+    int v = cached.load();
+    if (v > 0) return v;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&v, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+    cached.store(v);
+    return v;
+}
+
+constexpr long long kMixSpinLimit = 2000000000LL;       // cycles: about a second
+
+template <int D, typename T>
+tcu_status_t launch_mix(const MixParams &p, cudaStream_t stream) {
+    static std::atomic<int> configured{-1};
+    int dev = 0;
+    cudaGetDevice(&dev);
+    if (configured.load() != dev) {
+        if (cudaFuncSetAttribute(tcu_linattn_mix_kernel<D, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMixSmemBytes<D>) != cudaSuccess) return TCU_ERR_CUDA;
+        configured.store(dev);
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(p.batch * p.heads * p.jobs * p.ranks);
+    cfg.blockDim = dim3(kMixThreads);
+    cfg.dynamicSmemBytes = kMixSmemBytes<D>;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = p.ranks;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = p.ranks > 1 ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, tcu_linattn_mix_kernel<D, T>, p) == cudaSuccess ? TCU_OK : TCU_ERR_CUDA;
+}
+
+// `transposed`: the state that enters is stored as dv x dk.
+MixJob make_job(const uint8_t (&maps)[4], uint32_t dk, uint32_t dv, bool forward, const float *init, bool transposed, float *last, float in_scale,
+                float out_scale) {
+    MixJob j = {};
+    for (int i = 0; i < 4; ++i) j.map[i] = maps[i];
+    j.init = init;
+    j.last = last;
+    j.init_k = transposed ? 1 : dv;
+    j.init_v = transposed ? dk : 1;
+    j.dk = dk;
+    j.dv = dv;
+    j.lead = forward ? 1 : 0;
+    j.in_scale = in_scale;
+    j.out_scale = out_scale;
+    return j;
+}
+
+// Fills in what all jobs share and launches.  `arrays`: what the jobs' map indexes name.
+tcu_status_t run_mix(const tcu_linattn_t *a, MixParams &p, const tcu_tokens_t *const *arrays, const uint32_t *widths, int count, void *d_ws, cudaStream_t stream) {
+    int dev = 0;                      // (encoding needs a current context, which a thread that has made no CUDA call does not have)
+    if (!encode_fn() || cudaGetDevice(&dev) != cudaSuccess || cudaSetDevice(dev) != cudaSuccess) return TCU_ERR_CUDA;
+    for (int i = 0; i < count; ++i)
+        if (!encode_tokens(&p.map[i], a, *arrays[i], widths[i])) return TCU_ERR_CUDA;
     p.log_decay = a->d_log_decay;
     p.offsets = a->d_offsets;
+    p.error = &static_cast<WsStatus *>(d_ws)->error;
     p.tokens = a->tokens;
     p.batch = uint32_t(a->batch);
     p.heads = a->heads;
-    return p;
+    p.spin_limit = kMixSpinLimit;
+    for (uint32_t j = 0; j < p.jobs; ++j) {
+        MixJob &job = p.job[j];
+        for (int i = 0; i < 4; ++i) {
+            job.by_batch[i] = arrays[job.map[i]]->stride_batch != 0;
+            job.by_head[i] = arrays[job.map[i]]->stride_head != 0;
+        }
+        const tcu_tokens_t &o = *arrays[job.map[3]];
+        job.o = o.ptr;
+        job.o_batch = o.stride_batch;
+        job.o_token = o.stride_token;
+        job.o_head = o.stride_head;
+    }
+    const bool wide = a->dk > 64 || a->dv > 64;
+    // a walk is split over the blocks of a cluster while that leaves every block a few groups and no SM without work
+    const uint64_t sms = uint64_t(sm_count()), units = a->batch * a->heads * p.jobs, room = sms * (wide ? 1 : 2);
+    const uint64_t groups = ((a->d_offsets ? a->tokens / a->batch : a->tokens) + kGroup - 1) / kGroup;
+    p.ranks = 1;
+    while (p.ranks < 8 && units * p.ranks * 2 <= room && groups >= p.ranks * 8) p.ranks *= 2;
+    if (a->type == TCU_F16) return wide ? launch_mix<128, __half>(p, stream) : launch_mix<64, __half>(p, stream);
+    return wide ? launch_mix<128, __nv_bfloat16>(p, stream) : launch_mix<64, __nv_bfloat16>(p, stream);
+}
+
+// No tokens: the state that leaves is the state that enters.
+tcu_status_t copy_state(float *to, const float *from, size_t bytes, cudaStream_t stream) {
+    if (!to || to == from) return TCU_OK;
+    const cudaError_t e = from ? cudaMemcpyAsync(to, from, bytes, cudaMemcpyDeviceToDevice, stream) : cudaMemsetAsync(to, 0, bytes, stream);
+    return e == cudaSuccess ? TCU_OK : TCU_ERR_CUDA;
 }
 
 }  // namespace
@@ -110,10 +224,13 @@ tcu_status_t tcu_linattn_forward(const tcu_linattn_t *a, void *d_ws, size_t ws_b
     } else if (!a->d_state_out) {
         return TCU_OK;
     }
-    MixParams p = mix_params(a);
+    if (a->tokens == 0) return copy_state(a->d_state_out, a->d_state_in, size_t(a->batch) * a->heads * a->dk * a->dv * 4, stream);
+    const tcu_tokens_t *arrays[4] = {&a->q, &a->k, &a->v, &a->o};
+    const uint32_t widths[4] = {a->dk, a->dk, a->dv, a->dv};
+    MixParams p = {};
     p.jobs = 1;
-    p.job[0] = {view(a->q), view(a->k), view(a->v), view(a->o), a->d_state_in, a->d_state_out, a->dv, 1, a->dk, a->dv, 1, 1.0f, a->scale};
-    return run_mix(a, p, stream);
+    p.job[0] = make_job({0, 1, 2, 3}, a->dk, a->dv, true, a->d_state_in, false, a->d_state_out, 1.0f, a->scale);
+    return run_mix(a, p, arrays, widths, 4, d_ws, stream);
 }
 
 tcu_status_t tcu_linattn_backward(const tcu_linattn_t *a, void *d_ws, size_t ws_bytes, cudaStream_t stream) {
@@ -137,12 +254,16 @@ tcu_status_t tcu_linattn_backward(const tcu_linattn_t *a, void *d_ws, size_t ws_
     }
     const size_t state = size_t(a->batch) * a->heads * a->dk * a->dv * 4;
     if (overlaps(a->d_dstate_in, state, a->d_dstate_out, state) || overlaps(a->d_dstate_in, state, a->d_state_in, state)) return TCU_ERR_INVALID_ARG;
-    MixParams p = mix_params(a);
+    if (a->tokens == 0) return copy_state(a->d_dstate_in, a->d_dstate_out, state, stream);
+    enum { kQ, kK, kV, kDo, kDq, kDk, kDv };
+    const tcu_tokens_t *arrays[7] = {&a->q, &a->k, &a->v, &a->d_o, &a->d_q, &a->d_k, &a->d_v};
+    const uint32_t widths[7] = {a->dk, a->dk, a->dv, a->dv, a->dk, a->dk, a->dv};
+    MixParams p = {};
     p.jobs = 3;
-    p.job[0] = {view(a->d_o), view(a->v), view(a->k), view(a->d_q), a->d_state_in, nullptr, 1, a->dv, a->dv, a->dk, 1, 1.0f, a->scale};
-    p.job[1] = {view(a->k), view(a->q), view(a->d_o), view(a->d_v), a->d_dstate_out, a->d_dstate_in, a->dv, 1, a->dk, a->dv, 0, a->scale, 1.0f};
-    p.job[2] = {view(a->v), view(a->d_o), view(a->q), view(a->d_k), a->d_dstate_out, nullptr, 1, a->dv, a->dv, a->dk, 0, a->scale, 1.0f};
-    return run_mix(a, p, stream);
+    p.job[0] = make_job({kDo, kV, kK, kDq}, a->dv, a->dk, true, a->d_state_in, true, nullptr, 1.0f, a->scale);
+    p.job[1] = make_job({kK, kQ, kDo, kDv}, a->dk, a->dv, false, a->d_dstate_out, false, a->d_dstate_in, a->scale, 1.0f);
+    p.job[2] = make_job({kV, kDo, kQ, kDk}, a->dv, a->dk, false, a->d_dstate_out, true, nullptr, a->scale, 1.0f);
+    return run_mix(a, p, arrays, widths, 7, d_ws, stream);
 }
 
 tcu_status_t tcu_linattn_step(const tcu_linattn_t *a, cudaStream_t stream) {
