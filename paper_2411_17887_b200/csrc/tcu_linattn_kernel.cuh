@@ -18,16 +18,16 @@
 //     S = Q K^T,  O = P V with P = S * decays (rounded to the 16-bit type, A operand in tensor memory),
 //     E = Q X  (X rounded to the 16-bit type),  X^T += V^T K~  with K~ = decayed keys in two 16-bit terms.
 //
-// A block (one job, sequence, head and - in a cluster - part of the walk) runs the groups one after another.  Warps:
-//     8     TMA producer: K, Q, V of each group into a ring of five tiles
-//     9     tcgen05.mma issuer
-//     0-3   thread = token: scores -> P, then O + decayed E -> the slot that held Q
-//     4-7   thread = column of v: X out of tensor memory, rounded into the operand of E, multiplied by a^L and put back;
-//           thread = token: K -> K~
-//     10    TMA store of the outputs
+// A block (one job, sequence, head and - in a cluster - part of the walk) runs the groups one after another.  Roles:
+//     tokens    (8 warps, 4 when dk, dv <= 64) thread = token: scores -> P, then O + decayed E -> the slot that held Q
+//     state     (as many) thread = column of v: X out of tensor memory, rounded into the operand of E, multiplied by a^L and put
+//               back; thread = token: K -> K~
+//     producer  TMA: K, Q, V of each group into a ring of five tiles
+//     issuer    tcgen05.mma
+//     store     TMA: the outputs
 // Rounded to 16 bits are only operands of a product: P, and X as operand of E (the state itself stays in 32 bits in tensor
-// memory).  K~ enters the state in two terms, 16 bits of mantissa and more, because states are results of their own.  In
-// float16 X and K~ are brought to the type's range by powers of two found for every group, because a state without decay
+// memory).  K~ enters the state in two terms in float16, 22 bits of mantissa, and in three in bfloat16, 24 bits (two, 16
+// bits, left states 2e-6 to 5e-6 off where 32-bit sums are 2e-7 off).  In float16 X and K~ are brought to the type's range by powers of two found for every group, because a state without decay
 // outgrows the type and the low terms of small keys fall below it.
 //
 // When there are fewer (job, sequence, head) than SMs, the walk is split over the blocks of a cluster: each block first
@@ -52,7 +52,6 @@ namespace tcu {
 
 constexpr int kGroup = 128;              // tokens of a group: M of the products
 constexpr int kMixSlots = 5;             // tiles in the ring
-constexpr int kMixThreads = 352;
 constexpr int kHalfBytes = 16384;        // 128 tokens x 64 features: one 128-byte-swizzled block of rows
 constexpr int kMixCtlBytes = 2048;
 
@@ -89,7 +88,9 @@ struct MixCtl {
     uint64_t full[kMixSlots], empty[kMixSlots];
     uint64_t qk_done;                    // S is in tensor memory
     uint64_t x_ready;                    // X rounded into its operand, and multiplied by a^L in tensor memory
-    uint64_t kt_ready;                   // K~ written (and rows past the end of V cleared)
+    uint64_t kt_ready;                   // two terms of K~ written (and rows past the end of V cleared)
+    uint64_t two_done;                   // ... and multiplied
+    uint64_t third_ready;                // third term written over the second
     uint64_t p_ready;                    // P in tensor memory
     uint64_t o_done;                     // O and E are in tensor memory
     uint64_t o_free;                     // ... and have been read
@@ -98,13 +99,17 @@ struct MixCtl {
     uint64_t drained;
     uint32_t tmem_base;
     volatile uint32_t abort_flag;
-    float biggest[2][8];                 // float16: largest |k| and |X| seen by each of the four warps
+    float biggest[2][16];                // float16: largest |k| and |X| seen by each warp
     float unscale[2];                    // float16: the factor that takes E back to the size of X
     float power[kGroup + 4];             // a^m
-    float block[32];                     // factors of P along a block of 32 tokens
+    alignas(16) float block[32];         // factors of P along a block of 32 tokens
+    float near[32 + kGroup + 32];        // factors of P by distance, from 31 tokens on the wrong side of the diagonal (zero) on
 };
 static_assert(sizeof(MixCtl) <= kMixCtlBytes, "control block too large");
 
+// warps of the token role and of the state role: a thread has 64 columns of a row, of X and of K; then producer, issuer, store
+template <int D> constexpr int kMixRoleWarps = D / 16;
+template <int D> constexpr int kMixThreads = 32 * (2 * kMixRoleWarps<D> + 3);
 template <int D> constexpr int kMixTileBytes = D / 64 * kHalfBytes;
 template <int D> constexpr int kMixSmemBytes = 1024 + kMixCtlBytes + (kMixSlots + 1) * kMixTileBytes<D> + D * D * 2;
 static_assert(kMixSmemBytes<128> <= 232448 && 2 * (kMixSmemBytes<64> + 1024) <= 233472, "shared memory of an SM");
@@ -126,6 +131,20 @@ template <> struct Half2<__half> {
     }
     static __device__ __forceinline__ float2 unpack(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2 *>(&w)); }
 };
+
+// two products, sums at once
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    float2 r;
+    asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmul.rn.f32x2 z, x, y;\n\tmov.b64 {%0, %1}, z;\n\t}"
+        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 r;
+    asm("{\n\t.reg .b64 x, y, z, u;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\tfma.rn.f32x2 u, x, y, z;\n\tmov.b64 {%0, %1}, u;\n\t}"
+        : "=f"(r.x), "=f"(r.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return r;
+}
 
 struct MixWaiter {
     MixCtl *ctl;
@@ -173,14 +192,18 @@ struct MixPart {
 };
 
 template <int D, typename T>
-__global__ void __launch_bounds__(kMixThreads, D == 64 ? 2 : 1) tcu_linattn_mix_kernel(const __grid_constant__ MixParams p) {
+__global__ void __launch_bounds__(kMixThreads<D>, D == 64 ? 2 : 1) tcu_linattn_mix_kernel(const __grid_constant__ MixParams p) {
     using H = Half2<T>;
     constexpr bool kIsHalf = std::is_same<T, __half>::value;
+    constexpr bool kThird = !kIsHalf;                             // K~ in three terms
     constexpr int kTile = kMixTileBytes<D>;
     constexpr int kXHalf = D * 128;                               // one 64-wide half of the operand X: D rows of 128 bytes
-    // tensor memory: S (P in its first 64 columns), O, E, X.  With D = 64 O lies in the half of S that P leaves free, and two
-    // blocks share an SM.
+    constexpr int kWarps = kMixRoleWarps<D>, kRole = kWarps * 32; // warps and threads of the token role, and of the state role
+    // tensor memory: S, O, E, X.  P takes the place of S; with D = 128 two warps share the 128 columns of a token, so each
+    // 64 columns of S leave their P in their own first 32 columns.  With D = 64 P fills the first 64 columns of S and O the
+    // others, and two blocks share an SM.
     constexpr uint32_t kColS = 0, kColO = D == 128 ? 128 : 64, kColE = D == 128 ? 256 : 128, kColX = D == 128 ? 384 : 192;
+    constexpr uint32_t kColP1 = D == 128 ? 64 : 32;               // P of tokens 64 ... 127
     constexpr uint32_t kColumns = D == 128 ? 512 : 256;
 
     extern __shared__ uint8_t smem_raw[];
@@ -207,137 +230,201 @@ __global__ void __launch_bounds__(kMixThreads, D == 64 ? 2 : 1) tcu_linattn_mix_
     const bool split = p.ranks > 1;
     const bool totals = split && count > 0 && part.last < part.groups;       // later blocks need what this part leaves
     const bool owns_last = job.last && (part.groups == 0 ? rank == 0 : (part.last == part.groups && count > 0));
+    const bool entered = job.init || (split && rank > 0);                    // the walk starts from a state (else from zero)
     const uint32_t before = totals ? count : 0;                              // groups of the first phase
     const uint32_t tile0 = 2 * before;                                       // tiles loaded in the first phase
     const int bz = p.offsets ? 0 : int(b);
 
-    // decays: a^m = 2^(m log2 a); -inf becomes a value whose multiples are finite, so that a^0 = 1
-    const float log2a = fmaxf(p.log_decay[h] * 1.4426950408889634f, -1e30f);
-    if (threadIdx.x <= kGroup) ctl->power[threadIdx.x] = exp2f(log2a * float(threadIdx.x));
-    if (threadIdx.x < 32) ctl->block[threadIdx.x] = job.in_scale * job.out_scale * exp2f(log2a * float(part.lead ? 31 - int(threadIdx.x) : int(threadIdx.x)));
-    if (threadIdx.x == 0) {
+    // ---- loads.  Tile n of the block: K and V of the groups of the first phase, then K, Q and V of those of the walk.
+    auto slot_of = [&](uint32_t n) { return ring_at + (n % kMixSlots) * kTile; };
+    auto load = [&](uint32_t n) {
+        const uint32_t m = n - tile0, group = n < tile0 ? n >> 1 : m / 3;
+        const uint32_t which = n < tile0 ? (n & 1 ? 2 : 1) : (m % 3 == 0 ? 1 : m % 3 == 1 ? 0 : 2);
+        const int token = int(t0 + int64_t(part.in_time(part.first + group)) * kGroup);
+        const uint32_t bar = smem_u32(&ctl->full[n % kMixSlots]);
+        mbar_expect_tx(bar, kTile);
+        for (int half = 0; half < D / 64; ++half)
+            tma_load_4d(slot_of(n) + half * kHalfBytes, &p.map[job.map[which]], half * 64, token, int(h) * job.by_head[which],
+                        bz * job.by_batch[which], bar);
+    };
+    const uint32_t phase_one = split ? tile0 : tile0 + 3 * count, tiles = tile0 + 3 * count;
+    uint32_t issued = 0;
+    if (warp == 2 * kWarps && lane == 0) {
         for (int i = 0; i < kMixSlots; ++i) {
             mbar_init(smem_u32(&ctl->full[i]), 1);
             mbar_init(smem_u32(&ctl->empty[i]), 1);
         }
         mbar_init(smem_u32(&ctl->qk_done), 1);
-        mbar_init(smem_u32(&ctl->x_ready), 128);
-        mbar_init(smem_u32(&ctl->kt_ready), 128);
-        mbar_init(smem_u32(&ctl->p_ready), 128);
+        mbar_init(smem_u32(&ctl->x_ready), kRole);
+        mbar_init(smem_u32(&ctl->kt_ready), kRole);
+        mbar_init(smem_u32(&ctl->third_ready), kRole);
+        mbar_init(smem_u32(&ctl->p_ready), kRole);
         mbar_init(smem_u32(&ctl->o_done), 1);
-        mbar_init(smem_u32(&ctl->o_free), 128);
+        mbar_init(smem_u32(&ctl->o_free), kRole);
+        mbar_init(smem_u32(&ctl->two_done), 1);
         mbar_init(smem_u32(&ctl->kv_done), 1);
-        mbar_init(smem_u32(&ctl->o_staged), 128);
+        mbar_init(smem_u32(&ctl->o_staged), kRole);
         mbar_init(smem_u32(&ctl->drained), 1);
         ctl->abort_flag = 0;
         fence_barrier_init();
+        for (; issued < kMixSlots && issued < phase_one; ++issued) load(issued);       // the ring is empty
     }
-    if (warp == 9) {
+    if (warp == 2 * kWarps + 1) {
         tmem_alloc(smem_u32(&ctl->tmem_base), kColumns);
         tmem_relinquish();
+    }
+    // decays: a^m = 2^(m log2 a); -inf becomes a value whose multiples are finite, so that a^0 = 1
+    const float log2a = fmaxf(p.log_decay[h] * 1.4426950408889634f, -1e30f);
+    if (threadIdx.x <= kGroup) ctl->power[threadIdx.x] = exp2f(log2a * float(threadIdx.x));
+    if (threadIdx.x < 32) ctl->block[threadIdx.x] = job.in_scale * job.out_scale * exp2f(log2a * float(part.lead ? 31 - int(threadIdx.x) : int(threadIdx.x)));
+    if (threadIdx.x < 32 + kGroup + 32) {
+        const int apart = int(threadIdx.x) - 31;
+        ctl->near[threadIdx.x] = apart >= 0 ? job.in_scale * job.out_scale * exp2f(log2a * float(apart)) : 0.0f;
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = ctl->tmem_base;
     const MixWaiter w{ctl, p.error, p.spin_limit};
-    auto slot_of = [&](uint32_t n) { return ring_at + (n % kMixSlots) * kTile; };
 
-    // ---- roles.  Each takes the groups [0, before) of phase one, then [0, count) of phase two; `it` counts both.
+    // ---- roles.  Each takes the groups [0, before) of the first phase, then [0, count) of the walk; `it` counts both.
     // Rows of a tile: token i of the group at i * 128 bytes, 16-byte pieces exchanged by the swizzle (piece ^ (i & 7)).
-    uint32_t issued = 0;                                           // producer: tiles loaded
-    auto produce = [&](bool want_q) {
-        const uint32_t n = want_q ? count : before;
-        for (uint32_t i = 0; i < n; ++i) {
-            const int token = int(t0 + int64_t(part.in_time(part.first + i)) * kGroup);
-            for (int a = 0; a < 3; ++a) {
-                if (a == 1 && !want_q) continue;
-                const int which = a == 0 ? 1 : a == 1 ? 0 : 2;     // K, Q, V
-                const uint32_t s = issued % kMixSlots;
-                if (issued >= kMixSlots && !w.wait(ctl->empty[s], (issued / kMixSlots - 1) & 1)) return;
-                const uint32_t bar = smem_u32(&ctl->full[s]);
-                mbar_expect_tx(bar, kTile);
-                for (int half = 0; half < D / 64; ++half)
-                    tma_load_4d(ring_at + s * kTile + half * kHalfBytes, &p.map[job.map[which]], half * 64, token, int(h) * job.by_head[which],
-                                bz * job.by_batch[which], bar);
-                ++issued;
-            }
+    auto produce = [&](uint32_t end) {
+        for (; issued < end; ++issued) {
+            if (issued >= kMixSlots && !w.wait(ctl->empty[issued % kMixSlots], (issued / kMixSlots - 1) & 1)) return;
+            load(issued);
         }
     };
     auto full = [&](uint32_t n) { return w.wait(ctl->full[n % kMixSlots], (n / kMixSlots) & 1); };
+    auto full_warp = [&](uint32_t n) { return wait_warp(w, ctl->full[n % kMixSlots], (n / kMixSlots) & 1); };
 
-    // X^T += V^T K~: lanes are columns of v, columns are rows of the state.  With D = 64 the upper 64 lanes multiply whatever
-    // lies behind the tile; nobody reads them.
-    auto issue_state = [&](uint32_t k_slot, uint32_t v_slot) {
-        const uint32_t idesc = make_idesc(H::kType, D) | kIdescAMn | kIdescBMn;
-        for (int term = 0; term < 2; ++term) {
-            const uint32_t kt = term == 0 ? k_slot : low_at;
-            for (int s = 0; s < kGroup / 16; ++s)
-                mma_issue<false>(tmem + kColX, make_smem_desc_mn(v_slot + s * 2048, kHalfBytes), make_smem_desc_mn(kt + s * 2048, kHalfBytes), idesc, 1);
+    // ---- the issuer: a whole warp walks the loop, so that descriptors stay in uniform registers; one lane issues
+    const uint32_t idesc_s = make_idesc(H::kType, kGroup), idesc_d = make_idesc(H::kType, D);
+    // X^T += V^T K~, one term of K~: lanes are columns of v, columns are rows of the state.  With D = 64 the upper 64 lanes
+    // multiply whatever lies behind the tile; nobody reads them.
+    auto issue_state = [&](uint32_t kt, uint32_t v_slot, bool onto) {
+        const uint64_t va = make_smem_desc_mn(v_slot, kHalfBytes), kb = make_smem_desc_mn(kt, kHalfBytes);
+#pragma unroll
+        for (int s = 0; s < kGroup / 16; ++s)
+            mma_issue<false>(tmem + kColX, va + s * (2048 >> 4), kb + s * (2048 >> 4), idesc_d | kIdescAMn | kIdescBMn, onto || s > 0);
+    };
+    // the state's products of group `it`, in two steps; false when a wait was given up
+    auto state_two = [&](uint32_t it, uint32_t k_slot, uint32_t v_slot, bool wanted, bool onto) {
+        if (!wait_warp(w, ctl->kt_ready, it & 1)) return false;
+        tc_fence_after();
+        if (elect_one()) {
+            if (wanted) {
+                issue_state(k_slot, v_slot, onto);
+                issue_state(low_at, v_slot, true);
+            }
+            if (kThird) mma_commit(smem_u32(&ctl->two_done));
+        }
+        __syncwarp();
+        return true;
+    };
+    auto state_rest = [&](uint32_t it, uint32_t nk, uint32_t nv, bool wanted) {
+        if (kThird && wanted) {
+            if (!wait_warp(w, ctl->third_ready, it & 1)) return false;
+            tc_fence_after();
+        }
+        if (elect_one()) {
+            if (kThird && wanted) issue_state(low_at, slot_of(nv), true);
+            mma_commit(smem_u32(&ctl->kv_done));
+            mma_commit(smem_u32(&ctl->empty[nk % kMixSlots]));
+            mma_commit(smem_u32(&ctl->empty[nv % kMixSlots]));
+        }
+        __syncwarp();
+        return true;
+    };
+    auto multiply_totals = [&]() {
+        for (uint32_t i = 0; i < before; ++i) {
+            const uint32_t nk = 2 * i, nv = nk + 1;
+            if (!full_warp(nk) || !full_warp(nv) || !wait_warp(w, ctl->x_ready, i & 1)) return;
+            if (!state_two(i, slot_of(nk), slot_of(nv), true, i > 0) || !state_rest(i, nk, nv, true)) return;
         }
     };
-    auto multiply = [&](bool outputs) {
-        const uint32_t n = outputs ? count : before;
-        for (uint32_t i = 0; i < n; ++i) {
-            const uint32_t it = outputs ? before + i : i;
-            const bool want_state = !outputs || i + 1 < n || owns_last;
-            if (outputs) {
-                const uint32_t nk = tile0 + 3 * i, nq = nk + 1, nv = nk + 2;
-                const uint32_t k = slot_of(nk), q = slot_of(nq), v = slot_of(nv);
-                if (!full(nk) || !full(nq)) return;
-                // the last group's P has been multiplied (D = 64: and its O, which lies in S, has been read)
-                if (i > 0 && !w.wait(D == 64 ? ctl->o_free : ctl->o_done, (i - 1) & 1)) return;
-                tc_fence_after();
-                for (int half = 0; half < D / 64; ++half)
-                    for (int s = 0; s < 4; ++s)
-                        mma_issue<false>(tmem + kColS, make_smem_desc(q + half * kHalfBytes + s * 32), make_smem_desc(k + half * kHalfBytes + s * 32),
-                                         make_idesc(H::kType, kGroup), half + s > 0);
+    auto multiply = [&]() {
+        auto scores = [&](uint32_t i) {
+            const uint32_t nk = tile0 + 3 * i, nq = nk + 1;
+            if (!full_warp(nk) || !full_warp(nq)) return false;
+            // the last group's P has been multiplied (D = 64: and its O, which lies in S, has been read)
+            if (i > 0 && !wait_warp(w, D == 64 ? ctl->o_free : ctl->o_done, (i - 1) & 1)) return false;
+            tc_fence_after();
+            if (elect_one()) {
+                const uint64_t qa = make_smem_desc(slot_of(nq)), kb = make_smem_desc(slot_of(nk));
+#pragma unroll
+                for (int s = 0; s < D / 16; ++s)
+                    mma_issue<false>(tmem + kColS, qa + (s / 4) * (kHalfBytes >> 4) + (s % 4) * 2, kb + (s / 4) * (kHalfBytes >> 4) + (s % 4) * 2, idesc_s, s > 0);
                 mma_commit(smem_u32(&ctl->qk_done));
-                if (!w.wait(ctl->x_ready, it & 1)) return;
-                if (D == 128 && i > 0 && !w.wait(ctl->o_free, (i - 1) & 1)) return;
-                tc_fence_after();
-                for (int half = 0; half < D / 64; ++half)
-                    for (int s = 0; s < 4; ++s)
-                        mma_issue<false>(tmem + kColE, make_smem_desc(q + half * kHalfBytes + s * 32), make_smem_desc(x_at + half * kXHalf + s * 32),
-                                         make_idesc(H::kType, D), half + s > 0);
-                if (part.tokens_of(part.first + i) < kGroup && !w.wait(ctl->kt_ready, it & 1)) return;
-                if (!full(nv) || !w.wait(ctl->p_ready, i & 1)) return;
-                tc_fence_after();
-                for (int s = 0; s < kGroup / 16; ++s)
-                    mma_issue_ta(tmem + kColO, tmem + kColS + s * 8, make_smem_desc_mn(v + s * 2048, kHalfBytes), make_idesc(H::kType, D) | kIdescBMn, s > 0);
-                mma_commit(smem_u32(&ctl->o_done));
-                if (!w.wait(ctl->kt_ready, it & 1)) return;
-                tc_fence_after();
-                if (want_state) issue_state(k, v);
-                mma_commit(smem_u32(&ctl->kv_done));
-                mma_commit(smem_u32(&ctl->empty[nk % kMixSlots]));
-                mma_commit(smem_u32(&ctl->empty[nv % kMixSlots]));
-            } else {
-                const uint32_t nk = 2 * i, nv = nk + 1;
-                if (!full(nk) || !full(nv) || !w.wait(ctl->x_ready, it & 1) || !w.wait(ctl->kt_ready, it & 1)) return;
-                tc_fence_after();
-                issue_state(slot_of(nk), slot_of(nv));
-                mma_commit(smem_u32(&ctl->kv_done));
-                mma_commit(smem_u32(&ctl->empty[nk % kMixSlots]));
-                mma_commit(smem_u32(&ctl->empty[nv % kMixSlots]));
             }
+            __syncwarp();
+            return true;
+        };
+        if (count > 0 && !scores(0)) return;
+        for (uint32_t i = 0; i < count; ++i) {
+            const uint32_t it = before + i;
+            const uint32_t nk = tile0 + 3 * i, nq = nk + 1, nv = nk + 2;
+            const bool fresh = i == 0 && !entered, wanted = i + 1 < count || owns_last;
+            if (!wait_warp(w, ctl->x_ready, it & 1)) return;
+            if (i > 0 && !wait_warp(w, ctl->o_free, (i - 1) & 1)) return;
+            tc_fence_after();
+            if (!fresh && elect_one()) {
+                const uint64_t qa = make_smem_desc(slot_of(nq)), xb = make_smem_desc(x_at);
+#pragma unroll
+                for (int s = 0; s < D / 16; ++s)
+                    mma_issue<false>(tmem + kColE, qa + (s / 4) * (kHalfBytes >> 4) + (s % 4) * 2, xb + (s / 4) * (kXHalf >> 4) + (s % 4) * 2, idesc_d, s > 0);
+            }
+            __syncwarp();
+            if (part.tokens_of(part.first + i) < kGroup && !wait_warp(w, ctl->kt_ready, it & 1)) return;
+            if (!full_warp(nv) || !wait_warp(w, ctl->p_ready, i & 1)) return;
+            tc_fence_after();
+            if (elect_one()) {
+                const uint64_t vb = make_smem_desc_mn(slot_of(nv), kHalfBytes);
+#pragma unroll
+                for (int s = 0; s < kGroup / 16; ++s)
+                    mma_issue_ta(tmem + kColO, tmem + kColS + (s / 4) * kColP1 + (s % 4) * 8, vb + s * (2048 >> 4), idesc_d | kIdescBMn, s > 0);
+                mma_commit(smem_u32(&ctl->o_done));
+            }
+            __syncwarp();
+            // the next scores go before the last term of the state, while the state warps write it; with D = 64 they would
+            // have to wait for the outputs to be read, and the other block of the SM fills the gap
+            if (!state_two(it, slot_of(nk), slot_of(nv), wanted, !fresh)) return;
+            if (D == 128 && i + 1 < count && !scores(i + 1)) return;
+            if (!state_rest(it, nk, nv, wanted)) return;
+            if (D == 64 && i + 1 < count && !scores(i + 1)) return;
         }
     };
 
     const uint32_t lanes = tmem + (uint32_t(warp & 3) << 21);       // this warp's 32 lanes (bits 16 and up)
     const int row = (warp & 3) * 32 + lane;                         // token of the group, or column of v
+    const int part64 = (warp % kWarps) / 4 * 64;                    // this thread's 64 columns of a row (features, or rows of the state)
     const bool holds_x = (warp & 3) * 32 < D;                       // whole warps: X has D lanes
+    const uint32_t swizzled = uint32_t(row * 128), sw = uint32_t(row & 7);
 
-    // state warps: X <- values, from tensor memory or into it
+    // state warps: X <- values
     auto fill_x = [&](auto value) {
         if (holds_x) {
-            for (int c = 0; c < D; c += 32) {
+#pragma unroll 1
+            for (int c = 0; c < 64; c += 32) {
                 uint32_t v[32];
 #pragma unroll
-                for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(value(c + j));
-                tmem_st32(lanes + kColX + c, v);
+                for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(value(part64 + c + j));
+                tmem_st32(lanes + kColX + part64 + c, v);
             }
             tmem_st_wait();
+        }
+    };
+    // state warps: use(column, X) for this thread's values
+    auto read_x = [&](auto use) {
+        if (holds_x) {
+#pragma unroll 1
+            for (int c = 0; c < 64; c += 32) {
+                uint32_t v[32];
+                tmem_ld32(lanes + kColX + part64 + c, v);
+                tmem_ld_wait();
+#pragma unroll
+                for (int j = 0; j < 32; ++j) use(part64 + c + j, __uint_as_float(v[j]));
+            }
         }
     };
     // float16 only: powers of two that keep the operands inside the type.  X is held as 2^held X, so that the decayed keys of the
@@ -345,24 +432,12 @@ __global__ void __launch_bounds__(kMixThreads, D == 64 ? 2 : 1) tcu_linattn_mix_
     int held = 0;
     auto pow2 = [](int n) { return __uint_as_float(uint32_t(min(max(n, -126), 127) + 127) << 23); };
     auto exponent = [](float x) { return int((__float_as_uint(x) >> 23) & 0xFF) - 127; };
-    auto biggest_x = [&]() {
-        float big = 0.0f;
-        if (holds_x) {
-            for (int c = 0; c < D; c += 32) {
-                uint32_t v[32];
-                tmem_ld32(lanes + kColX + c, v);
-                tmem_ld_wait();
-#pragma unroll
-                for (int j = 0; j < 32; ++j) big = fmaxf(big, fabsf(__uint_as_float(v[j])));
-            }
-        }
-        return big;
-    };
     auto biggest_k = [&](uint32_t k_slot) {
         float big = 0.0f;
-        for (int c = 0; c < D / 8; ++c) {
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
             uint32_t k4[4];
-            ld_shared_v4(k_slot + (c >> 3) * kHalfBytes + row * 128 + (((c & 7) ^ (row & 7)) << 4), k4[0], k4[1], k4[2], k4[3]);
+            ld_shared_v4(k_slot + (part64 / 64) * kHalfBytes + swizzled + ((c ^ sw) << 4), k4[0], k4[1], k4[2], k4[3]);
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const float2 x = H::unpack(k4[e]);
@@ -374,24 +449,32 @@ __global__ void __launch_bounds__(kMixThreads, D == 64 ? 2 : 1) tcu_linattn_mix_
     // X rounded into the operand of E, times `shrink`, and X times `keep` left in tensor memory
     auto step_x = [&](float shrink, float keep, bool operand) {
         if (holds_x) {
-            for (int c = 0; c < D; c += 32) {
+                const float2 keep2 = make_float2(keep, keep), shrink2 = make_float2(shrink, shrink);
+#pragma unroll 1
+            for (int c = 0; c < 64; c += 32) {
                 uint32_t v[32];
-                tmem_ld32(lanes + kColX + c, v);
+                tmem_ld32(lanes + kColX + part64 + c, v);
                 tmem_ld_wait();
                 if (operand) {
 #pragma unroll
                     for (int j = 0; j < 32; j += 8) {
                         uint32_t w4[4];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            w4[e] = H::pack(__uint_as_float(v[j + 2 * e]) * (kIsHalf ? shrink : 1.0f), __uint_as_float(v[j + 2 * e + 1]) * (kIsHalf ? shrink : 1.0f));
-                        const int piece = ((c + j) & 63) >> 3;
-                        st_shared_v4(x_at + ((c + j) >> 6) * kXHalf + row * 128 + ((piece ^ (row & 7)) << 4), w4[0], w4[1], w4[2], w4[3]);
+                        for (int e = 0; e < 4; ++e) {
+                            float2 x = make_float2(__uint_as_float(v[j + 2 * e]), __uint_as_float(v[j + 2 * e + 1]));
+                            if (kIsHalf) x = mul2(x, shrink2);
+                            w4[e] = H::pack(x.x, x.y);
+                        }
+                        st_shared_v4(x_at + (part64 / 64) * kXHalf + swizzled + ((((c + j) >> 3) ^ sw) << 4), w4[0], w4[1], w4[2], w4[3]);
                     }
                 }
 #pragma unroll
-                for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * keep);
-                tmem_st32(lanes + kColX + c, v);
+                for (int j = 0; j < 32; j += 2) {
+                    const float2 x = mul2(make_float2(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), keep2);
+                    v[j] = __float_as_uint(x.x);
+                    v[j + 1] = __float_as_uint(x.y);
+                }
+                tmem_st32(lanes + kColX + part64 + c, v);
             }
             tmem_st_wait();
         }
@@ -399,31 +482,51 @@ __global__ void __launch_bounds__(kMixThreads, D == 64 ? 2 : 1) tcu_linattn_mix_
         tc_fence_before();
         mbar_arrive(smem_u32(&ctl->x_ready));
     };
-    auto step_k = [&](int tokens, uint32_t k_slot, uint32_t v_slot, bool wanted) {
+    // K~ in two terms, in the place of K and in the buffer of the low terms; with three, the last one in turn takes the place
+    // of the second when that has been multiplied
+    auto step_k = [&](uint32_t it, int tokens, uint32_t k_slot, uint32_t v_slot, bool wanted) {
+        uint32_t rest[kThird ? 32 : 1];
         if (wanted) {
             // walking order: token `row` of the group is j = row forward, tokens - 1 - row backward; a^(tokens - j - lead)
             const float f = row < tokens ? job.in_scale * ctl->power[part.lead ? tokens - 1 - row : row + 1] * (kIsHalf ? pow2(held) : 1.0f) : 0.0f;
-            for (int c = 0; c < D / 8; ++c) {
-                const uint32_t at = (c >> 3) * kHalfBytes + row * 128 + (((c & 7) ^ (row & 7)) << 4);
+            const float2 f2 = make_float2(f, f), minus = make_float2(-1.0f, -1.0f);
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
+                const uint32_t at = (part64 / 64) * kHalfBytes + swizzled + ((c ^ sw) << 4);
                 uint32_t k4[4], hi[4], lo[4];
                 ld_shared_v4(k_slot + at, k4[0], k4[1], k4[2], k4[3]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    float2 x = H::unpack(k4[e]);
-                    x.x = row < tokens ? x.x * f : 0.0f;
-                    x.y = row < tokens ? x.y * f : 0.0f;
+                    if (row >= tokens) k4[e] = 0;
+                    const float2 x = mul2(H::unpack(k4[e]), f2);
                     hi[e] = H::pack(x.x, x.y);
-                    const float2 y = H::unpack(hi[e]);
-                    lo[e] = H::pack(x.x - y.x, x.y - y.y);
+                    const float2 y = fma2(H::unpack(hi[e]), minus, x);
+                    lo[e] = H::pack(y.x, y.y);
+                    if (kThird) {
+                        const float2 z = fma2(H::unpack(lo[e]), minus, y);
+                        rest[kThird ? 4 * c + e : 0] = H::pack(z.x, z.y);
+                    }
                 }
                 st_shared_v4(k_slot + at, hi[0], hi[1], hi[2], hi[3]);
                 st_shared_v4(low_at + at, lo[0], lo[1], lo[2], lo[3]);
             }
         }
-        if (row >= tokens)             // what follows the sequence may hold anything: zero times it has to be zero
-            for (int c = 0; c < D / 8; ++c) st_shared_v4(v_slot + (c >> 3) * kHalfBytes + row * 128 + ((c & 7) << 4), 0, 0, 0, 0);
+        if (row >= tokens) {           // what follows the sequence may hold anything: zero times it has to be zero
+#pragma unroll
+            for (int c = 0; c < 8; ++c) st_shared_v4(v_slot + (part64 / 64) * kHalfBytes + swizzled + (c << 4), 0, 0, 0, 0);
+        }
         fence_proxy_async_smem();
         mbar_arrive(smem_u32(&ctl->kt_ready));
+        if (kThird && wanted) {
+            if (!wait_warp(w, ctl->two_done, it & 1)) return false;
+#pragma unroll
+            for (int c = 0; c < 8; ++c)
+                st_shared_v4(low_at + (part64 / 64) * kHalfBytes + swizzled + ((c ^ sw) << 4), rest[kThird ? 4 * c : 0], rest[kThird ? 4 * c + 1 : 0],
+                             rest[kThird ? 4 * c + 2 : 0], rest[kThird ? 4 * c + 3 : 0]);
+            fence_proxy_async_smem();
+            mbar_arrive(smem_u32(&ctl->third_ready));
+        }
+        return true;
     };
     auto carry = [&](bool outputs) {
         const uint32_t n = outputs ? count : before;
@@ -432,6 +535,7 @@ __global__ void __launch_bounds__(kMixThreads, D == 64 ? 2 : 1) tcu_linattn_mix_
             const uint32_t it = outputs ? before + i : i;
             const uint32_t nk = outputs ? tile0 + 3 * i : 2 * i, nv = outputs ? nk + 2 : nk + 1;
             const int tokens = part.tokens_of(part.first + i);
+            const bool fresh = i == 0 && !(outputs && entered);            // X is zero: the first product does not add to it
             float big_k = 0.0f, shrink = 1.0f, keep = ctl->power[tokens];
             if (kIsHalf) {
                 ok = ok && __all_sync(0xffffffffu, full(nk));
@@ -443,52 +547,54 @@ __global__ void __launch_bounds__(kMixThreads, D == 64 ? 2 : 1) tcu_linattn_mix_
                 tc_fence_after();
             }
             if (kIsHalf) {
-                float big_x = ok ? biggest_x() : 0.0f;
+                float big_x = 0.0f;
+                if (ok && !fresh) read_x([&](int, float x) { big_x = fmaxf(big_x, fabsf(x)); });
 #pragma unroll
                 for (int o = 16; o > 0; o >>= 1) {
                     big_k = fmaxf(big_k, __shfl_xor_sync(0xffffffffu, big_k, o));
                     big_x = fmaxf(big_x, __shfl_xor_sync(0xffffffffu, big_x, o));
                 }
                 if (lane == 0) {
-                    ctl->biggest[i & 1][warp & 3] = big_k;
-                    ctl->biggest[i & 1][4 + (warp & 3)] = big_x;
+                    ctl->biggest[i & 1][warp % kWarps] = big_k;
+                    ctl->biggest[i & 1][kWarps + warp % kWarps] = big_x;
                 }
-                ok = !named_barrier_or(1, 128, !ok);              // the four warps meet here, so they give up together
+                ok = !named_barrier_or(1, kRole, !ok);              // the warps of the role meet here, so they give up together
                 if (ok) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
+                    for (int j = 0; j < kWarps; ++j) {
                         big_k = fmaxf(big_k, ctl->biggest[i & 1][j]);
-                        big_x = fmaxf(big_x, ctl->biggest[i & 1][4 + j]);
+                        big_x = fmaxf(big_x, ctl->biggest[i & 1][kWarps + j]);
                     }
                     const int ex = min(max(exponent(big_x), -60), 127);
                     shrink = pow2(14 - ex);
-                    if (threadIdx.x == 128) ctl->unscale[i & 1] = pow2(ex - 14 - held);
+                    if (threadIdx.x == kRole) ctl->unscale[i & 1] = pow2(ex - 14 - held);
                     // the powers of a in K~ go from a^(1 - lead) to a^(tokens - lead)
-                    const float most = fmaxf(ctl->power[1 - job.lead], ctl->power[tokens - int(job.lead)]);
-                    const int now = min(max(14 - exponent(big_k * fabsf(job.in_scale) * most), -30), 100);
+                    const float top = fmaxf(ctl->power[1 - job.lead], ctl->power[tokens - int(job.lead)]);
+                    const int now = min(max(14 - exponent(big_k * fabsf(job.in_scale) * top), -30), 100);
                     keep *= pow2(now - held);
                     held = now;
                 }
             }
             if (!ok) break;
-            step_x(shrink, keep, outputs);
+            if (fresh) mbar_arrive(smem_u32(&ctl->x_ready));
+            else step_x(shrink, keep, outputs);
             ok = __all_sync(0xffffffffu, full(nk) && (tokens == kGroup || full(nv)));
             ok = ok && (!outputs || wait_warp(w, ctl->qk_done, i & 1));
-            if (ok) step_k(tokens, slot_of(nk), slot_of(nv), !outputs || i + 1 < n || owns_last);
+            if (ok) ok = step_k(it, tokens, slot_of(nk), slot_of(nv), !outputs || i + 1 < n || owns_last);
         }
         return ok;
     };
 
     // token warps
     auto attend = [&]() {
+        const int row0 = (warp & 3) * 32;
         for (uint32_t i = 0; i < count; ++i) {
             const int tokens = part.tokens_of(part.first + i);
             if (!wait_warp(w, ctl->qk_done, i & 1)) return;
             tc_fence_after();
-            const int row0 = (warp & 3) * 32;
+            // scores of 32 tokens at a time: all of them count, none, or (around the diagonal and the end) some
 #pragma unroll 1
-            for (int c = 0; c < kGroup; c += 32) {
-                // scores of tokens c ... c + 31: all of them count, none, or (around the diagonal and the end) some
+            for (int c = part64; c < (D == 128 ? part64 + 64 : kGroup); c += 32) {
                 const bool all = part.lead ? c + 31 <= row0 : c >= row0 + 31 && c + 31 < tokens;
                 const bool none = part.lead ? c > row0 + 31 : c + 31 < row0 || c >= tokens;
                 uint32_t out[16];
@@ -501,22 +607,32 @@ __global__ void __launch_bounds__(kMixThreads, D == 64 ? 2 : 1) tcu_linattn_mix_
                     tmem_ld_wait();
                     if (all) {
                         const float f = ctl->power[part.lead ? row - c - 31 : c - row];
+                        const float2 f2 = make_float2(f, f);
 #pragma unroll
-                        for (int j = 0; j < 16; ++j)
-                            out[j] = H::pack(__uint_as_float(v[2 * j]) * (f * ctl->block[2 * j]), __uint_as_float(v[2 * j + 1]) * (f * ctl->block[2 * j + 1]));
+                        for (int j = 0; j < 8; ++j) {
+                            const float4 t = reinterpret_cast<const float4 *>(ctl->block)[j];
+                            const float2 x = mul2(make_float2(__uint_as_float(v[4 * j]), __uint_as_float(v[4 * j + 1])), mul2(f2, make_float2(t.x, t.y)));
+                            const float2 y = mul2(make_float2(__uint_as_float(v[4 * j + 2]), __uint_as_float(v[4 * j + 3])), mul2(f2, make_float2(t.z, t.w)));
+                            out[2 * j] = H::pack(x.x, x.y);
+                            out[2 * j + 1] = H::pack(y.x, y.y);
+                        }
                     } else {
-                        const float f = job.in_scale * job.out_scale;
+                        // (what does not count may not be finite: it is left out, not multiplied by zero)
+                        const int apart = part.lead ? row - c : c - row;
+                        const float *factor = ctl->near + 31 + apart;
+                        if (part.lead) {
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) {
-                            const int apart = part.lead ? row - (c + j) : c + j - row;
-                            const bool counts = apart >= 0 && (part.lead || c + j < tokens);
-                            v[j] = counts ? __float_as_uint(__uint_as_float(v[j]) * (f * ctl->power[apart])) : 0u;
+                            for (int j = 0; j < 32; ++j) v[j] = apart >= j ? __float_as_uint(__uint_as_float(v[j]) * factor[-j]) : 0u;
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < 32; ++j)
+                                v[j] = apart + j >= 0 && c + j < tokens ? __float_as_uint(__uint_as_float(v[j]) * factor[j]) : 0u;
                         }
 #pragma unroll
                         for (int j = 0; j < 16; ++j) out[j] = H::pack(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1]));
                     }
                 }
-                tmem_st16(lanes + kColS + c / 2, out);         // never over scores still to be read
+                tmem_st16(lanes + kColS + (c / 64) * kColP1 + (c % 64) / 2, out);         // never over scores still to be read
             }
             tmem_st_wait();
             tc_fence_before();
@@ -524,36 +640,46 @@ __global__ void __launch_bounds__(kMixThreads, D == 64 ? 2 : 1) tcu_linattn_mix_
 
             if (!wait_warp(w, ctl->o_done, i & 1) || !wait_warp(w, ctl->x_ready, (before + i) & 1)) return;
             tc_fence_after();
-            const uint32_t slot = slot_of(tile0 + 3 * i + 1);
+            const bool fresh = i == 0 && !entered;                 // no state: E was not formed
+            const uint32_t slot = slot_of(tile0 + 3 * i + 1) + (part64 / 64) * kHalfBytes;
             const int order = part.lead ? row : tokens - 1 - row;
             float e = order >= 0 ? job.out_scale * ctl->power[order + int(job.lead)] : 0.0f;
             if (kIsHalf) e *= ctl->unscale[i & 1];
+            const float2 e2 = make_float2(e, e);
             const int64_t token = t0 + int64_t(part.in_time(part.first + i)) * kGroup + row;
             T *to = reinterpret_cast<T *>(job.o) + bz * job.o_batch + token * job.o_token + int64_t(h) * job.o_head;
 #pragma unroll 1
-            for (int c = 0; c < D; c += 32) {
+            for (int c = 0; c < 64; c += 32) {
                 uint32_t vo[32], ve[32];
-                tmem_ld32(lanes + kColO + c, vo);
-                tmem_ld32(lanes + kColE + c, ve);
+                tmem_ld32(lanes + kColO + part64 + c, vo);
+                if (!fresh) tmem_ld32(lanes + kColE + part64 + c, ve);
                 tmem_ld_wait();
+                if (!fresh) {
 #pragma unroll
-                for (int j = 0; j < 32; j += 8) {
-                    uint32_t w4[4];
+                    for (int j = 0; j < 32; j += 2) {
+                        const float2 x = fma2(e2, make_float2(__uint_as_float(ve[j]), __uint_as_float(ve[j + 1])), make_float2(__uint_as_float(vo[j]), __uint_as_float(vo[j + 1])));
+                        vo[j] = __float_as_uint(x.x);
+                        vo[j + 1] = __float_as_uint(x.y);
+                    }
+                }
+                uint32_t out[16];
 #pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        w4[k] = H::pack(fmaf(e, __uint_as_float(ve[j + 2 * k]), __uint_as_float(vo[j + 2 * k])),
-                                        fmaf(e, __uint_as_float(ve[j + 2 * k + 1]), __uint_as_float(vo[j + 2 * k + 1])));
-                    if (tokens == kGroup) {
-                        const int piece = ((c + j) & 63) >> 3;
-                        st_shared_v4(slot + ((c + j) >> 6) * kHalfBytes + row * 128 + ((piece ^ (row & 7)) << 4), w4[0], w4[1], w4[2], w4[3]);
-                    } else if (row < tokens) {
-                        if (uint32_t(c + j + 8) <= job.dv) {
-                            st_global_v4(to + c + j, w4[0], w4[1], w4[2], w4[3]);
+                for (int j = 0; j < 16; ++j) out[j] = H::pack(__uint_as_float(vo[2 * j]), __uint_as_float(vo[2 * j + 1]));
+                if (tokens == kGroup) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        st_shared_v4(slot + swizzled + (((c / 8 + j) ^ sw) << 4), out[4 * j], out[4 * j + 1], out[4 * j + 2], out[4 * j + 3]);
+                } else if (row < tokens) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int col = part64 + c + 8 * j;
+                        if (uint32_t(col + 8) <= job.dv) {
+                            st_global_v4(to + col, out[4 * j], out[4 * j + 1], out[4 * j + 2], out[4 * j + 3]);
                         } else {
-                            const T *x = reinterpret_cast<const T *>(w4);
+                            const T *x = reinterpret_cast<const T *>(out + 4 * j);
 #pragma unroll
                             for (int k = 0; k < 8; ++k)
-                                if (uint32_t(c + j + k) < job.dv) to[c + j + k] = x[k];
+                                if (uint32_t(col + k) < job.dv) to[col + k] = x[k];
                         }
                     }
                 }
@@ -584,25 +710,16 @@ __global__ void __launch_bounds__(kMixThreads, D == 64 ? 2 : 1) tcu_linattn_mix_
         if (!job.init || uint32_t(c) >= job.dk || uint32_t(row) >= job.dv) return 0.0f;
         return job.init[uint64_t(unit) * job.dk * job.dv + uint64_t(c) * job.init_k + uint64_t(row) * job.init_v];
     };
+    const bool token_role = warp < kWarps, state_role = warp >= kWarps && warp < 2 * kWarps;
 
-    // ---- phase one of a split walk: what this part leaves from a state of zero, and the states that enter the parts
+    // ---- the first phase of a split walk: what this part leaves from a state of zero, and the states that enter the parts
     if (split) {
-        if (warp == 8 && lane == 0) produce(false);
-        if (warp == 9 && lane == 0) multiply(false);
-        if (warp >= 4 && warp < 8 && totals) {
-            fill_x([](int) { return 0.0f; });
+        if (warp == 2 * kWarps && lane == 0) produce(tile0);
+        if (warp == 2 * kWarps + 1) multiply_totals();
+        if (state_role && totals) {
             if (carry(false) && wait_warp(w, ctl->kv_done, (before - 1) & 1)) {
                 tc_fence_after();
-                if (holds_x) {
-                    for (int c = 0; c < D; c += 32) {
-                        uint32_t v[32];
-                        tmem_ld32(lanes + kColX + c, v);
-                        tmem_ld_wait();
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) exchange[(c + j) * D + row] = __uint_as_float(v[j]) * (kIsHalf ? pow2(-held) : 1.0f);
-
-                    }
-                }
+                read_x([&](int c, float x) { exchange[c * D + row] = x * (kIsHalf ? pow2(-held) : 1.0f); });
             }
         }
         held = 0;
@@ -629,22 +746,33 @@ __global__ void __launch_bounds__(kMixThreads, D == 64 ? 2 : 1) tcu_linattn_mix_
             }
         }
         cluster_sync_all();
-        if (warp >= 4 && warp < 8) {
-            if (count > 0) fill_x([&](int c) { return exchange[c * D + row]; });
-            else fill_x(init_at);
+        if (state_role) {
+            if (count > 0 && entered) fill_x([&](int c) { return exchange[c * D + row]; });
+            else if (count == 0 && owns_last) fill_x(init_at);
         }
         fence_proxy_async_smem();                       // the next writes to the exchange buffer are TMA loads
         tc_fence_before();
         __syncthreads();
         tc_fence_after();
-    } else if (warp >= 4 && warp < 8) {
+    } else if (state_role && (entered || count == 0)) {
         fill_x(init_at);
     }
 
     // ---- the walk
-    if (warp == 8) {
+    if (token_role) {
+        attend();
+    } else if (state_role) {
+        const bool ok = carry(true);
+        if (owns_last && (count == 0 || (ok && wait_warp(w, ctl->kv_done, (before + count - 1) & 1)))) {
+            tc_fence_after();
+            float *to = job.last + uint64_t(unit) * job.dk * job.dv + row;
+            read_x([&](int c, float x) {
+                if (uint32_t(c) < job.dk && uint32_t(row) < job.dv) to[uint64_t(c) * job.dv] = x * (kIsHalf ? pow2(-held) : 1.0f);
+            });
+        }
+    } else if (warp == 2 * kWarps) {
         if (lane == 0) {
-            produce(true);
+            produce(tiles);
             if (ctl->abort_flag)                        // copies in flight must land before the block may exit
                 for (uint32_t n = issued > kMixSlots ? issued - kMixSlots : 0; n < issued; ++n) {
                     const uint32_t bar = smem_u32(&ctl->full[n % kMixSlots]);
@@ -652,41 +780,21 @@ __global__ void __launch_bounds__(kMixThreads, D == 64 ? 2 : 1) tcu_linattn_mix_
                     while (!mbar_try_wait(bar, (n / kMixSlots) & 1) && clock64() - since < p.spin_limit) {}
                 }
         }
-    } else if (warp == 9) {
-        if (lane == 0) {
-            multiply(true);
-            if (ctl->abort_flag) {                      // so must products: tensor memory is freed below
-                mma_commit(smem_u32(&ctl->drained));
-                const long long since = clock64();
-                while (!mbar_try_wait(smem_u32(&ctl->drained), 0) && clock64() - since < p.spin_limit) {}
-            }
+    } else if (warp == 2 * kWarps + 1) {
+        multiply();
+        if (ctl->abort_flag && elect_one()) {           // so must products: tensor memory is freed below
+            mma_commit(smem_u32(&ctl->drained));
+            const long long since = clock64();
+            while (!mbar_try_wait(smem_u32(&ctl->drained), 0) && clock64() - since < p.spin_limit) {}
         }
-    } else if (warp == 10) {
-        if (lane == 0) store();
-    } else if (warp >= 4) {
-        const bool ok = carry(true);
-        if (owns_last && (count == 0 || (ok && wait_warp(w, ctl->kv_done, (before + count - 1) & 1)))) {
-            tc_fence_after();
-            if (holds_x) {
-                for (int c = 0; c < D; c += 32) {
-                    uint32_t v[32];
-                    tmem_ld32(lanes + kColX + c, v);
-                    tmem_ld_wait();
-                    float *to = job.last + uint64_t(unit) * job.dk * job.dv + row;
-#pragma unroll
-                    for (int j = 0; j < 32; ++j)
-                        if (uint32_t(c + j) < job.dk && uint32_t(row) < job.dv) to[uint64_t(c + j) * job.dv] = __uint_as_float(v[j]) * (kIsHalf ? pow2(-held) : 1.0f);
-                }
-            }
-        }
-    } else {
-        attend();
+    } else if (lane == 0) {
+        store();
     }
     __syncwarp();
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (warp == 9) tmem_dealloc(tmem, kColumns);
+    if (warp == 2 * kWarps + 1) tmem_dealloc(tmem, kColumns);
 }
 
 // ---- single tokens ---------------------------------------------------------------------------------------------------

@@ -130,7 +130,7 @@ tcu_status_t launch_mix(const MixParams &p, cudaStream_t stream) {
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(p.batch * p.heads * p.jobs * p.ranks);
-    cfg.blockDim = dim3(kMixThreads);
+    cfg.blockDim = dim3(kMixThreads<D>);
     cfg.dynamicSmemBytes = kMixSmemBytes<D>;
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
