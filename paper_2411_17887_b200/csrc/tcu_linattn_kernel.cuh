@@ -19,16 +19,23 @@
 //     E = Q X  (X rounded to the 16-bit type),  X^T += V^T K~  with K~ = decayed keys in two 16-bit terms.
 //
 // A block (one job, sequence, head and - in a cluster - part of the walk) runs the groups one after another.  Roles:
-//     tokens    (8 warps, 4 when dk, dv <= 64) thread = token: scores -> P, then O + decayed E -> the slot that held Q
-//     state     (as many) thread = column of v: X out of tensor memory, rounded into the operand of E, multiplied by a^L and put
-//               back; thread = token: K -> K~
-//     producer  TMA: K, Q, V of each group into a ring of five tiles
-//     issuer    tcgen05.mma
-//     store     TMA: the outputs
+//     tokens    8 warps, thread = half a token: O + decayed E -> global memory, then the next scores -> P
+//     keys      8 warps, thread = half a token: K -> the terms of K~, the first in the place of K
+//     state     4 warps, thread = column of v: X out of tensor memory, rounded into the operand of E, times a^L and put back
+//     producer  TMA: K, Q, V of each group into a ring of tiles
+//     issuers   tcgen05.mma: one warp for scores and O, one for E and the state
+// What bounds it is not the tensor core (2560 of its cycles a group with D = 128) but the chain from group to group,
+//     X rescaled (and, meanwhile, K~ made) -> E and the products of X (512 cycles each, and 450 until they are known to be done),
+// and the elementwise work, 16 lanes a cycle and scheduler for conversions, permutations and packed arithmetic alike.  Hence the
+// roles, two issuers that do not wait for one another's turn, and as few instructions an element as possible.
+//
 // Rounded to 16 bits are only operands of a product: P, and X as operand of E (the state itself stays in 32 bits in tensor
-// memory).  K~ enters the state in two terms in float16, 22 bits of mantissa, and in three in bfloat16, 24 bits (two, 16
-// bits, left states 2e-6 to 5e-6 off where 32-bit sums are 2e-7 off).  In float16 X and K~ are brought to the type's range by powers of two found for every group, because a state without decay
-// outgrows the type and the low terms of small keys fall below it.
+// memory).  K~ enters the state in two terms: 22 bits of mantissa in float16, 16 in bfloat16.  There a third term follows
+// (24 bits, all that 32-bit arithmetic gives) in the groups that the decay until the end of the walk leaves above 2^-6, because
+// the last state is a result in 32 bits of its own; with two terms throughout it was 2e-6 to 5e-6 off, where 32-bit sums are
+// 2e-7 off.  (The rule goes by the decay alone: outputs do not depend on whether the state is asked for.)  In float16 X and K~
+// are brought to the type's range by powers of two found for every group, because a state without decay outgrows the type
+// and the low terms of small keys fall below it.
 //
 // When there are fewer (job, sequence, head) than SMs, the walk is split over the blocks of a cluster: each block first
 // forms the state that its part leaves from zero (K and V only), the blocks exchange them through distributed shared
@@ -51,7 +58,6 @@
 namespace tcu {
 
 constexpr int kGroup = 128;              // tokens of a group: M of the products
-constexpr int kMixSlots = 5;             // tiles in the ring
 constexpr int kHalfBytes = 16384;        // 128 tokens x 64 features: one 128-byte-swizzled block of rows
 constexpr int kMixCtlBytes = 2048;
 
@@ -61,8 +67,9 @@ struct MixTokens {
 };
 
 struct MixJob {
-    uint8_t map[4];                      // tensor maps of q, k, v, o
-    uint8_t by_batch[4], by_head[4];     // 0 where the array repeats along that axis
+    uint8_t map[3];                      // tensor maps of q, k, v
+    uint8_t by_batch[3], by_head[3];     // 0 where the array repeats along that axis
+    uint8_t wide_rows;                   // rows of o start on 32-byte boundaries
     void *o;
     int64_t o_batch, o_token, o_head;    // strides in elements
     const float *init;                   // state that enters the walk, or NULL; (sequence, head) entries of dk * dv values
@@ -74,62 +81,91 @@ struct MixJob {
 };
 
 struct alignas(64) MixParams {
-    CUtensorMap map[7];
+    CUtensorMap map[4];
     MixJob job[3];
     const float *log_decay;
     const int64_t *offsets;
     uint32_t *error;                     // status word
     uint64_t tokens;
     uint32_t batch, heads, jobs, ranks;  // ranks: blocks of a cluster
-    long long spin_limit;
 };
 
+// Which groups of a walk a block takes, and how many tokens.
+struct MixPart {
+    uint32_t len, groups, per, first, last;   // tokens and groups of the sequence, groups per block, this block's [first, last) in walking order
+    bool lead;
+    __device__ __forceinline__ uint32_t in_time(uint32_t p) const { return lead ? p : groups - 1 - p; }
+    __device__ __forceinline__ int tokens_of(uint32_t p) const { return int(min(len - in_time(p) * kGroup, uint32_t(kGroup))); }
+    // tokens that the sequence's walk takes after group p
+    __device__ __forceinline__ float tokens_after(uint32_t p) const { return float(lead ? len - min((p + 1) * kGroup, len) : in_time(p) * kGroup); }
+    __device__ __forceinline__ float tokens_of_rank(uint32_t r) const {
+        const uint32_t a = min(r * per, groups), b = min((r + 1) * per, groups);
+        const uint32_t lo = (lead ? a : groups - b) * kGroup, hi = (lead ? b : groups - a) * kGroup;
+        return float(min(hi, len) - min(lo, len));
+    }
+};
+
+constexpr int kMixMostSlots = 8;
 struct MixCtl {
-    uint64_t full[kMixSlots], empty[kMixSlots];
+    uint64_t full[kMixMostSlots], empty[kMixMostSlots];      // (a tile is free when both issuers have done with it)
     uint64_t qk_done;                    // S is in tensor memory
+    uint64_t p_ready;                    // P is
+    uint64_t pv_done;                    // O is (and S is free)
+    uint64_t e_done;                     // E is
+    uint64_t o_free;                     // O and E have been read
     uint64_t x_ready;                    // X rounded into its operand, and multiplied by a^L in tensor memory
-    uint64_t kt_ready;                   // two terms of K~ written (and rows past the end of V cleared)
-    uint64_t two_done;                   // ... and multiplied
-    uint64_t third_ready;                // third term written over the second
-    uint64_t p_ready;                    // P in tensor memory
-    uint64_t o_done;                     // O and E are in tensor memory
-    uint64_t o_free;                     // ... and have been read
+    uint64_t k_scaled;                   // float16: the power of two for K~ is known
+    uint64_t k_ready;                    // two terms of K~ written (and rows past the end of V cleared)
+    uint64_t first_done, third_ready;    // the first has been multiplied, and the third written in its place
     uint64_t kv_done;                    // the group is in X
-    uint64_t o_staged;                   // output tile written to shared memory
-    uint64_t drained;
+    uint64_t drained[2];
     uint32_t tmem_base;
     volatile uint32_t abort_flag;
-    float biggest[2][16];                // float16: largest |k| and |X| seen by each warp
+    MixJob job;                          // what the block works on
+    MixPart part;
+    uint32_t t0, b, h, count, before;    // first token of the sequence; sequence (0 when packed) and head; groups of the walk, of the first phase
+    uint32_t thirds;                     // third terms of K~ in the first phase
+    uint64_t state_at;                   // of the states, in values
+    bool split, entered, owns_last;      // the walk starts from a state (else from zero); its last state is wanted
+    float log2_decay;
+    float biggest_k[2][8], biggest_x[2][4];      // float16: largest values seen by each warp
+    int scale_k[2];                      // float16: K~ is used as 2^scale_k K~
     float unscale[2];                    // float16: the factor that takes E back to the size of X
     float power[kGroup + 4];             // a^m
-    alignas(16) float block[32];         // factors of P along a block of 32 tokens
-    float near[32 + kGroup + 32];        // factors of P by distance, from 31 tokens on the wrong side of the diagonal (zero) on
+    alignas(16) float block[16];         // factors of P along a block of 16 tokens
+    float rank_decay[8];                 // a^(tokens of a part)
+    float near[32 + kGroup + 32];        // factors of P by distance, in the order of the columns: the distance falls along a row forward
+                                         // in time (from 160 to -31; below zero, on the wrong side of the diagonal, 0) and grows backward
 };
 static_assert(sizeof(MixCtl) <= kMixCtlBytes, "control block too large");
 
-// warps of the token role and of the state role: a thread has 64 columns of a row, of X and of K; then producer, issuer, store
-template <int D> constexpr int kMixRoleWarps = D / 16;
-template <int D> constexpr int kMixThreads = 32 * (2 * kMixRoleWarps<D> + 3);
+constexpr int kTokenWarps = 8, kKeyWarps = 8, kStateWarp = kTokenWarps + kKeyWarps, kProducerWarp = kStateWarp + 4, kScoreWarp = kProducerWarp + 1,
+              kProductWarp = kScoreWarp + 1;
+constexpr int kMixThreads = 32 * (kProductWarp + 1);
+template <int D> constexpr int kMixSlots = D == 64 ? 8 : 5;                  // tiles in the ring
 template <int D> constexpr int kMixTileBytes = D / 64 * kHalfBytes;
-template <int D> constexpr int kMixSmemBytes = 1024 + kMixCtlBytes + (kMixSlots + 1) * kMixTileBytes<D> + D * D * 2;
-static_assert(kMixSmemBytes<128> <= 232448 && 2 * (kMixSmemBytes<64> + 1024) <= 233472, "shared memory of an SM");
+template <int D> constexpr int kMixSmemBytes = 1024 + kMixCtlBytes + (kMixSlots<D> + 1) * kMixTileBytes<D> + D * D * 2;
+static_assert(kMixSmemBytes<128> <= 232448 && kMixSmemBytes<64> <= 232448, "shared memory of a block");
+static_assert(kMixSlots<64> <= kMixMostSlots, "ring");
 
-template <typename T> struct Half2;
-template <> struct Half2<__nv_bfloat16> {
+template <typename T> struct Half2Of;
+template <> struct Half2Of<__nv_bfloat16> {
     static constexpr uint32_t kType = 2;             // as in make_idesc
     static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
         const __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
         return *reinterpret_cast<const uint32_t *>(&p);
     }
     static __device__ __forceinline__ float2 unpack(uint32_t w) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u)); }
+    using Pair = __nv_bfloat162;
 };
-template <> struct Half2<__half> {
+template <> struct Half2Of<__half> {
     static constexpr uint32_t kType = 1;
     static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
         const __half2 p = __floats2half2_rn(lo, hi);
         return *reinterpret_cast<const uint32_t *>(&p);
     }
     static __device__ __forceinline__ float2 unpack(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2 *>(&w)); }
+    using Pair = __half2;
 };
 
 // two products, sums at once
@@ -146,655 +182,723 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
     return r;
 }
 
-struct MixWaiter {
-    MixCtl *ctl;
-    uint32_t *error;
-    long long limit;
-    __device__ __forceinline__ bool wait(const uint64_t &barrier, uint32_t parity) const {
-        const uint32_t bar = smem_u32(&barrier);
-        if (mbar_try_wait(bar, parity)) return true;
-        const long long t0 = clock64();
-        uint32_t spins = 0;
-        while (!mbar_try_wait(bar, parity)) {
-            if ((++spins & 0xFF) == 0) {
-                if (ctl->abort_flag) return false;
-                if (clock64() - t0 > limit) {
-                    ctl->abort_flag = 1;
-                    atomicExch(error, 5u);
-                    return false;
-                }
-            }
-        }
-        return true;
-    }
+// Packed arithmetic on two 16-bit values; rounded once, to nearest.
+template <typename T>
+struct Half2 : Half2Of<T> {
+    using P = typename Half2Of<T>::Pair;
+    static __device__ __forceinline__ P as(uint32_t w) { return *reinterpret_cast<const P *>(&w); }
+    static __device__ __forceinline__ uint32_t bits(P p) { return *reinterpret_cast<const uint32_t *>(&p); }
+    static __device__ __forceinline__ uint32_t mul(uint32_t a, uint32_t b) { return bits(__hmul2_rn(as(a), as(b))); }
+    static __device__ __forceinline__ uint32_t fma(uint32_t a, uint32_t b, uint32_t c) { return bits(__hfma2(as(a), as(b), as(c))); }
+    static __device__ __forceinline__ uint32_t neg(uint32_t a) { return a ^ 0x80008000u; }
 };
 
+// Waits for the phase of a barrier; false when the wait was given up, after about a second.
+constexpr uint32_t kMixWaitRounds = 10000;
+__device__ __forceinline__ bool mix_wait(MixCtl *ctl, const uint64_t &barrier, uint32_t parity) {
+    const bool ok = mbar_wait_bounded(smem_u32(&barrier), parity, kMixWaitRounds);
+    if (!ok) ctl->abort_flag = 1;
+    return ok;
+}
 // the same for a whole warp, with one answer for all lanes
-__device__ __forceinline__ bool wait_warp(const MixWaiter &w, const uint64_t &barrier, uint32_t parity) {
-    return __all_sync(0xffffffffu, w.wait(barrier, parity));
+__device__ __forceinline__ bool mix_wait_warp(MixCtl *ctl, const uint64_t &barrier, uint32_t parity) {
+    return __all_sync(0xffffffffu, mix_wait(ctl, barrier, parity));
 }
 
-// Which groups of a walk a block takes, and how many tokens.
-struct MixPart {
-    uint32_t groups, per, first, last;        // groups of the sequence, per block, this block's [first, last) in walking order
-    int64_t len;
-    bool lead;
-    __device__ __forceinline__ uint32_t in_time(uint32_t p) const { return lead ? p : groups - 1 - p; }
-    __device__ __forceinline__ int tokens_of(uint32_t p) const {
-        const int64_t left = len - int64_t(in_time(p)) * kGroup;
-        return left < kGroup ? int(left) : kGroup;
-    }
-    __device__ __forceinline__ float tokens_of_rank(uint32_t r) const {
-        const uint32_t a = min(r * per, groups), b = min((r + 1) * per, groups);
-        const int64_t lo = int64_t(lead ? a : groups - b) * kGroup, hi = int64_t(lead ? b : groups - a) * kGroup;
-        return float((hi < len ? hi : len) - (lo < len ? lo : len));
-    }
-};
+// The same for the warps of a role: one of them polls, the others sleep at a named barrier (thirty polling warps took three
+// quarters of the issue slots that they were waiting for).  All get the same answer, so they give up together.
+__device__ __forceinline__ bool mix_gate(MixCtl *ctl, int id, int threads, bool leader, const uint64_t &barrier, uint32_t parity) {
+    bool failed = false;
+    if (leader) failed = !mix_wait_warp(ctl, barrier, parity);
+    return !named_barrier_or(id, threads, failed);
+}
+
+// A block, as its roles see it.  Each role is a function of its own, called for each of the two phases (a walk that is not split has
+// only the second): six programs share the SM's instruction cache, and when the compiler merged and copied them the kernel was four
+// times this size and spent most of its time fetching instructions.
+extern __shared__ uint8_t mix_smem[];
+// (an offset from the array, and found again by each role, so that the compiler knows the address space)
+__device__ __forceinline__ MixCtl *mix_ctl() { return reinterpret_cast<MixCtl *>(mix_smem + (-smem_u32(mix_smem) & 1023)); }
 
 template <int D, typename T>
-__global__ void __launch_bounds__(kMixThreads<D>, D == 64 ? 2 : 1) tcu_linattn_mix_kernel(const __grid_constant__ MixParams p) {
+struct Mix {
     using H = Half2<T>;
-    constexpr bool kIsHalf = std::is_same<T, __half>::value;
-    constexpr bool kThird = !kIsHalf;                             // K~ in three terms
-    constexpr int kTile = kMixTileBytes<D>;
-    constexpr int kXHalf = D * 128;                               // one 64-wide half of the operand X: D rows of 128 bytes
-    constexpr int kWarps = kMixRoleWarps<D>, kRole = kWarps * 32; // warps and threads of the token role, and of the state role
-    // tensor memory: S, O, E, X.  P takes the place of S; with D = 128 two warps share the 128 columns of a token, so each
-    // 64 columns of S leave their P in their own first 32 columns.  With D = 64 P fills the first 64 columns of S and O the
-    // others, and two blocks share an SM.
-    constexpr uint32_t kColS = 0, kColO = D == 128 ? 128 : 64, kColE = D == 128 ? 256 : 128, kColX = D == 128 ? 384 : 192;
-    constexpr uint32_t kColP1 = D == 128 ? 64 : 32;               // P of tokens 64 ... 127
-    constexpr uint32_t kColumns = D == 128 ? 512 : 256;
-
-    extern __shared__ uint8_t smem_raw[];
-    uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    MixCtl *ctl = reinterpret_cast<MixCtl *>(smem);
-    uint8_t *ring = smem + kMixCtlBytes;
-    const uint32_t ring_at = smem_u32(ring), low_at = ring_at + kMixSlots * kTile, x_at = low_at + kTile;
-    float *exchange = reinterpret_cast<float *>(ring);            // D x D state totals, between the two phases of a split walk
-
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t rank = blockIdx.x % p.ranks, work = blockIdx.x / p.ranks;
-    const MixJob &job = p.job[work % p.jobs];
-    const uint32_t unit = work / p.jobs, b = unit / p.heads, h = unit % p.heads;
-    // packed: whatever the offsets hold, no token outside the arrays is touched
-    const int64_t most = int64_t(p.tokens), t0 = p.offsets ? min(max(p.offsets[b], int64_t(0)), most) : 0;
-    MixPart part;
-    part.lead = job.lead != 0;
-    part.len = p.offsets ? min(max(p.offsets[b + 1], t0), most) - t0 : most;
-    part.groups = uint32_t((part.len + kGroup - 1) / kGroup);
-    part.per = (part.groups + p.ranks - 1) / p.ranks;
-    part.first = min(rank * part.per, part.groups);
-    part.last = min((rank + 1) * part.per, part.groups);
-    const uint32_t count = part.last - part.first;
-    const bool split = p.ranks > 1;
-    const bool totals = split && count > 0 && part.last < part.groups;       // later blocks need what this part leaves
-    const bool owns_last = job.last && (part.groups == 0 ? rank == 0 : (part.last == part.groups && count > 0));
-    const bool entered = job.init || (split && rank > 0);                    // the walk starts from a state (else from zero)
-    const uint32_t before = totals ? count : 0;                              // groups of the first phase
-    const uint32_t tile0 = 2 * before;                                       // tiles loaded in the first phase
-    const int bz = p.offsets ? 0 : int(b);
-
-    // ---- loads.  Tile n of the block: K and V of the groups of the first phase, then K, Q and V of those of the walk.
-    auto slot_of = [&](uint32_t n) { return ring_at + (n % kMixSlots) * kTile; };
-    auto load = [&](uint32_t n) {
-        const uint32_t m = n - tile0, group = n < tile0 ? n >> 1 : m / 3;
-        const uint32_t which = n < tile0 ? (n & 1 ? 2 : 1) : (m % 3 == 0 ? 1 : m % 3 == 1 ? 0 : 2);
-        const int token = int(t0 + int64_t(part.in_time(part.first + group)) * kGroup);
-        const uint32_t bar = smem_u32(&ctl->full[n % kMixSlots]);
-        mbar_expect_tx(bar, kTile);
-        for (int half = 0; half < D / 64; ++half)
-            tma_load_4d(slot_of(n) + half * kHalfBytes, &p.map[job.map[which]], half * 64, token, int(h) * job.by_head[which],
-                        bz * job.by_batch[which], bar);
-    };
-    const uint32_t phase_one = split ? tile0 : tile0 + 3 * count, tiles = tile0 + 3 * count;
-    uint32_t issued = 0;
-    if (warp == 2 * kWarps && lane == 0) {
-        for (int i = 0; i < kMixSlots; ++i) {
-            mbar_init(smem_u32(&ctl->full[i]), 1);
-            mbar_init(smem_u32(&ctl->empty[i]), 1);
-        }
-        mbar_init(smem_u32(&ctl->qk_done), 1);
-        mbar_init(smem_u32(&ctl->x_ready), kRole);
-        mbar_init(smem_u32(&ctl->kt_ready), kRole);
-        mbar_init(smem_u32(&ctl->third_ready), kRole);
-        mbar_init(smem_u32(&ctl->p_ready), kRole);
-        mbar_init(smem_u32(&ctl->o_done), 1);
-        mbar_init(smem_u32(&ctl->o_free), kRole);
-        mbar_init(smem_u32(&ctl->two_done), 1);
-        mbar_init(smem_u32(&ctl->kv_done), 1);
-        mbar_init(smem_u32(&ctl->o_staged), kRole);
-        mbar_init(smem_u32(&ctl->drained), 1);
-        ctl->abort_flag = 0;
-        fence_barrier_init();
-        for (; issued < kMixSlots && issued < phase_one; ++issued) load(issued);       // the ring is empty
+    static constexpr bool kIsHalf = std::is_same<T, __half>::value;
+    static constexpr float kThirdFrom = -6.0f;                           // bfloat16: log2 of the decay to the end from which on K~ has a third term
+    static __device__ __forceinline__ bool has_third(const MixCtl *ctl, const MixPart &part, uint32_t p) {
+        return !kIsHalf && ctl->log2_decay * part.tokens_after(p) > kThirdFrom;
     }
-    if (warp == 2 * kWarps + 1) {
-        tmem_alloc(smem_u32(&ctl->tmem_base), kColumns);
-        tmem_relinquish();
-    }
-    // decays: a^m = 2^(m log2 a); -inf becomes a value whose multiples are finite, so that a^0 = 1
-    const float log2a = fmaxf(p.log_decay[h] * 1.4426950408889634f, -1e30f);
-    if (threadIdx.x <= kGroup) ctl->power[threadIdx.x] = exp2f(log2a * float(threadIdx.x));
-    if (threadIdx.x < 32) ctl->block[threadIdx.x] = job.in_scale * job.out_scale * exp2f(log2a * float(part.lead ? 31 - int(threadIdx.x) : int(threadIdx.x)));
-    if (threadIdx.x < 32 + kGroup + 32) {
-        const int apart = int(threadIdx.x) - 31;
-        ctl->near[threadIdx.x] = apart >= 0 ? job.in_scale * job.out_scale * exp2f(log2a * float(apart)) : 0.0f;
-    }
-    tc_fence_before();
-    __syncthreads();
-    tc_fence_after();
-    const uint32_t tmem = ctl->tmem_base;
-    const MixWaiter w{ctl, p.error, p.spin_limit};
+    static constexpr uint32_t kTile = kMixTileBytes<D>, kSlots = kMixSlots<D>;
+    static constexpr uint32_t kAhead = 2;                                // groups ahead of their load that tiles are brought into L2
+    static constexpr int kXHalf = D * 128;                               // one 64-wide half of the operand X: D rows of 128 bytes
+    static constexpr int kCols = D / 2, kKeyCols = D / 2;                // features of a token that a thread of the token / key role has
+    // tensor memory: S, O, E, X.  P takes the place of S: two warps share the 128 columns of a token, and each 64 columns of S
+    // leave their P in their own first 32 columns.
+    static constexpr uint32_t kColS = 0, kColO = 128, kColE = 256, kColX = 384, kColumns = 512;
 
-    // ---- roles.  Each takes the groups [0, before) of the first phase, then [0, count) of the walk; `it` counts both.
+    // shared memory: control block, ring of tiles (between the phases: D x D state totals), second term of K~, operand X
+    static __device__ __forceinline__ uint32_t ring_at(const MixCtl *ctl) { return smem_u32(ctl) + kMixCtlBytes; }
+    static __device__ __forceinline__ uint32_t low_at(const MixCtl *ctl) { return ring_at(ctl) + kSlots * kTile; }
+    static __device__ __forceinline__ uint32_t x_at(const MixCtl *ctl) { return low_at(ctl) + kTile; }
+    static __device__ __forceinline__ uint32_t slot_at(const MixCtl *ctl, uint32_t tile) { return ring_at(ctl) + tile % kSlots * kTile; }
+    static __device__ __forceinline__ bool wait_full(MixCtl *ctl, uint32_t tile) { return mix_wait_warp(ctl, ctl->full[tile % kSlots], (tile / kSlots) & 1); }
     // Rows of a tile: token i of the group at i * 128 bytes, 16-byte pieces exchanged by the swizzle (piece ^ (i & 7)).
-    auto produce = [&](uint32_t end) {
-        for (; issued < end; ++issued) {
-            if (issued >= kMixSlots && !w.wait(ctl->empty[issued % kMixSlots], (issued / kMixSlots - 1) & 1)) return;
-            load(issued);
-        }
-    };
-    auto full = [&](uint32_t n) { return w.wait(ctl->full[n % kMixSlots], (n / kMixSlots) & 1); };
-    auto full_warp = [&](uint32_t n) { return wait_warp(w, ctl->full[n % kMixSlots], (n / kMixSlots) & 1); };
+    static __device__ __forceinline__ uint32_t piece_at(int row, int feature) {
+        return uint32_t((feature >> 6) * kHalfBytes + row * 128) + (((uint32_t(feature >> 3) & 7) ^ uint32_t(row & 7)) << 4);
+    }
+    static __device__ __forceinline__ float pow2(int n) { return __uint_as_float(uint32_t(min(max(n, -126), 127) + 127) << 23); }
+    static __device__ __forceinline__ int exponent(float x) { return int((__float_as_uint(x) >> 23) & 0xFF) - 127; }
 
-    // ---- the issuer: a whole warp walks the loop, so that descriptors stay in uniform registers; one lane issues
-    const uint32_t idesc_s = make_idesc(H::kType, kGroup), idesc_d = make_idesc(H::kType, D);
-    // X^T += V^T K~, one term of K~: lanes are columns of v, columns are rows of the state.  With D = 64 the upper 64 lanes
-    // multiply whatever lies behind the tile; nobody reads them.
-    auto issue_state = [&](uint32_t kt, uint32_t v_slot, bool onto) {
-        const uint64_t va = make_smem_desc_mn(v_slot, kHalfBytes), kb = make_smem_desc_mn(kt, kHalfBytes);
+    // ---- tokens: the outputs of group i - 1, then P of group i
+    static __device__ __noinline__ void tokens() {
+        MixCtl *ctl = mix_ctl();
+        const int warp = threadIdx.x >> 5, row0 = (warp & 3) * 32, row = row0 + (threadIdx.x & 31);
+        const int side = warp >> 2;                                                // which half of the row
+        const uint32_t lanes = ctl->tmem_base + (uint32_t(warp & 3) << 21);        // this warp's 32 lanes (bits 16 and up)
+        const MixPart part = ctl->part;
+        const uint32_t n = ctl->count;
+        if (n == 0) return;
+#pragma unroll 1
+        for (uint32_t i = 0; i <= n; ++i) {
+            if (i > 0) {
+                const uint32_t g = i - 1;
+                if (!mix_gate(ctl, 1, 32 * kTokenWarps, warp == 0, ctl->pv_done, g & 1)) return;
+                if (!mix_gate(ctl, 1, 32 * kTokenWarps, warp == 0, ctl->e_done, g & 1)) return;
+                tc_fence_after();
+                const bool no_e = g == 0 && !ctl->entered;                  // no state: E was not formed
+                const int tokens = part.tokens_of(part.first + g), order = part.lead ? row : tokens - 1 - row;
+                float e = order >= 0 ? ctl->job.out_scale * ctl->power[order + int(part.lead)] : 0.0f;
+                if (kIsHalf) e *= ctl->unscale[(ctl->before + g) & 1];
+                const float2 e2 = make_float2(e, e);
+                const uint32_t token = ctl->t0 + part.in_time(part.first + g) * kGroup + row;
+                T *to = reinterpret_cast<T *>(ctl->job.o) + ctl->b * ctl->job.o_batch + token * ctl->job.o_token + int64_t(ctl->h) * ctl->job.o_head;
+                const int dv = int(ctl->job.dv), wide_rows = ctl->job.wide_rows;
+#pragma unroll 1
+                for (int c = side * kCols; c < side * kCols + kCols; c += 16) {
+                    uint32_t vo[16], ve[16], out[8];
+                    tmem_ld16(lanes + kColO + c, vo);
+                    if (no_e) {
 #pragma unroll
-        for (int s = 0; s < kGroup / 16; ++s)
-            mma_issue<false>(tmem + kColX, va + s * (2048 >> 4), kb + s * (2048 >> 4), idesc_d | kIdescAMn | kIdescBMn, onto || s > 0);
-    };
-    // the state's products of group `it`, in two steps; false when a wait was given up
-    auto state_two = [&](uint32_t it, uint32_t k_slot, uint32_t v_slot, bool wanted, bool onto) {
-        if (!wait_warp(w, ctl->kt_ready, it & 1)) return false;
-        tc_fence_after();
-        if (elect_one()) {
-            if (wanted) {
-                issue_state(k_slot, v_slot, onto);
-                issue_state(low_at, v_slot, true);
+                        for (int j = 0; j < 16; ++j) ve[j] = 0;
+                    } else {
+                        tmem_ld16(lanes + kColE + c, ve);
+                    }
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const float2 x = fma2(e2, make_float2(__uint_as_float(ve[2 * j]), __uint_as_float(ve[2 * j + 1])),
+                                              make_float2(__uint_as_float(vo[2 * j]), __uint_as_float(vo[2 * j + 1])));
+                        out[j] = H::pack(x.x, x.y);
+                    }
+                    const int width = row < tokens ? dv - c : 0;            // features to write from here on
+                    if (wide_rows && width >= 16) {
+                        st_global_v8(to + c, out);
+                    } else {
+                        if (width >= 8) st_global_v4(to + c, out[0], out[1], out[2], out[3]);
+                        if (width >= 16) st_global_v4(to + c + 8, out[4], out[5], out[6], out[7]);
+                        else if (width > 0 && (width & 7)) {
+                            uint32_t tail[4];
+#pragma unroll
+                            for (int k = 0; k < 4; ++k) tail[k] = width < 8 ? out[k] : out[4 + k];
+#pragma unroll
+                            for (int k = 0; k < 7; ++k)
+                                if (k < (width & 7)) to[c + (width & 8) + k] = reinterpret_cast<const T *>(tail)[k];
+                        }
+                    }
+                }
+                tc_fence_before();
+                mbar_arrive(smem_u32(&ctl->o_free));
             }
-            if (kThird) mma_commit(smem_u32(&ctl->two_done));
+            if (i < n) {
+                const int tokens = part.tokens_of(part.first + i);
+                if (!mix_gate(ctl, 1, 32 * kTokenWarps, warp == 0, ctl->qk_done, i & 1)) return;
+                tc_fence_after();
+                // scores of 16 tokens at a time: all of them count, none, or (around the diagonal and the end) some
+#pragma unroll 1
+                for (int c = 64 * side; c < 64 * side + 64; c += 16) {
+                    const bool all = part.lead ? c + 15 <= row0 : c >= row0 + 31 && c + 15 < tokens;
+                    const bool none = part.lead ? c > row0 + 31 : c + 15 < row0 || c >= tokens;
+                    uint32_t out[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) out[j] = 0;
+                    if (!none) {
+                        uint32_t v[16];
+                        tmem_ld16(lanes + kColS + c, v);
+                        const float f = all ? ctl->power[part.lead ? row - c - 15 : c - row] : 0.0f;
+                        tmem_ld_wait();
+                        if (all) {
+                            const float2 f2 = make_float2(f, f);
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                const float4 t = reinterpret_cast<const float4 *>(ctl->block)[j];
+                                const float2 x = mul2(make_float2(__uint_as_float(v[4 * j]), __uint_as_float(v[4 * j + 1])), mul2(f2, make_float2(t.x, t.y)));
+                                const float2 y = mul2(make_float2(__uint_as_float(v[4 * j + 2]), __uint_as_float(v[4 * j + 3])), mul2(f2, make_float2(t.z, t.w)));
+                                out[2 * j] = H::pack(x.x, x.y);
+                                out[2 * j + 1] = H::pack(y.x, y.y);
+                            }
+                        } else {
+                            // columns lo ... hi count; the others may not be finite: they are left out, not multiplied by zero
+                            const int apart = part.lead ? row - c : c - row, lo = part.lead ? 0 : max(-apart, 0), hi = min(part.lead ? apart : tokens - 1 - c, 15);
+                            const uint32_t counts = hi >= lo ? (0xFFFFFFFFu >> (31 - hi)) & (0xFFFFFFFFu << lo) : 0u;
+                            const float *factor = ctl->near + (part.lead ? 160 - apart : 31 + apart);
+#pragma unroll
+                            for (int j = 0; j < 16; ++j) v[j] = counts & (1u << j) ? __float_as_uint(__uint_as_float(v[j]) * factor[j]) : 0u;
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) out[j] = H::pack(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1]));
+                        }
+                    }
+                    tmem_st8(lanes + kColS + 64 * side + (c % 64) / 2, out);          // never over scores still to be read
+                }
+                tmem_st_wait();
+                tc_fence_before();
+                mbar_arrive(smem_u32(&ctl->p_ready));
+            }
+        }
+    }
+
+    // ---- keys.  float16: powers of two, found for every group, keep the operands inside the type: X is held as 2^s X, so that the
+    // keys can be used as 2^s K~ with the largest near 2^14 (the low terms of small ones would fall below 2^-24).
+    static __device__ __noinline__ void keys(uint32_t phase) {
+        MixCtl *ctl = mix_ctl();
+        const int warp = (threadIdx.x >> 5) - kTokenWarps, lane = threadIdx.x & 31, row = (warp & 3) * 32 + lane;
+        const int at_feature = (warp >> 2) * kKeyCols;                             // this thread's half of the row
+        const MixPart part = ctl->part;
+        const uint32_t n = phase ? ctl->count : ctl->before;
+        const uint32_t made = phase && n > 0 && !ctl->owns_last ? n - 1 : n;       // the last group's are not needed if its state is not
+        uint32_t it = phase ? ctl->before : 0, tile = 2 * it;                      // groups before, their tiles
+        uint32_t thirds = phase ? ctl->thirds : 0;
+        auto gate = [&](const uint64_t &barrier, uint32_t parity) { return mix_gate(ctl, 2, 32 * kKeyWarps, warp == 0, barrier, parity); };
+        auto gate_full = [&](uint32_t tile) { return gate(ctl->full[tile % kSlots], (tile / kSlots) & 1); };
+#pragma unroll 1
+        for (uint32_t i = 0; i < made; ++i, ++it, tile += phase + 2) {
+            const uint32_t k_slot = slot_at(ctl, tile);
+            const int tokens = part.tokens_of(part.first + i);
+            const bool valid = row < tokens;
+            // walking order: token `row` of the group is j = row forward, tokens - 1 - row backward; a^(tokens - j - lead)
+            float f = valid ? ctl->job.in_scale * ctl->power[part.lead ? tokens - 1 - row : row + 1] : 0.0f;
+            if (!gate_full(tile)) return;
+            if (kIsHalf) {
+                float big = 0.0f;
+                if (valid) {
+#pragma unroll 1
+                    for (int c = 0; c < kKeyCols; c += 8) {
+                        uint32_t k4[4];
+                        ld_shared_v4(k_slot + piece_at(row, at_feature + c), k4[0], k4[1], k4[2], k4[3]);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float2 x = H::unpack(k4[e]);
+                            big = fmaxf(big, fmaxf(fabsf(x.x), fabsf(x.y)));
+                        }
+                    }
+                }
+                __syncwarp();
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
+                if (lane == 0) ctl->biggest_k[it & 1][warp] = big;
+                named_barrier_sync(2, 32 * kKeyWarps);
+#pragma unroll
+                for (int j = 0; j < kKeyWarps; ++j) big = fmaxf(big, ctl->biggest_k[it & 1][j]);
+                // the powers of a in K~ go from a^(1 - lead) to a^(tokens - lead)
+                const float top = fmaxf(ctl->power[1 - int(part.lead)], ctl->power[tokens - int(part.lead)]);
+                const int scale = min(max(14 - exponent(big * fabsf(ctl->job.in_scale) * top), -30), 100);
+                f *= pow2(scale);
+                // (published when the state warps have read the last one)
+                if (it > 0 && !gate(ctl->kv_done, (it - 1) & 1)) return;
+                if (warp == 0 && lane == 0) {
+                    ctl->scale_k[it & 1] = scale;
+                    mbar_arrive(smem_u32(&ctl->k_scaled));
+                }
+            } else if (it > 0 && !gate(ctl->kv_done, (it - 1) & 1)) {        // the buffers of the further terms are free
+                return;
+            }
+            if (phase && !gate(ctl->qk_done, i & 1)) return;                 // K itself has been multiplied
+            if (tokens < kGroup && !gate_full(tile + phase + 1)) return;
+            const bool third = has_third(ctl, part, part.first + i);
+            uint32_t rest[kIsHalf ? 1 : kKeyCols / 2];
+            if (kIsHalf || third) {
+                const float2 f2 = make_float2(f, f), minus = make_float2(-1.0f, -1.0f);
+#pragma unroll
+                for (int c = 0; c < kKeyCols; c += 8) {
+                    const uint32_t at = piece_at(row, at_feature + c);
+                    uint32_t k4[4], hi[4], lo[4];
+                    ld_shared_v4(k_slot + at, k4[0], k4[1], k4[2], k4[3]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float2 x = mul2(H::unpack(valid ? k4[e] : 0u), f2);
+                        hi[e] = H::pack(x.x, x.y);
+                        const float2 y = fma2(H::unpack(hi[e]), minus, x);
+                        lo[e] = H::pack(y.x, y.y);
+                        if (!kIsHalf) {
+                            const float2 z = fma2(H::unpack(lo[e]), minus, y);
+                            rest[kIsHalf ? 0 : c / 2 + e] = H::pack(z.x, z.y);
+                        }
+                    }
+                    st_shared_v4(k_slot + at, hi[0], hi[1], hi[2], hi[3]);
+                    st_shared_v4(low_at(ctl) + at, lo[0], lo[1], lo[2], lo[3]);
+                }
+            } else {
+                // packed arithmetic: with f = f1 + f2 in two terms, hi = k f1 rounded, its error k f1 - hi exactly (a product of two
+                // 8-bit mantissas has 16 bits), and lo = k f2 + that, rounded
+                const uint32_t f1 = H::pack(f, f), f2 = H::pack(f - H::unpack(f1).x, f - H::unpack(f1).x);
+#pragma unroll 2
+                for (int c = 0; c < kKeyCols; c += 8) {
+                    const uint32_t at = piece_at(row, at_feature + c);
+                    uint32_t k4[4], hi[4], lo[4];
+                    ld_shared_v4(k_slot + at, k4[0], k4[1], k4[2], k4[3]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const uint32_t k = valid ? k4[e] : 0u;
+                        hi[e] = H::mul(k, f1);
+                        lo[e] = H::fma(k, f2, H::fma(k, f1, H::neg(hi[e])));
+                    }
+                    st_shared_v4(k_slot + at, hi[0], hi[1], hi[2], hi[3]);
+                    st_shared_v4(low_at(ctl) + at, lo[0], lo[1], lo[2], lo[3]);
+                }
+            }
+            if (!valid) clear_v(row, tile + phase + 1, at_feature);
+            fence_proxy_async_smem();
+            mbar_arrive(smem_u32(&ctl->k_ready));
+            if (!kIsHalf && third) {
+                if (!gate(ctl->first_done, thirds & 1)) return;
+#pragma unroll
+                for (int c = 0; c < kKeyCols; c += 8)
+                    st_shared_v4(k_slot + piece_at(row, at_feature + c), rest[kIsHalf ? 0 : c / 2], rest[kIsHalf ? 0 : c / 2 + 1], rest[kIsHalf ? 0 : c / 2 + 2],
+                                 rest[kIsHalf ? 0 : c / 2 + 3]);
+                fence_proxy_async_smem();
+                mbar_arrive(smem_u32(&ctl->third_ready));
+                ++thirds;
+            }
+        }
+        if (made < n) {
+            const int tokens = part.tokens_of(part.first + made);
+            // (the issuers have to see every phase of k_ready: not before they have come this far)
+            if (it > 0 && !gate(ctl->kv_done, (it - 1) & 1)) return;
+            if (kIsHalf && warp == 0 && lane == 0) {
+                ctl->scale_k[it & 1] = 0;
+                mbar_arrive(smem_u32(&ctl->k_scaled));
+            }
+            if (!gate(ctl->qk_done, made & 1)) return;
+            if (tokens < kGroup) {
+                if (!gate_full(tile + 2)) return;
+                if (row >= tokens) clear_v(row, tile + 2, at_feature);
+            }
+            fence_proxy_async_smem();
+            mbar_arrive(smem_u32(&ctl->k_ready));
+        }
+    }
+    // what follows the sequence may hold anything: zero times it has to be zero
+    static __device__ __noinline__ void clear_v(int row, uint32_t tile, int at_feature) {
+        MixCtl *ctl = mix_ctl();
+#pragma unroll 1
+        for (int c = 0; c < kKeyCols; c += 8) st_shared_v4(slot_at(ctl, tile) + piece_at(row, at_feature + c), 0, 0, 0, 0);
+    }
+
+    // ---- state: thread = column of v (the first D lanes)
+    static __device__ __noinline__ void state(uint32_t phase) {
+        MixCtl *ctl = mix_ctl();
+        const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = (warp & 3) * 32 + lane;
+        const bool holds_x = (warp & 3) * 32 < D;                            // whole warps
+        const uint32_t x_lanes = ctl->tmem_base + (uint32_t(warp & 3) << 21) + kColX;
+        const MixPart part = ctl->part;
+        const uint32_t n = phase ? ctl->count : ctl->before, base = phase ? ctl->before : 0;
+        const bool entered = phase && ctl->entered;
+        const uint32_t dk = uint32_t(row) < ctl->job.dv ? ctl->job.dk : 0;   // rows of this thread's column in the states of the caller
+        float *exchange = reinterpret_cast<float *>(reinterpret_cast<uint8_t *>(ctl) + kMixCtlBytes) + row;
+        int held = 0;                                                        // float16: X is held as 2^held X
+        auto gate = [&](const uint64_t &barrier, uint32_t parity) { return mix_gate(ctl, 3, 128, warp == kStateWarp, barrier, parity); };
+#pragma unroll 1
+        for (uint32_t i = 0; i < n; ++i) {
+            const uint32_t it = base + i;
+            const bool fresh = i == 0 && !entered;                           // X is zero: the first product does not add to it
+            float shrink = 1.0f, keep = ctl->power[part.tokens_of(part.first + i)];
+            if (i > 0) {
+                if (!gate(ctl->kv_done, (it - 1) & 1)) return;
+                tc_fence_after();
+            }
+            if (kIsHalf) {
+                if (!gate(ctl->k_scaled, it & 1)) return;
+                float big = 0.0f;
+                if (!fresh && holds_x) {
+#pragma unroll 1
+                    for (int c = 0; c < D; c += 16) {
+                        uint32_t v[16];
+                        tmem_ld16(x_lanes + c, v);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) big = fmaxf(big, fabsf(__uint_as_float(v[j])));
+                    }
+                }
+#pragma unroll
+                for (int o = 16; o > 0; o >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
+                if (lane == 0) ctl->biggest_x[it & 1][warp & 3] = big;
+                named_barrier_sync(3, 128);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) big = fmaxf(big, ctl->biggest_x[it & 1][j]);
+                const int ex = min(max(exponent(big), -60), 127), now = ctl->scale_k[it & 1];
+                shrink = pow2(14 - ex);
+                if (threadIdx.x == 32 * kStateWarp) ctl->unscale[it & 1] = pow2(ex - 14 - held);
+                keep *= pow2(now - held);
+                held = now;
+            }
+            if (!fresh && holds_x) {
+                const float2 keep2 = make_float2(keep, keep), shrink2 = make_float2(shrink, shrink);
+                auto step = [&](uint32_t (&v)[16], int c) {
+                    if (phase) {
+#pragma unroll
+                        for (int j = 0; j < 16; j += 8) {
+                            uint32_t w4[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                float2 x = make_float2(__uint_as_float(v[j + 2 * e]), __uint_as_float(v[j + 2 * e + 1]));
+                                if (kIsHalf) x = mul2(x, shrink2);
+                                w4[e] = H::pack(x.x, x.y);
+                            }
+                            st_shared_v4(x_at(ctl) + ((c + j) >> 6) * kXHalf + row * 128 + (((uint32_t((c + j) >> 3) & 7) ^ uint32_t(row & 7)) << 4), w4[0], w4[1], w4[2], w4[3]);
+                        }
+                    }
+#pragma unroll
+                    for (int j = 0; j < 16; j += 2) {
+                        const float2 x = mul2(make_float2(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), keep2);
+                        v[j] = __float_as_uint(x.x);
+                        v[j + 1] = __float_as_uint(x.y);
+                    }
+                    tmem_st16(x_lanes + c, v);
+                };
+                uint32_t v0[16], v1[16];                                     // the next columns are on their way while these are worked on
+                tmem_ld16(x_lanes, v0);
+#pragma unroll 1
+                for (int c = 0; c < D; c += 32) {
+                    tmem_ld_wait();
+                    tmem_ld16(x_lanes + c + 16, v1);
+                    step(v0, c);
+                    tmem_ld_wait();
+                    if (c + 32 < D) tmem_ld16(x_lanes + c + 32, v0);
+                    step(v1, c + 16);
+                }
+                tmem_st_wait();
+                if (phase) fence_proxy_async_smem();
+            }
+            tc_fence_before();
+            mbar_arrive(smem_u32(&ctl->x_ready));
+        }
+        // the state that leaves: to the other blocks, or to the caller
+        if (phase ? !ctl->owns_last : n == 0) return;
+        if (n > 0 && !gate(ctl->kv_done, (base + n - 1) & 1)) return;
+        tc_fence_after();
+        if (!holds_x) return;
+        float *to = phase ? ctl->job.last + ctl->state_at + row : exchange;
+        const uint32_t pitch = phase ? ctl->job.dv : D, rows = phase ? dk : D;
+        const float back = kIsHalf ? pow2(-held) : 1.0f;
+#pragma unroll 1
+        for (uint32_t c = 0; c < D; c += 16) {
+            uint32_t v[16];
+            tmem_ld16(x_lanes + c, v);
+            tmem_ld_wait();
+#pragma unroll
+            for (uint32_t j = 0; j < 16; ++j)
+                if (c + j < rows) to[uint64_t(c + j) * pitch] = __uint_as_float(v[j]) * back;
+        }
+    }
+    // the state that enters the walk
+    static __device__ __noinline__ void enter() {
+        MixCtl *ctl = mix_ctl();
+        const int warp = threadIdx.x >> 5, row = (warp & 3) * 32 + (threadIdx.x & 31);
+        if (!(ctl->entered || ctl->count == 0) || (warp & 3) * 32 >= D) return;
+        const bool exchanged = ctl->split && ctl->count > 0;
+        const float *exchange = reinterpret_cast<const float *>(reinterpret_cast<uint8_t *>(ctl) + kMixCtlBytes) + row;
+        const float *from = exchanged ? exchange : ctl->job.init + ctl->state_at + uint64_t(row) * ctl->job.init_v;
+        const uint32_t pitch = exchanged ? D : ctl->job.init_k, rows = exchanged ? D : ctl->job.init && uint32_t(row) < ctl->job.dv ? ctl->job.dk : 0;
+#pragma unroll 1
+        for (uint32_t c = 0; c < D; c += 16) {
+            uint32_t v[16];
+#pragma unroll
+            for (uint32_t j = 0; j < 16; ++j) v[j] = c + j < rows ? __float_as_uint(from[uint64_t(c + j) * pitch]) : 0u;
+            tmem_st16(ctl->tmem_base + (uint32_t(warp & 3) << 21) + kColX + c, v);
+        }
+        tmem_st_wait();
+    }
+
+    // ---- loads (one thread): K and V of the groups of the first phase; K, Q and V of those of the walk
+    static __device__ __noinline__ void loads(const CUtensorMap *maps, uint32_t phase) {
+        MixCtl *ctl = mix_ctl();
+        const MixPart part = ctl->part;
+        const uint32_t n = phase ? ctl->count : ctl->before;
+        uint32_t tile = phase ? 2 * ctl->before : 0;
+#pragma unroll 1
+        for (uint32_t m = 0, group = 0, place = 0; group < n; ++m, ++tile) {
+            const uint32_t slot = tile % kSlots;
+            const uint32_t ahead = group + kAhead;
+            if (ahead < n) {                        // into L2, so that a load issued when its slot falls free takes less than the chain leaves it
+                const uint32_t which = place == 0 ? 1 : place == 1 && phase ? 0 : 2;
+#pragma unroll
+                for (int half = 0; half < D / 64; ++half)
+                    tma_prefetch_l2_4d(maps + ctl->job.map[which], half * 64, int(ctl->t0 + part.in_time(part.first + ahead) * kGroup), int(ctl->h * ctl->job.by_head[which]),
+                                       int(ctl->b * ctl->job.by_batch[which]));
+            }
+            if (tile >= kSlots && !mix_wait(ctl, ctl->empty[slot], (tile / kSlots - 1) & 1)) break;
+            const uint32_t which = place == 0 ? 1 : place == 1 && phase ? 0 : 2;
+            const uint32_t bar = smem_u32(&ctl->full[slot]), token = ctl->t0 + part.in_time(part.first + group) * kGroup;
+            mbar_expect_tx(bar, kTile);
+#pragma unroll
+            for (int half = 0; half < D / 64; ++half)
+                tma_load_4d(ring_at(ctl) + slot * kTile + half * kHalfBytes, maps + ctl->job.map[which], half * 64, int(token), int(ctl->h * ctl->job.by_head[which]),
+                            int(ctl->b * ctl->job.by_batch[which]), bar);
+            if (++place == phase + 2) {
+                place = 0;
+                ++group;
+            }
+        }
+        if (ctl->abort_flag)                        // copies in flight must land before the block may exit
+            for (uint32_t m = tile > kSlots ? tile - kSlots : 0; m < tile; ++m)
+                mbar_wait_bounded(smem_u32(&ctl->full[m % kSlots]), (m / kSlots) & 1, kMixWaitRounds);
+    }
+
+    // ---- products: a whole warp walks the loop, so that descriptors stay in uniform registers; one lane issues
+    static __device__ __forceinline__ void drain(MixCtl *ctl, int which) {
+        if (ctl->abort_flag && elect_one()) {       // products in flight must end: tensor memory is freed afterwards
+            mma_commit(smem_u32(&ctl->drained[which]));
+            mbar_wait_bounded(smem_u32(&ctl->drained[which]), 0, kMixWaitRounds);
         }
         __syncwarp();
-        return true;
-    };
-    auto state_rest = [&](uint32_t it, uint32_t nk, uint32_t nv, bool wanted) {
-        if (kThird && wanted) {
-            if (!wait_warp(w, ctl->third_ready, it & 1)) return false;
-            tc_fence_after();
-        }
-        if (elect_one()) {
-            if (kThird && wanted) issue_state(low_at, slot_of(nv), true);
-            mma_commit(smem_u32(&ctl->kv_done));
-            mma_commit(smem_u32(&ctl->empty[nk % kMixSlots]));
-            mma_commit(smem_u32(&ctl->empty[nv % kMixSlots]));
-        }
-        __syncwarp();
-        return true;
-    };
-    auto multiply_totals = [&]() {
-        for (uint32_t i = 0; i < before; ++i) {
-            const uint32_t nk = 2 * i, nv = nk + 1;
-            if (!full_warp(nk) || !full_warp(nv) || !wait_warp(w, ctl->x_ready, i & 1)) return;
-            if (!state_two(i, slot_of(nk), slot_of(nv), true, i > 0) || !state_rest(i, nk, nv, true)) return;
-        }
-    };
-    auto multiply = [&]() {
-        auto scores = [&](uint32_t i) {
-            const uint32_t nk = tile0 + 3 * i, nq = nk + 1;
-            if (!full_warp(nk) || !full_warp(nq)) return false;
-            // the last group's P has been multiplied (D = 64: and its O, which lies in S, has been read)
-            if (i > 0 && !wait_warp(w, D == 64 ? ctl->o_free : ctl->o_done, (i - 1) & 1)) return false;
+    }
+    // scores of group i, then O of the group
+    static __device__ __noinline__ void scores() {
+        MixCtl *ctl = mix_ctl();
+        const uint32_t n = ctl->count, base = ctl->before, tmem = ctl->tmem_base;
+        const uint32_t short_group = ctl->part.len % kGroup == 0 ? ~0u : (ctl->part.lead ? ctl->part.groups - 1 : 0u) - ctl->part.first;
+        const uint32_t idesc_s = make_idesc(H::kType, kGroup), idesc_o = make_idesc(H::kType, D) | kIdescBMn;
+        uint32_t tile = 2 * base;
+#pragma unroll 1
+        for (uint32_t i = 0; i < n; ++i, tile += 3) {
+            if (!wait_full(ctl, tile) || !wait_full(ctl, tile + 1)) break;
+            if (i > 0) {
+                if (!mix_wait_warp(ctl, ctl->pv_done, (i - 1) & 1)) break;                      // S holds P until it has been multiplied
+                // (the key warps must not miss that the last scores were done)
+                if (!mix_wait_warp(ctl, ctl->k_ready, (base + i - 1) & 1)) break;
+            }
             tc_fence_after();
             if (elect_one()) {
-                const uint64_t qa = make_smem_desc(slot_of(nq)), kb = make_smem_desc(slot_of(nk));
+                const uint64_t qa = make_smem_desc(slot_at(ctl, tile + 1)), kb = make_smem_desc(slot_at(ctl, tile));
 #pragma unroll
                 for (int s = 0; s < D / 16; ++s)
                     mma_issue<false>(tmem + kColS, qa + (s / 4) * (kHalfBytes >> 4) + (s % 4) * 2, kb + (s / 4) * (kHalfBytes >> 4) + (s % 4) * 2, idesc_s, s > 0);
                 mma_commit(smem_u32(&ctl->qk_done));
+                mma_commit(smem_u32(&ctl->empty[tile % kSlots]));
+                mma_commit(smem_u32(&ctl->empty[(tile + 1) % kSlots]));
             }
             __syncwarp();
-            return true;
-        };
-        if (count > 0 && !scores(0)) return;
-        for (uint32_t i = 0; i < count; ++i) {
-            const uint32_t it = before + i;
-            const uint32_t nk = tile0 + 3 * i, nq = nk + 1, nv = nk + 2;
-            const bool fresh = i == 0 && !entered, wanted = i + 1 < count || owns_last;
-            if (!wait_warp(w, ctl->x_ready, it & 1)) return;
-            if (i > 0 && !wait_warp(w, ctl->o_free, (i - 1) & 1)) return;
-            tc_fence_after();
-            if (!fresh && elect_one()) {
-                const uint64_t qa = make_smem_desc(slot_of(nq)), xb = make_smem_desc(x_at);
-#pragma unroll
-                for (int s = 0; s < D / 16; ++s)
-                    mma_issue<false>(tmem + kColE, qa + (s / 4) * (kHalfBytes >> 4) + (s % 4) * 2, xb + (s / 4) * (kXHalf >> 4) + (s % 4) * 2, idesc_d, s > 0);
-            }
-            __syncwarp();
-            if (part.tokens_of(part.first + i) < kGroup && !wait_warp(w, ctl->kt_ready, it & 1)) return;
-            if (!full_warp(nv) || !wait_warp(w, ctl->p_ready, i & 1)) return;
+            if (!wait_full(ctl, tile + 2) || !mix_wait_warp(ctl, ctl->p_ready, i & 1)) break;
+            if (i > 0 && !mix_wait_warp(ctl, ctl->o_free, (i - 1) & 1)) break;
+            if (i == short_group && !mix_wait_warp(ctl, ctl->k_ready, (base + i) & 1)) break;
             tc_fence_after();
             if (elect_one()) {
-                const uint64_t vb = make_smem_desc_mn(slot_of(nv), kHalfBytes);
+                const uint64_t vb = make_smem_desc_mn(slot_at(ctl, tile + 2), kHalfBytes);
 #pragma unroll
                 for (int s = 0; s < kGroup / 16; ++s)
-                    mma_issue_ta(tmem + kColO, tmem + kColS + (s / 4) * kColP1 + (s % 4) * 8, vb + s * (2048 >> 4), idesc_d | kIdescBMn, s > 0);
-                mma_commit(smem_u32(&ctl->o_done));
+                    mma_issue_ta(tmem + kColO, tmem + kColS + (s / 4) * 64 + (s % 4) * 8, vb + s * (2048 >> 4), idesc_o, s > 0);
+                mma_commit(smem_u32(&ctl->pv_done));
+                mma_commit(smem_u32(&ctl->empty[(tile + 2) % kSlots]));
             }
             __syncwarp();
-            // the next scores go before the last term of the state, while the state warps write it; with D = 64 they would
-            // have to wait for the outputs to be read, and the other block of the SM fills the gap
-            if (!state_two(it, slot_of(nk), slot_of(nv), wanted, !fresh)) return;
-            if (D == 128 && i + 1 < count && !scores(i + 1)) return;
-            if (!state_rest(it, nk, nv, wanted)) return;
-            if (D == 64 && i + 1 < count && !scores(i + 1)) return;
         }
-    };
-
-    const uint32_t lanes = tmem + (uint32_t(warp & 3) << 21);       // this warp's 32 lanes (bits 16 and up)
-    const int row = (warp & 3) * 32 + lane;                         // token of the group, or column of v
-    const int part64 = (warp % kWarps) / 4 * 64;                    // this thread's 64 columns of a row (features, or rows of the state)
-    const bool holds_x = (warp & 3) * 32 < D;                       // whole warps: X has D lanes
-    const uint32_t swizzled = uint32_t(row * 128), sw = uint32_t(row & 7);
-
-    // state warps: X <- values
-    auto fill_x = [&](auto value) {
-        if (holds_x) {
+        drain(ctl, 0);
+    }
+    // X^T += V^T K~, one term of K~: lanes are columns of v, columns are rows of the state.  With D = 64 the upper 64 lanes multiply
+    // whatever lies behind the tile; nobody reads them.
+    static __device__ __noinline__ void issue_state(uint32_t tmem, uint32_t v_slot, uint32_t term, bool onto) {
+        const uint32_t idesc = make_idesc(H::kType, D) | kIdescAMn | kIdescBMn;
+        const uint64_t va = make_smem_desc_mn(v_slot, kHalfBytes), ka = make_smem_desc_mn(term, kHalfBytes);
+#pragma unroll
+        for (int s = 0; s < kGroup / 16; ++s) mma_issue<false>(tmem + kColX, va + s * (2048 >> 4), ka + s * (2048 >> 4), idesc, onto || s > 0);
+    }
+    // E of group i, then its part of the state
+    static __device__ __noinline__ void products(uint32_t phase) {
+        MixCtl *ctl = mix_ctl();
+        const uint32_t n = phase ? ctl->count : ctl->before, tmem = ctl->tmem_base;
+        const bool entered = phase && ctl->entered, owns_last = !phase || ctl->owns_last;
+        const uint32_t idesc_e = make_idesc(H::kType, D);
+        const MixPart part = ctl->part;
+        uint32_t it = phase ? ctl->before : 0, tile = 2 * it, thirds = phase ? ctl->thirds : 0;
 #pragma unroll 1
-            for (int c = 0; c < 64; c += 32) {
-                uint32_t v[32];
-#pragma unroll
-                for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(value(part64 + c + j));
-                tmem_st32(lanes + kColX + part64 + c, v);
-            }
-            tmem_st_wait();
-        }
-    };
-    // state warps: use(column, X) for this thread's values
-    auto read_x = [&](auto use) {
-        if (holds_x) {
-#pragma unroll 1
-            for (int c = 0; c < 64; c += 32) {
-                uint32_t v[32];
-                tmem_ld32(lanes + kColX + part64 + c, v);
-                tmem_ld_wait();
-#pragma unroll
-                for (int j = 0; j < 32; ++j) use(part64 + c + j, __uint_as_float(v[j]));
-            }
-        }
-    };
-    // float16 only: powers of two that keep the operands inside the type.  X is held as 2^held X, so that the decayed keys of the
-    // group can be used as 2^held K~ with the largest near 2^14 (small ones would lose their low term below 2^-24).
-    int held = 0;
-    auto pow2 = [](int n) { return __uint_as_float(uint32_t(min(max(n, -126), 127) + 127) << 23); };
-    auto exponent = [](float x) { return int((__float_as_uint(x) >> 23) & 0xFF) - 127; };
-    auto biggest_k = [&](uint32_t k_slot) {
-        float big = 0.0f;
-#pragma unroll
-        for (int c = 0; c < 8; ++c) {
-            uint32_t k4[4];
-            ld_shared_v4(k_slot + (part64 / 64) * kHalfBytes + swizzled + ((c ^ sw) << 4), k4[0], k4[1], k4[2], k4[3]);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float2 x = H::unpack(k4[e]);
-                big = fmaxf(big, fmaxf(fabsf(x.x), fabsf(x.y)));
-            }
-        }
-        return big;
-    };
-    // X rounded into the operand of E, times `shrink`, and X times `keep` left in tensor memory
-    auto step_x = [&](float shrink, float keep, bool operand) {
-        if (holds_x) {
-                const float2 keep2 = make_float2(keep, keep), shrink2 = make_float2(shrink, shrink);
-#pragma unroll 1
-            for (int c = 0; c < 64; c += 32) {
-                uint32_t v[32];
-                tmem_ld32(lanes + kColX + part64 + c, v);
-                tmem_ld_wait();
-                if (operand) {
-#pragma unroll
-                    for (int j = 0; j < 32; j += 8) {
-                        uint32_t w4[4];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            float2 x = make_float2(__uint_as_float(v[j + 2 * e]), __uint_as_float(v[j + 2 * e + 1]));
-                            if (kIsHalf) x = mul2(x, shrink2);
-                            w4[e] = H::pack(x.x, x.y);
-                        }
-                        st_shared_v4(x_at + (part64 / 64) * kXHalf + swizzled + ((((c + j) >> 3) ^ sw) << 4), w4[0], w4[1], w4[2], w4[3]);
-                    }
-                }
-#pragma unroll
-                for (int j = 0; j < 32; j += 2) {
-                    const float2 x = mul2(make_float2(__uint_as_float(v[j]), __uint_as_float(v[j + 1])), keep2);
-                    v[j] = __float_as_uint(x.x);
-                    v[j + 1] = __float_as_uint(x.y);
-                }
-                tmem_st32(lanes + kColX + part64 + c, v);
-            }
-            tmem_st_wait();
-        }
-        if (operand) fence_proxy_async_smem();
-        tc_fence_before();
-        mbar_arrive(smem_u32(&ctl->x_ready));
-    };
-    // K~ in two terms, in the place of K and in the buffer of the low terms; with three, the last one in turn takes the place
-    // of the second when that has been multiplied
-    auto step_k = [&](uint32_t it, int tokens, uint32_t k_slot, uint32_t v_slot, bool wanted) {
-        uint32_t rest[kThird ? 32 : 1];
-        if (wanted) {
-            // walking order: token `row` of the group is j = row forward, tokens - 1 - row backward; a^(tokens - j - lead)
-            const float f = row < tokens ? job.in_scale * ctl->power[part.lead ? tokens - 1 - row : row + 1] * (kIsHalf ? pow2(held) : 1.0f) : 0.0f;
-            const float2 f2 = make_float2(f, f), minus = make_float2(-1.0f, -1.0f);
-#pragma unroll
-            for (int c = 0; c < 8; ++c) {
-                const uint32_t at = (part64 / 64) * kHalfBytes + swizzled + ((c ^ sw) << 4);
-                uint32_t k4[4], hi[4], lo[4];
-                ld_shared_v4(k_slot + at, k4[0], k4[1], k4[2], k4[3]);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if (row >= tokens) k4[e] = 0;
-                    const float2 x = mul2(H::unpack(k4[e]), f2);
-                    hi[e] = H::pack(x.x, x.y);
-                    const float2 y = fma2(H::unpack(hi[e]), minus, x);
-                    lo[e] = H::pack(y.x, y.y);
-                    if (kThird) {
-                        const float2 z = fma2(H::unpack(lo[e]), minus, y);
-                        rest[kThird ? 4 * c + e : 0] = H::pack(z.x, z.y);
-                    }
-                }
-                st_shared_v4(k_slot + at, hi[0], hi[1], hi[2], hi[3]);
-                st_shared_v4(low_at + at, lo[0], lo[1], lo[2], lo[3]);
-            }
-        }
-        if (row >= tokens) {           // what follows the sequence may hold anything: zero times it has to be zero
-#pragma unroll
-            for (int c = 0; c < 8; ++c) st_shared_v4(v_slot + (part64 / 64) * kHalfBytes + swizzled + (c << 4), 0, 0, 0, 0);
-        }
-        fence_proxy_async_smem();
-        mbar_arrive(smem_u32(&ctl->kt_ready));
-        if (kThird && wanted) {
-            if (!wait_warp(w, ctl->two_done, it & 1)) return false;
-#pragma unroll
-            for (int c = 0; c < 8; ++c)
-                st_shared_v4(low_at + (part64 / 64) * kHalfBytes + swizzled + ((c ^ sw) << 4), rest[kThird ? 4 * c : 0], rest[kThird ? 4 * c + 1 : 0],
-                             rest[kThird ? 4 * c + 2 : 0], rest[kThird ? 4 * c + 3 : 0]);
-            fence_proxy_async_smem();
-            mbar_arrive(smem_u32(&ctl->third_ready));
-        }
-        return true;
-    };
-    auto carry = [&](bool outputs) {
-        const uint32_t n = outputs ? count : before;
-        bool ok = true;
-        for (uint32_t i = 0; i < n; ++i) {
-            const uint32_t it = outputs ? before + i : i;
-            const uint32_t nk = outputs ? tile0 + 3 * i : 2 * i, nv = outputs ? nk + 2 : nk + 1;
-            const int tokens = part.tokens_of(part.first + i);
-            const bool fresh = i == 0 && !(outputs && entered);            // X is zero: the first product does not add to it
-            float big_k = 0.0f, shrink = 1.0f, keep = ctl->power[tokens];
-            if (kIsHalf) {
-                ok = ok && __all_sync(0xffffffffu, full(nk));
-                if (ok && row < tokens) big_k = biggest_k(slot_of(nk));
-                __syncwarp();
-            }
-            if (i > 0) {
-                ok = ok && wait_warp(w, ctl->kv_done, (it - 1) & 1);
-                tc_fence_after();
-            }
-            if (kIsHalf) {
-                float big_x = 0.0f;
-                if (ok && !fresh) read_x([&](int, float x) { big_x = fmaxf(big_x, fabsf(x)); });
-#pragma unroll
-                for (int o = 16; o > 0; o >>= 1) {
-                    big_k = fmaxf(big_k, __shfl_xor_sync(0xffffffffu, big_k, o));
-                    big_x = fmaxf(big_x, __shfl_xor_sync(0xffffffffu, big_x, o));
-                }
-                if (lane == 0) {
-                    ctl->biggest[i & 1][warp % kWarps] = big_k;
-                    ctl->biggest[i & 1][kWarps + warp % kWarps] = big_x;
-                }
-                ok = !named_barrier_or(1, kRole, !ok);              // the warps of the role meet here, so they give up together
-                if (ok) {
-#pragma unroll
-                    for (int j = 0; j < kWarps; ++j) {
-                        big_k = fmaxf(big_k, ctl->biggest[i & 1][j]);
-                        big_x = fmaxf(big_x, ctl->biggest[i & 1][kWarps + j]);
-                    }
-                    const int ex = min(max(exponent(big_x), -60), 127);
-                    shrink = pow2(14 - ex);
-                    if (threadIdx.x == kRole) ctl->unscale[i & 1] = pow2(ex - 14 - held);
-                    // the powers of a in K~ go from a^(1 - lead) to a^(tokens - lead)
-                    const float top = fmaxf(ctl->power[1 - job.lead], ctl->power[tokens - int(job.lead)]);
-                    const int now = min(max(14 - exponent(big_k * fabsf(job.in_scale) * top), -30), 100);
-                    keep *= pow2(now - held);
-                    held = now;
-                }
-            }
-            if (!ok) break;
-            if (fresh) mbar_arrive(smem_u32(&ctl->x_ready));
-            else step_x(shrink, keep, outputs);
-            ok = __all_sync(0xffffffffu, full(nk) && (tokens == kGroup || full(nv)));
-            ok = ok && (!outputs || wait_warp(w, ctl->qk_done, i & 1));
-            if (ok) ok = step_k(it, tokens, slot_of(nk), slot_of(nv), !outputs || i + 1 < n || owns_last);
-        }
-        return ok;
-    };
-
-    // token warps
-    auto attend = [&]() {
-        const int row0 = (warp & 3) * 32;
-        for (uint32_t i = 0; i < count; ++i) {
-            const int tokens = part.tokens_of(part.first + i);
-            if (!wait_warp(w, ctl->qk_done, i & 1)) return;
+        for (uint32_t i = 0; i < n; ++i, ++it, tile += phase + 2) {
+            const uint32_t nv = tile + phase + 1;
+            const bool fresh = i == 0 && !entered, wanted = i + 1 < n || owns_last, third = wanted && has_third(ctl, part, part.first + i);
+            if (!mix_wait_warp(ctl, ctl->x_ready, it & 1)) break;
+            if (phase && i > 0 && !mix_wait_warp(ctl, ctl->o_free, (i - 1) & 1)) break;
+            if (phase && !wait_full(ctl, tile + 1)) break;
             tc_fence_after();
-            // scores of 32 tokens at a time: all of them count, none, or (around the diagonal and the end) some
-#pragma unroll 1
-            for (int c = part64; c < (D == 128 ? part64 + 64 : kGroup); c += 32) {
-                const bool all = part.lead ? c + 31 <= row0 : c >= row0 + 31 && c + 31 < tokens;
-                const bool none = part.lead ? c > row0 + 31 : c + 31 < row0 || c >= tokens;
-                uint32_t out[16];
-                if (none) {
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) out[j] = 0;
-                } else {
-                    uint32_t v[32];
-                    tmem_ld32(lanes + kColS + c, v);
-                    tmem_ld_wait();
-                    if (all) {
-                        const float f = ctl->power[part.lead ? row - c - 31 : c - row];
-                        const float2 f2 = make_float2(f, f);
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            const float4 t = reinterpret_cast<const float4 *>(ctl->block)[j];
-                            const float2 x = mul2(make_float2(__uint_as_float(v[4 * j]), __uint_as_float(v[4 * j + 1])), mul2(f2, make_float2(t.x, t.y)));
-                            const float2 y = mul2(make_float2(__uint_as_float(v[4 * j + 2]), __uint_as_float(v[4 * j + 3])), mul2(f2, make_float2(t.z, t.w)));
-                            out[2 * j] = H::pack(x.x, x.y);
-                            out[2 * j + 1] = H::pack(y.x, y.y);
-                        }
-                    } else {
-                        // (what does not count may not be finite: it is left out, not multiplied by zero)
-                        const int apart = part.lead ? row - c : c - row;
-                        const float *factor = ctl->near + 31 + apart;
-                        if (part.lead) {
-#pragma unroll
-                            for (int j = 0; j < 32; ++j) v[j] = apart >= j ? __float_as_uint(__uint_as_float(v[j]) * factor[-j]) : 0u;
-                        } else {
-#pragma unroll
-                            for (int j = 0; j < 32; ++j)
-                                v[j] = apart + j >= 0 && c + j < tokens ? __float_as_uint(__uint_as_float(v[j]) * factor[j]) : 0u;
-                        }
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) out[j] = H::pack(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1]));
-                    }
-                }
-                tmem_st16(lanes + kColS + (c / 64) * kColP1 + (c % 64) / 2, out);         // never over scores still to be read
-            }
-            tmem_st_wait();
-            tc_fence_before();
-            mbar_arrive(smem_u32(&ctl->p_ready));
-
-            if (!wait_warp(w, ctl->o_done, i & 1) || !wait_warp(w, ctl->x_ready, (before + i) & 1)) return;
-            tc_fence_after();
-            const bool fresh = i == 0 && !entered;                 // no state: E was not formed
-            const uint32_t slot = slot_of(tile0 + 3 * i + 1) + (part64 / 64) * kHalfBytes;
-            const int order = part.lead ? row : tokens - 1 - row;
-            float e = order >= 0 ? job.out_scale * ctl->power[order + int(job.lead)] : 0.0f;
-            if (kIsHalf) e *= ctl->unscale[i & 1];
-            const float2 e2 = make_float2(e, e);
-            const int64_t token = t0 + int64_t(part.in_time(part.first + i)) * kGroup + row;
-            T *to = reinterpret_cast<T *>(job.o) + bz * job.o_batch + token * job.o_token + int64_t(h) * job.o_head;
-#pragma unroll 1
-            for (int c = 0; c < 64; c += 32) {
-                uint32_t vo[32], ve[32];
-                tmem_ld32(lanes + kColO + part64 + c, vo);
-                if (!fresh) tmem_ld32(lanes + kColE + part64 + c, ve);
-                tmem_ld_wait();
+            if (phase && elect_one()) {
                 if (!fresh) {
+                    const uint64_t qa = make_smem_desc(slot_at(ctl, tile + 1)), xb = make_smem_desc(x_at(ctl));
 #pragma unroll
-                    for (int j = 0; j < 32; j += 2) {
-                        const float2 x = fma2(e2, make_float2(__uint_as_float(ve[j]), __uint_as_float(ve[j + 1])), make_float2(__uint_as_float(vo[j]), __uint_as_float(vo[j + 1])));
-                        vo[j] = __float_as_uint(x.x);
-                        vo[j + 1] = __float_as_uint(x.y);
-                    }
+                    for (int s = 0; s < D / 16; ++s)
+                        mma_issue<false>(tmem + kColE, qa + (s / 4) * (kHalfBytes >> 4) + (s % 4) * 2, xb + (s / 4) * (kXHalf >> 4) + (s % 4) * 2, idesc_e, s > 0);
                 }
-                uint32_t out[16];
-#pragma unroll
-                for (int j = 0; j < 16; ++j) out[j] = H::pack(__uint_as_float(vo[2 * j]), __uint_as_float(vo[2 * j + 1]));
-                if (tokens == kGroup) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        st_shared_v4(slot + swizzled + (((c / 8 + j) ^ sw) << 4), out[4 * j], out[4 * j + 1], out[4 * j + 2], out[4 * j + 3]);
-                } else if (row < tokens) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int col = part64 + c + 8 * j;
-                        if (uint32_t(col + 8) <= job.dv) {
-                            st_global_v4(to + col, out[4 * j], out[4 * j + 1], out[4 * j + 2], out[4 * j + 3]);
-                        } else {
-                            const T *x = reinterpret_cast<const T *>(out + 4 * j);
-#pragma unroll
-                            for (int k = 0; k < 8; ++k)
-                                if (uint32_t(col + k) < job.dv) to[col + k] = x[k];
-                        }
-                    }
+                mma_commit(smem_u32(&ctl->e_done));
+                mma_commit(smem_u32(&ctl->empty[(tile + 1) % kSlots]));
+            }
+            __syncwarp();
+            if (!wait_full(ctl, nv) || !mix_wait_warp(ctl, ctl->k_ready, it & 1)) break;
+            tc_fence_after();
+            if (elect_one()) {
+                if (wanted) {
+                    issue_state(tmem, slot_at(ctl, nv), slot_at(ctl, tile), !fresh);
+                    if (third) mma_commit(smem_u32(&ctl->first_done));
+                    issue_state(tmem, slot_at(ctl, nv), low_at(ctl), true);
                 }
             }
-            tc_fence_before();
-            mbar_arrive(smem_u32(&ctl->o_free));
-            if (tokens == kGroup) fence_proxy_async_smem();
-            mbar_arrive(smem_u32(&ctl->o_staged));
-        }
-    };
-    auto store = [&]() {
-        for (uint32_t i = 0; i < count; ++i) {
-            if (!w.wait(ctl->o_staged, i & 1)) break;
-            const uint32_t n = tile0 + 3 * i + 1;
-            if (part.tokens_of(part.first + i) == kGroup) {
-                const int token = int(t0 + int64_t(part.in_time(part.first + i)) * kGroup);
-                for (int half = 0; half < D / 64; ++half)
-                    if (uint32_t(half * 64) < job.dv) tma_store_4d(&p.map[job.map[3]], slot_of(n) + half * kHalfBytes, half * 64, token, int(h), bz);
-                bulk_commit();
-                bulk_wait_read();
-            }
-            mbar_arrive(smem_u32(&ctl->empty[n % kMixSlots]));
-        }
-        bulk_wait_all();
-    };
-
-    auto init_at = [&](int c) -> float {
-        if (!job.init || uint32_t(c) >= job.dk || uint32_t(row) >= job.dv) return 0.0f;
-        return job.init[uint64_t(unit) * job.dk * job.dv + uint64_t(c) * job.init_k + uint64_t(row) * job.init_v];
-    };
-    const bool token_role = warp < kWarps, state_role = warp >= kWarps && warp < 2 * kWarps;
-
-    // ---- the first phase of a split walk: what this part leaves from a state of zero, and the states that enter the parts
-    if (split) {
-        if (warp == 2 * kWarps && lane == 0) produce(tile0);
-        if (warp == 2 * kWarps + 1) multiply_totals();
-        if (state_role && totals) {
-            if (carry(false) && wait_warp(w, ctl->kv_done, (before - 1) & 1)) {
+            __syncwarp();
+            if (third) {
+                if (!mix_wait_warp(ctl, ctl->third_ready, thirds & 1)) break;
                 tc_fence_after();
-                read_x([&](int c, float x) { exchange[c * D + row] = x * (kIsHalf ? pow2(-held) : 1.0f); });
+                ++thirds;
             }
-        }
-        held = 0;
-        __syncwarp();
-        cluster_sync_all();
-        if (threadIdx.x < 256) {
-            // element e of every part's total; the state that enters part r takes its place
-            const uint32_t slice = D * D / p.ranks;
-            for (uint32_t e = rank * slice + threadIdx.x; e < (rank + 1) * slice; e += 256) {
-                const uint32_t c = e / D, r = e % D;
-                float run = 0.0f;
-                if (job.init && c < job.dk && r < job.dv)
-                    run = job.init[uint64_t(unit) * job.dk * job.dv + uint64_t(c) * job.init_k + uint64_t(r) * job.init_v];
-                float total[8];
-#pragma unroll
-                for (uint32_t s = 0; s < 8; ++s)
-                    if (s < p.ranks && (s + 1) * part.per < part.groups) total[s] = ld_cluster_f32(cluster_map(smem_u32(exchange + e), s));
-#pragma unroll
-                for (uint32_t s = 0; s < 8; ++s) {
-                    if (s >= p.ranks || s * part.per >= part.groups) break;
-                    st_cluster_f32(cluster_map(smem_u32(exchange + e), s), run);
-                    if ((s + 1) * part.per < part.groups) run = fmaf(exp2f(log2a * part.tokens_of_rank(s)), run, total[s]);
+            if (elect_one()) {
+                if (third) issue_state(tmem, slot_at(ctl, nv), slot_at(ctl, tile), true);
+                mma_commit(smem_u32(&ctl->kv_done));
+                mma_commit(smem_u32(&ctl->empty[tile % kSlots]));
+                mma_commit(smem_u32(&ctl->empty[nv % kSlots]));
+                if (!phase) {                       // (nobody else uses them)
+                    mma_commit(smem_u32(&ctl->empty[tile % kSlots]));
+                    mma_commit(smem_u32(&ctl->empty[nv % kSlots]));
                 }
             }
+            __syncwarp();
         }
-        cluster_sync_all();
-        if (state_role) {
-            if (count > 0 && entered) fill_x([&](int c) { return exchange[c * D + row]; });
-            else if (count == 0 && owns_last) fill_x(init_at);
-        }
-        fence_proxy_async_smem();                       // the next writes to the exchange buffer are TMA loads
-        tc_fence_before();
-        __syncthreads();
-        tc_fence_after();
-    } else if (state_role && (entered || count == 0)) {
-        fill_x(init_at);
+        drain(ctl, 1);
     }
 
-    // ---- the walk
-    if (token_role) {
-        attend();
-    } else if (state_role) {
-        const bool ok = carry(true);
-        if (owns_last && (count == 0 || (ok && wait_warp(w, ctl->kv_done, (before + count - 1) & 1)))) {
-            tc_fence_after();
-            float *to = job.last + uint64_t(unit) * job.dk * job.dv + row;
-            read_x([&](int c, float x) {
-                if (uint32_t(c) < job.dk && uint32_t(row) < job.dv) to[uint64_t(c) * job.dv] = x * (kIsHalf ? pow2(-held) : 1.0f);
-            });
+    // ---- between the phases, all threads of the cluster: element e of every part's total, in walking order; the state that enters a
+    // part takes the place of its total
+    static __device__ __noinline__ void exchange(uint32_t ranks, uint32_t rank) {
+        MixCtl *ctl = mix_ctl();
+        __syncwarp();
+        cluster_sync_all();
+        const MixPart part = ctl->part;
+        const uint32_t slice = D * D / ranks, at = smem_u32(ctl) + kMixCtlBytes;
+        const float *init = ctl->job.init ? ctl->job.init + ctl->state_at : nullptr;
+#pragma unroll 1
+        for (uint32_t e = rank * slice + threadIdx.x; e < (rank + 1) * slice; e += kMixThreads) {
+            const uint32_t c = e / D, r = e % D;
+            float run = init && c < ctl->job.dk && r < ctl->job.dv ? init[uint64_t(c) * ctl->job.init_k + uint64_t(r) * ctl->job.init_v] : 0.0f;
+            float total[8];
+#pragma unroll
+            for (uint32_t s = 0; s < 8; ++s)
+                if ((s + 1) * part.per < part.groups) total[s] = ld_cluster_f32(cluster_map(at + 4 * e, s));
+#pragma unroll
+            for (uint32_t s = 0; s < 8; ++s) {
+                if (s >= ranks || s * part.per >= part.groups) break;
+                st_cluster_f32(cluster_map(at + 4 * e, s), run);
+                if ((s + 1) * part.per < part.groups) run = fmaf(ctl->rank_decay[s], run, total[s]);
+            }
         }
-    } else if (warp == 2 * kWarps) {
-        if (lane == 0) {
-            produce(tiles);
-            if (ctl->abort_flag)                        // copies in flight must land before the block may exit
-                for (uint32_t n = issued > kMixSlots ? issued - kMixSlots : 0; n < issued; ++n) {
-                    const uint32_t bar = smem_u32(&ctl->full[n % kMixSlots]);
-                    const long long since = clock64();
-                    while (!mbar_try_wait(bar, (n / kMixSlots) & 1) && clock64() - since < p.spin_limit) {}
-                }
+        cluster_sync_all();
+    }
+};
+
+template <int D, typename T>
+__global__ void __launch_bounds__(kMixThreads, 1) tcu_linattn_mix_kernel(const __grid_constant__ MixParams p) {
+    using M = Mix<D, T>;
+    MixCtl *ctl = mix_ctl();
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = blockIdx.x % p.ranks, work = blockIdx.x / p.ranks, unit = work / p.jobs, b = unit / p.heads, h = unit % p.heads;
+    const MixJob &job = p.job[work % p.jobs];
+    // packed: whatever the offsets hold, no token outside the arrays is touched
+    const int64_t most = int64_t(p.tokens), begin = p.offsets ? min(max(p.offsets[b], int64_t(0)), most) : 0;
+    MixPart part;
+    part.lead = job.lead != 0;
+    part.len = uint32_t(p.offsets ? min(max(p.offsets[b + 1], begin), most) - begin : most);
+    part.groups = (part.len + kGroup - 1) / kGroup;
+    part.per = (part.groups + p.ranks - 1) / p.ranks;
+    part.first = min(rank * part.per, part.groups);
+    part.last = min((rank + 1) * part.per, part.groups);
+    if (threadIdx.x == 0) {
+        const uint32_t count = part.last - part.first;
+        ctl->job = job;
+        ctl->part = part;
+        ctl->t0 = uint32_t(begin);
+        ctl->b = p.offsets ? 0 : b;
+        ctl->h = h;
+        ctl->state_at = uint64_t(unit) * job.dk * job.dv;
+        ctl->count = count;
+        // a split walk has a first phase, over K and V only, in the blocks whose totals later blocks need
+        ctl->before = p.ranks > 1 && part.last < part.groups ? count : 0;
+        ctl->split = p.ranks > 1;
+        ctl->log2_decay = fmaxf(p.log_decay[h] * 1.4426950408889634f, -1e30f);
+        uint32_t lo = part.first, hi = part.first + ctl->before;            // the groups with a third term are the last ones
+        while (lo < hi) {
+            const uint32_t mid = (lo + hi) / 2;
+            if (M::has_third(ctl, part, mid)) hi = mid;
+            else lo = mid + 1;
         }
-    } else if (warp == 2 * kWarps + 1) {
-        multiply();
-        if (ctl->abort_flag && elect_one()) {           // so must products: tensor memory is freed below
-            mma_commit(smem_u32(&ctl->drained));
-            const long long since = clock64();
-            while (!mbar_try_wait(smem_u32(&ctl->drained), 0) && clock64() - since < p.spin_limit) {}
+        ctl->thirds = part.first + ctl->before - lo;
+        ctl->entered = job.init || rank > 0;
+        ctl->owns_last = job.last && (part.groups == 0 ? rank == 0 : (part.last == part.groups && count > 0));
+    }
+    if (warp == kProducerWarp && lane == 0) {
+        for (uint32_t i = 0; i < M::kSlots; ++i) {
+            mbar_init(smem_u32(&ctl->full[i]), 1);
+            mbar_init(smem_u32(&ctl->empty[i]), 2);
         }
-    } else if (lane == 0) {
-        store();
+        for (uint64_t *one : {&ctl->qk_done, &ctl->pv_done, &ctl->e_done, &ctl->k_scaled, &ctl->first_done, &ctl->kv_done, &ctl->drained[0], &ctl->drained[1]}) mbar_init(smem_u32(one), 1);
+        mbar_init(smem_u32(&ctl->p_ready), 32 * kTokenWarps);
+        mbar_init(smem_u32(&ctl->o_free), 32 * kTokenWarps);
+        mbar_init(smem_u32(&ctl->x_ready), 128);
+        mbar_init(smem_u32(&ctl->k_ready), 32 * kKeyWarps);
+        mbar_init(smem_u32(&ctl->third_ready), 32 * kKeyWarps);
+        ctl->abort_flag = 0;
+        fence_barrier_init();
+    }
+    if (warp == kProductWarp) {
+        tmem_alloc(smem_u32(&ctl->tmem_base), M::kColumns);
+        tmem_relinquish();
+    }
+    // decays: a^m = 2^(m log2 a); -inf becomes a value whose multiples are finite, so that a^0 = 1
+    const float log2a = fmaxf(p.log_decay[h] * 1.4426950408889634f, -1e30f);
+    if (threadIdx.x < 32 + kGroup + 32) {
+        const int apart = int(threadIdx.x) - 31;
+        const float power = exp2f(log2a * float(max(apart, 0))), scale = job.in_scale * job.out_scale;
+        ctl->near[part.lead ? 191 - threadIdx.x : threadIdx.x] = apart >= 0 ? scale * power : 0.0f;
+        if (apart >= 0 && apart <= kGroup) ctl->power[apart] = power;
+        if (apart >= 0 && apart < 16) ctl->block[part.lead ? 15 - apart : apart] = scale * power;
+    }
+    if (threadIdx.x >= 256 && threadIdx.x < 264) ctl->rank_decay[threadIdx.x - 256] = exp2f(log2a * part.tokens_of_rank(threadIdx.x - 256));
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+
+#pragma unroll 1
+    for (uint32_t phase = p.ranks > 1 ? 0 : 1; phase < 2; ++phase) {
+        if (phase) {
+            if (warp >= kStateWarp && warp < kProducerWarp) M::enter();
+            if (p.ranks > 1) {
+                fence_proxy_async_smem();                               // the next writes to the exchange buffer are TMA loads
+                tc_fence_before();
+                __syncthreads();
+                tc_fence_after();
+            }
+        }
+        if (warp < kTokenWarps) {
+            if (phase) M::tokens();
+        } else if (warp < kStateWarp) {
+            M::keys(phase);
+        } else if (warp < kProducerWarp) {
+            M::state(phase);
+        } else if (warp == kProducerWarp) {
+            if (lane == 0) M::loads(p.map, phase);
+        } else if (warp == kScoreWarp) {
+            if (phase) M::scores();
+        } else {
+            M::products(phase);
+        }
+        if (!phase) M::exchange(p.ranks, rank);
     }
     __syncwarp();
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    if (warp == 2 * kWarps + 1) tmem_dealloc(tmem, kColumns);
+    if (warp == kProductWarp) tmem_dealloc(ctl->tmem_base, M::kColumns);
+    if (threadIdx.x == 0 && ctl->abort_flag) atomicExch(p.error, 5u);
 }
 
 // ---- single tokens ---------------------------------------------------------------------------------------------------

@@ -117,8 +117,6 @@ int sm_count() {
     return v;
 }
 
-constexpr long long kMixSpinLimit = 2000000000LL;       // cycles: about a second
-
 template <int D, typename T>
 tcu_status_t launch_mix(const MixParams &p, cudaStream_t stream) {
     static std::atomic<int> configured{-1};
@@ -130,7 +128,7 @@ tcu_status_t launch_mix(const MixParams &p, cudaStream_t stream) {
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(p.batch * p.heads * p.jobs * p.ranks);
-    cfg.blockDim = dim3(kMixThreads<D>);
+    cfg.blockDim = dim3(kMixThreads);
     cfg.dynamicSmemBytes = kMixSmemBytes<D>;
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
@@ -143,10 +141,10 @@ tcu_status_t launch_mix(const MixParams &p, cudaStream_t stream) {
 }
 
 // `transposed`: the state that enters is stored as dv x dk.
-MixJob make_job(const uint8_t (&maps)[4], uint32_t dk, uint32_t dv, bool forward, const float *init, bool transposed, float *last, float in_scale,
+MixJob make_job(const uint8_t (&maps)[3], uint32_t dk, uint32_t dv, bool forward, const float *init, bool transposed, float *last, float in_scale,
                 float out_scale) {
     MixJob j = {};
-    for (int i = 0; i < 4; ++i) j.map[i] = maps[i];
+    for (int i = 0; i < 3; ++i) j.map[i] = maps[i];
     j.init = init;
     j.last = last;
     j.init_k = transposed ? 1 : dv;
@@ -159,8 +157,9 @@ MixJob make_job(const uint8_t (&maps)[4], uint32_t dk, uint32_t dv, bool forward
     return j;
 }
 
-// Fills in what all jobs share and launches.  `arrays`: what the jobs' map indexes name.
-tcu_status_t run_mix(const tcu_linattn_t *a, MixParams &p, const tcu_tokens_t *const *arrays, const uint32_t *widths, int count, void *d_ws, cudaStream_t stream) {
+// Fills in what all jobs share and launches.  `arrays`: what the jobs' map indexes name; `outputs`: where each job writes.
+tcu_status_t run_mix(const tcu_linattn_t *a, MixParams &p, const tcu_tokens_t *const *arrays, const uint32_t *widths, int count,
+                     const tcu_tokens_t *const *outputs, void *d_ws, cudaStream_t stream) {
     int dev = 0;                      // (encoding needs a current context, which a thread that has made no CUDA call does not have)
     if (!encode_fn() || cudaGetDevice(&dev) != cudaSuccess || cudaSetDevice(dev) != cudaSuccess) return TCU_ERR_CUDA;
     for (int i = 0; i < count; ++i)
@@ -171,22 +170,22 @@ tcu_status_t run_mix(const tcu_linattn_t *a, MixParams &p, const tcu_tokens_t *c
     p.tokens = a->tokens;
     p.batch = uint32_t(a->batch);
     p.heads = a->heads;
-    p.spin_limit = kMixSpinLimit;
     for (uint32_t j = 0; j < p.jobs; ++j) {
         MixJob &job = p.job[j];
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < 3; ++i) {
             job.by_batch[i] = arrays[job.map[i]]->stride_batch != 0;
             job.by_head[i] = arrays[job.map[i]]->stride_head != 0;
         }
-        const tcu_tokens_t &o = *arrays[job.map[3]];
+        const tcu_tokens_t &o = *outputs[j];
         job.o = o.ptr;
         job.o_batch = o.stride_batch;
         job.o_token = o.stride_token;
         job.o_head = o.stride_head;
+        job.wide_rows = aligned(o.ptr, 32) && (a->d_offsets || o.stride_batch % 16 == 0) && o.stride_token % 16 == 0 && o.stride_head % 16 == 0;
     }
     const bool wide = a->dk > 64 || a->dv > 64;
     // a walk is split over the blocks of a cluster while that leaves every block a few groups and no SM without work
-    const uint64_t sms = uint64_t(sm_count()), units = a->batch * a->heads * p.jobs, room = sms * (wide ? 1 : 2);
+    const uint64_t sms = uint64_t(sm_count()), units = a->batch * a->heads * p.jobs, room = sms;
     const uint64_t groups = ((a->d_offsets ? a->tokens / a->batch : a->tokens) + kGroup - 1) / kGroup;
     p.ranks = 1;
     while (p.ranks < 8 && units * p.ranks * 2 <= room && groups >= p.ranks * 8) p.ranks *= 2;
@@ -225,12 +224,12 @@ tcu_status_t tcu_linattn_forward(const tcu_linattn_t *a, void *d_ws, size_t ws_b
         return TCU_OK;
     }
     if (a->tokens == 0) return copy_state(a->d_state_out, a->d_state_in, size_t(a->batch) * a->heads * a->dk * a->dv * 4, stream);
-    const tcu_tokens_t *arrays[4] = {&a->q, &a->k, &a->v, &a->o};
-    const uint32_t widths[4] = {a->dk, a->dk, a->dv, a->dv};
+    const tcu_tokens_t *arrays[3] = {&a->q, &a->k, &a->v}, *outputs[1] = {&a->o};
+    const uint32_t widths[3] = {a->dk, a->dk, a->dv};
     MixParams p = {};
     p.jobs = 1;
-    p.job[0] = make_job({0, 1, 2, 3}, a->dk, a->dv, true, a->d_state_in, false, a->d_state_out, 1.0f, a->scale);
-    return run_mix(a, p, arrays, widths, 4, d_ws, stream);
+    p.job[0] = make_job({0, 1, 2}, a->dk, a->dv, true, a->d_state_in, false, a->d_state_out, 1.0f, a->scale);
+    return run_mix(a, p, arrays, widths, 3, outputs, d_ws, stream);
 }
 
 tcu_status_t tcu_linattn_backward(const tcu_linattn_t *a, void *d_ws, size_t ws_bytes, cudaStream_t stream) {
@@ -255,15 +254,15 @@ tcu_status_t tcu_linattn_backward(const tcu_linattn_t *a, void *d_ws, size_t ws_
     const size_t state = size_t(a->batch) * a->heads * a->dk * a->dv * 4;
     if (overlaps(a->d_dstate_in, state, a->d_dstate_out, state) || overlaps(a->d_dstate_in, state, a->d_state_in, state)) return TCU_ERR_INVALID_ARG;
     if (a->tokens == 0) return copy_state(a->d_dstate_in, a->d_dstate_out, state, stream);
-    enum { kQ, kK, kV, kDo, kDq, kDk, kDv };
-    const tcu_tokens_t *arrays[7] = {&a->q, &a->k, &a->v, &a->d_o, &a->d_q, &a->d_k, &a->d_v};
-    const uint32_t widths[7] = {a->dk, a->dk, a->dv, a->dv, a->dk, a->dk, a->dv};
+    enum { kQ, kK, kV, kDo };
+    const tcu_tokens_t *arrays[4] = {&a->q, &a->k, &a->v, &a->d_o}, *outputs[3] = {&a->d_q, &a->d_v, &a->d_k};
+    const uint32_t widths[4] = {a->dk, a->dk, a->dv, a->dv};
     MixParams p = {};
     p.jobs = 3;
-    p.job[0] = make_job({kDo, kV, kK, kDq}, a->dv, a->dk, true, a->d_state_in, true, nullptr, 1.0f, a->scale);
-    p.job[1] = make_job({kK, kQ, kDo, kDv}, a->dk, a->dv, false, a->d_dstate_out, false, a->d_dstate_in, a->scale, 1.0f);
-    p.job[2] = make_job({kV, kDo, kQ, kDk}, a->dv, a->dk, false, a->d_dstate_out, true, nullptr, a->scale, 1.0f);
-    return run_mix(a, p, arrays, widths, 7, d_ws, stream);
+    p.job[0] = make_job({kDo, kV, kK}, a->dv, a->dk, true, a->d_state_in, true, nullptr, 1.0f, a->scale);
+    p.job[1] = make_job({kK, kQ, kDo}, a->dk, a->dv, false, a->d_dstate_out, false, a->d_dstate_in, a->scale, 1.0f);
+    p.job[2] = make_job({kV, kDo, kQ}, a->dv, a->dk, false, a->d_dstate_out, true, nullptr, a->scale, 1.0f);
+    return run_mix(a, p, arrays, widths, 4, outputs, d_ws, stream);
 }
 
 tcu_status_t tcu_linattn_step(const tcu_linattn_t *a, cudaStream_t stream) {
