@@ -19,11 +19,13 @@
 //     E = Q X  (X rounded to the 16-bit type),  X^T += V^T K~  with K~ = decayed keys in two 16-bit terms.
 //
 // A block (one job, sequence, head and - in a cluster - part of the walk) runs the groups one after another.  Roles:
-//     tokens    8 warps, thread = half a token: O + decayed E -> global memory, then the next scores -> P
+//     tokens    8 warps, thread = half a token: O + decayed E -> the tile that held Q, then the next scores -> P
 //     keys      8 warps, thread = half a token: K -> the terms of K~, the first in the place of K
 //     state     4 warps, thread = column of v: X out of tensor memory, rounded into the operand of E, times a^L and put back
 //     producer  TMA: K, Q, V of each group into a ring of tiles
 //     issuers   tcgen05.mma: one warp for scores and O, one for E and the state
+//     store     TMA: the outputs (stores of a row a thread, 32 bytes at a time, took 2000 cycles a group, and the load-store unit
+//               from all other roles)
 // What bounds it is not the tensor core (2560 of its cycles a group with D = 128) but the chain from group to group,
 //     X rescaled (and, meanwhile, K~ made) -> E and the products of X (512 cycles each, and 450 until they are known to be done),
 // and the elementwise work, 16 lanes a cycle and scheduler for conversions, permutations and packed arithmetic alike.  Hence the
@@ -67,9 +69,8 @@ struct MixTokens {
 };
 
 struct MixJob {
-    uint8_t map[3];                      // tensor maps of q, k, v
+    uint8_t map[4];                      // tensor maps of q, k, v, o
     uint8_t by_batch[3], by_head[3];     // 0 where the array repeats along that axis
-    uint8_t wide_rows;                   // rows of o start on 32-byte boundaries
     void *o;
     int64_t o_batch, o_token, o_head;    // strides in elements
     const float *init;                   // state that enters the walk, or NULL; (sequence, head) entries of dk * dv values
@@ -81,7 +82,7 @@ struct MixJob {
 };
 
 struct alignas(64) MixParams {
-    CUtensorMap map[4];
+    CUtensorMap map[7];
     MixJob job[3];
     const float *log_decay;
     const int64_t *offsets;
@@ -106,13 +107,15 @@ struct MixPart {
 };
 
 constexpr int kMixMostSlots = 8;
+constexpr int kNear = 160 + 1 + 47;
 struct MixCtl {
-    uint64_t full[kMixMostSlots], empty[kMixMostSlots];      // (a tile is free when both issuers have done with it)
+    uint64_t full[kMixMostSlots], empty[kMixMostSlots];      // (a tile is free when two have done with it: both issuers, or for Q one and the store)
     uint64_t qk_done;                    // S is in tensor memory
     uint64_t p_ready;                    // P is
     uint64_t pv_done;                    // O is (and S is free)
     uint64_t e_done;                     // E is
     uint64_t o_free;                     // O and E have been read
+    uint64_t o_staged;                   // the outputs are in shared memory
     uint64_t x_ready;                    // X rounded into its operand, and multiplied by a^L in tensor memory
     uint64_t k_scaled;                   // float16: the power of two for K~ is known
     uint64_t k_ready;                    // two terms of K~ written (and rows past the end of V cleared)
@@ -134,14 +137,15 @@ struct MixCtl {
     float power[kGroup + 4];             // a^m
     alignas(16) float block[16];         // factors of P along a block of 16 tokens
     float rank_decay[8];                 // a^(tokens of a part)
-    float near[32 + kGroup + 32];        // factors of P by distance, in the order of the columns: the distance falls along a row forward
-                                         // in time (from 160 to -31; below zero, on the wrong side of the diagonal, 0) and grows backward
+    // factors of P by distance, in the order of the columns: the distance falls along a row forward in time (from 160 to -47; below
+    // zero, on the wrong side of the diagonal, 0) and grows backward
+    float near[kNear];
 };
 static_assert(sizeof(MixCtl) <= kMixCtlBytes, "control block too large");
 
 constexpr int kTokenWarps = 8, kKeyWarps = 8, kStateWarp = kTokenWarps + kKeyWarps, kProducerWarp = kStateWarp + 4, kScoreWarp = kProducerWarp + 1,
-              kProductWarp = kScoreWarp + 1;
-constexpr int kMixThreads = 32 * (kProductWarp + 1);
+              kProductWarp = kScoreWarp + 1, kStoreWarp = kProductWarp + 1;
+constexpr int kMixThreads = 32 * (kStoreWarp + 1);
 template <int D> constexpr int kMixSlots = D == 64 ? 8 : 5;                  // tiles in the ring
 template <int D> constexpr int kMixTileBytes = D / 64 * kHalfBytes;
 template <int D> constexpr int kMixSmemBytes = 1024 + kMixCtlBytes + (kMixSlots<D> + 1) * kMixTileBytes<D> + D * D * 2;
@@ -190,7 +194,7 @@ struct Half2 : Half2Of<T> {
     static __device__ __forceinline__ uint32_t bits(P p) { return *reinterpret_cast<const uint32_t *>(&p); }
     static __device__ __forceinline__ uint32_t mul(uint32_t a, uint32_t b) { return bits(__hmul2_rn(as(a), as(b))); }
     static __device__ __forceinline__ uint32_t fma(uint32_t a, uint32_t b, uint32_t c) { return bits(__hfma2(as(a), as(b), as(c))); }
-    static __device__ __forceinline__ uint32_t neg(uint32_t a) { return a ^ 0x80008000u; }
+    static __device__ __forceinline__ uint32_t fms(uint32_t a, uint32_t b, uint32_t c) { return bits(__hfma2(as(a), as(b), __hneg2(as(c)))); }
 };
 
 // Waits for the phase of a barrier; false when the wait was given up, after about a second.
@@ -205,12 +209,9 @@ __device__ __forceinline__ bool mix_wait_warp(MixCtl *ctl, const uint64_t &barri
     return __all_sync(0xffffffffu, mix_wait(ctl, barrier, parity));
 }
 
-// The same for the warps of a role: one of them polls, the others sleep at a named barrier (thirty polling warps took three
-// quarters of the issue slots that they were waiting for).  All get the same answer, so they give up together.
-__device__ __forceinline__ bool mix_gate(MixCtl *ctl, int id, int threads, bool leader, const uint64_t &barrier, uint32_t parity) {
-    bool failed = false;
-    if (leader) failed = !mix_wait_warp(ctl, barrier, parity);
-    return !named_barrier_or(id, threads, failed);
+// The same for all warps of a role that also meet at a named barrier: they get the same answer, so that they give up together.
+__device__ __forceinline__ bool mix_wait_role(MixCtl *ctl, int id, int threads, const uint64_t &barrier, uint32_t parity) {
+    return !named_barrier_or(id, threads, !mix_wait_warp(ctl, barrier, parity));
 }
 
 // A block, as its roles see it.  Each role is a function of its own, called for each of the two phases (a walk that is not split has
@@ -231,7 +232,7 @@ struct Mix {
     static constexpr uint32_t kTile = kMixTileBytes<D>, kSlots = kMixSlots<D>;
     static constexpr uint32_t kAhead = 2;                                // groups ahead of their load that tiles are brought into L2
     static constexpr int kXHalf = D * 128;                               // one 64-wide half of the operand X: D rows of 128 bytes
-    static constexpr int kCols = D / 2, kKeyCols = D / 2;                // features of a token that a thread of the token / key role has
+    static constexpr int kCols = D / 2;                                  // features of a token that a thread of the token and key roles has
     // tensor memory: S, O, E, X.  P takes the place of S: two warps share the 128 columns of a token, and each 64 columns of S
     // leave their P in their own first 32 columns.
     static constexpr uint32_t kColS = 0, kColO = 128, kColE = 256, kColX = 384, kColumns = 512;
@@ -243,9 +244,8 @@ struct Mix {
     static __device__ __forceinline__ uint32_t slot_at(const MixCtl *ctl, uint32_t tile) { return ring_at(ctl) + tile % kSlots * kTile; }
     static __device__ __forceinline__ bool wait_full(MixCtl *ctl, uint32_t tile) { return mix_wait_warp(ctl, ctl->full[tile % kSlots], (tile / kSlots) & 1); }
     // Rows of a tile: token i of the group at i * 128 bytes, 16-byte pieces exchanged by the swizzle (piece ^ (i & 7)).
-    static __device__ __forceinline__ uint32_t piece_at(int row, int feature) {
-        return uint32_t((feature >> 6) * kHalfBytes + row * 128) + (((uint32_t(feature >> 3) & 7) ^ uint32_t(row & 7)) << 4);
-    }
+    // The 16 bytes of feature f = 64 h + 8 c are at h * kHalfBytes + (row_at(row) ^ c << 4).
+    static __device__ __forceinline__ uint32_t row_at(int row) { return uint32_t(row * 128 + ((row & 7) << 4)); }
     static __device__ __forceinline__ float pow2(int n) { return __uint_as_float(uint32_t(min(max(n, -126), 127) + 127) << 23); }
     static __device__ __forceinline__ int exponent(float x) { return int((__float_as_uint(x) >> 23) & 0xFF) - 127; }
 
@@ -257,101 +257,121 @@ struct Mix {
         const uint32_t lanes = ctl->tmem_base + (uint32_t(warp & 3) << 21);        // this warp's 32 lanes (bits 16 and up)
         const MixPart part = ctl->part;
         const uint32_t n = ctl->count;
+        float2 factor[8];                                                          // of P along a block of 16 tokens
+#pragma unroll
+        for (int j = 0; j < 8; ++j) factor[j] = reinterpret_cast<const float2 *>(ctl->block)[j];
+        // this thread's half of the row, in a tile
+        const uint32_t half_at = (D == 128 ? side * kHalfBytes : 0), at_row = row_at(row) ^ (D == 128 ? 0 : side * 64);
+        uint32_t tile = 2 * ctl->before + 1 - 3;                                   // of Q, of group i - 1
         if (n == 0) return;
 #pragma unroll 1
-        for (uint32_t i = 0; i <= n; ++i) {
+        for (uint32_t i = 0; i <= n; ++i, tile += 3) {
             if (i > 0) {
                 const uint32_t g = i - 1;
-                if (!mix_gate(ctl, 1, 32 * kTokenWarps, warp == 0, ctl->pv_done, g & 1)) return;
-                if (!mix_gate(ctl, 1, 32 * kTokenWarps, warp == 0, ctl->e_done, g & 1)) return;
-                tc_fence_after();
-                const bool no_e = g == 0 && !ctl->entered;                  // no state: E was not formed
                 const int tokens = part.tokens_of(part.first + g), order = part.lead ? row : tokens - 1 - row;
-                float e = order >= 0 ? ctl->job.out_scale * ctl->power[order + int(part.lead)] : 0.0f;
+                if (!mix_wait_warp(ctl, ctl->pv_done, g & 1) || !mix_wait_warp(ctl, ctl->e_done, g & 1)) return;
+                tc_fence_after();
+                float e = ctl->job.out_scale * ctl->power[max(order, 0) + int(part.lead)];
                 if (kIsHalf) e *= ctl->unscale[(ctl->before + g) & 1];
-                const float2 e2 = make_float2(e, e);
-                const uint32_t token = ctl->t0 + part.in_time(part.first + g) * kGroup + row;
-                T *to = reinterpret_cast<T *>(ctl->job.o) + ctl->b * ctl->job.o_batch + token * ctl->job.o_token + int64_t(ctl->h) * ctl->job.o_head;
-                const int dv = int(ctl->job.dv), wide_rows = ctl->job.wide_rows;
-#pragma unroll 1
-                for (int c = side * kCols; c < side * kCols + kCols; c += 16) {
-                    uint32_t vo[16], ve[16], out[8];
-                    tmem_ld16(lanes + kColO + c, vo);
-                    if (no_e) {
+                if (g == 0 && !ctl->entered) zero_e(lanes + side * kCols);          // no state: E was not formed
+                if (tokens == kGroup) {
+                    const uint32_t at = slot_at(ctl, tile) + half_at;
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) ve[j] = 0;
-                    } else {
-                        tmem_ld16(lanes + kColE + c, ve);
+                    for (int c = 0; c < kCols; c += 16) {
+                        uint32_t out[8];
+                        outputs(lanes + side * kCols + c, e, out);
+                        st_shared_v4(at + (at_row ^ (2 * c)), out[0], out[1], out[2], out[3]);
+                        st_shared_v4(at + (at_row ^ (2 * c + 16)), out[4], out[5], out[6], out[7]);
                     }
-                    tmem_ld_wait();
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float2 x = fma2(e2, make_float2(__uint_as_float(ve[2 * j]), __uint_as_float(ve[2 * j + 1])),
-                                              make_float2(__uint_as_float(vo[2 * j]), __uint_as_float(vo[2 * j + 1])));
-                        out[j] = H::pack(x.x, x.y);
-                    }
-                    const int width = row < tokens ? dv - c : 0;            // features to write from here on
-                    if (wide_rows && width >= 16) {
-                        st_global_v8(to + c, out);
-                    } else {
-                        if (width >= 8) st_global_v4(to + c, out[0], out[1], out[2], out[3]);
-                        if (width >= 16) st_global_v4(to + c + 8, out[4], out[5], out[6], out[7]);
-                        else if (width > 0 && (width & 7)) {
-                            uint32_t tail[4];
-#pragma unroll
-                            for (int k = 0; k < 4; ++k) tail[k] = width < 8 ? out[k] : out[4 + k];
-#pragma unroll
-                            for (int k = 0; k < 7; ++k)
-                                if (k < (width & 7)) to[c + (width & 8) + k] = reinterpret_cast<const T *>(tail)[k];
-                        }
-                    }
+                    fence_proxy_async_smem();
+                } else {
+                    T *to = reinterpret_cast<T *>(ctl->job.o) + ctl->b * ctl->job.o_batch + int64_t(ctl->h) * ctl->job.o_head +
+                            (ctl->t0 + part.in_time(part.first + g) * kGroup + row) * ctl->job.o_token + side * kCols;
+                    write_some(to, lanes + side * kCols, e, row < tokens ? int(ctl->job.dv) - side * kCols : 0);
                 }
                 tc_fence_before();
                 mbar_arrive(smem_u32(&ctl->o_free));
+                mbar_arrive(smem_u32(&ctl->o_staged));
             }
             if (i < n) {
                 const int tokens = part.tokens_of(part.first + i);
-                if (!mix_gate(ctl, 1, 32 * kTokenWarps, warp == 0, ctl->qk_done, i & 1)) return;
+                if (!mix_wait_warp(ctl, ctl->qk_done, i & 1)) return;
                 tc_fence_after();
                 // scores of 16 tokens at a time: all of them count, none, or (around the diagonal and the end) some
+                const uint32_t at = lanes + kColS + 64 * side;
 #pragma unroll 1
-                for (int c = 64 * side; c < 64 * side + 64; c += 16) {
-                    const bool all = part.lead ? c + 15 <= row0 : c >= row0 + 31 && c + 15 < tokens;
-                    const bool none = part.lead ? c > row0 + 31 : c + 15 < row0 || c >= tokens;
-                    uint32_t out[8];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) out[j] = 0;
-                    if (!none) {
-                        uint32_t v[16];
-                        tmem_ld16(lanes + kColS + c, v);
-                        const float f = all ? ctl->power[part.lead ? row - c - 15 : c - row] : 0.0f;
+                for (int c = 64 * side, k = 0; k < 64; c += 16, k += 16) {
+                    const int apart = part.lead ? row - c : c - row, apart0 = part.lead ? row0 - c : c - row0 - 31;     // tokens apart: of the first column; least of the warp
+                    const bool all = part.lead ? apart0 >= 15 : apart0 >= 0 && c + 15 < tokens;
+                    const bool none = part.lead ? apart0 < -31 : apart0 < -46 || c >= tokens;
+                    uint32_t v[16], out[8];
+                    if (all) {
+                        tmem_ld16(at + k, v);
+                        const float f = ctl->power[part.lead ? apart - 15 : apart];
+                        const float2 f2 = make_float2(f, f);
                         tmem_ld_wait();
-                        if (all) {
-                            const float2 f2 = make_float2(f, f);
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                const float4 t = reinterpret_cast<const float4 *>(ctl->block)[j];
-                                const float2 x = mul2(make_float2(__uint_as_float(v[4 * j]), __uint_as_float(v[4 * j + 1])), mul2(f2, make_float2(t.x, t.y)));
-                                const float2 y = mul2(make_float2(__uint_as_float(v[4 * j + 2]), __uint_as_float(v[4 * j + 3])), mul2(f2, make_float2(t.z, t.w)));
-                                out[2 * j] = H::pack(x.x, x.y);
-                                out[2 * j + 1] = H::pack(y.x, y.y);
-                            }
-                        } else {
+                        for (int j = 0; j < 8; ++j) {
+                            const float2 x = mul2(make_float2(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1])), mul2(f2, factor[j]));
+                            out[j] = H::pack(x.x, x.y);
+                        }
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) out[j] = 0;
+                        if (!none) {
                             // columns lo ... hi count; the others may not be finite: they are left out, not multiplied by zero
-                            const int apart = part.lead ? row - c : c - row, lo = part.lead ? 0 : max(-apart, 0), hi = min(part.lead ? apart : tokens - 1 - c, 15);
+                            tmem_ld16(at + k, v);
+                            const int lo = part.lead ? 0 : max(-apart, 0), hi = min(part.lead ? apart : tokens - 1 - c, 15);
                             const uint32_t counts = hi >= lo ? (0xFFFFFFFFu >> (31 - hi)) & (0xFFFFFFFFu << lo) : 0u;
-                            const float *factor = ctl->near + (part.lead ? 160 - apart : 31 + apart);
+                            const float *near = ctl->near + (part.lead ? 160 - apart : 47 + apart);
+                            tmem_ld_wait();
 #pragma unroll
-                            for (int j = 0; j < 16; ++j) v[j] = counts & (1u << j) ? __float_as_uint(__uint_as_float(v[j]) * factor[j]) : 0u;
+                            for (int j = 0; j < 16; ++j) v[j] = counts & (1u << j) ? __float_as_uint(__uint_as_float(v[j]) * near[j]) : 0u;
 #pragma unroll
                             for (int j = 0; j < 8; ++j) out[j] = H::pack(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1]));
                         }
                     }
-                    tmem_st8(lanes + kColS + 64 * side + (c % 64) / 2, out);          // never over scores still to be read
+                    tmem_st8(at + k / 2, out);                       // never over scores still to be read
                 }
                 tmem_st_wait();
                 tc_fence_before();
                 mbar_arrive(smem_u32(&ctl->p_ready));
+            }
+        }
+    }
+    // 16 features of a token: O + e E
+    static __device__ __forceinline__ void outputs(uint32_t at, float e, uint32_t (&out)[8]) {
+        uint32_t vo[16], ve[16];
+        const float2 e2 = make_float2(e, e);
+        tmem_ld16(at + kColO, vo);
+        tmem_ld16(at + kColE, ve);
+        tmem_ld_wait();
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float2 x = fma2(e2, make_float2(__uint_as_float(ve[2 * j]), __uint_as_float(ve[2 * j + 1])), make_float2(__uint_as_float(vo[2 * j]), __uint_as_float(vo[2 * j + 1])));
+            out[j] = H::pack(x.x, x.y);
+        }
+    }
+    static __device__ __noinline__ void zero_e(uint32_t at) {
+        const uint32_t zero[16] = {};
+#pragma unroll 1
+        for (int c = 0; c < kCols; c += 16) tmem_st16(at + kColE + c, zero);
+        tmem_st_wait();
+    }
+    // the first `width` features (none when it is not positive) of this thread's half of a token
+    static __device__ __noinline__ void write_some(T *to, uint32_t at, float e, int width) {
+#pragma unroll 1
+        for (int c = 0; c < kCols; c += 16, width -= 16) {
+            uint32_t out[8];
+            outputs(at + c, e, out);
+            if (width >= 8) st_global_v4(to + c, out[0], out[1], out[2], out[3]);
+            if (width >= 16) st_global_v4(to + c + 8, out[4], out[5], out[6], out[7]);
+            else if (width > 0) {
+#pragma unroll
+                for (int k = 0; k < 7; ++k) {
+                    const uint32_t word = width < 8 ? out[k / 2] : out[4 + k / 2];
+                    if (k < (width & 7)) reinterpret_cast<uint16_t *>(to)[c + (width & 8) + k] = uint16_t(word >> (16 * (k & 1)));
+                }
             }
         }
     }
@@ -361,29 +381,38 @@ struct Mix {
     static __device__ __noinline__ void keys(uint32_t phase) {
         MixCtl *ctl = mix_ctl();
         const int warp = (threadIdx.x >> 5) - kTokenWarps, lane = threadIdx.x & 31, row = (warp & 3) * 32 + lane;
-        const int at_feature = (warp >> 2) * kKeyCols;                             // this thread's half of the row
+        // this thread's half of the row, in a tile: pieces first ... first + kCols / 8 - 1 of a 64-wide half
+        const uint32_t half_at = (D == 128 ? (warp >> 2) * kHalfBytes : 0), at_row = row_at(row) ^ (D == 128 ? 0 : (warp >> 2) * 64);
         const MixPart part = ctl->part;
         const uint32_t n = phase ? ctl->count : ctl->before;
         const uint32_t made = phase && n > 0 && !ctl->owns_last ? n - 1 : n;       // the last group's are not needed if its state is not
         uint32_t it = phase ? ctl->before : 0, tile = 2 * it;                      // groups before, their tiles
         uint32_t thirds = phase ? ctl->thirds : 0;
-        auto gate = [&](const uint64_t &barrier, uint32_t parity) { return mix_gate(ctl, 2, 32 * kKeyWarps, warp == 0, barrier, parity); };
+        auto gate = [&](const uint64_t &barrier, uint32_t parity) {
+            return kIsHalf ? mix_wait_role(ctl, 2, 32 * kKeyWarps, barrier, parity) : mix_wait_warp(ctl, barrier, parity);
+        };
         auto gate_full = [&](uint32_t tile) { return gate(ctl->full[tile % kSlots], (tile / kSlots) & 1); };
+        // what follows the sequence may hold anything: zero times it has to be zero
+        auto clear = [&](uint32_t slot) {
 #pragma unroll 1
-        for (uint32_t i = 0; i < made; ++i, ++it, tile += phase + 2) {
-            const uint32_t k_slot = slot_at(ctl, tile);
+            for (uint32_t c = 0; c < kCols * 2; c += 16) st_shared_v4(slot + half_at + (at_row ^ c), 0, 0, 0, 0);
+        };
+        const uint32_t low = low_at(ctl) + half_at;
+#pragma unroll 1
+        for (uint32_t i = 0; i < n; ++i, ++it, tile += phase + 2) {
+            const uint32_t k_at = slot_at(ctl, tile) + half_at;
             const int tokens = part.tokens_of(part.first + i);
-            const bool valid = row < tokens;
             // walking order: token `row` of the group is j = row forward, tokens - 1 - row backward; a^(tokens - j - lead)
-            float f = valid ? ctl->job.in_scale * ctl->power[part.lead ? tokens - 1 - row : row + 1] : 0.0f;
-            if (!gate_full(tile)) return;
+            float f = ctl->job.in_scale * ctl->power[part.lead ? max(tokens - 1 - row, 0) : row + 1];
+            if (it > 0 && !gate(ctl->kv_done, (it - 1) & 1)) return;         // the buffer of the second term is free
             if (kIsHalf) {
+                if (!gate_full(tile)) return;
                 float big = 0.0f;
-                if (valid) {
+                if (row < tokens) {
 #pragma unroll 1
-                    for (int c = 0; c < kKeyCols; c += 8) {
+                    for (uint32_t c = 0; c < kCols * 2; c += 16) {
                         uint32_t k4[4];
-                        ld_shared_v4(k_slot + piece_at(row, at_feature + c), k4[0], k4[1], k4[2], k4[3]);
+                        ld_shared_v4(k_at + (at_row ^ c), k4[0], k4[1], k4[2], k4[3]);
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
                             const float2 x = H::unpack(k4[e]);
@@ -402,95 +431,78 @@ struct Mix {
                 const float top = fmaxf(ctl->power[1 - int(part.lead)], ctl->power[tokens - int(part.lead)]);
                 const int scale = min(max(14 - exponent(big * fabsf(ctl->job.in_scale) * top), -30), 100);
                 f *= pow2(scale);
-                // (published when the state warps have read the last one)
-                if (it > 0 && !gate(ctl->kv_done, (it - 1) & 1)) return;
                 if (warp == 0 && lane == 0) {
                     ctl->scale_k[it & 1] = scale;
                     mbar_arrive(smem_u32(&ctl->k_scaled));
                 }
-            } else if (it > 0 && !gate(ctl->kv_done, (it - 1) & 1)) {        // the buffers of the further terms are free
-                return;
             }
             if (phase && !gate(ctl->qk_done, i & 1)) return;                 // K itself has been multiplied
-            if (tokens < kGroup && !gate_full(tile + phase + 1)) return;
-            const bool third = has_third(ctl, part, part.first + i);
-            uint32_t rest[kIsHalf ? 1 : kKeyCols / 2];
-            if (kIsHalf || third) {
-                const float2 f2 = make_float2(f, f), minus = make_float2(-1.0f, -1.0f);
-#pragma unroll
-                for (int c = 0; c < kKeyCols; c += 8) {
-                    const uint32_t at = piece_at(row, at_feature + c);
-                    uint32_t k4[4], hi[4], lo[4];
-                    ld_shared_v4(k_slot + at, k4[0], k4[1], k4[2], k4[3]);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float2 x = mul2(H::unpack(valid ? k4[e] : 0u), f2);
-                        hi[e] = H::pack(x.x, x.y);
-                        const float2 y = fma2(H::unpack(hi[e]), minus, x);
-                        lo[e] = H::pack(y.x, y.y);
-                        if (!kIsHalf) {
-                            const float2 z = fma2(H::unpack(lo[e]), minus, y);
-                            rest[kIsHalf ? 0 : c / 2 + e] = H::pack(z.x, z.y);
-                        }
-                    }
-                    st_shared_v4(k_slot + at, hi[0], hi[1], hi[2], hi[3]);
-                    st_shared_v4(low_at(ctl) + at, lo[0], lo[1], lo[2], lo[3]);
+            if (!phase && !gate_full(tile)) return;
+            if (tokens < kGroup) {
+                if (!gate_full(tile + phase + 1)) return;
+                if (row >= tokens) {
+                    clear(slot_at(ctl, tile + phase + 1));
+                    clear(slot_at(ctl, tile));
                 }
+            }
+            const bool third = has_third(ctl, part, part.first + i);
+            if (i >= made) {                                                 // (not made)
+            } else if (kIsHalf) {
+#pragma unroll 2
+                for (uint32_t c = 0; c < kCols * 2; c += 16) split<false>(k_at + (at_row ^ c), low + (at_row ^ c), f, nullptr);
+            } else if (third) {
+                uint32_t rest[kCols / 2];
+#pragma unroll
+                for (uint32_t c = 0; c < kCols * 2; c += 16) split<true>(k_at + (at_row ^ c), low + (at_row ^ c), f, rest + c / 4);
+                fence_proxy_async_smem();
+                mbar_arrive(smem_u32(&ctl->k_ready));
+                if (!gate(ctl->first_done, thirds & 1)) return;
+                ++thirds;
+#pragma unroll
+                for (uint32_t c = 0; c < kCols * 2; c += 16) st_shared_v4(k_at + (at_row ^ c), rest[c / 4], rest[c / 4 + 1], rest[c / 4 + 2], rest[c / 4 + 3]);
+                fence_proxy_async_smem();
+                mbar_arrive(smem_u32(&ctl->third_ready));
+                continue;
             } else {
                 // packed arithmetic: with f = f1 + f2 in two terms, hi = k f1 rounded, its error k f1 - hi exactly (a product of two
                 // 8-bit mantissas has 16 bits), and lo = k f2 + that, rounded
                 const uint32_t f1 = H::pack(f, f), f2 = H::pack(f - H::unpack(f1).x, f - H::unpack(f1).x);
-#pragma unroll 2
-                for (int c = 0; c < kKeyCols; c += 8) {
-                    const uint32_t at = piece_at(row, at_feature + c);
+#pragma unroll 4
+                for (uint32_t c = 0; c < kCols * 2; c += 16) {
                     uint32_t k4[4], hi[4], lo[4];
-                    ld_shared_v4(k_slot + at, k4[0], k4[1], k4[2], k4[3]);
+                    ld_shared_v4(k_at + (at_row ^ c), k4[0], k4[1], k4[2], k4[3]);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const uint32_t k = valid ? k4[e] : 0u;
-                        hi[e] = H::mul(k, f1);
-                        lo[e] = H::fma(k, f2, H::fma(k, f1, H::neg(hi[e])));
+                        hi[e] = H::mul(k4[e], f1);
+                        lo[e] = H::fma(k4[e], f2, H::fms(k4[e], f1, hi[e]));
                     }
-                    st_shared_v4(k_slot + at, hi[0], hi[1], hi[2], hi[3]);
-                    st_shared_v4(low_at(ctl) + at, lo[0], lo[1], lo[2], lo[3]);
+                    st_shared_v4(k_at + (at_row ^ c), hi[0], hi[1], hi[2], hi[3]);
+                    st_shared_v4(low + (at_row ^ c), lo[0], lo[1], lo[2], lo[3]);
                 }
-            }
-            if (!valid) clear_v(row, tile + phase + 1, at_feature);
-            fence_proxy_async_smem();
-            mbar_arrive(smem_u32(&ctl->k_ready));
-            if (!kIsHalf && third) {
-                if (!gate(ctl->first_done, thirds & 1)) return;
-#pragma unroll
-                for (int c = 0; c < kKeyCols; c += 8)
-                    st_shared_v4(k_slot + piece_at(row, at_feature + c), rest[kIsHalf ? 0 : c / 2], rest[kIsHalf ? 0 : c / 2 + 1], rest[kIsHalf ? 0 : c / 2 + 2],
-                                 rest[kIsHalf ? 0 : c / 2 + 3]);
-                fence_proxy_async_smem();
-                mbar_arrive(smem_u32(&ctl->third_ready));
-                ++thirds;
-            }
-        }
-        if (made < n) {
-            const int tokens = part.tokens_of(part.first + made);
-            // (the issuers have to see every phase of k_ready: not before they have come this far)
-            if (it > 0 && !gate(ctl->kv_done, (it - 1) & 1)) return;
-            if (kIsHalf && warp == 0 && lane == 0) {
-                ctl->scale_k[it & 1] = 0;
-                mbar_arrive(smem_u32(&ctl->k_scaled));
-            }
-            if (!gate(ctl->qk_done, made & 1)) return;
-            if (tokens < kGroup) {
-                if (!gate_full(tile + 2)) return;
-                if (row >= tokens) clear_v(row, tile + 2, at_feature);
             }
             fence_proxy_async_smem();
             mbar_arrive(smem_u32(&ctl->k_ready));
         }
     }
-    // what follows the sequence may hold anything: zero times it has to be zero
-    static __device__ __noinline__ void clear_v(int row, uint32_t tile, int at_feature) {
-        MixCtl *ctl = mix_ctl();
-#pragma unroll 1
-        for (int c = 0; c < kKeyCols; c += 8) st_shared_v4(slot_at(ctl, tile) + piece_at(row, at_feature + c), 0, 0, 0, 0);
+    // eight keys times f, in 32 bits, as two terms or three
+    template <bool THIRD>
+    static __device__ __forceinline__ void split(uint32_t first, uint32_t second, float f, uint32_t *third) {
+        uint32_t k4[4], hi[4], lo[4];
+        const float2 f2 = make_float2(f, f), minus = make_float2(-1.0f, -1.0f);
+        ld_shared_v4(first, k4[0], k4[1], k4[2], k4[3]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float2 x = mul2(H::unpack(k4[e]), f2);
+            hi[e] = H::pack(x.x, x.y);
+            const float2 y = fma2(H::unpack(hi[e]), minus, x);
+            lo[e] = H::pack(y.x, y.y);
+            if (THIRD) {
+                const float2 z = fma2(H::unpack(lo[e]), minus, y);
+                third[e] = H::pack(z.x, z.y);
+            }
+        }
+        st_shared_v4(first, hi[0], hi[1], hi[2], hi[3]);
+        st_shared_v4(second, lo[0], lo[1], lo[2], lo[3]);
     }
 
     // ---- state: thread = column of v (the first D lanes)
@@ -505,7 +517,9 @@ struct Mix {
         const uint32_t dk = uint32_t(row) < ctl->job.dv ? ctl->job.dk : 0;   // rows of this thread's column in the states of the caller
         float *exchange = reinterpret_cast<float *>(reinterpret_cast<uint8_t *>(ctl) + kMixCtlBytes) + row;
         int held = 0;                                                        // float16: X is held as 2^held X
-        auto gate = [&](const uint64_t &barrier, uint32_t parity) { return mix_gate(ctl, 3, 128, warp == kStateWarp, barrier, parity); };
+        auto gate = [&](const uint64_t &barrier, uint32_t parity) {
+            return kIsHalf ? mix_wait_role(ctl, 3, 128, barrier, parity) : mix_wait_warp(ctl, barrier, parity);
+        };
 #pragma unroll 1
         for (uint32_t i = 0; i < n; ++i) {
             const uint32_t it = base + i;
@@ -542,18 +556,20 @@ struct Mix {
             }
             if (!fresh && holds_x) {
                 const float2 keep2 = make_float2(keep, keep), shrink2 = make_float2(shrink, shrink);
-                auto step = [&](uint32_t (&v)[16], int c) {
+                const uint32_t x_row = x_at(ctl) + row * 128, swizzle = uint32_t(row & 7) << 4;
+                auto step = [&](uint32_t (&v)[16], uint32_t c) {
                     if (phase) {
+                        const uint32_t at = x_row + (c >> 6) * kXHalf;
 #pragma unroll
-                        for (int j = 0; j < 16; j += 8) {
+                        for (uint32_t j = 0; j < 16; j += 8) {
                             uint32_t w4[4];
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) {
+                            for (uint32_t e = 0; e < 4; ++e) {
                                 float2 x = make_float2(__uint_as_float(v[j + 2 * e]), __uint_as_float(v[j + 2 * e + 1]));
                                 if (kIsHalf) x = mul2(x, shrink2);
                                 w4[e] = H::pack(x.x, x.y);
                             }
-                            st_shared_v4(x_at(ctl) + ((c + j) >> 6) * kXHalf + row * 128 + (((uint32_t((c + j) >> 3) & 7) ^ uint32_t(row & 7)) << 4), w4[0], w4[1], w4[2], w4[3]);
+                            st_shared_v4(at + (((c * 2 + j * 2) & 127) ^ swizzle), w4[0], w4[1], w4[2], w4[3]);
                         }
                     }
 #pragma unroll
@@ -567,7 +583,7 @@ struct Mix {
                 uint32_t v0[16], v1[16];                                     // the next columns are on their way while these are worked on
                 tmem_ld16(x_lanes, v0);
 #pragma unroll 1
-                for (int c = 0; c < D; c += 32) {
+                for (uint32_t c = 0; c < D; c += 32) {
                     tmem_ld_wait();
                     tmem_ld16(x_lanes + c + 16, v1);
                     step(v0, c);
@@ -735,7 +751,6 @@ struct Mix {
                         mma_issue<false>(tmem + kColE, qa + (s / 4) * (kHalfBytes >> 4) + (s % 4) * 2, xb + (s / 4) * (kXHalf >> 4) + (s % 4) * 2, idesc_e, s > 0);
                 }
                 mma_commit(smem_u32(&ctl->e_done));
-                mma_commit(smem_u32(&ctl->empty[(tile + 1) % kSlots]));
             }
             __syncwarp();
             if (!wait_full(ctl, nv) || !mix_wait_warp(ctl, ctl->k_ready, it & 1)) break;
@@ -766,6 +781,29 @@ struct Mix {
             __syncwarp();
         }
         drain(ctl, 1);
+    }
+
+    // ---- stores (one thread)
+    static __device__ __noinline__ void stores(const CUtensorMap *maps) {
+        MixCtl *ctl = mix_ctl();
+        const MixPart part = ctl->part;
+        const uint32_t n = ctl->count;
+        uint32_t tile = 2 * ctl->before + 1;
+#pragma unroll 1
+        for (uint32_t i = 0; i < n; ++i, tile += 3) {
+            if (!mix_wait(ctl, ctl->o_staged, i & 1)) break;
+            if (part.tokens_of(part.first + i) == kGroup) {
+#pragma unroll
+                for (int half = 0; half < D / 64; ++half)
+                    if (uint32_t(half * 64) < ctl->job.dv)
+                        tma_store_4d(maps + ctl->job.map[3], slot_at(ctl, tile) + half * kHalfBytes, half * 64, int(ctl->t0 + part.in_time(part.first + i) * kGroup),
+                                     int(ctl->h), int(ctl->b));
+                bulk_commit();
+                bulk_wait_read();
+            }
+            mbar_arrive(smem_u32(&ctl->empty[tile % kSlots]));
+        }
+        bulk_wait_all();
     }
 
     // ---- between the phases, all threads of the cluster: element e of every part's total, in walking order; the state that enters a
@@ -843,6 +881,7 @@ __global__ void __launch_bounds__(kMixThreads, 1) tcu_linattn_mix_kernel(const _
         for (uint64_t *one : {&ctl->qk_done, &ctl->pv_done, &ctl->e_done, &ctl->k_scaled, &ctl->first_done, &ctl->kv_done, &ctl->drained[0], &ctl->drained[1]}) mbar_init(smem_u32(one), 1);
         mbar_init(smem_u32(&ctl->p_ready), 32 * kTokenWarps);
         mbar_init(smem_u32(&ctl->o_free), 32 * kTokenWarps);
+        mbar_init(smem_u32(&ctl->o_staged), 32 * kTokenWarps);
         mbar_init(smem_u32(&ctl->x_ready), 128);
         mbar_init(smem_u32(&ctl->k_ready), 32 * kKeyWarps);
         mbar_init(smem_u32(&ctl->third_ready), 32 * kKeyWarps);
@@ -855,10 +894,10 @@ __global__ void __launch_bounds__(kMixThreads, 1) tcu_linattn_mix_kernel(const _
     }
     // decays: a^m = 2^(m log2 a); -inf becomes a value whose multiples are finite, so that a^0 = 1
     const float log2a = fmaxf(p.log_decay[h] * 1.4426950408889634f, -1e30f);
-    if (threadIdx.x < 32 + kGroup + 32) {
-        const int apart = int(threadIdx.x) - 31;
+    if (threadIdx.x < kNear) {
+        const int apart = int(threadIdx.x) - 47;
         const float power = exp2f(log2a * float(max(apart, 0))), scale = job.in_scale * job.out_scale;
-        ctl->near[part.lead ? 191 - threadIdx.x : threadIdx.x] = apart >= 0 ? scale * power : 0.0f;
+        ctl->near[part.lead ? kNear - 1 - threadIdx.x : threadIdx.x] = apart >= 0 ? scale * power : 0.0f;
         if (apart >= 0 && apart <= kGroup) ctl->power[apart] = power;
         if (apart >= 0 && apart < 16) ctl->block[part.lead ? 15 - apart : apart] = scale * power;
     }
@@ -888,8 +927,10 @@ __global__ void __launch_bounds__(kMixThreads, 1) tcu_linattn_mix_kernel(const _
             if (lane == 0) M::loads(p.map, phase);
         } else if (warp == kScoreWarp) {
             if (phase) M::scores();
-        } else {
+        } else if (warp == kProductWarp) {
             M::products(phase);
+        } else if (phase && lane == 0) {
+            M::stores(p.map);
         }
         if (!phase) M::exchange(p.ranks, rank);
     }

@@ -181,7 +181,8 @@ tcu_status_t run_mix(const tcu_linattn_t *a, MixParams &p, const tcu_tokens_t *c
         job.o_batch = o.stride_batch;
         job.o_token = o.stride_token;
         job.o_head = o.stride_head;
-        job.wide_rows = aligned(o.ptr, 32) && (a->d_offsets || o.stride_batch % 16 == 0) && o.stride_token % 16 == 0 && o.stride_head % 16 == 0;
+        job.map[3] = uint8_t(count + j);
+        if (!encode_tokens(&p.map[count + j], a, o, job.dv)) return TCU_ERR_CUDA;
     }
     const bool wide = a->dk > 64 || a->dv > 64;
     // a walk is split over the blocks of a cluster while that leaves every block a few groups and no SM without work
