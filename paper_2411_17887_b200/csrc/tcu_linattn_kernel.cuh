@@ -319,14 +319,21 @@ struct Mix {
 #pragma unroll
                         for (int j = 0; j < 8; ++j) out[j] = 0;
                         if (!none) {
-                            // columns lo ... hi count; the others may not be finite: they are left out, not multiplied by zero
+                            // what does not count may not be finite: it is left out, not multiplied by its factor of zero
                             tmem_ld16(at + k, v);
-                            const int lo = part.lead ? 0 : max(-apart, 0), hi = min(part.lead ? apart : tokens - 1 - c, 15);
-                            const uint32_t counts = hi >= lo ? (0xFFFFFFFFu >> (31 - hi)) & (0xFFFFFFFFu << lo) : 0u;
+                            const int hi = tokens - c;               // (past the end of a short group the factors are not zero)
                             const float *near = ctl->near + (part.lead ? 160 - apart : 47 + apart);
                             tmem_ld_wait();
 #pragma unroll
-                            for (int j = 0; j < 16; ++j) v[j] = counts & (1u << j) ? __float_as_uint(__uint_as_float(v[j]) * near[j]) : 0u;
+                            for (int j = 0; j < 16; ++j) {
+                                const float f = near[j];
+                                v[j] = f != 0.0f ? __float_as_uint(__uint_as_float(v[j]) * f) : 0u;
+                            }
+                            if (!part.lead && hi < 16) {
+#pragma unroll
+                                for (int j = 0; j < 16; ++j)
+                                    if (j >= hi) v[j] = 0u;
+                            }
 #pragma unroll
                             for (int j = 0; j < 8; ++j) out[j] = H::pack(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1]));
                         }
@@ -397,10 +404,9 @@ struct Mix {
 #pragma unroll 1
             for (uint32_t c = 0; c < kCols * 2; c += 16) st_shared_v4(slot + half_at + (at_row ^ c), 0, 0, 0, 0);
         };
-        const uint32_t low = low_at(ctl) + half_at;
 #pragma unroll 1
         for (uint32_t i = 0; i < n; ++i, ++it, tile += phase + 2) {
-            const uint32_t k_at = slot_at(ctl, tile) + half_at;
+            const uint32_t k_at = slot_at(ctl, tile) + half_at, low = low_at(ctl) + half_at;
             const int tokens = part.tokens_of(part.first + i);
             // walking order: token `row` of the group is j = row forward, tokens - 1 - row backward; a^(tokens - j - lead)
             float f = ctl->job.in_scale * ctl->power[part.lead ? max(tokens - 1 - row, 0) : row + 1];
@@ -739,9 +745,8 @@ struct Mix {
         for (uint32_t i = 0; i < n; ++i, ++it, tile += phase + 2) {
             const uint32_t nv = tile + phase + 1;
             const bool fresh = i == 0 && !entered, wanted = i + 1 < n || owns_last, third = wanted && has_third(ctl, part, part.first + i);
-            if (!mix_wait_warp(ctl, ctl->x_ready, it & 1)) break;
-            if (phase && i > 0 && !mix_wait_warp(ctl, ctl->o_free, (i - 1) & 1)) break;
-            if (phase && !wait_full(ctl, tile + 1)) break;
+            if (phase && (!wait_full(ctl, tile + 1) || (i > 0 && !mix_wait_warp(ctl, ctl->o_free, (i - 1) & 1)))) break;
+            if (!wait_full(ctl, nv) || !mix_wait_warp(ctl, ctl->x_ready, it & 1)) break;
             tc_fence_after();
             if (phase && elect_one()) {
                 if (!fresh) {
@@ -753,7 +758,7 @@ struct Mix {
                 mma_commit(smem_u32(&ctl->e_done));
             }
             __syncwarp();
-            if (!wait_full(ctl, nv) || !mix_wait_warp(ctl, ctl->k_ready, it & 1)) break;
+            if (!mix_wait_warp(ctl, ctl->k_ready, it & 1)) break;
             tc_fence_after();
             if (elect_one()) {
                 if (wanted) {
@@ -813,21 +818,31 @@ struct Mix {
         __syncwarp();
         cluster_sync_all();
         const MixPart part = ctl->part;
-        const uint32_t slice = D * D / ranks, at = smem_u32(ctl) + kMixCtlBytes;
+        const uint32_t slice = D * D / ranks, at = smem_u32(ctl) + kMixCtlBytes, dk = ctl->job.dk, dv = ctl->job.dv;
         const float *init = ctl->job.init ? ctl->job.init + ctl->state_at : nullptr;
 #pragma unroll 1
-        for (uint32_t e = rank * slice + threadIdx.x; e < (rank + 1) * slice; e += kMixThreads) {
+        for (uint32_t e = rank * slice + 4 * threadIdx.x; e < (rank + 1) * slice; e += 4 * kMixThreads) {
             const uint32_t c = e / D, r = e % D;
-            float run = init && c < ctl->job.dk && r < ctl->job.dv ? init[uint64_t(c) * ctl->job.init_k + uint64_t(r) * ctl->job.init_v] : 0.0f;
-            float total[8];
+            float4 run = make_float4(0.0f, 0.0f, 0.0f, 0.0f), total[8];
+            if (init && c < dk) {
+                const float *from = init + uint64_t(c) * ctl->job.init_k;
+                const uint32_t pitch = ctl->job.init_v;
+                if (r < dv) run.x = from[uint64_t(r) * pitch];
+                if (r + 1 < dv) run.y = from[uint64_t(r + 1) * pitch];
+                if (r + 2 < dv) run.z = from[uint64_t(r + 2) * pitch];
+                if (r + 3 < dv) run.w = from[uint64_t(r + 3) * pitch];
+            }
 #pragma unroll
             for (uint32_t s = 0; s < 8; ++s)
-                if ((s + 1) * part.per < part.groups) total[s] = ld_cluster_f32(cluster_map(at + 4 * e, s));
+                if ((s + 1) * part.per < part.groups) total[s] = ld_cluster_f32x4(cluster_map(at + 4 * e, s));
 #pragma unroll
             for (uint32_t s = 0; s < 8; ++s) {
                 if (s >= ranks || s * part.per >= part.groups) break;
-                st_cluster_f32(cluster_map(at + 4 * e, s), run);
-                if ((s + 1) * part.per < part.groups) run = fmaf(ctl->rank_decay[s], run, total[s]);
+                st_cluster_f32x4(cluster_map(at + 4 * e, s), run);
+                if ((s + 1) * part.per < part.groups) {
+                    const float a = ctl->rank_decay[s];
+                    run = make_float4(fmaf(a, run.x, total[s].x), fmaf(a, run.y, total[s].y), fmaf(a, run.z, total[s].z), fmaf(a, run.w, total[s].w));
+                }
             }
         }
         cluster_sync_all();
