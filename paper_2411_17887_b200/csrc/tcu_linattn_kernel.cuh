@@ -818,10 +818,10 @@ struct Mix {
         __syncwarp();
         cluster_sync_all();
         const MixPart part = ctl->part;
-        const uint32_t slice = D * D / ranks, at = smem_u32(ctl) + kMixCtlBytes, dk = ctl->job.dk, dv = ctl->job.dv;
+        const uint32_t at = smem_u32(ctl) + kMixCtlBytes, dk = ctl->job.dk, dv = ctl->job.dv;
         const float *init = ctl->job.init ? ctl->job.init + ctl->state_at : nullptr;
 #pragma unroll 1
-        for (uint32_t e = rank * slice + 4 * threadIdx.x; e < (rank + 1) * slice; e += 4 * kMixThreads) {
+        for (uint32_t e = 4 * (rank * kMixThreads + threadIdx.x); e < D * D; e += 4 * ranks * kMixThreads) {
             const uint32_t c = e / D, r = e % D;
             float4 run = make_float4(0.0f, 0.0f, 0.0f, 0.0f), total[8];
             if (init && c < dk) {

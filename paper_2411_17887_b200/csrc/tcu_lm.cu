@@ -117,26 +117,65 @@ int sm_count() {
     return v;
 }
 
+constexpr uint32_t kMostRanks = 8;       // blocks of a cluster, as far as every device schedules them
+
 template <int D, typename T>
-tcu_status_t launch_mix(const MixParams &p, cudaStream_t stream) {
-    static std::atomic<int> configured{-1};
-    int dev = 0;
-    cudaGetDevice(&dev);
-    if (configured.load() != dev) {
-        if (cudaFuncSetAttribute(tcu_linattn_mix_kernel<D, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMixSmemBytes<D>) != cudaSuccess) return TCU_ERR_CUDA;
-        configured.store(dev);
-    }
+cudaLaunchConfig_t mix_config(uint32_t blocks, uint32_t ranks, cudaLaunchAttribute *attr, cudaStream_t stream) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(p.batch * p.heads * p.jobs * p.ranks);
+    cfg.gridDim = dim3(blocks);
     cfg.blockDim = dim3(kMixThreads);
     cfg.dynamicSmemBytes = kMixSmemBytes<D>;
     cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = p.ranks;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr->id = cudaLaunchAttributeClusterDimension;
+    attr->val.clusterDim.x = ranks;
+    attr->val.clusterDim.y = attr->val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = p.ranks > 1 ? 1 : 0;
+    cfg.numAttrs = ranks > 1 ? 1 : 0;
+    return cfg;
+}
+
+// Into how many parts a walk is split, over the blocks of a cluster, when there are few.  A block fills an SM, and clusters of r
+// blocks fill the SMs worse the larger r is (clusters of 8: 15 at a time, 120 blocks of 148).  In units of a group of the walk,
+// 3.4 us: a group of the first phase takes 0.65, the exchange of states and the second start 3.  `groups` of an average walk.
+// Measured: 16 heads of 8191 tokens at D = 128: 1 rank 204 us, 2 176, 3 123, 4 103, 5 86, 6 75 (taken), 8 119 (two waves); the
+// three walks of 64 heads of 4096 tokens: 1 rank 316 us (taken), 2 387, 4 457.
+template <int D, typename T>
+tcu_status_t choose_ranks(uint64_t units, uint64_t groups, uint32_t *ranks) {
+    static std::atomic<int> configured{-1};
+    static std::atomic<int> at_once[kMostRanks + 1];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return TCU_ERR_CUDA;
+    if (configured.load() != dev) {
+        if (cudaFuncSetAttribute(tcu_linattn_mix_kernel<D, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMixSmemBytes<D>) != cudaSuccess) return TCU_ERR_CUDA;
+        at_once[1] = sm_count();
+        for (uint32_t r = 2; r <= kMostRanks; ++r) {
+            cudaLaunchAttribute attr;
+            const cudaLaunchConfig_t cfg = mix_config<D, T>(r, r, &attr, nullptr);
+            int n = 0;
+            at_once[r] = cudaOccupancyMaxActiveClusters(&n, tcu_linattn_mix_kernel<D, T>, &cfg) == cudaSuccess ? n : 0;
+        }
+        configured.store(dev);
+    }
+    *ranks = 1;
+    double best = 0;
+    for (uint32_t r = 1; r <= kMostRanks && (r == 1 || groups >= 2 * r); ++r) {
+        const uint64_t n = uint64_t(at_once[r].load());
+        if (n == 0) continue;
+        const double cost = double((units + n - 1) / n) * (r == 1 ? double(groups) : 1.65 * double((groups + r - 1) / r) + 3.0);
+        if (r == 1 || cost < best) {
+            best = cost;
+            *ranks = r;
+        }
+    }
+    return TCU_OK;
+}
+
+template <int D, typename T>
+tcu_status_t launch_mix(MixParams &p, uint64_t groups, cudaStream_t stream) {
+    const uint32_t units = p.batch * p.heads * p.jobs;
+    if (tcu_status_t st = choose_ranks<D, T>(units, groups, &p.ranks)) return st;
+    cudaLaunchAttribute attr;
+    const cudaLaunchConfig_t cfg = mix_config<D, T>(units * p.ranks, p.ranks, &attr, stream);
     return cudaLaunchKernelEx(&cfg, tcu_linattn_mix_kernel<D, T>, p) == cudaSuccess ? TCU_OK : TCU_ERR_CUDA;
 }
 
@@ -185,13 +224,9 @@ tcu_status_t run_mix(const tcu_linattn_t *a, MixParams &p, const tcu_tokens_t *c
         if (!encode_tokens(&p.map[count + j], a, o, job.dv)) return TCU_ERR_CUDA;
     }
     const bool wide = a->dk > 64 || a->dv > 64;
-    // a walk is split over the blocks of a cluster while that leaves every block a few groups and no SM without work
-    const uint64_t sms = uint64_t(sm_count()), units = a->batch * a->heads * p.jobs, room = sms;
     const uint64_t groups = ((a->d_offsets ? a->tokens / a->batch : a->tokens) + kGroup - 1) / kGroup;
-    p.ranks = 1;
-    while (p.ranks < 8 && units * p.ranks * 2 <= room && groups >= p.ranks * 8) p.ranks *= 2;
-    if (a->type == TCU_F16) return wide ? launch_mix<128, __half>(p, stream) : launch_mix<64, __half>(p, stream);
-    return wide ? launch_mix<128, __nv_bfloat16>(p, stream) : launch_mix<64, __nv_bfloat16>(p, stream);
+    if (a->type == TCU_F16) return wide ? launch_mix<128, __half>(p, groups, stream) : launch_mix<64, __half>(p, groups, stream);
+    return wide ? launch_mix<128, __nv_bfloat16>(p, groups, stream) : launch_mix<64, __nv_bfloat16>(p, groups, stream);
 }
 
 // No tokens: the state that leaves is the state that enters.

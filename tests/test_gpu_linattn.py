@@ -66,6 +66,19 @@ def test_against_the_definition(shape, dtype, states):
 
 
 @pytest.mark.parametrize("dtype", DTYPES, ids=["bf16", "f16"])
+@pytest.mark.parametrize("shape", [(1, 2040, 2, 24, 40), (1, 2040, 1, 128, 72), (1, 3200, 3, 32, 32), (1, 4300, 16, 16, 24), (2, 1300, 11, 16, 16)], ids=str)
+def test_walks_split_over_blocks(shape, dtype):
+    """Few heads of many tokens: parts of a walk start from the states of the parts before them, in either direction."""
+    b, t, h, dk, dv = shape
+    q, k, v, d_o, decay, s0, d_last = draw(t + h, b, t, h, dk, dv, dtype, True)
+    decay[0] = -1e-3
+    scale = dk ** -0.5
+    o, last = api.linear_attention(q, k, v, decay, initial_state=s0, output_final_state=True)
+    check_forward(q, k, v, decay, scale, s0, o, last)
+    check_backward(q, k, v, decay, scale, s0, d_o, d_last, api.linear_attention_backward(d_o, q, k, v, decay, initial_state=s0, d_final_state=d_last))
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=["bf16", "f16"])
 def test_decays_at_their_ends(dtype):
     """No decay, a decay of a few tokens, one that underflows inside a group of tokens, and no memory at all."""
     q, k, v, d_o, decay, s0, d_last = draw(5, 1, 300, 5, 64, 64, dtype, True)
