@@ -7,6 +7,7 @@
 #include <atomic>
 #include <initializer_list>
 #include <mutex>
+#include <type_traits>
 
 #include "tcu_embedding_kernel.cuh"
 #include "tcu_linattn_kernel.cuh"
@@ -350,23 +351,33 @@ int vec_of(size_t d, size_t stride, size_t eb, std::initializer_list<const void 
 }
 
 template <typename T, typename ID>
-void launch_lookup(int vec, const void *ids, uint64_t n, const void *table, uint32_t rows, size_t d, size_t stride, float scale, void *out,
+void launch_lookup(int vec, const void *ids, uint32_t n, const void *table, uint32_t rows, uint32_t d, size_t stride, float scale, void *out,
                    cudaStream_t stream) {
-    const uint32_t packs = uint32_t(d / vec);
-    const uint64_t total = n * packs, blocks = (total + 255) / 256;
-    const uint32_t grid = uint32_t(blocks < 148 * 64 ? blocks : 148 * 64);
+    const uint32_t packs = d / vec;
+    uint32_t tx = 1;
+    while (tx < packs && tx < 256) tx <<= 1;
+    const bool many = uint64_t(n) * packs >= uint64_t(256) * 148 * 8;          // enough for every SM with several rows a thread
+    const uint32_t rows_each = (many ? 4 : 1) * (256 / tx);
+    const dim3 block(tx, 256 / tx), grid((n + rows_each - 1) / rows_each, (packs + tx - 1) / tx);
     auto go = [&](auto kernel) {
-        kernel<<<grid, 256, 0, stream>>>(static_cast<const ID *>(ids), n, static_cast<const T *>(table), rows, packs, stride, scale, static_cast<T *>(out));
+        kernel<<<grid, block, 0, stream>>>(static_cast<const ID *>(ids), n, static_cast<const T *>(table), rows, d, stride, scale, static_cast<T *>(out));
+    };
+    auto rows_of = [&](auto v) {
+        constexpr int VEC = decltype(v)::value;
+        if (many) go(tcu_embedding_lookup_kernel<T, ID, VEC, 4>);
+        else go(tcu_embedding_lookup_kernel<T, ID, VEC, 1>);
     };
     if constexpr (sizeof(T) == 2) {
-        if (vec == 8) return go(tcu_embedding_lookup_kernel<T, ID, 8>);
+        if (vec == 8) return rows_of(std::integral_constant<int, 8>{});
     }
-    if (vec == 4) return go(tcu_embedding_lookup_kernel<T, ID, 4>);
-    go(tcu_embedding_lookup_kernel<T, ID, 1>);
+    if (vec == 4) return rows_of(std::integral_constant<int, 4>{});
+    rows_of(std::integral_constant<int, 1>{});
 }
 
+bool few_tokens(size_t n, size_t rows, size_t d) { return n <= kFewTokens && (d == 0 || rows <= kFewElements / d); }
+
 struct EmbeddingWs {
-    size_t keys[2], tokens[2], counts, totals, tail, head, bytes;
+    size_t keys[2], tokens[2], counts, totals, starts, joins, join, begins, tail, head, bytes;
     uint32_t tiles, pieces;
 };
 EmbeddingWs embedding_ws(size_t n, size_t rows, size_t d) {
@@ -385,11 +396,32 @@ EmbeddingWs embedding_ws(size_t n, size_t rows, size_t d) {
     }
     w.counts = take(size_t(kDigits) * w.tiles * 4);
     w.totals = take(kDigits * 4);
+    w.starts = take((size_t(w.pieces) + 1) * 8);
+    w.joins = take(4);
+    w.join = take(size_t(w.pieces) * 8);
+    w.begins = take(rows * 4);
     w.tail = take(size_t(w.pieces) * d * 4);
     w.head = take(size_t(w.pieces) * d * 4);
     w.bytes = at;
     return w;
 }
+
+// A kernel that may be set up while the one ahead of it in the stream, of the same sequence, still runs.
+template <typename... P, typename... A>
+void launch_next(void (*kernel)(P...), dim3 grid, dim3 block, cudaStream_t stream, A... args) {
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.stream = stream;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    (void)cudaLaunchKernelEx(&cfg, kernel, P(args)...);        // the caller asks for the error once, at the end
+}
+
+constexpr uint32_t kMostTilesAdded = 128;       // tiles whose counts every block of the sort adds up by itself
 
 template <typename ID>
 void sort_tokens(const void *ids, uint32_t n, uint32_t rows, const EmbeddingWs &w, uint8_t *ws, cudaStream_t stream, int &out) {
@@ -397,13 +429,15 @@ void sort_tokens(const void *ids, uint32_t n, uint32_t rows, const EmbeddingWs &
     while (bits < 32 && (uint64_t(1) << bits) <= rows) ++bits;          // the value `rows` itself must fit
     auto at = [&](size_t o) { return reinterpret_cast<uint32_t *>(ws + o); };
     const uint32_t *keys = nullptr, *tokens = nullptr;
+    const ID *id = static_cast<const ID *>(ids);
     out = 0;
     for (int shift = 0; shift < bits; shift += kDigitBits) {
-        const ID *id = static_cast<const ID *>(ids);
-        tcu_sort_count_kernel<ID><<<w.tiles, kSortThreads, 0, stream>>>(id, keys, n, rows, shift, w.tiles, at(w.counts));
-        tcu_sort_scan_kernel<<<kDigits, kSortThreads, 0, stream>>>(at(w.counts), w.tiles, at(w.totals));
-        tcu_sort_scatter_kernel<ID><<<w.tiles, kSortThreads, 0, stream>>>(id, keys, tokens, n, rows, shift, w.tiles, at(w.counts), at(w.totals),
-                                                                          at(w.keys[out]), at(w.tokens[out]));
+        if (shift == 0) tcu_sort_count_kernel<ID><<<w.tiles, kSortThreads, 0, stream>>>(id, keys, n, rows, shift, at(w.counts), at(w.joins));
+        else launch_next(tcu_sort_count_kernel<ID>, w.tiles, kSortThreads, stream, id, keys, n, rows, shift, at(w.counts), nullptr);
+        const bool scanned = w.tiles > kMostTilesAdded;
+        if (scanned) launch_next(tcu_sort_scan_kernel, kDigits / 32, 1024, stream, at(w.counts), w.tiles, at(w.totals));
+        launch_next(scanned ? tcu_sort_scatter_kernel<ID, true> : tcu_sort_scatter_kernel<ID, false>, w.tiles, kSortThreads, stream, id, keys, tokens, n, rows,
+                    shift, w.tiles, at(w.counts), at(w.totals), at(w.keys[out]), at(w.tokens[out]));
         keys = at(w.keys[out]);
         tokens = at(w.tokens[out]);
         out ^= 1;
@@ -413,20 +447,37 @@ void sort_tokens(const void *ids, uint32_t n, uint32_t rows, const EmbeddingWs &
 
 template <typename T, typename TT>
 void launch_sum(int vec, const void *d_out, void *table, const SumParams &s, cudaStream_t stream) {
-    auto go = [&](auto sum, auto join) {
-        const uint32_t packs = s.d / vec;
-        uint32_t tx = 1;
+    launch_next(tcu_embedding_cut_kernel, s.pieces / 4 + 1, 128, stream, s);
+    auto go = [&](auto v) {
+        constexpr int VEC = decltype(v)::value;
+        const uint32_t packs = s.d / VEC;
+        uint32_t tx = 1;                                        // a group of threads for the columns of a piece
         while (tx < packs && tx < 128) tx <<= 1;
-        const dim3 block(tx, 256 / tx > 0 ? 256 / tx : 1);
-        const dim3 grid((s.pieces + block.y - 1) / block.y, (packs + tx - 1) / tx);
-        sum<<<grid, block, 0, stream>>>(static_cast<const T *>(d_out), static_cast<TT *>(table), s);
-        join<<<grid, block, 0, stream>>>(static_cast<TT *>(table), s);
+        const dim3 block(tx, 128 / tx), grid((s.pieces + block.y - 1) / block.y, (packs + tx - 1) / tx);
+        launch_next(tcu_embedding_sum_kernel<T, TT, VEC>, grid, block, stream, static_cast<const T *>(d_out), static_cast<TT *>(table), s);
+        launch_next(tcu_embedding_join_kernel<TT, VEC < 4 ? VEC : 4>, 148 * 8, 128, stream, static_cast<TT *>(table), s);
     };
     if constexpr (sizeof(T) == 2) {
-        if (vec == 8) return go(tcu_embedding_sum_kernel<T, TT, 8>, tcu_embedding_join_kernel<TT, 8>);
+        if (vec == 8) return go(std::integral_constant<int, 8>{});
     }
-    if (vec == 4) return go(tcu_embedding_sum_kernel<T, TT, 4>, tcu_embedding_join_kernel<TT, 4>);
-    go(tcu_embedding_sum_kernel<T, TT, 1>, tcu_embedding_join_kernel<TT, 1>);
+    if (vec == 4) return go(std::integral_constant<int, 4>{});
+    go(std::integral_constant<int, 1>{});
+}
+
+template <typename T, typename TT, typename ID>
+void launch_few(int vec, const void *d_out, const void *ids, void *table, uint32_t n, uint32_t rows, uint32_t d, float scale, int accumulate, cudaStream_t stream) {
+    const uint32_t cols = (d + kFewCols - 1) / kFewCols;
+    const uint64_t each = (uint64_t(rows) * cols + 148 * 3 - 1) / (148 * 3);       // three blocks an SM, of a row a warp to kFewRows
+    const uint32_t rows_each = uint32_t(each < 8 ? 8 : each < kFewRows ? each : kFewRows);
+    auto go = [&](auto kernel) {
+        kernel<<<dim3((rows + rows_each - 1) / rows_each, cols), 256, 0, stream>>>(static_cast<const T *>(d_out), static_cast<const ID *>(ids), static_cast<TT *>(table), n, rows, d,
+                                                                                   scale, accumulate);
+    };
+    if constexpr (sizeof(T) == 2) {
+        if (vec == 8) return go(tcu_embedding_few_kernel<T, TT, ID, 8>);
+    }
+    if (vec == 4) return go(tcu_embedding_few_kernel<T, TT, ID, 4>);
+    go(tcu_embedding_few_kernel<T, TT, ID, 1>);
 }
 
 }  // namespace
@@ -446,8 +497,8 @@ tcu_status_t tcu_embedding_forward(const void *d_ids, int id_bytes, size_t n, co
     const int vec = vec_of(d, table_stride, eb, {d_table, d_out});
     auto go = [&](auto t) {
         using T = decltype(t);
-        if (id_bytes == 4) launch_lookup<T, int32_t>(vec, d_ids, n, d_table, uint32_t(rows), d, table_stride, scale, d_out, stream);
-        else launch_lookup<T, int64_t>(vec, d_ids, n, d_table, uint32_t(rows), d, table_stride, scale, d_out, stream);
+        if (id_bytes == 4) launch_lookup<T, int32_t>(vec, d_ids, uint32_t(n), d_table, uint32_t(rows), uint32_t(d), table_stride, scale, d_out, stream);
+        else launch_lookup<T, int64_t>(vec, d_ids, uint32_t(n), d_table, uint32_t(rows), uint32_t(d), table_stride, scale, d_out, stream);
     };
     if (type == TCU_F32) go(float{});
     else if (type == TCU_F16) go(__half{});
@@ -457,8 +508,7 @@ tcu_status_t tcu_embedding_forward(const void *d_ids, int id_bytes, size_t n, co
 
 size_t tcu_embedding_workspace_bytes(size_t n, size_t rows, size_t d) {
     if (n > kMostTokens || rows > kMostTokens) return 0;
-    const size_t bytes = embedding_ws(n, rows, d).bytes;
-    return bytes ? bytes : 256;
+    return few_tokens(n, rows, d) ? 256 : embedding_ws(n, rows, d).bytes;
 }
 
 tcu_status_t tcu_embedding_backward(const void *d_out, tcu_float_t type, const void *d_ids, int id_bytes, size_t n, size_t rows, size_t d, float scale,
@@ -477,6 +527,24 @@ tcu_status_t tcu_embedding_backward(const void *d_out, tcu_float_t type, const v
     if (!d_ws || ws_bytes < tcu_embedding_workspace_bytes(n, rows, d)) return TCU_ERR_WORKSPACE;
     if (!aligned(d_ws, 256)) return TCU_ERR_INVALID_ARG;
     if (overlaps(d_table, rows * d * tb, d_out, n * d * eb) || overlaps(d_table, rows * d * tb, d_ids, n * id_bytes)) return TCU_ERR_INVALID_ARG;
+    int vec = vec_of(d, d, eb, {d_out});
+    while (vec > 1 && !aligned(d_table, size_t(vec) * tb)) vec = vec == 8 ? 4 : 1;
+    auto with_types = [&](auto go) {
+        if (type == TCU_F32) go(float{}, float{});
+        else if (type == TCU_F16 && table_type == TCU_F16) go(__half{}, __half{});
+        else if (type == TCU_F16) go(__half{}, float{});
+        else if (table_type == TCU_BF16) go(__nv_bfloat16{}, __nv_bfloat16{});
+        else go(__nv_bfloat16{}, float{});
+    };
+    if (few_tokens(n, rows, d)) {
+        with_types([&](auto t, auto tt) {
+            using T = decltype(t);
+            using TT = decltype(tt);
+            if (id_bytes == 4) launch_few<T, TT, int32_t>(vec, d_out, d_ids, d_table, uint32_t(n), uint32_t(rows), uint32_t(d), scale, accumulate != 0, stream);
+            else launch_few<T, TT, int64_t>(vec, d_out, d_ids, d_table, uint32_t(n), uint32_t(rows), uint32_t(d), scale, accumulate != 0, stream);
+        });
+        return launched();
+    }
     const EmbeddingWs w = embedding_ws(n, rows, d);
     uint8_t *ws = static_cast<uint8_t *>(d_ws);
     int last = 0;
@@ -491,15 +559,13 @@ tcu_status_t tcu_embedding_backward(const void *d_out, tcu_float_t type, const v
     s.accumulate = accumulate != 0;
     s.pieces = uint32_t(((s.accumulate ? 0 : rows) + n + kPiece - 1) / kPiece);
     s.scale = scale;
+    s.joins = reinterpret_cast<uint32_t *>(ws + w.joins);
+    s.starts = reinterpret_cast<uint2 *>(ws + w.starts);
+    s.join = reinterpret_cast<uint2 *>(ws + w.join);
+    s.begins = reinterpret_cast<uint32_t *>(ws + w.begins);
     s.tail = reinterpret_cast<float *>(ws + w.tail);
     s.head = reinterpret_cast<float *>(ws + w.head);
-    int vec = vec_of(d, d, eb, {d_out});
-    while (vec > 1 && !aligned(d_table, size_t(vec) * tb < 16 ? vec * tb : 16)) vec = vec == 8 ? 4 : 1;
-    if (type == TCU_F32) launch_sum<float, float>(vec, d_out, d_table, s, stream);
-    else if (type == TCU_F16 && table_type == TCU_F16) launch_sum<__half, __half>(vec, d_out, d_table, s, stream);
-    else if (type == TCU_F16) launch_sum<__half, float>(vec, d_out, d_table, s, stream);
-    else if (table_type == TCU_BF16) launch_sum<__nv_bfloat16, __nv_bfloat16>(vec, d_out, d_table, s, stream);
-    else launch_sum<__nv_bfloat16, float>(vec, d_out, d_table, s, stream);
+    with_types([&](auto t, auto tt) { launch_sum<decltype(t), decltype(tt)>(vec, d_out, d_table, s, stream); });
     return launched();
 }
 

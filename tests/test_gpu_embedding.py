@@ -88,6 +88,20 @@ def test_table_gradient(kind, n, rows, d, dtype, table_type):
     assert torch.equal(got, api.embedding_backward(d_out, ids, rows, scale=1.3, dtype=table_type))       # the same bits again
 
 
+@pytest.mark.parametrize("dtype,table_type", [(torch.bfloat16, torch.float32), (torch.float16, torch.float16)], ids=str)
+@pytest.mark.parametrize("kind,n,rows,d", [
+    ("uniform", 1024, 4000, 40), ("uniform", 1025, 900, 264), ("skewed", 30, 70000, 240), ("outside", 4097, 511, 33), ("uniform", 8193, 20, 8), ("skewed", 12289, 30000, 136), ("one", 9000, 70000, 1100),
+    ("uniform", 5000, 300000, 4), ("skewed", 270000, 5000, 6), ("outside", 300001, 600, 3)])
+def test_table_gradient_of_many_tokens(kind, n, rows, d, dtype, table_type):
+    """Either side of the tokens that one launch takes; one, two and three passes of the sort; counts added and scanned."""
+    test_table_gradient(kind, n, rows, d, dtype, table_type)
+
+
+@pytest.mark.parametrize("kind,n,rows,d", [("skewed", 9001, 5000, 72), ("one", 6000, 9, 130), ("outside", 5000, 50, 33), ("uniform", 4500, 100000, 16)])
+def test_sums_of_many_tokens_added_to_another(kind, n, rows, d):
+    test_table_gradient_added_to_another(kind, n, rows, d)
+
+
 @pytest.mark.parametrize("kind,n,rows,d", [("skewed", 3000, 500, 64), ("one", 1000, 9, 130), ("outside", 200, 50, 33), ("uniform", 3, 100000, 16)])
 def test_table_gradient_added_to_another(kind, n, rows, d):
     ids = ids_of(kind, n, rows)
