@@ -70,6 +70,8 @@ def segmented_scan(x: torch.Tensor, offsets: torch.Tensor, s: int = 16, exclusiv
 
 # ------------------------------------------------------------------------------------------------ language-model operators
 _FLOAT = {torch.float32: B.TCU_F32, torch.float16: B.TCU_F16, torch.bfloat16: B.TCU_BF16}
+# the handle alone: a torch.cuda.Stream around it costs 3 us, a third of a small call
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 _status = {}          # device index -> (buffer, pointer): where the linear-attention kernels record a wait that ran out
 
 
@@ -79,16 +81,17 @@ def _stream(device: torch.device) -> int:
         raise ValueError(f"a CUDA tensor is needed, not one on {device}")
     if device.index != torch.cuda.current_device():
         raise ValueError(f"tensors are on {device}, the current device is cuda:{torch.cuda.current_device()}")
-    return torch.cuda.current_stream().cuda_stream
+    return _raw_stream(device.index)
 
 
 def _status_ptr(device: torch.device) -> int:
-    if device.index not in _status:
+    held = _status.get(device.index)
+    if held is None:
         buf = torch.zeros(B.tcu_linattn_workspace_bytes() + 256, dtype=torch.uint8, device=device)
         if not torch.cuda.is_current_stream_capturing():
             torch.cuda.current_stream().synchronize()       # other streams may use it next
-        _status[device.index] = (buf, buf.data_ptr() + (-buf.data_ptr()) % 256)
-    return _status[device.index][1]
+        held = _status[device.index] = (buf, buf.data_ptr() + (-buf.data_ptr()) % 256)
+    return held[1]
 
 
 def linear_attention_status(device=None) -> int:
@@ -100,76 +103,91 @@ def linear_attention_status(device=None) -> int:
     return B.tcu_scan_device_status(_status[index][1], torch.cuda.current_stream().cuda_stream)
 
 
-def _check_all(first: torch.Tensor, **others) -> None:
+def _refuse(dtype: torch.dtype, device: torch.device, **others) -> None:
+    """Says which of the arrays is not like the first one."""
     for name, x in others.items():
-        if x.dtype != first.dtype:
-            raise TypeError(f"{name} is {x.dtype}, the first argument {first.dtype}")
-        if x.device != first.device:
-            raise ValueError(f"{name} is on {x.device}, the first argument on {first.device}")
-
-
-def _strides(x: torch.Tensor):
-    """(batch, token, head) strides of (b, t, h, d), or of packed (t, h, d); an extent of one has stride 0."""
-    st = [s if n > 1 else 0 for s, n in zip(x.stride()[:-1], x.shape[:-1])]
-    return st if len(st) == 3 else [0] + st
+        if x.dtype != dtype:
+            raise TypeError(f"{name} is {x.dtype}, the first argument {dtype}")
+        if x.device != device:
+            raise ValueError(f"{name} is on {x.device}, the first argument on {device}")
 
 
 def _tokens(x: torch.Tensor):
-    """The array as the library takes it - features contiguous, pointer and strides multiples of 16 bytes - and its
-    description; an array that is not like that is copied into one that is."""
-    st = _strides(x)
-    if (x.stride(-1) != 1 and x.shape[-1] > 1) or x.data_ptr() % 16 or any(s % 8 for s in st) or (st[1] == 0 and x.shape[-3] > 1):
-        y = _like(x, x.shape[-1])
+    """An array (b, t, h, d), or packed (t, h, d), as the library takes it - features contiguous, pointer and strides multiples
+    of 16 bytes - and its description (pointer, batch, token, head strides; an extent of one has stride 0).  An array that is
+    not like that is copied into one that is."""
+    if x.dim() == 4:
+        b, t, h, d = x.shape
+        sb, st, sh, sd = x.stride()
+    else:
+        b, (t, h, d) = 1, x.shape
+        sb, (st, sh, sd) = 0, x.stride()
+    if b == 1:
+        sb = 0
+    if t == 1:
+        st = 0
+    if h == 1:
+        sh = 0
+    ptr = x.data_ptr()
+    if (sd != 1 and d > 1) or (ptr | 2 * (sb | st | sh)) & 15 or (st == 0 and t > 1):
+        y = _like(x, d)
         y.copy_(x)
-        x, st = y, _strides(y)
-    return x, (x.data_ptr(), *st)
+        return _tokens(y)
+    return x, (ptr, sb, st, sh)
 
 
 def _like(x: torch.Tensor, d: int) -> torch.Tensor:
     """An empty (..., d) array with the leading shape of x whose rows start on 16-byte boundaries."""
     if d % 8 == 0:
-        return torch.empty((*x.shape[:-1], d), dtype=x.dtype, device=x.device)
-    return torch.empty((*x.shape[:-1], d + (-d) % 8), dtype=x.dtype, device=x.device)[..., :d]
+        return x.new_empty((*x.shape[:-1], d))
+    return x.new_empty((*x.shape[:-1], d + (-d) % 8))[..., :d]
+
+
+def _check_decay(log_decay, heads, device) -> None:
+    if log_decay.dtype != torch.float32 or log_decay.shape != (heads,) or log_decay.device != device or not log_decay.is_contiguous():
+        raise ValueError("log_decay: a contiguous float32 tensor of one value for each head, on the device of q")
 
 
 class _Mix:
     """Checked and described arguments of one linear-attention call."""
 
-    def __init__(self, q, k, v, log_decay, scale, offsets, states):
-        _check_all(q, k=k, v=v)
-        if q.dtype not in (torch.float16, torch.bfloat16):
-            raise TypeError(f"linear attention takes float16 or bfloat16, not {q.dtype}")
+    __slots__ = ("head", "decay", "offsets", "state_shape", "log_decay", "dk", "dv", "stream", "status")
+
+    def __init__(self, q, k, v, log_decay, scale, offsets, **states):
+        dtype, device, shape = q.dtype, q.device, q.shape
+        if k.dtype != dtype or v.dtype != dtype or k.device != device or v.device != device:
+            _refuse(dtype, device, k=k, v=v)
+        if dtype not in (torch.float16, torch.bfloat16):
+            raise TypeError(f"linear attention takes float16 or bfloat16, not {dtype}")
         packed = offsets is not None
-        if q.dim() != (3 if packed else 4):
+        if len(shape) != (3 if packed else 4):
             raise ValueError("q is (batch, tokens, heads, dk), or (tokens, heads, dk) with offsets")
-        if k.shape != q.shape or v.shape[:-1] != q.shape[:-1]:
-            raise ValueError(f"shapes do not go together: q {tuple(q.shape)}, k {tuple(k.shape)}, v {tuple(v.shape)}")
-        self.heads, self.dk, self.dv = q.shape[-2], q.shape[-1], v.shape[-1]
-        self.tokens = q.shape[-3]
+        if k.shape != shape or v.shape[:-1] != shape[:-1]:
+            raise ValueError(f"shapes do not go together: q {tuple(shape)}, k {tuple(k.shape)}, v {tuple(v.shape)}")
+        tokens, heads, self.dk = shape[-3:]
+        self.dv = v.shape[-1]
         if packed:
-            if offsets.dtype != torch.int64 or offsets.dim() != 1 or offsets.numel() < 1 or not offsets.is_contiguous() or offsets.device != q.device:
+            if offsets.dtype != torch.int64 or offsets.dim() != 1 or offsets.numel() < 1 or not offsets.is_contiguous() or offsets.device != device:
                 raise ValueError("offsets: a contiguous int64 tensor of batch + 1 values on the device of q")
-            self.batch = offsets.numel() - 1
+            batch = offsets.numel() - 1
         else:
-            self.batch = q.shape[0]
-        if log_decay.shape != (self.heads,) or log_decay.dtype != torch.float32 or log_decay.device != q.device or not log_decay.is_contiguous():
-            raise ValueError("log_decay: a contiguous float32 tensor of one value for each head, on the device of q")
-        self.scale = self.dk ** -0.5 if scale is None else float(scale)
-        self.offsets, self.log_decay, self.first = offsets, log_decay, q
-        self.state_shape = (self.batch, self.heads, self.dk, self.dv)
+            batch = shape[0]
+        _check_decay(log_decay, heads, device)
+        self.state_shape = (batch, heads, self.dk, self.dv)
         for name, s in states.items():
-            if s is not None and (s.shape != self.state_shape or s.dtype != torch.float32 or not s.is_contiguous() or s.device != q.device):
+            if s is not None and (s.shape != self.state_shape or s.dtype != torch.float32 or not s.is_contiguous() or s.device != device):
                 raise ValueError(f"{name}: a contiguous float32 tensor of shape {self.state_shape} on the device of q")
-        self.stream = _stream(q.device)
-        self.status = _status_ptr(q.device)
+        self.head = (_FLOAT[dtype], batch, tokens, heads, self.dk, self.dv, self.dk ** -0.5 if scale is None else float(scale), log_decay.data_ptr())
+        self.offsets = offsets.data_ptr() if packed else 0
+        self.log_decay = log_decay
+        self.stream = _stream(device)
+        self.status = _status_ptr(device)
 
     def new_state(self):
-        return torch.empty(self.state_shape, dtype=torch.float32, device=self.first.device)
+        return self.log_decay.new_empty(self.state_shape)
 
     def args(self, q, k, v, o=B.NO_TOKENS, **more):
-        return B.tcu_linattn_args(_FLOAT[self.first.dtype], self.batch, self.tokens, self.heads, self.dk, self.dv, self.scale,
-                                  self.log_decay.data_ptr(), q, k, v, o, d_offsets=0 if self.offsets is None else self.offsets.data_ptr(),
-                                  **more)
+        return B.tcu_linattn_args(*self.head, q, k, v, o, d_offsets=self.offsets, **more)
 
 
 def _ptr(x) -> int:
@@ -181,11 +199,11 @@ def _out(x: torch.Tensor) -> torch.Tensor:
 
 
 def _attention_forward(q, k, v, log_decay, scale, initial_state, offsets, output_final_state):
-    m = _Mix(q, k, v, log_decay, scale, offsets, {"initial_state": initial_state})
+    m = _Mix(q, k, v, log_decay, scale, offsets, initial_state=initial_state)
     last = m.new_state() if output_final_state else None
     o = _like(v, m.dv)
-    (q, qv), (k, kv), (v, vv) = _tokens(q), _tokens(k), _tokens(v)
-    B.check(B.tcu_linattn_forward(m.args(qv, kv, vv, (o.data_ptr(), *_strides(o)), d_state_in=_ptr(initial_state), d_state_out=_ptr(last)),
+    (q, qv), (k, kv), (v, vv), (_, ov) = _tokens(q), _tokens(k), _tokens(v), _tokens(o)
+    B.check(B.tcu_linattn_forward(m.args(qv, kv, vv, ov, d_state_in=_ptr(initial_state), d_state_out=_ptr(last)),
                                   m.status, 256, m.stream))
     return _out(o), last
 
@@ -193,15 +211,15 @@ def _attention_forward(q, k, v, log_decay, scale, initial_state, offsets, output
 def linear_attention_backward(d_o, q, k, v, log_decay, scale=None, initial_state=None, offsets=None, d_final_state=None):
     """Gradients of :func:`linear_attention` with respect to q, k, v and the initial state (None without one), from the
     gradient of its output and, where it has one, of the final state."""
-    m = _Mix(q, k, v, log_decay, scale, offsets, {"initial_state": initial_state, "d_final_state": d_final_state})
-    _check_all(q, d_o=d_o)
+    m = _Mix(q, k, v, log_decay, scale, offsets, initial_state=initial_state, d_final_state=d_final_state)
+    if d_o.dtype != q.dtype or d_o.device != q.device:
+        _refuse(q.dtype, q.device, d_o=d_o)
     if d_o.shape != v.shape:
         raise ValueError(f"d_o is {tuple(d_o.shape)}, v {tuple(v.shape)}")
     d_first = m.new_state() if initial_state is not None else None
     d_q, d_k, d_v = _like(q, m.dk), _like(k, m.dk), _like(v, m.dv)
     (q, qv), (k, kv), (v, vv), (d_o, ov) = _tokens(q), _tokens(k), _tokens(v), _tokens(d_o)
-    B.check(B.tcu_linattn_backward(m.args(qv, kv, vv, d_o=ov, d_q=(d_q.data_ptr(), *_strides(d_q)), d_k=(d_k.data_ptr(), *_strides(d_k)),
-                                          d_v=(d_v.data_ptr(), *_strides(d_v)), d_state_in=_ptr(initial_state),
+    B.check(B.tcu_linattn_backward(m.args(qv, kv, vv, d_o=ov, d_q=_tokens(d_q)[1], d_k=_tokens(d_k)[1], d_v=_tokens(d_v)[1], d_state_in=_ptr(initial_state),
                                           d_dstate_out=_ptr(d_final_state), d_dstate_in=_ptr(d_first)), m.status, 256, m.stream))
     return _out(d_q), _out(d_k), _out(d_v), d_first
 
@@ -241,25 +259,34 @@ def linear_attention_step(q, k, v, log_decay, state, scale=None, slots=None):
     """One token for each sequence: updates `state` in place and returns o (batch, heads, dv).  q, k (batch, heads, dk),
     v (batch, heads, dv); state (pool, heads, dk, dv) float32; slots: None (sequence b has entry b), or an int32 tensor of
     each sequence's entry, all different; an entry outside the pool marks a sequence to skip (its output is zero)."""
-    _check_all(q, k=k, v=v)
-    if q.dtype not in (torch.float16, torch.bfloat16):
-        raise TypeError(f"linear attention takes float16 or bfloat16, not {q.dtype}")
-    if q.dim() != 3 or k.shape != q.shape or v.shape[:2] != q.shape[:2] or v.dim() != 3:
-        raise ValueError(f"shapes do not go together: q {tuple(q.shape)}, k {tuple(k.shape)}, v {tuple(v.shape)}")
-    batch, heads, dk = q.shape
+    dtype, device, shape = q.dtype, q.device, q.shape
+    if k.dtype != dtype or v.dtype != dtype or k.device != device or v.device != device:
+        _refuse(dtype, device, k=k, v=v)
+    if dtype not in (torch.float16, torch.bfloat16):
+        raise TypeError(f"linear attention takes float16 or bfloat16, not {dtype}")
+    if len(shape) != 3 or k.shape != shape or v.dim() != 3 or v.shape[:2] != shape[:2]:
+        raise ValueError(f"shapes do not go together: q {tuple(shape)}, k {tuple(k.shape)}, v {tuple(v.shape)}")
+    batch, heads, dk = shape
     dv = v.shape[-1]
-    if state.dim() != 4 or state.shape[1:] != (heads, dk, dv) or state.dtype != torch.float32 or not state.is_contiguous() or state.device != q.device:
+    pool = state.shape
+    if len(pool) != 4 or pool[1:] != (heads, dk, dv) or state.dtype != torch.float32 or not state.is_contiguous() or state.device != device:
         raise ValueError(f"state: a contiguous float32 tensor of shape (pool, {heads}, {dk}, {dv}) on the device of q")
-    if log_decay.shape != (heads,) or log_decay.dtype != torch.float32 or log_decay.device != q.device or not log_decay.is_contiguous():
-        raise ValueError("log_decay: a contiguous float32 tensor of one value for each head, on the device of q")
-    if slots is not None and (slots.shape != (batch,) or slots.dtype != torch.int32 or not slots.is_contiguous() or slots.device != q.device):
+    _check_decay(log_decay, heads, device)
+    if slots is not None and (slots.shape != (batch,) or slots.dtype != torch.int32 or not slots.is_contiguous() or slots.device != device):
         raise ValueError("slots: a contiguous int32 tensor of one value for each sequence, on the device of q")
-    q, k, v = (x if x.stride(-1) == 1 or x.shape[-1] == 1 else x.contiguous() for x in (q, k, v))
-    o = torch.empty((batch, heads, dv), dtype=q.dtype, device=q.device)
-    view = lambda x: (x.data_ptr(), x.stride(0), 0, x.stride(1))  # noqa: E731
-    args = B.tcu_linattn_args(_FLOAT[q.dtype], batch, 1, heads, dk, dv, dk ** -0.5 if scale is None else float(scale), log_decay.data_ptr(),
-                              view(q), view(k), view(v), view(o), d_slots=_ptr(slots), pool_slots=state.shape[0], d_state_out=state.data_ptr())
-    B.check(B.tcu_linattn_step(args, _stream(q.device)))
+    o = q.new_empty((batch, heads, dv))
+
+    def view(x):
+        sb, sh, sd = x.stride()
+        if sd != 1 and x.shape[-1] > 1:
+            x = x.contiguous()
+            sb, sh, sd = x.stride()
+        return x, (x.data_ptr(), sb, 0, sh)
+
+    (q, qv), (k, kv), (v, vv) = view(q), view(k), view(v)
+    args = B.tcu_linattn_args(_FLOAT[dtype], batch, 1, heads, dk, dv, dk ** -0.5 if scale is None else float(scale), log_decay.data_ptr(),
+                              qv, kv, vv, (o.data_ptr(), heads * dv, 0, dv), d_slots=_ptr(slots), pool_slots=pool[0], d_state_out=state.data_ptr())
+    B.check(B.tcu_linattn_step(args, _stream(device)))
     return o
 
 
@@ -273,34 +300,38 @@ def embedding_backward(d_out, ids, num_rows, scale=1.0, dtype=torch.float32, out
     """Gradient of :func:`embedding` with respect to its table: (num_rows, d) of `dtype` (float32, or the type of d_out), row v
     the sum of scale * d_out over the tokens with id v, zero where there is none.  With `out` the sums are added to it
     instead (rows without tokens are not touched)."""
-    d_out, ids = d_out.contiguous(), _ids(ids, d_out.device)
+    device, kind = d_out.device, d_out.dtype
+    d_out, ids = d_out.contiguous(), _ids(ids, device)
     d = d_out.shape[-1]
-    if d_out.dtype not in _FLOAT or d_out.shape[:-1] != ids.shape:
-        raise ValueError(f"d_out {tuple(d_out.shape)} {d_out.dtype} does not go with ids {tuple(ids.shape)}")
+    if kind not in _FLOAT or d_out.shape[:-1] != ids.shape:
+        raise ValueError(f"d_out {tuple(d_out.shape)} {kind} does not go with ids {tuple(ids.shape)}")
     table = out
     if out is None:
-        table = torch.empty((num_rows, d), dtype=dtype, device=d_out.device)
-    elif out.shape != (num_rows, d) or not out.is_contiguous() or out.device != d_out.device:
+        table = torch.empty((num_rows, d), dtype=dtype, device=device)
+    elif out.shape != (num_rows, d) or not out.is_contiguous() or out.device != device:
         raise ValueError(f"out: a contiguous tensor of shape ({num_rows}, {d}) on the device of d_out")
-    if table.dtype != torch.float32 and table.dtype != d_out.dtype:
-        raise TypeError(f"the table's gradient is float32 or {d_out.dtype}, not {table.dtype}")
+    if table.dtype != torch.float32 and table.dtype != kind:
+        raise TypeError(f"the table's gradient is float32 or {kind}, not {table.dtype}")
     n = ids.numel()
     ws_bytes = B.tcu_embedding_workspace_bytes(n, num_rows, d)
-    ws = torch.empty(ws_bytes, dtype=torch.uint8, device=d_out.device)
-    B.check(B.tcu_embedding_backward(d_out, _FLOAT[d_out.dtype], ids, ids.element_size(), n, num_rows, d, float(scale), out is not None,
-                                     table, _FLOAT[table.dtype], ws, ws_bytes, _stream(d_out.device)))
+    ws = ids.new_empty((ws_bytes + 7) // 8, dtype=torch.int64) if ws_bytes else None
+    B.check(B.tcu_embedding_backward(d_out, _FLOAT[kind], ids, ids.element_size(), n, num_rows, d, float(scale), out is not None,
+                                     table, _FLOAT[table.dtype], ws, ws_bytes, _stream(device)))
     return table
 
 
 def _embedding_forward(ids, table, scale):
-    if table.dim() != 2 or table.dtype not in _FLOAT:
+    kind, device = table.dtype, table.device
+    if table.dim() != 2 or kind not in _FLOAT:
         raise ValueError("table: (rows, d), float32, float16 or bfloat16")
-    ids = _ids(ids, table.device)
-    if (table.stride(1) != 1 and table.shape[1] > 1) or (table.stride(0) < table.shape[1] and table.shape[0] > 1):
+    ids = _ids(ids, device)
+    rows, d = table.shape
+    pitch, step = table.stride()
+    if (step != 1 and d > 1) or (pitch < d and rows > 1):
         table = table.contiguous()
-    out = torch.empty((*ids.shape, table.shape[1]), dtype=table.dtype, device=table.device)
-    B.check(B.tcu_embedding_forward(ids, ids.element_size(), ids.numel(), table, table.shape[0], table.shape[1], max(table.stride(0), table.shape[1]),
-                                    _FLOAT[table.dtype], float(scale), out, _stream(table.device)))
+        pitch = d
+    out = table.new_empty((*ids.shape, d))
+    B.check(B.tcu_embedding_forward(ids, ids.element_size(), ids.numel(), table, rows, d, max(pitch, d), _FLOAT[kind], float(scale), out, _stream(device)))
     return out
 
 
