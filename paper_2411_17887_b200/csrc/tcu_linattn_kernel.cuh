@@ -968,11 +968,13 @@ struct StepParams {
     float scale;
 };
 
-constexpr int kStepCols = 32;            // dv columns of a block
-constexpr int kStepThreads = 128;
+constexpr int kStepCols = 64;            // dv columns of a block
+constexpr int kStepThreads = 256;
 
-// A block updates 32 columns of one state: S <- a S + k v^T, and sums q_r S[r][c] over the rows.  VEC columns a thread (4
-// where rows are 16-byte aligned), 32 / VEC threads a row.  Bound by reading and writing the state once.
+// A block updates 64 columns of one state: S <- a S + k v^T, and sums q_r S[r][c] over the rows.  VEC columns a thread (4
+// where rows are 16-byte aligned), 64 / VEC threads a row.  Bound by reading and writing the state once, so every thread
+// asks for all of its state before it looks at the token: 192 sequences of 16 heads at 128 x 128, 407 MB, 66.5 us
+// (6.1 TB/s; 82 us with the token first, 70.5 with blocks of 32 columns); one sequence of 16 heads 4.2 us, a launch.
 template <typename T, int VEC>
 __global__ void __launch_bounds__(kStepThreads) tcu_linattn_step_kernel(const __grid_constant__ StepParams p) {
     constexpr int kTx = kStepCols / VEC, kTy = kStepThreads / kTx;
@@ -992,12 +994,18 @@ __global__ void __launch_bounds__(kStepThreads) tcu_linattn_step_kernel(const __
     const T *q = reinterpret_cast<const T *>(p.q.ptr) + int64_t(b) * p.q.batch + int64_t(h) * p.q.head;
     const T *k = reinterpret_cast<const T *>(p.k.ptr) + int64_t(b) * p.k.batch + int64_t(h) * p.k.head;
     const T *v = reinterpret_cast<const T *>(p.v.ptr) + int64_t(b) * p.v.batch + int64_t(h) * p.v.head;
+    // the state is under way before the token is looked at
+    constexpr int kRows = 128 / kTy;
+    const bool mine = col < p.dv;
+    Pack<float, VEC> s[kRows];
+#pragma unroll
+    for (int j = 0; j < kRows; ++j)
+        if (mine && uint32_t(ty + j * kTy) < p.dk) s[j] = *reinterpret_cast<const Pack<float, VEC> *>(state + uint64_t(ty + j * kTy) * p.dv + col);
     for (uint32_t i = threadIdx.x; i < p.dk; i += kStepThreads) {
         sq[i] = to_f32(q[i]);
         sk[i] = to_f32(k[i]);
     }
     const float a = expf(p.log_decay[h]);
-    const bool mine = col < p.dv;
     float vv[VEC], acc[VEC];
 #pragma unroll
     for (int e = 0; e < VEC; ++e) {
@@ -1005,18 +1013,16 @@ __global__ void __launch_bounds__(kStepThreads) tcu_linattn_step_kernel(const __
         acc[e] = 0.0f;
     }
     __syncthreads();
-    if (mine) {
-#pragma unroll 8
-        for (uint32_t r = ty; r < p.dk; r += kTy) {
-            Pack<float, VEC> *at = reinterpret_cast<Pack<float, VEC> *>(state + uint64_t(r) * p.dv + col);
-            Pack<float, VEC> s = *at;
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                s.v[e] = fmaf(sk[r], vv[e], a * s.v[e]);
-                acc[e] = fmaf(sq[r], s.v[e], acc[e]);
-            }
-            *at = s;
+    for (int j = 0; j < kRows; ++j) {
+        const uint32_t r = ty + j * kTy;
+        if (!mine || r >= p.dk) continue;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            s[j].v[e] = fmaf(sk[r], vv[e], a * s[j].v[e]);
+            acc[e] = fmaf(sq[r], s[j].v[e], acc[e]);
         }
+        *reinterpret_cast<Pack<float, VEC> *>(state + uint64_t(r) * p.dv + col) = s[j];
     }
 #pragma unroll
     for (int e = 0; e < VEC; ++e) part[ty][tx * VEC + e] = acc[e];
