@@ -62,11 +62,19 @@ typedef struct {
                                    sum over the repeated axis afterwards)                                           */
     const float *d_dstate_out;  /* backward: NULL (zero), or the gradient with respect to the state after the last token */
     float *d_dstate_in;         /* backward: NULL, or receives the gradient with respect to the state before the first */
+    void *d_scratch;            /* forward and backward: NULL, or tcu_linattn_scratch_bytes() of 256-byte aligned memory, with
+                                   which many heads are spread evenly over the SMs; needs no clearing; not to be shared by
+                                   calls that may overlap                                                           */
+    uint64_t scratch_bytes;     /* size of it                                                                       */
 } tcu_linattn_t;
 
 /* Workspace of the forward and backward calls: the status of bounded waits (tcu_scan_device_status reads it).  Clear it
  * once with tcu_scan_workspace_init; any number of calls, concurrent ones too, may share it. */
 size_t tcu_linattn_workspace_bytes(void);
+
+/* Bytes of scratch with which a forward (or backward) call with these arguments runs faster; 0 if it would not, as when there are
+ * no more sequences times heads (backward: three times that) than SMs.  Looks at sizes alone (whether d_offsets is given among them). */
+size_t tcu_linattn_scratch_bytes(const tcu_linattn_t *args, int backward);
 
 /* o and, if asked for, the state after the last token.
  *   q, k, v, o  16-byte aligned pointers, strides multiples of 8 elements; the bytes from o's first element to its last must not overlap an input's

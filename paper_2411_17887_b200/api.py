@@ -72,7 +72,7 @@ def segmented_scan(x: torch.Tensor, offsets: torch.Tensor, s: int = 16, exclusiv
 _FLOAT = {torch.float32: B.TCU_F32, torch.float16: B.TCU_F16, torch.bfloat16: B.TCU_BF16}
 # the handle alone: a torch.cuda.Stream around it costs 3 us, a third of a small call
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
-_status = {}          # device index -> (buffer, pointer): where the linear-attention kernels record a wait that ran out
+_status = {}          # device index -> (buffer, pointer, SMs): where the linear-attention kernels record a wait that ran out
 
 
 def _stream(device: torch.device) -> int:
@@ -90,7 +90,7 @@ def _status_ptr(device: torch.device) -> int:
         buf = torch.zeros(B.tcu_linattn_workspace_bytes() + 256, dtype=torch.uint8, device=device)
         if not torch.cuda.is_current_stream_capturing():
             torch.cuda.current_stream().synchronize()       # other streams may use it next
-        held = _status[device.index] = (buf, buf.data_ptr() + (-buf.data_ptr()) % 256)
+        held = _status[device.index] = (buf, buf.data_ptr() + (-buf.data_ptr()) % 256, torch.cuda.get_device_properties(device).multi_processor_count)
     return held[1]
 
 
@@ -186,8 +186,14 @@ class _Mix:
     def new_state(self):
         return self.log_decay.new_empty(self.state_shape)
 
-    def args(self, q, k, v, o=B.NO_TOKENS, **more):
-        return B.tcu_linattn_args(*self.head, q, k, v, o, d_offsets=self.offsets, **more)
+    def call(self, fn, backward, q, k, v, o=B.NO_TOKENS, **more):
+        args = B.tcu_linattn_args(*self.head, q, k, v, o, d_offsets=self.offsets, **more)
+        if self.head[1] * self.head[3] * (3 if backward else 1) > _status[self.log_decay.device.index][2]:
+            size = B.tcu_linattn_scratch_bytes(args, backward)
+            if size:
+                scratch = self.log_decay.new_empty((size + 3) // 4)
+                args = B.tcu_linattn_with_scratch(args, scratch.data_ptr(), size)
+        B.check(fn(args, self.status, 256, self.stream))
 
 
 def _ptr(x) -> int:
@@ -203,8 +209,7 @@ def _attention_forward(q, k, v, log_decay, scale, initial_state, offsets, output
     last = m.new_state() if output_final_state else None
     o = _like(v, m.dv)
     (q, qv), (k, kv), (v, vv), (_, ov) = _tokens(q), _tokens(k), _tokens(v), _tokens(o)
-    B.check(B.tcu_linattn_forward(m.args(qv, kv, vv, ov, d_state_in=_ptr(initial_state), d_state_out=_ptr(last)),
-                                  m.status, 256, m.stream))
+    m.call(B.tcu_linattn_forward, 0, qv, kv, vv, ov, d_state_in=_ptr(initial_state), d_state_out=_ptr(last))
     return _out(o), last
 
 
@@ -219,8 +224,8 @@ def linear_attention_backward(d_o, q, k, v, log_decay, scale=None, initial_state
     d_first = m.new_state() if initial_state is not None else None
     d_q, d_k, d_v = _like(q, m.dk), _like(k, m.dk), _like(v, m.dv)
     (q, qv), (k, kv), (v, vv), (d_o, ov) = _tokens(q), _tokens(k), _tokens(v), _tokens(d_o)
-    B.check(B.tcu_linattn_backward(m.args(qv, kv, vv, d_o=ov, d_q=_tokens(d_q)[1], d_k=_tokens(d_k)[1], d_v=_tokens(d_v)[1], d_state_in=_ptr(initial_state),
-                                          d_dstate_out=_ptr(d_final_state), d_dstate_in=_ptr(d_first)), m.status, 256, m.stream))
+    m.call(B.tcu_linattn_backward, 1, qv, kv, vv, d_o=ov, d_q=_tokens(d_q)[1], d_k=_tokens(d_k)[1], d_v=_tokens(d_v)[1], d_state_in=_ptr(initial_state),
+           d_dstate_out=_ptr(d_final_state), d_dstate_in=_ptr(d_first))
     return _out(d_q), _out(d_k), _out(d_v), d_first
 
 

@@ -92,6 +92,8 @@ _lib.tcu_scan_last_stats.restype = _int
 _f32, _u64 = ctypes.c_float, ctypes.c_uint64
 _lib.tcu_linattn_workspace_bytes.argtypes = []
 _lib.tcu_linattn_workspace_bytes.restype = _sz
+_lib.tcu_linattn_scratch_bytes.argtypes = [ctypes.c_char_p, _int]
+_lib.tcu_linattn_scratch_bytes.restype = _sz
 _lib.tcu_linattn_forward.argtypes = [ctypes.c_char_p, _vp, _sz, _vp]
 _lib.tcu_linattn_forward.restype = _int
 _lib.tcu_linattn_backward.argtypes = [ctypes.c_char_p, _vp, _sz, _vp]
@@ -224,16 +226,26 @@ def tcu_widen_copy(d_in, d_out, n: int, dt: int, stream=0) -> int:
 
 # tcu_linattn_t, packed as bytes (a call costs less this way than through a ctypes.Structure of nested structures): every
 # member is naturally aligned, a token array is (pointer, stride_batch, stride_token, stride_head)
-_LINATTN = struct.Struct("=IIQQIIIfQQQQ" + "Qqqq" * 4 + "QQ" + "Qqqq" * 4 + "QQ")
+_LINATTN = struct.Struct("=IIQQIIIfQQQQ" + "Qqqq" * 4 + "QQ" + "Qqqq" * 4 + "QQQQ")
 NO_TOKENS = (0, 0, 0, 0)
 
 
 def tcu_linattn_args(dtype: int, batch: int, tokens: int, heads: int, dk: int, dv: int, scale: float, d_log_decay: int, q, k, v, o=NO_TOKENS, *,
                      d_offsets: int = 0, d_slots: int = 0, pool_slots: int = 0, d_state_in: int = 0, d_state_out: int = 0, d_o=NO_TOKENS,
-                     d_q=NO_TOKENS, d_k=NO_TOKENS, d_v=NO_TOKENS, d_dstate_out: int = 0, d_dstate_in: int = 0) -> bytes:
+                     d_q=NO_TOKENS, d_k=NO_TOKENS, d_v=NO_TOKENS, d_dstate_out: int = 0, d_dstate_in: int = 0, d_scratch: int = 0,
+                     scratch_bytes: int = 0) -> bytes:
     """The argument structure of the linear-attention calls; pointers are integers (0 for NULL)."""
     return _LINATTN.pack(_LINATTN.size, dtype, batch, tokens, heads, dk, dv, scale, d_log_decay, d_offsets, d_slots, pool_slots,
-                         *q, *k, *v, *o, d_state_in, d_state_out, *d_o, *d_q, *d_k, *d_v, d_dstate_out, d_dstate_in)
+                         *q, *k, *v, *o, d_state_in, d_state_out, *d_o, *d_q, *d_k, *d_v, d_dstate_out, d_dstate_in, d_scratch, scratch_bytes)
+
+
+def tcu_linattn_with_scratch(args: bytes, d_scratch: int, scratch_bytes: int) -> bytes:
+    """`args` with these as its last two members."""
+    return args[:-16] + struct.pack("=QQ", d_scratch, scratch_bytes)
+
+
+def tcu_linattn_scratch_bytes(args: bytes, backward: int) -> int:
+    return _lib.tcu_linattn_scratch_bytes(args, backward)
 
 
 def tcu_linattn_workspace_bytes() -> int:

@@ -89,7 +89,11 @@ struct alignas(64) MixParams {
     uint32_t *error;                     // status word
     uint64_t tokens;
     uint32_t batch, heads, jobs, ranks;  // ranks: blocks of a cluster
+    // walks cut where a block's share of all the groups ends: by block, a flag and the state that it hands to the next one
+    uint32_t *flags;
+    float *handed;
 };
+constexpr uint32_t kMostOrdered = 256;   // sequences that are put in order
 
 // Which groups of a walk a block takes, and how many tokens.
 struct MixPart {
@@ -128,7 +132,12 @@ struct MixCtl {
     MixPart part;
     uint32_t t0, b, h, count, before;    // first token of the sequence; sequence (0 when packed) and head; groups of the walk, of the first phase
     uint32_t thirds;                     // third terms of K~ in the first phase
-    uint64_t state_at;                   // of the states, in values
+    const uint32_t *wait_flag;           // NULL, or set once the state that enters has been handed over
+    uint64_t patience;                   // nanoseconds to wait for that
+    uint64_t places_from, places_to;     // what is left of the block's share
+    bool none, settle;                   // no walk was left; the block goes on with another: nothing may be under way when this one ends
+    bool hands;                          // the state is for the next block
+    uint32_t sequence;                   // packed, in order: which one
     bool split, entered, owns_last;      // the walk starts from a state (else from zero); its last state is wanted
     float log2_decay;
     float biggest_k[2][8], biggest_x[2][4];      // float16: largest values seen by each warp
@@ -196,6 +205,12 @@ struct Half2 : Half2Of<T> {
     static __device__ __forceinline__ uint32_t fma(uint32_t a, uint32_t b, uint32_t c) { return bits(__hfma2(as(a), as(b), as(c))); }
     static __device__ __forceinline__ uint32_t fms(uint32_t a, uint32_t b, uint32_t c) { return bits(__hfma2(as(a), as(b), __hneg2(as(c)))); }
 };
+
+__device__ __forceinline__ uint64_t global_ns() {
+    uint64_t t;
+    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t) : : "memory");
+    return t;
+}
 
 // Waits for the phase of a barrier; false when the wait was given up, after about a second.
 constexpr uint32_t kMixWaitRounds = 10000;
@@ -608,7 +623,7 @@ struct Mix {
         if (n > 0 && !gate(ctl->kv_done, (base + n - 1) & 1)) return;
         tc_fence_after();
         if (!holds_x) return;
-        float *to = phase ? ctl->job.last + ctl->state_at + row : exchange;
+        float *to = phase ? ctl->job.last + row : exchange;
         const uint32_t pitch = phase ? ctl->job.dv : D, rows = phase ? dk : D;
         const float back = kIsHalf ? pow2(-held) : 1.0f;
 #pragma unroll 1
@@ -621,15 +636,145 @@ struct Mix {
                 if (c + j < rows) to[uint64_t(c + j) * pitch] = __uint_as_float(v[j]) * back;
         }
     }
+    // ---- what a block works on.  One thread writes it down.
+    static __device__ __forceinline__ void take(const MixParams &p, const MixPart &part, uint32_t job_index, uint32_t b, uint32_t h, int64_t begin, uint32_t rank, bool cut) {
+        MixCtl *ctl = mix_ctl();
+        const MixJob &job = p.job[job_index];
+        const uint32_t count = part.last - part.first;
+        const bool handed = cut && part.first > 0, hands = cut && part.last < part.groups;
+        const uint64_t size = uint64_t(job.dk) * job.dv, state_at = (uint64_t(b) * p.heads + h) * size;
+        ctl->job = job;
+        if (job.init) ctl->job.init = job.init + state_at;
+        if (job.last) ctl->job.last = job.last + state_at;
+        if (handed) {
+            ctl->job.init = p.handed + (blockIdx.x - 1) * size;
+            ctl->job.init_k = job.dv;
+            ctl->job.init_v = 1;
+        }
+        if (hands) ctl->job.last = p.handed + blockIdx.x * size;
+        ctl->wait_flag = handed ? p.flags + blockIdx.x - 1 : nullptr;
+        ctl->patience = 1000000000ull + 100000ull * part.first;
+        ctl->hands = hands;
+        ctl->part = part;
+        ctl->t0 = uint32_t(begin);
+        ctl->b = p.offsets ? 0 : b;
+        ctl->h = h;
+        ctl->count = count;
+        // a split walk has a first phase, over K and V only, in the blocks whose totals later blocks need
+        ctl->before = p.ranks > 1 && part.last < part.groups ? count : 0;
+        ctl->split = p.ranks > 1;
+        ctl->log2_decay = fmaxf(p.log_decay[h] * 1.4426950408889634f, -1e30f);
+        uint32_t lo = part.first, hi = part.first + ctl->before;           // the groups with a third term are the last ones
+        while (lo < hi) {
+            const uint32_t mid = (lo + hi) / 2;
+            if (has_third(ctl, part, mid)) hi = mid;
+            else lo = mid + 1;
+        }
+        ctl->thirds = part.first + ctl->before - lo;
+        ctl->entered = job.init || part.first > 0;
+        ctl->owns_last = hands || (job.last && (part.groups == 0 ? rank == 0 : (part.last == part.groups && count > 0)));
+    }
+    // One thread: the next walk of a block whose share is a stretch of the list of all walks, in which a walk has a place for every
+    // group, and one more for what it costs to begin it.  From the last walk back to the first: what the next block waits for comes
+    // first, what this one waits for last.
+    static __device__ __noinline__ void next_walk(const MixParams &p) {
+        MixCtl *ctl = mix_ctl();
+        const uint64_t lo = ctl->places_from;
+        uint64_t to = ctl->places_to, walk = 0;
+        MixPart part;
+        part.len = uint32_t(p.tokens);
+        part.groups = (part.len + kGroup - 1) / kGroup;
+        part.per = part.groups;
+        do {
+            ctl->none = to == lo;
+            if (to == lo) return;
+            walk = (to - 1) / (part.groups + 1);
+            const uint64_t at = walk * (part.groups + 1), from = max(lo, at);
+            part.first = min(uint32_t(from - at), part.groups);
+            part.last = min(uint32_t(to - at), part.groups);
+            to = from;
+        } while (part.first == part.groups);         // only the place for its beginning: there is nothing to do
+        const uint32_t unit = uint32_t(walk / p.jobs), job = uint32_t(walk - uint64_t(unit) * p.jobs);
+        part.lead = p.job[job].lead != 0;
+        ctl->settle = to > lo;
+        ctl->places_to = to;
+        take(p, part, job, unit / p.heads, unit % p.heads, 0, 0, true);
+    }
+    // Whether there is another walk (all threads); if so, its barriers may be set up.
+    static __device__ __forceinline__ bool goes_on() {
+        MixCtl *ctl = mix_ctl();
+        if (!ctl->settle || ctl->abort_flag) return false;
+        if (threadIdx.x == 32 * kProducerWarp)
+            for (uint64_t *one = &ctl->full[0]; one <= &ctl->drained[1]; ++one)
+                if (one < &ctl->full[kSlots] || (one >= &ctl->empty[0] && one < &ctl->empty[kSlots]) || one >= &ctl->qk_done) mbar_inval(smem_u32(one));
+        __syncthreads();                     // everybody has seen what the next walk replaces
+        return true;
+    }
+    // One thread.
+    static __device__ __forceinline__ void begin_barriers() {
+        MixCtl *ctl = mix_ctl();
+        for (uint32_t i = 0; i < kSlots; ++i) {
+            mbar_init(smem_u32(&ctl->full[i]), 1);
+            mbar_init(smem_u32(&ctl->empty[i]), 2);
+        }
+        for (uint64_t *one : {&ctl->qk_done, &ctl->pv_done, &ctl->e_done, &ctl->k_scaled, &ctl->first_done, &ctl->kv_done, &ctl->drained[0], &ctl->drained[1]}) mbar_init(smem_u32(one), 1);
+        mbar_init(smem_u32(&ctl->p_ready), 32 * kTokenWarps);
+        mbar_init(smem_u32(&ctl->o_free), 32 * kTokenWarps);
+        mbar_init(smem_u32(&ctl->o_staged), 32 * kTokenWarps);
+        mbar_init(smem_u32(&ctl->x_ready), 128);
+        mbar_init(smem_u32(&ctl->k_ready), 32 * kKeyWarps);
+        mbar_init(smem_u32(&ctl->third_ready), 32 * kKeyWarps);
+        fence_barrier_init();
+    }
+    // All threads: decays a^m = 2^(m log2 a); -inf becomes a value whose multiples are finite, so that a^0 = 1
+    static __device__ __forceinline__ void tables(float log2a, bool lead, float scale, const MixPart &part) {
+        MixCtl *ctl = mix_ctl();
+        if (threadIdx.x < kNear) {
+            const int apart = int(threadIdx.x) - 47;
+            const float power = exp2f(log2a * float(max(apart, 0)));
+            ctl->near[lead ? kNear - 1 - threadIdx.x : threadIdx.x] = apart >= 0 ? scale * power : 0.0f;
+            if (apart >= 0 && apart <= kGroup) ctl->power[apart] = power;
+            if (apart >= 0 && apart < 16) ctl->block[lead ? 15 - apart : apart] = scale * power;
+        }
+        if (threadIdx.x >= 256 && threadIdx.x < 264) ctl->rank_decay[threadIdx.x - 256] = exp2f(log2a * part.tokens_of_rank(threadIdx.x - 256));
+    }
+    // All threads: which sequence comes `place`-th, the longest first.  (The ring is not in use yet.)
+    static __device__ __noinline__ uint32_t in_order(const int64_t *offsets, uint32_t batch, uint32_t place) {
+        MixCtl *ctl = mix_ctl();
+        int64_t *lens = reinterpret_cast<int64_t *>(reinterpret_cast<uint8_t *>(ctl) + kMixCtlBytes);
+        const uint32_t mine = threadIdx.x;
+        if (mine < batch) lens[mine] = offsets[mine + 1] - offsets[mine];
+        __syncthreads();
+        if (mine < batch) {
+            const int64_t len = lens[mine];
+            uint32_t longer = 0;
+            for (uint32_t i = 0; i < batch; ++i) longer += lens[i] > len || (lens[i] == len && i < mine);
+            if (longer == place) ctl->sequence = mine;
+        }
+        __syncthreads();
+        return ctl->sequence;
+    }
     // the state that enters the walk
+    template <bool CUT>
     static __device__ __noinline__ void enter() {
         MixCtl *ctl = mix_ctl();
         const int warp = threadIdx.x >> 5, row = (warp & 3) * 32 + (threadIdx.x & 31);
         if (!(ctl->entered || ctl->count == 0) || (warp & 3) * 32 >= D) return;
         const bool exchanged = ctl->split && ctl->count > 0;
         const float *exchange = reinterpret_cast<const float *>(reinterpret_cast<uint8_t *>(ctl) + kMixCtlBytes) + row;
-        const float *from = exchanged ? exchange : ctl->job.init + ctl->state_at + uint64_t(row) * ctl->job.init_v;
+        const float *from = exchanged ? exchange : ctl->job.init + uint64_t(row) * ctl->job.init_v;
         const uint32_t pitch = exchanged ? D : ctl->job.init_k, rows = exchanged ? D : ctl->job.init && uint32_t(row) < ctl->job.dv ? ctl->job.dk : 0;
+        if (CUT && ctl->wait_flag) {                 // (a block waits only for the one before it, all of them run at once, and what that
+            const uint64_t from = global_ns();       // one hands over it works on first)
+            while (ld_acquire_u32(ctl->wait_flag) == 0) {
+                if (global_ns() - from > ctl->patience) {
+                    ctl->abort_flag = 1;
+                    break;
+                }
+                __nanosleep(200);
+            }
+            __syncwarp();
+        }
 #pragma unroll 1
         for (uint32_t c = 0; c < D; c += 16) {
             uint32_t v[16];
@@ -670,6 +815,8 @@ struct Mix {
                 ++group;
             }
         }
+        if (phase && ctl->settle)
+            for (uint32_t m = tile > kSlots ? tile - kSlots : 0; m < tile && !ctl->abort_flag; ++m) mix_wait(ctl, ctl->empty[m % kSlots], (m / kSlots) & 1);
         if (ctl->abort_flag)                        // copies in flight must land before the block may exit
             for (uint32_t m = tile > kSlots ? tile - kSlots : 0; m < tile; ++m)
                 mbar_wait_bounded(smem_u32(&ctl->full[m % kSlots]), (m / kSlots) & 1, kMixWaitRounds);
@@ -785,6 +932,7 @@ struct Mix {
             }
             __syncwarp();
         }
+        if (phase && ctl->settle && n > 0 && !ctl->abort_flag) mix_wait_warp(ctl, ctl->kv_done, (it - 1) & 1);
         drain(ctl, 1);
     }
 
@@ -819,7 +967,7 @@ struct Mix {
         cluster_sync_all();
         const MixPart part = ctl->part;
         const uint32_t at = smem_u32(ctl) + kMixCtlBytes, dk = ctl->job.dk, dv = ctl->job.dv;
-        const float *init = ctl->job.init ? ctl->job.init + ctl->state_at : nullptr;
+        const float *init = ctl->job.init;
 #pragma unroll 1
         for (uint32_t e = 4 * (rank * kMixThreads + threadIdx.x); e < D * D; e += 4 * ranks * kMixThreads) {
             const uint32_t c = e / D, r = e % D;
@@ -849,110 +997,99 @@ struct Mix {
     }
 };
 
-template <int D, typename T>
+// kWhole: a block, or a cluster of them, has one walk; kOrdered: the same with the walks of long sequences first; kCut: a block has
+// a share of all walks, which begins and ends anywhere.  (A kernel that does the one or the other costs small calls 1 to 2 us.)
+enum { kWhole, kOrdered, kCut };
+template <int D, typename T, int KIND>
 __global__ void __launch_bounds__(kMixThreads, 1) tcu_linattn_mix_kernel(const __grid_constant__ MixParams p) {
     using M = Mix<D, T>;
     MixCtl *ctl = mix_ctl();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t rank = blockIdx.x % p.ranks, work = blockIdx.x / p.ranks, unit = work / p.jobs, b = unit / p.heads, h = unit % p.heads;
-    const MixJob &job = p.job[work % p.jobs];
-    // packed: whatever the offsets hold, no token outside the arrays is touched
-    const int64_t most = int64_t(p.tokens), begin = p.offsets ? min(max(p.offsets[b], int64_t(0)), most) : 0;
-    MixPart part;
-    part.lead = job.lead != 0;
-    part.len = uint32_t(p.offsets ? min(max(p.offsets[b + 1], begin), most) - begin : most);
-    part.groups = (part.len + kGroup - 1) / kGroup;
-    part.per = (part.groups + p.ranks - 1) / p.ranks;
-    part.first = min(rank * part.per, part.groups);
-    part.last = min((rank + 1) * part.per, part.groups);
+    constexpr bool CUT = KIND == kCut;
+    const uint32_t ranks = CUT ? 1 : p.ranks, rank = CUT ? 0 : blockIdx.x % p.ranks;
     if (threadIdx.x == 0) {
-        const uint32_t count = part.last - part.first;
-        ctl->job = job;
-        ctl->part = part;
-        ctl->t0 = uint32_t(begin);
-        ctl->b = p.offsets ? 0 : b;
-        ctl->h = h;
-        ctl->state_at = uint64_t(unit) * job.dk * job.dv;
-        ctl->count = count;
-        // a split walk has a first phase, over K and V only, in the blocks whose totals later blocks need
-        ctl->before = p.ranks > 1 && part.last < part.groups ? count : 0;
-        ctl->split = p.ranks > 1;
-        ctl->log2_decay = fmaxf(p.log_decay[h] * 1.4426950408889634f, -1e30f);
-        uint32_t lo = part.first, hi = part.first + ctl->before;            // the groups with a third term are the last ones
-        while (lo < hi) {
-            const uint32_t mid = (lo + hi) / 2;
-            if (M::has_third(ctl, part, mid)) hi = mid;
-            else lo = mid + 1;
-        }
-        ctl->thirds = part.first + ctl->before - lo;
-        ctl->entered = job.init || rank > 0;
-        ctl->owns_last = job.last && (part.groups == 0 ? rank == 0 : (part.last == part.groups && count > 0));
-    }
-    if (warp == kProducerWarp && lane == 0) {
-        for (uint32_t i = 0; i < M::kSlots; ++i) {
-            mbar_init(smem_u32(&ctl->full[i]), 1);
-            mbar_init(smem_u32(&ctl->empty[i]), 2);
-        }
-        for (uint64_t *one : {&ctl->qk_done, &ctl->pv_done, &ctl->e_done, &ctl->k_scaled, &ctl->first_done, &ctl->kv_done, &ctl->drained[0], &ctl->drained[1]}) mbar_init(smem_u32(one), 1);
-        mbar_init(smem_u32(&ctl->p_ready), 32 * kTokenWarps);
-        mbar_init(smem_u32(&ctl->o_free), 32 * kTokenWarps);
-        mbar_init(smem_u32(&ctl->o_staged), 32 * kTokenWarps);
-        mbar_init(smem_u32(&ctl->x_ready), 128);
-        mbar_init(smem_u32(&ctl->k_ready), 32 * kKeyWarps);
-        mbar_init(smem_u32(&ctl->third_ready), 32 * kKeyWarps);
         ctl->abort_flag = 0;
-        fence_barrier_init();
+        if (CUT) {
+            const uint64_t places = (uint64_t(p.tokens + kGroup - 1) / kGroup + 1) * p.batch * p.heads * p.jobs;
+            ctl->places_from = places * blockIdx.x / gridDim.x;
+            ctl->places_to = places * (blockIdx.x + 1) / gridDim.x;
+        }
+        ctl->settle = false;
     }
-    if (warp == kProductWarp) {
+    auto allocate = [&] {
+        if (warp != kProductWarp) return;
         tmem_alloc(smem_u32(&ctl->tmem_base), M::kColumns);
         tmem_relinquish();
-    }
-    // decays: a^m = 2^(m log2 a); -inf becomes a value whose multiples are finite, so that a^0 = 1
-    const float log2a = fmaxf(p.log_decay[h] * 1.4426950408889634f, -1e30f);
-    if (threadIdx.x < kNear) {
-        const int apart = int(threadIdx.x) - 47;
-        const float power = exp2f(log2a * float(max(apart, 0))), scale = job.in_scale * job.out_scale;
-        ctl->near[part.lead ? kNear - 1 - threadIdx.x : threadIdx.x] = apart >= 0 ? scale * power : 0.0f;
-        if (apart >= 0 && apart <= kGroup) ctl->power[apart] = power;
-        if (apart >= 0 && apart < 16) ctl->block[part.lead ? 15 - apart : apart] = scale * power;
-    }
-    if (threadIdx.x >= 256 && threadIdx.x < 264) ctl->rank_decay[threadIdx.x - 256] = exp2f(log2a * part.tokens_of_rank(threadIdx.x - 256));
-    tc_fence_before();
-    __syncthreads();
-    tc_fence_after();
+    };
+    if (CUT) allocate();
+#pragma unroll 1
+    do {
+        if (warp == kProducerWarp && lane == 0) M::begin_barriers();
+        if constexpr (CUT) {
+            if (threadIdx.x == 0) M::next_walk(p);
+            __syncthreads();
+            if (ctl->none) break;
+            M::tables(ctl->log2_decay, ctl->part.lead, ctl->job.in_scale * ctl->job.out_scale, ctl->part);
+        } else {
+            const uint32_t work = blockIdx.x / ranks, unit = work / p.jobs, h = unit % p.heads;
+            uint32_t b = unit / p.heads;
+            if (KIND == kOrdered) b = M::in_order(p.offsets, p.batch, b);
+            const MixJob &job = p.job[work % p.jobs];
+            // packed: whatever the offsets hold, no token outside the arrays is touched
+            const int64_t most = int64_t(p.tokens), begin = p.offsets ? min(max(p.offsets[b], int64_t(0)), most) : 0;
+            MixPart part;
+            part.lead = job.lead != 0;
+            part.len = uint32_t(p.offsets ? min(max(p.offsets[b + 1], begin), most) - begin : most);
+            part.groups = (part.len + kGroup - 1) / kGroup;
+            part.per = (part.groups + ranks - 1) / ranks;
+            part.first = min(rank * part.per, part.groups);
+            part.last = min((rank + 1) * part.per, part.groups);
+            if (threadIdx.x == 0) M::take(p, part, work % p.jobs, b, h, begin, rank, false);
+            M::tables(fmaxf(p.log_decay[h] * 1.4426950408889634f, -1e30f), part.lead, job.in_scale * job.out_scale, part);
+            allocate();
+        }
+        tc_fence_before();
+        __syncthreads();
+        tc_fence_after();
 
 #pragma unroll 1
-    for (uint32_t phase = p.ranks > 1 ? 0 : 1; phase < 2; ++phase) {
-        if (phase) {
-            if (warp >= kStateWarp && warp < kProducerWarp) M::enter();
-            if (p.ranks > 1) {
-                fence_proxy_async_smem();                               // the next writes to the exchange buffer are TMA loads
-                tc_fence_before();
-                __syncthreads();
-                tc_fence_after();
+        for (uint32_t phase = ranks > 1 ? 0 : 1; phase < 2; ++phase) {
+            if (phase) {
+                if (warp >= kStateWarp && warp < kProducerWarp) M::template enter<CUT>();
+                if (ranks > 1) {
+                    fence_proxy_async_smem();                               // the next writes to the exchange buffer are TMA loads
+                    tc_fence_before();
+                    __syncthreads();
+                    tc_fence_after();
+                }
             }
+            if (warp < kTokenWarps) {
+                if (phase) M::tokens();
+            } else if (warp < kStateWarp) {
+                M::keys(phase);
+            } else if (warp < kProducerWarp) {
+                M::state(phase);
+            } else if (warp == kProducerWarp) {
+                if (lane == 0) M::loads(p.map, phase);
+            } else if (warp == kScoreWarp) {
+                if (phase) M::scores();
+            } else if (warp == kProductWarp) {
+                M::products(phase);
+            } else if (phase && lane == 0) {
+                M::stores(p.map);
+            }
+            if (!CUT && !phase) M::exchange(ranks, rank);
         }
-        if (warp < kTokenWarps) {
-            if (phase) M::tokens();
-        } else if (warp < kStateWarp) {
-            M::keys(phase);
-        } else if (warp < kProducerWarp) {
-            M::state(phase);
-        } else if (warp == kProducerWarp) {
-            if (lane == 0) M::loads(p.map, phase);
-        } else if (warp == kScoreWarp) {
-            if (phase) M::scores();
-        } else if (warp == kProductWarp) {
-            M::products(phase);
-        } else if (phase && lane == 0) {
-            M::stores(p.map);
+        __syncwarp();
+        if (CUT) fence_proxy_async_smem();   // the next walk's tiles are TMA loads
+        tc_fence_before();
+        __syncthreads();
+        tc_fence_after();
+        if (CUT && threadIdx.x == 0 && ctl->hands) {
+            __threadfence();
+            st_release_u32(p.flags + blockIdx.x, 1);
         }
-        if (!phase) M::exchange(p.ranks, rank);
-    }
-    __syncwarp();
-    tc_fence_before();
-    __syncthreads();
-    tc_fence_after();
+    } while (CUT && M::goes_on());
     if (warp == kProductWarp) tmem_dealloc(ctl->tmem_base, M::kColumns);
     if (threadIdx.x == 0 && ctl->abort_flag) atomicExch(p.error, 5u);
 }

@@ -147,13 +147,13 @@ tcu_status_t choose_ranks(uint64_t units, uint64_t groups, uint32_t *ranks) {
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return TCU_ERR_CUDA;
     if (configured.load() != dev) {
-        if (cudaFuncSetAttribute(tcu_linattn_mix_kernel<D, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMixSmemBytes<D>) != cudaSuccess) return TCU_ERR_CUDA;
+        if (cudaFuncSetAttribute(tcu_linattn_mix_kernel<D, T, kWhole>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMixSmemBytes<D>) != cudaSuccess) return TCU_ERR_CUDA;
         at_once[1] = sm_count();
         for (uint32_t r = 2; r <= kMostRanks; ++r) {
             cudaLaunchAttribute attr;
             const cudaLaunchConfig_t cfg = mix_config<D, T>(r, r, &attr, nullptr);
             int n = 0;
-            at_once[r] = cudaOccupancyMaxActiveClusters(&n, tcu_linattn_mix_kernel<D, T>, &cfg) == cudaSuccess ? n : 0;
+            at_once[r] = cudaOccupancyMaxActiveClusters(&n, tcu_linattn_mix_kernel<D, T, kWhole>, &cfg) == cudaSuccess ? n : 0;
         }
         configured.store(dev);
     }
@@ -171,13 +171,51 @@ tcu_status_t choose_ranks(uint64_t units, uint64_t groups, uint32_t *ranks) {
     return TCU_OK;
 }
 
+// More walks than SMs: whether they are cut into equal shares of all the groups, one for each SM, with the state handed from
+// block to block, instead of running whole in waves of which the last is not full.  In units of a group: a walk costs one more to
+// begin, shares about ten more in all (three walks begun instead of two, and 148 blocks at once wait longer for memory than fewer).
+// Measured at D = 128: the gradients of 64 heads of 4096 tokens, 192 walks, 210 us whole, 170 cut; the outputs of 256 heads of
+// 4096 tokens 237 whole, 238 cut (whole).  Packed sequences differ in length: cut as well, 24 of them with 12 heads took 164 us
+// where whole walks took 153, and 137 with the long ones first.
+bool cut_pays(const tcu_linattn_t *a, uint32_t jobs) {
+    const uint64_t units = a->batch * a->heads * jobs, sms = uint64_t(sm_count()), places = (a->tokens + kGroup - 1) / kGroup + 1;
+    return sms > 0 && units > sms && a->tokens > 0 && !a->d_offsets && units * places / sms + 10 < (units + sms - 1) / sms * places;
+}
+size_t flag_bytes() { return (size_t(sm_count()) * 4 + 255) / 256 * 256; }
+size_t scratch_bytes(const tcu_linattn_t *a, uint32_t jobs) { return cut_pays(a, jobs) ? flag_bytes() + size_t(sm_count()) * a->dk * a->dv * 4 : 0; }
+
+template <int D, typename T, int KIND>
+tcu_status_t launch_kind(const MixParams &p, const cudaLaunchConfig_t &cfg) {
+    static std::atomic<int> configured{-1};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) return TCU_ERR_CUDA;
+    if (configured.load() != dev) {
+        if (cudaFuncSetAttribute(tcu_linattn_mix_kernel<D, T, KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMixSmemBytes<D>) != cudaSuccess) return TCU_ERR_CUDA;
+        configured.store(dev);
+    }
+    return cudaLaunchKernelEx(&cfg, tcu_linattn_mix_kernel<D, T, KIND>, p) == cudaSuccess ? TCU_OK : TCU_ERR_CUDA;
+}
+
 template <int D, typename T>
-tcu_status_t launch_mix(MixParams &p, uint64_t groups, cudaStream_t stream) {
-    const uint32_t units = p.batch * p.heads * p.jobs;
-    if (tcu_status_t st = choose_ranks<D, T>(units, groups, &p.ranks)) return st;
+tcu_status_t launch_mix(const tcu_linattn_t *a, MixParams &p, uint64_t groups, cudaStream_t stream) {
+    const uint32_t units = p.batch * p.heads * p.jobs, sms = uint32_t(sm_count());
     cudaLaunchAttribute attr;
+    if (a->d_scratch && cut_pays(a, p.jobs)) {
+        p.ranks = 1;
+        p.flags = static_cast<uint32_t *>(a->d_scratch);
+        p.handed = reinterpret_cast<float *>(static_cast<uint8_t *>(a->d_scratch) + flag_bytes());
+        if (cudaMemsetAsync(p.flags, 0, flag_bytes(), stream) != cudaSuccess) return TCU_ERR_CUDA;
+        cudaLaunchConfig_t cfg = mix_config<D, T>(sms, 1, &attr, stream);
+        attr.id = cudaLaunchAttributeCooperative;          // blocks wait for one another: all of them run at once
+        attr.val.cooperative = 1;
+        cfg.numAttrs = 1;
+        return launch_kind<D, T, kCut>(p, cfg);
+    }
+    if (tcu_status_t st = choose_ranks<D, T>(units, groups, &p.ranks)) return st;
     const cudaLaunchConfig_t cfg = mix_config<D, T>(units * p.ranks, p.ranks, &attr, stream);
-    return cudaLaunchKernelEx(&cfg, tcu_linattn_mix_kernel<D, T>, p) == cudaSuccess ? TCU_OK : TCU_ERR_CUDA;
+    // (an order costs a look at all lengths; it matters where blocks come in waves)
+    if (p.offsets && p.ranks == 1 && p.batch > 1 && p.batch <= kMostOrdered && units > sms) return launch_kind<D, T, kOrdered>(p, cfg);
+    return launch_kind<D, T, kWhole>(p, cfg);
 }
 
 // `transposed`: the state that enters is stored as dv x dk.
@@ -200,6 +238,7 @@ MixJob make_job(const uint8_t (&maps)[3], uint32_t dk, uint32_t dv, bool forward
 // Fills in what all jobs share and launches.  `arrays`: what the jobs' map indexes name; `outputs`: where each job writes.
 tcu_status_t run_mix(const tcu_linattn_t *a, MixParams &p, const tcu_tokens_t *const *arrays, const uint32_t *widths, int count,
                      const tcu_tokens_t *const *outputs, void *d_ws, cudaStream_t stream) {
+    if (a->d_scratch && (a->scratch_bytes < scratch_bytes(a, p.jobs) || !aligned(a->d_scratch, 256))) return TCU_ERR_WORKSPACE;
     int dev = 0;                      // (encoding needs a current context, which a thread that has made no CUDA call does not have)
     if (!encode_fn() || cudaGetDevice(&dev) != cudaSuccess || cudaSetDevice(dev) != cudaSuccess) return TCU_ERR_CUDA;
     for (int i = 0; i < count; ++i)
@@ -226,8 +265,8 @@ tcu_status_t run_mix(const tcu_linattn_t *a, MixParams &p, const tcu_tokens_t *c
     }
     const bool wide = a->dk > 64 || a->dv > 64;
     const uint64_t groups = ((a->d_offsets ? a->tokens / a->batch : a->tokens) + kGroup - 1) / kGroup;
-    if (a->type == TCU_F16) return wide ? launch_mix<128, __half>(p, groups, stream) : launch_mix<64, __half>(p, groups, stream);
-    return wide ? launch_mix<128, __nv_bfloat16>(p, groups, stream) : launch_mix<64, __nv_bfloat16>(p, groups, stream);
+    if (a->type == TCU_F16) return wide ? launch_mix<128, __half>(a, p, groups, stream) : launch_mix<64, __half>(a, p, groups, stream);
+    return wide ? launch_mix<128, __nv_bfloat16>(a, p, groups, stream) : launch_mix<64, __nv_bfloat16>(a, p, groups, stream);
 }
 
 // No tokens: the state that leaves is the state that enters.
@@ -242,6 +281,11 @@ tcu_status_t copy_state(float *to, const float *from, size_t bytes, cudaStream_t
 extern "C" {
 
 size_t tcu_linattn_workspace_bytes(void) { return kStatusBytes; }
+
+size_t tcu_linattn_scratch_bytes(const tcu_linattn_t *a, int backward) {
+    if (!has_struct(a) || a->dk == 0 || a->dk > 128 || a->dv == 0 || a->dv > 128 || a->batch > (uint64_t(1) << 31) || a->batch * a->heads * 3 > (uint64_t(1) << 31)) return 0;
+    return scratch_bytes(a, backward ? 3 : 1);
+}
 
 tcu_status_t tcu_linattn_forward(const tcu_linattn_t *a, void *d_ws, size_t ws_bytes, cudaStream_t stream) {
     if (tcu_status_t st = check_linattn(a, d_ws, ws_bytes)) return st;

@@ -200,6 +200,46 @@ def test_packed(dtype, dk, dv):
                        [part(x) for x in grads[:3]] + [grads[3][i:i + 1]])
 
 
+@pytest.mark.parametrize("dtype", DTYPES, ids=["bf16", "f16"])
+@pytest.mark.parametrize("shape", [(2, 300, 80, 16, 24), (1, 700, 150, 32, 16), (1, 520, 60, 24, 72), (5, 130, 31, 8, 128), (1, 100, 149, 16, 16)], ids=str)
+@pytest.mark.parametrize("states", [False, True], ids=["plain", "states"])
+def test_more_walks_than_multiprocessors(shape, dtype, states):
+    """Walks are cut where a multiprocessor's share of them ends, and the state is handed over; states in place as well."""
+    b, t, h, dk, dv = shape
+    q, k, v, d_o, decay, s0, d_last = draw(t + h, b, t, h, dk, dv, dtype, states)
+    decay[: h // 2] = -1e-3 * (1 + torch.arange(h // 2, device="cuda"))
+    scale = dk ** -0.5
+    o, last = api.linear_attention(q, k, v, decay, initial_state=s0, output_final_state=True)
+    check_forward(q, k, v, decay, scale, s0, o, last)
+    check_backward(q, k, v, decay, scale, s0, d_o, d_last, api.linear_attention_backward(d_o, q, k, v, decay, initial_state=s0, d_final_state=d_last))
+    assert torch.equal(o, api.linear_attention(q, k, v, decay, initial_state=s0)[0])
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=["bf16", "f16"])
+@pytest.mark.parametrize("seed", [0, 1, 2])
+def test_packed_and_more_walks_than_multiprocessors(dtype, seed):
+    """One walk over many blocks, whole blocks of empty sequences, several short walks to a block; more than 32 sequences."""
+    rng = np.random.default_rng(seed)
+    h, dk, dv = 5, 24, 16
+    lens = [int(n) for n in rng.choice([0, 1, 3, 40, 128, 129, 300], 45)]
+    lens[[0, 22, 44][seed]] = 2500
+    lens[5:9] = [0] * 4
+    off = np.concatenate([[0], np.cumsum(lens)])
+    q, k, v, d_o, decay, _, _ = draw(71 + seed, 1, int(off[-1]), h, dk, dv, dtype)
+    q, k, v, d_o = (x[0] for x in (q, k, v, d_o))
+    decay[0] = -1e-3
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    s0, d_last = (torch.randn((len(lens), h, dk, dv), generator=g, device="cuda") for _ in range(2))
+    offsets = torch.from_numpy(off).cuda()
+    o, last = api.linear_attention(q, k, v, decay, initial_state=s0, offsets=offsets, output_final_state=True)
+    grads = api.linear_attention_backward(d_o, q, k, v, decay, initial_state=s0, offsets=offsets, d_final_state=d_last)
+    for i in range(len(lens)):
+        part = lambda x: x[off[i]:off[i + 1]][None]  # noqa: E731
+        check_forward(part(q), part(k), part(v), decay, dk ** -0.5, s0[i:i + 1], part(o), last[i:i + 1])
+        check_backward(part(q), part(k), part(v), decay, dk ** -0.5, s0[i:i + 1], part(d_o), d_last[i:i + 1],
+                       [part(x) for x in grads[:3]] + [grads[3][i:i + 1]])
+
+
 def test_empty_calls():
     decay = torch.zeros(2, device="cuda")
     empty = torch.empty((0, 5, 2, 64), dtype=torch.bfloat16, device="cuda")
