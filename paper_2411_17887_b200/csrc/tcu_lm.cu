@@ -239,8 +239,11 @@ MixJob make_job(const uint8_t (&maps)[3], uint32_t dk, uint32_t dv, bool forward
 tcu_status_t run_mix(const tcu_linattn_t *a, MixParams &p, const tcu_tokens_t *const *arrays, const uint32_t *widths, int count,
                      const tcu_tokens_t *const *outputs, void *d_ws, cudaStream_t stream) {
     if (a->d_scratch && (a->scratch_bytes < scratch_bytes(a, p.jobs) || !aligned(a->d_scratch, 256))) return TCU_ERR_WORKSPACE;
-    int dev = 0;                      // (encoding needs a current context, which a thread that has made no CUDA call does not have)
-    if (!encode_fn() || cudaGetDevice(&dev) != cudaSuccess || cudaSetDevice(dev) != cudaSuccess) return TCU_ERR_CUDA;
+    if (!encode_fn()) return TCU_ERR_CUDA;
+    thread_local int bound = -1;      // encoding needs a current context, which a thread that has made no CUDA call does not have
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || (bound != dev && cudaSetDevice(dev) != cudaSuccess)) return TCU_ERR_CUDA;
+    bound = dev;
     for (int i = 0; i < count; ++i)
         if (!encode_tokens(&p.map[i], a, *arrays[i], widths[i])) return TCU_ERR_CUDA;
     p.log_decay = a->d_log_decay;

@@ -240,6 +240,25 @@ def test_packed_and_more_walks_than_multiprocessors(dtype, seed):
                        [part(x) for x in grads[:3]] + [grads[3][i:i + 1]])
 
 
+def test_scratch_sizes_and_refusals():
+    """Scratch memory is asked for where many walks leave a last wave short of blocks, and has to be as large as asked for."""
+    from paper_2411_17887_b200 import binding as B
+
+    def args(b, t, h, **more):
+        at = lambda i: (i << 28, t * h * 64, h * 64, 64)  # noqa: E731
+        return B.tcu_linattn_args(B.TCU_BF16, b, t, h, 64, 64, 1.0, 9 << 28, at(1), at(2), at(3), at(4), d_o=at(5), d_q=at(6), d_k=at(7), d_v=at(8), **more)
+
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    assert B.tcu_linattn_scratch_bytes(args(1, 4096, sms), 0) == 0                        # one wave, full
+    assert B.tcu_linattn_scratch_bytes(args(1, 4096, sms + 9, d_offsets=10 << 28), 0) == 0
+    size = B.tcu_linattn_scratch_bytes(args(1, 4096, sms + 9), 0)
+    assert size >= sms * (64 * 64 * 4 + 4)
+    assert B.tcu_linattn_scratch_bytes(args(1, 4096, sms // 3 + 3), 1) == size
+    buf = torch.empty(256, dtype=torch.uint8, device="cuda").zero_()
+    for where, n in ((11 << 28, size - 1), ((11 << 28) + 16, size)):
+        assert B.tcu_linattn_forward(args(1, 4096, sms + 9, d_scratch=where, scratch_bytes=n), buf, 256) == B.TCU_ERR_WORKSPACE
+
+
 def test_empty_calls():
     decay = torch.zeros(2, device="cuda")
     empty = torch.empty((0, 5, 2, 64), dtype=torch.bfloat16, device="cuda")
