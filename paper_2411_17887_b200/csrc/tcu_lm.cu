@@ -138,8 +138,8 @@ cudaLaunchConfig_t mix_config(uint32_t blocks, uint32_t ranks, cudaLaunchAttribu
 // Into how many parts a walk is split, over the blocks of a cluster, when there are few.  A block fills an SM, and clusters of r
 // blocks fill the SMs worse the larger r is (clusters of 8: 15 at a time, 120 blocks of 148).  In units of a group of the walk,
 // 3.4 us: a group of the first phase takes 0.65, the exchange of states and the second start 3.  `groups` of an average walk.
-// Measured: 16 heads of 8191 tokens at D = 128: 1 rank 204 us, 2 176, 3 123, 4 103, 5 86, 6 75 (taken), 8 119 (two waves); the
-// three walks of 64 heads of 4096 tokens: 1 rank 316 us (taken), 2 387, 4 457.
+// Measured: 16 heads of 8191 tokens at D = 128: 1 rank 204 us, 2 176, 3 123, 4 103, 5 86, 6 75 (taken), 8 119 (two waves); outputs and
+// gradients of 64 heads of 4096 tokens, whole walks: 1 rank 316 us, 2 387, 4 457.
 template <int D, typename T>
 tcu_status_t choose_ranks(uint64_t units, uint64_t groups, uint32_t *ranks) {
     static std::atomic<int> configured{-1};
@@ -173,13 +173,14 @@ tcu_status_t choose_ranks(uint64_t units, uint64_t groups, uint32_t *ranks) {
 
 // More walks than SMs: whether they are cut into equal shares of all the groups, one for each SM, with the state handed from
 // block to block, instead of running whole in waves of which the last is not full.  In units of a group: a walk costs one more to
-// begin, shares about ten more in all (three walks begun instead of two, and 148 blocks at once wait longer for memory than fewer).
-// Measured at D = 128: the gradients of 64 heads of 4096 tokens, 192 walks, 210 us whole, 170 cut; the outputs of 256 heads of
-// 4096 tokens 237 whole, 238 cut (whole).  Packed sequences differ in length: cut as well, 24 of them with 12 heads took 164 us
-// where whole walks took 153, and 137 with the long ones first.
+// begin, the shares about four more in all.  Measured, bfloat16, whole against cut: gradients of 64 heads of 4096 tokens at
+// 128 x 128 (192 walks) 210 us, 163; outputs of 200 heads of 2048 tokens 121, 102; of 170 heads of 8192 tokens 412, 286; of 160 heads
+// of 1024 tokens at 64 x 64 51, 39; gradients of 250 heads of 300 tokens 89, 94 (whole).  Packed sequences differ in length, and a
+// long one is as long in parts that wait for one another: cut as well, 24 of them with 12 heads took 164 us where whole
+// walks took 153, and 138 with the long ones first.
 bool cut_pays(const tcu_linattn_t *a, uint32_t jobs) {
     const uint64_t units = a->batch * a->heads * jobs, sms = uint64_t(sm_count()), places = (a->tokens + kGroup - 1) / kGroup + 1;
-    return sms > 0 && units > sms && a->tokens > 0 && !a->d_offsets && units * places / sms + 10 < (units + sms - 1) / sms * places;
+    return sms > 0 && units > sms && a->tokens > 0 && !a->d_offsets && units * places / sms + 4 < (units + sms - 1) / sms * places;
 }
 size_t flag_bytes() { return (size_t(sm_count()) * 4 + 255) / 256 * 256; }
 size_t scratch_bytes(const tcu_linattn_t *a, uint32_t jobs) { return cut_pays(a, jobs) ? flag_bytes() + size_t(sm_count()) * a->dk * a->dv * 4 : 0; }
@@ -403,7 +404,8 @@ void launch_lookup(int vec, const void *ids, uint32_t n, const void *table, uint
     const uint32_t packs = d / vec;
     uint32_t tx = 1;
     while (tx < packs && tx < 256) tx <<= 1;
-    const bool many = uint64_t(n) * packs >= uint64_t(256) * 148 * 8;          // enough for every SM with several rows a thread
+    const bool many = uint64_t(n) * packs >= uint64_t(256) * 148 * 8;          // enough for every SM with several rows a thread (at this size the same
+                                                                               // 4.1 us; 32749 rows of 2048, copied: 41 us a row a thread, 32 four)
     const uint32_t rows_each = (many ? 4 : 1) * (256 / tx);
     const dim3 block(tx, 256 / tx), grid((n + rows_each - 1) / rows_each, (packs + tx - 1) / tx);
     auto go = [&](auto kernel) {
@@ -468,7 +470,9 @@ void launch_next(void (*kernel)(P...), dim3 grid, dim3 block, cudaStream_t strea
     (void)cudaLaunchKernelEx(&cfg, kernel, P(args)...);        // the caller asks for the error once, at the end
 }
 
-constexpr uint32_t kMostTilesAdded = 128;       // tiles whose counts every block of the sort adds up by itself
+// Tiles whose counts every block of the sort adds up by itself; more are scanned by a kernel between.  65536 tokens of 64 columns, 64 tiles:
+// 38 us either way; 128 tiles: added 56, scanned 43.
+constexpr uint32_t kMostTilesAdded = 32;
 
 template <typename ID>
 void sort_tokens(const void *ids, uint32_t n, uint32_t rows, const EmbeddingWs &w, uint8_t *ws, cudaStream_t stream, int &out) {
