@@ -112,8 +112,8 @@ _lib.tcu_status_string.restype = ctypes.c_char_p
 
 def _p(x):
     """Device/host pointer of a tensor-like (``data_ptr()``), an int, or None."""
-    if x is None:
-        return None
+    if x is None or type(x) is int:
+        return x
     if hasattr(x, "data_ptr"):
         return x.data_ptr()
     return int(x)

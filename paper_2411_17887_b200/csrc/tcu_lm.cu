@@ -210,7 +210,8 @@ tcu_status_t launch_mix(const tcu_linattn_t *a, MixParams &p, uint64_t groups, c
         attr.id = cudaLaunchAttributeCooperative;          // blocks wait for one another: all of them run at once
         attr.val.cooperative = 1;
         cfg.numAttrs = 1;
-        return launch_kind<D, T, kCut>(p, cfg);
+        if (launch_kind<D, T, kCut>(p, cfg) == TCU_OK) return TCU_OK;
+        (void)cudaGetLastError();                          // not all SMs are this process's to use: whole walks
     }
     if (tcu_status_t st = choose_ranks<D, T>(units, groups, &p.ranks)) return st;
     const cudaLaunchConfig_t cfg = mix_config<D, T>(units * p.ranks, p.ranks, &attr, stream);

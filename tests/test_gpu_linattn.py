@@ -240,6 +240,25 @@ def test_packed_and_more_walks_than_multiprocessors(dtype, seed):
                        [part(x) for x in grads[:3]] + [grads[3][i:i + 1]])
 
 
+def test_cut_walks_on_two_streams_and_in_a_graph():
+    q, k, v, _, decay, s0, _ = draw(91, 2, 700, 80, 32, 64, torch.bfloat16, True)
+    want = api.linear_attention(q, k, v, decay, initial_state=s0, output_final_state=True)
+    torch.cuda.synchronize()
+    sides, got = [torch.cuda.Stream(), torch.cuda.Stream()], []
+    for _ in range(5):
+        for side in sides:                              # each call has scratch memory of its own
+            with torch.cuda.stream(side):
+                got.append(api.linear_attention(q, k, v, decay, initial_state=s0, output_final_state=True))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got.append(api.linear_attention(q, k, v, decay, initial_state=s0, output_final_state=True))
+    for _ in range(3):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for one in got for a, b in zip(one, want))
+
+
 def test_scratch_sizes_and_refusals():
     """Scratch memory is asked for where many walks leave a last wave short of blocks, and has to be as large as asked for."""
     from paper_2411_17887_b200 import binding as B
