@@ -789,6 +789,16 @@ struct Mix {
         tmem_st_wait();
     }
 
+    // One thread, while the block is being set up: the first group's tiles on their way into L2, and with them the descriptors.
+    static __device__ __forceinline__ void first_tiles(const CUtensorMap *maps, const MixJob &job, const MixPart &part, int token, int b, int h) {
+        if (part.first >= part.last) return;
+        const int at = token + int(part.in_time(part.first) * kGroup);
+#pragma unroll
+        for (int which = 0; which < 3; ++which)
+#pragma unroll
+            for (int half = 0; half < D / 64; ++half)
+                tma_prefetch_l2_4d(maps + job.map[which], half * 64, at, h * int(job.by_head[which]), b * int(job.by_batch[which]));
+    }
     // ---- loads (one thread): K and V of the groups of the first phase; K, Q and V of those of the walk
     static __device__ __noinline__ void loads(const CUtensorMap *maps, uint32_t phase) {
         MixCtl *ctl = mix_ctl();
@@ -1048,6 +1058,7 @@ __global__ void __launch_bounds__(kMixThreads, 1) tcu_linattn_mix_kernel(const _
             part.per = (part.groups + ranks - 1) / ranks;
             part.first = min(rank * part.per, part.groups);
             part.last = min((rank + 1) * part.per, part.groups);
+            if (warp == kProducerWarp && lane == 0) M::first_tiles(p.map, job, part, int(begin), p.offsets ? 0 : int(b), int(h));
             if (threadIdx.x == 0) M::take(p, part, work % p.jobs, b, h, begin, rank, false);
             M::tables(fmaxf(p.log_decay[h] * 1.4426950408889634f, -1e30f), part.lead, job.in_scale * job.out_scale, part);
             allocate();
