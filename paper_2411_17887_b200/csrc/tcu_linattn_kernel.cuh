@@ -142,6 +142,7 @@ struct MixCtl {
     bool none, settle;                   // no walk was left; the block goes on with another: nothing may be under way when this one ends
     bool hands;                          // the state is for the next block
     uint32_t sequence;                   // packed, in order: which one
+    bool clipped;                        // dense: a store of a whole group ends where the sequence does
     bool split, entered, owns_last;      // the walk starts from a state (else from zero); its last state is wanted
     float log2_decay;
     float biggest_k[2][8], biggest_x[2][4];      // float16: largest values seen by each warp
@@ -293,7 +294,7 @@ struct Mix {
                 float e = ctl->job.out_scale * ctl->power[max(order, 0) + int(part.lead)];
                 if (kIsHalf) e *= ctl->unscale[(ctl->before + g) & 1];
                 if (g == 0 && !ctl->entered) zero_e(lanes + side * kCols);          // no state: E was not formed
-                if (tokens == kGroup) {
+                if (tokens == kGroup || ctl->clipped) {
                     const uint32_t at = slot_at(ctl, tile) + half_at;
 #pragma unroll
                     for (int c = 0; c < kCols; c += 16) {
@@ -662,6 +663,7 @@ struct Mix {
         ctl->part = part;
         ctl->t0 = uint32_t(begin);
         ctl->b = p.offsets ? 0 : b;
+        ctl->clipped = !p.offsets;
         ctl->h = h;
         ctl->count = count;
         // a split walk has a first phase, over K and V only, in the blocks whose totals later blocks need
@@ -742,19 +744,31 @@ struct Mix {
         }
         if (threadIdx.x >= 256 && threadIdx.x < 264) ctl->rank_decay[threadIdx.x - 256] = exp2f(log2a * part.tokens_of_rank(threadIdx.x - 256));
     }
-    // All threads: which sequence comes `place`-th, the longest first.  (The ring is not in use yet.)
+    // All threads: which sequence comes `place`-th, the longest first.  A thread counts, for one sequence, the longer ones among half of
+    // them, four at a time.  (The ring is not in use yet.)
     static __device__ __noinline__ uint32_t in_order(const int64_t *offsets, uint32_t batch, uint32_t place) {
         MixCtl *ctl = mix_ctl();
-        int64_t *lens = reinterpret_cast<int64_t *>(reinterpret_cast<uint8_t *>(ctl) + kMixCtlBytes);
-        const uint32_t mine = threadIdx.x;
-        if (mine < batch) lens[mine] = offsets[mine + 1] - offsets[mine];
-        __syncthreads();
-        if (mine < batch) {
-            const int64_t len = lens[mine];
-            uint32_t longer = 0;
-            for (uint32_t i = 0; i < batch; ++i) longer += lens[i] > len || (lens[i] == len && i < mine);
-            if (longer == place) ctl->sequence = mine;
+        static_assert(kMixThreads >= 2 * kMostOrdered, "two threads a sequence");
+        uint32_t *lens = reinterpret_cast<uint32_t *>(reinterpret_cast<uint8_t *>(ctl) + kMixCtlBytes), *longer = lens + kMostOrdered;
+        const uint32_t mine = threadIdx.x % kMostOrdered, half = (batch + 7) / 8 * 4;
+        if (threadIdx.x < kMostOrdered) {
+            lens[mine] = mine < batch ? uint32_t(max(offsets[mine + 1] - offsets[mine], int64_t(0))) : 0;
+            longer[mine] = 0;
         }
+        __syncthreads();
+        if (threadIdx.x < 2 * kMostOrdered && mine < batch) {
+            const uint32_t len = lens[mine], from = threadIdx.x < kMostOrdered ? 0 : half, to = min(from + half, (batch + 3) / 4 * 4);
+            uint32_t count = 0;
+#pragma unroll 4
+            for (uint32_t i = from; i < to; i += 4) {
+                const uint4 other = *reinterpret_cast<const uint4 *>(lens + i);
+                count += (other.x > len || (other.x == len && i < mine)) + (other.y > len || (other.y == len && i + 1 < mine)) +
+                         (other.z > len || (other.z == len && i + 2 < mine)) + (other.w > len || (other.w == len && i + 3 < mine));
+            }
+            atomicAdd(&longer[mine], count);
+        }
+        __syncthreads();
+        if (threadIdx.x < batch && longer[mine] == place) ctl->sequence = mine;
         __syncthreads();
         return ctl->sequence;
     }
@@ -959,7 +973,7 @@ struct Mix {
 #pragma unroll 1
         for (uint32_t i = 0; i < n; ++i, tile += 3) {
             if (!mix_wait(ctl, ctl->o_staged, i & 1)) break;
-            if (part.tokens_of(part.first + i) == kGroup) {
+            if (ctl->clipped || part.tokens_of(part.first + i) == kGroup) {
 #pragma unroll
                 for (int half = 0; half < D / 64; ++half)
                     if (uint32_t(half * 64) < ctl->job.dv)
