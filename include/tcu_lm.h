@@ -63,7 +63,8 @@ typedef struct {
     const float *d_dstate_out;  /* backward: NULL (zero), or the gradient with respect to the state after the last token */
     float *d_dstate_in;         /* backward: NULL, or receives the gradient with respect to the state before the first */
     void *d_scratch;            /* forward and backward: NULL, or tcu_linattn_scratch_bytes() of 256-byte aligned memory, with
-                                   which many heads are spread evenly over the SMs; needs no clearing; not to be shared by
+                                   which many heads, or packed sequences of different lengths, are
+                                   spread evenly over the SMs; needs no clearing; not to be shared by
                                    calls that may overlap                                                           */
     uint64_t scratch_bytes;     /* size of it                                                                       */
 } tcu_linattn_t;

@@ -96,8 +96,9 @@ struct alignas(64) MixParams {
     // walks cut where a block's share of all the groups ends: by block, a flag and the state that it hands to the next one
     uint32_t *flags;
     float *handed;
+    const uint32_t *order;               // packed, long sequences first: which one comes where
 };
-constexpr uint32_t kMostOrdered = 256;   // sequences that are put in order
+constexpr uint32_t kMostOrdered = 512;   // sequences that are put in order
 
 // Which groups of a walk a block takes, and how many tokens.
 struct MixPart {
@@ -141,7 +142,6 @@ struct MixCtl {
     uint64_t places_from, places_to;     // what is left of the block's share
     bool none, settle;                   // no walk was left; the block goes on with another: nothing may be under way when this one ends
     bool hands;                          // the state is for the next block
-    uint32_t sequence;                   // packed, in order: which one
     bool clipped;                        // dense: a store of a whole group ends where the sequence does
     bool split, entered, owns_last;      // the walk starts from a state (else from zero); its last state is wanted
     float log2_decay;
@@ -744,34 +744,6 @@ struct Mix {
         }
         if (threadIdx.x >= 256 && threadIdx.x < 264) ctl->rank_decay[threadIdx.x - 256] = exp2f(log2a * part.tokens_of_rank(threadIdx.x - 256));
     }
-    // All threads: which sequence comes `place`-th, the longest first.  A thread counts, for one sequence, the longer ones among half of
-    // them, four at a time.  (The ring is not in use yet.)
-    static __device__ __noinline__ uint32_t in_order(const int64_t *offsets, uint32_t batch, uint32_t place) {
-        MixCtl *ctl = mix_ctl();
-        static_assert(kMixThreads >= 2 * kMostOrdered, "two threads a sequence");
-        uint32_t *lens = reinterpret_cast<uint32_t *>(reinterpret_cast<uint8_t *>(ctl) + kMixCtlBytes), *longer = lens + kMostOrdered;
-        const uint32_t mine = threadIdx.x % kMostOrdered, half = (batch + 7) / 8 * 4;
-        if (threadIdx.x < kMostOrdered) {
-            lens[mine] = mine < batch ? uint32_t(max(offsets[mine + 1] - offsets[mine], int64_t(0))) : 0;
-            longer[mine] = 0;
-        }
-        __syncthreads();
-        if (threadIdx.x < 2 * kMostOrdered && mine < batch) {
-            const uint32_t len = lens[mine], from = threadIdx.x < kMostOrdered ? 0 : half, to = min(from + half, (batch + 3) / 4 * 4);
-            uint32_t count = 0;
-#pragma unroll 4
-            for (uint32_t i = from; i < to; i += 4) {
-                const uint4 other = *reinterpret_cast<const uint4 *>(lens + i);
-                count += (other.x > len || (other.x == len && i < mine)) + (other.y > len || (other.y == len && i + 1 < mine)) +
-                         (other.z > len || (other.z == len && i + 2 < mine)) + (other.w > len || (other.w == len && i + 3 < mine));
-            }
-            atomicAdd(&longer[mine], count);
-        }
-        __syncthreads();
-        if (threadIdx.x < batch && longer[mine] == place) ctl->sequence = mine;
-        __syncthreads();
-        return ctl->sequence;
-    }
     // the state that enters the walk
     template <bool CUT>
     static __device__ __noinline__ void enter() {
@@ -1025,6 +997,25 @@ struct Mix {
     }
 };
 
+// The places of packed sequences, the longest first: thread i counts the sequences that come before sequence i, four at a time.
+// (One block: found by every block of the walk for itself, this cost each of them 2.4 us with 200 sequences.)
+__global__ void __launch_bounds__(kMostOrdered) tcu_linattn_order_kernel(const int64_t *offsets, uint32_t batch, uint32_t *order) {
+    __shared__ alignas(16) uint32_t lens[kMostOrdered];
+    begin_in_sequence();
+    const uint32_t mine = threadIdx.x, len = mine < batch ? uint32_t(max(offsets[mine + 1] - offsets[mine], int64_t(0))) : 0;
+    lens[mine] = len;
+    __syncthreads();
+    if (mine >= batch) return;
+    uint32_t before = 0;
+#pragma unroll 4
+    for (uint32_t i = 0; i < batch; i += 4) {
+        const uint4 other = *reinterpret_cast<const uint4 *>(lens + i);
+        before += (other.x > len || (other.x == len && i < mine)) + (other.y > len || (other.y == len && i + 1 < mine)) +
+                  (other.z > len || (other.z == len && i + 2 < mine)) + (other.w > len || (other.w == len && i + 3 < mine));
+    }
+    order[before] = mine;
+}
+
 // kWhole: a block, or a cluster of them, has one walk; kOrdered: the same with the walks of long sequences first; kCut: a block has
 // a share of all walks, which begins and ends anywhere.  (A kernel that does the one or the other costs small calls 1 to 2 us.)
 enum { kWhole, kOrdered, kCut };
@@ -1061,7 +1052,10 @@ __global__ void __launch_bounds__(kMixThreads, 1) tcu_linattn_mix_kernel(const _
         } else {
             const uint32_t work = blockIdx.x / ranks, unit = work / p.jobs, h = unit % p.heads;
             uint32_t b = unit / p.heads;
-            if (KIND == kOrdered) b = M::in_order(p.offsets, p.batch, b);
+            if (KIND == kOrdered) {
+                begin_in_sequence();
+                b = p.order[b];
+            }
             const MixJob &job = p.job[work % p.jobs];
             // packed: whatever the offsets hold, no token outside the arrays is touched
             const int64_t most = int64_t(p.tokens), begin = p.offsets ? min(max(p.offsets[b], int64_t(0)), most) : 0;

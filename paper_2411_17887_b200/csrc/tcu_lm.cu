@@ -177,13 +177,21 @@ tcu_status_t choose_ranks(uint64_t units, uint64_t groups, uint32_t *ranks) {
 // 128 x 128 (192 walks) 210 us, 163; outputs of 200 heads of 2048 tokens 121, 102; of 170 heads of 8192 tokens 412, 286; of 160 heads
 // of 1024 tokens at 64 x 64 51, 39; gradients of 250 heads of 300 tokens 89, 94 (whole).  Packed sequences differ in length, and a
 // long one is as long in parts that wait for one another: cut as well, 24 of them with 12 heads took 164 us where whole
-// walks took 153, and 138 with the long ones first.
+// walks took 153, and 137 with the long ones first.
 bool cut_pays(const tcu_linattn_t *a, uint32_t jobs) {
     const uint64_t units = a->batch * a->heads * jobs, sms = uint64_t(sm_count()), places = (a->tokens + kGroup - 1) / kGroup + 1;
     return sms > 0 && units > sms && a->tokens > 0 && !a->d_offsets && units * places / sms + 4 < (units + sms - 1) / sms * places;
 }
+// More walks than SMs of packed sequences: the long ones first, in an order found by a kernel ahead.  Measured, bfloat16: 64 sequences
+// of 50 to 3000 tokens with 16 heads 268 us as they come, 239 in order; one of 4000 after 31 of 100 with 12 heads 123, 107; 200 of 60 with
+// 16 heads, where no order helps, 174, 179.
+bool order_pays(const tcu_linattn_t *a, uint32_t jobs) {
+    return a->d_offsets && a->tokens > 0 && a->batch > 1 && a->batch <= kMostOrdered && a->batch * a->heads * jobs > uint64_t(sm_count());
+}
 size_t flag_bytes() { return (size_t(sm_count()) * 4 + 255) / 256 * 256; }
-size_t scratch_bytes(const tcu_linattn_t *a, uint32_t jobs) { return cut_pays(a, jobs) ? flag_bytes() + size_t(sm_count()) * a->dk * a->dv * 4 : 0; }
+size_t scratch_bytes(const tcu_linattn_t *a, uint32_t jobs) {
+    return cut_pays(a, jobs) ? flag_bytes() + size_t(sm_count()) * a->dk * a->dv * 4 : order_pays(a, jobs) ? kMostOrdered * 4 : 0;
+}
 
 template <int D, typename T, int KIND>
 tcu_status_t launch_kind(const MixParams &p, const cudaLaunchConfig_t &cfg) {
@@ -199,14 +207,14 @@ tcu_status_t launch_kind(const MixParams &p, const cudaLaunchConfig_t &cfg) {
 
 template <int D, typename T>
 tcu_status_t launch_mix(const tcu_linattn_t *a, MixParams &p, uint64_t groups, cudaStream_t stream) {
-    const uint32_t units = p.batch * p.heads * p.jobs, sms = uint32_t(sm_count());
+    const uint32_t units = p.batch * p.heads * p.jobs;
     cudaLaunchAttribute attr;
     if (a->d_scratch && cut_pays(a, p.jobs)) {
         p.ranks = 1;
         p.flags = static_cast<uint32_t *>(a->d_scratch);
         p.handed = reinterpret_cast<float *>(static_cast<uint8_t *>(a->d_scratch) + flag_bytes());
         if (cudaMemsetAsync(p.flags, 0, flag_bytes(), stream) != cudaSuccess) return TCU_ERR_CUDA;
-        cudaLaunchConfig_t cfg = mix_config<D, T>(sms, 1, &attr, stream);
+        cudaLaunchConfig_t cfg = mix_config<D, T>(uint32_t(sm_count()), 1, &attr, stream);
         attr.id = cudaLaunchAttributeCooperative;          // blocks wait for one another: all of them run at once
         attr.val.cooperative = 1;
         cfg.numAttrs = 1;
@@ -215,8 +223,16 @@ tcu_status_t launch_mix(const tcu_linattn_t *a, MixParams &p, uint64_t groups, c
     }
     if (tcu_status_t st = choose_ranks<D, T>(units, groups, &p.ranks)) return st;
     const cudaLaunchConfig_t cfg = mix_config<D, T>(units * p.ranks, p.ranks, &attr, stream);
-    // (an order costs a look at all lengths; it matters where blocks come in waves)
-    if (p.offsets && p.ranks == 1 && p.batch > 1 && p.batch <= kMostOrdered && units > sms) return launch_kind<D, T, kOrdered>(p, cfg);
+    if (a->d_scratch && p.ranks == 1 && order_pays(a, p.jobs)) {
+        uint32_t *order = static_cast<uint32_t *>(a->d_scratch);
+        tcu_linattn_order_kernel<<<1, kMostOrdered, 0, stream>>>(p.offsets, p.batch, order);
+        p.order = order;
+        cudaLaunchConfig_t next = cfg;
+        attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr.val.programmaticStreamSerializationAllowed = 1;
+        next.numAttrs = 1;
+        return launch_kind<D, T, kOrdered>(p, next);
+    }
     return launch_kind<D, T, kWhole>(p, cfg);
 }
 
