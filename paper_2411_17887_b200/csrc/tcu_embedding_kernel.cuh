@@ -11,8 +11,8 @@
 // row v follows the last of its tokens, and the list is cut into equal pieces: a piece costs about the same whether it
 // holds rows without tokens (a store of zeros each) or the many tokens of one row.  A row whose tokens end in a later
 // piece leaves a partial sum, and a last kernel adds the partial sums of such rows in order.  65536 skewed tokens of 1024
-// bfloat16 columns into 50000 float32 rows: 92 us, of which the sort 16 (16384 tokens or 4 tiles: 12; bound by the latency of
-// what its four launches read), the cuts 3, the sums 60 (339 MB, 5.6 TB/s; reading 134 MB and then clearing 205 takes 66)
+// bfloat16 columns into 50000 float32 rows: 92 us, of which the sort 16 (bound by the latency of what its four
+// launches read), the cuts 3, the sums 60 (339 MB, 5.6 TB/s; reading 134 MB and then clearing 205 takes 66)
 // and the join 9.
 #pragma once
 
@@ -270,6 +270,94 @@ __global__ void __launch_bounds__(kSortThreads) tcu_sort_scatter_kernel(const ID
     }
 }
 
+// All passes of the sort in one block, for up to kBlockTokens tokens: 1024 threads of 4 tokens, which stay in shared memory between
+// the passes.  Gradient of 1025 tokens of 500 columns into 4099 rows 19 us (23 by the launches above), 4096 tokens of 1024 27 (27);
+// with 8 tokens a thread 8192 tokens of 256 took 37 us, 30 by launches.
+constexpr uint32_t kBlockTokens = 4096;
+constexpr int kBlockThreads = 1024, kBlockRounds = kBlockTokens / kBlockThreads, kBlockWarps = kBlockThreads / 32;
+struct BlockSort {
+    uint32_t keys[kBlockTokens];
+    uint16_t tokens[kBlockTokens];
+    uint16_t seen[kBlockWarps][kDigits];               // tokens of a digit in a warp, then in the warps before it
+    uint32_t base[kDigits], warp_sum[kBlockWarps];
+};
+template <typename ID>
+__global__ void __launch_bounds__(kBlockThreads) tcu_sort_block_kernel(const ID *__restrict__ ids, uint32_t n, uint32_t rows, int bits, uint32_t *keys_out,
+                                                                       uint32_t *tokens_out, uint32_t *joins) {
+    extern __shared__ BlockSort block_sort[];
+    BlockSort &s = block_sort[0];
+    const uint32_t t = threadIdx.x, lane = t & 31, warp = t >> 5, first = warp * (32 * kBlockRounds) + lane;
+    begin_in_sequence();
+    if (t == 0) *joins = 0;
+    uint32_t key[kBlockRounds], token[kBlockRounds], rank[kBlockRounds];
+#pragma unroll
+    for (int r = 0; r < kBlockRounds; ++r) {
+        token[r] = first + r * 32;
+        key[r] = token[r] < n ? row_of(ids, token[r], rows) : 0;
+    }
+    for (int shift = 0; shift < bits; shift += kDigitBits) {
+        for (uint32_t i = t; i < kBlockWarps * kDigits / 2; i += kBlockThreads) reinterpret_cast<uint32_t *>(&s.seen[0][0])[i] = 0;
+        __syncthreads();
+        // tokens of one digit find one another by a match
+#pragma unroll
+        for (int r = 0; r < kBlockRounds; ++r) {
+            const bool valid = first + r * 32 < n;
+            const uint32_t digit = valid ? (key[r] >> shift) & (kDigits - 1) : uint32_t(kDigits);
+            const uint32_t same = __match_any_sync(0xffffffffu, digit);
+            const uint32_t ahead = __popc(same & ((1u << lane) - 1));
+            const uint32_t old = valid ? s.seen[warp][digit] : 0;
+            __syncwarp();
+            if (valid && ahead == 0) s.seen[warp][digit] = uint16_t(old + __popc(same));
+            __syncwarp();
+            rank[r] = old + ahead;
+        }
+        __syncthreads();
+        uint32_t total = 0;                            // of digit t
+        if (t < kDigits) {
+#pragma unroll 8
+            for (int w = 0; w < kBlockWarps; ++w) {
+                const uint32_t c = s.seen[w][t];
+                s.seen[w][t] = uint16_t(total);
+                total += c;
+            }
+        }
+        uint32_t sum = total;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t u = __shfl_up_sync(0xffffffffu, sum, o);
+            if (lane >= uint32_t(o)) sum += u;
+        }
+        if (lane == 31) s.warp_sum[warp] = sum;
+        __syncthreads();
+        if (t < kDigits) {
+            uint32_t before = sum - total;
+            for (uint32_t w = 0; w < warp; ++w) before += s.warp_sum[w];
+            s.base[t] = before;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < kBlockRounds; ++r) {
+            if (first + r * 32 >= n) continue;
+            const uint32_t digit = (key[r] >> shift) & (kDigits - 1), to = s.base[digit] + s.seen[warp][digit] + rank[r];
+            s.keys[to] = key[r];
+            s.tokens[to] = uint16_t(token[r]);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < kBlockRounds; ++r) {
+            if (first + r * 32 >= n) continue;
+            key[r] = s.keys[first + r * 32];
+            token[r] = s.tokens[first + r * 32];
+        }
+    }
+#pragma unroll
+    for (int r = 0; r < kBlockRounds; ++r) {
+        if (first + r * 32 >= n) continue;
+        keys_out[first + r * 32] = key[r];
+        tokens_out[first + r * 32] = token[r];
+    }
+}
+
 // ---- segmented sum -------------------------------------------------------------------------------------------------
 struct SumParams {
     const uint32_t *keys, *tokens;     // sorted: row (or `rows` for a token that is left out) and token
@@ -481,9 +569,9 @@ __global__ void __launch_bounds__(128) tcu_embedding_join_kernel(TT *__restrict_
 }
 
 // ---- few tokens ----------------------------------------------------------------------------------------------------
-// Measured, bfloat16 to float32, skewed ids: 1024 tokens of 500 columns into 4099 rows 12 us, by the sort 22; of 1024 columns
-// into 4000 rows 14 against 24, 16000 rows 26 against 32, 32000 rows 65 against 44: rows reach memory out of order from
-// here, which is slow once the table does not stay in L2.  All tokens in one row: 25 us against 20.
+// Measured, bfloat16 to float32, skewed ids: 1024 tokens of 500 columns into 4099 rows 12 us, by the sort 19; of 1024 columns
+// into 4000 rows 15 against 22, 16000 rows 27 against 29, 32000 rows 42 to 65 (by device) against 45: rows reach memory out of
+// order from here, which can be slow once the table does not stay in L2.  All tokens in one row: 25 us against 18.
 constexpr uint32_t kFewTokens = 1024;      // at most
 constexpr uint64_t kFewElements = uint64_t(1) << 24;       // of the table, at most
 constexpr uint32_t kFewRows = 256;         // rows of a block, at most

@@ -489,7 +489,7 @@ void launch_next(void (*kernel)(P...), dim3 grid, dim3 block, cudaStream_t strea
 
 // Tiles whose counts every block of the sort adds up by itself; more are scanned by a kernel between.  65536 tokens of 64 columns, 64 tiles:
 // 38 us either way; 128 tiles: added 56, scanned 43.
-constexpr uint32_t kMostTilesAdded = 32;
+constexpr uint32_t kMostTilesAdded = 64;
 
 template <typename ID>
 void sort_tokens(const void *ids, uint32_t n, uint32_t rows, const EmbeddingWs &w, uint8_t *ws, cudaStream_t stream, int &out) {
@@ -499,6 +499,17 @@ void sort_tokens(const void *ids, uint32_t n, uint32_t rows, const EmbeddingWs &
     const uint32_t *keys = nullptr, *tokens = nullptr;
     const ID *id = static_cast<const ID *>(ids);
     out = 0;
+    if (n <= kBlockTokens) {
+        static std::atomic<int> configured{-1};
+        int dev = 0;
+        if (cudaGetDevice(&dev) != cudaSuccess) return;
+        if (configured.load() != dev) {
+            if (cudaFuncSetAttribute(tcu_sort_block_kernel<ID>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(sizeof(BlockSort))) != cudaSuccess) return;
+            configured.store(dev);
+        }
+        tcu_sort_block_kernel<ID><<<1, kBlockThreads, sizeof(BlockSort), stream>>>(id, n, rows, bits, at(w.keys[0]), at(w.tokens[0]), at(w.joins));
+        return;
+    }
     for (int shift = 0; shift < bits; shift += kDigitBits) {
         if (shift == 0) tcu_sort_count_kernel<ID><<<w.tiles, kSortThreads, 0, stream>>>(id, keys, n, rows, shift, at(w.counts), at(w.joins));
         else launch_next(tcu_sort_count_kernel<ID>, w.tiles, kSortThreads, stream, id, keys, n, rows, shift, at(w.counts), nullptr);

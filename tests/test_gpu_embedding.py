@@ -90,7 +90,7 @@ def test_table_gradient(kind, n, rows, d, dtype, table_type):
 
 @pytest.mark.parametrize("dtype,table_type", [(torch.bfloat16, torch.float32), (torch.float16, torch.float16)], ids=str)
 @pytest.mark.parametrize("kind,n,rows,d", [
-    ("uniform", 1024, 4000, 40), ("uniform", 1025, 900, 264), ("skewed", 30, 70000, 240), ("outside", 4097, 511, 33), ("uniform", 8193, 20, 8), ("skewed", 12289, 30000, 136), ("one", 9000, 70000, 1100),
+    ("uniform", 1024, 4000, 40), ("one", 8192, 300, 16), ("outside", 8191, 520, 12), ("skewed", 2000, 300000, 8), ("uniform", 8193, 30000, 12), ("uniform", 1025, 900, 264), ("one", 4096, 300, 16), ("skewed", 30, 70000, 240), ("outside", 4097, 511, 33), ("uniform", 8193, 20, 8), ("skewed", 12289, 30000, 136), ("one", 9000, 70000, 1100),
     ("uniform", 5000, 300000, 4), ("skewed", 270000, 5000, 6), ("outside", 300001, 600, 3)])
 def test_table_gradient_of_many_tokens(kind, n, rows, d, dtype, table_type):
     """Either side of the tokens that one launch takes; one, two and three passes of the sort; counts added and scanned."""
