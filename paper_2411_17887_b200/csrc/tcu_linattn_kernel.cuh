@@ -140,7 +140,7 @@ struct MixCtl {
     const uint32_t *wait_flag;           // NULL, or set once the state that enters has been handed over
     uint64_t patience;                   // nanoseconds to wait for that
     uint64_t places_from, places_to;     // what is left of the block's share
-    bool none, settle;                   // no walk was left; the block goes on with another: nothing may be under way when this one ends
+    bool none, more;                     // no walk was left; the block goes on with another
     bool hands;                          // the state is for the next block
     bool clipped;                        // dense: a store of a whole group ends where the sequence does
     bool split, entered, owns_last;      // the walk starts from a state (else from zero); its last state is wanted
@@ -702,14 +702,14 @@ struct Mix {
         } while (part.first == part.groups);         // only the place for its beginning: there is nothing to do
         const uint32_t unit = uint32_t(walk / p.jobs), job = uint32_t(walk - uint64_t(unit) * p.jobs);
         part.lead = p.job[job].lead != 0;
-        ctl->settle = to > lo;
+        ctl->more = to > lo;
         ctl->places_to = to;
         take(p, part, job, unit / p.heads, unit % p.heads, 0, 0, true);
     }
     // Whether there is another walk (all threads); if so, its barriers may be set up.
     static __device__ __forceinline__ bool goes_on() {
         MixCtl *ctl = mix_ctl();
-        if (!ctl->settle || ctl->abort_flag) return false;
+        if (!ctl->more || ctl->abort_flag) return false;
         if (threadIdx.x == 32 * kProducerWarp)
             for (uint64_t *one = &ctl->full[0]; one <= &ctl->drained[1]; ++one)
                 if (one < &ctl->full[kSlots] || (one >= &ctl->empty[0] && one < &ctl->empty[kSlots]) || one >= &ctl->qk_done) mbar_inval(smem_u32(one));
@@ -815,7 +815,7 @@ struct Mix {
                 ++group;
             }
         }
-        if (phase && ctl->settle)
+        if (phase)                                  // commits that free the last tiles arrive on barriers of this block: not after it has ended
             for (uint32_t m = tile > kSlots ? tile - kSlots : 0; m < tile && !ctl->abort_flag; ++m) mix_wait(ctl, ctl->empty[m % kSlots], (m / kSlots) & 1);
         if (ctl->abort_flag)                        // copies in flight must land before the block may exit
             for (uint32_t m = tile > kSlots ? tile - kSlots : 0; m < tile; ++m)
@@ -932,7 +932,8 @@ struct Mix {
             }
             __syncwarp();
         }
-        if (phase && ctl->settle && n > 0 && !ctl->abort_flag) mix_wait_warp(ctl, ctl->kv_done, (it - 1) & 1);
+        // (the last one is not waited for by anybody else when no state is wanted; the first phase's is, by the state role)
+        if (phase && n > 0 && !ctl->abort_flag) mix_wait_warp(ctl, ctl->kv_done, (it - 1) & 1);
         drain(ctl, 1);
     }
 
@@ -1033,7 +1034,7 @@ __global__ void __launch_bounds__(kMixThreads, 1) tcu_linattn_mix_kernel(const _
             ctl->places_from = places * blockIdx.x / gridDim.x;
             ctl->places_to = places * (blockIdx.x + 1) / gridDim.x;
         }
-        ctl->settle = false;
+        ctl->more = false;
     }
     auto allocate = [&] {
         if (warp != kProductWarp) return;
