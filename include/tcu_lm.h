@@ -92,6 +92,14 @@ tcu_status_t tcu_linattn_forward(const tcu_linattn_t *args, void *d_ws, size_t w
  * The decays are constants of the model: no gradient with respect to them is computed. */
 tcu_status_t tcu_linattn_backward(const tcu_linattn_t *args, void *d_ws, size_t ws_bytes, cudaStream_t stream);
 
+/* Self-test of the ways in which these calls give up (compare tcu_scan_selftest_timeout): the ordinary forward (or backward) call,
+ * except that group `silent_group` (128 tokens each, counted from 0 as the block that walks them comes to them) of every walk never
+ * reports its part of the state as done, and that every device-side wait gives up after `limit_ms` milliseconds (1..1000)
+ * instead of about a second.  The kernel winds down and returns; after the stream has drained, tcu_scan_device_status(d_ws) is
+ * TCU_ERR_TIMEOUT if any walk has so many groups, outputs and states are not valid, and tcu_scan_workspace_init clears the condition. */
+tcu_status_t tcu_linattn_selftest_timeout(const tcu_linattn_t *args, int backward, uint32_t silent_group, unsigned limit_ms, void *d_ws,
+                                          size_t ws_bytes, cudaStream_t stream);
+
 /* One token for each of `batch` sequences: the state of each (an entry of the pool d_state_out, (pool_slots, heads, dk, dv)) is
  * updated in place, and o written.  q, k, v, o: stride_token is not used; any alignment of elements.  The pool: 16-byte
  * aligned.  Needs no workspace. */

@@ -98,6 +98,8 @@ _lib.tcu_linattn_forward.argtypes = [ctypes.c_char_p, _vp, _sz, _vp]
 _lib.tcu_linattn_forward.restype = _int
 _lib.tcu_linattn_backward.argtypes = [ctypes.c_char_p, _vp, _sz, _vp]
 _lib.tcu_linattn_backward.restype = _int
+_lib.tcu_linattn_selftest_timeout.argtypes = [ctypes.c_char_p, _int, ctypes.c_uint32, ctypes.c_uint, _vp, _sz, _vp]
+_lib.tcu_linattn_selftest_timeout.restype = _int
 _lib.tcu_linattn_step.argtypes = [ctypes.c_char_p, _vp]
 _lib.tcu_linattn_step.restype = _int
 _lib.tcu_embedding_forward.argtypes = [_vp, _int, _sz, _vp, _sz, _sz, _sz, _int, _f32, _vp, _vp]
@@ -258,6 +260,10 @@ def tcu_linattn_forward(args: bytes, d_ws, ws_bytes: int, stream=0) -> int:
 
 def tcu_linattn_backward(args: bytes, d_ws, ws_bytes: int, stream=0) -> int:
     return _lib.tcu_linattn_backward(args, _p(d_ws), ws_bytes, stream)
+
+
+def tcu_linattn_selftest_timeout(args: bytes, backward: int, silent_group: int, limit_ms: int, d_ws, ws_bytes: int, stream=0) -> int:
+    return _lib.tcu_linattn_selftest_timeout(args, backward, silent_group, limit_ms, _p(d_ws), ws_bytes, stream)
 
 
 def tcu_linattn_step(args: bytes, stream=0) -> int:

@@ -47,7 +47,9 @@
 // Measured, bfloat16 at D = 128: 256 heads of 4096 tokens, 1.08 GB, 225 to 240 us (4.5 to 4.8 TB/s; 3.7 us a group with all SMs in
 // use); 148 heads of 2048 tokens: 50 % of the memory's time and 37 % of the tensor pipe's.  One group takes 8.8 us with the launch.
 //
-// Every wait is bounded; one that runs out records TCU_ERR_TIMEOUT in the workspace and the block winds down.
+// Every wait is bounded; one that runs out records TCU_ERR_TIMEOUT in the workspace and the block winds down: each role returns at
+// its next wait that fails, the producer after its copies have landed, the issuers after their products have ended (drain), and a
+// block whose first phase was given up leaves the second out.  tcu_linattn_selftest_timeout takes these ways.
 #pragma once
 
 #include <cuda.h>
@@ -97,6 +99,8 @@ struct alignas(64) MixParams {
     uint32_t *flags;
     float *handed;
     const uint32_t *order;               // packed, long sequences first: which one comes where
+    uint32_t rounds;                     // tries of 100 us after which a wait is given up
+    uint32_t silent;                     // self-test: 0, or 1 + the group of every walk whose part of the state is never announced
 };
 constexpr uint32_t kMostOrdered = 512;   // sequences that are put in order
 
@@ -133,6 +137,7 @@ struct MixCtl {
     uint64_t drained[2];
     uint32_t tmem_base;
     volatile uint32_t abort_flag;
+    uint32_t rounds, silent;             // as in MixParams
     MixJob job;                          // what the block works on
     MixPart part;
     uint32_t t0, b, h, count, before;    // first token of the sequence; sequence (0 when packed) and head; groups of the walk, of the first phase
@@ -220,7 +225,7 @@ __device__ __forceinline__ uint64_t global_ns() {
 // Waits for the phase of a barrier; false when the wait was given up, after about a second.
 constexpr uint32_t kMixWaitRounds = 10000;
 __device__ __forceinline__ bool mix_wait(MixCtl *ctl, const uint64_t &barrier, uint32_t parity) {
-    const bool ok = mbar_wait_bounded(smem_u32(&barrier), parity, kMixWaitRounds);
+    const bool ok = mbar_wait_bounded_at(smem_u32(&barrier), parity, smem_u32(&ctl->rounds));
     if (!ok) ctl->abort_flag = 1;
     return ok;
 }
@@ -658,7 +663,7 @@ struct Mix {
         }
         if (hands) ctl->job.last = p.handed + blockIdx.x * size;
         ctl->wait_flag = handed ? p.flags + blockIdx.x - 1 : nullptr;
-        ctl->patience = 1000000000ull + 100000ull * part.first;
+        ctl->patience = 100000ull * p.rounds;
         ctl->hands = hands;
         ctl->part = part;
         ctl->t0 = uint32_t(begin);
@@ -790,9 +795,9 @@ struct Mix {
         MixCtl *ctl = mix_ctl();
         const MixPart part = ctl->part;
         const uint32_t n = phase ? ctl->count : ctl->before;
-        uint32_t tile = phase ? 2 * ctl->before : 0;
+        uint32_t tile = phase ? 2 * ctl->before : 0, group = 0;
 #pragma unroll 1
-        for (uint32_t m = 0, group = 0, place = 0; group < n; ++m, ++tile) {
+        for (uint32_t place = 0; group < n; ++tile) {
             const uint32_t slot = tile % kSlots;
             const uint32_t ahead = group + kAhead;
             if (ahead < n) {                        // into L2, so that a load issued when its slot falls free takes less than the chain leaves it
@@ -815,11 +820,11 @@ struct Mix {
                 ++group;
             }
         }
-        if (phase)                                  // commits that free the last tiles arrive on barriers of this block: not after it has ended
-            for (uint32_t m = tile > kSlots ? tile - kSlots : 0; m < tile && !ctl->abort_flag; ++m) mix_wait(ctl, ctl->empty[m % kSlots], (m / kSlots) & 1);
-        if (ctl->abort_flag)                        // copies in flight must land before the block may exit
-            for (uint32_t m = tile > kSlots ? tile - kSlots : 0; m < tile; ++m)
-                mbar_wait_bounded(smem_u32(&ctl->full[m % kSlots]), (m / kSlots) & 1, kMixWaitRounds);
+        const uint32_t last = tile > kSlots ? tile - kSlots : 0;
+        if (phase && group == n)                    // commits that free the last tiles arrive on barriers of this block: not after it has ended
+            for (uint32_t m = last; m < tile && mix_wait(ctl, ctl->empty[m % kSlots], (m / kSlots) & 1); ++m) {}
+        if (!phase || ctl->abort_flag)              // copies in flight must land before the block may exit, or (from others, in the exchange) write there
+            for (uint32_t m = last; m < tile; ++m) mbar_wait_bounded(smem_u32(&ctl->full[m % kSlots]), (m / kSlots) & 1, kMixWaitRounds);
     }
 
     // ---- products: a whole warp walks the loop, so that descriptors stay in uniform registers; one lane issues
@@ -888,6 +893,7 @@ struct Mix {
         const uint32_t idesc_e = make_idesc(H::kType, D);
         const MixPart part = ctl->part;
         uint32_t it = phase ? ctl->before : 0, tile = 2 * it, thirds = phase ? ctl->thirds : 0;
+        const uint32_t end = it + n, silent = ctl->silent;
 #pragma unroll 1
         for (uint32_t i = 0; i < n; ++i, ++it, tile += phase + 2) {
             const uint32_t nv = tile + phase + 1;
@@ -922,18 +928,20 @@ struct Mix {
             }
             if (elect_one()) {
                 if (third) issue_state(tmem, slot_at(ctl, nv), slot_at(ctl, tile), true);
-                mma_commit(smem_u32(&ctl->kv_done));
-                mma_commit(smem_u32(&ctl->empty[tile % kSlots]));
-                mma_commit(smem_u32(&ctl->empty[nv % kSlots]));
-                if (!phase) {                       // (nobody else uses them)
+                if (it + 1 != silent) {
+                    mma_commit(smem_u32(&ctl->kv_done));
                     mma_commit(smem_u32(&ctl->empty[tile % kSlots]));
                     mma_commit(smem_u32(&ctl->empty[nv % kSlots]));
+                    if (!phase) {                   // (nobody else uses them)
+                        mma_commit(smem_u32(&ctl->empty[tile % kSlots]));
+                        mma_commit(smem_u32(&ctl->empty[nv % kSlots]));
+                    }
                 }
             }
             __syncwarp();
         }
         // (the last one is not waited for by anybody else when no state is wanted; the first phase's is, by the state role)
-        if (phase && n > 0 && !ctl->abort_flag) mix_wait_warp(ctl, ctl->kv_done, (it - 1) & 1);
+        if (phase && n > 0 && it == end) mix_wait_warp(ctl, ctl->kv_done, (it - 1) & 1);
         drain(ctl, 1);
     }
 
@@ -1029,6 +1037,8 @@ __global__ void __launch_bounds__(kMixThreads, 1) tcu_linattn_mix_kernel(const _
     const uint32_t ranks = CUT ? 1 : p.ranks, rank = CUT ? 0 : blockIdx.x % p.ranks;
     if (threadIdx.x == 0) {
         ctl->abort_flag = 0;
+        ctl->rounds = p.rounds;
+        ctl->silent = p.silent;
         if (CUT) {
             const uint64_t places = (uint64_t(p.tokens + kGroup - 1) / kGroup + 1) * p.batch * p.heads * p.jobs;
             ctl->places_from = places * blockIdx.x / gridDim.x;
@@ -1079,6 +1089,8 @@ __global__ void __launch_bounds__(kMixThreads, 1) tcu_linattn_mix_kernel(const _
 #pragma unroll 1
         for (uint32_t phase = ranks > 1 ? 0 : 1; phase < 2; ++phase) {
             if (phase) {
+                // a first phase that was given up left the barriers anywhere: what would wait on them now could take an old phase for a new one
+                if (!CUT && ranks > 1 && ctl->abort_flag) break;
                 if (warp >= kStateWarp && warp < kProducerWarp) M::template enter<CUT>();
                 if (ranks > 1) {
                     fence_proxy_async_smem();                               // the next writes to the exchange buffer are TMA loads

@@ -264,6 +264,7 @@ tcu_status_t run_mix(const tcu_linattn_t *a, MixParams &p, const tcu_tokens_t *c
     bound = dev;
     for (int i = 0; i < count; ++i)
         if (!encode_tokens(&p.map[i], a, *arrays[i], widths[i])) return TCU_ERR_CUDA;
+    if (p.rounds == 0) p.rounds = kMixWaitRounds;
     p.log_decay = a->d_log_decay;
     p.offsets = a->d_offsets;
     p.error = &static_cast<WsStatus *>(d_ws)->error;
@@ -290,6 +291,11 @@ tcu_status_t run_mix(const tcu_linattn_t *a, MixParams &p, const tcu_tokens_t *c
     return wide ? launch_mix<128, __nv_bfloat16>(a, p, groups, stream) : launch_mix<64, __nv_bfloat16>(a, p, groups, stream);
 }
 
+// What a self-test changes: `rounds` and `silent` of MixParams (0: nothing).
+struct Waits {
+    uint32_t rounds, silent;
+};
+
 // No tokens: the state that leaves is the state that enters.
 tcu_status_t copy_state(float *to, const float *from, size_t bytes, cudaStream_t stream) {
     if (!to || to == from) return TCU_OK;
@@ -297,18 +303,7 @@ tcu_status_t copy_state(float *to, const float *from, size_t bytes, cudaStream_t
     return e == cudaSuccess ? TCU_OK : TCU_ERR_CUDA;
 }
 
-}  // namespace
-
-extern "C" {
-
-size_t tcu_linattn_workspace_bytes(void) { return kStatusBytes; }
-
-size_t tcu_linattn_scratch_bytes(const tcu_linattn_t *a, int backward) {
-    if (!has_struct(a) || a->dk == 0 || a->dk > 128 || a->dv == 0 || a->dv > 128 || a->batch > (uint64_t(1) << 31) || a->batch * a->heads * 3 > (uint64_t(1) << 31)) return 0;
-    return scratch_bytes(a, backward ? 3 : 1);
-}
-
-tcu_status_t tcu_linattn_forward(const tcu_linattn_t *a, void *d_ws, size_t ws_bytes, cudaStream_t stream) {
+tcu_status_t forward(const tcu_linattn_t *a, void *d_ws, size_t ws_bytes, const Waits &waits, cudaStream_t stream) {
     if (tcu_status_t st = check_linattn(a, d_ws, ws_bytes)) return st;
     if (a->batch == 0) return TCU_OK;
     const bool packed = a->d_offsets != nullptr;
@@ -329,12 +324,14 @@ tcu_status_t tcu_linattn_forward(const tcu_linattn_t *a, void *d_ws, size_t ws_b
     const tcu_tokens_t *arrays[3] = {&a->q, &a->k, &a->v}, *outputs[1] = {&a->o};
     const uint32_t widths[3] = {a->dk, a->dk, a->dv};
     MixParams p = {};
+    p.rounds = waits.rounds;
+    p.silent = waits.silent;
     p.jobs = 1;
     p.job[0] = make_job({0, 1, 2}, a->dk, a->dv, true, a->d_state_in, false, a->d_state_out, 1.0f, a->scale);
     return run_mix(a, p, arrays, widths, 3, outputs, d_ws, stream);
 }
 
-tcu_status_t tcu_linattn_backward(const tcu_linattn_t *a, void *d_ws, size_t ws_bytes, cudaStream_t stream) {
+tcu_status_t backward(const tcu_linattn_t *a, void *d_ws, size_t ws_bytes, const Waits &waits, cudaStream_t stream) {
     if (tcu_status_t st = check_linattn(a, d_ws, ws_bytes)) return st;
     if (a->batch == 0) return TCU_OK;
     const bool packed = a->d_offsets != nullptr;
@@ -360,11 +357,39 @@ tcu_status_t tcu_linattn_backward(const tcu_linattn_t *a, void *d_ws, size_t ws_
     const tcu_tokens_t *arrays[4] = {&a->q, &a->k, &a->v, &a->d_o}, *outputs[3] = {&a->d_q, &a->d_v, &a->d_k};
     const uint32_t widths[4] = {a->dk, a->dk, a->dv, a->dv};
     MixParams p = {};
+    p.rounds = waits.rounds;
+    p.silent = waits.silent;
     p.jobs = 3;
     p.job[0] = make_job({kDo, kV, kK}, a->dv, a->dk, true, a->d_state_in, true, nullptr, 1.0f, a->scale);
     p.job[1] = make_job({kK, kQ, kDo}, a->dk, a->dv, false, a->d_dstate_out, false, a->d_dstate_in, a->scale, 1.0f);
     p.job[2] = make_job({kV, kDo, kQ}, a->dv, a->dk, false, a->d_dstate_out, true, nullptr, a->scale, 1.0f);
     return run_mix(a, p, arrays, widths, 4, outputs, d_ws, stream);
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t tcu_linattn_workspace_bytes(void) { return kStatusBytes; }
+
+size_t tcu_linattn_scratch_bytes(const tcu_linattn_t *a, int backward) {
+    if (!has_struct(a) || a->dk == 0 || a->dk > 128 || a->dv == 0 || a->dv > 128 || a->batch > (uint64_t(1) << 31) || a->batch * a->heads * 3 > (uint64_t(1) << 31)) return 0;
+    return scratch_bytes(a, backward ? 3 : 1);
+}
+
+tcu_status_t tcu_linattn_forward(const tcu_linattn_t *a, void *d_ws, size_t ws_bytes, cudaStream_t stream) {
+    return forward(a, d_ws, ws_bytes, {}, stream);
+}
+
+tcu_status_t tcu_linattn_backward(const tcu_linattn_t *a, void *d_ws, size_t ws_bytes, cudaStream_t stream) {
+    return backward(a, d_ws, ws_bytes, {}, stream);
+}
+
+tcu_status_t tcu_linattn_selftest_timeout(const tcu_linattn_t *a, int backward_pass, uint32_t silent_group, unsigned limit_ms, void *d_ws, size_t ws_bytes,
+                                          cudaStream_t stream) {
+    if (limit_ms == 0 || limit_ms > 1000 || silent_group == ~0u) return TCU_ERR_INVALID_ARG;
+    const Waits waits = {limit_ms * 10, silent_group + 1};             // tries of 100 us
+    return backward_pass ? backward(a, d_ws, ws_bytes, waits, stream) : forward(a, d_ws, ws_bytes, waits, stream);
 }
 
 tcu_status_t tcu_linattn_step(const tcu_linattn_t *a, cudaStream_t stream) {

@@ -52,6 +52,27 @@ __device__ __forceinline__ uint32_t mbar_wait_bounded(uint32_t bar, uint32_t par
         : "memory");
     return ok;
 }
+// The same with the number of tries in shared memory, read only where the first one fails.
+__device__ __forceinline__ uint32_t mbar_wait_bounded_at(uint32_t bar, uint32_t parity, uint32_t rounds_at) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t.reg .u32 n;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 100000;\n\t"
+        "@p bra MBAR_END_%=;\n\t"
+        "ld.shared.u32 n, [%3];\n"
+        "MBAR_TRY_%=:\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, 100000;\n\t"
+        "@p bra MBAR_END_%=;\n\t"
+        "sub.u32 n, n, 1;\n\t"
+        "setp.ne.u32 q, n, 0;\n\t"
+        "@q bra MBAR_TRY_%=;\n"
+        "MBAR_END_%=:\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity), "r"(rounds_at)
+        : "memory");
+    return ok;
+}
 __device__ __forceinline__ void fence_barrier_init() {
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
 }
