@@ -226,6 +226,7 @@ tcu_status_t launch_mix(const tcu_linattn_t *a, MixParams &p, uint64_t groups, c
     if (a->d_scratch && p.ranks == 1 && order_pays(a, p.jobs)) {
         uint32_t *order = static_cast<uint32_t *>(a->d_scratch);
         tcu_linattn_order_kernel<<<1, kMostOrdered, 0, stream>>>(p.offsets, p.batch, order);
+        if (tcu_status_t st = launched()) return st;           // the walk would take its sequences from memory that nobody has written
         p.order = order;
         cudaLaunchConfig_t next = cfg;
         attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -497,9 +498,10 @@ EmbeddingWs embedding_ws(size_t n, size_t rows, size_t d) {
     return w;
 }
 
-// A kernel that may be set up while the one ahead of it in the stream, of the same sequence, still runs.
+// A kernel that may be set up while the one ahead of it in the stream, of the same sequence, still runs.  A sequence ends at its
+// first launch that fails: the kernels behind it index memory by what the ones before have written.
 template <typename... P, typename... A>
-void launch_next(void (*kernel)(P...), dim3 grid, dim3 block, cudaStream_t stream, A... args) {
+tcu_status_t launch_next(void (*kernel)(P...), dim3 grid, dim3 block, cudaStream_t stream, A... args) {
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr.val.programmaticStreamSerializationAllowed = 1;
@@ -509,7 +511,9 @@ void launch_next(void (*kernel)(P...), dim3 grid, dim3 block, cudaStream_t strea
     cfg.stream = stream;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    (void)cudaLaunchKernelEx(&cfg, kernel, P(args)...);        // the caller asks for the error once, at the end
+    if (cudaLaunchKernelEx(&cfg, kernel, P(args)...) == cudaSuccess) return TCU_OK;
+    (void)cudaGetLastError();
+    return TCU_ERR_CUDA;
 }
 
 // Tiles whose counts every block of the sort adds up by itself; more are scanned by a kernel between.  65536 tokens of 64 columns, 64 tiles:
@@ -517,7 +521,7 @@ void launch_next(void (*kernel)(P...), dim3 grid, dim3 block, cudaStream_t strea
 constexpr uint32_t kMostTilesAdded = 64;
 
 template <typename ID>
-void sort_tokens(const void *ids, uint32_t n, uint32_t rows, const EmbeddingWs &w, uint8_t *ws, cudaStream_t stream, int &out) {
+tcu_status_t sort_tokens(const void *ids, uint32_t n, uint32_t rows, const EmbeddingWs &w, uint8_t *ws, cudaStream_t stream, int &out) {
     int bits = 1;
     while (bits < 32 && (uint64_t(1) << bits) <= rows) ++bits;          // the value `rows` itself must fit
     auto at = [&](size_t o) { return reinterpret_cast<uint32_t *>(ws + o); };
@@ -527,45 +531,56 @@ void sort_tokens(const void *ids, uint32_t n, uint32_t rows, const EmbeddingWs &
     if (n <= kBlockTokens) {
         static std::atomic<int> configured{-1};
         int dev = 0;
-        if (cudaGetDevice(&dev) != cudaSuccess) return;
+        if (cudaGetDevice(&dev) != cudaSuccess) return TCU_ERR_CUDA;
         if (configured.load() != dev) {
-            if (cudaFuncSetAttribute(tcu_sort_block_kernel<ID>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(sizeof(BlockSort))) != cudaSuccess) return;
+            if (cudaFuncSetAttribute(tcu_sort_block_kernel<ID>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(sizeof(BlockSort))) != cudaSuccess) {
+                (void)cudaGetLastError();
+                return TCU_ERR_CUDA;
+            }
             configured.store(dev);
         }
         tcu_sort_block_kernel<ID><<<1, kBlockThreads, sizeof(BlockSort), stream>>>(id, n, rows, bits, at(w.keys[0]), at(w.tokens[0]), at(w.joins));
-        return;
+        return launched();
     }
     for (int shift = 0; shift < bits; shift += kDigitBits) {
-        if (shift == 0) tcu_sort_count_kernel<ID><<<w.tiles, kSortThreads, 0, stream>>>(id, keys, n, rows, shift, at(w.counts), at(w.joins));
-        else launch_next(tcu_sort_count_kernel<ID>, w.tiles, kSortThreads, stream, id, keys, n, rows, shift, at(w.counts), nullptr);
+        tcu_status_t st = TCU_OK;
+        if (shift == 0) {
+            tcu_sort_count_kernel<ID><<<w.tiles, kSortThreads, 0, stream>>>(id, keys, n, rows, shift, at(w.counts), at(w.joins));
+            st = launched();
+        } else {
+            st = launch_next(tcu_sort_count_kernel<ID>, w.tiles, kSortThreads, stream, id, keys, n, rows, shift, at(w.counts), nullptr);
+        }
         const bool scanned = w.tiles > kMostTilesAdded;
-        if (scanned) launch_next(tcu_sort_scan_kernel, kDigits / 32, 1024, stream, at(w.counts), w.tiles, at(w.totals));
-        launch_next(scanned ? tcu_sort_scatter_kernel<ID, true> : tcu_sort_scatter_kernel<ID, false>, w.tiles, kSortThreads, stream, id, keys, tokens, n, rows,
-                    shift, w.tiles, at(w.counts), at(w.totals), at(w.keys[out]), at(w.tokens[out]));
+        if (st == TCU_OK && scanned) st = launch_next(tcu_sort_scan_kernel, kDigits / 32, 1024, stream, at(w.counts), w.tiles, at(w.totals));
+        if (st == TCU_OK)
+            st = launch_next(scanned ? tcu_sort_scatter_kernel<ID, true> : tcu_sort_scatter_kernel<ID, false>, w.tiles, kSortThreads, stream, id, keys, tokens, n, rows,
+                             shift, w.tiles, at(w.counts), at(w.totals), at(w.keys[out]), at(w.tokens[out]));
+        if (st != TCU_OK) return st;
         keys = at(w.keys[out]);
         tokens = at(w.tokens[out]);
         out ^= 1;
     }
     out ^= 1;
+    return TCU_OK;
 }
 
 template <typename T, typename TT>
-void launch_sum(int vec, const void *d_out, void *table, const SumParams &s, cudaStream_t stream) {
-    launch_next(tcu_embedding_cut_kernel, s.pieces / 4 + 1, 128, stream, s);
+tcu_status_t launch_sum(int vec, const void *d_out, void *table, const SumParams &s, cudaStream_t stream) {
+    if (tcu_status_t st = launch_next(tcu_embedding_cut_kernel, s.pieces / 4 + 1, 128, stream, s)) return st;
     auto go = [&](auto v) {
         constexpr int VEC = decltype(v)::value;
         const uint32_t packs = s.d / VEC;
         uint32_t tx = 1;                                        // a group of threads for the columns of a piece
         while (tx < packs && tx < 128) tx <<= 1;
         const dim3 block(tx, 128 / tx), grid((s.pieces + block.y - 1) / block.y, (packs + tx - 1) / tx);
-        launch_next(tcu_embedding_sum_kernel<T, TT, VEC>, grid, block, stream, static_cast<const T *>(d_out), static_cast<TT *>(table), s);
-        launch_next(tcu_embedding_join_kernel<TT, VEC < 4 ? VEC : 4>, 148 * 8, 128, stream, static_cast<TT *>(table), s);
+        if (tcu_status_t st = launch_next(tcu_embedding_sum_kernel<T, TT, VEC>, grid, block, stream, static_cast<const T *>(d_out), static_cast<TT *>(table), s)) return st;
+        return launch_next(tcu_embedding_join_kernel<TT, VEC < 4 ? VEC : 4>, 148 * 8, 128, stream, static_cast<TT *>(table), s);
     };
     if constexpr (sizeof(T) == 2) {
         if (vec == 8) return go(std::integral_constant<int, 8>{});
     }
     if (vec == 4) return go(std::integral_constant<int, 4>{});
-    go(std::integral_constant<int, 1>{});
+    return go(std::integral_constant<int, 1>{});
 }
 
 template <typename T, typename TT, typename ID>
@@ -652,8 +667,9 @@ tcu_status_t tcu_embedding_backward(const void *d_out, tcu_float_t type, const v
     const EmbeddingWs w = embedding_ws(n, rows, d);
     uint8_t *ws = static_cast<uint8_t *>(d_ws);
     int last = 0;
-    if (id_bytes == 4) sort_tokens<int32_t>(d_ids, uint32_t(n), uint32_t(rows), w, ws, stream, last);
-    else sort_tokens<int64_t>(d_ids, uint32_t(n), uint32_t(rows), w, ws, stream, last);
+    tcu_status_t st = id_bytes == 4 ? sort_tokens<int32_t>(d_ids, uint32_t(n), uint32_t(rows), w, ws, stream, last)
+                                    : sort_tokens<int64_t>(d_ids, uint32_t(n), uint32_t(rows), w, ws, stream, last);
+    if (st != TCU_OK) return st;
     SumParams s = {};
     s.keys = reinterpret_cast<uint32_t *>(ws + w.keys[last]);
     s.tokens = reinterpret_cast<uint32_t *>(ws + w.tokens[last]);
@@ -669,8 +685,8 @@ tcu_status_t tcu_embedding_backward(const void *d_out, tcu_float_t type, const v
     s.begins = reinterpret_cast<uint32_t *>(ws + w.begins);
     s.tail = reinterpret_cast<float *>(ws + w.tail);
     s.head = reinterpret_cast<float *>(ws + w.head);
-    with_types([&](auto t, auto tt) { launch_sum<decltype(t), decltype(tt)>(vec, d_out, d_table, s, stream); });
-    return launched();
+    with_types([&](auto t, auto tt) { st = launch_sum<decltype(t), decltype(tt)>(vec, d_out, d_table, s, stream); });
+    return st;
 }
 
 }  // extern "C"

@@ -1,0 +1,94 @@
+"""A CUDA call that fails on the host ends a call of the language-model operators: nothing is queued behind it (the kernels of a
+sequence index memory by what the ones before have written), and the caller gets TCU_ERR_CUDA.  The library's host code runs
+here on a runtime without a GPU, of which one call is made to fail."""
+import ctypes
+import os
+import subprocess
+
+import pytest
+
+HERE = os.path.dirname(os.path.abspath(__file__))
+ROOT = os.path.dirname(HERE)
+
+
+@pytest.fixture(scope="module")
+def lib(tmp_path_factory):
+    out = str(tmp_path_factory.mktemp("fake") / "libtcu_lm_fake.so")
+    subprocess.run(["nvcc", "-gencode", "arch=compute_100a,code=compute_100a", "-std=c++17", "-O0", "--cudart", "none", "-shared", "-Xcompiler", "-fPIC", "-Xlinker", "-Bsymbolic",
+                    "-I", os.path.join(ROOT, "include"), "-o", out, os.path.join(ROOT, "paper_2411_17887_b200", "csrc", "tcu_lm.cu"),
+                    os.path.join(HERE, "fake_cudart.cpp")], check=True)
+    return ctypes.CDLL(out, mode=os.RTLD_LOCAL | os.RTLD_NOW)
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2411_17887_b200 import build
+    build.build()
+    from paper_2411_17887_b200 import binding
+    return binding
+
+
+def p(x):
+    return ctypes.c_void_p(x)
+
+
+def gradient(lib, n, id_bytes, table=1 << 32):
+    rows, d = 30000, 64
+    size = lib.tcu_embedding_workspace_bytes
+    size.restype, size.argtypes = ctypes.c_size_t, [ctypes.c_size_t] * 3
+    return lib.tcu_embedding_backward(p(2 << 32), 2, p(3 << 32), id_bytes, ctypes.c_size_t(n), ctypes.c_size_t(rows), ctypes.c_size_t(d), ctypes.c_float(1.0), 0,
+                                      p(table), 0, p(4 << 32), ctypes.c_size_t(size(n, rows, d)), None)
+
+
+def attention(lib, B, backward, batch, tokens, heads, packed):
+    at = lambda i: (i << 36, 0 if packed else tokens * heads * 64, heads * 64, 64)  # noqa: E731
+    args = B.tcu_linattn_args(B.TCU_BF16, batch, tokens, heads, 64, 64, 1.0, 1 << 35, at(1), at(2), at(3), at(4), d_o=at(5), d_q=at(6), d_k=at(7), d_v=at(8),
+                              d_offsets=(1 << 34) if packed else 0)
+    size = lib.tcu_linattn_scratch_bytes
+    size.restype = ctypes.c_size_t
+    scratch = size(args, backward)
+    args = B.tcu_linattn_with_scratch(args, (1 << 33) if scratch else 0, scratch)
+    return (lib.tcu_linattn_backward if backward else lib.tcu_linattn_forward)(args, p(1 << 32), ctypes.c_size_t(256), None)
+
+
+CALLS = {
+    "gradient of 2000 tokens": lambda lib, B: gradient(lib, 2000, 8),            # sorted in one block
+    "gradient of 2001 tokens": lambda lib, B: gradient(lib, 2001, 4),
+    "gradient of 9000 tokens": lambda lib, B: gradient(lib, 9000, 8),            # counts added up by every block
+    "gradient of 90000 tokens": lambda lib, B: gradient(lib, 90000, 4),          # and scanned
+    "gradient of 40 tokens": lambda lib, B: gradient(lib, 40, 8),                # one launch
+    "packed sequences in order": lambda lib, B: attention(lib, B, 0, 20, 3000, 16, True),
+    "packed sequences": lambda lib, B: attention(lib, B, 0, 2, 3000, 16, True),
+    "whole walks": lambda lib, B: attention(lib, B, 0, 1, 700, 3, False),
+    "gradients": lambda lib, B: attention(lib, B, 1, 1, 700, 3, False),
+}
+FAILS = ("cudaLaunchKernel", "cudaLaunchKernelExC", "cudaFuncSetAttribute", "cudaGetDevice")
+
+
+@pytest.mark.parametrize("what", CALLS)
+def test_nothing_follows_a_call_that_failed(lib, B, what):
+    run = CALLS[what]
+    met = 0
+    for name in FAILS:
+        # (what a first call sets and remembers has to fail before any call that succeeds)
+        for at in range(1, 20):
+            lib.fake_reset(name.encode(), at)
+            status = run(lib, B)
+            if not lib.fake_failed():
+                break
+            met += 1
+            assert status == B.TCU_ERR_CUDA, (name, at)
+            assert lib.fake_launches_after_failure() == 0, (name, at)
+    assert met > 0
+    lib.fake_reset(b"", 0)
+    assert run(lib, B) == B.TCU_OK
+    assert lib.fake_launches() > 0
+
+
+def test_walks_that_cannot_be_cut_run_whole(lib, B):
+    """A cooperative launch that does not fit is no error: the walks run whole."""
+    run = lambda: attention(lib, B, 0, 2, 700, 80, False)  # noqa: E731
+    lib.fake_reset(b"", 0)
+    assert run() == B.TCU_OK and lib.fake_launches() == 1
+    lib.fake_reset(b"cudaLaunchKernelExC", 1)
+    assert run() == B.TCU_OK and lib.fake_launches() == 2
