@@ -37,7 +37,8 @@
 // the last state is a result in 32 bits of its own; with two terms throughout it was 2e-6 to 5e-6 off, where 32-bit sums are
 // 2e-7 off.  (The rule goes by the decay alone: outputs do not depend on whether the state is asked for.)  In float16 X and K~
 // are brought to the type's range by powers of two found for every group, because a state without decay outgrows the type
-// and the low terms of small keys fall below it.
+// and the low terms of small keys fall below it; and P by one found for every token, because scores do either (products of a
+// hundred features; small gradients).
 //
 // When there are fewer (job, sequence, head) than SMs, the walk is split over the blocks of a cluster: each block first
 // forms the state that its part leaves from zero (K and V only), the blocks exchange them through distributed shared
@@ -288,13 +289,20 @@ struct Mix {
         // this thread's half of the row, in a tile
         const uint32_t half_at = (D == 128 ? side * kHalfBytes : 0), at_row = row_at(row) ^ (D == 128 ? 0 : side * 64);
         uint32_t tile = 2 * ctl->before + 1 - 3;                                   // of Q, of group i - 1
+        float back = 1.0f;                                                         // float16: the factor that takes O back to its size
+        bool ok = true;                                                            // no wait has run out (float16: two warps meet in every group, and
+                                                                                   // give up there, together)
         if (n == 0) return;
 #pragma unroll 1
         for (uint32_t i = 0; i <= n; ++i, tile += 3) {
             if (i > 0) {
                 const uint32_t g = i - 1;
+                ok = mix_wait_warp(ctl, ctl->pv_done, g & 1) && mix_wait_warp(ctl, ctl->e_done, g & 1);
+                if (!ok && (!kIsHalf || i == n)) return;
+            }
+            if (i > 0 && ok) {
+                const uint32_t g = i - 1;
                 const int tokens = part.tokens_of(part.first + g), order = part.lead ? row : tokens - 1 - row;
-                if (!mix_wait_warp(ctl, ctl->pv_done, g & 1) || !mix_wait_warp(ctl, ctl->e_done, g & 1)) return;
                 tc_fence_after();
                 float e = ctl->job.out_scale * ctl->power[max(order, 0) + int(part.lead)];
                 if (kIsHalf) e *= ctl->unscale[(ctl->before + g) & 1];
@@ -304,7 +312,7 @@ struct Mix {
 #pragma unroll
                     for (int c = 0; c < kCols; c += 16) {
                         uint32_t out[8];
-                        outputs(lanes + side * kCols + c, e, out);
+                        outputs(lanes + side * kCols + c, e, back, out);
                         st_shared_v4(at + (at_row ^ (2 * c)), out[0], out[1], out[2], out[3]);
                         st_shared_v4(at + (at_row ^ (2 * c + 16)), out[4], out[5], out[6], out[7]);
                     }
@@ -312,7 +320,7 @@ struct Mix {
                 } else {
                     T *to = reinterpret_cast<T *>(ctl->job.o) + ctl->b * ctl->job.o_batch + int64_t(ctl->h) * ctl->job.o_head +
                             (ctl->t0 + part.in_time(part.first + g) * kGroup + row) * ctl->job.o_token + side * kCols;
-                    write_some(to, lanes + side * kCols, e, row < tokens ? int(ctl->job.dv) - side * kCols : 0);
+                    write_some(to, lanes + side * kCols, e, back, row < tokens ? int(ctl->job.dv) - side * kCols : 0);
                 }
                 tc_fence_before();
                 mbar_arrive(smem_u32(&ctl->o_free));
@@ -320,48 +328,45 @@ struct Mix {
             }
             if (i < n) {
                 const int tokens = part.tokens_of(part.first + i);
-                if (!mix_wait_warp(ctl, ctl->qk_done, i & 1)) return;
+                ok = ok && mix_wait_warp(ctl, ctl->qk_done, i & 1);
+                if (!kIsHalf && !ok) return;
                 tc_fence_after();
-                // scores of 16 tokens at a time: all of them count, none, or (around the diagonal and the end) some
                 const uint32_t at = lanes + kColS + 64 * side;
+                float up = 1.0f;
+                if (kIsHalf) {
+                    // float16: a token's scores are used as 2^s P with the largest near 2^14 (as they are, they can leave the type on
+                    // either side).  Each half of the row leaves its largest where O will be: that was read above.
+                    float big = 0.0f, other = 0.0f;
+                    if (ok) {
+#pragma unroll 1
+                        for (int c = 64 * side, k = 0; k < 64; c += 16, k += 16) {
+                            float2 x[8];
+                            decayed(part.lead, row, row0, c, tokens, at + k, factor, x);
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) big = fmaxf(big, fmaxf(fabsf(x[j].x), fabsf(x[j].y)));
+                        }
+                        tmem_st1(lanes + kColO + side * kCols, __float_as_uint(big));
+                        tmem_st_wait();
+                        tc_fence_before();
+                    }
+                    if (named_barrier_or(4 + (warp & 3), 64, !ok)) return;
+                    tc_fence_after();
+                    other = __uint_as_float(tmem_ld1(lanes + kColO + (side ^ 1) * kCols));
+                    tmem_ld_wait();
+                    big = fmaxf(big, other);
+                    const int shift = big > 0.0f ? min(max(14 - exponent(big), -126), 126) : 0;
+                    up = pow2(shift);
+                    back = pow2(-shift);
+                }
 #pragma unroll 1
                 for (int c = 64 * side, k = 0; k < 64; c += 16, k += 16) {
-                    const int apart = part.lead ? row - c : c - row, apart0 = part.lead ? row0 - c : c - row0 - 31;     // tokens apart: of the first column; least of the warp
-                    const bool all = part.lead ? apart0 >= 15 : apart0 >= 0 && c + 15 < tokens;
-                    const bool none = part.lead ? apart0 < -31 : apart0 < -46 || c >= tokens;
-                    uint32_t v[16], out[8];
-                    if (all) {
-                        tmem_ld16(at + k, v);
-                        const float f = ctl->power[part.lead ? apart - 15 : apart];
-                        const float2 f2 = make_float2(f, f);
-                        tmem_ld_wait();
+                    float2 x[8];
+                    uint32_t out[8];
+                    decayed(part.lead, row, row0, c, tokens, at + k, factor, x);
 #pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            const float2 x = mul2(make_float2(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1])), mul2(f2, factor[j]));
-                            out[j] = H::pack(x.x, x.y);
-                        }
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) out[j] = 0;
-                        if (!none) {
-                            // what does not count may not be finite: it is left out, not multiplied by its factor of zero
-                            tmem_ld16(at + k, v);
-                            const int hi = tokens - c;               // (past the end of a short group the factors are not zero)
-                            const float *near = ctl->near + (part.lead ? 160 - apart : 47 + apart);
-                            tmem_ld_wait();
-#pragma unroll
-                            for (int j = 0; j < 16; ++j) {
-                                const float f = near[j];
-                                v[j] = f != 0.0f ? __float_as_uint(__uint_as_float(v[j]) * f) : 0u;
-                            }
-                            if (!part.lead && hi < 16) {
-#pragma unroll
-                                for (int j = 0; j < 16; ++j)
-                                    if (j >= hi) v[j] = 0u;
-                            }
-#pragma unroll
-                            for (int j = 0; j < 8; ++j) out[j] = H::pack(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1]));
-                        }
+                    for (int j = 0; j < 8; ++j) {
+                        if (kIsHalf) x[j] = mul2(x[j], make_float2(up, up));
+                        out[j] = H::pack(x[j].x, x[j].y);
                     }
                     tmem_st8(at + k / 2, out);                       // never over scores still to be read
                 }
@@ -371,8 +376,47 @@ struct Mix {
             }
         }
     }
-    // 16 features of a token: O + e E
-    static __device__ __forceinline__ void outputs(uint32_t at, float e, uint32_t (&out)[8]) {
+    // P, not yet rounded, of a token (`row`; the first of the warp: row0) and the 16 tokens of columns c...: all of them count, none,
+    // or (around the diagonal and the end) some
+    static __device__ __forceinline__ void decayed(bool lead, int row, int row0, int c, int tokens, uint32_t at, const float2 (&factor)[8], float2 (&x)[8]) {
+        const MixCtl *ctl = mix_ctl();
+        const int apart = lead ? row - c : c - row, apart0 = lead ? row0 - c : c - row0 - 31;     // tokens apart: of the first column; least of the warp
+        const bool all = lead ? apart0 >= 15 : apart0 >= 0 && c + 15 < tokens;
+        const bool none = lead ? apart0 < -31 : apart0 < -46 || c >= tokens;
+        uint32_t v[16];
+        if (all) {
+            tmem_ld16(at, v);
+            const float f = ctl->power[lead ? apart - 15 : apart];
+            const float2 f2 = make_float2(f, f);
+            tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = mul2(make_float2(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1])), mul2(f2, factor[j]));
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) x[j] = make_float2(0.0f, 0.0f);
+            if (!none) {
+                // what does not count may not be finite: it is left out, not multiplied by its factor of zero
+                tmem_ld16(at, v);
+                const int hi = tokens - c;                           // (past the end of a short group the factors are not zero)
+                const float *near = ctl->near + (lead ? 160 - apart : 47 + apart);
+                tmem_ld_wait();
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const float f = near[j];
+                    v[j] = f != 0.0f ? __float_as_uint(__uint_as_float(v[j]) * f) : 0u;
+                }
+                if (!lead && hi < 16) {
+#pragma unroll
+                    for (int j = 0; j < 16; ++j)
+                        if (j >= hi) v[j] = 0u;
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[j] = make_float2(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1]));
+            }
+        }
+    }
+    // 16 features of a token: O (times `back` in float16) + e E
+    static __device__ __forceinline__ void outputs(uint32_t at, float e, float back, uint32_t (&out)[8]) {
         uint32_t vo[16], ve[16];
         const float2 e2 = make_float2(e, e);
         tmem_ld16(at + kColO, vo);
@@ -380,7 +424,9 @@ struct Mix {
         tmem_ld_wait();
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const float2 x = fma2(e2, make_float2(__uint_as_float(ve[2 * j]), __uint_as_float(ve[2 * j + 1])), make_float2(__uint_as_float(vo[2 * j]), __uint_as_float(vo[2 * j + 1])));
+            float2 o = make_float2(__uint_as_float(vo[2 * j]), __uint_as_float(vo[2 * j + 1]));
+            if (kIsHalf) o = mul2(o, make_float2(back, back));
+            const float2 x = fma2(e2, make_float2(__uint_as_float(ve[2 * j]), __uint_as_float(ve[2 * j + 1])), o);
             out[j] = H::pack(x.x, x.y);
         }
     }
@@ -391,11 +437,11 @@ struct Mix {
         tmem_st_wait();
     }
     // the first `width` features (none when it is not positive) of this thread's half of a token
-    static __device__ __noinline__ void write_some(T *to, uint32_t at, float e, int width) {
+    static __device__ __noinline__ void write_some(T *to, uint32_t at, float e, float back, int width) {
 #pragma unroll 1
         for (int c = 0; c < kCols; c += 16, width -= 16) {
             uint32_t out[8];
-            outputs(at + c, e, out);
+            outputs(at + c, e, back, out);
             if (width >= 8) st_global_v4(to + c, out[0], out[1], out[2], out[3]);
             if (width >= 16) st_global_v4(to + c + 8, out[4], out[5], out[6], out[7]);
             else if (width > 0) {

@@ -1,0 +1,107 @@
+"""Linear attention over the range of its types: scores, keys, states, gradients and decays that are large, small or not numbers.
+
+The bounds are those of lm_reference.py without its allowance for scores and keys that fall below float16's smallest step: scores,
+states and keys are brought to the type's range by powers of two that put the largest of a token (scores) or of a group (the
+others) near 2^14, so that a step of 2^-24 is 2^-38 of that largest, and half of it is lost at most.  What remains is the step of
+the outputs themselves, 2^-24, and, with S and X the largest score and state there can be,
+    2^-38 (128 S max |v| + dk max |q| X)."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2411_17887_b200 import api
+from tests.lm_reference import U, assert_within, f64, mix, transpose
+from tests.test_gpu_linattn import draw
+
+pytestmark = pytest.mark.gpu
+DTYPES = [torch.bfloat16, torch.float16]
+# walks run whole (64 and 128 wide), in parts of a cluster, and cut over blocks
+SHAPES = [(1, 300, 2, 64, 64), (2, 300, 2, 128, 128), (1, 2100, 1, 128, 72), (2, 300, 80, 16, 24)]
+each = lambda f: pytest.mark.parametrize("dtype", DTYPES, ids=["bf16", "f16"])(pytest.mark.parametrize("shape", SHAPES, ids=str)(f))  # noqa: E731
+
+
+@pytest.fixture(autouse=True)
+def _device():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    yield
+    assert api.linear_attention_status() == 0
+
+
+def bounded(dtype, q, k, v, decay, lead, init, in_scale, out_scale):
+    o, x = mix(q, k, v, decay, lead, init, in_scale, out_scale)
+    ao, ax = mix(*(np.abs(y) for y in (q, k, v)), decay, lead, None if init is None else np.abs(init), abs(in_scale), abs(out_scale))
+    u, (t, dk) = U[dtype], (q.shape[1], q.shape[3])
+    big_q, big_k, big_v = (np.abs(y).max() for y in (q, k, v))
+    score = dk * big_q * big_k * abs(in_scale * out_scale)
+    state = t * big_k * big_v * abs(in_scale) + (0.0 if init is None else np.abs(init).max())
+    small = 2.0 ** -24 + 2.0 ** -38 * (128 * score * big_v + dk * big_q * state * abs(out_scale)) if dtype == torch.float16 else 0.0
+    return o, u * np.abs(o) + (1.02 * u + 1e-5) * ao + small + 1e-30, x, (2.0 ** -16 + 1e-5) * ax + 1e-30
+
+
+def check_outputs(q, k, v, decay, scale, s0, o, last):
+    want, eo, x, ex = bounded(q.dtype, f64(q), f64(k), f64(v), f64(decay), 1, None if s0 is None else f64(s0), 1.0, scale)
+    assert np.abs(want).max() < 6e4                                  # the outputs themselves are inside float16
+    assert_within(o, want, eo, "o")
+    if last is not None:
+        assert_within(last, x, ex, "final state")
+
+
+def check_gradients(q, k, v, decay, scale, s0, d_o, d_last, got):
+    dtype, none = q.dtype, lambda x: None if x is None else f64(x)
+    q, k, v, d_o, decay, s0, d_last = f64(q), f64(k), f64(v), f64(d_o), f64(decay), none(s0), none(d_last)
+    dq, eq, _, _ = bounded(dtype, d_o, v, k, decay, 1, transpose(s0), 1.0, scale)
+    dv, ev, d0, e0 = bounded(dtype, k, q, d_o, decay, 0, d_last, scale, 1.0)
+    dk, ek, _, _ = bounded(dtype, v, d_o, q, decay, 0, transpose(d_last), scale, 1.0)
+    assert max(np.abs(x).max() for x in (dq, dk, dv)) < 6e4
+    for name, x, want, e in zip(("dq", "dk", "dv", "d_initial_state"), got, (dq, dk, dv, d0), (eq, ek, ev, e0)):
+        if x is not None:
+            assert_within(x, want, e, name)
+
+
+@each
+def test_scores_above_the_type(shape, dtype):
+    """Products of a hundred features leave float16, what they weigh does not."""
+    b, t, h, dk, dv = shape
+    _, _, v, _, decay, _, _ = draw(5 + t, b, t, h, dk, dv, dtype)
+    q, k = ((60 + 60 * torch.rand((b, t, h, dk), device="cuda")).to(dtype) for _ in range(2))
+    v = (v.float() * 1e-3).to(dtype)
+    decay.fill_(-0.05)
+    scale = 1.0 if dk < 100 else dk ** -0.5
+    assert (q.float() * k.float()).sum(-1).max() * scale > 65504
+    o, last = api.linear_attention(q, k, v, decay, scale=scale, output_final_state=True)
+    check_outputs(q, k, v, decay, scale, None, o, last)
+
+
+@pytest.mark.parametrize("size", [1e-5, 1e-6])
+@each
+def test_small_gradients(shape, dtype, size):
+    """Gradients of outputs as a mean over many tokens leaves them, times large keys and values."""
+    b, t, h, dk, dv = shape
+    q, k, v, d_o, decay, _, _ = draw(6 + t, b, t, h, dk, dv, dtype)
+    q, k = ((x.float() * 100).to(dtype) for x in (q, k))
+    d_o = (d_o.float() * size).to(dtype)
+    check_gradients(q, k, v, decay, dk ** -0.5, None, d_o, None, api.linear_attention_backward(d_o, q, k, v, decay))
+
+
+@each
+def test_gradients_of_large_scores(shape, dtype):
+    b, t, h, dk, dv = shape
+    q, k, v, d_o, decay, s0, d_last = draw(4 + t, b, t, h, dk, dv, dtype, True)
+    q, k = ((x.float() * 1e-3).to(dtype) for x in (q, k))
+    v, d_o = ((60 + 60 * torch.rand((b, t, h, dv), device="cuda")).to(dtype) for _ in range(2))
+    decay.fill_(-0.05)
+    assert (v.float() * d_o.float()).sum(-1).max() > 65504
+    check_gradients(q, k, v, decay, 1.0, s0, d_o, d_last, api.linear_attention_backward(d_o, q, k, v, decay, 1.0, s0, d_final_state=d_last))
+
+
+@each
+def test_tokens_of_very_different_size(shape, dtype):
+    """Queries over thirty binary orders of magnitude in one group: every token has a power of two of its own."""
+    b, t, h, dk, dv = shape
+    q, k, v, _, decay, _, _ = draw(7 + t, b, t, h, dk, dv, dtype)
+    q = (q.float() * torch.exp2(-12.0 * torch.rand((b, t, h, 1), device="cuda"))).to(dtype)
+    q[:, ::7] *= 1000
+    k, v = (k.float() * 50).to(dtype), (v.float() * 1e-3).to(dtype)
+    o, last = api.linear_attention(q, k, v, decay, scale=1.0, output_final_state=True)
+    check_outputs(q, k, v, decay, 1.0, None, o, last)
