@@ -455,7 +455,10 @@ struct Mix {
     }
 
     // ---- keys.  float16: powers of two, found for every group, keep the operands inside the type: X is held as 2^s X, so that the
-    // keys can be used as 2^s K~ with the largest near 2^14 (the low terms of small ones would fall below 2^-24).
+    // keys can be used as 2^s K~ with the largest near 2^14 (the low terms of small ones would fall below 2^-24).  What the decay takes
+    // from the keys it has taken from X as well; the rest of s is at most 52: keys (with in_scale) down to 2^-55 keep both terms, and
+    // states up to 2^75 stay inside 32 bits.  A group whose keys are all zero says nothing about s.
+    static constexpr int kMostKeyScale = 52;
     static __device__ __noinline__ void keys(uint32_t phase) {
         MixCtl *ctl = mix_ctl();
         const int warp = (threadIdx.x >> 5) - kTokenWarps, lane = threadIdx.x & 31, row = (warp & 3) * 32 + lane;
@@ -466,6 +469,7 @@ struct Mix {
         const uint32_t made = phase && n > 0 && !ctl->owns_last ? n - 1 : n;       // the last group's are not needed if its state is not
         uint32_t it = phase ? ctl->before : 0, tile = 2 * it;                      // groups before, their tiles
         uint32_t thirds = phase ? ctl->thirds : 0;
+        int scale = 0;                                                             // float16: K~ is used as 2^scale K~
         auto gate = [&](const uint64_t &barrier, uint32_t parity) {
             return kIsHalf ? mix_wait_role(ctl, 2, 32 * kKeyWarps, barrier, parity) : mix_wait_warp(ctl, barrier, parity);
         };
@@ -506,7 +510,8 @@ struct Mix {
                 for (int j = 0; j < kKeyWarps; ++j) big = fmaxf(big, ctl->biggest_k[it & 1][j]);
                 // the powers of a in K~ go from a^(1 - lead) to a^(tokens - lead)
                 const float top = fmaxf(ctl->power[1 - int(part.lead)], ctl->power[tokens - int(part.lead)]);
-                const int scale = min(max(14 - exponent(big * fabsf(ctl->job.in_scale) * top), -30), 100);
+                big *= fabsf(ctl->job.in_scale);
+                if (big > 0.0f && top > 0.0f) scale = min(max(min(max(13 - exponent(big), -30), kMostKeyScale) - exponent(top), -126), 126);
                 f *= pow2(scale);
                 if (warp == 0 && lane == 0) {
                     ctl->scale_k[it & 1] = scale;
@@ -628,7 +633,8 @@ struct Mix {
                 const int ex = min(max(exponent(big), -60), 127), now = ctl->scale_k[it & 1];
                 shrink = pow2(14 - ex);
                 if (threadIdx.x == 32 * kStateWarp) ctl->unscale[it & 1] = pow2(ex - 14 - held);
-                keep *= pow2(now - held);
+                keep *= pow2((now - held) / 2);              // (as two factors: the powers may be 252 apart)
+                keep *= pow2(now - held - (now - held) / 2);
                 held = now;
             }
             if (!fresh && holds_x) {

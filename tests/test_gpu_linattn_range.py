@@ -105,3 +105,43 @@ def test_tokens_of_very_different_size(shape, dtype):
     k, v = (k.float() * 50).to(dtype), (v.float() * 1e-3).to(dtype)
     o, last = api.linear_attention(q, k, v, decay, scale=1.0, output_final_state=True)
     check_outputs(q, k, v, decay, 1.0, None, o, last)
+
+
+@pytest.mark.parametrize("size", [1e9, 1e15])
+@each
+def test_groups_without_keys_keep_a_large_state(shape, dtype, size):
+    """Masked tokens: keys of zero, whole groups of them, with states far above them in either direction.  (Gradients of 1e15
+    would not be inside float16.)"""
+    b, t, h, dk, dv = shape
+    q, k, v, d_o, decay, s0, d_last = draw(9 + t, b, t, h, dk, dv, dtype, True)
+    decay.fill_(-1e-3)
+    s0, d_last = s0 * size, d_last * size
+    for x in (q, k, d_o):
+        x[:, 128:256] = 0
+    for keys in (k, torch.zeros_like(k)):
+        o, last = api.linear_attention(q, keys, v, decay, scale=1 / size, initial_state=s0, output_final_state=True)
+        check_outputs(q, keys, v, decay, 1 / size, s0, o, last)
+    if size == 1e9:
+        k, v = ((x.float() * 1e-6).to(dtype) for x in (k, v))
+        got = api.linear_attention_backward(d_o, q, k, v, decay, 1 / size, s0, d_final_state=d_last)
+        check_gradients(q, k, v, decay, 1 / size, s0, d_o, d_last, got)
+
+
+@each
+def test_keys_of_every_size(shape, dtype):
+    """Groups of large, ordinary, tiny and no keys, one after another: the power of two that goes with a group changes by more than a
+    factor of float32's smallest number, and back."""
+    b, t, h, dk, dv = shape
+    q, k, v, _, decay, s0, _ = draw(10 + t, b, t, h, dk, dv, dtype, True)
+    decay.fill_(-1e-4)
+    size = torch.ones(t, device="cuda")
+    for i in range(0, t, 128):
+        size[i:i + 128] = (1.0, 1e-6, 0.0, 1e3)[i // 128 % 4]
+    k = (k.float() * size[None, :, None, None]).to(dtype)
+    for scale in (1e-3, 2.0 ** -60):
+        q2 = (q.float() * (1.0 if scale == 1e-3 else 1e4)).to(dtype)
+        o, last = api.linear_attention(q2, k, v, decay, scale=scale, initial_state=s0, output_final_state=True)
+        check_outputs(q2, k, v, decay, scale, s0, o, last)
+    d_o, d_last = v, torch.zeros_like(s0)                            # (here queries and scale are the keys of two of the walks)
+    got = api.linear_attention_backward(d_o, k, q, v, decay, 2.0 ** -50, None, d_final_state=d_last)
+    check_gradients(k, q, v, decay, 2.0 ** -50, None, d_o, d_last, got)
