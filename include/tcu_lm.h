@@ -45,7 +45,8 @@ typedef struct {
     uint32_t heads, dk, dv;     /* dk, dv: 1 to 128                                                                 */
     float scale;                /* a factor on every output                                                         */
     const float *d_log_decay;   /* `heads` values, log of the decay of each head (-inf: no memory; values above 0 let
-                                   the state grow and are the caller's concern)                                    */
+                                   the state grow and are the caller's concern; NaN: outputs, states and gradients
+                                   of the head are NaN, other heads are not affected)                              */
     const int64_t *d_offsets;   /* NULL: dense.  Packed: batch + 1 values, sequence b holds tokens [offsets[b],
                                    offsets[b+1]); non-decreasing, first 0, last `tokens` (not checked: they live on the device); empty
                                    sequences are allowed                                                            */

@@ -726,7 +726,7 @@ struct Mix {
         // a split walk has a first phase, over K and V only, in the blocks whose totals later blocks need
         ctl->before = p.ranks > 1 && part.last < part.groups ? count : 0;
         ctl->split = p.ranks > 1;
-        ctl->log2_decay = fmaxf(p.log_decay[h] * 1.4426950408889634f, -1e30f);
+        ctl->log2_decay = log2_of(p.log_decay[h]);
         uint32_t lo = part.first, hi = part.first + ctl->before;           // the groups with a third term are the last ones
         while (lo < hi) {
             const uint32_t mid = (lo + hi) / 2;
@@ -789,7 +789,12 @@ struct Mix {
         mbar_init(smem_u32(&ctl->third_ready), 32 * kKeyWarps);
         fence_barrier_init();
     }
-    // All threads: decays a^m = 2^(m log2 a); -inf becomes a value whose multiples are finite, so that a^0 = 1
+    // -inf becomes a value whose multiples are finite, so that a^0 = 1; a NaN stays one and reaches every output and state of its head
+    static __device__ __forceinline__ float log2_of(float log_decay) {
+        const float x = log_decay * 1.4426950408889634f;
+        return x < -1e30f ? -1e30f : x;
+    }
+    // All threads: decays a^m = 2^(m log2 a)
     static __device__ __forceinline__ void tables(float log2a, bool lead, float scale, const MixPart &part) {
         MixCtl *ctl = mix_ctl();
         if (threadIdx.x < kNear) {
@@ -1131,7 +1136,7 @@ __global__ void __launch_bounds__(kMixThreads, 1) tcu_linattn_mix_kernel(const _
             part.last = min((rank + 1) * part.per, part.groups);
             if (warp == kProducerWarp && lane == 0) M::first_tiles(p.map, job, part, int(begin), p.offsets ? 0 : int(b), int(h));
             if (threadIdx.x == 0) M::take(p, part, work % p.jobs, b, h, begin, rank, false);
-            M::tables(fmaxf(p.log_decay[h] * 1.4426950408889634f, -1e30f), part.lead, job.in_scale * job.out_scale, part);
+            M::tables(M::log2_of(p.log_decay[h]), part.lead, job.in_scale * job.out_scale, part);
             allocate();
         }
         tc_fence_before();

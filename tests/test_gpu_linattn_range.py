@@ -145,3 +145,27 @@ def test_keys_of_every_size(shape, dtype):
     d_o, d_last = v, torch.zeros_like(s0)                            # (here queries and scale are the keys of two of the walks)
     got = api.linear_attention_backward(d_o, k, q, v, decay, 2.0 ** -50, None, d_final_state=d_last)
     check_gradients(k, q, v, decay, 2.0 ** -50, None, d_o, d_last, got)
+
+
+@each
+def test_a_decay_that_is_no_number(shape, dtype):
+    """A model that has gone wrong shows it, in prompts and gradients as in single tokens; other heads keep their bits."""
+    b, t, h, dk, dv = shape
+    q, k, v, d_o, decay, s0, d_last = draw(8 + t, b, t, max(h, 2), dk, dv, dtype, True)
+
+    def all_of(decay, s0=s0, d_last=d_last):
+        o, last = api.linear_attention(q, k, v, decay, initial_state=s0, output_final_state=True)
+        dq, dk, dv, d_first = api.linear_attention_backward(d_o, q, k, v, decay, initial_state=s0, d_final_state=d_last)
+        state = torch.zeros_like(last) if s0 is None else s0.clone()
+        step = api.linear_attention_step(q[:, 0], k[:, 0], v[:, 0], decay, state)
+        return [o.transpose(1, 2), last, dq.transpose(1, 2), dk.transpose(1, 2), dv.transpose(1, 2), state, step] + ([] if d_first is None else [d_first])
+
+    for states in ((s0, d_last), (None, None)):
+        want = all_of(decay, *states)
+        for head in (0, q.shape[2] - 1):
+            bad = decay.clone()
+            bad[head] = float("nan")
+            others = torch.arange(len(decay), device="cuda") != head
+            for x, w in zip(all_of(bad, *states), want):
+                assert torch.isnan(x[:, head]).all()
+                assert torch.equal(x[:, others], w[:, others])
