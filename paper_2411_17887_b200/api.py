@@ -3,6 +3,7 @@ torch (plumbing) and calls the C-ABI entry points.  No arithmetic happens here."
 from __future__ import annotations
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding as B
 
@@ -238,6 +239,7 @@ class _LinearAttention(torch.autograd.Function):
         return _attention_forward(q, k, v, log_decay, scale, initial_state, offsets, output_final_state)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, d_o, d_last):
         q, k, v, log_decay, initial_state, offsets = ctx.saved_tensors
         d_o = torch.zeros_like(v) if d_o is None else d_o
@@ -248,8 +250,8 @@ class _LinearAttention(torch.autograd.Function):
 
 def linear_attention(q, k, v, log_decay, scale=None, initial_state=None, offsets=None, output_final_state=False):
     """Causal linear attention with a decay for each head: S_t = a S_{t-1} + k_t v_t^T, o_t = scale * S_t^T q_t with
-    a = exp(log_decay[head]).  Returns (o, final state), the state None unless asked for; differentiable in q, k, v and the
-    initial state.
+    a = exp(log_decay[head]).  Returns (o, final state), the state None unless asked for; differentiable, once, in q, k, v
+    and the initial state.
 
     q, k (batch, tokens, heads, dk) and v (batch, tokens, heads, dv), float16 or bfloat16, any strides (dk, dv at most 128);
     or packed (tokens, heads, d) with `offsets`, an int64 tensor of batch + 1 values on the GPU: sequence b is
@@ -348,13 +350,14 @@ class _Embedding(torch.autograd.Function):
         return _embedding_forward(ids, table, scale)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, d_out):
         return None, embedding_backward(d_out, ctx.saved_tensors[0], ctx.rows, ctx.scale, ctx.dtype), None
 
 
 def embedding(ids, table, scale=1.0):
     """scale * table[ids], rounded once to the table's type; an id outside the table gives a row of zeros.  ids int32 or int64
-    of any shape; differentiable in the table."""
+    of any shape; differentiable, once, in the table."""
     if table.requires_grad and torch.is_grad_enabled():
         return _Embedding.apply(ids, table, scale)
     return _embedding_forward(ids, table, scale)

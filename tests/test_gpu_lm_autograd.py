@@ -1,0 +1,33 @@
+"""The language-model operators under autograd: what they cannot differentiate they refuse, and what they write in place they say."""
+import pytest
+import torch
+
+from paper_2411_17887_b200 import api
+from tests.test_gpu_linattn import draw
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True)
+def _device():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+
+
+def test_second_derivatives_are_refused():
+    """A penalty on gradients reaches the parameters by way of the gradients themselves: without an error it would lose that part."""
+    q, k, v, _, decay, s0, _ = draw(1, 1, 50, 2, 16, 16, torch.bfloat16, True)
+    for which in range(4):
+        args = [q, k, v, s0]
+        root = torch.ones_like(args[which]).requires_grad_()
+        args[which] = args[which] * root ** 2
+        o, last = api.linear_attention(*args[:3], decay, initial_state=args[3], output_final_state=True)
+        g, = torch.autograd.grad(o.float().square().sum() + last.square().sum(), root, create_graph=True)
+        assert torch.isfinite(g).all() and g.abs().sum() > 0
+        with pytest.raises(RuntimeError, match="once_differentiable"):
+            g.float().square().sum().backward()
+    root = torch.randn((9, 8), device="cuda").requires_grad_()
+    out = api.embedding(torch.arange(9, device="cuda"), root ** 2)
+    g, = torch.autograd.grad(out.square().sum(), root, create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        g.square().sum().backward()
