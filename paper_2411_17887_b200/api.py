@@ -3,6 +3,7 @@ torch (plumbing) and calls the C-ABI entry points.  No arithmetic happens here."
 from __future__ import annotations
 
 import torch
+from torch.autograd import forward_ad
 from torch.autograd.function import once_differentiable
 
 from . import binding as B
@@ -102,6 +103,13 @@ def linear_attention_status(device=None) -> int:
     if index not in _status:
         return B.TCU_OK
     return B.tcu_scan_device_status(_status[index][1], torch.cuda.current_stream().cuda_stream)
+
+
+def _no_tangents(**arrays) -> None:
+    """The kernels see values alone: a tangent that one of the arrays carries would be lost."""
+    for name, x in arrays.items():
+        if x is not None and forward_ad.unpack_dual(x).tangent is not None:
+            raise NotImplementedError(f"{name} carries a tangent: forward-mode derivatives are not computed here")
 
 
 def _refuse(dtype: torch.dtype, device: torch.device, **others) -> None:
@@ -217,6 +225,8 @@ def _attention_forward(q, k, v, log_decay, scale, initial_state, offsets, output
 def linear_attention_backward(d_o, q, k, v, log_decay, scale=None, initial_state=None, offsets=None, d_final_state=None):
     """Gradients of :func:`linear_attention` with respect to q, k, v and the initial state (None without one), from the
     gradient of its output and, where it has one, of the final state."""
+    if forward_ad._current_level >= 0:
+        _no_tangents(d_o=d_o, q=q, k=k, v=v, log_decay=log_decay, initial_state=initial_state, d_final_state=d_final_state)
     m = _Mix(q, k, v, log_decay, scale, offsets, initial_state=initial_state, d_final_state=d_final_state)
     if d_o.dtype != q.dtype or d_o.device != q.device:
         _refuse(q.dtype, q.device, d_o=d_o)
@@ -257,7 +267,8 @@ def linear_attention(q, k, v, log_decay, scale=None, initial_state=None, offsets
     or packed (tokens, heads, d) with `offsets`, an int64 tensor of batch + 1 values on the GPU: sequence b is
     [offsets[b], offsets[b + 1]).  log_decay (heads,) float32, at most 0, a constant of the model (no gradient); scale: dk ** -0.5
     by default; states (batch, heads, dk, dv) float32."""
-    if torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad or (initial_state is not None and initial_state.requires_grad)):
+    if forward_ad._current_level >= 0 or (torch.is_grad_enabled() and (q.requires_grad or k.requires_grad or v.requires_grad or
+                                                                       (initial_state is not None and initial_state.requires_grad))):
         return _LinearAttention.apply(q, k, v, log_decay, scale, initial_state, offsets, output_final_state)
     return _attention_forward(q, k, v, log_decay, scale, initial_state, offsets, output_final_state)
 
@@ -266,6 +277,8 @@ def linear_attention_step(q, k, v, log_decay, state, scale=None, slots=None):
     """One token for each sequence: updates `state` in place and returns o (batch, heads, dv).  q, k (batch, heads, dk),
     v (batch, heads, dv); state (pool, heads, dk, dv) float32; slots: None (sequence b has entry b), or an int32 tensor of
     each sequence's entry, all different; an entry outside the pool marks a sequence to skip (its output is zero)."""
+    if forward_ad._current_level >= 0:
+        _no_tangents(q=q, k=k, v=v, log_decay=log_decay, state=state)
     dtype, device, shape = q.dtype, q.device, q.shape
     if k.dtype != dtype or v.dtype != dtype or k.device != device or v.device != device:
         _refuse(dtype, device, k=k, v=v)
@@ -307,6 +320,8 @@ def embedding_backward(d_out, ids, num_rows, scale=1.0, dtype=torch.float32, out
     """Gradient of :func:`embedding` with respect to its table: (num_rows, d) of `dtype` (float32, or the type of d_out), row v
     the sum of scale * d_out over the tokens with id v, zero where there is none.  With `out` the sums are added to it
     instead (rows without tokens are not touched)."""
+    if forward_ad._current_level >= 0:
+        _no_tangents(d_out=d_out, out=out)
     device, kind = d_out.device, d_out.dtype
     d_out, ids = d_out.contiguous(), _ids(ids, device)
     d = d_out.shape[-1]
@@ -358,6 +373,6 @@ class _Embedding(torch.autograd.Function):
 def embedding(ids, table, scale=1.0):
     """scale * table[ids], rounded once to the table's type; an id outside the table gives a row of zeros.  ids int32 or int64
     of any shape; differentiable, once, in the table."""
-    if table.requires_grad and torch.is_grad_enabled():
+    if forward_ad._current_level >= 0 or (table.requires_grad and torch.is_grad_enabled()):
         return _Embedding.apply(ids, table, scale)
     return _embedding_forward(ids, table, scale)

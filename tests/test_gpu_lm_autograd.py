@@ -31,3 +31,32 @@ def test_second_derivatives_are_refused():
     g, = torch.autograd.grad(out.square().sum(), root, create_graph=True)
     with pytest.raises(RuntimeError, match="once_differentiable"):
         g.square().sum().backward()
+
+
+def test_tangents_are_refused():
+    """Forward-mode derivatives: an output without its tangent would read as one that does not depend on the input."""
+    q, k, v, d_o, decay, s0, _ = draw(2, 1, 50, 2, 16, 16, torch.bfloat16, True)
+    table, ids, grad = torch.randn((9, 8), device="cuda"), torch.arange(9, device="cuda"), torch.zeros((9, 8), device="cuda")
+    plain = api.linear_attention(q, k, v, decay, initial_state=s0)[0], api.embedding(ids, table)
+    step = lambda q, k, v, decay, s0: api.linear_attention_step(q[:, 0], k[:, 0], v[:, 0], decay, s0.clone())  # noqa: E731
+    calls = [lambda q, k, v, decay, s0: api.linear_attention(q, k, v, decay, initial_state=s0), step,
+             lambda q, k, v, decay, s0: api.linear_attention_backward(d_o, q, k, v, decay, initial_state=s0)]
+    with torch.autograd.forward_ad.dual_level():
+        dual = lambda x: torch.autograd.forward_ad.make_dual(x, torch.ones_like(x))  # noqa: E731
+        for which in range(5):
+            args = [q, k, v, decay, s0]
+            args[which] = dual(args[which])
+            for call in calls:
+                with pytest.raises(NotImplementedError):
+                    call(*args)
+        with pytest.raises(NotImplementedError):
+            api.linear_attention_backward(dual(d_o), q, k, v, decay)
+        with pytest.raises(NotImplementedError):
+            api.embedding(ids, dual(table))
+        with pytest.raises(NotImplementedError):
+            api.embedding_backward(dual(table), ids, 9)
+        with pytest.raises(NotImplementedError):
+            api.embedding_backward(table, ids, 9, out=dual(grad))
+        # without one the calls are as ever
+        assert torch.equal(api.linear_attention(q, k, v, decay, initial_state=s0)[0], plain[0])
+        assert torch.equal(api.embedding(ids, table), plain[1])
