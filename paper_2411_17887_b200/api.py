@@ -105,6 +105,18 @@ def linear_attention_status(device=None) -> int:
     return B.tcu_scan_device_status(_status[index][1], torch.cuda.current_stream().cuda_stream)
 
 
+def _written(x: torch.Tensor) -> None:
+    """Tells autograd that a kernel has written to x: a backward pass that has saved x then raises instead of using what it holds now."""
+    if not x.is_inference():                                # (which have no version)
+        torch.autograd.graph.increment_version(x)
+
+
+def _not_recorded(**arrays) -> None:
+    for name, x in arrays.items():
+        if x.requires_grad:
+            raise RuntimeError(f"{name} requires a gradient, and this call has none: make it under torch.no_grad()")
+
+
 def _no_tangents(**arrays) -> None:
     """The kernels see values alone: a tangent that one of the arrays carries would be lost."""
     for name, x in arrays.items():
@@ -276,9 +288,12 @@ def linear_attention(q, k, v, log_decay, scale=None, initial_state=None, offsets
 def linear_attention_step(q, k, v, log_decay, state, scale=None, slots=None):
     """One token for each sequence: updates `state` in place and returns o (batch, heads, dv).  q, k (batch, heads, dk),
     v (batch, heads, dv); state (pool, heads, dk, dv) float32; slots: None (sequence b has entry b), or an int32 tensor of
-    each sequence's entry, all different; an entry outside the pool marks a sequence to skip (its output is zero)."""
+    each sequence's entry, all different; an entry outside the pool marks a sequence to skip (its output is zero).
+    No gradient is computed: with gradients enabled, inputs that require one are refused."""
     if forward_ad._current_level >= 0:
         _no_tangents(q=q, k=k, v=v, log_decay=log_decay, state=state)
+    if torch.is_grad_enabled():
+        _not_recorded(q=q, k=k, v=v, state=state)
     dtype, device, shape = q.dtype, q.device, q.shape
     if k.dtype != dtype or v.dtype != dtype or k.device != device or v.device != device:
         _refuse(dtype, device, k=k, v=v)
@@ -307,6 +322,7 @@ def linear_attention_step(q, k, v, log_decay, state, scale=None, slots=None):
     args = B.tcu_linattn_args(_FLOAT[dtype], batch, 1, heads, dk, dv, dk ** -0.5 if scale is None else float(scale), log_decay.data_ptr(),
                               qv, kv, vv, (o.data_ptr(), heads * dv, 0, dv), d_slots=_ptr(slots), pool_slots=pool[0], d_state_out=state.data_ptr())
     B.check(B.tcu_linattn_step(args, _stream(device)))
+    _written(state)
     return o
 
 
@@ -322,6 +338,8 @@ def embedding_backward(d_out, ids, num_rows, scale=1.0, dtype=torch.float32, out
     instead (rows without tokens are not touched)."""
     if forward_ad._current_level >= 0:
         _no_tangents(d_out=d_out, out=out)
+    if out is not None and torch.is_grad_enabled():
+        _not_recorded(out=out)
     device, kind = d_out.device, d_out.dtype
     d_out, ids = d_out.contiguous(), _ids(ids, device)
     d = d_out.shape[-1]
@@ -339,6 +357,8 @@ def embedding_backward(d_out, ids, num_rows, scale=1.0, dtype=torch.float32, out
     ws = ids.new_empty((ws_bytes + 7) // 8, dtype=torch.int64) if ws_bytes else None
     B.check(B.tcu_embedding_backward(d_out, _FLOAT[kind], ids, ids.element_size(), n, num_rows, d, float(scale), out is not None,
                                      table, _FLOAT[table.dtype], ws, ws_bytes, _stream(device)))
+    if out is not None:
+        _written(out)
     return table
 
 

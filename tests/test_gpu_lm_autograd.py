@@ -60,3 +60,47 @@ def test_tangents_are_refused():
         # without one the calls are as ever
         assert torch.equal(api.linear_attention(q, k, v, decay, initial_state=s0)[0], plain[0])
         assert torch.equal(api.embedding(ids, table), plain[1])
+
+
+def test_what_is_written_in_place_is_known():
+    """A state, or a sum, that a backward pass has saved and that is then written to: torch raises, as for its own operators."""
+    q, k, v, d_o, decay, s0, _ = draw(3, 1, 50, 2, 16, 16, torch.bfloat16, True)
+    token = [x[:, 0].clone() for x in (q, k, v)]
+    q.requires_grad_()
+    o, _ = api.linear_attention(q, k, v, decay, initial_state=s0)
+    api.linear_attention_step(*token, decay, s0)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        o.backward(d_o)
+    ids, held, x = torch.arange(9, device="cuda"), torch.randn((9, 8), device="cuda"), torch.randn((9, 8), device="cuda", requires_grad=True)
+    y = (x * held).sum()
+    api.embedding_backward(torch.ones((9, 8), device="cuda"), ids, 9, out=held)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        y.backward()
+    # a state that has been through nothing but steps, made where versions are not kept
+    with torch.inference_mode():
+        pool = torch.zeros((1, 2, 16, 16), device="cuda")
+    api.linear_attention_step(*token, decay, pool)
+    with torch.inference_mode():
+        api.linear_attention_step(*token, decay, pool)
+        api.embedding_backward(torch.ones((9, 8), device="cuda"), ids, 9, out=held)
+
+
+def test_steps_do_not_lose_gradients():
+    """Single tokens have no backward pass: inputs that want one are refused, unless gradients are off."""
+    q, k, v, _, decay, s0, _ = draw(4, 1, 1, 2, 16, 16, torch.bfloat16, True)
+    args = [x[:, 0] for x in (q, k, v)] + [decay, s0]
+    want_state = s0.clone()
+    want = api.linear_attention_step(*args[:4], want_state)
+    for which in (0, 1, 2, 4):
+        some = list(args)
+        some[which] = some[which].clone().requires_grad_()
+        with pytest.raises(RuntimeError, match="no_grad"):
+            api.linear_attention_step(*some)
+    assert torch.equal(s0, args[4])
+    with torch.no_grad():
+        state = s0.clone().requires_grad_()
+        assert torch.equal(api.linear_attention_step(args[0].clone().requires_grad_(), *args[1:4], state), want)
+        assert torch.equal(state, want_state)
+    grad = torch.zeros((9, 8), device="cuda", requires_grad=True)
+    with pytest.raises(RuntimeError, match="no_grad"):
+        api.embedding_backward(torch.ones((9, 8), device="cuda"), torch.arange(9, device="cuda"), 9, out=grad)
