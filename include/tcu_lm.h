@@ -71,7 +71,8 @@ typedef struct {
 } tcu_linattn_t;
 
 /* Workspace of the forward and backward calls: the status of bounded waits (tcu_scan_device_status reads it).  Clear it
- * once with tcu_scan_workspace_init; any number of calls, concurrent ones too, may share it. */
+ * once with tcu_scan_workspace_init; any number of calls, concurrent ones too, may share it.  It may lie in page-locked host memory
+ * as well, where the host clears it (zeros), and reads without waiting what its third 32-bit word holds: 0, or TCU_ERR_TIMEOUT. */
 size_t tcu_linattn_workspace_bytes(void);
 
 /* Bytes of scratch with which a forward (or backward) call with these arguments runs faster; 0 if it would not, as when there are

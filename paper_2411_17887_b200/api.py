@@ -2,6 +2,9 @@
 torch (plumbing) and calls the C-ABI entry points.  No arithmetic happens here."""
 from __future__ import annotations
 
+import ctypes
+import threading
+
 import torch
 from torch.autograd import forward_ad
 from torch.autograd.function import once_differentiable
@@ -74,7 +77,21 @@ def segmented_scan(x: torch.Tensor, offsets: torch.Tensor, s: int = 16, exclusiv
 _FLOAT = {torch.float32: B.TCU_F32, torch.float16: B.TCU_F16, torch.bfloat16: B.TCU_BF16}
 # the handle alone: a torch.cuda.Stream around it costs 3 us, a third of a small call
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
-_status = {}          # device index -> (buffer, pointer, SMs): where the linear-attention kernels record a wait that ran out
+
+class _Status:
+    """Where the linear-attention kernels of a device record a wait that ran out: a workspace in page-locked host memory, cleared by the
+    host (a captured call leaves no clearing in its graph) and read by it without waiting for anything."""
+
+    def __init__(self, index: int):
+        size = B.tcu_linattn_workspace_bytes()
+        self.buffer = torch.zeros(size + 256, dtype=torch.uint8, pin_memory=True)
+        self.ptr = self.buffer.data_ptr() + (-self.buffer.data_ptr()) % 256
+        self.error = ctypes.c_uint32.from_address(self.ptr + 8)          # the third word
+        self.multiprocessors = torch.cuda.get_device_properties(index).multi_processor_count
+
+
+_status = {}          # device index -> _Status
+_status_lock = threading.Lock()
 
 
 def _stream(device: torch.device) -> int:
@@ -86,14 +103,12 @@ def _stream(device: torch.device) -> int:
     return _raw_stream(device.index)
 
 
-def _status_ptr(device: torch.device) -> int:
-    held = _status.get(device.index)
+def _status_of(index: int) -> _Status:
+    held = _status.get(index)
     if held is None:
-        buf = torch.zeros(B.tcu_linattn_workspace_bytes() + 256, dtype=torch.uint8, device=device)
-        if not torch.cuda.is_current_stream_capturing():
-            torch.cuda.current_stream().synchronize()       # other streams may use it next
-        held = _status[device.index] = (buf, buf.data_ptr() + (-buf.data_ptr()) % 256, torch.cuda.get_device_properties(device).multi_processor_count)
-    return held[1]
+        with _status_lock:                       # (kernels write to it: no thread may drop another's)
+            held = _status.get(index) or _status.setdefault(index, _Status(index))
+    return held
 
 
 def linear_attention_status(device=None) -> int:
@@ -102,7 +117,8 @@ def linear_attention_status(device=None) -> int:
     index = torch.cuda.current_device() if device is None else torch.device(device).index
     if index not in _status:
         return B.TCU_OK
-    return B.tcu_scan_device_status(_status[index][1], torch.cuda.current_stream().cuda_stream)
+    torch.cuda.current_stream().synchronize()
+    return B.TCU_ERR_TIMEOUT if _status[index].error.value else B.TCU_OK
 
 
 def _written(x: torch.Tensor) -> None:
@@ -202,19 +218,19 @@ class _Mix:
         self.offsets = offsets.data_ptr() if packed else 0
         self.log_decay = log_decay
         self.stream = _stream(device)
-        self.status = _status_ptr(device)
+        self.status = _status_of(device.index)
 
     def new_state(self):
         return self.log_decay.new_empty(self.state_shape)
 
     def call(self, fn, backward, q, k, v, o=B.NO_TOKENS, **more):
         args = B.tcu_linattn_args(*self.head, q, k, v, o, d_offsets=self.offsets, **more)
-        if self.head[1] * self.head[3] * (3 if backward else 1) > _status[self.log_decay.device.index][2]:
+        if self.head[1] * self.head[3] * (3 if backward else 1) > self.status.multiprocessors:
             size = B.tcu_linattn_scratch_bytes(args, backward)
             if size:
                 scratch = self.log_decay.new_empty((size + 3) // 4)
                 args = B.tcu_linattn_with_scratch(args, scratch.data_ptr(), size)
-        B.check(fn(args, self.status, 256, self.stream))
+        B.check(fn(args, self.status.ptr, 256, self.stream))
 
 
 def _ptr(x) -> int:

@@ -1184,7 +1184,7 @@ __global__ void __launch_bounds__(kMixThreads, 1) tcu_linattn_mix_kernel(const _
         }
     } while (CUT && M::goes_on());
     if (warp == kProductWarp) tmem_dealloc(ctl->tmem_base, M::kColumns);
-    if (threadIdx.x == 0 && ctl->abort_flag) atomicExch(p.error, 5u);
+    if (threadIdx.x == 0 && ctl->abort_flag) st_system_u32(p.error, 5u);             // (it may lie on the host)
 }
 
 // ---- single tokens ---------------------------------------------------------------------------------------------------
