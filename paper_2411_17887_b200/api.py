@@ -112,12 +112,19 @@ def _status_of(index: int) -> _Status:
 
 
 def linear_attention_status(device=None) -> int:
-    """Waits for the current stream; 0, or TCU_ERR_TIMEOUT if a linear-attention call on `device` gave up a wait (its
-    outputs are then not valid)."""
-    index = torch.cuda.current_device() if device is None else torch.device(device).index
+    """Waits for the current stream of `device` (an index, "cuda" or "cuda:1"; the current device by default); 0, or
+    TCU_ERR_TIMEOUT if a linear-attention call on it gave up a wait (its outputs are then not valid)."""
+    index = None
+    if device is not None:
+        device = torch.device("cuda", device) if isinstance(device, int) else torch.device(device)
+        if device.type != "cuda":
+            raise ValueError(f"a CUDA device is needed, not {device}")
+        index = device.index
+    if index is None:
+        index = torch.cuda.current_device()
     if index not in _status:
         return B.TCU_OK
-    torch.cuda.current_stream().synchronize()
+    torch.cuda.current_stream(index).synchronize()
     return B.TCU_ERR_TIMEOUT if _status[index].error.value else B.TCU_OK
 
 
