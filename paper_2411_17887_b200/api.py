@@ -108,12 +108,16 @@ def _status_of(index: int) -> _Status:
     if held is None:
         with _status_lock:                       # (kernels write to it: no thread may drop another's)
             held = _status.get(index) or _status.setdefault(index, _Status(index))
+    if held.error.value:
+        held.error.value = 0
+        raise RuntimeError(f"an earlier linear-attention call on cuda:{index} gave up a wait: its outputs are not valid")
     return held
 
 
 def linear_attention_status(device=None) -> int:
     """Waits for the current stream of `device` (an index, "cuda" or "cuda:1"; the current device by default); 0, or
-    TCU_ERR_TIMEOUT if a linear-attention call on it gave up a wait (its outputs are then not valid)."""
+    TCU_ERR_TIMEOUT if a linear-attention call on it gave up a wait (its outputs are then not valid).  Whoever learns of it
+    first clears it: this function, or the next linear-attention call on the device, which raises."""
     index = None
     if device is not None:
         device = torch.device("cuda", device) if isinstance(device, int) else torch.device(device)
@@ -125,7 +129,9 @@ def linear_attention_status(device=None) -> int:
     if index not in _status:
         return B.TCU_OK
     torch.cuda.current_stream(index).synchronize()
-    return B.TCU_ERR_TIMEOUT if _status[index].error.value else B.TCU_OK
+    gave_up = _status[index].error.value != 0
+    _status[index].error.value = 0
+    return B.TCU_ERR_TIMEOUT if gave_up else B.TCU_OK
 
 
 def _written(x: torch.Tensor) -> None:

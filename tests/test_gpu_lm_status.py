@@ -80,3 +80,20 @@ def test_threads_share_one_status(monkeypatch):
     for one in threads:
         one.join()
     assert len(got) == 8 and all(one is got[0] for one in got) and api._status == {0: got[0]}
+
+
+def test_the_next_call_raises():
+    """A loop that never asks for the status does not go on with invalid tensors."""
+    q, k, v, d_o, decay, _, _ = draw(2, 1, 200, 2, 64, 64, torch.bfloat16)
+    want = api.linear_attention(q, k, v, decay)[0]
+    for call in (lambda: api.linear_attention(q, k, v, decay), lambda: api.linear_attention_backward(d_o, q, k, v, decay),
+                 lambda: api.linear_attention(q.clone().requires_grad_(), k, v, decay)):
+        give_up()
+        with pytest.raises(RuntimeError, match="gave up a wait"):
+            call()
+        call()                                          # it is said once
+        assert api.linear_attention_status() == B.TCU_OK
+        give_up()
+        assert api.linear_attention_status("cuda") == B.TCU_ERR_TIMEOUT
+        call()
+    assert torch.equal(api.linear_attention(q, k, v, decay)[0], want)
