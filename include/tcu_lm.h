@@ -109,7 +109,7 @@ tcu_status_t tcu_linattn_step(const tcu_linattn_t *args, cudaStream_t stream);
 
 /* out[n][0..d) = scale * table[ids[n]][0..d): products in fp32, rounded once to the type.
  *   d_ids      device, n values of 4 or 8 bytes (id_bytes), signed; an id outside [0, rows) gives a row of zeros
- *   d_table    device, rows x d, row stride table_stride elements;  d_out  device, n x d dense, of the same type */
+ *   d_table    device, rows x d, row stride table_stride elements (at most 2^38);  d_out  device, n x d dense, of the same type */
 tcu_status_t tcu_embedding_forward(const void *d_ids, int id_bytes, size_t n, const void *d_table, size_t rows, size_t d,
                                    size_t table_stride, tcu_float_t type, float scale, void *d_out, cudaStream_t stream);
 

@@ -30,14 +30,16 @@ tcu_status_t launched() { return cudaGetLastError() == cudaSuccess ? TCU_OK : TC
 // ---- linear attention
 bool has_struct(const tcu_linattn_t *a) { return a && a->struct_bytes == sizeof(tcu_linattn_t); }
 
-// First and one-past-last byte that a token array may touch (packed: batch is 1).
+// First and one-past-last byte that a token array may touch (packed: batch is 1); to the end of all addresses if it has no such last byte.
 struct Span {
     uintptr_t lo, hi;
 };
 Span span_of(const tcu_tokens_t &x, uint64_t batch, uint64_t tokens, uint32_t heads, uint32_t width, size_t eb) {
-    const uint64_t last = (batch - 1) * uint64_t(x.stride_batch) + (tokens - 1) * uint64_t(x.stride_token) + uint64_t(heads - 1) * uint64_t(x.stride_head) + width;
+    using Wide = unsigned __int128;
     const auto lo = reinterpret_cast<uintptr_t>(x.ptr);
-    return {lo, lo + last * eb};
+    const Wide last = Wide(batch - 1) * uint64_t(x.stride_batch) + Wide(tokens - 1) * uint64_t(x.stride_token) + Wide(heads - 1) * uint64_t(x.stride_head) + width;
+    const Wide end = lo + last * eb;
+    return {lo, end > ~uintptr_t(0) ? ~uintptr_t(0) : uintptr_t(end)};
 }
 bool spans_meet(const Span &a, const Span &b) { return a.lo < b.hi && b.lo < a.hi; }
 
@@ -60,14 +62,18 @@ struct WsStatus {
     uint32_t epoch, done, error;
 };
 
-// What forward and backward share.  `empty` is set when there is nothing to walk (states may still have to be written).
+// Sequences times heads, so that three jobs of eight blocks each are a grid.  (Batch and heads alone may have a product of more than 64 bits.)
+constexpr uint64_t kMostWalks = ((uint64_t(1) << 31) - 1) / 24;
+bool too_many(const tcu_linattn_t *a) { return a->heads > 0 && a->batch > kMostWalks / a->heads; }
+constexpr uint64_t kMostMixTokens = (uint64_t(1) << 31) - 256;
+
+// What forward and backward share.
 tcu_status_t check_linattn(const tcu_linattn_t *a, const void *d_ws, size_t ws_bytes) {
     if (!has_struct(a)) return TCU_ERR_INVALID_ARG;
     if (a->type != TCU_F16 && a->type != TCU_BF16) return TCU_ERR_INVALID_ARG;
     if (a->heads == 0 || a->dk == 0 || a->dv == 0) return TCU_ERR_INVALID_ARG;
     if (a->dk > 128 || a->dv > 128) return TCU_ERR_UNSUPPORTED;
-    if (a->tokens > (uint64_t(1) << 31) - 256) return TCU_ERR_UNSUPPORTED;
-    if (a->batch > (uint64_t(1) << 31) || a->batch * a->heads * 3 * 8 > (uint64_t(1) << 31) - 1) return TCU_ERR_UNSUPPORTED;
+    if (a->tokens > kMostMixTokens || too_many(a)) return TCU_ERR_UNSUPPORTED;
     if (a->batch == 0) return TCU_OK;
     if (!d_ws || ws_bytes < kStatusBytes) return TCU_ERR_WORKSPACE;
     if (!aligned(d_ws, 16) || !a->d_log_decay || !aligned(a->d_log_decay, 4)) return TCU_ERR_INVALID_ARG;
@@ -374,7 +380,7 @@ extern "C" {
 size_t tcu_linattn_workspace_bytes(void) { return kStatusBytes; }
 
 size_t tcu_linattn_scratch_bytes(const tcu_linattn_t *a, int backward) {
-    if (!has_struct(a) || a->dk == 0 || a->dk > 128 || a->dv == 0 || a->dv > 128 || a->batch > (uint64_t(1) << 31) || a->batch * a->heads * 3 > (uint64_t(1) << 31)) return 0;
+    if (!has_struct(a) || a->dk == 0 || a->dk > 128 || a->dv == 0 || a->dv > 128 || a->tokens > kMostMixTokens || too_many(a)) return 0;
     return scratch_bytes(a, backward ? 3 : 1);
 }
 
@@ -606,13 +612,13 @@ extern "C" {
 tcu_status_t tcu_embedding_forward(const void *d_ids, int id_bytes, size_t n, const void *d_table, size_t rows, size_t d, size_t table_stride,
                                    tcu_float_t type, float scale, void *d_out, cudaStream_t stream) {
     if (!valid_float(type) || (id_bytes != 4 && id_bytes != 8)) return TCU_ERR_INVALID_ARG;
-    if (table_stride < d) return TCU_ERR_INVALID_ARG;
+    if (table_stride < d || (rows > 1 && table_stride > uint64_t(1) << 38)) return TCU_ERR_INVALID_ARG;
     if (n > kMostTokens || rows > kMostTokens || d > kMostColumns) return TCU_ERR_UNSUPPORTED;
     if (n == 0 || d == 0) return TCU_OK;
     const size_t eb = float_bytes(type);
     if (!d_ids || !d_out || (!d_table && rows > 0)) return TCU_ERR_INVALID_ARG;
     if (!aligned(d_ids, id_bytes) || !aligned(d_table, eb) || !aligned(d_out, eb)) return TCU_ERR_INVALID_ARG;
-    if (overlaps(d_out, n * d * eb, d_table, rows ? ((rows - 1) * table_stride + d) * eb : 0) || overlaps(d_out, n * d * eb, d_ids, n * id_bytes)) return TCU_ERR_INVALID_ARG;
+    if (overlaps(d_out, n * d * eb, d_table, rows > 1 ? ((rows - 1) * table_stride + d) * eb : rows * d * eb) || overlaps(d_out, n * d * eb, d_ids, n * id_bytes)) return TCU_ERR_INVALID_ARG;
     const int vec = vec_of(d, table_stride, eb, {d_table, d_out});
     auto go = [&](auto t) {
         using T = decltype(t);

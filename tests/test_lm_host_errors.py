@@ -1,6 +1,5 @@
-"""A CUDA call that fails on the host ends a call of the language-model operators: nothing is queued behind it (the kernels of a
-sequence index memory by what the ones before have written), and the caller gets TCU_ERR_CUDA.  The library's host code runs
-here on a runtime without a GPU, of which one call is made to fail."""
+"""The host code of the language-model operators on a runtime without a GPU.  A CUDA call that fails on the host ends a call of the language-model operators: nothing is queued behind it (the kernels of a
+sequence index memory by what the ones before have written), and the caller gets TCU_ERR_CUDA.  And what is refused is refused before anything is queued."""
 import ctypes
 import os
 import subprocess
@@ -92,3 +91,31 @@ def test_walks_that_cannot_be_cut_run_whole(lib, B):
     assert run() == B.TCU_OK and lib.fake_launches() == 1
     lib.fake_reset(b"cudaLaunchKernelExC", 1)
     assert run() == B.TCU_OK and lib.fake_launches() == 2
+
+
+@pytest.mark.parametrize("batch,heads", [(1 << 31, 1 << 30), (1 << 31, 1), (1 << 26, 2), (3, (1 << 32) - 1), ((1 << 63) + 1, 2), ((1 << 64) - 1, (1 << 32) - 1)])
+def test_more_walks_than_a_grid_has_blocks(lib, B, batch, heads):
+    """Also where batch times heads wraps around in 64 bits to a small number."""
+    at = lambda i: (i << 36, 1 << 20, 64, 64)  # noqa: E731
+    args = B.tcu_linattn_args(B.TCU_BF16, batch, 100, heads, 64, 64, 1.0, 1 << 35, at(1), at(2), at(3), at(4), d_o=at(5), d_q=at(6), d_k=at(7), d_v=at(8))
+    lib.fake_reset(b"", 0)
+    for fn in (lib.tcu_linattn_forward, lib.tcu_linattn_backward):
+        assert fn(args, p(1 << 32), ctypes.c_size_t(256), None) == B.TCU_ERR_UNSUPPORTED
+    for backward in (0, 1):
+        assert lib.tcu_linattn_scratch_bytes(args, backward) == 0
+    assert lib.fake_launches() == 0
+
+
+def test_arrays_as_large_as_the_addresses(lib, B):
+    """An array whose last byte has no address overlaps whatever lies behind its first one."""
+    big = (1 << 36, (1 << 38) - 8, 64, 64)                               # 2^25 sequences of 2^39 bytes each
+    o = ((1 << 36) + (1 << 30), 64, 64, 64)
+    args = B.tcu_linattn_args(B.TCU_BF16, (1 << 25) + 1, 1, 1, 64, 64, 1.0, 1 << 35, big, (1 << 60, 0, 0, 0), (1 << 60, 0, 0, 0), o)
+    lib.fake_reset(b"", 0)
+    assert lib.tcu_linattn_forward(args, p(1 << 32), ctypes.c_size_t(256), None) == B.TCU_ERR_INVALID_ARG
+    assert lib.fake_launches() == 0
+    table = lambda stride, rows: lib.tcu_embedding_forward(p(3 << 32), 8, ctypes.c_size_t(10), p(2 << 40), ctypes.c_size_t(rows), ctypes.c_size_t(8),  # noqa: E731
+                                                           ctypes.c_size_t(stride), 2, ctypes.c_float(1.0), p((2 << 40) + 4096), None)
+    assert table(1 << 62, 9) == B.TCU_ERR_INVALID_ARG
+    assert lib.fake_launches() == 0
+    assert table(1 << 62, 1) == B.TCU_OK                                 # one row: no stride
