@@ -104,7 +104,8 @@ tcu_status_t tcu_linattn_selftest_timeout(const tcu_linattn_t *args, int backwar
 
 /* One token for each of `batch` sequences: the state of each (an entry of the pool d_state_out, (pool_slots, heads, dk, dv)) is
  * updated in place, and o written.  q, k, v, o: stride_token is not used; any alignment of elements.  The pool: 16-byte
- * aligned.  Needs no workspace. */
+ * aligned.  Needs no workspace.  o may be v, with its strides; its elements must not be elements of q or k (which is looked at only
+ * where they begin at the same address), nor of another head's or sequence's v: blocks read and write in any order. */
 tcu_status_t tcu_linattn_step(const tcu_linattn_t *args, cudaStream_t stream);
 
 /* out[n][0..d) = scale * table[ids[n]][0..d): products in fp32, rounded once to the type.

@@ -414,6 +414,8 @@ tcu_status_t tcu_linattn_step(const tcu_linattn_t *a, cudaStream_t stream) {
         if (x->stride_batch < 0 || x->stride_head < 0 || x->stride_batch >= limit || x->stride_head >= limit) return TCU_ERR_INVALID_ARG;
     }
     if ((a->batch > 1 && a->o.stride_batch == 0) || (a->heads > 1 && a->o.stride_head == 0)) return TCU_ERR_INVALID_ARG;
+    // Each block reads q and k of its head, and v in the columns of o that it writes; a head has more than one block from dv = 65 on.
+    if (a->dv > uint32_t(kStepCols) && (a->o.ptr == a->q.ptr || a->o.ptr == a->k.ptr)) return TCU_ERR_INVALID_ARG;
     StepParams p = {view(a->q), view(a->k), view(a->v), view(a->o), a->d_state_out, a->d_slots, a->d_log_decay, a->pool_slots,
                     uint32_t(a->batch), a->heads, a->dk, a->dv, a->scale};
     const dim3 grid(uint32_t(a->batch) * a->heads, (a->dv + kStepCols - 1) / kStepCols);

@@ -119,3 +119,14 @@ def test_arrays_as_large_as_the_addresses(lib, B):
     assert table(1 << 62, 9) == B.TCU_ERR_INVALID_ARG
     assert lib.fake_launches() == 0
     assert table(1 << 62, 1) == B.TCU_OK                                 # one row: no stride
+
+
+def test_a_step_does_not_write_over_what_other_blocks_read(lib, B):
+    """From 65 columns on a head's blocks read all of q and k while another writes its part of o."""
+    q, k, v = ((i << 36, 2 * 128, 0, 128) for i in range(1, 4))
+    for dv in (64, 65, 128):
+        for o, ok in (((4 << 36, 2 * 128, 0, 128), True), (v, True), (q, dv <= 64), (k, dv <= 64)):
+            args = B.tcu_linattn_args(B.TCU_BF16, 3, 1, 2, 128, dv, 1.0, 1 << 35, q, k, v, o, d_state_out=5 << 36, pool_slots=3)
+            lib.fake_reset(b"", 0)
+            assert lib.tcu_linattn_step(args, None) == (B.TCU_OK if ok else B.TCU_ERR_INVALID_ARG)
+            assert lib.fake_launches() == ok
