@@ -25,6 +25,12 @@ bool overlaps(const void *a, size_t an, const void *b, size_t bn) {
     auto pa = reinterpret_cast<uintptr_t>(a), pb = reinterpret_cast<uintptr_t>(b);
     return a && b && pa < pb + bn && pb < pa + an;
 }
+// Whether a runtime call went well; if not, its error is taken here and is not left for the check of a later launch.
+bool ok(cudaError_t e) {
+    if (e == cudaSuccess) return true;
+    (void)cudaGetLastError();
+    return false;
+}
 tcu_status_t launched() { return cudaGetLastError() == cudaSuccess ? TCU_OK : TCU_ERR_CUDA; }
 
 // ---- linear attention
@@ -94,7 +100,7 @@ EncodeTiledFn encode_fn() {
     std::call_once(once, [] {
         void *p = nullptr;
         cudaDriverEntryPointQueryResult q;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess)
+        if (ok(cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q)) && q == cudaDriverEntryPointSuccess)
             fn = reinterpret_cast<EncodeTiledFn>(p);
     });
     return fn;
@@ -119,7 +125,7 @@ int sm_count() {
     int v = cached.load();
     if (v > 0) return v;
     int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&v, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+    if (!ok(cudaGetDevice(&dev)) || !ok(cudaDeviceGetAttribute(&v, cudaDevAttrMultiProcessorCount, dev))) return 0;
     cached.store(v);
     return v;
 }
@@ -151,15 +157,15 @@ tcu_status_t choose_ranks(uint64_t units, uint64_t groups, uint32_t *ranks) {
     static std::atomic<int> configured{-1};
     static std::atomic<int> at_once[kMostRanks + 1];
     int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) return TCU_ERR_CUDA;
+    if (!ok(cudaGetDevice(&dev))) return TCU_ERR_CUDA;
     if (configured.load() != dev) {
-        if (cudaFuncSetAttribute(tcu_linattn_mix_kernel<D, T, kWhole>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMixSmemBytes<D>) != cudaSuccess) return TCU_ERR_CUDA;
+        if (!ok(cudaFuncSetAttribute(tcu_linattn_mix_kernel<D, T, kWhole>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMixSmemBytes<D>))) return TCU_ERR_CUDA;
         at_once[1] = sm_count();
         for (uint32_t r = 2; r <= kMostRanks; ++r) {
             cudaLaunchAttribute attr;
             const cudaLaunchConfig_t cfg = mix_config<D, T>(r, r, &attr, nullptr);
             int n = 0;
-            at_once[r] = cudaOccupancyMaxActiveClusters(&n, tcu_linattn_mix_kernel<D, T, kWhole>, &cfg) == cudaSuccess ? n : 0;
+            at_once[r] = ok(cudaOccupancyMaxActiveClusters(&n, tcu_linattn_mix_kernel<D, T, kWhole>, &cfg)) ? n : 0;
         }
         configured.store(dev);
     }
@@ -203,12 +209,12 @@ template <int D, typename T, int KIND>
 tcu_status_t launch_kind(const MixParams &p, const cudaLaunchConfig_t &cfg) {
     static std::atomic<int> configured{-1};
     int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) return TCU_ERR_CUDA;
+    if (!ok(cudaGetDevice(&dev))) return TCU_ERR_CUDA;
     if (configured.load() != dev) {
-        if (cudaFuncSetAttribute(tcu_linattn_mix_kernel<D, T, KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMixSmemBytes<D>) != cudaSuccess) return TCU_ERR_CUDA;
+        if (!ok(cudaFuncSetAttribute(tcu_linattn_mix_kernel<D, T, KIND>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMixSmemBytes<D>))) return TCU_ERR_CUDA;
         configured.store(dev);
     }
-    return cudaLaunchKernelEx(&cfg, tcu_linattn_mix_kernel<D, T, KIND>, p) == cudaSuccess ? TCU_OK : TCU_ERR_CUDA;
+    return ok(cudaLaunchKernelEx(&cfg, tcu_linattn_mix_kernel<D, T, KIND>, p)) ? TCU_OK : TCU_ERR_CUDA;
 }
 
 template <int D, typename T>
@@ -219,13 +225,12 @@ tcu_status_t launch_mix(const tcu_linattn_t *a, MixParams &p, uint64_t groups, c
         p.ranks = 1;
         p.flags = static_cast<uint32_t *>(a->d_scratch);
         p.handed = reinterpret_cast<float *>(static_cast<uint8_t *>(a->d_scratch) + flag_bytes());
-        if (cudaMemsetAsync(p.flags, 0, flag_bytes(), stream) != cudaSuccess) return TCU_ERR_CUDA;
+        if (!ok(cudaMemsetAsync(p.flags, 0, flag_bytes(), stream))) return TCU_ERR_CUDA;
         cudaLaunchConfig_t cfg = mix_config<D, T>(uint32_t(sm_count()), 1, &attr, stream);
         attr.id = cudaLaunchAttributeCooperative;          // blocks wait for one another: all of them run at once
         attr.val.cooperative = 1;
         cfg.numAttrs = 1;
-        if (launch_kind<D, T, kCut>(p, cfg) == TCU_OK) return TCU_OK;
-        (void)cudaGetLastError();                          // not all SMs are this process's to use: whole walks
+        if (launch_kind<D, T, kCut>(p, cfg) == TCU_OK) return TCU_OK;                  // else not all SMs are this process's to use: whole walks
     }
     if (tcu_status_t st = choose_ranks<D, T>(units, groups, &p.ranks)) return st;
     const cudaLaunchConfig_t cfg = mix_config<D, T>(units * p.ranks, p.ranks, &attr, stream);
@@ -267,7 +272,7 @@ tcu_status_t run_mix(const tcu_linattn_t *a, MixParams &p, const tcu_tokens_t *c
     if (!encode_fn()) return TCU_ERR_CUDA;
     thread_local int bound = -1;      // encoding needs a current context, which a thread that has made no CUDA call does not have
     int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || (bound != dev && cudaSetDevice(dev) != cudaSuccess)) return TCU_ERR_CUDA;
+    if (!ok(cudaGetDevice(&dev)) || (bound != dev && !ok(cudaSetDevice(dev)))) return TCU_ERR_CUDA;
     bound = dev;
     for (int i = 0; i < count; ++i)
         if (!encode_tokens(&p.map[i], a, *arrays[i], widths[i])) return TCU_ERR_CUDA;
@@ -306,8 +311,7 @@ struct Waits {
 // No tokens: the state that leaves is the state that enters.
 tcu_status_t copy_state(float *to, const float *from, size_t bytes, cudaStream_t stream) {
     if (!to || to == from) return TCU_OK;
-    const cudaError_t e = from ? cudaMemcpyAsync(to, from, bytes, cudaMemcpyDeviceToDevice, stream) : cudaMemsetAsync(to, 0, bytes, stream);
-    return e == cudaSuccess ? TCU_OK : TCU_ERR_CUDA;
+    return ok(from ? cudaMemcpyAsync(to, from, bytes, cudaMemcpyDeviceToDevice, stream) : cudaMemsetAsync(to, 0, bytes, stream)) ? TCU_OK : TCU_ERR_CUDA;
 }
 
 tcu_status_t forward(const tcu_linattn_t *a, void *d_ws, size_t ws_bytes, const Waits &waits, cudaStream_t stream) {
@@ -519,9 +523,7 @@ tcu_status_t launch_next(void (*kernel)(P...), dim3 grid, dim3 block, cudaStream
     cfg.stream = stream;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, kernel, P(args)...) == cudaSuccess) return TCU_OK;
-    (void)cudaGetLastError();
-    return TCU_ERR_CUDA;
+    return ok(cudaLaunchKernelEx(&cfg, kernel, P(args)...)) ? TCU_OK : TCU_ERR_CUDA;
 }
 
 // Tiles whose counts every block of the sort adds up by itself; more are scanned by a kernel between.  65536 tokens of 64 columns, 64 tiles:
@@ -539,12 +541,9 @@ tcu_status_t sort_tokens(const void *ids, uint32_t n, uint32_t rows, const Embed
     if (n <= kBlockTokens) {
         static std::atomic<int> configured{-1};
         int dev = 0;
-        if (cudaGetDevice(&dev) != cudaSuccess) return TCU_ERR_CUDA;
+        if (!ok(cudaGetDevice(&dev))) return TCU_ERR_CUDA;
         if (configured.load() != dev) {
-            if (cudaFuncSetAttribute(tcu_sort_block_kernel<ID>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(sizeof(BlockSort))) != cudaSuccess) {
-                (void)cudaGetLastError();
-                return TCU_ERR_CUDA;
-            }
+            if (!ok(cudaFuncSetAttribute(tcu_sort_block_kernel<ID>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(sizeof(BlockSort))))) return TCU_ERR_CUDA;
             configured.store(dev);
         }
         tcu_sort_block_kernel<ID><<<1, kBlockThreads, sizeof(BlockSort), stream>>>(id, n, rows, bits, at(w.keys[0]), at(w.tokens[0]), at(w.joins));
@@ -648,7 +647,7 @@ tcu_status_t tcu_embedding_backward(const void *d_out, tcu_float_t type, const v
     if (!d_table || !aligned(d_table, tb)) return TCU_ERR_INVALID_ARG;
     if (n == 0) {
         if (accumulate) return TCU_OK;
-        return cudaMemsetAsync(d_table, 0, rows * d * tb, stream) == cudaSuccess ? TCU_OK : TCU_ERR_CUDA;
+        return ok(cudaMemsetAsync(d_table, 0, rows * d * tb, stream)) ? TCU_OK : TCU_ERR_CUDA;
     }
     if (!d_out || !d_ids || !aligned(d_ids, id_bytes) || !aligned(d_out, eb)) return TCU_ERR_INVALID_ARG;
     if (!d_ws || ws_bytes < tcu_embedding_workspace_bytes(n, rows, d)) return TCU_ERR_WORKSPACE;

@@ -24,7 +24,7 @@ extern "C" {
 void fake_reset(const char *name, int at) {
     std::strncpy(fail_name, name, sizeof(fail_name) - 1);
     fail_at = at;
-    calls_of_it = launches = after_failure = last_error = 0;
+    calls_of_it = launches = after_failure = 0;                              // (not last_error: the library has to have taken it)
     failed = false;
 }
 int fake_launches() { return launches; }

@@ -130,3 +130,29 @@ def test_a_step_does_not_write_over_what_other_blocks_read(lib, B):
             lib.fake_reset(b"", 0)
             assert lib.tcu_linattn_step(args, None) == (B.TCU_OK if ok else B.TCU_ERR_INVALID_ARG)
             assert lib.fake_launches() == ok
+
+
+def test_no_error_is_left_for_a_later_call(lib, B, tmp_path):
+    """Errors that a call has reported, or has found a way around, are not found again by the launch check of the next one.  (A library of
+    its own, that remembers nothing.)"""
+    import shutil
+    for name in ("cudaOccupancyMaxActiveClusters", "cudaFuncSetAttribute", "cudaGetDevice", "cudaDeviceGetAttribute", "cudaMemsetAsync", "cudaMemcpyAsync"):
+        one = str(tmp_path / f"{name}.so")
+        shutil.copy(lib._name, one)
+        one = ctypes.CDLL(one, mode=os.RTLD_LOCAL | os.RTLD_NOW)
+        one.fake_reset(name.encode(), 1)
+        calls = [CALLS[what] for what in ("packed sequences in order", "gradient of 2000 tokens")] + [lambda lib, B: attention(lib, B, 0, 2, 700, 80, False)]
+        calls.append(lambda lib, B: lib.tcu_linattn_forward(B.tcu_linattn_args(B.TCU_BF16, 1, 0, 1, 64, 64, 1.0, 1 << 35, *[(0, 0, 0, 0)] * 4, d_state_in=1 << 36,
+                                                                               d_state_out=1 << 37), p(1 << 32), ctypes.c_size_t(256), None))
+        for call in calls:
+            call(one, B)
+        assert one.fake_failed()
+        one.fake_reset(b"", 0)
+        assert gradient(one, 40, 8) == B.TCU_OK, name                    # its one launch is checked
+        assert [call(one, B) for call in calls] == [B.TCU_OK] * 4
+        if name == "cudaOccupancyMaxActiveClusters":
+            one = str(tmp_path / "again.so")
+            shutil.copy(lib._name, one)
+            one = ctypes.CDLL(one, mode=os.RTLD_LOCAL | os.RTLD_NOW)
+            one.fake_reset(name.encode(), 3)
+            assert calls[0](one, B) == B.TCU_OK                          # clusters of that size are not used, that is all
