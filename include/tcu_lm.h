@@ -56,11 +56,12 @@ typedef struct {
     uint64_t pool_slots;        /* step only: entries of the pool (at least `batch` when d_slots is NULL)           */
     tcu_tokens_t q, k, v, o;    /* o: written by forward and step                                                   */
     const float *d_state_in;    /* NULL (zero), or the state before the first token                                 */
-    float *d_state_out;         /* NULL, or receives the state after the last token (may be d_state_in itself);
-                                   step: the pool, updated in place                                                 */
+    float *d_state_out;         /* NULL, or receives the state after the last token (may be d_state_in itself, but
+                                   not overlap it otherwise); step: the pool, updated in place                      */
     tcu_tokens_t d_o;           /* backward: gradient with respect to o                                             */
     tcu_tokens_t d_q, d_k, d_v; /* backward: receive the gradients (per head, also where an input has a stride of 0:
-                                   sum over the repeated axis afterwards)                                           */
+                                   sum over the repeated axis afterwards); no element of one may be an element of
+                                   another (looked at only where they begin at the same address)                    */
     const float *d_dstate_out;  /* backward: NULL (zero), or the gradient with respect to the state after the last token */
     float *d_dstate_in;         /* backward: NULL, or receives the gradient with respect to the state before the first */
     void *d_scratch;            /* forward and backward: NULL, or tcu_linattn_scratch_bytes() of 256-byte aligned memory, with

@@ -331,7 +331,9 @@ tcu_status_t forward(const tcu_linattn_t *a, void *d_ws, size_t ws_bytes, const 
     } else if (!a->d_state_out) {
         return TCU_OK;
     }
-    if (a->tokens == 0) return copy_state(a->d_state_out, a->d_state_in, size_t(a->batch) * a->heads * a->dk * a->dv * 4, stream);
+    const size_t state = size_t(a->batch) * a->heads * a->dk * a->dv * 4;
+    if (a->d_state_out != a->d_state_in && overlaps(a->d_state_out, state, a->d_state_in, state)) return TCU_ERR_INVALID_ARG;
+    if (a->tokens == 0) return copy_state(a->d_state_out, a->d_state_in, state, stream);
     const tcu_tokens_t *arrays[3] = {&a->q, &a->k, &a->v}, *outputs[1] = {&a->o};
     const uint32_t widths[3] = {a->dk, a->dk, a->dv};
     MixParams p = {};
@@ -358,6 +360,8 @@ tcu_status_t backward(const tcu_linattn_t *a, void *d_ws, size_t ws_bytes, const
         for (int i = 0; i < 4; ++i)
             for (int w = 4; w < 7; ++w)
                 if (spans_meet(at[i], at[w])) return TCU_ERR_INVALID_ARG;
+        // (gradients may lie between one another, as in one array of all three)
+        if (a->d_q.ptr == a->d_k.ptr || a->d_q.ptr == a->d_v.ptr || a->d_k.ptr == a->d_v.ptr) return TCU_ERR_INVALID_ARG;
     } else if (!a->d_dstate_in) {
         return TCU_OK;
     }

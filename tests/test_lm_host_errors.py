@@ -156,3 +156,25 @@ def test_no_error_is_left_for_a_later_call(lib, B, tmp_path):
             one = ctypes.CDLL(one, mode=os.RTLD_LOCAL | os.RTLD_NOW)
             one.fake_reset(name.encode(), 3)
             assert calls[0](one, B) == B.TCU_OK                          # clusters of that size are not used, that is all
+
+
+def test_results_do_not_overlap(lib, B):
+    """States that overlap without being the same, and two gradients in one place, are written by blocks in any order."""
+    at = lambda i: (i << 36, 0, 64, 64)  # noqa: E731
+    lib.fake_reset(b"", 0)
+
+    def call(backward=0, tokens=100, d_q=at(6), d_k=at(7), d_v=at(8), **states):
+        args = B.tcu_linattn_args(B.TCU_BF16, 1, tokens, 1, 64, 64, 1.0, 1 << 35, at(1), at(2), at(3), at(4), d_o=at(5), d_q=d_q, d_k=d_k, d_v=d_v, **states)
+        return (lib.tcu_linattn_backward if backward else lib.tcu_linattn_forward)(args, p(1 << 32), ctypes.c_size_t(256), None)
+
+    s0, size = 1 << 37, 64 * 64 * 4
+    for tokens in (0, 100):
+        assert call(tokens=tokens, d_state_in=s0, d_state_out=s0) == B.TCU_OK
+        assert call(tokens=tokens, d_state_in=s0, d_state_out=s0 + size) == B.TCU_OK
+        for off in (16, size - 16, -16):
+            assert call(tokens=tokens, d_state_in=s0, d_state_out=s0 + off) == B.TCU_ERR_INVALID_ARG
+    assert call(backward=1) == B.TCU_OK
+    joined = [(6 << 36 | 128 * i, 0, 192, 192) for i in range(3)]
+    assert call(backward=1, d_q=joined[0], d_k=joined[1], d_v=joined[2]) == B.TCU_OK
+    for bad in (dict(d_q=at(7)), dict(d_q=at(8)), dict(d_v=at(7))):
+        assert call(backward=1, **bad) == B.TCU_ERR_INVALID_ARG
