@@ -1,7 +1,7 @@
 /*
  * tcu_lm.h - C ABI of the language-model operators of the tensor-core-unit library (B200, sm_100a).
  *
- * Two operators that are prefix sums at heart, beside the plain scans of tcu_scan.h:
+ * Beside the plain scans of tcu_scan.h:
  *
  *  - Linear attention with a constant decay for each head: an inclusive scan whose elements are dk x dv matrices.
  *    Per sequence and head, with a = exp(log_decay[head]) and a state S of dk x dv values,
@@ -86,7 +86,9 @@ size_t tcu_linattn_scratch_bytes(const tcu_linattn_t *args, int backward);
  * TCU_ERR_UNSUPPORTED: dk or dv above 128, more than 2^31 - 256 tokens, more than 2^31 - 1 blocks of work.
  * Non-finite values: a product with a non-finite k or v reaches every output of its sequence that shares the token's group of
  * 128 tokens (counted from the start of the sequence), earlier ones too; other sequences never see it.  Tokens past the
- * end of a packed sequence are never part of it, whatever they hold. */
+ * end of a packed sequence are never part of it, whatever they hold.
+ * float16: scores, keys and states are brought to the type's range inside, so that only inputs and outputs are bound by it; states
+ * up to 2^75, and keys times scale from 2^-55 on, keep their 32 bits. */
 tcu_status_t tcu_linattn_forward(const tcu_linattn_t *args, void *d_ws, size_t ws_bytes, cudaStream_t stream);
 
 /* Gradients with respect to q, k, v and the state before the first token, from d_o and d_dstate_out.  Reads q, k, v, d_o, d_state_in;

@@ -45,8 +45,10 @@
 // memory, and each walks its part from the state that enters it.  When there are more, they are cut into equal shares for the SMs,
 // and a block hands the state at the end of its share to the next one through memory.
 //
-// Measured, bfloat16 at D = 128: 256 heads of 4096 tokens, 1.08 GB, 225 to 240 us (4.5 to 4.8 TB/s; 3.7 us a group with all SMs in
-// use); 148 heads of 2048 tokens: 50 % of the memory's time and 37 % of the tensor pipe's.  One group takes 8.8 us with the launch.
+// Measured at D = 128: 256 heads of 4096 tokens in bfloat16, 1.08 GB, 232 us at full clock (4.7 TB/s; 4.1 us a group with all SMs in
+// use), 262 to 276 (4.0) in a benchmark that keeps the device busy; 148 heads of 2048 tokens 72 to 76 us, 50 % of the memory's
+// time and 33 % of the tensor pipe's, in float16 89 us (its scores and keys are read a second time, for their powers of two).
+// One group takes 9.2 us with the launch.
 //
 // Every wait is bounded; one that runs out records TCU_ERR_TIMEOUT in the workspace and the block winds down: each role returns at
 // its next wait that fails, the producer after its copies have landed, the issuers after their products have ended (drain), and a
