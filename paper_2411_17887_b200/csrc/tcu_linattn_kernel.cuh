@@ -35,7 +35,10 @@
 // memory).  K~ enters the state in two terms: 22 bits of mantissa in float16, 16 in bfloat16.  There a third term follows
 // (24 bits, all that 32-bit arithmetic gives) in the groups that the decay until the end of the walk leaves above 2^-6, because
 // the last state is a result in 32 bits of its own; with two terms throughout it was 2e-6 to 5e-6 off, where 32-bit sums are
-// 2e-7 off.  (The rule goes by the decay alone: outputs do not depend on whether the state is asked for.)  In float16 X and K~
+// 2e-7 off.  (The rule goes by the decay alone: outputs do not depend on whether the state is asked for.)  What is left is the
+// tensor core's sum in 32 bits, which drops what falls below its last bit instead of rounding it: without decay, products of one
+// sign are short by 2e-8 to 3e-8 of the sum for every 16 tokens and term (4e-5 after 8192 tokens, where rounded sums are 7e-6 off;
+// of either sign 1e-6), and float16 values below 2^-14 of either sign count as 2^-14 in what is dropped.  In float16 X and K~
 // are brought to the type's range by powers of two found for every group, because a state without decay outgrows the type
 // and the low terms of small keys fall below it; and P by one found for every token, because scores do either (products of a
 // hundred features; small gradients).
