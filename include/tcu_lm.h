@@ -10,6 +10,9 @@
  *    chunks is the state.  Prompts (with states in and out, dense or packed), training (gradients), single tokens.
  *  - Token embedding: out[n] = scale * table[ids[n]], and its table gradient, a segmented sum over the tokens in
  *    the order of their ids.
+ *  - Gated linear recurrence: for every channel an inclusive scan with the gates as factors,
+ *        h_t = f_t h_{t-1} + i_t x_t            f = sigmoid(gate)
+ *    over prompts (states in and out, dense or packed), its gradients (the same scan backward in time), single tokens.
  *
  * The general conventions of tcu_scan.h hold: caller-owned device memory, nothing allocated, everything asynchronous
  * on `stream`, argument errors found on the host before anything is queued, bounded device-side waits, launches that
@@ -130,6 +133,67 @@ size_t tcu_embedding_workspace_bytes(size_t n, size_t rows, size_t d);
 tcu_status_t tcu_embedding_backward(const void *d_out, tcu_float_t type, const void *d_ids, int id_bytes, size_t n, size_t rows,
                                     size_t d, float scale, int accumulate, void *d_table, tcu_float_t table_type,
                                     void *d_ws, size_t ws_bytes, cudaStream_t stream);
+
+/* ---- gated linear recurrence */
+/* what a token's x is multiplied by: 1 - f, 1, or sqrt(1 - f^2) */
+typedef enum { TCU_INPUT_COMPLEMENT = 0, TCU_INPUT_ONE = 1, TCU_INPUT_ROOT = 2 } tcu_input_gate_t;
+
+/* A (batch, token, channel) array: channels are contiguous, the other strides are given in elements (0 to 2^38; 0 repeats an input
+ * along that axis; what is written has no stride of 0 along an axis of more than one).  Packed: stride_batch is not used. */
+typedef struct {
+    void *ptr;
+    int64_t stride_batch, stride_token;
+} tcu_rows_t;
+
+/* Arguments of the recurrence's calls.  Zero-initialise, set struct_bytes = sizeof(tcu_gated_t), then set what the call uses.
+ * States are fp32, (batch, channels) dense.  Any alignment of elements; arrays whose channels, strides and pointers are all multiples
+ * of two elements are read two channels at a time. */
+typedef struct {
+    uint32_t struct_bytes;
+    uint32_t type;              /* tcu_float_t: x, gate, y and their gradients                                      */
+    uint32_t input_gate;        /* tcu_input_gate_t                                                                 */
+    uint32_t channels;          /* 1 to 2^30                                                                        */
+    uint64_t batch;             /* sequences                                                                        */
+    uint64_t tokens;            /* tokens of each sequence; packed: of all sequences together; step: not used       */
+    const int64_t *d_offsets;   /* NULL: dense.  Packed: batch + 1 values, sequence b holds tokens [offsets[b], offsets[b+1]);
+                                   non-decreasing, from 0 to at most `tokens` (not checked: they live on the device; what leaves the
+                                   range is taken as its end); empty sequences are allowed, rows behind the last one
+                                   are not touched                                                                  */
+    const int32_t *d_slots;     /* step only: NULL, or for each sequence its entry in the state pool; entries outside it mark a
+                                   sequence to skip (its output is zero); no two sequences may share an entry       */
+    uint64_t pool_slots;        /* step only: entries of the pool (at least `batch` when d_slots is NULL)           */
+    tcu_rows_t x, gate, y;      /* y: written by forward (NULL pointer: states and marks alone) and step            */
+    const float *d_state_in;    /* forward: NULL (zero), or the state before the first token                        */
+    float *d_state_out;         /* forward: NULL, or receives the state after the last token (may be d_state_in itself, but not
+                                   overlap it otherwise); step: the pool, (pool_slots, channels), updated in place  */
+    float *d_marks;             /* forward: NULL, or receives the states that the backward call starts from; backward: what
+                                   the forward call with the same x, gate, d_offsets, d_state_in left here          */
+    uint64_t marks_bytes;       /* size of it: tcu_gated_marks_bytes()                                              */
+    tcu_rows_t d_y;             /* backward: gradient with respect to y                                             */
+    tcu_rows_t d_x, d_gate;     /* backward: receive the gradients (of every element of (batch, token, channel), also where an input has
+                                   a stride of 0); no element of one may be an element of the other                 */
+    const float *d_dstate_out;  /* backward: NULL (zero), or the gradient with respect to the state after the last token */
+    float *d_dstate_in;         /* backward: NULL, or receives the gradient with respect to the state before the first; may be
+                                   d_dstate_out itself, but not overlap it otherwise                                */
+} tcu_gated_t;
+
+/* Bytes of d_marks for `tokens` tokens in all of `batch` sequences (dense: batch times those of one); 0 for sizes whose bytes
+ * have no number of 64 bits. */
+size_t tcu_gated_marks_bytes(uint64_t batch, uint64_t tokens, uint32_t channels);
+
+/* y and, if asked for, the state after the last token (a sequence without tokens: the state before).  What is written must not
+ * overlap an input, from the first byte of each to the last.  Gates of -inf (f = 0) and +inf (f = 1) are as any other; NaN and infinities stay in
+ * their channel and sequence, from their token on.
+ * TCU_ERR_UNSUPPORTED: more than 2^31 - 1 blocks of 64 channels of a sequence, or 2^40 tokens. */
+tcu_status_t tcu_gated_forward(const tcu_gated_t *args, cudaStream_t stream);
+
+/* Gradients with respect to x, gate and the state before the first token, from d_y and d_dstate_out.  With D_t the gradient with
+ * respect to h_t:  D_t = dy_t + f_{t+1} D_{t+1},  dx_t = i_t D_t,  dgate_t = D_t (h_{t-1} df_t/dgate + x_t di_t/dgate).
+ * y and the states themselves are not used: h is formed again from the marks, in 32 bits. */
+tcu_status_t tcu_gated_backward(const tcu_gated_t *args, cudaStream_t stream);
+
+/* One token for each of `batch` sequences: the state of each is updated in place, and y written (y may be x or gate, with its strides). */
+tcu_status_t tcu_gated_step(const tcu_gated_t *args, cudaStream_t stream);
 
 #ifdef __cplusplus
 }

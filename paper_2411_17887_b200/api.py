@@ -425,3 +425,166 @@ def embedding(ids, table, scale=1.0):
     if forward_ad._current_level >= 0 or (table.requires_grad and torch.is_grad_enabled()):
         return _Embedding.apply(ids, table, scale)
     return _embedding_forward(ids, table, scale)
+
+
+# ------------------------------------------------------------------------------------------------ gated recurrence
+def _channels(x: torch.Tensor):
+    """An array (b, t, d), or packed (t, d), with its channels contiguous (copied if they are not), and its description."""
+    if x.shape[-1] > 1 and x.stride(-1) != 1:
+        x = x.contiguous()
+    if x.dim() == 3:
+        return x, (x.data_ptr(), x.stride(0), x.stride(1))
+    return x, (x.data_ptr(), 0, x.stride(0))
+
+
+def _input_gate(name) -> int:
+    kind = B.INPUT_GATES.get(name)
+    if kind is None:
+        raise ValueError(f"input_gate is one of {', '.join(B.INPUT_GATES)}, not {name!r}")
+    return kind
+
+
+class _Gated:
+    """Checked and described arguments of one call of the gated recurrence over whole sequences."""
+
+    __slots__ = ("head", "x", "offsets", "state_shape", "mark_shape", "stream")
+
+    def __init__(self, x, gate, offsets, input_gate, **states):
+        dtype, device, shape = x.dtype, x.device, x.shape
+        if gate.dtype != dtype or gate.device != device:
+            _refuse(dtype, device, gate=gate)
+        if dtype not in _FLOAT:
+            raise TypeError(f"the gated recurrence takes float32, float16 or bfloat16, not {dtype}")
+        packed = offsets is not None
+        if len(shape) != (2 if packed else 3):
+            raise ValueError("x is (batch, tokens, channels), or (tokens, channels) with offsets")
+        if gate.shape != shape:
+            raise ValueError(f"shapes do not go together: x {tuple(shape)}, gate {tuple(gate.shape)}")
+        if packed and (offsets.dtype != torch.int64 or offsets.dim() != 1 or offsets.numel() < 1 or not offsets.is_contiguous() or offsets.device != device):
+            raise ValueError("offsets: a contiguous int64 tensor of batch + 1 values on the device of x")
+        tokens, channels = shape[-2:]
+        if channels == 0:
+            raise ValueError("there are no channels")
+        batch = offsets.numel() - 1 if packed else shape[0]
+        self.state_shape = (batch, channels)
+        self.mark_shape = (B.tcu_gated_marks_bytes(batch, tokens if packed else batch * tokens, channels) // (4 * channels), channels)
+        for name, s in states.items():
+            want = self.mark_shape if name == "marks" else self.state_shape
+            if s is not None and (s.shape != want or s.dtype != torch.float32 or not s.is_contiguous() or s.device != device):
+                raise ValueError(f"{name}: a contiguous float32 tensor of shape {want} on the device of x")
+        self.head = (_FLOAT[dtype], _input_gate(input_gate), channels, batch, tokens)
+        self.x = x
+        self.offsets = offsets.data_ptr() if packed else 0
+        self.stream = _stream(device)
+
+    def new(self, shape):
+        return self.x.new_empty(shape, dtype=torch.float32)
+
+    def call(self, fn, x, gate, y=B.NO_ROWS, marks=None, **more):
+        B.check(fn(B.tcu_gated_args(*self.head, x, gate, y, d_offsets=self.offsets, d_marks=_ptr(marks), marks_bytes=0 if marks is None else 4 * marks.numel(), **more),
+                   self.stream))
+
+
+def _gated_forward(x, gate, initial_state, offsets, output_final_state, input_gate, output_marks, output=True):
+    m = _Gated(x, gate, offsets, input_gate, initial_state=initial_state)
+    y = x.new_empty(x.shape) if output else None
+    last = m.new(m.state_shape) if output_final_state else None
+    marks = m.new(m.mark_shape) if output_marks else None
+    (x, xv), (gate, gv) = _channels(x), _channels(gate)
+    m.call(B.tcu_gated_forward, xv, gv, _channels(y)[1] if output else B.NO_ROWS, marks, d_state_in=_ptr(initial_state), d_state_out=_ptr(last))
+    return y, last, marks
+
+
+def gated_recurrence_backward(d_y, x, gate, initial_state=None, offsets=None, d_final_state=None, input_gate="complement", marks=None):
+    """Gradients of :func:`gated_recurrence` with respect to x, gate and the initial state (None without one), from the gradient
+    of its output and, where it has one, of the final state.  `marks`: what the forward call with these x, gate and initial state
+    gave for ``output_marks=True``; without them they are computed once more."""
+    if forward_ad._current_level >= 0:
+        _no_tangents(d_y=d_y, x=x, gate=gate, initial_state=initial_state, d_final_state=d_final_state, marks=marks)
+    if d_y.dtype != x.dtype or d_y.device != x.device:
+        _refuse(x.dtype, x.device, d_y=d_y)
+    if d_y.shape != x.shape:
+        raise ValueError(f"d_y is {tuple(d_y.shape)}, x {tuple(x.shape)}")
+    m = _Gated(x, gate, offsets, input_gate, initial_state=initial_state, d_final_state=d_final_state, marks=marks)
+    if marks is None:
+        marks = _gated_forward(x, gate, initial_state, offsets, False, input_gate, True, output=False)[2]
+    d_x, d_gate = x.new_empty(x.shape), x.new_empty(x.shape)
+    d_first = m.new(m.state_shape) if initial_state is not None else None
+    (x, xv), (gate, gv), (d_y, yv) = _channels(x), _channels(gate), _channels(d_y)
+    m.call(B.tcu_gated_backward, xv, gv, marks=marks, d_y=yv, d_x=_channels(d_x)[1], d_gate=_channels(d_gate)[1], d_dstate_out=_ptr(d_final_state),
+           d_dstate_in=_ptr(d_first))
+    return d_x, d_gate, d_first
+
+
+class _GatedRecurrence(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, gate, initial_state, offsets, output_final_state, input_gate, output_marks):
+        y, last, marks = _gated_forward(x, gate, initial_state, offsets, output_final_state, input_gate, True)
+        ctx.save_for_backward(x, gate, initial_state, offsets, marks)
+        ctx.input_gate = input_gate
+        ctx.set_materialize_grads(False)
+        ctx.mark_non_differentiable(marks)
+        return y, last, marks
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, d_y, d_last, _):
+        x, gate, initial_state, offsets, marks = ctx.saved_tensors
+        d_y = torch.zeros_like(x) if d_y is None else d_y
+        d_last = None if d_last is None else d_last.contiguous()
+        d_x, d_gate, d_first = gated_recurrence_backward(d_y, x, gate, initial_state, offsets, d_last, ctx.input_gate, marks)
+        return d_x, d_gate, d_first, None, None, None, None
+
+
+def gated_recurrence(x, gate, initial_state=None, offsets=None, output_final_state=False, input_gate="complement", output_marks=False):
+    """Gated linear recurrence, for every channel on its own: h_t = f_t h_{t-1} + i_t x_t with f = sigmoid(gate) and i = 1 - f
+    (input_gate "complement"), 1 ("one") or sqrt(1 - f^2) ("root").  Returns (h, final state), the state None unless asked for, and with
+    ``output_marks=True`` (h, final state, marks), the marks for :func:`gated_recurrence_backward`; differentiable, once, in x, gate
+    and the initial state.
+
+    x, gate (batch, tokens, channels), float32, float16 or bfloat16, any strides; or packed (tokens, channels) with `offsets`, an int64
+    tensor of batch + 1 values on the GPU: sequence b is [offsets[b], offsets[b + 1]), rows behind the last one are left as they
+    are (of fresh memory).  States (batch, channels) float32."""
+    if forward_ad._current_level >= 0 or (torch.is_grad_enabled() and (x.requires_grad or gate.requires_grad or
+                                                                       (initial_state is not None and initial_state.requires_grad))):
+        y, last, marks = _GatedRecurrence.apply(x, gate, initial_state, offsets, output_final_state, input_gate, output_marks)
+    else:
+        y, last, marks = _gated_forward(x, gate, initial_state, offsets, output_final_state, input_gate, output_marks)
+    return (y, last, marks) if output_marks else (y, last)
+
+
+def gated_recurrence_step(x, gate, state, slots=None, input_gate="complement"):
+    """One token for each sequence: updates `state` in place and returns h (batch, channels).  x, gate (batch, channels); state
+    (pool, channels) float32; slots: None (sequence b has entry b), or an int32 tensor of each sequence's entry, all different; an entry
+    outside the pool marks a sequence to skip (its output is zero).  No gradient is computed: with gradients enabled, inputs
+    that require one are refused."""
+    if forward_ad._current_level >= 0:
+        _no_tangents(x=x, gate=gate, state=state)
+    if torch.is_grad_enabled():
+        _not_recorded(x=x, gate=gate, state=state)
+    dtype, device, shape = x.dtype, x.device, x.shape
+    if gate.dtype != dtype or gate.device != device:
+        _refuse(dtype, device, gate=gate)
+    if dtype not in _FLOAT:
+        raise TypeError(f"the gated recurrence takes float32, float16 or bfloat16, not {dtype}")
+    if len(shape) != 2 or gate.shape != shape or shape[1] == 0:
+        raise ValueError(f"shapes do not go together: x {tuple(shape)}, gate {tuple(gate.shape)}")
+    batch, channels = shape
+    pool = state.shape
+    if len(pool) != 2 or pool[1] != channels or state.dtype != torch.float32 or not state.is_contiguous() or state.device != device:
+        raise ValueError(f"state: a contiguous float32 tensor of shape (pool, {channels}) on the device of x")
+    if slots is not None and (slots.shape != (batch,) or slots.dtype != torch.int32 or not slots.is_contiguous() or slots.device != device):
+        raise ValueError("slots: a contiguous int32 tensor of one value for each sequence, on the device of x")
+    kind = _input_gate(input_gate)
+    y = x.new_empty(shape)
+
+    def view(r):
+        if channels > 1 and r.stride(1) != 1:
+            r = r.contiguous()
+        return r, (r.data_ptr(), r.stride(0), 0)
+
+    (x, xv), (gate, gv) = view(x), view(gate)
+    args = B.tcu_gated_args(_FLOAT[dtype], kind, channels, batch, 1, xv, gv, (y.data_ptr(), channels, 0), d_slots=_ptr(slots), pool_slots=pool[0], d_state_out=state.data_ptr())
+    B.check(B.tcu_gated_step(args, _stream(device)))
+    _written(state)
+    return y

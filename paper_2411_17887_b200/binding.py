@@ -108,6 +108,11 @@ _lib.tcu_embedding_workspace_bytes.argtypes = [_sz, _sz, _sz]
 _lib.tcu_embedding_workspace_bytes.restype = _sz
 _lib.tcu_embedding_backward.argtypes = [_vp, _int, _vp, _int, _sz, _sz, _sz, _f32, _int, _vp, _int, _vp, _sz, _vp]
 _lib.tcu_embedding_backward.restype = _int
+_lib.tcu_gated_marks_bytes.argtypes = [_u64, _u64, ctypes.c_uint32]
+_lib.tcu_gated_marks_bytes.restype = _sz
+for _name in ("tcu_gated_forward", "tcu_gated_backward", "tcu_gated_step"):
+    getattr(_lib, _name).argtypes = [ctypes.c_char_p, _vp]
+    getattr(_lib, _name).restype = _int
 _lib.tcu_status_string.argtypes = [_int]
 _lib.tcu_status_string.restype = ctypes.c_char_p
 
@@ -283,6 +288,36 @@ def tcu_embedding_backward(d_out, dtype: int, d_ids, id_bytes: int, n: int, rows
                            table_dtype: int, d_ws, ws_bytes: int, stream=0) -> int:
     return _lib.tcu_embedding_backward(_p(d_out), dtype, _p(d_ids), id_bytes, n, rows, d, scale, int(accumulate), _p(d_table), table_dtype,
                                        _p(d_ws), ws_bytes, stream)
+
+
+# tcu_gated_t, packed as bytes; an array of rows is (pointer, stride_batch, stride_token)
+_GATED = struct.Struct("=IIIIQQQQQ" + "Qqq" * 3 + "QQQQ" + "Qqq" * 3 + "QQ")
+NO_ROWS = (0, 0, 0)
+INPUT_GATES = {"complement": 0, "one": 1, "root": 2}
+
+
+def tcu_gated_args(dtype: int, input_gate: int, channels: int, batch: int, tokens: int, x, gate, y=NO_ROWS, *, d_offsets: int = 0, d_slots: int = 0, pool_slots: int = 0,
+                   d_state_in: int = 0, d_state_out: int = 0, d_marks: int = 0, marks_bytes: int = 0, d_y=NO_ROWS, d_x=NO_ROWS, d_gate=NO_ROWS, d_dstate_out: int = 0,
+                   d_dstate_in: int = 0) -> bytes:
+    """The argument structure of the gated recurrence's calls; pointers are integers (0 for NULL)."""
+    return _GATED.pack(_GATED.size, dtype, input_gate, channels, batch, tokens, d_offsets, d_slots, pool_slots, *x, *gate, *y, d_state_in, d_state_out, d_marks, marks_bytes,
+                       *d_y, *d_x, *d_gate, d_dstate_out, d_dstate_in)
+
+
+def tcu_gated_marks_bytes(batch: int, tokens: int, channels: int) -> int:
+    return _lib.tcu_gated_marks_bytes(batch, tokens, channels)
+
+
+def tcu_gated_forward(args: bytes, stream=0) -> int:
+    return _lib.tcu_gated_forward(args, stream)
+
+
+def tcu_gated_backward(args: bytes, stream=0) -> int:
+    return _lib.tcu_gated_backward(args, stream)
+
+
+def tcu_gated_step(args: bytes, stream=0) -> int:
+    return _lib.tcu_gated_step(args, stream)
 
 
 def tcu_scan_last_stats() -> dict:

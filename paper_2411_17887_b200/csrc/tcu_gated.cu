@@ -1,0 +1,202 @@
+// Host side of the gated linear recurrence (include/tcu_lm.h): argument checks, launches.
+#include "tcu_lm.h"
+
+#include <cuda_runtime.h>
+
+#include <initializer_list>
+#include <type_traits>
+
+#include "tcu_gated_kernel.cuh"
+#include "tcu_host.h"
+
+namespace {
+
+using namespace tcu;
+
+constexpr uint64_t kMostWalks = (uint64_t(1) << 31) - 1;
+constexpr uint64_t kMostTokens = uint64_t(1) << 40;
+constexpr uint32_t kMostChannels = uint32_t(1) << 30;
+constexpr int64_t kMostStride = int64_t(1) << 38;
+
+// First and one-past-last byte that an array may touch; to the end of all addresses if it has no such last byte.
+struct Span {
+    uintptr_t lo, hi;
+};
+bool meet(const Span &a, const Span &b) { return a.lo < b.hi && b.lo < a.hi; }
+
+struct Sizes {
+    bool packed;
+    uint64_t batch, tokens;
+    uint32_t channels;
+    size_t element;
+    Span span(const tcu_rows_t &r) const {
+        using Wide = unsigned __int128;
+        const auto lo = reinterpret_cast<uintptr_t>(r.ptr);
+        if (tokens == 0 || batch == 0) return {lo, lo};
+        const Wide last = (packed ? Wide(0) : Wide(batch - 1) * uint64_t(r.stride_batch)) + Wide(tokens - 1) * uint64_t(r.stride_token) + channels;
+        const Wide end = lo + last * element;
+        return {lo, end > ~uintptr_t(0) ? ~uintptr_t(0) : uintptr_t(end)};
+    }
+    Span states(const float *s) const {
+        const auto lo = reinterpret_cast<uintptr_t>(s);
+        const unsigned __int128 end = (unsigned __int128)(lo) + (unsigned __int128)(batch) * channels * 4;
+        return {lo, end > ~uintptr_t(0) ? ~uintptr_t(0) : uintptr_t(end)};
+    }
+    bool right(const tcu_rows_t &r, bool written) const {
+        if (!r.ptr || !aligned(r.ptr, element)) return false;
+        for (int64_t s : {packed ? 0 : r.stride_batch, r.stride_token})
+            if (s < 0 || s > kMostStride) return false;
+        return !written || !((!packed && batch > 1 && r.stride_batch == 0) || (tokens > 1 && r.stride_token == 0));
+    }
+    // whether two channels can be moved at a time
+    bool pairs(std::initializer_list<const tcu_rows_t *> rows) const {
+        if (channels % 2) return false;
+        for (const tcu_rows_t *r : rows) {
+            if (!r->ptr) continue;
+            if (!aligned(r->ptr, 2 * element) || (tokens > 1 && r->stride_token % 2) || (!packed && batch > 1 && r->stride_batch % 2)) return false;
+        }
+        return true;
+    }
+};
+
+GatedRows rows(const tcu_rows_t &r) { return {r.ptr, r.stride_batch, r.stride_token}; }
+
+GatedParams params(const tcu_gated_t *a) {
+    GatedParams p = {};
+    p.x = rows(a->x);
+    p.gate = rows(a->gate);
+    p.y = rows(a->y);
+    p.d_y = rows(a->d_y);
+    p.d_x = rows(a->d_x);
+    p.d_gate = rows(a->d_gate);
+    p.offsets = a->d_offsets;
+    p.state_in = a->d_state_in;
+    p.state_out = a->d_state_out;
+    p.d_state_out = a->d_dstate_out;
+    p.d_state_in = a->d_dstate_in;
+    p.marks = a->d_marks;
+    p.tokens = a->tokens;
+    p.channels = a->channels;
+    p.strips = (a->channels + kGatedChannels - 1) / kGatedChannels;
+    return p;
+}
+
+tcu_status_t check(const tcu_gated_t *a, Sizes &s) {
+    if (!a || a->struct_bytes != sizeof(tcu_gated_t)) return TCU_ERR_INVALID_ARG;
+    if (!valid_float(int(a->type)) || a->input_gate > TCU_INPUT_ROOT || a->channels == 0) return TCU_ERR_INVALID_ARG;
+    if (a->channels > kMostChannels || a->tokens > kMostTokens) return TCU_ERR_UNSUPPORTED;
+    const uint64_t strips = (uint64_t(a->channels) + kGatedChannels - 1) / kGatedChannels;
+    if (a->batch > kMostWalks / strips) return TCU_ERR_UNSUPPORTED;
+    if (!aligned(a->d_offsets, 8)) return TCU_ERR_INVALID_ARG;
+    for (const void *q : {static_cast<const void *>(a->d_state_in), static_cast<const void *>(a->d_state_out), static_cast<const void *>(a->d_marks),
+                          static_cast<const void *>(a->d_dstate_out), static_cast<const void *>(a->d_dstate_in)})
+        if (!aligned(q, 4)) return TCU_ERR_INVALID_ARG;
+    s = {a->d_offsets != nullptr, a->batch, a->tokens, a->channels, float_bytes(tcu_float_t(a->type))};
+    return TCU_OK;
+}
+
+
+// Calls go(type, input gate, pairs) with these as types.
+template <typename F>
+void dispatch(const tcu_gated_t *a, bool pairs, F go) {
+    auto input = [&](auto t) {
+        auto pair = [&](auto in) {
+            if (pairs) go(t, in, std::true_type{});
+            else go(t, in, std::false_type{});
+        };
+        if (a->input_gate == TCU_INPUT_COMPLEMENT) pair(std::integral_constant<int, kInputComplement>{});
+        else if (a->input_gate == TCU_INPUT_ONE) pair(std::integral_constant<int, kInputOne>{});
+        else pair(std::integral_constant<int, kInputRoot>{});
+    };
+    if (a->type == TCU_F32) input(float{});
+    else if (a->type == TCU_F16) input(__half{});
+    else input(__nv_bfloat16{});
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t tcu_gated_marks_bytes(uint64_t batch, uint64_t tokens, uint32_t channels) {
+    const unsigned __int128 bytes = ((unsigned __int128)(tokens / kGatedTile) + batch) * channels * 4;
+    return bytes >> 63 ? 0 : size_t(bytes);
+}
+
+tcu_status_t tcu_gated_forward(const tcu_gated_t *a, cudaStream_t stream) {
+    Sizes s;
+    if (tcu_status_t st = check(a, s)) return st;
+    if (a->batch == 0) return TCU_OK;
+    const bool tokens = a->tokens > 0;
+    if (tokens && (!s.right(a->x, false) || !s.right(a->gate, false) || (a->y.ptr && !s.right(a->y, true)))) return TCU_ERR_INVALID_ARG;
+    const uint64_t all = s.packed ? a->tokens : a->batch * a->tokens;
+    const size_t marks = tcu_gated_marks_bytes(a->batch, all, a->channels);
+    if (a->d_marks && (marks == 0 || a->marks_bytes < marks)) return TCU_ERR_WORKSPACE;
+    const Span inputs[] = {s.span(a->x), s.span(a->gate)};
+    const Span y = a->y.ptr ? s.span(a->y) : Span{0, 0};
+    const Span kept = a->d_marks ? Span{reinterpret_cast<uintptr_t>(a->d_marks), reinterpret_cast<uintptr_t>(a->d_marks) + marks} : Span{0, 0};
+    const Span in = a->d_state_in ? s.states(a->d_state_in) : Span{0, 0}, out = a->d_state_out ? s.states(a->d_state_out) : Span{0, 0};
+    for (const Span &w : {y, kept, out})
+        for (const Span &i : inputs)
+            if (meet(w, i)) return TCU_ERR_INVALID_ARG;
+    if (meet(y, kept) || meet(y, out) || meet(y, in) || meet(kept, out) || meet(kept, in)) return TCU_ERR_INVALID_ARG;
+    if (a->d_state_in != a->d_state_out && meet(in, out)) return TCU_ERR_INVALID_ARG;
+    const GatedParams p = params(a);
+    dispatch(a, s.pairs({&a->x, &a->gate, &a->y}), [&](auto t, auto in_gate, auto pair) {
+        tcu_gated_forward_kernel<decltype(t), decltype(in_gate)::value, decltype(pair)::value><<<uint32_t(a->batch * p.strips), kGatedWarps * 32, 0, stream>>>(p);
+    });
+    return launched();
+}
+
+tcu_status_t tcu_gated_backward(const tcu_gated_t *a, cudaStream_t stream) {
+    Sizes s;
+    if (tcu_status_t st = check(a, s)) return st;
+    if (a->batch == 0) return TCU_OK;
+    if (a->tokens > 0) {
+        for (const tcu_rows_t *r : {&a->x, &a->gate, &a->d_y})
+            if (!s.right(*r, false)) return TCU_ERR_INVALID_ARG;
+        for (const tcu_rows_t *r : {&a->d_x, &a->d_gate})
+            if (!s.right(*r, true)) return TCU_ERR_INVALID_ARG;
+        if (a->d_x.ptr == a->d_gate.ptr) return TCU_ERR_INVALID_ARG;
+    }
+    const size_t marks = tcu_gated_marks_bytes(a->batch, s.packed ? a->tokens : a->batch * a->tokens, a->channels);
+    if (!a->d_marks || marks == 0 || a->marks_bytes < marks) return TCU_ERR_WORKSPACE;
+    const Span kept = {reinterpret_cast<uintptr_t>(a->d_marks), reinterpret_cast<uintptr_t>(a->d_marks) + marks};
+    const Span in = a->d_dstate_out ? s.states(a->d_dstate_out) : Span{0, 0}, out = a->d_dstate_in ? s.states(a->d_dstate_in) : Span{0, 0};
+    const Span inputs[] = {s.span(a->x), s.span(a->gate), s.span(a->d_y), kept};
+    const Span dx = s.span(a->d_x), dg = s.span(a->d_gate);
+    for (const Span &w : {dx, dg, out})
+        for (const Span &i : inputs)
+            if (meet(w, i)) return TCU_ERR_INVALID_ARG;
+    if (meet(dx, in) || meet(dg, in) || meet(dx, out) || meet(dg, out)) return TCU_ERR_INVALID_ARG;
+    if (a->d_dstate_in != a->d_dstate_out && meet(in, out)) return TCU_ERR_INVALID_ARG;
+    const GatedParams p = params(a);
+    dispatch(a, s.pairs({&a->x, &a->gate, &a->d_y, &a->d_x, &a->d_gate}), [&](auto t, auto in_gate, auto pair) {
+        tcu_gated_backward_kernel<decltype(t), decltype(in_gate)::value, decltype(pair)::value><<<uint32_t(a->batch * p.strips), kGatedWarps * 32, 0, stream>>>(p);
+    });
+    return launched();
+}
+
+tcu_status_t tcu_gated_step(const tcu_gated_t *a, cudaStream_t stream) {
+    Sizes s;
+    if (tcu_status_t st = check(a, s)) return st;
+    if (a->d_offsets) return TCU_ERR_INVALID_ARG;
+    if (a->batch == 0) return TCU_OK;
+    s.tokens = 1;
+    if (!s.right(a->x, false) || !s.right(a->gate, false) || !s.right(a->y, true)) return TCU_ERR_INVALID_ARG;
+    if (!a->d_state_out || !aligned(a->d_slots, 4) || (!a->d_slots && a->pool_slots < a->batch)) return TCU_ERR_INVALID_ARG;
+    if (a->batch > (kMostWalks * 256) / a->channels) return TCU_ERR_UNSUPPORTED;
+    Sizes pool = s;
+    pool.batch = a->pool_slots;
+    const Span states = pool.states(a->d_state_out), y = s.span(a->y);
+    if (meet(states, y) || meet(states, s.span(a->x)) || meet(states, s.span(a->gate))) return TCU_ERR_INVALID_ARG;
+    for (const tcu_rows_t *r : {&a->x, &a->gate})
+        if (meet(y, s.span(*r)) && !(r->ptr == a->y.ptr && (a->batch == 1 || r->stride_batch == a->y.stride_batch))) return TCU_ERR_INVALID_ARG;
+    const GatedParams p = params(a);
+    const uint64_t blocks = (a->batch * a->channels + 255) / 256;
+    dispatch(a, false, [&](auto t, auto in_gate, auto) {
+        tcu_gated_step_kernel<decltype(t), decltype(in_gate)::value><<<uint32_t(blocks), 256, 0, stream>>>(p, a->d_slots, a->pool_slots, uint32_t(a->batch));
+    });
+    return launched();
+}
+
+}  // extern "C"

@@ -10,6 +10,7 @@
 #include <type_traits>
 
 #include "tcu_embedding_kernel.cuh"
+#include "tcu_host.h"
 #include "tcu_linattn_kernel.cuh"
 
 namespace {
@@ -17,21 +18,6 @@ namespace {
 using namespace tcu;
 
 constexpr size_t kStatusBytes = 256;       // the header of a scan workspace: one status word is used
-
-size_t float_bytes(tcu_float_t t) { return t == TCU_F32 ? 4 : 2; }
-bool valid_float(int t) { return t == TCU_F32 || t == TCU_F16 || t == TCU_BF16; }
-bool aligned(const void *p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
-bool overlaps(const void *a, size_t an, const void *b, size_t bn) {
-    auto pa = reinterpret_cast<uintptr_t>(a), pb = reinterpret_cast<uintptr_t>(b);
-    return a && b && pa < pb + bn && pb < pa + an;
-}
-// Whether a runtime call went well; if not, its error is taken here and is not left for the check of a later launch.
-bool ok(cudaError_t e) {
-    if (e == cudaSuccess) return true;
-    (void)cudaGetLastError();
-    return false;
-}
-tcu_status_t launched() { return cudaGetLastError() == cudaSuccess ? TCU_OK : TCU_ERR_CUDA; }
 
 // ---- linear attention
 bool has_struct(const tcu_linattn_t *a) { return a && a->struct_bytes == sizeof(tcu_linattn_t); }
@@ -512,22 +498,6 @@ EmbeddingWs embedding_ws(size_t n, size_t rows, size_t d) {
     w.head = take(size_t(w.pieces) * d * 4);
     w.bytes = at;
     return w;
-}
-
-// A kernel that may be set up while the one ahead of it in the stream, of the same sequence, still runs.  A sequence ends at its
-// first launch that fails: the kernels behind it index memory by what the ones before have written.
-template <typename... P, typename... A>
-tcu_status_t launch_next(void (*kernel)(P...), dim3 grid, dim3 block, cudaStream_t stream, A... args) {
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr.val.programmaticStreamSerializationAllowed = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid;
-    cfg.blockDim = block;
-    cfg.stream = stream;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    return ok(cudaLaunchKernelEx(&cfg, kernel, P(args)...)) ? TCU_OK : TCU_ERR_CUDA;
 }
 
 // Tiles whose counts every block of the sort adds up by itself; more are scanned by a kernel between.  65536 tokens of 64 columns, 64 tiles:

@@ -1,0 +1,271 @@
+"""Gated linear recurrence: outputs, states and gradients against 64 bits with derived bounds, over lengths, widths, types, strides,
+packed sequences and gates at their ends."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2411_17887_b200 import api
+from tests import gated_reference as ref
+from tests.lm_reference import assert_within, f64
+
+pytestmark = pytest.mark.gpu
+TYPES = [torch.float32, torch.float16, torch.bfloat16]
+KINDS = ["complement", "one", "root"]
+
+
+@pytest.fixture(autouse=True)
+def _device():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+
+
+def draw(shape, dtype, seed=0, memory=3.0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    normal = lambda *s: torch.randn(s, generator=g, device="cuda")  # noqa: E731
+    x, d_y = normal(*shape).to(dtype), normal(*shape).to(dtype)
+    gate = (memory * torch.rand(shape[-1], generator=g, device="cuda") + 2.0 * normal(*shape)).to(dtype)
+    return x, gate, d_y
+
+
+def check(x, gate, d_y, kind, first=None, d_last=None, lens=None):
+    """Everything that a call returns, sequence by sequence, against 64 bits."""
+    dtype, d = x.dtype, x.shape[-1]
+    offsets = None if lens is None else torch.tensor([0] + list(lens), device="cuda").cumsum(0)
+    batch = len(lens) if lens is not None else x.shape[0]
+    y, last, marks = api.gated_recurrence(x, gate, first, offsets, True, kind, output_marks=True)
+    d_x, d_gate, d_first = api.gated_recurrence_backward(d_y, x, gate, first, offsets, d_last, kind, marks=marks)
+    assert y.dtype == d_x.dtype == d_gate.dtype == dtype and last.dtype == torch.float32 and (d_first is None) == (first is None)
+    again = api.gated_recurrence_backward(d_y, x, gate, first, offsets, d_last, kind)
+    assert torch.equal(again[0], d_x) and torch.equal(again[1], d_gate)                # the same bits again, with marks of its own
+    zero, at = np.zeros(d), 0
+    for b in range(batch):
+        if lens is None:
+            pick = lambda z: z[b]  # noqa: E731
+        else:
+            pick = lambda z: z[at:at + lens[b]]  # noqa: E731
+        s0, s1 = (zero if s is None else f64(s[b]) for s in (first, d_last))
+        (h, e), (want, bound) = ref.forward(f64(pick(x)), f64(pick(gate)), kind, s0, dtype)
+        assert_within(pick(y), h, e, f"y of {b}")
+        assert_within(last[b], want, bound, f"state of {b}")
+        dx, dg, d0 = ref.backward(f64(pick(x)), f64(pick(gate)), f64(pick(d_y)), kind, s0, s1, dtype)
+        assert_within(pick(d_x), *dx, f"d_x of {b}")
+        assert_within(pick(d_gate), *dg, f"d_gate of {b}")
+        if first is not None:
+            assert_within(d_first[b], *d0, f"d_first of {b}")
+        at += 0 if lens is None else lens[b]
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=["f32", "f16", "bf16"])
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("b,t,d,states", [(1, 1, 1, False), (1, 37, 64, True), (2, 64, 66, False), (1, 65, 1, True), (3, 129, 127, True), (2, 300, 130, False),
+                                          (1, 1000, 8, True), (2, 2049, 192, False)])
+def test_dense(b, t, d, states, kind, dtype):
+    x, gate, d_y = draw((b, t, d), dtype, t + d)
+    first = torch.randn((b, d), device="cuda") if states else None
+    check(x, gate, d_y, kind, first, torch.randn((b, d), device="cuda") if states else None)
+
+
+@pytest.mark.parametrize("t", [511, 513, 1024, 4097, 9000])
+def test_long_memory(t):
+    """Gates close to one: the state is a sum over thousands of tokens."""
+    x, gate, d_y = draw((1, t, 40), torch.float32, t, memory=9.0)
+    check(x, gate, d_y, "complement", torch.ones((1, 40), device="cuda"))
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=["f32", "f16", "bf16"])
+@pytest.mark.parametrize("lens,d", [([5, 0, 1, 64, 65, 0, 200], 70), ([0, 0], 9), ([1] * 40, 64), ([700, 3, 1500], 33), ([128, 64, 63], 128)])
+def test_packed(lens, d, dtype):
+    x, gate, d_y = draw((sum(lens), d), dtype, sum(lens))
+    states = torch.randn((2, len(lens), d), device="cuda")
+    check(x, gate, d_y, "complement", states[0], states[1], lens)
+    check(x, gate, d_y, "root", None, None, lens)
+
+
+def test_rows_behind_the_last_sequence():
+    x, gate, d_y = draw((100, 24), torch.bfloat16, 5)
+    x[70:] = gate[70:] = d_y[70:] = float("nan")
+    offsets = torch.tensor([0, 30, 70], device="cuda")
+    y, last, marks = api.gated_recurrence(x, gate, None, offsets, True, output_marks=True)
+    d_x, d_gate, _ = api.gated_recurrence_backward(d_y, x, gate, None, offsets, marks=marks)
+    assert all(torch.isfinite(z).all() for z in (y[:70], last, d_x[:70], d_gate[:70]))
+    # what the C entry writes: rows behind the last sequence are as they were
+    from paper_2411_17887_b200 import binding as B
+    held = torch.full((3, 100, 24), 7.0, device="cuda", dtype=torch.bfloat16)
+    row = lambda z: (z.data_ptr(), 0, 24)  # noqa: E731
+    args = dict(d_offsets=offsets.data_ptr(), d_marks=marks.data_ptr(), marks_bytes=marks.numel() * 4)
+    stream = torch.cuda.current_stream().cuda_stream
+    assert B.tcu_gated_forward(B.tcu_gated_args(B.TCU_BF16, 0, 24, 2, 100, row(x), row(gate), row(held[0]), **args), stream) == B.TCU_OK
+    assert B.tcu_gated_backward(B.tcu_gated_args(B.TCU_BF16, 0, 24, 2, 100, row(x), row(gate), d_y=row(d_y), d_x=row(held[1]), d_gate=row(held[2]), **args), stream) == B.TCU_OK
+    assert (held[:, 70:] == 7.0).all()
+    assert torch.equal(held[:, :70], torch.stack([y, d_x, d_gate])[:, :70])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+def test_strides(dtype):
+    """Views of larger arrays, at every alignment, an input that repeats over the batch, and transposed ones."""
+    wide, other, _ = draw((3, 90, 2 * 37), dtype, 11)
+    d_y = torch.randn((3, 90, 37), device="cuda").to(dtype)
+    for x, gate in ((wide[..., :37], wide[..., 37:]), (wide[..., 1:38], other[..., 3:40]), (wide[:1, :, :37].expand(3, -1, -1), other[..., 37:]),
+                    (wide.transpose(0, 1).contiguous().transpose(0, 1)[..., :37], other[..., ::2]), (wide.flip(1)[:, ::3][..., :37], other[:, ::3][..., :37])):
+        check(x, gate, d_y[:, :x.shape[1]], "complement")
+    x, gate = wide[..., 2:38], wide[..., 38:]
+    check(x, gate, d_y[..., :36], "one", torch.randn((3, 36), device="cuda"))
+
+
+def test_no_tokens():
+    first = torch.randn((2, 10), device="cuda")
+    empty = torch.empty((2, 0, 10), device="cuda", dtype=torch.float16)
+    y, last = api.gated_recurrence(empty, empty, first, output_final_state=True)
+    assert y.shape == (2, 0, 10) and torch.equal(last, first)
+    d_x, d_gate, d_first = api.gated_recurrence_backward(empty, empty, empty, first, d_final_state=2 * first)
+    assert d_x.shape == d_gate.shape == (2, 0, 10) and torch.equal(d_first, 2 * first)
+    assert not api.gated_recurrence(empty, empty, output_final_state=True)[1].any()
+    none = torch.empty((0, 5, 10), device="cuda", dtype=torch.float16)
+    y, last = api.gated_recurrence(none, none, output_final_state=True)
+    assert y.shape == (0, 5, 10) and last.shape == (0, 10)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_gates_at_their_ends(kind):
+    """f = 0 forgets everything, f = 1 keeps everything; finite gradients either way."""
+    x, gate, d_y = draw((1, 200, 8), torch.float32, 3)
+    ends = torch.tensor([float("inf"), float("-inf"), 100.0, -100.0, 20.0, -20.0, 0.0, 88.0], device="cuda")
+    gate[:, ::3] = ends
+    gate[:, 1::3] = ends.flip(0)
+    check(x, gate, d_y, kind, torch.ones((1, 8), device="cuda"), torch.ones((1, 8), device="cuda"))
+
+
+def test_what_is_not_finite_stays_in_its_channel():
+    x, gate, d_y = draw((2, 150, 70), torch.bfloat16, 4)
+    clean = api.gated_recurrence(x, gate, output_final_state=True)
+    x[0, 100, 3], gate[1, 20, 69], x[0, 0, 10] = float("inf"), float("nan"), float("nan")
+    y, last = api.gated_recurrence(x, gate, output_final_state=True)
+    bad = torch.zeros_like(y, dtype=torch.bool)
+    bad[0, 100:, 3] = bad[1, 20:, 69] = bad[0, :, 10] = True
+    assert torch.equal(y[~bad], clean[0][~bad]) and not torch.isfinite(y[0, 100, 3]) and torch.isnan(y[1, 20:, 69]).all() and torch.isnan(y[0, :, 10]).all()
+    assert torch.equal(last[~bad[:, -1]], clean[1][~bad[:, -1]])
+
+
+def test_differences():
+    """The gradients of the kernel against differences of the 64-bit recurrence."""
+    for kind in KINDS:
+        x, gate, d_y = draw((1, 20, 3), torch.float32, 9)
+        first, d_last = torch.randn((1, 3), device="cuda"), torch.randn((1, 3), device="cuda")
+        got = api.gated_recurrence_backward(d_y, x, gate, first, None, d_last, kind)
+        args = [f64(x[0]), f64(gate[0]), f64(first[0])]
+
+        def loss(x, g, s):
+            (h, _), (last, _) = ref.forward(x, g, kind, s, torch.float32)
+            return (h * f64(d_y[0])).sum() + (last * f64(d_last[0])).sum()
+
+        for which in range(3):
+            for at in np.ndindex(args[which].shape):
+                moved = []
+                for step in (1e-5, -1e-5):
+                    some = [a.copy() for a in args]
+                    some[which][at] += step
+                    moved.append(loss(*some))
+                # second order of the difference (third derivatives of a few units times 1e-10) and cancellation (1e-14 / 1e-5), then 32 bits
+                assert abs((moved[0] - moved[1]) / 2e-5 - float(got[which][0][at])) < 1e-5, (kind, which, at)
+
+
+def test_autograd():
+    x, gate, d_y = draw((2, 130, 66), torch.bfloat16, 8)
+    first = torch.randn((2, 66), device="cuda")
+    leaves = [z.clone().requires_grad_() for z in (x, gate, first)]
+    y, last = api.gated_recurrence(*leaves, output_final_state=True, input_gate="root")
+    (y.float() * d_y.float()).sum().add(last.sum()).backward()
+    want = api.gated_recurrence_backward(d_y, x, gate, first, None, torch.ones_like(first), "root")
+    for leaf, grad in zip(leaves, want):
+        assert torch.equal(leaf.grad, grad)
+    y, last = api.gated_recurrence(leaves[0], gate, output_final_state=True)                 # the state alone is used
+    leaves[0].grad = None
+    last.sum().backward()
+    assert torch.equal(leaves[0].grad, api.gated_recurrence_backward(torch.zeros_like(x), x, gate, None, None, torch.ones_like(first))[0])
+    y, _ = api.gated_recurrence(leaves[0], leaves[1])
+    y.sum().backward()                                                                       # the gradient of a sum has strides of zero
+    root = torch.ones_like(x).requires_grad_()
+    y, _ = api.gated_recurrence(x * root ** 2, gate)
+    g, = torch.autograd.grad(y.float().square().sum(), root, create_graph=True)
+    with pytest.raises(RuntimeError, match="once_differentiable"):
+        g.float().sum().backward()
+    with torch.autograd.forward_ad.dual_level():
+        dual = torch.autograd.forward_ad.make_dual(x, torch.ones_like(x))
+        for call in (lambda: api.gated_recurrence(dual, gate), lambda: api.gated_recurrence(x, gate, torch.autograd.forward_ad.make_dual(first, first)),
+                     lambda: api.gated_recurrence_backward(dual, x, gate), lambda: api.gated_recurrence_step(dual[:, 0], gate[:, 0], first.clone())):
+            with pytest.raises(NotImplementedError):
+                call()
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=["f32", "f16", "bf16"])
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("b,d", [(1, 1), (3, 130), (70, 1000), (5, 4099)])
+def test_step(b, d, kind, dtype):
+    """One token after another is the recurrence; entries outside the pool are skipped, the others' states are not touched."""
+    x, gate, _ = draw((b, 4, d), dtype, b + d)
+    pool = torch.randn((b + 3, d), device="cuda")
+    slots = torch.randperm(b + 3, device="cuda")[:b].to(torch.int32)
+    if b > 2:
+        slots[1], slots[2] = -1, b + 3
+    live = (slots >= 0) & (slots < b + 3)
+    held, first = pool.clone(), pool[slots.long().clamp(0, b + 2)]
+    ys = torch.stack([api.gated_recurrence_step(x[:, t], gate[:, t], pool, slots, kind) for t in range(4)], 1)
+    for k in range(b):
+        if not live[k]:
+            assert not ys[k].any()
+            continue
+        (h, e), (last, bound) = ref.forward(f64(x[k]), f64(gate[k]), kind, f64(first[k]), dtype)
+        assert_within(ys[k], h, e, "y")
+        assert_within(pool[slots[k].long()], last, bound, "state")
+    rest = torch.ones(b + 3, dtype=torch.bool, device="cuda")
+    rest[slots[live].long()] = False
+    assert torch.equal(pool[rest], held[rest])
+
+
+def test_step_refuses_gradients_and_says_what_it_wrote():
+    x, gate, _ = draw((2, 8), torch.float32, 1)
+    pool = torch.zeros((2, 8), device="cuda")
+    for which in range(3):
+        args = [x, gate, pool]
+        args[which] = args[which].clone().requires_grad_()
+        with pytest.raises(RuntimeError, match="no_grad"):
+            api.gated_recurrence_step(*args)
+    version = pool._version
+    api.gated_recurrence_step(x, gate, pool)
+    assert pool._version > version
+    assert torch.equal(api.gated_recurrence_step(x.t().contiguous().t(), gate, torch.zeros_like(pool)), api.gated_recurrence(x[:, None], gate[:, None])[0][:, 0])
+
+
+def test_graph_and_streams():
+    """A captured forward and backward pass, replayed on new inputs, and two streams at once."""
+    sets = [draw((1, 700, 200), torch.bfloat16, s) for s in range(3)]
+
+    def both(x, gate, d_y):
+        y, last, marks = api.gated_recurrence(x, gate, output_final_state=True, output_marks=True)
+        return (y, last, *api.gated_recurrence_backward(d_y, x, gate, marks=marks)[:2])
+
+    want = [both(*s) for s in sets]
+    held = [z.clone() for z in sets[0]]
+    graph = torch.cuda.CUDAGraph()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        both(*held)
+    torch.cuda.current_stream().wait_stream(side)
+    with torch.cuda.graph(graph):
+        outs = both(*held)
+    for k in (1, 2, 0):
+        for z, new in zip(held, sets[k]):
+            z.copy_(new)
+        graph.replay()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want[k]))
+    streams = [torch.cuda.Stream() for _ in sets]
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(5):
+        for stream, s in zip(streams, sets):
+            with torch.cuda.stream(stream):
+                got.append(both(*s))
+    torch.cuda.synchronize()
+    for k, outs in enumerate(got):
+        assert all(torch.equal(a, b) for a, b in zip(outs, want[k % 3]))
