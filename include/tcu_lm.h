@@ -14,6 +14,8 @@
  *        h_t = f_t h_{t-1} + i_t x_t            f = sigmoid(gate)
  *    over prompts (states in and out, dense or packed), its gradients (the same scan backward in time), single tokens.
  *
+ *  - Layer norm and its gradients, the sums over rows of the parameters' among them.
+ *
  * The general conventions of tcu_scan.h hold: caller-owned device memory, nothing allocated, everything asynchronous
  * on `stream`, argument errors found on the host before anything is queued, bounded device-side waits, launches that
  * can be captured into a CUDA graph.
@@ -194,6 +196,22 @@ tcu_status_t tcu_gated_backward(const tcu_gated_t *args, cudaStream_t stream);
 
 /* One token for each of `batch` sequences: the state of each is updated in place, and y written (y may be x or gate, with its strides). */
 tcu_status_t tcu_gated_step(const tcu_gated_t *args, cudaStream_t stream);
+
+/* ---- layer norm: y = weight * (x - mean) / sqrt(variance + eps) + bias over each row of d elements, the variance that of all d elements
+ *   d_x        device, rows x d of `type`, row stride x_stride elements (0 to 2^38);  d_y  device, rows x d dense (may be d_x, with x_stride = d)
+ *   d_weight, d_bias   device, d values of param_type - fp32, or the same as `type` - or NULL: 1, 0
+ * Sums in fp32, values are rounded once.  A row's result depends on its own values alone, and is the same from call to call.
+ * TCU_ERR_UNSUPPORTED: d above 32768, rows above 2^40, another param_type. */
+tcu_status_t tcu_layer_norm_forward(const void *d_x, size_t rows, size_t d, size_t x_stride, tcu_float_t type, const void *d_weight, const void *d_bias,
+                                    tcu_float_t param_type, float eps, void *d_y, cudaStream_t stream);
+
+/* Gradients from d_dy, that of y (row stride dy_stride), and x: d_dx (rows x d dense of `type`, or NULL; may be d_dy, with dy_stride = d),
+ * d_dweight and d_dbias (d values of param_type each, or NULL: sums over all rows, the same bits from call to call; zero without rows).
+ *   d_ws       tcu_layer_norm_workspace_bytes(rows, d) bytes, 16-byte aligned, if either of the sums is wanted; needs no clearing; not to be shared
+ *              by calls that may overlap */
+size_t tcu_layer_norm_workspace_bytes(size_t rows, size_t d);
+tcu_status_t tcu_layer_norm_backward(const void *d_dy, size_t dy_stride, const void *d_x, size_t x_stride, size_t rows, size_t d, tcu_float_t type, const void *d_weight,
+                                     tcu_float_t param_type, float eps, void *d_dx, void *d_dweight, void *d_dbias, void *d_ws, size_t ws_bytes, cudaStream_t stream);
 
 #ifdef __cplusplus
 }

@@ -588,3 +588,89 @@ def gated_recurrence_step(x, gate, state, slots=None, input_gate="complement"):
     B.check(B.tcu_gated_step(args, _stream(device)))
     _written(state)
     return y
+
+
+# ------------------------------------------------------------------------------------------------ layer norm
+def _rows(x: torch.Tensor):
+    """x as rows of its last axis: a tensor whose rows lie one stride apart, their number and the stride (copied if they do not)."""
+    d = x.shape[-1]
+    if x.dim() == 2 and (x.stride(1) == 1 or d == 1):
+        return x, x.shape[0], x.stride(0)
+    x = x.contiguous()
+    return x, x.numel() // d, d
+
+
+def _check_norm(x, eps, **params):
+    """The type of the parameters."""
+    if x.dtype not in _FLOAT:
+        raise TypeError(f"layer norm takes float32, float16 or bfloat16, not {x.dtype}")
+    if x.dim() < 1 or x.shape[-1] == 0:
+        raise ValueError(f"x is {tuple(x.shape)}: there is no last axis to normalise")
+    if not 0.0 <= eps < float("inf"):
+        raise ValueError(f"eps is {eps}")
+    kind = None
+    for name, p in params.items():
+        if p is None:
+            continue
+        if p.shape != x.shape[-1:] or not p.is_contiguous() or p.device != x.device:
+            raise ValueError(f"{name}: a contiguous tensor of shape ({x.shape[-1]},) on the device of x")
+        if p.dtype not in (torch.float32, x.dtype) or (kind is not None and p.dtype != kind):
+            raise TypeError(f"{name} is {p.dtype}: float32 or the type of x, and all parameters alike")
+        kind = p.dtype
+    return kind or torch.float32
+
+
+def _norm_forward(x, weight, bias, eps):
+    kind = _check_norm(x, eps, weight=weight, bias=bias)
+    y = x.new_empty(x.shape)
+    x, rows, stride = _rows(x)
+    B.check(B.tcu_layer_norm_forward(x, rows, x.shape[-1], stride, _FLOAT[x.dtype], weight, bias, _FLOAT[kind], eps, y, _stream(x.device)))
+    return y
+
+
+def layer_norm_backward(d_y, x, weight=None, eps=1e-5, params=True):
+    """Gradients of :func:`layer_norm` with respect to x, weight and bias, from that of its output: (d_x, d_weight, d_bias), the
+    last two of the weight's type (float32 without one), None with ``params=False``."""
+    if forward_ad._current_level >= 0:
+        _no_tangents(d_y=d_y, x=x, weight=weight)
+    return _norm_backward(d_y, x, weight, None, eps, True, params, params)
+
+
+def _norm_backward(d_y, x, weight, bias, eps, want_x, want_weight, want_bias):
+    kind = _check_norm(x, eps, weight=weight, bias=bias)
+    if d_y.dtype != x.dtype or d_y.device != x.device:
+        _refuse(x.dtype, x.device, d_y=d_y)
+    if d_y.shape != x.shape:
+        raise ValueError(f"d_y is {tuple(d_y.shape)}, x {tuple(x.shape)}")
+    d = x.shape[-1]
+    d_x = x.new_empty(x.shape) if want_x else None
+    d_weight = x.new_empty(d, dtype=kind) if want_weight else None
+    d_bias = x.new_empty(d, dtype=kind) if want_bias else None
+    x, rows, stride = _rows(x)
+    d_y, _, dy_stride = _rows(d_y)
+    size = B.tcu_layer_norm_workspace_bytes(rows, d) if want_weight or want_bias else 0
+    ws = x.new_empty(size // 4, dtype=torch.float32) if size else None
+    B.check(B.tcu_layer_norm_backward(d_y, dy_stride, x, stride, rows, d, _FLOAT[x.dtype], weight, _FLOAT[kind], eps, d_x, d_weight, d_bias, ws, size, _stream(x.device)))
+    return d_x, d_weight, d_bias
+
+
+class _LayerNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, eps):
+        ctx.save_for_backward(x, weight, bias)
+        ctx.eps = eps
+        return _norm_forward(x, weight, bias, eps)
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, d_y):
+        return (*_norm_backward(d_y, *ctx.saved_tensors, ctx.eps, *ctx.needs_input_grad[:3]), None)
+
+
+def layer_norm(x, weight=None, bias=None, eps=1e-5):
+    """weight * (x - mean) / sqrt(variance + eps) + bias over the last axis of x, rounded once to its type; differentiable, once, in x, weight
+    and bias.  x float32, float16 or bfloat16, of at most 32768 elements along that axis; weight and bias (d,), float32 or of x's type."""
+    if forward_ad._current_level >= 0 or (torch.is_grad_enabled() and (x.requires_grad or (weight is not None and weight.requires_grad) or
+                                                                       (bias is not None and bias.requires_grad))):
+        return _LayerNorm.apply(x, weight, bias, float(eps))
+    return _norm_forward(x, weight, bias, float(eps))

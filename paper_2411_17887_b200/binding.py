@@ -113,6 +113,12 @@ _lib.tcu_gated_marks_bytes.restype = _sz
 for _name in ("tcu_gated_forward", "tcu_gated_backward", "tcu_gated_step"):
     getattr(_lib, _name).argtypes = [ctypes.c_char_p, _vp]
     getattr(_lib, _name).restype = _int
+_lib.tcu_layer_norm_forward.argtypes = [_vp, _sz, _sz, _sz, _int, _vp, _vp, _int, _f32, _vp, _vp]
+_lib.tcu_layer_norm_forward.restype = _int
+_lib.tcu_layer_norm_workspace_bytes.argtypes = [_sz, _sz]
+_lib.tcu_layer_norm_workspace_bytes.restype = _sz
+_lib.tcu_layer_norm_backward.argtypes = [_vp, _sz, _vp, _sz, _sz, _sz, _int, _vp, _int, _f32, _vp, _vp, _vp, _vp, _sz, _vp]
+_lib.tcu_layer_norm_backward.restype = _int
 _lib.tcu_status_string.argtypes = [_int]
 _lib.tcu_status_string.restype = ctypes.c_char_p
 
@@ -318,6 +324,20 @@ def tcu_gated_backward(args: bytes, stream=0) -> int:
 
 def tcu_gated_step(args: bytes, stream=0) -> int:
     return _lib.tcu_gated_step(args, stream)
+
+
+def tcu_layer_norm_forward(d_x, rows: int, d: int, x_stride: int, dtype: int, d_weight, d_bias, param_dtype: int, eps: float, d_y, stream=0) -> int:
+    return _lib.tcu_layer_norm_forward(_p(d_x), rows, d, x_stride, dtype, _p(d_weight), _p(d_bias), param_dtype, eps, _p(d_y), stream)
+
+
+def tcu_layer_norm_workspace_bytes(rows: int, d: int) -> int:
+    return _lib.tcu_layer_norm_workspace_bytes(rows, d)
+
+
+def tcu_layer_norm_backward(d_dy, dy_stride: int, d_x, x_stride: int, rows: int, d: int, dtype: int, d_weight, param_dtype: int, eps: float, d_dx, d_dweight, d_dbias,
+                            d_ws, ws_bytes: int, stream=0) -> int:
+    return _lib.tcu_layer_norm_backward(_p(d_dy), dy_stride, _p(d_x), x_stride, rows, d, dtype, _p(d_weight), param_dtype, eps, _p(d_dx), _p(d_dweight), _p(d_dbias),
+                                        _p(d_ws), ws_bytes, stream)
 
 
 def tcu_scan_last_stats() -> dict:
