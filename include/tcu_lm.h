@@ -15,6 +15,7 @@
  *    over prompts (states in and out, dense or packed), its gradients (the same scan backward in time), single tokens.
  *
  *  - Layer norm and its gradients, the sums over rows of the parameters' among them.
+ *  - Sampling of a token for each row of logits: the first one at which a prefix sum of weights passes a random number.
  *
  * The general conventions of tcu_scan.h hold: caller-owned device memory, nothing allocated, everything asynchronous
  * on `stream`, argument errors found on the host before anything is queued, bounded device-side waits, launches that
@@ -212,6 +213,39 @@ tcu_status_t tcu_layer_norm_forward(const void *d_x, size_t rows, size_t d, size
 size_t tcu_layer_norm_workspace_bytes(size_t rows, size_t d);
 tcu_status_t tcu_layer_norm_backward(const void *d_dy, size_t dy_stride, const void *d_x, size_t x_stride, size_t rows, size_t d, tcu_float_t type, const void *d_weight,
                                      tcu_float_t param_type, float eps, void *d_dx, void *d_dweight, void *d_dbias, void *d_ws, size_t ws_bytes, cudaStream_t stream);
+
+/* ---- sampling
+ * For each row of logits with largest value m, every token has the weight w = exp((logit - m) / temperature).  In the order of falling
+ * logits, the lower token first among equals, the tokens kept are the first top_k, as far as w >= min_p, and of these the fewest
+ * whose weights add up to at least top_p times the weight of them all; always the first one.  The token drawn is the first, in the order of tokens, up to and
+ * with which the kept weights add up to more than u times their sum; its log probability is log(w / that sum).
+ * Logits that are NaN count as minus infinity, tokens at minus infinity are never drawn; a row of nothing else gives token -1
+ * (log probability minus infinity).  Where m is plus infinity the tokens with it have weight 1, the others 0.
+ * Zero-initialise, set struct_bytes = sizeof(tcu_sample_t), then set what the call uses (top_p: 1 keeps all). */
+typedef struct {
+    uint32_t struct_bytes;
+    uint32_t type;              /* tcu_float_t of the logits                                                        */
+    uint64_t rows;
+    uint32_t vocabulary;        /* 1 to 2^18                                                                        */
+    uint32_t uniform_f64;       /* u is fp64 (1) or fp32 (0)                                                        */
+    const void *d_logits;       /* rows x vocabulary, any alignment of elements                                     */
+    uint64_t logits_stride;     /* of a row, in elements, 0 to 2^38                                                 */
+    const void *d_uniform;      /* a random number u of each row, from 0 to below 1 (below 0 or NaN: 0; from 1 on: the last token kept) */
+    const float *d_temperature; /* of each row, or NULL: `temperature` for all; 0 (or below, or NaN: from memory): the first token alone */
+    const int32_t *d_top_k;     /* of each row, or NULL: `top_k` for all; 0 or below: no limit                      */
+    const float *d_top_p;       /* of each row, or NULL: `top_p` for all; 1 or above (or NaN: from memory): no limit */
+    const float *d_min_p;       /* of each row, or NULL: `min_p` for all; 0 or below (or NaN: from memory): no limit */
+    double temperature;
+    int64_t top_k;
+    double top_p, min_p;
+    int64_t *d_tokens;          /* receives the token of each row                                                   */
+    float *d_log_probs;         /* NULL, or receives the log of its probability                                     */
+} tcu_sample_t;
+
+/* What is written must not overlap an input.  Weights and sums are 64-bit floating point, sums that top_p is compared with fixed point of 42 bits: the
+ * token is that of exact arithmetic unless u or top_p lies within about 1e-12 (top_p: 1e-9) of the border between two.
+ * TCU_ERR_UNSUPPORTED: more than 2^18 tokens, or 2^28 - 1 rows. */
+tcu_status_t tcu_sample(const tcu_sample_t *args, cudaStream_t stream);
 
 #ifdef __cplusplus
 }

@@ -674,3 +674,54 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5):
                                                                        (bias is not None and bias.requires_grad))):
         return _LayerNorm.apply(x, weight, bias, float(eps))
     return _norm_forward(x, weight, bias, float(eps))
+
+
+# ------------------------------------------------------------------------------------------------ sampling
+def _setting(name, value, rows, dtype, device):
+    """(pointer, value for all rows): a tensor holds one for each row."""
+    if isinstance(value, torch.Tensor):
+        if value.shape != (rows,) or value.dtype != dtype or not value.is_contiguous() or value.device != device:
+            raise ValueError(f"{name}: a number, or a contiguous {dtype} tensor of one value for each row, on the device of the logits")
+        return value.data_ptr(), 0
+    if value != value:
+        raise ValueError(f"{name} is {value}")
+    return 0, value
+
+
+def sample(logits, uniform, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, output_log_prob=False):
+    """One token for each row of logits (rows, vocabulary), float32, float16 or bfloat16: int64 (rows,); with ``output_log_prob=True`` also the log
+    of the probability that it was drawn with, float32.
+
+    Every token has the weight exp((logit - largest) / temperature).  In the order of falling logits, the lower token first among
+    equals, the first `top_k` are kept (0: all), as far as their weight is at least `min_p`, and of these the fewest whose weights add up
+    to `top_p` of the weight of them all; at least one.  `uniform` (rows,), float32 or float64 from [0, 1), picks the token: the first, in the order of tokens,
+    with which the kept weights add up to more than that part of their sum.  temperature 0 takes the largest logit, the lowest token
+    among equals.  The settings are numbers, or a tensor with one for each row (float32; top_k: int32).  NaN counts as minus infinity; a row that holds
+    nothing above it gives -1.  No gradient is computed: with gradients enabled, logits that require one are refused."""
+    if forward_ad._current_level >= 0:
+        _no_tangents(logits=logits, uniform=uniform)
+    if torch.is_grad_enabled():
+        _not_recorded(logits=logits)
+    dtype, device = logits.dtype, logits.device
+    if dtype not in _FLOAT:
+        raise TypeError(f"sampling takes float32, float16 or bfloat16, not {dtype}")
+    if logits.dim() != 2 or logits.shape[1] == 0:
+        raise ValueError(f"logits: (rows, vocabulary), not {tuple(logits.shape)}")
+    rows, vocabulary = logits.shape
+    if uniform.shape != (rows,) or uniform.dtype not in (torch.float32, torch.float64) or not uniform.is_contiguous() or uniform.device != device:
+        raise ValueError("uniform: a contiguous float32 or float64 tensor of one value for each row, on the device of the logits")
+    d_temperature, temperature = _setting("temperature", temperature, rows, torch.float32, device)
+    d_top_k, top_k = _setting("top_k", top_k, rows, torch.int32, device)
+    d_top_p, top_p = _setting("top_p", top_p, rows, torch.float32, device)
+    d_min_p, min_p = _setting("min_p", min_p, rows, torch.float32, device)
+    if not 0.0 <= temperature < float("inf"):
+        raise ValueError(f"temperature is {temperature}")
+    if vocabulary > 1 and logits.stride(1) != 1:
+        logits = logits.contiguous()
+    tokens = logits.new_empty(rows, dtype=torch.int64)
+    log_prob = logits.new_empty(rows, dtype=torch.float32) if output_log_prob else None
+    args = B.tcu_sample_args(_FLOAT[dtype], rows, vocabulary, logits.data_ptr(), logits.stride(0), uniform.data_ptr(), int(uniform.dtype == torch.float64), tokens.data_ptr(),
+                             _ptr(log_prob), d_temperature=d_temperature, d_top_k=d_top_k, d_top_p=d_top_p, d_min_p=d_min_p, temperature=float(temperature),
+                             top_k=min(max(int(top_k), 0), 1 << 40), top_p=float(top_p), min_p=float(min_p))
+    B.check(B.tcu_sample(args, _stream(device)))
+    return (tokens, log_prob) if output_log_prob else tokens

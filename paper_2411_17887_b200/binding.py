@@ -119,6 +119,8 @@ _lib.tcu_layer_norm_workspace_bytes.argtypes = [_sz, _sz]
 _lib.tcu_layer_norm_workspace_bytes.restype = _sz
 _lib.tcu_layer_norm_backward.argtypes = [_vp, _sz, _vp, _sz, _sz, _sz, _int, _vp, _int, _f32, _vp, _vp, _vp, _vp, _sz, _vp]
 _lib.tcu_layer_norm_backward.restype = _int
+_lib.tcu_sample.argtypes = [ctypes.c_char_p, _vp]
+_lib.tcu_sample.restype = _int
 _lib.tcu_status_string.argtypes = [_int]
 _lib.tcu_status_string.restype = ctypes.c_char_p
 
@@ -338,6 +340,21 @@ def tcu_layer_norm_backward(d_dy, dy_stride: int, d_x, x_stride: int, rows: int,
                             d_ws, ws_bytes: int, stream=0) -> int:
     return _lib.tcu_layer_norm_backward(_p(d_dy), dy_stride, _p(d_x), x_stride, rows, d, dtype, _p(d_weight), param_dtype, eps, _p(d_dx), _p(d_dweight), _p(d_dbias),
                                         _p(d_ws), ws_bytes, stream)
+
+
+_SAMPLE = struct.Struct("=IIQIIQQQQQQQdqddQQ")                  # tcu_sample_t
+
+
+def tcu_sample_args(dtype: int, rows: int, vocabulary: int, d_logits: int, logits_stride: int, d_uniform: int, uniform_f64: int, d_tokens: int, d_log_probs: int = 0, *,
+                    d_temperature: int = 0, d_top_k: int = 0, d_top_p: int = 0, d_min_p: int = 0, temperature: float = 1.0, top_k: int = 0, top_p: float = 1.0,
+                    min_p: float = 0.0) -> bytes:
+    """The argument structure of tcu_sample; pointers are integers (0 for NULL)."""
+    return _SAMPLE.pack(_SAMPLE.size, dtype, rows, vocabulary, uniform_f64, d_logits, logits_stride, d_uniform, d_temperature, d_top_k, d_top_p, d_min_p,
+                        temperature, top_k, top_p, min_p, d_tokens, d_log_probs)
+
+
+def tcu_sample(args: bytes, stream=0) -> int:
+    return _lib.tcu_sample(args, stream)
 
 
 def tcu_scan_last_stats() -> dict:
