@@ -14,8 +14,9 @@ namespace {
 using namespace tcu;
 
 constexpr uint64_t kMostWalks = (uint64_t(1) << 31) - 1;
-constexpr uint64_t kMostTokens = uint64_t(1) << 40;
+constexpr uint64_t kMostTokens = (uint64_t(1) << 31) - 8192;                // (positions ahead of the last tile are 32-bit integers too)
 constexpr uint32_t kMostChannels = uint32_t(1) << 30;
+constexpr uint64_t kSms = 148;
 constexpr int64_t kMostStride = int64_t(1) << 38;
 
 // First and one-past-last byte that an array may touch; to the end of all addresses if it has no such last byte.
@@ -48,14 +49,20 @@ struct Sizes {
             if (s < 0 || s > kMostStride) return false;
         return !written || !((!packed && batch > 1 && r.stride_batch == 0) || (tokens > 1 && r.stride_token == 0));
     }
-    // whether two channels can be moved at a time
-    bool pairs(std::initializer_list<const tcu_rows_t *> rows) const {
-        if (channels % 2) return false;
-        for (const tcu_rows_t *r : rows) {
-            if (!r->ptr) continue;
-            if (!aligned(r->ptr, 2 * element) || (tokens > 1 && r->stride_token % 2) || (!packed && batch > 1 && r->stride_batch % 2)) return false;
+    // whether all rows of an array begin at multiples of `bytes`, and have a number of them
+    bool multiples(const tcu_rows_t &r, size_t bytes) const {
+        const int64_t each = int64_t(bytes / element);
+        return !r.ptr || (channels % each == 0 && aligned(r.ptr, bytes) && (tokens <= 1 || r.stride_token % each == 0) && (packed || batch <= 1 || r.stride_batch % each == 0));
+    }
+    // How arrays are read and written: 16 bytes and two channels at a time, 4 bytes and two channels, or one channel.
+    int way(std::initializer_list<const tcu_rows_t *> in, std::initializer_list<const tcu_rows_t *> out) const {
+        bool sixteen = true, four = true, two = true;
+        for (const tcu_rows_t *r : in) {
+            sixteen = sixteen && multiples(*r, 16);
+            four = four && multiples(*r, 4);
         }
-        return true;
+        for (const tcu_rows_t *r : out) two = two && multiples(*r, 2 * element);
+        return two && sixteen ? 0 : two && four ? 1 : 2;
     }
 };
 
@@ -96,21 +103,44 @@ tcu_status_t check(const tcu_gated_t *a, Sizes &s) {
 }
 
 
-// Calls go(type, input gate, pairs) with these as types.
+// Calls go(type, input gate) with these as types.
 template <typename F>
-void dispatch(const tcu_gated_t *a, bool pairs, F go) {
+void dispatch(const tcu_gated_t *a, F go) {
     auto input = [&](auto t) {
-        auto pair = [&](auto in) {
-            if (pairs) go(t, in, std::true_type{});
-            else go(t, in, std::false_type{});
-        };
-        if (a->input_gate == TCU_INPUT_COMPLEMENT) pair(std::integral_constant<int, kInputComplement>{});
-        else if (a->input_gate == TCU_INPUT_ONE) pair(std::integral_constant<int, kInputOne>{});
-        else pair(std::integral_constant<int, kInputRoot>{});
+        if (a->input_gate == TCU_INPUT_COMPLEMENT) go(t, std::integral_constant<int, kInputComplement>{});
+        else if (a->input_gate == TCU_INPUT_ONE) go(t, std::integral_constant<int, kInputOne>{});
+        else go(t, std::integral_constant<int, kInputRoot>{});
     };
     if (a->type == TCU_F32) input(float{});
     else if (a->type == TCU_F16) input(__half{});
     else input(__nv_bfloat16{});
+}
+
+// Blocks of a cluster that walk a sequence together: as many as keep all blocks on the SMs at once, two an SM, and have a tile each.  16383 tokens of
+// 2048 channels, 32 walks: 8 blocks 61 us, 4 blocks 82; 8 x 4096 tokens, 256 walks: one block 84 us, two 111.  Packed sequences are of lengths
+// that the host does not know, and the longest alone may take most of the time: up to four times as many blocks (24 sequences of 1504 channels,
+// 16001 tokens: of 0 to 3972 each, one block 90 us, two 73; of 667 each 38 and 52).
+uint32_t blocks_of_walk(uint64_t walks, const Sizes &s) {
+    const uint64_t most = s.packed ? 4 * 2 * kSms : 2 * kSms, tiles = s.packed ? 4 * s.tokens / s.batch / 128 : (s.tokens + 127) / 128;
+    uint32_t ranks = 1;
+    while (ranks < kGatedMaxCluster && walks * ranks * 2 <= most && ranks * 2 <= tiles) ranks *= 2;
+    return ranks;
+}
+
+tcu_status_t launch_walks(void (*kernel)(GatedParams), const GatedParams &p, uint64_t batch, uint32_t shared, cudaStream_t stream) {
+    if (!ok(cudaFuncSetAttribute(reinterpret_cast<const void *>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, int(shared)))) return TCU_ERR_CUDA;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = p.ranks;
+    attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(uint32_t(batch * p.strips * p.ranks));
+    cfg.blockDim = dim3(kGatedWarps * 32);
+    cfg.dynamicSmemBytes = shared;
+    cfg.stream = stream;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return ok(cudaLaunchKernelEx(&cfg, kernel, p)) ? TCU_OK : TCU_ERR_CUDA;
 }
 
 }  // namespace
@@ -118,7 +148,7 @@ void dispatch(const tcu_gated_t *a, bool pairs, F go) {
 extern "C" {
 
 size_t tcu_gated_marks_bytes(uint64_t batch, uint64_t tokens, uint32_t channels) {
-    const unsigned __int128 bytes = ((unsigned __int128)(tokens / kGatedTile) + batch) * channels * 4;
+    const unsigned __int128 bytes = ((unsigned __int128)(tokens / kGatedMark) + batch) * channels * 4;
     return bytes >> 63 ? 0 : size_t(bytes);
 }
 
@@ -140,11 +170,18 @@ tcu_status_t tcu_gated_forward(const tcu_gated_t *a, cudaStream_t stream) {
             if (meet(w, i)) return TCU_ERR_INVALID_ARG;
     if (meet(y, kept) || meet(y, out) || meet(y, in) || meet(kept, out) || meet(kept, in)) return TCU_ERR_INVALID_ARG;
     if (a->d_state_in != a->d_state_out && meet(in, out)) return TCU_ERR_INVALID_ARG;
-    const GatedParams p = params(a);
-    dispatch(a, s.pairs({&a->x, &a->gate, &a->y}), [&](auto t, auto in_gate, auto pair) {
-        tcu_gated_forward_kernel<decltype(t), decltype(in_gate)::value, decltype(pair)::value><<<uint32_t(a->batch * p.strips), kGatedWarps * 32, 0, stream>>>(p);
+    GatedParams p = params(a);
+    tcu_status_t st = TCU_OK;
+    p.ranks = blocks_of_walk(a->batch * p.strips, s);
+    const int way = s.way({&a->x, &a->gate}, {&a->y});
+    dispatch(a, [&](auto t, auto in) {
+        using T = decltype(t);
+        constexpr int kInput = decltype(in)::value, kLast = sizeof(T) == 2 ? 2 : 4;
+        if (way == 0) st = launch_walks(tcu_gated_forward_kernel<T, kInput, 16, true>, p, a->batch, forward_bytes<T, 16>(p.ranks), stream);
+        else if (way == 1) st = launch_walks(tcu_gated_forward_kernel<T, kInput, 4, true>, p, a->batch, forward_bytes<T, 4>(p.ranks), stream);
+        else st = launch_walks(tcu_gated_forward_kernel<T, kInput, kLast, false>, p, a->batch, forward_bytes<T, kLast>(p.ranks), stream);
     });
-    return launched();
+    return st;
 }
 
 tcu_status_t tcu_gated_backward(const tcu_gated_t *a, cudaStream_t stream) {
@@ -169,11 +206,18 @@ tcu_status_t tcu_gated_backward(const tcu_gated_t *a, cudaStream_t stream) {
             if (meet(w, i)) return TCU_ERR_INVALID_ARG;
     if (meet(dx, in) || meet(dg, in) || meet(dx, out) || meet(dg, out)) return TCU_ERR_INVALID_ARG;
     if (a->d_dstate_in != a->d_dstate_out && meet(in, out)) return TCU_ERR_INVALID_ARG;
-    const GatedParams p = params(a);
-    dispatch(a, s.pairs({&a->x, &a->gate, &a->d_y, &a->d_x, &a->d_gate}), [&](auto t, auto in_gate, auto pair) {
-        tcu_gated_backward_kernel<decltype(t), decltype(in_gate)::value, decltype(pair)::value><<<uint32_t(a->batch * p.strips), kGatedWarps * 32, 0, stream>>>(p);
+    GatedParams p = params(a);
+    tcu_status_t st = TCU_OK;
+    p.ranks = blocks_of_walk(a->batch * p.strips, s);
+    const int way = s.way({&a->x, &a->gate, &a->d_y}, {&a->d_x, &a->d_gate});
+    dispatch(a, [&](auto t, auto in) {
+        using T = decltype(t);
+        constexpr int kInput = decltype(in)::value, kLast = sizeof(T) == 2 ? 2 : 4;
+        if (way == 0) st = launch_walks(tcu_gated_backward_kernel<T, kInput, 16, true>, p, a->batch, backward_bytes<T, 16>(p.ranks), stream);
+        else if (way == 1) st = launch_walks(tcu_gated_backward_kernel<T, kInput, 4, true>, p, a->batch, backward_bytes<T, 4>(p.ranks), stream);
+        else st = launch_walks(tcu_gated_backward_kernel<T, kInput, kLast, false>, p, a->batch, backward_bytes<T, kLast>(p.ranks), stream);
     });
-    return launched();
+    return st;
 }
 
 tcu_status_t tcu_gated_step(const tcu_gated_t *a, cudaStream_t stream) {
@@ -193,8 +237,8 @@ tcu_status_t tcu_gated_step(const tcu_gated_t *a, cudaStream_t stream) {
         if (meet(y, s.span(*r)) && !(r->ptr == a->y.ptr && (a->batch == 1 || r->stride_batch == a->y.stride_batch))) return TCU_ERR_INVALID_ARG;
     const GatedParams p = params(a);
     const uint64_t blocks = (a->batch * a->channels + 255) / 256;
-    dispatch(a, false, [&](auto t, auto in_gate, auto) {
-        tcu_gated_step_kernel<decltype(t), decltype(in_gate)::value><<<uint32_t(blocks), 256, 0, stream>>>(p, a->d_slots, a->pool_slots, uint32_t(a->batch));
+    dispatch(a, [&](auto t, auto in) {
+        tcu_gated_step_kernel<decltype(t), decltype(in)::value><<<uint32_t(blocks), 256, 0, stream>>>(p, a->d_slots, a->pool_slots, uint32_t(a->batch));
     });
     return launched();
 }

@@ -3,21 +3,30 @@
 // an inclusive scan over pairs (f, b) with (f, b) before (f', b') giving (f f', f' b + b').  Its gradients are the same scan
 // backward in time: with D_t the gradient with respect to h_t and C_t what flows into it from later tokens,
 //     D_t = dy_t + C_t    C_{t-1} = f_t D_t    dx_t = i_t D_t    dgate_t = D_t (h_{t-1} f_t' + x_t i_t')
-// where h is formed once more from the states that the forward pass leaves every kGatedTile tokens (marks).
+// where h is formed once more from the states that the forward pass leaves every kGatedMark tokens (marks).
 //
-// A block walks a sequence for 64 channels, a tile of kGatedTile tokens at a time: a warp takes kGatedSteps tokens of it, two
-// channels a lane, and scans them in registers; the warps' pairs go through shared memory, and what arrives at a warp from
-// before is added as P_t h (P the product of the f so far): every value is read and written once.
+// A block walks a sequence for 64 channels, a tile of 128 tokens (backward, and for 32-bit elements: 64) at a time: a warp takes 16 (8)
+// tokens of it, two channels a lane, and scans them in registers; the warps' pairs go through shared memory, and what arrives at a warp from
+// before is added as P_t h (P the product of the f so far): every value is read and written once.  Where there are fewer walks than
+// SMs hold blocks, the blocks of a cluster walk a sequence together, a tile each, and tell one another their tiles' pairs.  The order of
+// all sums follows from the sizes alone.
+//
+// What bounds it: instructions (28 an element forward, two of them on the special-function unit; 52 backward) and the barrier of a tile, close behind
+// memory.  8 x 4096 tokens of 2048 bfloat16 channels: forward 84 us (403 MB, 4.8 TB/s, 0.73 of the copy rate), backward 149 us (671 MB, 4.5
+// TB/s).  Tried: values through registers instead of shared memory (215 us, loads wait for the store of the tile before), 8 tokens a warp forward
+// (110), two channels an instruction (no gain: moves into register pairs), a barrier of the block for the tile's arrival (88).
 #pragma once
+
+#include <cooperative_groups.h>
 
 #include "tcu_float.cuh"
 
 namespace tcu {
 
-constexpr int kGatedSteps = 8;                           // tokens of a warp
+constexpr int kGatedMark = 64;             // tokens between marks
 constexpr int kGatedWarps = 8;
-constexpr int kGatedTile = kGatedSteps * kGatedWarps;    // tokens of a tile, and between marks
 constexpr int kGatedChannels = 64;
+constexpr int kGatedMaxCluster = 8;
 
 enum GatedInput { kInputComplement = 0, kInputOne = 1, kInputRoot = 2 };
 
@@ -33,78 +42,100 @@ struct GatedParams {
     float *state_out;
     const float *d_state_out;
     float *d_state_in;
-    float *marks;              // (tokens / kGatedTile + batch, channels): sequence b's begin at row first token / kGatedTile + b
+    float *marks;              // (tokens / kGatedMark + batch, channels): sequence b's begin at row first token / kGatedMark + b
     uint64_t tokens;           // of each sequence (dense), of all together (packed)
     uint32_t channels, strips;
+    uint32_t ranks;            // blocks of a cluster
 };
 
-// The two channels of a lane: one access where they are aligned for it (PAIR), else one each.
+// Stores the two channels of a lane: in one access where they are aligned for it (PAIR), else one each.
 template <typename T, bool PAIR>
-struct Two {
-    Pack<T, 2> raw;
-    __device__ __forceinline__ void load(const T *p, bool first, bool second) {
-        if constexpr (PAIR) {
-            if (first) raw = *reinterpret_cast<const Pack<T, 2> *>(p);
-        } else {
-            if (first) raw.v[0] = p[0];
-            if (second) raw.v[1] = p[1];
-        }
+__device__ __forceinline__ void store_two(T *p, float a, float b, bool first, bool second) {
+    if constexpr (PAIR) {
+        if (first) *reinterpret_cast<Pack<T, 2> *>(p) = Pack<T, 2>{{from_f32<T>(a), from_f32<T>(b)}};
+    } else {
+        if (first) p[0] = from_f32<T>(a);
+        if (second) p[1] = from_f32<T>(b);
     }
-    static __device__ __forceinline__ void store(T *p, float a, float b, bool first, bool second) {
-        if constexpr (PAIR) {
-            if (first) *reinterpret_cast<Pack<T, 2> *>(p) = Pack<T, 2>{{from_f32<T>(a), from_f32<T>(b)}};
-        } else {
-            if (first) p[0] = from_f32<T>(a);
-            if (second) p[1] = from_f32<T>(b);
-        }
-    }
-    __device__ __forceinline__ float get(int c) const { return to_f32<T>(raw.v[c]); }
-};
+}
 
-// exp(-|g|) to a few 2^-23 of itself: 2^t for the rounded product t of -|g| and log2(e), and to first order what the rounding and the
-// second half of log2(e) leave.
-__device__ __forceinline__ float exp_minus(float g) {
-    constexpr double kLog2e = 1.4426950408889634;
-    constexpr float kHigh = float(kLog2e), kLow = float(kLog2e - double(kHigh));
-    const float u = -fminf(fabsf(g), 200.0f);            // (below 2^-150 either way; infinities would leave inf - inf)
-    const float t = u * kHigh, left = fmaf(u, kLow, fmaf(u, kHigh, -t));
-    float a;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(a) : "f"(t));
-    return fmaf(a, left * 0.69314718f, a);
+// Arithmetic on the two channels of a lane.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) { return make_float2(fmaf(a.x, b.x, c.x), fmaf(a.y, b.y, c.y)); }
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) { return make_float2(a.x * b.x, a.y * b.y); }
+__device__ __forceinline__ float2 add2(float2 a, float2 b) { return make_float2(a.x + b.x, a.y + b.y); }
+__device__ __forceinline__ float2 both(float v) { return make_float2(v, v); }
+__device__ __forceinline__ float reciprocal(float v) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ float minus_size(float g) {              // -|g|, at least -200: exp is 0 from -104 on, and infinities would leave inf - inf
+    float u;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(u) : "f"(-fabsf(g)), "f"(-200.0f));
+    return u;
 }
 
 // f = sigmoid(g) and 1 - f.  The smaller of the two is a / (1 + a), a = exp(-|g|), to a few 2^-23 of itself, the larger one less it:
-// f of a channel with a long memory is off by its rounding alone.
-__device__ __forceinline__ void sigmoids(float g, float &f, float &rest) {
-    const float a = exp_minus(g);
-    const float less = __fdividef(a, 1.0f + a), more = 1.0f - less;
-    const bool keep = g >= 0.0f;
-    f = keep ? more : less;
-    rest = keep ? less : more;
-    if (g != g) f = rest = g;                            // (fminf drops a NaN)
+// f of a channel with a long memory is off by its rounding alone.  a is 2^t for the rounded product t of -|g| and log2(e); where
+// the inputs have 32 bits, what the rounding leaves, -|g| - t ln 2, is added to first order.  (Without it a is off by |t| 2^-25 of itself.)
+template <bool FINE>
+__device__ __forceinline__ void sigmoids(float2 g, float2 &f, float2 &rest) {
+    float2 u, t;
+    if constexpr (FINE) {
+        u = make_float2(minus_size(g.x), minus_size(g.y));
+        t = mul2(u, both(1.4426950408889634f));
+    } else {
+        t = make_float2(fabsf(g.x) * -1.4426950408889634f, fabsf(g.y) * -1.4426950408889634f);
+    }
+    float2 a;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(a.x) : "f"(t.x));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(a.y) : "f"(t.y));
+    if constexpr (FINE) a = fma2(a, fma2(t, both(-0.6931471805599453f), u), a);
+    const float2 sum = make_float2(1.0f + a.x, 1.0f + a.y);
+    const float2 less = mul2(a, make_float2(reciprocal(sum.x), reciprocal(sum.y))), more = make_float2(1.0f - less.x, 1.0f - less.y);
+    f = make_float2(g.x >= 0.0f ? more.x : less.x, g.y >= 0.0f ? more.y : less.y);
+    rest = make_float2(g.x >= 0.0f ? less.x : more.x, g.y >= 0.0f ? less.y : more.y);
 }
 
 template <int INPUT>
-__device__ __forceinline__ float input_of(float f, float rest) {
+__device__ __forceinline__ float2 input_of(float2 f, float2 rest) {
     if constexpr (INPUT == kInputComplement) return rest;
-    if constexpr (INPUT == kInputOne) return 1.0f;
-    float i;
-    asm("sqrt.approx.f32 %0, %1;" : "=f"(i) : "f"(rest * (1.0f + f)));
+    if constexpr (INPUT == kInputOne) return both(1.0f);
+    const float2 square = fma2(rest, f, rest);
+    float2 i;
+    asm("sqrt.approx.f32 %0, %1;" : "=f"(i.x) : "f"(square.x));
+    asm("sqrt.approx.f32 %0, %1;" : "=f"(i.y) : "f"(square.y));
     return i;
 }
-
-// Derivative of the input's factor by the gate.
 template <int INPUT>
-__device__ __forceinline__ float input_slope(float f, float rest, float i) {
-    if constexpr (INPUT == kInputComplement) return -f * rest;
-    if constexpr (INPUT == kInputOne) return 0.0f;
-    return -f * f * __fdividef(i, 1.0f + f);
+__device__ __forceinline__ float2 taken_in(float2 f, float2 rest, float2 x) {
+    if constexpr (INPUT == kInputOne) return x;
+    else return mul2(input_of<INPUT>(f, rest), x);
+}
+
+// The gate's gradient over that of h, h_{t-1} f' + x i', from what has been taken in, i x: f' = f (1 - f), and i' is -f (1 - f), 0 or
+// -f^2 i / (1 + f).
+template <int INPUT>
+__device__ __forceinline__ float2 gate_slope(float2 f, float2 rest, float2 before, float2 in) {
+    if constexpr (INPUT == kInputComplement) return mul2(f, fma2(rest, before, make_float2(-in.x, -in.y)));
+    if constexpr (INPUT == kInputOne) return mul2(f, mul2(rest, before));
+    const float2 more = make_float2(f.x * reciprocal(1.0f + f.x), f.y * reciprocal(1.0f + f.y));
+    return mul2(f, fma2(rest, before, mul2(more, make_float2(-in.x, -in.y))));
+}
+
+// One token of one channel.
+template <int INPUT>
+__device__ __forceinline__ float next_state(float g, float x, float h) {
+    float2 f, rest;
+    sigmoids<true>(both(g), f, rest);
+    return fmaf(f.x, h, taken_in<INPUT>(f, rest, both(x)).x);
 }
 
 // One block's place: sequence, channels, tokens.
 struct GatedWalk {
     uint32_t seq, c0;
-    int64_t begin, len;        // of the sequence, in rows of the arrays (packed) or of its own (dense: begin 0)
+    int64_t begin;             // of the sequence, in rows of the arrays (dense: 0)
+    int len;
     uint64_t mark;             // row of its first mark
     __device__ __forceinline__ GatedWalk(const GatedParams &p, uint32_t walk) {
         seq = walk / p.strips;
@@ -112,12 +143,12 @@ struct GatedWalk {
         if (p.offsets) {
             // offsets that are not as they should be may give wrong results, but no access outside the arrays
             begin = min(max(p.offsets[seq], int64_t(0)), int64_t(p.tokens));
-            len = min(max(p.offsets[seq + 1], begin), int64_t(p.tokens)) - begin;
-            mark = uint64_t(begin) / kGatedTile + seq;
+            len = int(min(max(p.offsets[seq + 1], begin), int64_t(p.tokens)) - begin);
+            mark = uint64_t(begin) / kGatedMark + seq;
         } else {
             begin = 0;
-            len = int64_t(p.tokens);
-            mark = uint64_t(seq) * p.tokens / kGatedTile + seq;
+            len = int(p.tokens);
+            mark = uint64_t(seq) * p.tokens / kGatedMark + seq;
         }
     }
     template <typename T>
@@ -126,167 +157,357 @@ struct GatedWalk {
     }
 };
 
-template <typename T, int INPUT, bool PAIR>
-__global__ void __launch_bounds__(kGatedWarps * 32) tcu_gated_forward_kernel(const GatedParams p) {
-    __shared__ float4 pairs[2][kGatedWarps][32];
-    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const GatedWalk w(p, blockIdx.x);
-    const uint32_t c = w.c0 + 2 * lane;
-    const bool c0 = c < p.channels, c1 = c + 1 < p.channels;
-    const T *px = w.at<T>(p, p.x, c), *pg = w.at<T>(p, p.gate, c);
-    T *py = p.y.ptr ? w.at<T>(p, p.y, c) : nullptr;
-    float h[2] = {0.0f, 0.0f};
-    const uint64_t st = uint64_t(w.seq) * p.channels + c;
-    if (p.state_in) {
-        if (c0) h[0] = p.state_in[st];
-        if (c1) h[1] = p.state_in[st + 1];
+// Rows of the inputs on their way to shared memory.  A warp copies what it reads itself, so that no barrier of the block waits for data.
+// COPY bytes an access, 16 or 4 where all rows begin at multiples of them.  COPY 2: rows of 16-bit elements that begin anywhere are copied in the aligned
+// words that hold them (a word that holds an element lies in the same allocation), and shifted by one element, where a row begins in
+// the middle of a word, when they are read.
+__device__ __forceinline__ void copy_async4(void *to, const void *from) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(uint32_t(__cvta_generic_to_shared(to))), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copy_async16(void *to, const void *from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(uint32_t(__cvta_generic_to_shared(to))), "l"(from) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void copies_but(void) {                  // waits for all but the last N commits of this thread
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void commit_copies() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+
+template <typename T, int STEPS, int COPY>
+struct alignas(16) GatedRowsOf {           // of a warp
+    T v[STEPS][kGatedChannels + (COPY == 2 ? 2 : 0)];
+};
+
+// One array's rows, those of a tile after those of another.  Rows that are not there, and channels, are left as they are.
+template <typename T, int STEPS, int COPY>
+struct GatedSource {
+    static constexpr int kEach = COPY == 2 ? 2 : COPY / int(sizeof(T));        // elements of a piece
+    static constexpr int kRow = kGatedChannels / kEach;                        // pieces of a row
+    static constexpr int kRows = kRow < 32 ? 32 / kRow : 1, kCols = kRow < 32 ? 1 : kRow / 32;         // rows of an access, accesses of a row
+    const T *at;                           // row of this lane's first piece of the next tile
+    int64_t stride, step;                  // a row to the next one, a tile to the next one (in elements)
+    __device__ __forceinline__ GatedSource(const T *array, int first, int64_t stride, int tokens_on) : stride(stride) {
+        at = array + (int64_t(first) + row()) * stride;
+        step = tokens_on * stride;
     }
-    uint32_t buf = 0;
-    for (int64_t t0 = 0; t0 < w.len; t0 += kGatedTile, buf ^= 1) {
-        const int64_t t = t0 + warp * kGatedSteps;
-        const int n = int(min(int64_t(kGatedSteps), w.len - t));          // tokens of this warp, or none
-        Two<T, PAIR> x[kGatedSteps], g[kGatedSteps];
+    static __device__ __forceinline__ int row() { return kRows == 1 ? 0 : int((threadIdx.x & 31) / kRow); }
+    // How many elements the row of token s of a tile that begins with `row` lies behind the word that it begins in.
+    static __device__ __forceinline__ uint32_t shift(const T *row, int64_t stride, int s) {
+        return COPY == 2 ? uint32_t((reinterpret_cast<uintptr_t>(row) / sizeof(T) + uint64_t(stride) * s) & 1) : 0;
+    }
+    template <bool ALL>
+    __device__ __forceinline__ void copy(GatedRowsOf<T, STEPS, COPY> &rows, int n, int channels) {
+        const uint32_t lane = threadIdx.x & 31;
+        const T *src = at;
 #pragma unroll
-        for (int s = 0; s < kGatedSteps; ++s) {
-            x[s].load(px + (t + s) * p.x.token, s < n && c0, s < n && c1);
-            g[s].load(pg + (t + s) * p.gate.token, s < n && c0, s < n && c1);
-        }
-        if (p.marks && warp == 0) {
-            float *m = p.marks + (w.mark + uint64_t(t0) / kGatedTile) * p.channels + c;
-            if (c0) m[0] = h[0];
-            if (c1) m[1] = h[1];
-        }
-        float prod[kGatedSteps][2], local[kGatedSteps][2], a[2] = {1.0f, 1.0f}, b[2] = {0.0f, 0.0f};
+        for (int k = 0; k < STEPS; k += kRows, src += stride * kRows) {
+            if constexpr (COPY == 2) {
+                const int off = int(shift(src, 0, 0));
+                if ((ALL || k < n) && 2 * int(lane) - off < channels) copy_async4(&rows.v[k][2 * lane], src + (2 * int(lane) - off));
+            } else {
 #pragma unroll
-        for (int s = 0; s < kGatedSteps; ++s) {
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                if (s < n) {
-                    float f, rest;
-                    sigmoids(g[s].get(e), f, rest);
-                    a[e] *= f;
-                    b[e] = f * b[e] + input_of<INPUT>(f, rest) * x[s].get(e);
+                for (int j = 0; j < kCols; ++j) {
+                    const int c = (lane % kRow + j * 32) * kEach;
+                    if ((ALL || row() + k < n) && c < channels) {
+                        if constexpr (COPY == 16) copy_async16(&rows.v[row() + k][c], src + c);
+                        else copy_async4(&rows.v[row() + k][c], src + c);
+                    }
                 }
-                prod[s][e] = a[e];
-                local[s][e] = b[e];
             }
         }
-        pairs[buf][warp][lane] = make_float4(a[0], b[0], a[1], b[1]);
-        __syncthreads();
-        float mine[2] = {h[0], h[1]};
-#pragma unroll
-        for (uint32_t k = 0; k < kGatedWarps; ++k) {
-            const float4 q = pairs[buf][k][lane];
-            if (k == warp) mine[0] = h[0], mine[1] = h[1];
-            h[0] = q.x * h[0] + q.y;
-            h[1] = q.z * h[1] + q.w;
-        }
-        if (py) {
-#pragma unroll
-            for (int s = 0; s < kGatedSteps; ++s)
-                Two<T, PAIR>::store(py + (t + s) * p.y.token, prod[s][0] * mine[0] + local[s][0], prod[s][1] * mine[1] + local[s][1], s < n && c0, s < n && c1);
+        if constexpr (COPY == 2) {         // the 33rd words, lane s that of row s
+            if (int(lane) < min(n, STEPS) && channels == kGatedChannels && shift(at, stride, lane)) copy_async4(&rows.v[lane][kGatedChannels], at + stride * lane + (kGatedChannels - 1));
         }
     }
-    if (p.state_out && warp == 0) {
-        if (c0) p.state_out[st] = h[0];
-        if (c1) p.state_out[st + 1] = h[1];
+    // the first n rows are there, and `channels`
+    __device__ __forceinline__ void load(GatedRowsOf<T, STEPS, COPY> &rows, int n, int channels) {
+        if (n >= STEPS) copy<true>(rows, n, channels);
+        else copy<false>(rows, n, channels);
+        at += step;
+    }
+};
+
+// Two channels of a token of a warp, whose row is `shift` elements behind a word.
+template <typename T, int STEPS, int COPY>
+__device__ __forceinline__ float2 pair_of(const GatedRowsOf<T, STEPS, COPY> &rows, int s, uint32_t shift) {
+    const uint32_t lane = threadIdx.x & 31;
+    Pack<T, 2> v;
+    if constexpr (COPY == 2) {
+        const uint32_t *words = reinterpret_cast<const uint32_t *>(&rows.v[s][2 * lane]);
+        const uint32_t both = __funnelshift_r(words[0], words[1], shift * 16);
+        v = *reinterpret_cast<const Pack<T, 2> *>(&both);
+    } else {
+        v = *reinterpret_cast<const Pack<T, 2> *>(&rows.v[s][2 * lane]);
+    }
+    return make_float2(to_f32<T>(v.v[0]), to_f32<T>(v.v[1]));
+}
+
+// Sets the rows from n on to a value.  What the tokens that are not there look like: a gate of infinity, f = 1, and zeros, nothing that comes in,
+// so that states and gradients pass them as they are.
+template <typename T, int STEPS, int COPY>
+__device__ __forceinline__ void fill_rows(GatedRowsOf<T, STEPS, COPY> &rows, int n, float value) {
+    const uint32_t lane = threadIdx.x & 31;
+    for (int s = max(n, 0); s < STEPS; ++s)
+        for (uint32_t c = lane; c < sizeof(rows.v[0]) / sizeof(T); c += 32) rows.v[s][c] = from_f32<T>(value);
+    __syncwarp();
+}
+
+template <typename T, bool PAIR, int STEPS>
+__device__ __forceinline__ void store_rows(T *at, int64_t stride, int n, bool c0, bool c1, const float2 (&v)[STEPS]) {
+    if (n >= STEPS) {
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s, at += stride) store_two<T, PAIR>(at, v[s].x, v[s].y, c0, c1);
+    } else {
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s, at += stride) store_two<T, PAIR>(at, v[s].x, v[s].y, s < n && c0, s < n && c1);
     }
 }
 
-template <typename T, int INPUT, bool PAIR>
-__global__ void __launch_bounds__(kGatedWarps * 32) tcu_gated_backward_kernel(const GatedParams p) {
-    __shared__ float4 ahead[2][kGatedWarps][32], back[2][kGatedWarps][32];
-    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const GatedWalk w(p, blockIdx.x);
+// The pairs of a lane's two channels: (f, f', b, b').
+__device__ __forceinline__ float4 pairs_of(float2 f, float2 b) { return make_float4(f.x, f.y, b.x, b.y); }
+__device__ __forceinline__ float2 apply(const float4 &q, float2 h) { return fma2(make_float2(q.x, q.y), h, make_float2(q.z, q.w)); }
+__device__ __forceinline__ float4 after(const float4 &q, const float4 &before) {
+    return pairs_of(mul2(make_float2(q.x, q.y), make_float2(before.x, before.y)), apply(q, make_float2(before.z, before.w)));
+}
+
+// Where the pairs of a tile's warps, and of the tiles that the blocks of a cluster walk at the same time, meet.  There are two sets of
+// each, used in turn: who writes one again has met everybody that read it at the barrier of the other.
+struct GatedMeeting {
+    float4 warps[2][kGatedWarps][32];
+    float4 tiles[][2][32];                         // (ranks, 2, 32)
+};
+
+// From what comes into the tiles of all blocks (`carry`, replaced by what leaves them) what comes into this warp's tokens.  In walking order, which is the order of tokens or (BACK) its reverse.
+template <bool BACK>
+__device__ __forceinline__ float2 meet(GatedMeeting &m, uint32_t buf, const float4 &own, uint32_t rank, uint32_t ranks, float2 &carry) {
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31, place = BACK ? kGatedWarps - 1 - warp : warp;
+    m.warps[buf][place][lane] = own;
+    __syncthreads();
+    float2 mine;
+    if (ranks == 1) {
+        mine = carry;
+#pragma unroll
+        for (uint32_t k = 0; k < kGatedWarps; ++k) {
+            const float4 q = m.warps[buf][k][lane];
+            if (k < place) mine = apply(q, mine);
+            carry = apply(q, carry);
+        }
+        return mine;
+    }
+    auto cluster = cooperative_groups::this_cluster();
+    if (warp == 0) {                               // what the warps ahead add up to, and the whole tile, for all blocks
+        float4 sum = make_float4(1.0f, 1.0f, 0.0f, 0.0f);
+#pragma unroll
+        for (uint32_t k = 0; k < kGatedWarps; ++k) {
+            const float4 q = m.warps[buf][k][lane];
+            m.warps[buf][k][lane] = sum;
+            sum = after(q, sum);
+        }
+#pragma unroll 4
+        for (uint32_t k = 0; k < ranks; ++k) cluster.map_shared_rank(&m, k)->tiles[rank][buf][lane] = sum;
+        asm volatile("fence.acq_rel.cluster;" ::: "memory");      // (for what this warp has told, and the block has read: the others need none)
+    }
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    float2 at_tile = carry;
+#pragma unroll 4
+    for (uint32_t k = 0; k < ranks; ++k) {
+        if (k == rank) at_tile = carry;
+        carry = apply(m.tiles[k][buf][lane], carry);
+    }
+    return apply(m.warps[buf][place][lane], at_tile);
+}
+
+constexpr uint32_t kForwardStages = 3, kBackwardStages = 2;
+template <typename T>
+constexpr int kForwardSteps = sizeof(T) == 2 ? 16 : 8;                  // tokens of a warp
+constexpr int kBackwardSteps = 8;
+template <typename T, int COPY>
+constexpr uint32_t forward_bytes(uint32_t ranks) {
+    return kForwardStages * 2 * kGatedWarps * sizeof(GatedRowsOf<T, kForwardSteps<T>, COPY>) + sizeof(float4) * 32 * (2 * kGatedWarps + (ranks > 1 ? 2 * ranks : 0));
+}
+template <typename T, int COPY>
+constexpr uint32_t backward_bytes(uint32_t ranks) {
+    return kBackwardStages * 3 * kGatedWarps * sizeof(GatedRowsOf<T, kBackwardSteps, COPY>) + sizeof(float4) * 32 * (4 * kGatedWarps + (ranks > 1 ? 2 * ranks : 0));
+}
+
+// Blocks of a cluster walk a sequence together, block r tile r of every `ranks` tiles.
+template <typename T, int INPUT, int COPY, bool PAIR>
+__global__ void __launch_bounds__(kGatedWarps * 32, sizeof(T) == 2 ? 2 : 3) tcu_gated_forward_kernel(const GatedParams p) {
+    constexpr int STEPS = kForwardSteps<T>, TILE = STEPS * kGatedWarps;
+    static_assert(TILE % kGatedMark == 0 && kGatedMark % STEPS == 0, "marks lie where a warp begins");
+    extern __shared__ __align__(16) uint8_t shared[];
+    using Stage = GatedRowsOf<T, STEPS, COPY>[kGatedWarps];
+    using Source = GatedSource<T, STEPS, COPY>;
+    Stage *xs = reinterpret_cast<Stage *>(shared), *gs = xs + kForwardStages;
+    GatedMeeting &meeting = *reinterpret_cast<GatedMeeting *>(gs + kForwardStages);
+    const int warp = threadIdx.x >> 5;
+    const uint32_t lane = threadIdx.x & 31, rank = blockIdx.x % p.ranks;
+    const GatedWalk w(p, blockIdx.x / p.ranks);
     const uint32_t c = w.c0 + 2 * lane;
+    const int wide = int(min(p.channels - w.c0, uint32_t(kGatedChannels)));
     const bool c0 = c < p.channels, c1 = c + 1 < p.channels;
-    const T *px = w.at<T>(p, p.x, c), *pg = w.at<T>(p, p.gate, c), *pd = w.at<T>(p, p.d_y, c);
-    T *pdx = w.at<T>(p, p.d_x, c), *pdg = w.at<T>(p, p.d_gate, c);
-    float flow[2] = {0.0f, 0.0f};                                          // C at the end of the tile
+    const T *px = w.at<T>(p, p.x, w.c0), *pg = w.at<T>(p, p.gate, w.c0);
+    float2 carry = make_float2(0.0f, 0.0f);
+    const uint64_t st = uint64_t(w.seq) * p.channels + c;
+    if (p.state_in) {
+        if (c0) carry.x = p.state_in[st];
+        if (c1) carry.y = p.state_in[st + 1];
+    }
+    const int stride = int(p.ranks) * TILE;
+    int t = int(rank) * TILE + warp * STEPS;                       // first token of this warp
+    Source from_x(px, t, p.x.token, stride), from_g(pg, t, p.gate.token, stride);
+    auto fetch = [&](uint32_t stage, int at) {
+        if (at < w.len) {
+            from_x.load(xs[stage][warp], w.len - at, wide);
+            from_g.load(gs[stage][warp], w.len - at, wide);
+        }
+        commit_copies();
+    };
+    fetch(0, t);
+    fetch(1, t + stride);
+    T *py = w.at<T>(p, p.y, c) + t * p.y.token;
+    uint32_t buf = 0, stage = 0;
+    for (int done = 0; done < w.len; done += stride, t += stride, buf ^= 1) {
+        copies_but<1>();
+        __syncwarp();                                              // the rows are here, and the ones before have been read
+        fetch(stage == 0 ? 2 : stage - 1, t + 2 * stride);
+        const int n = w.len - t;                                   // tokens of this warp, if it has so many
+        const bool here = n > 0;
+        float2 prod[STEPS], local[STEPS], a = both(1.0f), b = both(0.0f);
+        if (here) {
+            if (n < STEPS) {
+                fill_rows(xs[stage][warp], n, 0.0f);
+                fill_rows(gs[stage][warp], n, INFINITY);
+            }
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s) {
+                const float2 x = pair_of(xs[stage][warp], s, Source::shift(px + t * p.x.token, p.x.token, s));
+                const float2 g = pair_of(gs[stage][warp], s, Source::shift(pg + t * p.gate.token, p.gate.token, s));
+                float2 f, rest;
+                sigmoids<sizeof(T) == 4>(g, f, rest);
+                a = mul2(a, f);
+                b = fma2(f, b, taken_in<INPUT>(f, rest, x));
+                prod[s] = a;
+                local[s] = b;
+            }
+        }
+        const float2 mine = meet<false>(meeting, buf, pairs_of(a, b), rank, p.ranks, carry);
+        if (here) {
+            if (p.marks && warp * STEPS % kGatedMark == 0) {
+                float *m = p.marks + (w.mark + uint32_t(t) / kGatedMark) * p.channels + c;
+                if (c0) m[0] = mine.x;
+                if (c1) m[1] = mine.y;
+            }
+            if (p.y.ptr) {
+#pragma unroll
+                for (int s = 0; s < STEPS; ++s) local[s] = fma2(prod[s], mine, local[s]);
+                store_rows<T, PAIR, STEPS>(py, p.y.token, n, c0, c1, local);
+            }
+        }
+        py += stride * p.y.token;
+        stage = stage == 2 ? 0 : stage + 1;
+    }
+    if (p.ranks > 1) cooperative_groups::this_cluster().sync();           // (nobody leaves, or writes the state, before all have read)
+    if (p.state_out && warp == 0 && rank == 0) {
+        if (c0) p.state_out[st] = carry.x;
+        if (c1) p.state_out[st + 1] = carry.y;
+    }
+}
+
+template <typename T, int INPUT, int COPY, bool PAIR>
+__global__ void __launch_bounds__(kGatedWarps * 32, 2) tcu_gated_backward_kernel(const GatedParams p) {
+    constexpr int STEPS = kBackwardSteps, TILE = STEPS * kGatedWarps;
+    static_assert(TILE == kGatedMark, "a tile begins with a mark");
+    extern __shared__ __align__(16) uint8_t shared[];
+    using Stage = GatedRowsOf<T, STEPS, COPY>[kGatedWarps];
+    using Source = GatedSource<T, STEPS, COPY>;
+    Stage *xs = reinterpret_cast<Stage *>(shared), *gs = xs + kBackwardStages, *ds = gs + kBackwardStages;
+    auto *ahead = reinterpret_cast<float4(*)[kGatedWarps][32]>(ds + kBackwardStages);
+    GatedMeeting &meeting = *reinterpret_cast<GatedMeeting *>(ahead + 2);
+    const int warp = threadIdx.x >> 5;
+    const uint32_t lane = threadIdx.x & 31, rank = blockIdx.x % p.ranks;
+    const GatedWalk w(p, blockIdx.x / p.ranks);
+    const uint32_t c = w.c0 + 2 * lane;
+    const int wide = int(min(p.channels - w.c0, uint32_t(kGatedChannels)));
+    const bool c0 = c < p.channels, c1 = c + 1 < p.channels;
+    const T *px = w.at<T>(p, p.x, w.c0), *pg = w.at<T>(p, p.gate, w.c0), *pd = w.at<T>(p, p.d_y, w.c0);
+    float2 flow = make_float2(0.0f, 0.0f);                                 // C at the end of the blocks' tiles
     const uint64_t st = uint64_t(w.seq) * p.channels + c;
     if (p.d_state_out) {
-        if (c0) flow[0] = p.d_state_out[st];
-        if (c1) flow[1] = p.d_state_out[st + 1];
+        if (c0) flow.x = p.d_state_out[st];
+        if (c1) flow.y = p.d_state_out[st + 1];
     }
+    const int tiles = (w.len + TILE - 1) / TILE, stride = int(p.ranks) * TILE;
+    int t = (tiles - 1 - int(rank)) * TILE + warp * STEPS;   // first token of this warp; below 0: there is none
+    Source from_x(px, t, p.x.token, -stride), from_g(pg, t, p.gate.token, -stride), from_d(pd, t, p.d_y.token, -stride);
+    float2 mark = both(0.0f);                                // the state that the tile begins with
+    auto fetch = [&](uint32_t stage, int at) {
+        if (at >= 0) {
+            from_x.load(xs[stage][warp], w.len - at, wide);
+            from_g.load(gs[stage][warp], w.len - at, wide);
+            from_d.load(ds[stage][warp], w.len - at, wide);
+            const float *m = p.marks + (w.mark + uint32_t(at) / kGatedMark) * p.channels + c;
+            if (c0) mark.x = m[0];
+            if (c1) mark.y = m[1];
+        }
+        commit_copies();
+    };
+    fetch(0, t);
+    T *pdx = w.at<T>(p, p.d_x, c) + t * p.d_x.token, *pdg = w.at<T>(p, p.d_gate, c) + t * p.d_gate.token;
     uint32_t buf = 0;
-    const int64_t tiles = (w.len + kGatedTile - 1) / kGatedTile;
-    for (int64_t tile = tiles - 1; tile >= 0; --tile, buf ^= 1) {
-        const int64_t t = tile * kGatedTile + warp * kGatedSteps;
-        const int n = int(min(int64_t(kGatedSteps), w.len - t));
-        Two<T, PAIR> x[kGatedSteps], g[kGatedSteps], d[kGatedSteps];
+    for (int done = 0; done < tiles; done += int(p.ranks), t -= stride, buf ^= 1) {
+        copies_but<0>();
+        __syncwarp();
+        float2 h = mark;
+        fetch(buf ^ 1, t - stride);
+        const int n = w.len - t;                             // tokens of this warp, if it has so many
+        const bool here = t >= 0;
+        float2 f[STEPS], rest[STEPS], in[STEPS], a = both(1.0f), b = both(0.0f), r = both(0.0f);
+        if (here) {
+            if (n < STEPS) {
+                fill_rows(xs[buf][warp], n, 0.0f);
+                fill_rows(gs[buf][warp], n, INFINITY);
+                fill_rows(ds[buf][warp], n, 0.0f);
+            }
 #pragma unroll
-        for (int s = 0; s < kGatedSteps; ++s) {
-            x[s].load(px + (t + s) * p.x.token, s < n && c0, s < n && c1);
-            g[s].load(pg + (t + s) * p.gate.token, s < n && c0, s < n && c1);
-            d[s].load(pd + (t + s) * p.d_y.token, s < n && c0, s < n && c1);
-        }
-        float h[2] = {0.0f, 0.0f};
-        const float *m = p.marks + (w.mark + tile) * p.channels + c;
-        if (c0) h[0] = m[0];
-        if (c1) h[1] = m[1];
-        float f[kGatedSteps][2], rest[kGatedSteps][2], a[2] = {1.0f, 1.0f}, b[2] = {0.0f, 0.0f}, r[2] = {0.0f, 0.0f};
-#pragma unroll
-        for (int s = 0; s < kGatedSteps; ++s) {
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                if (s < n) {
-                    sigmoids(g[s].get(e), f[s][e], rest[s][e]);
-                    a[e] *= f[s][e];
-                    b[e] = f[s][e] * b[e] + input_of<INPUT>(f[s][e], rest[s][e]) * x[s].get(e);
-                }
+            for (int s = 0; s < STEPS; ++s) {
+                sigmoids<sizeof(T) == 4>(pair_of(gs[buf][warp], s, Source::shift(pg + t * p.gate.token, p.gate.token, s)), f[s], rest[s]);
+                in[s] = taken_in<INPUT>(f[s], rest[s], pair_of(xs[buf][warp], s, Source::shift(px + t * p.x.token, p.x.token, s)));
+                a = mul2(a, f[s]);
+                b = fma2(f[s], b, in[s]);
+                r = fma2(a, pair_of(ds[buf][warp], s, Source::shift(pd + t * p.d_y.token, p.d_y.token, s)), r);       // of d_t flows back to the first token: d_t times all f up to its own
             }
         }
+        ahead[buf][warp][lane] = pairs_of(a, b);
+        float2 out = meet<true>(meeting, buf, pairs_of(a, r), rank, p.ranks, flow);
+        if (here) {
 #pragma unroll
-        for (int s = kGatedSteps - 1; s >= 0; --s) {
+            for (int k = 0; k < kGatedWarps - 1; ++k)
+                if (k < warp) h = apply(ahead[buf][k][lane], h);
+            float2 before[STEPS];
 #pragma unroll
-            for (int e = 0; e < 2; ++e)
-                if (s < n) r[e] = f[s][e] * (r[e] + d[s].get(e));
-        }
-        ahead[buf][warp][lane] = make_float4(a[0], b[0], a[1], b[1]);
-        back[buf][warp][lane] = make_float4(a[0], r[0], a[1], r[1]);
-        __syncthreads();
-        for (uint32_t k = 0; k < warp; ++k) {
-            const float4 q = ahead[buf][k][lane];
-            h[0] = q.x * h[0] + q.y;
-            h[1] = q.z * h[1] + q.w;
-        }
-        float mine[2] = {flow[0], flow[1]};
-#pragma unroll
-        for (int k = kGatedWarps - 1; k >= 0; --k) {
-            const float4 q = back[buf][k][lane];
-            if (uint32_t(k) == warp) mine[0] = flow[0], mine[1] = flow[1];
-            flow[0] = q.x * flow[0] + q.y;
-            flow[1] = q.z * flow[1] + q.w;
-        }
-        float before[kGatedSteps][2];
-#pragma unroll
-        for (int s = 0; s < kGatedSteps; ++s) {
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                before[s][e] = h[e];
-                if (s < n) h[e] = f[s][e] * h[e] + input_of<INPUT>(f[s][e], rest[s][e]) * x[s].get(e);
+            for (int s = 0; s < STEPS; ++s) {
+                before[s] = h;
+                h = fma2(f[s], h, in[s]);
             }
-        }
 #pragma unroll
-        for (int s = kGatedSteps - 1; s >= 0; --s) {
-            float dx[2], dg[2];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                dx[e] = dg[e] = 0.0f;
-                if (s < n) {
-                    const float grad = d[s].get(e) + mine[e], ff = f[s][e], i = input_of<INPUT>(ff, rest[s][e]);
-                    dx[e] = i * grad;
-                    dg[e] = grad * (before[s][e] * (ff * rest[s][e]) + x[s].get(e) * input_slope<INPUT>(ff, rest[s][e], i));
-                    mine[e] = ff * grad;
-                }
+            for (int s = STEPS - 1; s >= 0; --s) {
+                const float2 grad = add2(pair_of(ds[buf][warp], s, Source::shift(pd + t * p.d_y.token, p.d_y.token, s)), out);
+                out = mul2(f[s], grad);
+                before[s] = mul2(grad, gate_slope<INPUT>(f[s], rest[s], before[s], in[s]));
+                rest[s] = taken_in<INPUT>(f[s], rest[s], grad);
             }
-            Two<T, PAIR>::store(pdx + (t + s) * p.d_x.token, dx[0], dx[1], s < n && c0, s < n && c1);
-            Two<T, PAIR>::store(pdg + (t + s) * p.d_gate.token, dg[0], dg[1], s < n && c0, s < n && c1);
+            store_rows<T, PAIR, STEPS>(pdx, p.d_x.token, n, c0, c1, rest);
+            store_rows<T, PAIR, STEPS>(pdg, p.d_gate.token, n, c0, c1, before);
         }
+        pdx -= stride * p.d_x.token;
+        pdg -= stride * p.d_gate.token;
     }
-    if (p.d_state_in && warp == 0) {
-        if (c0) p.d_state_in[st] = flow[0];
-        if (c1) p.d_state_in[st + 1] = flow[1];
+    if (p.ranks > 1) cooperative_groups::this_cluster().sync();
+    if (p.d_state_in && warp == 0 && rank == 0) {
+        if (c0) p.d_state_in[st] = flow.x;
+        if (c1) p.d_state_in[st + 1] = flow.y;
     }
 }
 
@@ -304,9 +525,8 @@ __global__ void __launch_bounds__(256) tcu_gated_step_kernel(const GatedParams p
         return;
     }
     float *state = p.state_out + uint64_t(slot) * p.channels + c;
-    float f, rest;
-    sigmoids(to_f32<T>(static_cast<const T *>(p.gate.ptr)[int64_t(seq) * p.gate.batch + c]), f, rest);
-    const float h = f * *state + input_of<INPUT>(f, rest) * to_f32<T>(static_cast<const T *>(p.x.ptr)[int64_t(seq) * p.x.batch + c]);
+    const float g = to_f32<T>(static_cast<const T *>(p.gate.ptr)[int64_t(seq) * p.gate.batch + c]), x = to_f32<T>(static_cast<const T *>(p.x.ptr)[int64_t(seq) * p.x.batch + c]);
+    const float h = next_state<INPUT>(g, x, *state);
     *state = h;
     *y = from_f32<T>(h);
 }

@@ -46,7 +46,7 @@ def test_forward_refusals(B):
     for at in (X, Y, Y + 25536, S0 + 256):
         assert bad(d_marks=at, marks_bytes=need, d_state_in=S0) == B.TCU_ERR_INVALID_ARG
     assert bad(channels=(1 << 30) + 1) == B.TCU_ERR_UNSUPPORTED
-    assert bad(tokens=(1 << 40) + 1) == B.TCU_ERR_UNSUPPORTED
+    assert bad(tokens=(1 << 31) - 8191) == B.TCU_ERR_UNSUPPORTED
     assert bad(batch=1 << 31) == B.TCU_ERR_UNSUPPORTED
     assert bad(batch=1 << 63, channels=1 << 30) == B.TCU_ERR_UNSUPPORTED
     assert B.tcu_gated_marks_bytes(1 << 62, 1 << 40, 1 << 30) == 0
