@@ -202,7 +202,7 @@ tcu_status_t tcu_gated_step(const tcu_gated_t *args, cudaStream_t stream);
  *   d_x        device, rows x d of `type`, row stride x_stride elements (0 to 2^38);  d_y  device, rows x d dense (may be d_x, with x_stride = d)
  *   d_weight, d_bias   device, d values of param_type - fp32, or the same as `type` - or NULL: 1, 0
  * Sums in fp32, values are rounded once.  A row's result depends on its own values alone, and is the same from call to call.
- * TCU_ERR_UNSUPPORTED: d above 32768, rows above 2^40, another param_type. */
+ * TCU_ERR_UNSUPPORTED: d above 16384, rows above 2^31 - 1, another param_type. */
 tcu_status_t tcu_layer_norm_forward(const void *d_x, size_t rows, size_t d, size_t x_stride, tcu_float_t type, const void *d_weight, const void *d_bias,
                                     tcu_float_t param_type, float eps, void *d_y, cudaStream_t stream);
 

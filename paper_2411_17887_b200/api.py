@@ -669,7 +669,7 @@ class _LayerNorm(torch.autograd.Function):
 
 def layer_norm(x, weight=None, bias=None, eps=1e-5):
     """weight * (x - mean) / sqrt(variance + eps) + bias over the last axis of x, rounded once to its type; differentiable, once, in x, weight
-    and bias.  x float32, float16 or bfloat16, of at most 32768 elements along that axis; weight and bias (d,), float32 or of x's type."""
+    and bias.  x float32, float16 or bfloat16, of at most 16384 elements along that axis; weight and bias (d,), float32 or of x's type."""
     if forward_ad._current_level >= 0 or (torch.is_grad_enabled() and (x.requires_grad or (weight is not None and weight.requires_grad) or
                                                                        (bias is not None and bias.requires_grad))):
         return _LayerNorm.apply(x, weight, bias, float(eps))

@@ -14,11 +14,10 @@ namespace {
 
 using namespace tcu;
 
-constexpr uint64_t kMostRows = uint64_t(1) << 40;
+constexpr uint64_t kMostRows = (uint64_t(1) << 31) - 1;
 constexpr uint64_t kMostStride = uint64_t(1) << 38;
-constexpr int kMostHeld = 32;                                        // elements of a row that a thread holds
-constexpr size_t kMostWidth = size_t(kNormMaxThreads) * kMostHeld;
-constexpr uint32_t kSms = 148;
+constexpr size_t kMostWidth = size_t(kNormThreads) * 32;
+constexpr uint32_t kSms = 148, kForwardThreads = 896, kBackwardThreads = 512;       // of an SM, by what registers allow
 
 bool extent(size_t rows, size_t d, size_t stride, size_t eb, size_t &bytes) {
     const unsigned __int128 n = rows == 0 ? 0 : ((unsigned __int128)(rows - 1) * stride + d) * eb;
@@ -26,31 +25,53 @@ bool extent(size_t rows, size_t d, size_t stride, size_t eb, size_t &bytes) {
     return !(n >> 63);
 }
 
-// How a row is divided: elements a thread holds, threads of a row, whether they are a block.
+// How a row is divided: elements a thread holds, lanes of a row (0: a block of `threads`).  Sixteen elements a thread: the steps of a sum cost as much as
+// ten elements (2048 columns, eight a thread: forward 77 us instead of 50); 32 only where a block would have more than 512 threads.
 struct Shape {
-    int vec, held;
+    int vec, held, lanes;
     uint32_t threads;
-    bool block;
+    bool full;                 // every thread has all its elements
     uint64_t blocks;
 };
-Shape shape_of(size_t rows, size_t d, int vec) {
+// (on_sm: threads that an SM holds at once)
+Shape shape_of(size_t rows, size_t d, int vec, uint32_t on_sm) {
     Shape s = {};
     s.vec = vec;
-    s.held = 8;
+    s.held = 16;
     if (d <= 32 * 16) {
-        s.held = d <= 32 * 8 ? 8 : 16;
-        s.threads = 32;
-        s.blocks = (rows + kNormWarpRows - 1) / kNormWarpRows;
-        const uint64_t most = kSms * 8;
+        s.lanes = d <= 8 * 16 ? 8 : d <= 16 * 16 ? 16 : 32;
+        s.threads = kNormWarps * 32;
+        const uint64_t of_block = s.threads / s.lanes, most = kSms * (on_sm / s.threads);
+        s.blocks = (rows + of_block - 1) / of_block;
         if (s.blocks > most) s.blocks = most;
-        return s;
+        s.full = d == size_t(s.lanes) * s.held;
+    } else {
+        s.held = d <= kNormThreads * 16 ? 16 : 32;
+        s.threads = uint32_t((d + size_t(s.held) * 32 - 1) / (size_t(s.held) * 32)) * 32;
+        const uint64_t most = uint64_t(kSms) * (on_sm / s.threads);
+        s.blocks = rows < most ? rows : most;
+        s.full = d == size_t(s.threads) * s.held;
     }
-    while (size_t(kNormMaxThreads) * s.held < d) s.held *= 2;
-    s.block = true;
-    s.threads = uint32_t((d + size_t(s.held) * 32 - 1) / (size_t(s.held) * 32)) * 32;
-    const uint64_t most = uint64_t(kSms) * (1024 / s.threads);
-    s.blocks = rows < most ? rows : most;
     return s;
+}
+// Elements a read: 16 bytes, 4 (two elements of 16 bits), or one element.
+int vector_of(size_t eb, size_t d, std::initializer_list<size_t> strides, std::initializer_list<const void *> arrays) {
+    for (size_t bytes = 16; bytes > eb; bytes = bytes == 16 && eb == 2 ? 4 : eb) {
+        bool fits = d % (bytes / eb) == 0;
+        for (size_t s : strides) fits = fits && s % (bytes / eb) == 0;
+        for (const void *q : arrays) fits = fits && aligned(q, bytes);
+        if (fits) return int(bytes / eb);
+    }
+    return 1;
+}
+
+// Launches a kernel with the rows that its threads have on their way, of `arrays` arrays, in shared memory.
+template <typename K>
+tcu_status_t launch(K kernel, const Shape &s, size_t eb, int arrays, const NormParams &p, cudaStream_t stream) {
+    const size_t shared = s.vec * eb == 16 ? size_t(arrays) * norm_ahead(int(s.held * eb)) * s.threads * s.held * eb : 0;
+    if (shared > 32768 && !ok(cudaFuncSetAttribute(reinterpret_cast<const void *>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, int(shared)))) return TCU_ERR_CUDA;
+    kernel<<<uint32_t(s.blocks), s.threads, shared, stream>>>(p);
+    return launched();
 }
 
 template <typename F>
@@ -60,22 +81,24 @@ void with_type(tcu_float_t type, F go) {
     else go(__nv_bfloat16{});
 }
 
-// Calls go(vector, elements held, block) with these as types.
+// Calls go(vector, elements held, lanes, full) with these as types.
 template <typename T, typename F>
 void with_shape(const Shape &s, F go) {
     constexpr int kVec = 16 / sizeof(T);
-    auto held = [&](auto vec) {
-        if (!s.block) {
-            if (s.held == 8) go(vec, std::integral_constant<int, 8>{}, std::false_type{});
-            else go(vec, std::integral_constant<int, 16>{}, std::false_type{});
-        } else {
-            if (s.held == 8) go(vec, std::integral_constant<int, 8>{}, std::true_type{});
-            else if (s.held == 16) go(vec, std::integral_constant<int, 16>{}, std::true_type{});
-            else go(vec, std::integral_constant<int, 32>{}, std::true_type{});
-        }
+    auto divided = [&](auto vec, auto full) {
+        constexpr std::integral_constant<int, 16> kHeld{};
+        if (s.lanes == 8) go(vec, kHeld, std::integral_constant<int, 8>{}, full);
+        else if (s.lanes == 16) go(vec, kHeld, std::integral_constant<int, 16>{}, full);
+        else if (s.lanes == 32) go(vec, kHeld, std::integral_constant<int, 32>{}, full);
+        else if (s.held == 16) go(vec, kHeld, std::integral_constant<int, 0>{}, full);
+        else go(vec, std::integral_constant<int, 32>{}, std::integral_constant<int, 0>{}, full);
     };
-    if (s.vec > 1) held(std::integral_constant<int, kVec>{});
-    else held(std::integral_constant<int, 1>{});
+    if (s.vec == kVec && s.full) return divided(std::integral_constant<int, kVec>{}, std::true_type{});
+    if (s.vec == kVec) return divided(std::integral_constant<int, kVec>{}, std::false_type{});
+    if constexpr (sizeof(T) == 2) {
+        if (s.vec == 2) return divided(std::integral_constant<int, 2>{}, std::false_type{});
+    }
+    divided(std::integral_constant<int, 1>{}, std::false_type{});
 }
 
 tcu_status_t check(size_t rows, size_t d, tcu_float_t type, tcu_float_t param_type, float eps) {
@@ -87,7 +110,7 @@ tcu_status_t check(size_t rows, size_t d, tcu_float_t type, tcu_float_t param_ty
 
 NormParams params(size_t rows, size_t d, tcu_float_t param_type, float eps) {
     NormParams p = {};
-    p.rows = rows;
+    p.rows = uint32_t(rows);
     p.d = uint32_t(d);
     p.param_f32 = param_type == TCU_F32;
     p.eps = eps;
@@ -110,28 +133,26 @@ tcu_status_t tcu_layer_norm_forward(const void *d_x, size_t rows, size_t d, size
     if (!extent(rows, d, x_stride, eb, xb) || !extent(rows, d, d, eb, yb)) return TCU_ERR_INVALID_ARG;
     const bool in_place = d_x == d_y && (rows == 1 || x_stride == d);          // a row is read whole before it is written
     if ((!in_place && overlaps(d_y, yb, d_x, xb)) || overlaps(d_y, yb, d_weight, d * pb) || overlaps(d_y, yb, d_bias, d * pb)) return TCU_ERR_INVALID_ARG;
-    const int vec = int(16 / eb);
-    const bool wide = d % vec == 0 && (rows == 1 || x_stride % vec == 0) && aligned(d_x, 16) && aligned(d_y, 16);
-    const Shape s = shape_of(rows, d, wide ? vec : 1);
+    const Shape s = shape_of(rows, d, vector_of(eb, d, {rows > 1 ? x_stride : 0}, {d_x, d_y}), kForwardThreads);
     NormParams p = params(rows, d, param_type, eps);
     p.x = d_x;
     p.x_stride = x_stride;
     p.weight = d_weight;
     p.bias = d_bias;
     p.y = d_y;
+    tcu_status_t st = TCU_OK;
     with_type(type, [&](auto t) {
         using T = decltype(t);
-        with_shape<T>(s, [&](auto v, auto e, auto block) {
-            tcu_norm_forward_kernel<T, decltype(v)::value, decltype(e)::value, decltype(block)::value>
-                <<<uint32_t(s.blocks), s.block ? s.threads : kNormWarpRows * 32, 0, stream>>>(p);
+        with_shape<T>(s, [&](auto v, auto e, auto lanes, auto full) {
+            st = launch(tcu_norm_forward_kernel<T, decltype(v)::value, decltype(e)::value, decltype(lanes)::value, decltype(full)::value>, s, eb, 1, p, stream);
         });
     });
-    return launched();
+    return st;
 }
 
 size_t tcu_layer_norm_workspace_bytes(size_t rows, size_t d) {
     if (d == 0 || d > kMostWidth || rows > kMostRows) return 0;
-    return shape_of(rows, d, 1).blocks * 2 * d * 4 + 256;
+    return shape_of(rows, d, 1, kBackwardThreads).blocks * 2 * d * 4 + 256;
 }
 
 tcu_status_t tcu_layer_norm_backward(const void *d_dy, size_t dy_stride, const void *d_x, size_t x_stride, size_t rows, size_t d, tcu_float_t type, const void *d_weight,
@@ -162,9 +183,7 @@ tcu_status_t tcu_layer_norm_backward(const void *d_dy, size_t dy_stride, const v
     for (const void *q : {static_cast<const void *>(d_dweight), static_cast<const void *>(d_dbias)})
         if (overlaps(d_dx, out, q, d * pb) || (sums && overlaps(d_ws, need, q, d * pb))) return TCU_ERR_INVALID_ARG;
     if (sums && overlaps(d_ws, need, d_dx, out)) return TCU_ERR_INVALID_ARG;
-    const int vec = int(16 / eb);
-    const bool wide = d % vec == 0 && (rows == 1 || (x_stride % vec == 0 && dy_stride % vec == 0)) && aligned(d_x, 16) && aligned(d_dy, 16) && aligned(d_dx, 16);
-    const Shape s = shape_of(rows, d, wide ? vec : 1);
+    const Shape s = shape_of(rows, d, vector_of(eb, d, {rows > 1 ? x_stride : 0, rows > 1 ? dy_stride : 0}, {d_x, d_dy, d_dx}), kBackwardThreads);
     NormParams p = params(rows, d, param_type, eps);
     p.x = d_x;
     p.x_stride = x_stride;
@@ -173,19 +192,18 @@ tcu_status_t tcu_layer_norm_backward(const void *d_dy, size_t dy_stride, const v
     p.weight = d_weight;
     p.d_x = d_dx;
     p.parts = sums ? static_cast<float *>(d_ws) : nullptr;
+    tcu_status_t st = TCU_OK;
     with_type(type, [&](auto t) {
         using T = decltype(t);
-        with_shape<T>(s, [&](auto v, auto e, auto block) {
-            tcu_norm_backward_kernel<T, decltype(v)::value, decltype(e)::value, decltype(block)::value>
-                <<<uint32_t(s.blocks), s.block ? s.threads : kNormWarpRows * 32, 0, stream>>>(p);
+        with_shape<T>(s, [&](auto v, auto e, auto lanes, auto full) {
+            st = launch(tcu_norm_backward_kernel<T, decltype(v)::value, decltype(e)::value, decltype(lanes)::value, decltype(full)::value>, s, eb, 2, p, stream);
         });
     });
-    tcu_status_t st = launched();
     if (st != TCU_OK || !sums) return st;
     const uint32_t joins = uint32_t((2 * d + 31) / 32);
     with_type(param_type, [&](auto t) {
         using P = decltype(t);
-        st = launch_next(tcu_norm_join_kernel<P>, joins, 256, stream, p.parts, uint32_t(s.blocks), p.d, static_cast<P *>(d_dweight), static_cast<P *>(d_dbias));
+        st = launch_next(tcu_norm_join_kernel<P>, joins, 1024, stream, p.parts, uint32_t(s.blocks), p.d, static_cast<P *>(d_dweight), static_cast<P *>(d_dbias));
     });
     return st;
 }

@@ -44,7 +44,7 @@ def check(x, d_y, weight, bias, eps=1e-5):
 
 @pytest.mark.parametrize("dtype,param_type", TYPES, ids=str)
 @pytest.mark.parametrize("rows,d", [(1, 1), (3, 2), (7, 64), (9, 255), (33, 256), (5, 257), (100, 501), (17, 512), (6, 513), (40, 1024), (3, 2056), (11, 4097), (2, 8192), (3, 8200),
-                                    (2, 16383), (1, 16384), (2, 20000), (2, 32768)])
+                                    (2, 16383), (1, 16384), (2, 10000), (30, 40), (1000, 128), (65, 130), (77, 8), (5, 12002), (64, 62)])
 def test_sizes(rows, d, dtype, param_type):
     check(*draw(rows, d, dtype, param_type, rows + d))
 
