@@ -17,24 +17,33 @@ constexpr uint64_t kMostRows = ((uint64_t(1) << 31) - 1) / kSampleMaxCluster;
 constexpr uint64_t kMostStride = uint64_t(1) << 38;
 constexpr uint32_t kSms = 148;
 
-// Blocks of a row: as many as hold it in parts of 32 KB, more where that leaves SMs idle and parts of 1024 tokens.
-uint32_t blocks_of(uint64_t rows, uint32_t vocabulary, size_t eb) {
-    uint32_t blocks = 1;
-    while (blocks < kSampleMaxCluster &&
-           (uint64_t(vocabulary) * eb > uint64_t(blocks) * 32768 || (rows * blocks * 2 <= kSms && vocabulary >= blocks * 2 * 1024)))
-        blocks *= 2;
-    return blocks;
+// How a row is divided: 16-byte packs a thread, blocks (a power of two).  As few packs as 8 blocks do with; where that is more blocks than the SMs hold
+// at once, four each, up to eight packs, so that fewer blocks have to meet.
+struct Division {
+    int packs;
+    uint32_t blocks;
+};
+Division divide(uint64_t rows, uint32_t vocabulary, size_t eb) {
+    const uint64_t need = vocabulary + 16 / eb - 1;                    // with what may lie ahead of the row on its first 16 bytes
+    auto packs = [&](uint32_t blocks) {
+        const uint64_t step = uint64_t(blocks) * kSampleThreads * (16 / eb);
+        return int((need + step - 1) / step);
+    };
+    uint32_t blocks = kSampleMaxCluster;
+    while (blocks > 1 && (packs(blocks / 2) == packs(blocks) || (rows * blocks > 4 * kSms && packs(blocks / 2) <= 8))) blocks /= 2;
+    return {packs(blocks), blocks};
 }
 
 template <typename T>
-tcu_status_t launch(const SampleParams &p, uint32_t blocks, size_t shared, uint64_t rows, cudaStream_t stream) {
-    if (!ok(cudaFuncSetAttribute(tcu_sample_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kMostVocabulary / kSampleMaxCluster * sizeof(T) + 256)))) return TCU_ERR_CUDA;
+tcu_status_t launch(const SampleParams &p, const Division &d, uint64_t rows, cudaStream_t stream) {
+    const size_t shared = size_t(d.packs) * kSampleThreads * 16;
+    if (shared > 32768 && !ok(cudaFuncSetAttribute(tcu_sample_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(shared)))) return TCU_ERR_CUDA;
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = blocks;
+    attr.val.clusterDim.x = d.blocks;
     attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(uint32_t(rows * blocks));
+    cfg.gridDim = dim3(uint32_t(rows * d.blocks));
     cfg.blockDim = dim3(kSampleThreads);
     cfg.dynamicSmemBytes = shared;
     cfg.stream = stream;
@@ -81,13 +90,11 @@ tcu_status_t tcu_sample(const tcu_sample_t *a, cudaStream_t stream) {
     p.min_p = {a->d_min_p, a->min_p};
     p.tokens = a->d_tokens;
     p.log_probs = a->d_log_probs;
-    const uint32_t blocks = blocks_of(a->rows, a->vocabulary, eb), vec = uint32_t(16 / eb);
-    // the row and what may lie ahead of it on its first 16 bytes, in parts of whole 16 bytes
-    p.part = ((a->vocabulary + vec - 1 + blocks - 1) / blocks + vec - 1) / vec * vec;
-    const size_t shared = p.part * eb;
-    if (a->type == TCU_F32) return launch<float>(p, blocks, shared, a->rows, stream);
-    if (a->type == TCU_F16) return launch<__half>(p, blocks, shared, a->rows, stream);
-    return launch<__nv_bfloat16>(p, blocks, shared, a->rows, stream);
+    const Division d = divide(a->rows, a->vocabulary, eb);
+    p.packs = d.packs;
+    if (a->type == TCU_F32) return launch<float>(p, d, a->rows, stream);
+    if (a->type == TCU_F16) return launch<__half>(p, d, a->rows, stream);
+    return launch<__nv_bfloat16>(p, d, a->rows, stream);
 }
 
 }  // extern "C"

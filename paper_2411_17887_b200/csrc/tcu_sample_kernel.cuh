@@ -4,25 +4,35 @@
 // prefix of that order, so that it is told by its last logit and how many of the tokens with that one belong to it.  The token
 // drawn is the first, in the order of tokens, up to and with which the kept weights add up to more than u times their sum.
 //
-// A row is read once, into the shared memory of a cluster of blocks, a part each.  The last kept logit is found by histograms: of
-// numbers of tokens for top_k, of weights for top_p - linear in the logit first, then of the logit's bits as an integer, 11 bits a time.
-// Sums that decide which token it is are exact enough that it is the token of the definition: weights in 64-bit floating point, in histograms
+// A row is read once, into the shared memory of a cluster of blocks, a part each: a warp holds consecutive tokens, so that the sums of warps and
+// blocks, which tell each other theirs, are those of ranges of tokens.  Without limits a block's weights are relative to its own largest
+// logit, and the blocks meet once.  The last kept logit is looked for among candidates, up to 256 of which every block sorts for itself: for top_k
+// the tokens from the k-th of the largest logits of 32 ranges a block on (there are k of these at least), or those in the bin that a histogram
+// of numbers names; for top_p those in the bin that a histogram of weights names.  That one is of 32-bit weights, and sums of 64-bit ones say whether the
+// bin is right.  Where a bin has more tokens, exact histograms of the logit's bits as an integer follow, 9 bits a time.
+//
+// Sums that decide which token it is are exact enough that it is the token of the definition: weights in 64-bit floating point, in exact histograms
 // in fixed point with 42 bits (three limbs of 14, each sum of at most 2^18 tokens within 32 bits), whose sums do not depend on their order.
 #pragma once
 
 #include <cooperative_groups.h>
 
+#include <type_traits>
+
 #include "tcu_float.cuh"
 
 namespace tcu {
 
-constexpr int kSampleThreads = 512;
+constexpr int kSampleThreads = 256;
 constexpr int kSampleWarps = kSampleThreads / 32;
-constexpr int kSampleBins = 2048;
+constexpr int kSampleBins = 2048, kSampleFineBits = 9, kSampleFine = 1 << kSampleFineBits;      // of a first histogram, and of those that follow
 constexpr int kSampleMaxCluster = 8;
+constexpr int kSampleList = 256;                      // candidates that are sorted
+constexpr int kSampleRanges = 32;                     // of a block: eight lanes' tokens each
 constexpr uint32_t kMostVocabulary = 1u << 18;
 constexpr double kSampleFixed = 4398046511104.0;      // 2^42
 constexpr int kSampleLimb = 14;
+static_assert(kSampleList == kSampleThreads && kSampleRanges * kSampleMaxCluster <= kSampleList, "a candidate, or a range, each thread");
 
 // A setting of all rows, or one for each.
 template <typename T>
@@ -35,7 +45,8 @@ struct Setting {
 struct SampleParams {
     const void *logits;
     uint64_t stride;
-    uint32_t vocabulary, part;             // tokens of a row, and (a multiple of 16 bytes) of a block
+    uint32_t vocabulary;
+    int packs;                 // 16-byte packs of a thread
     const void *uniform;
     int uniform_f64;
     Setting<float> temperature, top_p, min_p;
@@ -43,6 +54,23 @@ struct SampleParams {
     int64_t *tokens;
     float *log_probs;
 };
+
+// 2^(j/64), by the exponential's series
+struct SampleTable {
+    double v[64];
+    constexpr SampleTable() : v() {
+        for (int j = 0; j < 64; ++j) {
+            const double x = j * (0.69314718055994530942 / 64);
+            double term = 1.0, sum = 1.0;
+            for (int k = 1; k < 24; ++k) {
+                term *= x / k;
+                sum += term;
+            }
+            v[j] = sum;
+        }
+    }
+};
+__device__ constexpr SampleTable kSampleTable{};
 
 // What the blocks of a cluster tell one another.
 struct SampleWord {
@@ -52,19 +80,21 @@ struct SampleWord {
 
 struct SampleFound {
     int bin;                               // or -1
-    uint32_t count;                        // of the bin (counts)
-    uint64_t before, in, total;            // sums ahead of the bin, of the bin, of all bins
+    uint64_t before, in;                   // sums ahead of the bin, of the bin
 };
 
 struct SampleShared {
-    uint32_t hist[3][kSampleBins];
+    double table[64];
     SampleWord slots[2][kSampleMaxCluster];
     SampleFound found[2];
     double warp_sum[kSampleWarps];
     uint64_t warp_u64[kSampleWarps];
-    uint32_t warp_u32[kSampleWarps], warp_ties[kSampleWarps];
+    uint32_t warp_u32[2][kSampleWarps], warp_ties[kSampleWarps];
     float warp_max[kSampleWarps];
-    uint32_t least_key;
+    uint32_t list[kSampleList];            // keys of this block's candidates
+    uint32_t ranges[kSampleRanges];        // keys of the largest logits of its ranges
+    uint32_t keys[kSampleList], sorted[kSampleList];       // of all blocks' candidates, or ranges
+    uint32_t hist[kSampleBins];            // or three limbs of kSampleFine bins
 };
 
 __device__ __forceinline__ uint32_t sample_key(float v) {        // the order of logits as that of unsigned integers
@@ -74,31 +104,78 @@ __device__ __forceinline__ uint32_t sample_key(float v) {        // the order of
 __device__ __forceinline__ float sample_value(uint32_t key) {
     return __uint_as_float(key ^ (key & 0x80000000u ? 0x80000000u : 0xffffffffu));
 }
-constexpr uint32_t kKeyNothing = 0x007fffffu;                    // that of minus infinity
+
+// NaN as minus infinity, no zero below zero.
+__device__ __forceinline__ float sane(float v) { return fmaxf(v, -INFINITY) + 0.0f; }
+template <typename T, int VEC>
+__device__ __forceinline__ void sane_pack(Pack<T, VEC> &p) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) p.v[e] = sane(p.v[e]);
+    } else if constexpr (std::is_same_v<T, __half>) {
+        __half2 *two = reinterpret_cast<__half2 *>(p.v);
+#pragma unroll
+        for (int e = 0; e < VEC / 2; ++e) two[e] = __hadd2(__hmax2(two[e], __float2half2_rn(-INFINITY)), __float2half2_rn(0.0f));
+    } else {
+        __nv_bfloat162 *two = reinterpret_cast<__nv_bfloat162 *>(p.v);
+#pragma unroll
+        for (int e = 0; e < VEC / 2; ++e) two[e] = __hadd2(__hmax2(two[e], __float2bfloat162_rn(-INFINITY)), __float2bfloat162_rn(0.0f));
+    }
+}
 
 template <typename T>
 struct Sampler {
     static constexpr int kVec = 16 / sizeof(T);
+    using Packed = Pack<T, kVec>;
     const SampleParams &p;
     SampleShared &s;
-    T *held;                               // this block's part of the row, minus infinity where it has no token
+    Packed *held;                          // this thread's tokens, at(j) on, in steps of kSampleThreads; minus infinity where there are none
     cooperative_groups::cluster_group cluster;
-    uint32_t rank, ranks, phase = 0, found_phase = 0;
-    uint32_t row, n;
-    int64_t first;                         // token of held[0]
-    float top = 0.0f;
-    double inverse = 1.0;                  // of the temperature
+    uint32_t rank, ranks, phase = 0, found_phase = 0, row;
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    int first;                             // token of the block's first element
+    float top = 0.0f;                      // what weights are relative to
+    double inverse = 1.0, sixty_fourths = 1.0;      // 1 / temperature; 64 log2(e) / temperature
 
-    __device__ Sampler(const SampleParams &p, SampleShared &s, T *held)
-        : p(p), s(s), held(held), cluster(cooperative_groups::this_cluster()) {
+    __device__ Sampler(const SampleParams &p, SampleShared &s, void *held) : p(p), s(s), held(static_cast<Packed *>(held) + threadIdx.x), cluster(cooperative_groups::this_cluster()) {
         rank = cluster.block_rank();
         ranks = cluster.num_blocks();
         row = blockIdx.x / ranks;
     }
+    __device__ __forceinline__ int at(int j) const { return first + ((int(warp) * p.packs + j) * 32 + int(lane)) * kVec; }
+    // f(logit) for this thread's tokens.
+    template <typename F>
+    __device__ __forceinline__ void each(F f) const {
+#pragma unroll 1
+        for (int j = 0; j < p.packs; ++j) {
+            const Packed q = held[j * kSampleThreads];
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) f(to_f32<T>(q.v[e]));
+        }
+    }
 
-    // The weight of a token; logits at the top have 1 also where that is infinite.
-    __device__ __forceinline__ double weight(float v) const { return v == top ? 1.0 : exp((double(v) - double(top)) * inverse); }
-    __device__ __forceinline__ uint64_t fixed(float v) const { return uint64_t(__double2ll_rn(weight(v) * kSampleFixed)); }
+    // exp((x - top) / temperature), by table (P. T. P. Tang, 1989): with y = 64 log2(e) (x - top) / temperature = k + r, k the nearest integer,
+    // 2^(y/64) = 2^floor(k/64) 2^(k mod 64 / 64) (1 + q + q^2/2 + q^3/6 + q^4/24), q = r ln 2 / 64: |q| < 0.0055, what is left out is below
+    // 5e-14 of it.  Zero below 2^-1000; 1 for the top itself.
+    __device__ __forceinline__ double weight(float x) const {
+        const double y = (double(x) - double(top)) * sixty_fourths;
+        constexpr double kMagic = 6755399441055744.0, kLn = 0.69314718055994530942 / 64;
+        const double t = y + kMagic;
+        const int k = __double2loint(t);
+        const double q = (y - (t - kMagic)) * kLn;
+        const double m = s.table[k & 63];
+        double poly = fma(q, 1.0 / 24, 1.0 / 6);
+        poly = fma(q, poly, 0.5);
+        poly = fma(q * q, poly, q);
+        const double w = fma(m, poly, m);
+        const bool far = uint32_t(__double2hiint(y)) > 0xC0EF4000u;                            // y below -64000
+        return far ? 0.0 : __hiloint2double(__double2hiint(w) + (k >> 6) * 1048576, __double2loint(w));
+    }
+    __device__ __forceinline__ uint64_t fixed(float x) const { return uint64_t(__double2ll_rn(weight(x) * kSampleFixed)); }
+    __device__ __forceinline__ void set_temperature(double temperature) {
+        inverse = 1.0 / temperature;
+        sixty_fourths = inverse * (64 * 1.4426950408889634074);
+    }
 
     // Every block's word, at every block.  All threads call it; what is told has to be ready in thread 0's to kSampleMaxCluster - 1's `mine`.
     __device__ const SampleWord *exchange(const SampleWord &mine) {
@@ -109,106 +186,134 @@ struct Sampler {
         return slots;
     }
 
-    __device__ float block_max(float v) {
+    // The block's largest logit, from the threads'; s.ranges holds the keys of its ranges' (0 for one without a token).
+    __device__ float block_max(float x) {
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(~0u, v, o));
-        if ((threadIdx.x & 31) == 0) s.warp_max[threadIdx.x >> 5] = v;
-        __syncthreads();
-        v = s.warp_max[threadIdx.x & (kSampleWarps - 1)];
+        for (int o = 1; o < 8; o <<= 1) x = fmaxf(x, __shfl_xor_sync(~0u, x, o));
+        if (lane % 8 == 0) s.ranges[warp * 4 + lane / 8] = x > -INFINITY ? sample_key(x) : 0;
 #pragma unroll
-        for (int o = kSampleWarps / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(~0u, v, o));
-        return v;
-    }
-    __device__ uint32_t block_min(uint32_t v) {
-        v = __reduce_min_sync(~0u, v);
+        for (int o = 8; o < 32; o <<= 1) x = fmaxf(x, __shfl_xor_sync(~0u, x, o));
+        if (lane == 0) s.warp_max[warp] = x;
         __syncthreads();
-        if ((threadIdx.x & 31) == 0) s.warp_u32[threadIdx.x >> 5] = v;
-        __syncthreads();
-        return __reduce_min_sync(~0u, s.warp_u32[threadIdx.x & (kSampleWarps - 1)]);
+        x = s.warp_max[lane & (kSampleWarps - 1)];
+#pragma unroll
+        for (int o = kSampleWarps / 2; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor_sync(~0u, x, o));
+        return x;
     }
-    __device__ uint32_t cluster_min(uint32_t v) {
-        const SampleWord *w = exchange({0.0, block_min(v), 0});
-        uint32_t least = w[0].b;
-        for (uint32_t k = 1; k < ranks; ++k) least = min(least, w[k].b);
+    // The least of all threads' values, of two at once.
+    __device__ uint2 block_min(uint32_t a, uint32_t b) {
+        a = __reduce_min_sync(~0u, a);
+        b = __reduce_min_sync(~0u, b);
+        __syncthreads();
+        if (lane == 0) s.warp_u32[0][warp] = a, s.warp_u32[1][warp] = b;
+        __syncthreads();
+        return make_uint2(__reduce_min_sync(~0u, s.warp_u32[0][lane & (kSampleWarps - 1)]), __reduce_min_sync(~0u, s.warp_u32[1][lane & (kSampleWarps - 1)]));
+    }
+    __device__ uint2 cluster_min(uint32_t a, uint32_t b) {
+        const uint2 mine = block_min(a, b);
+        const SampleWord *w = exchange({0.0, mine.x, mine.y});
+        uint2 least = make_uint2(w[0].b, w[0].c);
+        for (uint32_t k = 1; k < ranks; ++k) least = make_uint2(min(least.x, w[k].b), min(least.y, w[k].c));
         return least;
     }
-
-    // Reads the block's part of the row (addresses in steps of 16 bytes, whatever the row begins at) and finds the largest logit.
-    __device__ void load() {
-        const T *at = static_cast<const T *>(p.logits) + uint64_t(row) * p.stride;
-        const uint32_t off = uint32_t(reinterpret_cast<uintptr_t>(at) % 16) / sizeof(T);       // tokens ahead of the row on its first 16 bytes
-        const int64_t begin = int64_t(rank) * p.part;
-        first = begin - off;
-        n = p.part;
-        float most = -INFINITY;
-        for (uint32_t i = threadIdx.x * kVec; i < n; i += kSampleThreads * kVec) {
-            Pack<T, kVec> v;
-            const int64_t token = first + i;
-            if (token >= 0 && token + kVec <= p.vocabulary) {
-                v = *reinterpret_cast<const Pack<T, kVec> *>(at + token);
-            } else {
+    // The sum of all threads' values, warp after warp; s.warp_sum holds the warps' sums.
+    __device__ double block_sum(double x) {
 #pragma unroll
-                for (int e = 0; e < kVec; ++e) v.v[e] = token + e >= 0 && token + e < p.vocabulary ? at[token + e] : from_f32<T>(-INFINITY);
-            }
+        for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(~0u, x, o);
+        __syncthreads();
+        if (lane == 0) s.warp_sum[warp] = x;
+        __syncthreads();
+        double sum = 0.0;
+        for (int k = 0; k < kSampleWarps; ++k) sum += s.warp_sum[k];
+        return sum;
+    }
+    template <typename Keep>
+    __device__ double thread_sum(Keep keep) const {            // of the weights of the tokens that are kept
+        double sum[4] = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll 1
+        for (int j = 0; j < p.packs; ++j) {
+            const Packed q = held[j * kSampleThreads];
 #pragma unroll
             for (int e = 0; e < kVec; ++e) {
-                float f = to_f32<T>(v.v[e]) + 0.0f;                  // (no zero below zero: the two are equal)
-                if (f != f) f = -INFINITY;
-                most = fmaxf(most, f);
-                v.v[e] = from_f32<T>(f);
+                const float x = to_f32<T>(q.v[e]);
+                if (keep(x)) sum[e & 3] += weight(x);
             }
-            *reinterpret_cast<Pack<T, kVec> *>(held + i) = v;
         }
-        most = block_max(most);
-        const SampleWord *w = exchange({double(most), 0, 0});
-        top = float(w[0].a);
-        for (uint32_t k = 1; k < ranks; ++k) top = fmaxf(top, float(w[k].a));
+        return (sum[0] + sum[1]) + (sum[2] + sum[3]);
     }
 
-    __device__ __forceinline__ float logit(uint32_t i) const { return to_f32<T>(held[i]); }
+    // Reads the block's part of the row (addresses in steps of 16 bytes, whatever the row begins at); the thread's largest logit.
+    __device__ float load() {
+        const T *from = static_cast<const T *>(p.logits) + uint64_t(row) * p.stride;
+        first = int(rank * kSampleThreads * p.packs * kVec) - int(reinterpret_cast<uintptr_t>(from) % 16 / sizeof(T));   // (what lies ahead of the row on its first 16 bytes)
+        if (threadIdx.x < 64) s.table[threadIdx.x] = kSampleTable.v[threadIdx.x];
+        float most = -INFINITY;
+#pragma unroll 4
+        for (int j = 0; j < p.packs; ++j) {
+            const int token = at(j);
+            Packed q;
+            if (token >= 0 && token + kVec <= int(p.vocabulary)) {
+                q = *reinterpret_cast<const Packed *>(from + token);
+            } else {
+#pragma unroll
+                for (int e = 0; e < kVec; ++e) q.v[e] = token + e >= 0 && token + e < int(p.vocabulary) ? from[token + e] : from_f32<T>(-INFINITY);
+            }
+            sane_pack<T, kVec>(q);
+            held[j * kSampleThreads] = q;
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) most = fmaxf(most, to_f32<T>(q.v[e]));
+        }
+        return most;
+    }
+    // An infinite logit leaves no weight to any other: it becomes 0, the others minus infinity.
+    __device__ void only_infinite() {
+        for (int j = 0; j < p.packs; ++j)
+            for (int e = 0; e < kVec; ++e) {
+                T &x = held[j * kSampleThreads].v[e];
+                x = from_f32<T>(to_f32<T>(x) == INFINITY ? 0.0f : -INFINITY);
+            }
+    }
 
-    // Histogram over the row's tokens of bin_of (below 0: not counted) - of weights, or of numbers - and the first bin with which the
-    // sum from `before` on reaches `target`; the target is taken from the sum of all bins by target_of.
-    template <bool WEIGHTS, typename BinOf, typename TargetOf>
-    __device__ SampleFound histogram(BinOf bin_of, uint64_t before, TargetOf target_of) {
-        constexpr int kLimbs = WEIGHTS ? 3 : 1;
+    // Histogram over the row's tokens of bin_of (below 0: not counted) - LIMBS 1: of what(logit); 3: of exact weights, in limbs - and the first
+    // bin with which the sum reaches `target`.
+    template <int LIMBS, int BINS, typename BinOf, typename What>
+    __device__ SampleFound histogram(BinOf bin_of, What what, double target) {
+        static_assert(LIMBS * BINS <= kSampleBins, "in shared memory");
         SampleFound *found = &s.found[found_phase];
         found_phase ^= 1;
-        for (int l = 0; l < kLimbs; ++l)
-            for (uint32_t b = threadIdx.x; b < kSampleBins; b += kSampleThreads) s.hist[l][b] = 0;
+        for (uint32_t b = threadIdx.x; b < LIMBS * BINS; b += kSampleThreads) s.hist[b] = 0;
         if (threadIdx.x == 0) found->bin = -1;
         __syncthreads();
-        for (uint32_t i = threadIdx.x; i < n; i += kSampleThreads) {
-            const float v = logit(i);
-            const int b = bin_of(v);
-            if (b < 0) continue;
-            if constexpr (WEIGHTS) {
-                const uint64_t w = fixed(v);
-                atomicAdd(&s.hist[0][b], uint32_t(w) & ((1u << kSampleLimb) - 1));
-                atomicAdd(&s.hist[1][b], uint32_t(w >> kSampleLimb) & ((1u << kSampleLimb) - 1));
-                atomicAdd(&s.hist[2][b], uint32_t(w >> (2 * kSampleLimb)));
-            } else {
-                atomicAdd(&s.hist[0][b], 1u);
+        each([&](float x) {
+            const int b = bin_of(x);
+            if (b >= 0) {
+                if constexpr (LIMBS == 3) {
+                    const uint64_t w = fixed(x);
+                    atomicAdd(&s.hist[b], uint32_t(w) & ((1u << kSampleLimb) - 1));
+                    atomicAdd(&s.hist[BINS + b], uint32_t(w >> kSampleLimb) & ((1u << kSampleLimb) - 1));
+                    atomicAdd(&s.hist[2 * BINS + b], uint32_t(w >> (2 * kSampleLimb)));
+                } else {
+                    atomicAdd(&s.hist[b], what(x));
+                }
             }
-        }
+        });
         cluster.sync();
         // this block's share of the bins, a few each thread
-        const uint32_t share = kSampleBins / ranks, each = (share + kSampleThreads - 1) / kSampleThreads;
-        const uint32_t own = rank * share + threadIdx.x * each;
-        const bool some = threadIdx.x * each < share;
-        uint64_t mine[kSampleBins / kSampleThreads], sum = 0;
-        for (uint32_t j = 0; j < each; ++j) {
-            uint64_t v = 0;
-            if (some)
+        const uint32_t share = BINS / ranks, each_thread = (share + kSampleThreads - 1) / kSampleThreads;
+        const uint32_t own = rank * share + threadIdx.x * each_thread;
+        const bool some = threadIdx.x * each_thread < share;
+        uint64_t mine[BINS / kSampleThreads], sum = 0;
+#pragma unroll
+        for (uint32_t j = 0; j < BINS / kSampleThreads; ++j) {
+            mine[j] = 0;
+            if (some && j < each_thread)
                 for (uint32_t k = 0; k < ranks; ++k) {
-                    const auto *h = cluster.map_shared_rank(&s.hist[0][0], k) + own + j;
-                    v += h[0];
-                    if constexpr (WEIGHTS) v += (uint64_t(h[kSampleBins]) << kSampleLimb) + (uint64_t(h[2 * kSampleBins]) << (2 * kSampleLimb));
+                    const auto *h = cluster.map_shared_rank(s.hist, k) + own + j;
+                    mine[j] += h[0];
+                    if constexpr (LIMBS == 3) mine[j] += (uint64_t(h[BINS]) << kSampleLimb) + (uint64_t(h[2 * BINS]) << (2 * kSampleLimb));
                 }
-            mine[j] = v;
-            sum += v;
+            sum += mine[j];
         }
-        const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
         uint64_t upto = sum;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -217,262 +322,508 @@ struct Sampler {
         }
         if (lane == 31) s.warp_u64[warp] = upto;
         __syncthreads();
-        uint64_t ahead = 0, all = 0;
+        uint64_t ahead = upto - sum, all = 0;
         for (uint32_t k = 0; k < kSampleWarps; ++k) {
             if (k < warp) ahead += s.warp_u64[k];
             all += s.warp_u64[k];
         }
-        ahead += upto - sum;
         const SampleWord *w = exchange({__longlong_as_double(int64_t(all)), 0, 0});
-        uint64_t total = 0;
-        for (uint32_t k = 0; k < ranks; ++k) {
-            const uint64_t q = uint64_t(__double_as_longlong(w[k].a));
-            if (k < rank) ahead += q;
-            total += q;
-        }
-        const double target = target_of(total);
-        ahead += before;
-        for (uint32_t j = 0; j < each; ++j) {
-            if (some && double(ahead) < target && double(ahead + mine[j]) >= target) {
-                const SampleFound f = {int(own + j), 0, ahead, mine[j], total};
+        for (uint32_t k = 0; k < rank; ++k) ahead += uint64_t(__double_as_longlong(w[k].a));
+#pragma unroll
+        for (uint32_t j = 0; j < BINS / kSampleThreads; ++j) {
+            if (mine[j] && double(ahead) < target && double(ahead + mine[j]) >= target) {
+                const SampleFound f = {int(own + j), ahead, mine[j]};
                 for (uint32_t k = 0; k < ranks; ++k) *cluster.map_shared_rank(found, k) = f;
             }
             ahead += mine[j];
         }
         cluster.sync();
-        SampleFound f = *found;
-        f.total = total;
-        return f;
+        return *found;
     }
 
-    // The prefix (in falling order) of the tokens with a key of at least `least` that reaches a target: its last key, how many of the tokens with
-    // that key it takes, and whether these are all.  False: the tokens do not reach the target.
-    template <bool WEIGHTS, typename TargetOf>
-    __device__ bool reach(uint32_t least, TargetOf target_of, uint32_t &last, uint32_t &ties, bool &whole, uint64_t &total) {
+    // A prefix of the falling order: the tokens above `edge`, and those of it - all (whole), or the first `ties`.
+    struct Prefix {
+        float edge;
+        uint32_t ties;
+        bool whole;
+    };
+
+    // Where a logit lies in the first histogram, linear in it: 64 bins to a factor of e in weight.
+    __device__ __forceinline__ int bin(float x, float cut, float scale) const {
+        return x < cut ? -1 : x == top ? 0 : int(fminf((top - x) * scale, float(kSampleBins - 1)));
+    }
+
+    // The prefix of the tokens from `cut` on that reaches a number of them.  False: there are fewer.
+    __device__ bool reach_number(float cut, double k, Prefix &out) {
         const float scale = float(inverse * 64.0);
-        auto linear = [&](float v) {
-            return sample_key(v) < least ? -1 : v == top ? 0 : int(fminf((top - v) * scale, float(kSampleBins - 1)));
-        };
-        SampleFound f = histogram<WEIGHTS>(linear, 0, target_of);
-        total = f.total;
+        const SampleFound f = histogram<1, kSampleBins>([&](float x) { return bin(x, cut, scale); }, [](float) { return 1u; }, k);
         if (f.bin < 0) return false;
-        const double target = target_of(total);
-        uint32_t lo = ~0u, hi_not = ~0u;                     // keys of the bin: from lo to ~hi_not
-        for (uint32_t i = threadIdx.x; i < n; i += kSampleThreads) {
-            const float v = logit(i);
-            if (linear(v) != f.bin) continue;
-            lo = min(lo, sample_key(v));
-            hi_not = min(hi_not, ~sample_key(v));
-        }
-        lo = cluster_min(lo);
-        uint32_t hi = ~cluster_min(hi_not);
-        while (lo < hi) {
-            const int bits = 32 - __clz(hi - lo), shift = bits > 11 ? bits - 11 : 0;
-            const SampleFound g = histogram<WEIGHTS>(
-                [&](float v) {
-                    const uint32_t key = sample_key(v);
-                    return key < lo || key > hi ? -1 : int((hi - key) >> shift);
-                },
-                f.before, [&](uint64_t) { return target; });
-            if (g.bin < 0) break;                            // (not met: these bins add up to the one before)
-            f = g;
-            hi -= uint32_t(f.bin) << shift;
-            lo = max(lo, hi - ((1u << shift) - 1));
-        }
-        last = hi;
-        // the fewest of the tokens with this key that reach the target
-        const uint64_t one = WEIGHTS ? fixed(sample_value(hi)) : 1, many = one ? f.in / one : 1;
-        uint64_t c = one ? uint64_t(fmax(ceil((target - double(f.before)) / double(one)), 1.0)) : 1;
-        while (c > 1 && double(f.before + (c - 1) * one) >= target) --c;
-        while (c < many && double(f.before + c * one) < target) ++c;
-        ties = uint32_t(c);
-        whole = c >= many;
+        out = in_bin<false>(cut, scale, f.bin, k - double(f.before));
         return true;
     }
-
-    // The least key whose weight is at least min_p: found by every warp's lanes, 32 keys at a time.
-    __device__ uint32_t least_key(double min_p) {
-        uint64_t lo = kKeyNothing + 1, hi = sample_key(top);             // hi has weight 1
-        const uint32_t lane = threadIdx.x & 31;
-        while (lo < hi) {
-            const uint64_t step = (hi - lo + 31) / 32, at = lo + step * lane;
-            const uint32_t in = __ballot_sync(~0u, at < hi && weight(sample_value(uint32_t(at))) >= min_p);
-            // of the keys looked at, those from the first that is in on are in
-            const uint32_t looked = __popc(__ballot_sync(~0u, at < hi)), f = in ? uint32_t(__ffs(int(in)) - 1) : looked;
-            if (f < looked) hi = lo + step * f;
-            if (f > 0) lo += step * (f - 1) + 1;
-        }
-        return uint32_t(hi);
-    }
-
-    __device__ void put(int64_t token, float log_prob) {
-        p.tokens[row] = token;
-        if (p.log_probs) p.log_probs[row] = log_prob;
-    }
-
-    __device__ void run() {
-        load();
-        if (top == -INFINITY) {
-            if (rank == 0 && threadIdx.x == 0) put(-1, -INFINITY);
-            cluster.sync();
-            return;
-        }
-        const double temperature = p.temperature.at(row), min_p = p.min_p.at(row), top_p = p.top_p.at(row);
-        const double k = p.top_k.at(row);
-        const bool warm = temperature > 0.0;
-        inverse = warm && top < INFINITY ? 1.0 / temperature : 1.0;      // (with an infinite logit the others have no weight at any temperature)
-        if (!warm || k == 1.0 || min_p > 1.0 || top_p <= 0.0) {          // the first token alone
-            uint32_t at = ~0u;
-            for (uint32_t i = threadIdx.x; i < n; i += kSampleThreads)
-                if (logit(i) == top) at = min(at, uint32_t(first + i));
-            at = cluster_min(at);
-            if (rank == 0 && threadIdx.x == 0) put(at, 0.0f);
-            cluster.sync();
-            return;
-        }
-        uint32_t least = kKeyNothing + 1, ties = 0;                      // kept: keys above `least`, and those of it, the first `ties` if not all
-        bool whole = true;
-        if (min_p > 0.0) least = least_key(min_p);
-        uint64_t total = 0;
-        bool edge = false;                                               // whether top_k ends within (or with) the tokens of key `least`
-        if (k > 0.0 && k < double(p.vocabulary)) edge = reach<false>(least, [&](uint64_t) { return k; }, least, ties, whole, total);
-        if (top_p < 1.0) {
-            const uint64_t group = edge ? ties * fixed(sample_value(least)) : 0;
-            uint32_t last = 0, some = 0;
-            bool all = true;
-            if (reach<true>(edge ? least + 1 : least, [&](uint64_t sum) { return top_p * double(sum + group); }, last, some, all, total)) {
-                least = last;
-                ties = some;
-                whole = all;
-            } else if (edge) {
-                const uint64_t one = fixed(sample_value(least));
-                const double target = top_p * double(total + group);
-                uint32_t c = 1;
-                if (one) c = uint32_t(fmin(fmax(ceil((target - double(total)) / double(one)), 1.0), double(ties)));
-                while (c > 1 && double(total + (c - 1) * one) >= target) --c;
-                while (c < ties && double(total + c * one) < target) ++c;
-                whole = whole && c == ties;
-                ties = c;
-            }
-        }
-        draw(least, ties, whole);
-        cluster.sync();
-    }
-
-    // Draws from the tokens with keys above `least`, and of those with it all (whole) or the first `ties`.
-    __device__ void draw(uint32_t least, uint32_t ties, bool whole) {
-        const uint32_t lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-        const uint32_t each = ((n + kSampleWarps - 1) / kSampleWarps + 31) / 32 * 32;         // tokens of a warp
-        const uint32_t begin = min(warp * each, n), end = min(begin + each, n);
-        const uint32_t edge = whole ? 0u : least;                                             // (0: no token has this key)
-        const uint32_t from = whole ? least : least + 1;
-        const double w_edge = whole ? 0.0 : weight(sample_value(least));
-        double sum = 0.0;
-        uint32_t count = 0;
-        for (uint32_t i = begin + lane; i < end; i += 32) {
-            const float v = logit(i);
-            const uint32_t key = sample_key(v);
-            if (key >= from) sum += weight(v);
-            count += key == edge;
-        }
+    // The same for a weight, of `sum` of all that is looked at.
+    __device__ bool reach_weight(float cut, double target, double sum, Prefix &out) {
+        const float scale = float(inverse * 64.0);
+        // weights to about 2^-22, as parts of 2^30 of the sum
+        const float to_part = float(1073741824.0 / sum), octaves = float(inverse * 1.4426950408889634);
+        const SampleFound f = histogram<1, kSampleBins>(
+            [&](float x) { return bin(x, cut, scale); },
+            [&](float x) {
+                float w;
+                asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(w) : "f"(fmaxf((x - top) * octaves, -1000.0f)));
+                return uint32_t(__float2uint_rn(w * to_part));
+            },
+            target / sum * 1073741824.0);
+        int at = f.bin < 0 ? bin(cut, cut, scale) : f.bin, turn = 0;
+        for (;;) {
+            // the sums ahead of the bin and of it; the next bins on either side that have a token
+            double ahead[2] = {0.0, 0.0}, of_bin[2] = {0.0, 0.0};
+            uint32_t below = ~0u, above = ~0u;
+#pragma unroll 1
+            for (int j = 0; j < p.packs; ++j) {
+                const Packed q = held[j * kSampleThreads];
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
-        count = __reduce_add_sync(~0u, count);
-        __syncthreads();
-        if (lane == 0) {
-            s.warp_sum[warp] = sum;
-            s.warp_ties[warp] = count;
-        }
-        __syncthreads();
-        double block_sum = 0.0;
-        uint32_t block_ties = 0;
-        for (int k = 0; k < kSampleWarps; ++k) {
-            block_sum += s.warp_sum[k];
-            block_ties += s.warp_ties[k];
-        }
-        const SampleWord *words = exchange({block_sum, block_ties, 0});
-        // sums with the edge's tokens that belong to it, block after block
-        auto with_edge = [&](double some, uint32_t before, uint32_t here) {
-            const uint32_t left = before < ties ? ties - before : 0;
-            return whole ? some : some + double(min(left, here)) * w_edge;
-        };
-        double total = 0.0;
-        uint32_t seen = 0;
-        for (uint32_t k = 0; k < ranks; ++k) {
-            total += with_edge(words[k].a, seen, words[k].b);
-            seen += words[k].b;
-        }
-        double u = p.uniform_f64 ? static_cast<const double *>(p.uniform)[row] : double(static_cast<const float *>(p.uniform)[row]);
-        if (!(u > 0.0)) u = 0.0;
-        const double target = u * total;
-        // the block, then its warp, in which the sum passes the target (the last one that adds anything, if rounding leaves none)
-        double ahead = 0.0, before = 0.0;
-        uint32_t ties_ahead = 0, ties_before = 0, who = 0;
-        bool past = false;
-        for (uint32_t k = 0; k < ranks && !past; ++k) {
-            const double add = with_edge(words[k].a, ties_ahead, words[k].b);
-            if (add > 0.0) {
-                who = k;
-                before = ahead;
-                ties_before = ties_ahead;
-                past = ahead + add > target;
+                for (int e = 0; e < kVec; ++e) {
+                    const float x = to_f32<T>(q.v[e]);
+                    const int b = bin(x, cut, scale);
+                    if (b >= 0) {
+                        if (b <= at) {
+                            const double w = weight(x);
+                            if (b < at) ahead[e & 1] += w;
+                            else of_bin[e & 1] += w;
+                        }
+                        if (b < at) below = min(below, uint32_t(at - b));
+                        if (b > at) above = min(above, uint32_t(b - at));
+                    }
+                }
             }
-            ahead += add;
-            ties_ahead += words[k].b;
-        }
-        if (who != rank) return;
-        ahead = before;
-        ties_ahead = ties_before;
-        past = false;
-        who = 0;
-        for (uint32_t k = 0; k < kSampleWarps && !past; ++k) {
-            const double add = with_edge(s.warp_sum[k], ties_ahead, s.warp_ties[k]);
-            if (add > 0.0) {
-                who = k;
-                before = ahead;
-                ties_before = ties_ahead;
-                past = ahead + add > target;
+            const double in_here = block_sum(of_bin[0] + of_bin[1]), ahead_here = block_sum(ahead[0] + ahead[1]);
+            const SampleWord *w = exchange({ahead_here, uint32_t(__double2hiint(in_here)), uint32_t(__double2loint(in_here))});
+            double before = 0.0, in = 0.0;
+            for (uint32_t k = 0; k < ranks; ++k) {
+                before += w[k].a;
+                in += __hiloint2double(int(w[k].b), int(w[k].c));
             }
-            ahead += add;
-            ties_ahead += s.warp_ties[k];
+            // (the bin is left in one direction only: sums that are the same but for rounding must not send it back)
+            const bool down = before >= target && turn <= 0, up = before + in < target && before < target && turn >= 0;
+            if (!down && !up) {
+                out = in_bin<true>(cut, scale, at, fmax(target - before, 0.0));
+                return true;
+            }
+            const uint2 next = cluster_min(below, above);
+            const uint32_t by = down ? next.x : next.y;
+            if (by == ~0u) return false;                     // (rounding leaves less than the target)
+            turn = down ? -1 : 1;
+            at += turn * int(by);
         }
-        if (who != warp) return;
-        // the warp's tokens, 32 at a time
-        int64_t token = -1;
-        float chosen = 0.0f;
-        past = false;
-        for (uint32_t i0 = begin; i0 < end && !past; i0 += 32) {
-            const uint32_t i = i0 + lane;
-            const float v = i < end ? logit(i) : -INFINITY;
-            const uint32_t key = sample_key(v);
-            const uint32_t tied = __ballot_sync(~0u, key == edge);
-            const bool kept = key >= from || (key == edge && ties_before + __popc(tied & ((1u << lane) - 1)) < ties);
-            ties_before += __popc(tied);
-            const double w = kept ? weight(v) : 0.0;
-            double upto = w;
+    }
+    // The prefix that ends in a bin: with `left` of its tokens' number, or weight.
+    template <bool WEIGHTS>
+    __device__ Prefix in_bin(float cut, float scale, int which, double left) {
+        const uint32_t total = sort_candidates([&](float x) { return bin(x, cut, scale) == which; });
+        if (total <= kSampleList) return WEIGHTS ? prefix_of(total, total, 0.0, left) : prefix_of(total, uint32_t(fmin(left, double(total))), 1.0, 0.0);
+        uint32_t lo = ~0u, hi_not = ~0u;                     // keys of the bin: from lo to ~hi_not
+        each([&](float x) {
+            if (bin(x, cut, scale) == which) {
+                lo = min(lo, sample_key(x));
+                hi_not = min(hi_not, ~sample_key(x));
+            }
+        });
+        const uint2 ends = cluster_min(lo, hi_not);
+        lo = ends.x;
+        uint32_t hi = ~ends.y;
+        double before = 0.0, one = WEIGHTS ? double(fixed(sample_value(hi))) : 1.0, target = WEIGHTS ? left * kSampleFixed : left, many = total;
+        while (lo < hi) {
+            const int bits = 32 - __clz(hi - lo), shift = bits > kSampleFineBits ? bits - kSampleFineBits : 0;
+            auto bin_of = [&](float x) {
+                const uint32_t key = sample_key(x);
+                return key < lo || key > hi ? -1 : int((hi - key) >> shift);
+            };
+            const SampleFound g = histogram<WEIGHTS ? 3 : 1, kSampleFine>(bin_of, [](float) { return 1u; }, target - before);
+            if (g.bin < 0) {                                 // (rounding: the last of them)
+                if (shift == 0) hi = lo;
+                else hi = lo + ((hi - lo) & ((1u << shift) - 1));
+            } else {
+                before += double(g.before);
+                hi -= uint32_t(g.bin) << shift;
+                lo = max(lo, hi - ((1u << shift) - 1));
+            }
+            one = WEIGHTS ? double(fixed(sample_value(hi))) : 1.0;
+            many = one > 0.0 ? double(g.bin < 0 ? 1 : g.in) / one : 1.0;
+        }
+        const uint32_t most = uint32_t(fmax(rint(many), 1.0)), ties = uint32_t(fewest(before, one, target, most));
+        return {sample_value(hi), ties, ties >= most};
+    }
+    // The least c from 1 to `many` with before + c one >= target.
+    __device__ static uint64_t fewest(double before, double one, double target, uint64_t many) {
+        if (!(one > 0.0)) return 1;
+        uint64_t c = uint64_t(fmin(fmax(ceil((target - before) / one), 1.0), double(many)));
+        while (c > 1 && before + double(c - 1) * one >= target) --c;
+        while (c < many && before + double(c) * one < target) ++c;
+        return c;
+    }
+
+    // Sorts s.keys, of which `total` are above 0, into s.sorted, falling.
+    __device__ void sort_keys(uint32_t total) {
+        __syncthreads();
+        const uint32_t key = s.keys[threadIdx.x];
+        uint32_t before = 0;                                 // those ahead of this one: larger ones, and equal ones of lower threads
+        const uint4 *keys = reinterpret_cast<const uint4 *>(s.keys);
+        for (uint32_t i = 0; i < kSampleList / 4 && 4 * i < total; ++i) {
+            const uint4 q = keys[i];
+            const uint32_t k = 4 * i;
+            before += (q.x > key || (q.x == key && k < threadIdx.x)) + (q.y > key || (q.y == key && k + 1 < threadIdx.x)) +
+                      (q.z > key || (q.z == key && k + 2 < threadIdx.x)) + (q.w > key || (q.w == key && k + 3 < threadIdx.x));
+        }
+        if (key) s.sorted[before] = key;
+        __syncthreads();
+    }
+    // The candidates, if the row has no more than kSampleList of them: their number; s.sorted holds their keys, falling, at every block.
+    template <typename Is>
+    __device__ uint32_t sort_candidates(Is is) {
+        uint32_t mine = 0;
+        each([&](float x) { mine += is(x); });
+        uint32_t upto = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t q = __shfl_up_sync(~0u, upto, o);
+            if (lane >= uint32_t(o)) upto += q;
+        }
+        __syncthreads();
+        if (lane == 31) s.warp_u32[0][warp] = upto;
+        __syncthreads();
+        uint32_t to = upto - mine, here = 0;
+        for (uint32_t k = 0; k < kSampleWarps; ++k) {
+            if (k < warp) to += s.warp_u32[0][k];
+            here += s.warp_u32[0][k];
+        }
+        if (here <= kSampleList && mine)
+            each([&](float x) {
+                if (is(x)) s.list[to++] = sample_key(x);
+            });
+        const SampleWord *w = exchange({0.0, here, 0});
+        uint32_t total = 0;
+        for (uint32_t k = 0; k < ranks; ++k) total += w[k].b;
+        if (total > kSampleList) return total;
+        uint32_t from = threadIdx.x, key = 0;
+        if (threadIdx.x < total) {
+            uint32_t k = 0;
+            while (from >= w[k].b) from -= w[k++].b;
+            key = cluster.map_shared_rank(s.list, k)[from];
+        }
+        s.keys[threadIdx.x] = key;
+        sort_keys(total);
+        // (nobody writes its list again before all have read it)
+        cluster.sync();
+        return total;
+    }
+    // Of the first `most` of `total` sorted candidates, for top_p below 1, those whose weights reach the target (below 0: top_p of theirs).
+    __device__ Prefix prefix_of(uint32_t total, uint32_t most, double top_p, double target) {
+        uint32_t m = most;
+        if (top_p < 1.0) {
+            const uint32_t i = threadIdx.x;
+            double upto = i < most ? weight(sample_value(s.sorted[i])) : 0.0;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
                 const double q = __shfl_up_sync(~0u, upto, o);
                 if (lane >= uint32_t(o)) upto += q;
             }
-            const uint32_t over = __ballot_sync(~0u, w > 0.0 && before + upto > target), any = __ballot_sync(~0u, w > 0.0);
+            __syncthreads();
+            if (lane == 31) s.warp_sum[warp] = upto;
+            __syncthreads();
+            double all = 0.0, ahead = 0.0;
+            for (uint32_t k = 0; k < kSampleWarps; ++k) {
+                if (k == warp) ahead = all;
+                all += s.warp_sum[k];
+            }
+            if (target < 0.0) target = top_p * all;
+            m = min(most, block_min(i < most && ahead + upto >= target ? i : most - 1, 0).x + 1);
+        }
+        const uint32_t key = s.sorted[m - 1];
+        const uint32_t above = block_min(threadIdx.x < total && s.sorted[threadIdx.x] == key ? threadIdx.x : ~0u, 0).x;       // the first with this key
+        return {sample_value(key), m - above, m >= total || s.sorted[m] != key};
+    }
+
+    // The least logit whose weight is at least min_p.
+    __device__ float least_value(double min_p) {
+        uint64_t lo = sample_key(-3.402823466e38f), hi = sample_key(top);             // hi has weight 1
+        // 32 neighbours of where it should be, then, if it is not among them, 32 keys at a time
+        const float guess = float(double(top) + log(min_p) / inverse);
+        const uint64_t near = sample_key(fminf(fmaxf(guess, -3.402823466e38f), top));
+        const uint64_t begin = near > lo + 16 ? near - 16 : lo, key = begin + lane;
+        uint32_t in = __ballot_sync(~0u, key >= hi || weight(sample_value(uint32_t(key))) >= min_p);
+        if (in && (!(in & 1u) || begin == lo)) return sample_value(uint32_t(min(begin + __ffs(int(in)) - 1, hi)));
+        while (lo < hi) {
+            const uint64_t step = (hi - lo + 31) / 32, at = lo + step * lane;
+            in = __ballot_sync(~0u, at < hi && weight(sample_value(uint32_t(at))) >= min_p);
+            // of the keys looked at, those from the first that is in on are in
+            const uint32_t looked = __popc(__ballot_sync(~0u, at < hi)), f = in ? uint32_t(__ffs(int(in)) - 1) : looked;
+            if (f < looked) hi = lo + step * f;
+            if (f > 0) lo += step * (f - 1) + 1;
+        }
+        return sample_value(uint32_t(hi));
+    }
+
+    __device__ __forceinline__ void put(int64_t token, float log_prob) {
+        p.tokens[row] = token;
+        if (p.log_probs) p.log_probs[row] = log_prob;
+    }
+    __device__ __forceinline__ void put_drawn(int64_t token, float x, double largest, double sum) {
+        put(token, float((double(x) - largest) * inverse - log(sum)));
+    }
+
+    __device__ void run() {
+        const double temperature = p.temperature.at(row), min_p = p.min_p.at(row), top_p = p.top_p.at(row), k = p.top_k.at(row);
+        const float of_block = block_max(load());
+        const bool limited_k = k > 0.0 && k < double(p.vocabulary), limited_m = min_p > 0.0, limited_p = top_p < 1.0;
+        if (!(temperature > 0.0) || k == 1.0 || min_p > 1.0 || top_p <= 0.0) return greedy(of_block);
+        set_temperature(temperature);
+        if (!limited_k && !limited_m && !limited_p) return whole(of_block);
+
+        if (limited_k && threadIdx.x / kSampleRanges < ranks)                        // its ranges, to all blocks
+            cluster.map_shared_rank(s.keys, threadIdx.x / kSampleRanges)[rank * kSampleRanges + threadIdx.x % kSampleRanges] = s.ranges[threadIdx.x % kSampleRanges];
+        const SampleWord *w = exchange({double(of_block), 0, 0});
+        top = float(w[0].a);
+        for (uint32_t r = 1; r < ranks; ++r) top = fmaxf(top, float(w[r].a));
+        if (top == -INFINITY) {
+            if (rank == 0 && threadIdx.x == 0) put(-1, -INFINITY);
+            return;
+        }
+        float from_k = -INFINITY;                            // at least k tokens lie from here on
+        if (limited_k && k <= ranks * kSampleRanges && top < INFINITY) {
+            if (threadIdx.x >= ranks * kSampleRanges) s.keys[threadIdx.x] = 0;
+            s.sorted[threadIdx.x] = 0;
+            sort_keys(ranks * kSampleRanges);
+            const uint32_t key = s.sorted[uint32_t(k) - 1];
+            if (key) from_k = sample_value(key);
+        }
+        if (top == INFINITY) {
+            only_infinite();
+            top = 0.0f;
+        }
+        const float low = limited_m ? least_value(min_p) : -3.402823466e38f;         // tokens below have less than min_p, or no weight
+        Prefix kept = {low, 0, true};
+        bool done = false;
+        if (limited_k) {
+            const float cut = fmaxf(low, from_k);
+            const uint32_t total = sort_candidates([&](float x) { return x >= cut; });
+            if (total <= kSampleList) {
+                kept = prefix_of(total, uint32_t(fmin(k, double(total))), top_p, -1.0);
+                done = true;
+            } else {
+                reach_number(cut, k, kept);                  // (or there are fewer than k from `low` on: all of them)
+            }
+        }
+        if (limited_p && !done) {
+            // what top_k and min_p leave: the tokens above the edge (from the edge on), and so many of it
+            const float from = kept.whole ? kept.edge : sample_value(sample_key(kept.edge) + 1);
+            const double sum_here = block_sum(thread_sum([&](float x) { return x >= from; }));
+            const SampleWord *q = exchange({sum_here, 0, 0});
+            double sum = 0.0;
+            for (uint32_t r = 0; r < ranks; ++r) sum += q[r].a;
+            const double at_edge = kept.whole ? 0.0 : weight(kept.edge), target = top_p * (sum + kept.ties * at_edge);
+            if (!kept.whole && sum < target) {               // it ends within the edge
+                kept.ties = uint32_t(fewest(sum, at_edge, target, kept.ties));
+            } else {
+                // all tokens below (1 - top_p) of the mean weight together do not make up what may be left out
+                float cut = float(double(top) + log((1.0 - top_p) * sum / p.vocabulary) / inverse);
+                cut -= 1e-5f * fabsf(cut) + 1e-5f / float(inverse);                // (below it, whatever the rounding)
+                cut = cut == cut ? fminf(fmaxf(cut, from), top) : from;
+                reach_weight(cut, target, sum, kept);
+            }
+        }
+        draw(kept);
+    }
+
+    // The lowest token among those with the largest logit.
+    __device__ void greedy(float of_block) {
+        uint32_t token = ~0u;
+#pragma unroll 1
+        for (int j = 0; j < p.packs; ++j) {
+            const Packed q = held[j * kSampleThreads];
+#pragma unroll
+            for (int e = 0; e < kVec; ++e)
+                if (to_f32<T>(q.v[e]) == of_block) token = min(token, uint32_t(at(j) + e));
+        }
+        const uint32_t lowest = block_min(token, 0).x;
+        const SampleWord *w = exchange({double(of_block), lowest, 0});
+        uint32_t best = 0;
+        for (uint32_t k = 1; k < ranks; ++k)
+            if (w[k].a > w[best].a) best = k;
+        if (rank == 0 && threadIdx.x == 0) {
+            if (w[best].a == -INFINITY) put(-1, -INFINITY);
+            else put(w[best].b, 0.0f);
+        }
+    }
+
+    // Without limits: weights relative to the block's own largest logit.
+    __device__ void whole(float of_block) {
+        top = of_block;
+        if (top == INFINITY) {
+            only_infinite();
+            top = 0.0f;
+        }
+        const double sum = top == -INFINITY ? 0.0 : block_sum(thread_sum([](float) { return true; }));
+        const SampleWord *w = exchange({sum, __float_as_uint(of_block), 0});
+        float largest = -INFINITY;
+        for (uint32_t k = 0; k < ranks; ++k) largest = fmaxf(largest, __uint_as_float(w[k].b));
+        if (largest == -INFINITY) {
+            if (rank == 0 && threadIdx.x == 0) put(-1, -INFINITY);
+            return;
+        }
+        const float own = top;
+        top = largest == INFINITY ? 0.0f : largest;
+        // lane k: what block k adds, relative to the row's largest
+        const float m = __uint_as_float(w[lane % ranks].b);
+        const double scale = m == -INFINITY || (largest == INFINITY && m < INFINITY) ? 0.0 : m == largest ? 1.0 : weight(m);
+        const Place place = place_of(lane < ranks ? w[lane % ranks].a * scale : 0.0);
+        if (place.who != rank) return;
+        const double largest_weighed = top;
+        top = own;
+        find({-3.402823466e38f, 0, true}, 0, 0.0, (place.target - place.before) / __shfl_sync(~0u, scale, place.who), place.total, largest_weighed);
+    }
+
+    // Where a random number lies among the lanes' sums: the first lane with which they pass it (the last one that adds anything, if rounding
+    // leaves none), and what the lanes before it add up to.
+    struct Place {
+        uint32_t who;
+        double before, target, total;
+    };
+    __device__ Place place_of(double add) const {
+        double upto = add;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const double q = __shfl_up_sync(~0u, upto, o);
+            if (lane >= uint32_t(o)) upto += q;
+        }
+        Place place;
+        place.total = __shfl_sync(~0u, upto, 31);
+        place.target = uniform() * place.total;
+        const uint32_t over = __ballot_sync(~0u, add > 0.0 && upto > place.target), any = __ballot_sync(~0u, add > 0.0);
+        place.who = over ? __ffs(int(over)) - 1 : any ? 31 - __clz(int(any)) : 0;
+        place.before = __shfl_sync(~0u, upto - add, place.who);
+        return place;
+    }
+
+    __device__ __forceinline__ double uniform() const {
+        const double u = p.uniform_f64 ? static_cast<const double *>(p.uniform)[row] : double(static_cast<const float *>(p.uniform)[row]);
+        return u > 0.0 ? u : 0.0;
+    }
+
+    // Draws from a prefix.
+    __device__ void draw(const Prefix &kept) {
+        uint32_t ties = 0;
+        if (!kept.whole) {
+            each([&](float x) { ties += x == kept.edge; });
+            ties = __reduce_add_sync(~0u, ties);
+        }
+        const double at_edge = kept.whole ? 0.0 : weight(kept.edge);
+        const double sum = block_sum(thread_sum([&](float x) { return kept.whole ? x >= kept.edge : x > kept.edge; }));
+        if (lane == 0) s.warp_ties[warp] = ties;
+        __syncthreads();
+        uint32_t here = 0;
+        for (int k = 0; k < kSampleWarps; ++k) here += s.warp_ties[k];
+        const SampleWord *w = exchange({sum, here, 0});
+        // lane k: what block k adds, with those of the edge's tokens that belong to the prefix
+        const uint32_t tied = lane < ranks ? w[lane].b : 0;
+        uint32_t upto = tied;
+#pragma unroll
+        for (int o = 1; o < kSampleMaxCluster; o <<= 1) {
+            const uint32_t q = __shfl_up_sync(~0u, upto, o);
+            if (lane >= uint32_t(o)) upto += q;
+        }
+        const Place place = place_of(lane < ranks ? with_edge(kept, w[lane].a, upto - tied, tied, at_edge) : 0.0);
+        const uint32_t ties_before = __shfl_sync(~0u, upto - tied, place.who);
+        if (place.who == rank) find(kept, ties_before, at_edge, place.target - place.before, place.total, top);
+    }
+    // A sum with those of the edge's `here` tokens that belong to the prefix, `before` of them lying ahead.
+    __device__ __forceinline__ static double with_edge(const Prefix &kept, double sum, uint32_t before, uint32_t here, double at_edge) {
+        return kept.whole || before >= kept.ties ? sum : sum + double(min(kept.ties - before, here)) * at_edge;
+    }
+
+    // The block's token with which the kept weights add up to more than the target; s.warp_sum and s.warp_ties are those of its warps.
+    __device__ void find(const Prefix &kept, uint32_t ties_ahead, double at_edge, double target, double total, double largest) {
+        double ahead = 0.0, before = 0.0;
+        uint32_t ties_before = ties_ahead, who = 0;
+        bool past = false;
+        for (uint32_t k = 0; k < kSampleWarps && !past; ++k) {
+            const uint32_t here = kept.whole ? 0 : s.warp_ties[k];
+            const double add = with_edge(kept, s.warp_sum[k], ties_ahead, here, at_edge);
+            if (add > 0.0) {
+                who = k;
+                before = ahead;
+                ties_before = ties_ahead;
+                past = ahead + add > target;
+            }
+            ahead += add;
+            ties_ahead += here;
+        }
+        if (who != warp) return;
+        // the warp's tokens, a pack of each lane at a time: the lane in which the sum passes the target, then its token
+        int token = -1;
+        float chosen = 0.0f;
+        past = false;
+#pragma unroll 1
+        for (int j = 0; j < p.packs && !past; ++j) {
+            const Packed pack = held[j * kSampleThreads];
+            auto value = [&](int e) { return to_f32<T>(pack.v[e]); };
+            double w[kVec], sum = 0.0;
+            uint32_t tied = 0;
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) tied += !kept.whole && value(e) == kept.edge;
+            uint32_t upto_ties = tied;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const uint32_t q = __shfl_up_sync(~0u, upto_ties, o);
+                if (lane >= uint32_t(o)) upto_ties += q;
+            }
+            uint32_t seen = ties_before + upto_ties - tied;
+#pragma unroll
+            for (int e = 0; e < kVec; ++e) {
+                const float x = value(e);
+                const bool at_the_edge = !kept.whole && x == kept.edge;
+                w[e] = x > kept.edge || (x == kept.edge && (kept.whole || seen < kept.ties)) ? weight(x) : 0.0;
+                seen += at_the_edge;
+                sum += w[e];
+            }
+            double upto = sum;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const double q = __shfl_up_sync(~0u, upto, o);
+                if (lane >= uint32_t(o)) upto += q;
+            }
+            const uint32_t over = __ballot_sync(~0u, sum > 0.0 && before + upto > target), any = __ballot_sync(~0u, sum > 0.0);
             past = over != 0;
-            const int at = over ? __ffs(int(over)) - 1 : any ? 31 - __clz(int(any)) : -1;
-            if (at >= 0) {
-                token = first + i0 + at;
-                chosen = __shfl_sync(~0u, v, at);
+            const int who_lane = over ? __ffs(int(over)) - 1 : any ? 31 - __clz(int(any)) : -1;
+            if (who_lane >= 0) {
+                // (the lane's first token past the target, or its last one with a weight)
+                double run = before + upto - sum;
+                int e_found = -1;
+#pragma unroll
+                for (int e = 0; e < kVec; ++e) {
+                    const bool open = e_found < 0 || !(run > target);
+                    run += w[e];
+                    if (open && w[e] > 0.0) e_found = e;
+                }
+                float x = 0.0f;
+#pragma unroll
+                for (int e = 0; e < kVec; ++e)
+                    if (e == e_found) x = value(e);
+                token = __shfl_sync(~0u, at(j) + e_found, who_lane);
+                chosen = __shfl_sync(~0u, x, who_lane);
             }
             before += __shfl_sync(~0u, upto, 31);
+            ties_before += __shfl_sync(~0u, upto_ties, 31);
         }
-        if (lane == 0) put(token, float((chosen == top ? 0.0 : (double(chosen) - double(top)) * inverse) - log(total)));
+        if (lane == 0) put_drawn(token, chosen, largest, total);
     }
 };
 
 template <typename T>
-__global__ void __launch_bounds__(kSampleThreads) tcu_sample_kernel(const SampleParams p) {
+__global__ void __launch_bounds__(kSampleThreads, 4) tcu_sample_kernel(const SampleParams p) {
     extern __shared__ __align__(16) uint8_t held[];
     __shared__ SampleShared shared;
-    Sampler<T>(p, shared, reinterpret_cast<T *>(held)).run();
+    Sampler<T>(p, shared, held).run();
 }
 
 }  // namespace tcu
