@@ -32,7 +32,7 @@ constexpr int kSampleRanges = 32;                     // of a block: eight lanes
 constexpr uint32_t kMostVocabulary = 1u << 18;
 constexpr double kSampleFixed = 4398046511104.0;      // 2^42
 constexpr int kSampleLimb = 14;
-static_assert(kSampleList == kSampleThreads && kSampleRanges * kSampleMaxCluster <= kSampleList, "a candidate, or a range, each thread");
+static_assert(kSampleList == kSampleThreads && kSampleRanges * kSampleMaxCluster <= kSampleThreads, "a candidate, or a range, each thread");
 
 // A setting of all rows, or one for each.
 template <typename T>
@@ -55,12 +55,12 @@ struct SampleParams {
     float *log_probs;
 };
 
-// 2^(j/64), by the exponential's series
+// 2^(j/32), by the exponential's series
 struct SampleTable {
-    double v[64];
+    double v[32];
     constexpr SampleTable() : v() {
-        for (int j = 0; j < 64; ++j) {
-            const double x = j * (0.69314718055994530942 / 64);
+        for (int j = 0; j < 32; ++j) {
+            const double x = j * (0.69314718055994530942 / 32);
             double term = 1.0, sum = 1.0;
             for (int k = 1; k < 24; ++k) {
                 term *= x / k;
@@ -84,16 +84,19 @@ struct SampleFound {
 };
 
 struct SampleShared {
-    double table[64];
+    double table[32];
     SampleWord slots[2][kSampleMaxCluster];
     SampleFound found[2];
     double warp_sum[kSampleWarps];
     uint64_t warp_u64[kSampleWarps];
     uint32_t warp_u32[2][kSampleWarps], warp_ties[kSampleWarps];
     float warp_max[kSampleWarps];
-    uint32_t list[kSampleList];            // keys of this block's candidates
+    uint32_t count;                        // of this block's candidates
+    uint2 list[kSampleList];               // their keys and tokens
+    uint2 all[kSampleList], sorted[kSampleList];           // of all blocks' candidates; in falling order
     uint32_t ranges[kSampleRanges];        // keys of the largest logits of its ranges
-    uint32_t keys[kSampleList], sorted[kSampleList];       // of all blocks' candidates, or ranges
+    uint32_t all_ranges[kSampleMaxCluster * kSampleRanges];
+    float from_k;
     uint32_t hist[kSampleBins];            // or three limbs of kSampleFine bins
 };
 
@@ -104,6 +107,8 @@ __device__ __forceinline__ uint32_t sample_key(float v) {        // the order of
 __device__ __forceinline__ float sample_value(uint32_t key) {
     return __uint_as_float(key ^ (key & 0x80000000u ? 0x80000000u : 0xffffffffu));
 }
+
+constexpr uint32_t kKeyNothing = 0x007fffffu;                    // that of minus infinity
 
 // NaN as minus infinity, no zero below zero.
 __device__ __forceinline__ float sane(float v) { return fmaxf(v, -INFINITY) + 0.0f; }
@@ -135,7 +140,7 @@ struct Sampler {
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     int first;                             // token of the block's first element
     float top = 0.0f;                      // what weights are relative to
-    double inverse = 1.0, sixty_fourths = 1.0;      // 1 / temperature; 64 log2(e) / temperature
+    double inverse = 1.0, parts = 1.0;         // 1 / temperature; 32 log2(e) / temperature
 
     __device__ Sampler(const SampleParams &p, SampleShared &s, void *held) : p(p), s(s), held(static_cast<Packed *>(held) + threadIdx.x), cluster(cooperative_groups::this_cluster()) {
         rank = cluster.block_rank();
@@ -154,27 +159,26 @@ struct Sampler {
         }
     }
 
-    // exp((x - top) / temperature), by table (P. T. P. Tang, 1989): with y = 64 log2(e) (x - top) / temperature = k + r, k the nearest integer,
-    // 2^(y/64) = 2^floor(k/64) 2^(k mod 64 / 64) (1 + q + q^2/2 + q^3/6 + q^4/24), q = r ln 2 / 64: |q| < 0.0055, what is left out is below
-    // 5e-14 of it.  Zero below 2^-1000; 1 for the top itself.
+    // exp((x - top) / temperature), by table (P. T. P. Tang, 1989): with y = 32 log2(e) (x - top) / temperature = k + r, k the nearest integer,
+    // 2^(y/32) = 2^floor(k/32) 2^(k mod 32 / 32) exp(q), q = r ln 2 / 32 below 0.011: what the series leaves out is below 1.3e-12 of it.  (A table of 64
+    // needs no shorter series, and twice the time to be read.)  Zero below 2^-1000; exactly 1 for the top itself.
     __device__ __forceinline__ double weight(float x) const {
-        const double y = (double(x) - double(top)) * sixty_fourths;
-        constexpr double kMagic = 6755399441055744.0, kLn = 0.69314718055994530942 / 64;
+        const double y = (double(x) - double(top)) * parts;
+        constexpr double kMagic = 6755399441055744.0, kLn = 0.69314718055994530942 / 32;
         const double t = y + kMagic;
         const int k = __double2loint(t);
-        const double q = (y - (t - kMagic)) * kLn;
-        const double m = s.table[k & 63];
-        double poly = fma(q, 1.0 / 24, 1.0 / 6);
-        poly = fma(q, poly, 0.5);
-        poly = fma(q * q, poly, q);
-        const double w = fma(m, poly, m);
-        const bool far = uint32_t(__double2hiint(y)) > 0xC0EF4000u;                            // y below -64000
-        return far ? 0.0 : __hiloint2double(__double2hiint(w) + (k >> 6) * 1048576, __double2loint(w));
+        const double r = y - (t - kMagic), m = s.table[k & 31];
+        double poly = fma(r, kLn * kLn * kLn * kLn / 24, kLn * kLn * kLn / 6);
+        poly = fma(r, poly, kLn * kLn / 2);
+        poly = fma(r, poly, kLn);
+        const double w = fma(m, r * poly, m);
+        const bool far = uint32_t(__double2hiint(y)) > 0xC0DF4000u;                            // y below -32000
+        return far ? 0.0 : __hiloint2double(__double2hiint(w) + (k >> 5) * 1048576, __double2loint(w));
     }
     __device__ __forceinline__ uint64_t fixed(float x) const { return uint64_t(__double2ll_rn(weight(x) * kSampleFixed)); }
     __device__ __forceinline__ void set_temperature(double temperature) {
         inverse = 1.0 / temperature;
-        sixty_fourths = inverse * (64 * 1.4426950408889634074);
+        parts = inverse * (32 * 1.4426950408889634074);
     }
 
     // Every block's word, at every block.  All threads call it; what is told has to be ready in thread 0's to kSampleMaxCluster - 1's `mine`.
@@ -246,7 +250,7 @@ struct Sampler {
     __device__ float load() {
         const T *from = static_cast<const T *>(p.logits) + uint64_t(row) * p.stride;
         first = int(rank * kSampleThreads * p.packs * kVec) - int(reinterpret_cast<uintptr_t>(from) % 16 / sizeof(T));   // (what lies ahead of the row on its first 16 bytes)
-        if (threadIdx.x < 64) s.table[threadIdx.x] = kSampleTable.v[threadIdx.x];
+        if (threadIdx.x < 32) s.table[threadIdx.x] = kSampleTable.v[threadIdx.x];
         float most = -INFINITY;
 #pragma unroll 4
         for (int j = 0; j < p.packs; ++j) {
@@ -420,8 +424,13 @@ struct Sampler {
     // The prefix that ends in a bin: with `left` of its tokens' number, or weight.
     template <bool WEIGHTS>
     __device__ Prefix in_bin(float cut, float scale, int which, double left) {
-        const uint32_t total = sort_candidates([&](float x) { return bin(x, cut, scale) == which; });
-        if (total <= kSampleList) return WEIGHTS ? prefix_of(total, total, 0.0, left) : prefix_of(total, uint32_t(fmin(left, double(total))), 1.0, 0.0);
+        const uint32_t total = list_candidates([&](float x) { return bin(x, cut, scale) == which; });
+        if (total <= kSampleList) {
+            sort_candidates(total);
+            const Prefix out = prefix_of(total, WEIGHTS ? reach_sorted(total, 1.0, left) : uint32_t(fmin(left, double(total))));
+            cluster.sync();                                  // (nobody lists others before all have read these)
+            return out;
+        }
         uint32_t lo = ~0u, hi_not = ~0u;                     // keys of the bin: from lo to ~hi_not
         each([&](float x) {
             if (bin(x, cut, scale) == which) {
@@ -432,9 +441,9 @@ struct Sampler {
         const uint2 ends = cluster_min(lo, hi_not);
         lo = ends.x;
         uint32_t hi = ~ends.y;
-        double before = 0.0, one = WEIGHTS ? double(fixed(sample_value(hi))) : 1.0, target = WEIGHTS ? left * kSampleFixed : left, many = total;
-        while (lo < hi) {
-            const int bits = 32 - __clz(hi - lo), shift = bits > kSampleFineBits ? bits - kSampleFineBits : 0;
+        double before = 0.0, one = WEIGHTS ? double(fixed(sample_value(hi))) : 1.0, target = WEIGHTS ? left * kSampleFixed : left, many = 1.0;
+        do {
+            const int bits = 32 - __clz(int(hi - lo)), shift = bits > kSampleFineBits ? bits - kSampleFineBits : 0;
             auto bin_of = [&](float x) {
                 const uint32_t key = sample_key(x);
                 return key < lo || key > hi ? -1 : int((hi - key) >> shift);
@@ -450,7 +459,7 @@ struct Sampler {
             }
             one = WEIGHTS ? double(fixed(sample_value(hi))) : 1.0;
             many = one > 0.0 ? double(g.bin < 0 ? 1 : g.in) / one : 1.0;
-        }
+        } while (lo < hi);
         const uint32_t most = uint32_t(fmax(rint(many), 1.0)), ties = uint32_t(fewest(before, one, target, most));
         return {sample_value(hi), ties, ties >= most};
     }
@@ -463,85 +472,116 @@ struct Sampler {
         return c;
     }
 
-    // Sorts s.keys, of which `total` are above 0, into s.sorted, falling.
-    __device__ void sort_keys(uint32_t total) {
-        __syncthreads();
-        const uint32_t key = s.keys[threadIdx.x];
-        uint32_t before = 0;                                 // those ahead of this one: larger ones, and equal ones of lower threads
-        const uint4 *keys = reinterpret_cast<const uint4 *>(s.keys);
-        for (uint32_t i = 0; i < kSampleList / 4 && 4 * i < total; ++i) {
-            const uint4 q = keys[i];
-            const uint32_t k = 4 * i;
-            before += (q.x > key || (q.x == key && k < threadIdx.x)) + (q.y > key || (q.y == key && k + 1 < threadIdx.x)) +
-                      (q.z > key || (q.z == key && k + 2 < threadIdx.x)) + (q.w > key || (q.w == key && k + 3 < threadIdx.x));
-        }
-        if (key) s.sorted[before] = key;
-        __syncthreads();
-    }
-    // The candidates, if the row has no more than kSampleList of them: their number; s.sorted holds their keys, falling, at every block.
+    // Lists this block's candidates, in any order, and tells how many the row has of them, or that they are more than kSampleList.
     template <typename Is>
-    __device__ uint32_t sort_candidates(Is is) {
-        uint32_t mine = 0;
-        each([&](float x) { mine += is(x); });
-        uint32_t upto = mine;
+    __device__ uint32_t list_candidates(Is is) {
+        if (threadIdx.x == 0) s.count = 0;
+        __syncthreads();
+#pragma unroll 1
+        for (int j = 0; j < p.packs; ++j) {
+            const Packed q = held[j * kSampleThreads];
 #pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const uint32_t q = __shfl_up_sync(~0u, upto, o);
-            if (lane >= uint32_t(o)) upto += q;
+            for (int e = 0; e < kVec; ++e)
+                if (is(to_f32<T>(q.v[e]))) list_one(to_f32<T>(q.v[e]), at(j) + e);
         }
         __syncthreads();
-        if (lane == 31) s.warp_u32[0][warp] = upto;
-        __syncthreads();
-        uint32_t to = upto - mine, here = 0;
-        for (uint32_t k = 0; k < kSampleWarps; ++k) {
-            if (k < warp) to += s.warp_u32[0][k];
-            here += s.warp_u32[0][k];
-        }
-        if (here <= kSampleList && mine)
-            each([&](float x) {
-                if (is(x)) s.list[to++] = sample_key(x);
-            });
-        const SampleWord *w = exchange({0.0, here, 0});
+        return count_candidates(0.0, 0.0, nullptr, nullptr);
+    }
+    __device__ __forceinline__ void list_one(float x, int token) {
+        if (*const_cast<volatile uint32_t *>(&s.count) > kSampleList) return;                // too many: no more need to be counted
+        const uint32_t to = atomicAdd(&s.count, 1u);
+        if (to < kSampleList) s.list[to] = make_uint2(sample_key(x), uint32_t(token));
+    }
+    // The row's number of candidates, and its sums of two values.
+    __device__ uint32_t count_candidates(double a, double b, double *sum_a, double *sum_b) {
+        const SampleWord *w = exchange({a, s.count, 0});
         uint32_t total = 0;
         for (uint32_t k = 0; k < ranks; ++k) total += w[k].b;
-        if (total > kSampleList) return total;
-        uint32_t from = threadIdx.x, key = 0;
-        if (threadIdx.x < total) {
-            uint32_t k = 0;
-            while (from >= w[k].b) from -= w[k++].b;
-            key = cluster.map_shared_rank(s.list, k)[from];
+        if (sum_a) {
+            *sum_a = 0.0;
+            for (uint32_t k = 0; k < ranks; ++k) *sum_a += w[k].a;
+            const SampleWord *q = exchange({b, 0, 0});
+            *sum_b = 0.0;
+            for (uint32_t k = 0; k < ranks; ++k) *sum_b += q[k].a;
         }
-        s.keys[threadIdx.x] = key;
-        sort_keys(total);
-        // (nobody writes its list again before all have read it)
-        cluster.sync();
         return total;
     }
-    // Of the first `most` of `total` sorted candidates, for top_p below 1, those whose weights reach the target (below 0: top_p of theirs).
-    __device__ Prefix prefix_of(uint32_t total, uint32_t most, double top_p, double target) {
-        uint32_t m = most;
-        if (top_p < 1.0) {
-            const uint32_t i = threadIdx.x;
-            double upto = i < most ? weight(sample_value(s.sorted[i])) : 0.0;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const double q = __shfl_up_sync(~0u, upto, o);
-                if (lane >= uint32_t(o)) upto += q;
+    // All blocks' `total` candidates (no more than kSampleList) to s.sorted, in falling order, the lower token first among equals.
+    __device__ void sort_candidates(uint32_t total) {
+        uint2 mine = make_uint2(0, 0);
+        if (threadIdx.x < total) {
+            uint32_t k = 0, from = threadIdx.x;
+            for (uint32_t n = *cluster.map_shared_rank(&s.count, 0); from >= n; n = *cluster.map_shared_rank(&s.count, k)) {
+                from -= n;
+                ++k;
             }
-            __syncthreads();
-            if (lane == 31) s.warp_sum[warp] = upto;
-            __syncthreads();
-            double all = 0.0, ahead = 0.0;
-            for (uint32_t k = 0; k < kSampleWarps; ++k) {
-                if (k == warp) ahead = all;
-                all += s.warp_sum[k];
-            }
-            if (target < 0.0) target = top_p * all;
-            m = min(most, block_min(i < most && ahead + upto >= target ? i : most - 1, 0).x + 1);
+            mine = cluster.map_shared_rank(s.list, k)[from];
         }
-        const uint32_t key = s.sorted[m - 1];
-        const uint32_t above = block_min(threadIdx.x < total && s.sorted[threadIdx.x] == key ? threadIdx.x : ~0u, 0).x;       // the first with this key
-        return {sample_value(key), m - above, m >= total || s.sorted[m] != key};
+        s.all[threadIdx.x] = mine;
+        __syncthreads();
+        if (threadIdx.x < total) {
+            uint32_t before = 0;
+            for (uint32_t i = 0; i < total; ++i) {
+                const uint2 q = s.all[i];
+                before += q.x > mine.x || (q.x == mine.x && q.y < mine.y);
+            }
+            s.sorted[before] = mine;
+        }
+        __syncthreads();
+    }
+    // How many of the first `most` sorted candidates it takes until their weights reach the target (below 0: top_p of theirs).
+    __device__ uint32_t reach_sorted(uint32_t most, double top_p, double target) {
+        const uint32_t i = threadIdx.x;
+        double all, upto = i < most ? weight(sample_value(s.sorted[i].x)) : 0.0;
+        upto = block_prefix(upto, all);
+        if (target < 0.0) target = top_p * all;
+        return min(most, block_min(i < most && upto >= target ? i : most - 1, 0).x + 1);
+    }
+    // The sum of the threads' values up to each thread's, and of all.
+    __device__ double block_prefix(double x, double &all) {
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const double q = __shfl_up_sync(~0u, x, o);
+            if (lane >= uint32_t(o)) x += q;
+        }
+        __syncthreads();
+        if (lane == 31) s.warp_sum[warp] = x;
+        __syncthreads();
+        double ahead = 0.0;
+        all = 0.0;
+        for (uint32_t k = 0; k < kSampleWarps; ++k) {
+            if (k == warp) ahead = all;
+            all += s.warp_sum[k];
+        }
+        return ahead + x;
+    }
+    // The prefix of the first m of `total` sorted candidates, which hold all tokens of their last one's logit.
+    __device__ Prefix prefix_of(uint32_t total, uint32_t m) {
+        const uint32_t key = s.sorted[m - 1].x;
+        const uint32_t above = block_min(threadIdx.x < total && s.sorted[threadIdx.x].x == key ? threadIdx.x : ~0u, 0).x;       // the first with this key
+        return {sample_value(key), m - above, m >= total || s.sorted[m].x != key};
+    }
+    // Draws from candidates that hold all tokens to be kept: the first `most` of them, and of these those that reach the target.  By one block; the
+    // others lend it their lists.
+    __device__ void draw_listed(uint32_t total, uint32_t most, double top_p, double target) {
+        if (rank == 0) {
+            sort_candidates(total);
+            const uint32_t m = top_p < 1.0 ? reach_sorted(most, top_p, target) : most, i = threadIdx.x;
+            // in the order of tokens
+            const uint2 mine = i < m ? s.sorted[i] : make_uint2(0, 0);
+            if (i < m) {
+                uint32_t before = 0;
+                for (uint32_t k = 0; k < m; ++k) before += s.sorted[k].y < mine.y;
+                s.all[before] = mine;
+            }
+            __syncthreads();
+            const float x = i < m ? sample_value(s.all[i].x) : 0.0f;
+            double sum;
+            const double w = i < m ? weight(x) : 0.0, upto = block_prefix(w, sum), target_u = uniform() * sum;
+            const uint2 found = block_min(w > 0.0 && upto > target_u ? i : ~0u, w > 0.0 ? ~i : ~0u);
+            if (i == (found.x != ~0u ? found.x : ~found.y)) put_drawn(s.all[i].y, x, top, sum);
+        }
+        cluster.sync();
     }
 
     // The least logit whose weight is at least min_p.
@@ -580,8 +620,8 @@ struct Sampler {
         set_temperature(temperature);
         if (!limited_k && !limited_m && !limited_p) return whole(of_block);
 
-        if (limited_k && threadIdx.x / kSampleRanges < ranks)                        // its ranges, to all blocks
-            cluster.map_shared_rank(s.keys, threadIdx.x / kSampleRanges)[rank * kSampleRanges + threadIdx.x % kSampleRanges] = s.ranges[threadIdx.x % kSampleRanges];
+        if (threadIdx.x / kSampleRanges < ranks)                     // its ranges, to all blocks
+            cluster.map_shared_rank(s.all_ranges, threadIdx.x / kSampleRanges)[rank * kSampleRanges + threadIdx.x % kSampleRanges] = s.ranges[threadIdx.x % kSampleRanges];
         const SampleWord *w = exchange({double(of_block), 0, 0});
         top = float(w[0].a);
         for (uint32_t r = 1; r < ranks; ++r) top = fmaxf(top, float(w[r].a));
@@ -589,41 +629,54 @@ struct Sampler {
             if (rank == 0 && threadIdx.x == 0) put(-1, -INFINITY);
             return;
         }
-        float from_k = -INFINITY;                            // at least k tokens lie from here on
-        if (limited_k && k <= ranks * kSampleRanges && top < INFINITY) {
-            if (threadIdx.x >= ranks * kSampleRanges) s.keys[threadIdx.x] = 0;
-            s.sorted[threadIdx.x] = 0;
-            sort_keys(ranks * kSampleRanges);
-            const uint32_t key = s.sorted[uint32_t(k) - 1];
-            if (key) from_k = sample_value(key);
-        }
+        // from here on lie at least k tokens (for top_p alone: so many that most of them can be sorted)
+        float from_k = top < INFINITY && (limited_k || limited_p) ? from_ranges(limited_k ? k : 0.6 * ranks * kSampleRanges) : -INFINITY;
         if (top == INFINITY) {
             only_infinite();
             top = 0.0f;
         }
         const float low = limited_m ? least_value(min_p) : -3.402823466e38f;         // tokens below have less than min_p, or no weight
         Prefix kept = {low, 0, true};
-        bool done = false;
         if (limited_k) {
             const float cut = fmaxf(low, from_k);
-            const uint32_t total = sort_candidates([&](float x) { return x >= cut; });
-            if (total <= kSampleList) {
-                kept = prefix_of(total, uint32_t(fmin(k, double(total))), top_p, -1.0);
-                done = true;
-            } else {
-                reach_number(cut, k, kept);                  // (or there are fewer than k from `low` on: all of them)
-            }
+            const uint32_t total = list_candidates([&](float x) { return x >= cut; });
+            if (total <= kSampleList) return draw_listed(total, uint32_t(fmin(k, double(total))), top_p, -1.0);
+            reach_number(cut, k, kept);                      // (or there are fewer than k from `low` on: all of them)
+        } else if (limited_m) {
+            const uint32_t total = list_candidates([&](float x) { return x >= low; });
+            if (total <= kSampleList) return draw_listed(total, total, top_p, -1.0);
         }
-        if (limited_p && !done) {
+        if (limited_p) {
             // what top_k and min_p leave: the tokens above the edge (from the edge on), and so many of it
             const float from = kept.whole ? kept.edge : sample_value(sample_key(kept.edge) + 1);
-            const double sum_here = block_sum(thread_sum([&](float x) { return x >= from; }));
-            const SampleWord *q = exchange({sum_here, 0, 0});
-            double sum = 0.0;
-            for (uint32_t r = 0; r < ranks; ++r) sum += q[r].a;
+            // their weight, and that of the largest ones, which are listed
+            const float cut_list = fmaxf(from, from_k);
+            double sums[2] = {0.0, 0.0}, large = 0.0, sum, sum_large;
+            if (threadIdx.x == 0) s.count = 0;
+            __syncthreads();
+#pragma unroll 1
+            for (int j = 0; j < p.packs; ++j) {
+                const Packed q = held[j * kSampleThreads];
+#pragma unroll
+                for (int e = 0; e < kVec; ++e) {
+                    const float x = to_f32<T>(q.v[e]);
+                    if (x >= from) {
+                        const double weighs = weight(x);
+                        sums[e & 1] += weighs;
+                        if (x >= cut_list) {
+                            large += weighs;
+                            list_one(x, at(j) + e);
+                        }
+                    }
+                }
+            }
+            const double sum_here = block_sum(sums[0] + sums[1]), large_here = block_sum(large);
+            const uint32_t total = count_candidates(sum_here, large_here, &sum, &sum_large);
             const double at_edge = kept.whole ? 0.0 : weight(kept.edge), target = top_p * (sum + kept.ties * at_edge);
             if (!kept.whole && sum < target) {               // it ends within the edge
                 kept.ties = uint32_t(fewest(sum, at_edge, target, kept.ties));
+            } else if (total <= kSampleList && sum_large >= target * (1.0 + 1e-9)) {
+                return draw_listed(total, total, top_p, target);
             } else {
                 // all tokens below (1 - top_p) of the mean weight together do not make up what may be left out
                 float cut = float(double(top) + log((1.0 - top_p) * sum / p.vocabulary) / inverse);
@@ -633,6 +686,28 @@ struct Sampler {
             }
         }
         draw(kept);
+    }
+
+    // A logit from which on at least k tokens lie, from the largest logits of the row's ranges: by their keys' upper half; minus infinity if there are
+    // fewer ranges.
+    __device__ float from_ranges(double k) {
+        const uint32_t n = ranks * kSampleRanges;
+        if (k > n) return -INFINITY;
+        if (warp == 0) {
+            uint32_t mine[kSampleMaxCluster];
+#pragma unroll
+            for (uint32_t r = 0; r < kSampleMaxCluster; ++r) mine[r] = r < ranks ? s.all_ranges[r * kSampleRanges + lane] >> 16 : 0;
+            uint32_t from = 0;
+            for (uint32_t bit = 1u << 15; bit; bit >>= 1) {
+                uint32_t count = 0;
+#pragma unroll
+                for (uint32_t r = 0; r < kSampleMaxCluster; ++r) count += mine[r] >= (from | bit);
+                if (double(__reduce_add_sync(~0u, count)) >= k) from |= bit;
+            }
+            if (lane == 0) s.from_k = from ? sample_value(max(from << 16, kKeyNothing + 1)) : -INFINITY;
+        }
+        __syncthreads();
+        return s.from_k;
     }
 
     // The lowest token among those with the largest logit.
