@@ -1,11 +1,12 @@
 #!/usr/bin/env python3
 """A small language model on the library's operators, trained and then served.
 
-    python examples/linear_lm.py [--steps 160]
+    python examples/linear_lm.py [--steps 160] [--gated] [--temperature 0.7]
 
 Token embedding (its table also gives the logits), layers of linear attention with a decay for each head, torch for the
-projections between them.  Training runs lookup, attention and the gradients of both; serving takes prompts of different
-lengths packed one behind the other, keeps their states in a pool, and goes on one token at a time.  The sequences follow a
+projections between them; with --gated, every second layer is a layer norm and a gated recurrence instead.  Training runs lookup, attention and the gradients of both; serving takes prompts of different
+lengths packed one behind the other, keeps their states in a pool, and goes on one token at a time: the likeliest, or one
+drawn from the likely ones.  The sequences follow a
 fixed permutation of the vocabulary, so that the model can learn every next token.
 """
 from __future__ import annotations
@@ -39,13 +40,44 @@ class Layer(torch.nn.Module):
     def out(self, x: torch.Tensor, o: torch.Tensor) -> torch.Tensor:
         return x + o.flatten(-2) @ self.back.to(x.dtype)
 
+    def whole(self, x: torch.Tensor, offsets, keep_state: bool):
+        o, last = api.linear_attention(*self.qkv(x), self.log_decay, offsets=offsets, output_final_state=keep_state)
+        return self.out(x, o), last
+
+    def token(self, x: torch.Tensor, pool: torch.Tensor, slots: torch.Tensor) -> torch.Tensor:
+        return self.out(x, api.linear_attention_step(*self.qkv(x), self.log_decay, pool, slots=slots))
+
+
+class GatedLayer(torch.nn.Module):
+    def __init__(self, width: int):
+        super().__init__()
+        self.weight, self.bias = torch.nn.Parameter(torch.ones(width)), torch.nn.Parameter(torch.zeros(width))
+        self.into = torch.nn.Parameter(torch.randn(width, 2 * width) * width ** -0.5)
+        self.back = torch.nn.Parameter(torch.randn(width, width) * width ** -0.5)
+        # channels that remember from two tokens to a hundred
+        self.gate_bias = torch.nn.Parameter(torch.linspace(0.0, 4.6, width))
+
+    def inputs(self, x: torch.Tensor):
+        u, gate = (api.layer_norm(x, self.weight, self.bias) @ self.into.to(x.dtype)).chunk(2, -1)                           # views, one beside the other
+        return u, gate + self.gate_bias.to(x.dtype)
+
+    def out(self, x: torch.Tensor, h: torch.Tensor) -> torch.Tensor:
+        return x + h @ self.back.to(x.dtype)
+
+    def whole(self, x: torch.Tensor, offsets, keep_state: bool):
+        h, last = api.gated_recurrence(*self.inputs(x), offsets=offsets, output_final_state=keep_state, input_gate="root")
+        return self.out(x, h), last
+
+    def token(self, x: torch.Tensor, pool: torch.Tensor, slots: torch.Tensor) -> torch.Tensor:
+        return self.out(x, api.gated_recurrence_step(*self.inputs(x), pool, slots=slots, input_gate="root"))
+
 
 class LinearLM(torch.nn.Module):
-    def __init__(self, vocabulary: int = 500, width: int = 128, heads: int = 4, d_head: int = 32, layers: int = 2):
+    def __init__(self, vocabulary: int = 500, width: int = 128, heads: int = 4, d_head: int = 32, layers: int = 2, gated: bool = False):
         super().__init__()
         self.width = width
         self.table = torch.nn.Parameter(torch.randn(vocabulary, width) * width ** -0.5)
-        self.layers = torch.nn.ModuleList(Layer(width, heads, d_head) for _ in range(layers))
+        self.layers = torch.nn.ModuleList(GatedLayer(width) if gated and i % 2 else Layer(width, heads, d_head) for i in range(layers))
 
     def embed(self, ids: torch.Tensor):
         table = self.table.to(torch.bfloat16)
@@ -56,8 +88,7 @@ class LinearLM(torch.nn.Module):
         table, x = self.embed(ids)
         states = []
         for layer in self.layers:
-            o, last = api.linear_attention(*layer.qkv(x), layer.log_decay, offsets=offsets, output_final_state=keep_states)
-            x = layer.out(x, o)
+            x, last = layer.whole(x, offsets, keep_states)
             states.append(last)
         return x @ table.T, states
 
@@ -66,7 +97,7 @@ class LinearLM(torch.nn.Module):
         """Logits after one more token of each sequence; sequence b has entry slots[b] of every layer's pool of states."""
         table, x = self.embed(ids)
         for layer, pool in zip(self.layers, pools):
-            x = layer.out(x, api.linear_attention_step(*layer.qkv(x), layer.log_decay, pool, slots=slots))
+            x = layer.token(x, pool, slots)
         return x @ table.T
 
 
@@ -92,8 +123,9 @@ def train(model: LinearLM, successor: torch.Tensor, steps: int, batch: int = 32,
 
 
 @torch.no_grad()
-def serve(model: LinearLM, prompts: list[torch.Tensor], new_tokens: int, entries: int | None = None):
-    """The tokens that follow each prompt, and the logits that they were chosen by."""
+def serve(model: LinearLM, prompts: list[torch.Tensor], new_tokens: int, entries: int | None = None, temperature: float = 0.0, **limits):
+    """The tokens that follow each prompt, and the logits that they were chosen by.  temperature above 0: tokens are drawn, within the
+    limits of api.sample (top_k, top_p, min_p)."""
     device = prompts[0].device
     offsets = torch.tensor([0] + [len(p) for p in prompts], device=device).cumsum(0)
     logits, states = model(torch.cat(prompts), offsets=offsets, keep_states=True)
@@ -108,7 +140,10 @@ def serve(model: LinearLM, prompts: list[torch.Tensor], new_tokens: int, entries
     chosen, seen = [], []
     for _ in range(new_tokens):
         seen.append(logits)
-        chosen.append(logits.argmax(-1))
+        if temperature > 0.0:
+            chosen.append(api.sample(logits, torch.rand(len(prompts), device=device), temperature, **limits))
+        else:
+            chosen.append(logits.argmax(-1))
         logits = model.step(chosen[-1], pools, slots)
     return torch.stack(chosen, 1), torch.stack(seen, 1)
 
@@ -116,14 +151,16 @@ def serve(model: LinearLM, prompts: list[torch.Tensor], new_tokens: int, entries
 def main() -> None:
     args = argparse.ArgumentParser(description=__doc__.split("\n")[0])
     args.add_argument("--steps", type=int, default=160)
+    args.add_argument("--gated", action="store_true", help="every second layer a gated recurrence")
+    args.add_argument("--temperature", type=float, default=0.0, help="above 0: tokens are drawn")
     args = args.parse_args()
     torch.manual_seed(0)
-    model = LinearLM().cuda()
+    model = LinearLM(gated=args.gated).cuda()
     successor = torch.randperm(500, device="cuda")
     losses = train(model, successor, args.steps)
     print(f"loss {losses[0]:.3f} -> {losses[-1]:.3f} in {args.steps} steps")
     prompts = [sequences(successor, 1, n)[0] for n in (0, 6, 130, 40)]
-    tokens, _ = serve(model, prompts, 20)
+    tokens, _ = serve(model, prompts, 20, temperature=args.temperature, **(dict(top_k=50, top_p=0.95) if args.temperature > 0.0 else {}))
     before = torch.cat([torch.stack([p[-1] for p in prompts])[:, None], tokens[:, :-1]], 1)
     print(f"{len(prompts)} prompts, 20 tokens each: {int((tokens == successor[before]).sum())} of {tokens.numel()} follow the permutation")
     if api.linear_attention_status():

@@ -487,7 +487,7 @@ class _Gated:
 
 def _gated_forward(x, gate, initial_state, offsets, output_final_state, input_gate, output_marks, output=True):
     m = _Gated(x, gate, offsets, input_gate, initial_state=initial_state)
-    y = x.new_empty(x.shape) if output else None
+    y = _fresh(x) if output else None
     last = m.new(m.state_shape) if output_final_state else None
     marks = m.new(m.mark_shape) if output_marks else None
     (x, xv), (gate, gv) = _channels(x), _channels(gate)
@@ -508,7 +508,7 @@ def gated_recurrence_backward(d_y, x, gate, initial_state=None, offsets=None, d_
     m = _Gated(x, gate, offsets, input_gate, initial_state=initial_state, d_final_state=d_final_state, marks=marks)
     if marks is None:
         marks = _gated_forward(x, gate, initial_state, offsets, False, input_gate, True, output=False)[2]
-    d_x, d_gate = x.new_empty(x.shape), x.new_empty(x.shape)
+    d_x, d_gate = _fresh(x), _fresh(x)
     d_first = m.new(m.state_shape) if initial_state is not None else None
     (x, xv), (gate, gv), (d_y, yv) = _channels(x), _channels(gate), _channels(d_y)
     m.call(B.tcu_gated_backward, xv, gv, marks=marks, d_y=yv, d_x=_channels(d_x)[1], d_gate=_channels(d_gate)[1], d_dstate_out=_ptr(d_final_state),
@@ -576,7 +576,7 @@ def gated_recurrence_step(x, gate, state, slots=None, input_gate="complement"):
     if slots is not None and (slots.shape != (batch,) or slots.dtype != torch.int32 or not slots.is_contiguous() or slots.device != device):
         raise ValueError("slots: a contiguous int32 tensor of one value for each sequence, on the device of x")
     kind = _input_gate(input_gate)
-    y = x.new_empty(shape)
+    y = _fresh(x)
 
     def view(r):
         if channels > 1 and r.stride(1) != 1:
@@ -591,25 +591,26 @@ def gated_recurrence_step(x, gate, state, slots=None, input_gate="complement"):
 
 
 # ------------------------------------------------------------------------------------------------ layer norm
+def _fresh(x: torch.Tensor) -> torch.Tensor:
+    """An empty tensor of x's shape and type, contiguous."""
+    return torch.empty_like(x, memory_format=torch.contiguous_format)
+
+
 def _rows(x: torch.Tensor):
     """x as rows of its last axis: a tensor whose rows lie one stride apart, their number and the stride (copied if they do not)."""
     d = x.shape[-1]
-    if x.dim() == 2 and (x.stride(1) == 1 or d == 1):
-        return x, x.shape[0], x.stride(0)
+    if x.dim() == 2:
+        stride, step = x.stride()
+        if step == 1 or d == 1:
+            return x, x.shape[0], stride
     x = x.contiguous()
     return x, x.numel() // d, d
 
 
-def _check_norm(x, eps, **params):
+def _check_norm(x, eps, weight, bias):
     """The type of the parameters."""
-    if x.dtype not in _FLOAT:
-        raise TypeError(f"layer norm takes float32, float16 or bfloat16, not {x.dtype}")
-    if x.dim() < 1 or x.shape[-1] == 0:
-        raise ValueError(f"x is {tuple(x.shape)}: there is no last axis to normalise")
-    if not 0.0 <= eps < float("inf"):
-        raise ValueError(f"eps is {eps}")
     kind = None
-    for name, p in params.items():
+    for name, p in (("weight", weight), ("bias", bias)):
         if p is None:
             continue
         if p.shape != x.shape[-1:] or not p.is_contiguous() or p.device != x.device:
@@ -617,14 +618,21 @@ def _check_norm(x, eps, **params):
         if p.dtype not in (torch.float32, x.dtype) or (kind is not None and p.dtype != kind):
             raise TypeError(f"{name} is {p.dtype}: float32 or the type of x, and all parameters alike")
         kind = p.dtype
+    if x.dtype not in _FLOAT:
+        raise TypeError(f"layer norm takes float32, float16 or bfloat16, not {x.dtype}")
+    if x.dim() < 1 or x.shape[-1] == 0:
+        raise ValueError(f"x is {tuple(x.shape)}: there is no last axis to normalise")
+    if not 0.0 <= eps < float("inf"):
+        raise ValueError(f"eps is {eps}")
     return kind or torch.float32
 
 
 def _norm_forward(x, weight, bias, eps):
-    kind = _check_norm(x, eps, weight=weight, bias=bias)
-    y = x.new_empty(x.shape)
+    kind = _check_norm(x, eps, weight, bias)
+    stream = _stream(x.device)
+    y = _fresh(x)
     x, rows, stride = _rows(x)
-    B.check(B.tcu_layer_norm_forward(x, rows, x.shape[-1], stride, _FLOAT[x.dtype], weight, bias, _FLOAT[kind], eps, y, _stream(x.device)))
+    B.check(B.tcu_layer_norm_forward(x.data_ptr(), rows, x.shape[-1], stride, _FLOAT[x.dtype], _ptr(weight), _ptr(bias), _FLOAT[kind], eps, y.data_ptr(), stream))
     return y
 
 
@@ -637,13 +645,13 @@ def layer_norm_backward(d_y, x, weight=None, eps=1e-5, params=True):
 
 
 def _norm_backward(d_y, x, weight, bias, eps, want_x, want_weight, want_bias):
-    kind = _check_norm(x, eps, weight=weight, bias=bias)
+    kind = _check_norm(x, eps, weight, bias)
     if d_y.dtype != x.dtype or d_y.device != x.device:
         _refuse(x.dtype, x.device, d_y=d_y)
     if d_y.shape != x.shape:
         raise ValueError(f"d_y is {tuple(d_y.shape)}, x {tuple(x.shape)}")
     d = x.shape[-1]
-    d_x = x.new_empty(x.shape) if want_x else None
+    d_x = _fresh(x) if want_x else None
     d_weight = x.new_empty(d, dtype=kind) if want_weight else None
     d_bias = x.new_empty(d, dtype=kind) if want_bias else None
     x, rows, stride = _rows(x)

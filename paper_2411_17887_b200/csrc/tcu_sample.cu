@@ -18,7 +18,8 @@ constexpr uint64_t kMostStride = uint64_t(1) << 38;
 constexpr uint32_t kSms = 148;
 
 // How a row is divided: 16-byte packs a thread, blocks (a power of two).  As few packs as 8 blocks do with; where that is more blocks than the SMs hold
-// at once, four each, up to eight packs, so that fewer blocks have to meet.
+// at once, four each, up to 64 tokens a thread, since what a thread does besides costs as much as 20 tokens: 192 rows of 50001 fp32 logits, 8 blocks of 28
+// tokens a thread: top_k 42 us, top_p 102; 4 blocks of 56: 32 and 52.  More do not pay: 256 rows of 128000 bfloat16 logits, 64 tokens 75 us, 128 106.
 struct Division {
     int packs;
     uint32_t blocks;
@@ -30,14 +31,14 @@ Division divide(uint64_t rows, uint32_t vocabulary, size_t eb) {
         return int((need + step - 1) / step);
     };
     uint32_t blocks = kSampleMaxCluster;
-    while (blocks > 1 && (packs(blocks / 2) == packs(blocks) || (rows * blocks > 4 * kSms && packs(blocks / 2) <= 8))) blocks /= 2;
+    while (blocks > 1 && (packs(blocks / 2) == packs(blocks) || (rows * blocks > 4 * kSms && packs(blocks / 2) * (16 / eb) <= 64))) blocks /= 2;
     return {packs(blocks), blocks};
 }
 
 template <typename T>
 tcu_status_t launch(const SampleParams &p, const Division &d, uint64_t rows, cudaStream_t stream) {
     const size_t shared = size_t(d.packs) * kSampleThreads * 16;
-    if (shared > 32768 && !ok(cudaFuncSetAttribute(tcu_sample_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(shared)))) return TCU_ERR_CUDA;
+    if (shared + sizeof(SampleShared) > 48000 && !ok(cudaFuncSetAttribute(tcu_sample_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(shared)))) return TCU_ERR_CUDA;
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeClusterDimension;
     attr.val.clusterDim.x = d.blocks;

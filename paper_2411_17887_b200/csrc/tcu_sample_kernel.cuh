@@ -6,13 +6,18 @@
 //
 // A row is read once, into the shared memory of a cluster of blocks, a part each: a warp holds consecutive tokens, so that the sums of warps and
 // blocks, which tell each other theirs, are those of ranges of tokens.  Without limits a block's weights are relative to its own largest
-// logit, and the blocks meet once.  The last kept logit is looked for among candidates, up to 256 of which every block sorts for itself: for top_k
-// the tokens from the k-th of the largest logits of 32 ranges a block on (there are k of these at least), or those in the bin that a histogram
-// of numbers names; for top_p those in the bin that a histogram of weights names.  That one is of 32-bit weights, and sums of 64-bit ones say whether the
+// logit, and the blocks meet once.  The last kept logit is looked for among candidates, up to 512, which are listed and sorted: for top_k
+// the tokens from the k-th of the largest logits of 64 ranges a block on (there are k of these at least), or those in the bin that a histogram
+// of numbers names; for top_p the largest few hundred, found the same way, if they have the weight, or those in the bin that a histogram of weights names.  That one is of 32-bit weights, and sums of 64-bit ones say whether the
 // bin is right.  Where a bin has more tokens, exact histograms of the logit's bits as an integer follow, 9 bits a time.
 //
 // Sums that decide which token it is are exact enough that it is the token of the definition: weights in 64-bit floating point, in exact histograms
 // in fixed point with 42 bits (three limbs of 14, each sum of at most 2^18 tokens within 32 bits), whose sums do not depend on their order.
+//
+// What bounds it: 64-bit arithmetic, 12 instructions a weight, and, with limits, the times that the blocks of a row have to meet.  256 rows of 128000
+// bfloat16 logits (66 MB, 10 us to read): largest logit alone 27 us, temperature 75, top_k 50 61, top_p 0.9 112.  192 rows of 50001 fp32 logits:
+// 18, 43, 33 and 53; top_p 0.99 at temperature 1.2, some ten thousand tokens, 149.  Tried: weights in all histograms in three limbs (top_p 284 us), logits in
+// registers (they spill), weights by exp() (whole rows 203 us), all candidates sorted by every block for itself (top_k 128).
 #pragma once
 
 #include <cooperative_groups.h>
@@ -27,12 +32,12 @@ constexpr int kSampleThreads = 256;
 constexpr int kSampleWarps = kSampleThreads / 32;
 constexpr int kSampleBins = 2048, kSampleFineBits = 9, kSampleFine = 1 << kSampleFineBits;      // of a first histogram, and of those that follow
 constexpr int kSampleMaxCluster = 8;
-constexpr int kSampleList = 256;                      // candidates that are sorted
-constexpr int kSampleRanges = 32;                     // of a block: eight lanes' tokens each
+constexpr int kSampleList = 512;                      // candidates that are sorted, two a thread
+constexpr int kSampleRanges = 64;                     // of a block: four lanes' tokens each
 constexpr uint32_t kMostVocabulary = 1u << 18;
 constexpr double kSampleFixed = 4398046511104.0;      // 2^42
 constexpr int kSampleLimb = 14;
-static_assert(kSampleList == kSampleThreads && kSampleRanges * kSampleMaxCluster <= kSampleThreads, "a candidate, or a range, each thread");
+static_assert(kSampleList == 2 * kSampleThreads && kSampleRanges == 2 * 32, "two candidates each thread, two ranges each lane of a warp");
 
 // A setting of all rows, or one for each.
 template <typename T>
@@ -55,23 +60,6 @@ struct SampleParams {
     float *log_probs;
 };
 
-// 2^(j/32), by the exponential's series
-struct SampleTable {
-    double v[32];
-    constexpr SampleTable() : v() {
-        for (int j = 0; j < 32; ++j) {
-            const double x = j * (0.69314718055994530942 / 32);
-            double term = 1.0, sum = 1.0;
-            for (int k = 1; k < 24; ++k) {
-                term *= x / k;
-                sum += term;
-            }
-            v[j] = sum;
-        }
-    }
-};
-__device__ constexpr SampleTable kSampleTable{};
-
 // What the blocks of a cluster tell one another.
 struct SampleWord {
     double a;
@@ -84,7 +72,7 @@ struct SampleFound {
 };
 
 struct SampleShared {
-    double table[32];
+    double table[32];                      // 2^(j/32)
     SampleWord slots[2][kSampleMaxCluster];
     SampleFound found[2];
     double warp_sum[kSampleWarps];
@@ -93,11 +81,16 @@ struct SampleShared {
     float warp_max[kSampleWarps];
     uint32_t count;                        // of this block's candidates
     uint2 list[kSampleList];               // their keys and tokens
-    uint2 all[kSampleList], sorted[kSampleList];           // of all blocks' candidates; in falling order
     uint32_t ranges[kSampleRanges];        // keys of the largest logits of its ranges
     uint32_t all_ranges[kSampleMaxCluster * kSampleRanges];
     float from_k;
-    uint32_t hist[kSampleBins];            // or three limbs of kSampleFine bins
+    union {
+        uint32_t hist[kSampleBins];        // or three limbs of kSampleFine bins
+        struct {
+            uint64_t sorted[kSampleList];                  // all blocks' candidates, in falling order: candidate()
+            uint64_t order[kSampleList];                   // those kept, in the order of tokens
+        };
+    };
 };
 
 __device__ __forceinline__ uint32_t sample_key(float v) {        // the order of logits as that of unsigned integers
@@ -193,10 +186,10 @@ struct Sampler {
     // The block's largest logit, from the threads'; s.ranges holds the keys of its ranges' (0 for one without a token).
     __device__ float block_max(float x) {
 #pragma unroll
-        for (int o = 1; o < 8; o <<= 1) x = fmaxf(x, __shfl_xor_sync(~0u, x, o));
-        if (lane % 8 == 0) s.ranges[warp * 4 + lane / 8] = x > -INFINITY ? sample_key(x) : 0;
+        for (int o = 1; o < 4; o <<= 1) x = fmaxf(x, __shfl_xor_sync(~0u, x, o));
+        if (lane % 4 == 0) s.ranges[warp * 8 + lane / 4] = x > -INFINITY ? sample_key(x) : 0;
 #pragma unroll
-        for (int o = 8; o < 32; o <<= 1) x = fmaxf(x, __shfl_xor_sync(~0u, x, o));
+        for (int o = 4; o < 32; o <<= 1) x = fmaxf(x, __shfl_xor_sync(~0u, x, o));
         if (lane == 0) s.warp_max[warp] = x;
         __syncthreads();
         x = s.warp_max[lane & (kSampleWarps - 1)];
@@ -250,7 +243,7 @@ struct Sampler {
     __device__ float load() {
         const T *from = static_cast<const T *>(p.logits) + uint64_t(row) * p.stride;
         first = int(rank * kSampleThreads * p.packs * kVec) - int(reinterpret_cast<uintptr_t>(from) % 16 / sizeof(T));   // (what lies ahead of the row on its first 16 bytes)
-        if (threadIdx.x < 32) s.table[threadIdx.x] = kSampleTable.v[threadIdx.x];
+        if (threadIdx.x < 32) s.table[threadIdx.x] = exp2(threadIdx.x / 32.0);
         float most = -INFINITY;
 #pragma unroll 4
         for (int j = 0; j < p.packs; ++j) {
@@ -506,36 +499,85 @@ struct Sampler {
         }
         return total;
     }
-    // All blocks' `total` candidates (no more than kSampleList) to s.sorted, in falling order, the lower token first among equals.
+    // A candidate as a number: in rising order the logits fall, the lower token first among equals.  Or, for the order of tokens, turned around.
+    static __device__ __forceinline__ uint64_t candidate(uint32_t key, uint32_t token) { return uint64_t(~key) << 32 | token; }
+    static __device__ __forceinline__ uint64_t turned(uint64_t v) { return v << 32 | v >> 32; }
+    static __device__ __forceinline__ float logit_of(uint64_t v) { return sample_value(~uint32_t(v >> 32)); }
+
+    // Sorts the first `total` of a list (of kSampleList, two a thread), rising.  Few of them (a thread each) by counting those ahead of each: 25 steps of
+    // reading four for a hundred.  More by a bitonic network over the next power of two, whose steps of up to 32 stay within a warp's 64 elements.
+    __device__ void sort(uint64_t *list, uint32_t total) {
+        __syncthreads();
+        if (total <= 160) {
+            const uint64_t mine = threadIdx.x < total ? list[threadIdx.x] : 0;
+            uint32_t before = 0;
+            if (threadIdx.x < total) {
+                uint32_t k = 0;
+                for (; k + 4 <= total; k += 4) before += (list[k] < mine) + (list[k + 1] < mine) + (list[k + 2] < mine) + (list[k + 3] < mine);
+                for (; k < total; ++k) before += list[k] < mine;
+            }
+            __syncthreads();
+            if (threadIdx.x < total) list[before] = mine;
+            __syncthreads();
+            return;
+        }
+        uint32_t n = 64;
+        while (n < total) n *= 2;
+        for (uint32_t i = threadIdx.x; i < n; i += kSampleThreads)
+            if (i >= total) list[i] = ~0ull;
+        __syncthreads();
+        const bool works = 2 * threadIdx.x < n;
+        for (uint32_t size = 2; size <= n; size *= 2) {
+            for (uint32_t step = size / 2; step > 0; step /= 2) {
+                if (works) {
+                    const uint32_t low = 2 * threadIdx.x - (threadIdx.x & (step - 1)), high = low + step;
+                    const uint64_t x = list[low], y = list[high];
+                    if ((x > y) == ((low & size) == 0)) {
+                        list[low] = y;
+                        list[high] = x;
+                    }
+                }
+                if (step > 32 || (step == 1 && size >= 64)) __syncthreads();       // (what follows reaches, or has come from, other warps' elements)
+                else __syncwarp();
+            }
+        }
+        __syncthreads();
+    }
+    // All blocks' `total` candidates (no more than kSampleList) to s.sorted.
     __device__ void sort_candidates(uint32_t total) {
-        uint2 mine = make_uint2(0, 0);
-        if (threadIdx.x < total) {
-            uint32_t k = 0, from = threadIdx.x;
+        for (uint32_t i = threadIdx.x; i < total; i += kSampleThreads) {
+            uint32_t k = 0, from = i;
             for (uint32_t n = *cluster.map_shared_rank(&s.count, 0); from >= n; n = *cluster.map_shared_rank(&s.count, k)) {
                 from -= n;
                 ++k;
             }
-            mine = cluster.map_shared_rank(s.list, k)[from];
+            const uint2 q = cluster.map_shared_rank(s.list, k)[from];
+            s.sorted[i] = candidate(q.x, q.y);
         }
-        s.all[threadIdx.x] = mine;
-        __syncthreads();
-        if (threadIdx.x < total) {
-            uint32_t before = 0;
-            for (uint32_t i = 0; i < total; ++i) {
-                const uint2 q = s.all[i];
-                before += q.x > mine.x || (q.x == mine.x && q.y < mine.y);
-            }
-            s.sorted[before] = mine;
+        sort(s.sorted, total);
+    }
+    // This thread's two of the first m of a list, 2 i and 2 i + 1: their weights, and the sums up to them.
+    struct Two {
+        double w[2], upto[2], all;
+    };
+    template <bool TURNED>
+    __device__ Two two_of(const uint64_t *list, uint32_t m) {
+        Two two;
+#pragma unroll
+        for (uint32_t e = 0; e < 2; ++e) {
+            const uint32_t i = 2 * threadIdx.x + e;
+            two.w[e] = i < m ? weight(logit_of(TURNED ? turned(list[i]) : list[i])) : 0.0;
         }
-        __syncthreads();
+        two.upto[1] = block_prefix(two.w[0] + two.w[1], two.all);
+        two.upto[0] = two.upto[1] - two.w[1];
+        return two;
     }
     // How many of the first `most` sorted candidates it takes until their weights reach the target (below 0: top_p of theirs).
     __device__ uint32_t reach_sorted(uint32_t most, double top_p, double target) {
-        const uint32_t i = threadIdx.x;
-        double all, upto = i < most ? weight(sample_value(s.sorted[i].x)) : 0.0;
-        upto = block_prefix(upto, all);
-        if (target < 0.0) target = top_p * all;
-        return min(most, block_min(i < most && upto >= target ? i : most - 1, 0).x + 1);
+        const Two two = two_of<false>(s.sorted, most);
+        if (target < 0.0) target = top_p * two.all;
+        const uint32_t i = 2 * threadIdx.x;
+        return min(most, block_min(i < most && two.upto[0] >= target ? i : i + 1 < most && two.upto[1] >= target ? i + 1 : most - 1, 0).x + 1);
     }
     // The sum of the threads' values up to each thread's, and of all.
     __device__ double block_prefix(double x, double &all) {
@@ -557,29 +599,30 @@ struct Sampler {
     }
     // The prefix of the first m of `total` sorted candidates, which hold all tokens of their last one's logit.
     __device__ Prefix prefix_of(uint32_t total, uint32_t m) {
-        const uint32_t key = s.sorted[m - 1].x;
-        const uint32_t above = block_min(threadIdx.x < total && s.sorted[threadIdx.x].x == key ? threadIdx.x : ~0u, 0).x;       // the first with this key
-        return {sample_value(key), m - above, m >= total || s.sorted[m].x != key};
+        const uint32_t key = uint32_t(s.sorted[m - 1] >> 32);
+        uint32_t mine = ~0u;
+        for (uint32_t i = threadIdx.x; i < total && mine == ~0u; i += kSampleThreads)
+            if (uint32_t(s.sorted[i] >> 32) == key) mine = i;
+        const uint32_t above = block_min(mine, 0).x;         // the first with this key
+        return {sample_value(~key), m - above, m >= total || uint32_t(s.sorted[m] >> 32) != key};
     }
     // Draws from candidates that hold all tokens to be kept: the first `most` of them, and of these those that reach the target.  By one block; the
     // others lend it their lists.
     __device__ void draw_listed(uint32_t total, uint32_t most, double top_p, double target) {
         if (rank == 0) {
             sort_candidates(total);
-            const uint32_t m = top_p < 1.0 ? reach_sorted(most, top_p, target) : most, i = threadIdx.x;
+            const uint32_t m = top_p < 1.0 ? reach_sorted(most, top_p, target) : most;
             // in the order of tokens
-            const uint2 mine = i < m ? s.sorted[i] : make_uint2(0, 0);
-            if (i < m) {
-                uint32_t before = 0;
-                for (uint32_t k = 0; k < m; ++k) before += s.sorted[k].y < mine.y;
-                s.all[before] = mine;
-            }
-            __syncthreads();
-            const float x = i < m ? sample_value(s.all[i].x) : 0.0f;
-            double sum;
-            const double w = i < m ? weight(x) : 0.0, upto = block_prefix(w, sum), target_u = uniform() * sum;
-            const uint2 found = block_min(w > 0.0 && upto > target_u ? i : ~0u, w > 0.0 ? ~i : ~0u);
-            if (i == (found.x != ~0u ? found.x : ~found.y)) put_drawn(s.all[i].y, x, top, sum);
+            for (uint32_t i = threadIdx.x; i < m; i += kSampleThreads) s.order[i] = turned(s.sorted[i]);
+            sort(s.order, m);
+            const Two two = two_of<true>(s.order, m);
+            const double target_u = uniform() * two.all;
+            const uint32_t i = 2 * threadIdx.x;
+            // the first past the target; the last one with a weight, if rounding leaves none
+            const uint32_t past = two.w[0] > 0.0 && two.upto[0] > target_u ? i : two.w[1] > 0.0 && two.upto[1] > target_u ? i + 1 : ~0u;
+            const uint2 found = block_min(past, two.w[1] > 0.0 ? ~(i + 1) : two.w[0] > 0.0 ? ~i : ~0u);
+            const uint32_t at = found.x != ~0u ? found.x : ~found.y;
+            if (threadIdx.x == 0) put_drawn(int64_t(s.order[at] >> 32), logit_of(turned(s.order[at])), top, two.all);
         }
         cluster.sync();
     }
@@ -620,8 +663,8 @@ struct Sampler {
         set_temperature(temperature);
         if (!limited_k && !limited_m && !limited_p) return whole(of_block);
 
-        if (threadIdx.x / kSampleRanges < ranks)                     // its ranges, to all blocks
-            cluster.map_shared_rank(s.all_ranges, threadIdx.x / kSampleRanges)[rank * kSampleRanges + threadIdx.x % kSampleRanges] = s.ranges[threadIdx.x % kSampleRanges];
+        for (uint32_t r = threadIdx.x / kSampleRanges; r < ranks; r += kSampleThreads / kSampleRanges)        // its ranges, to all blocks
+            cluster.map_shared_rank(s.all_ranges, r)[rank * kSampleRanges + threadIdx.x % kSampleRanges] = s.ranges[threadIdx.x % kSampleRanges];
         const SampleWord *w = exchange({double(of_block), 0, 0});
         top = float(w[0].a);
         for (uint32_t r = 1; r < ranks; ++r) top = fmaxf(top, float(w[r].a));
@@ -630,7 +673,7 @@ struct Sampler {
             return;
         }
         // from here on lie at least k tokens (for top_p alone: so many that most of them can be sorted)
-        float from_k = top < INFINITY && (limited_k || limited_p) ? from_ranges(limited_k ? k : 0.6 * ranks * kSampleRanges) : -INFINITY;
+        float from_k = top < INFINITY && (limited_k || limited_p) ? from_ranges(limited_k ? k : most_ranges()) : -INFINITY;
         if (top == INFINITY) {
             only_infinite();
             top = 0.0f;
@@ -688,20 +731,26 @@ struct Sampler {
         draw(kept);
     }
 
+    // So many of the ranges' largest logits that about 130 tokens lie from the last of them on: n ranges of tokens in no order have none of m
+    // tokens for a part exp(-m / n) of them.
+    __device__ double most_ranges() const {
+        const double n = ranks * kSampleRanges;
+        return fmax(floor(n - n * exp(-130.0 / n)), 1.0);
+    }
     // A logit from which on at least k tokens lie, from the largest logits of the row's ranges: by their keys' upper half; minus infinity if there are
     // fewer ranges.
     __device__ float from_ranges(double k) {
         const uint32_t n = ranks * kSampleRanges;
         if (k > n) return -INFINITY;
         if (warp == 0) {
-            uint32_t mine[kSampleMaxCluster];
+            uint32_t mine[2 * kSampleMaxCluster];
 #pragma unroll
-            for (uint32_t r = 0; r < kSampleMaxCluster; ++r) mine[r] = r < ranks ? s.all_ranges[r * kSampleRanges + lane] >> 16 : 0;
+            for (uint32_t r = 0; r < 2 * kSampleMaxCluster; ++r) mine[r] = r < 2 * ranks ? s.all_ranges[r * 32 + lane] >> 16 : 0;
             uint32_t from = 0;
             for (uint32_t bit = 1u << 15; bit; bit >>= 1) {
                 uint32_t count = 0;
 #pragma unroll
-                for (uint32_t r = 0; r < kSampleMaxCluster; ++r) count += mine[r] >= (from | bit);
+                for (uint32_t r = 0; r < 2 * kSampleMaxCluster; ++r) count += mine[r] >= (from | bit);
                 if (double(__reduce_add_sync(~0u, count)) >= k) from |= bit;
             }
             if (lane == 0) s.from_k = from ? sample_value(max(from << 16, kKeyNothing + 1)) : -INFINITY;
