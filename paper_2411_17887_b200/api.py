@@ -430,11 +430,11 @@ def embedding(ids, table, scale=1.0):
 # ------------------------------------------------------------------------------------------------ gated recurrence
 def _channels(x: torch.Tensor):
     """An array (b, t, d), or packed (t, d), with its channels contiguous (copied if they are not), and its description."""
-    if x.shape[-1] > 1 and x.stride(-1) != 1:
+    strides = x.stride()
+    if strides[-1] != 1 and x.shape[-1] > 1:
         x = x.contiguous()
-    if x.dim() == 3:
-        return x, (x.data_ptr(), x.stride(0), x.stride(1))
-    return x, (x.data_ptr(), 0, x.stride(0))
+        strides = x.stride()
+    return x, (x.data_ptr(), strides[0] if len(strides) == 3 else 0, strides[-2])
 
 
 def _input_gate(name) -> int:
@@ -447,7 +447,7 @@ def _input_gate(name) -> int:
 class _Gated:
     """Checked and described arguments of one call of the gated recurrence over whole sequences."""
 
-    __slots__ = ("head", "x", "offsets", "state_shape", "mark_shape", "stream")
+    __slots__ = ("head", "x", "offsets", "state_shape", "mark_shape", "strides", "stream")
 
     def __init__(self, x, gate, offsets, input_gate, **states):
         dtype, device, shape = x.dtype, x.device, x.shape
@@ -467,7 +467,8 @@ class _Gated:
             raise ValueError("there are no channels")
         batch = offsets.numel() - 1 if packed else shape[0]
         self.state_shape = (batch, channels)
-        self.mark_shape = (B.tcu_gated_marks_bytes(batch, tokens if packed else batch * tokens, channels) // (4 * channels), channels)
+        self.mark_shape = ((tokens if packed else batch * tokens) // 64 + batch, channels)            # (tcu_gated_marks_bytes)
+        self.strides = (0 if packed else tokens * channels, channels)                                # of a fresh array
         for name, s in states.items():
             want = self.mark_shape if name == "marks" else self.state_shape
             if s is not None and (s.shape != want or s.dtype != torch.float32 or not s.is_contiguous() or s.device != device):
@@ -478,7 +479,7 @@ class _Gated:
         self.stream = _stream(device)
 
     def new(self, shape):
-        return self.x.new_empty(shape, dtype=torch.float32)
+        return torch.empty(shape, dtype=torch.float32, device=self.x.device)
 
     def call(self, fn, x, gate, y=B.NO_ROWS, marks=None, **more):
         B.check(fn(B.tcu_gated_args(*self.head, x, gate, y, d_offsets=self.offsets, d_marks=_ptr(marks), marks_bytes=0 if marks is None else 4 * marks.numel(), **more),
@@ -488,10 +489,12 @@ class _Gated:
 def _gated_forward(x, gate, initial_state, offsets, output_final_state, input_gate, output_marks, output=True):
     m = _Gated(x, gate, offsets, input_gate, initial_state=initial_state)
     y = _fresh(x) if output else None
-    last = m.new(m.state_shape) if output_final_state else None
+    last = None
+    if output_final_state:
+        last = m.new(m.state_shape) if initial_state is None else torch.empty_like(initial_state)
     marks = m.new(m.mark_shape) if output_marks else None
     (x, xv), (gate, gv) = _channels(x), _channels(gate)
-    m.call(B.tcu_gated_forward, xv, gv, _channels(y)[1] if output else B.NO_ROWS, marks, d_state_in=_ptr(initial_state), d_state_out=_ptr(last))
+    m.call(B.tcu_gated_forward, xv, gv, (y.data_ptr(), *m.strides) if output else B.NO_ROWS, marks, d_state_in=_ptr(initial_state), d_state_out=_ptr(last))
     return y, last, marks
 
 
@@ -509,9 +512,9 @@ def gated_recurrence_backward(d_y, x, gate, initial_state=None, offsets=None, d_
     if marks is None:
         marks = _gated_forward(x, gate, initial_state, offsets, False, input_gate, True, output=False)[2]
     d_x, d_gate = _fresh(x), _fresh(x)
-    d_first = m.new(m.state_shape) if initial_state is not None else None
+    d_first = torch.empty_like(initial_state) if initial_state is not None else None
     (x, xv), (gate, gv), (d_y, yv) = _channels(x), _channels(gate), _channels(d_y)
-    m.call(B.tcu_gated_backward, xv, gv, marks=marks, d_y=yv, d_x=_channels(d_x)[1], d_gate=_channels(d_gate)[1], d_dstate_out=_ptr(d_final_state),
+    m.call(B.tcu_gated_backward, xv, gv, marks=marks, d_y=yv, d_x=(d_x.data_ptr(), *m.strides), d_gate=(d_gate.data_ptr(), *m.strides), d_dstate_out=_ptr(d_final_state),
            d_dstate_in=_ptr(d_first))
     return d_x, d_gate, d_first
 
@@ -652,13 +655,15 @@ def _norm_backward(d_y, x, weight, bias, eps, want_x, want_weight, want_bias):
         raise ValueError(f"d_y is {tuple(d_y.shape)}, x {tuple(x.shape)}")
     d = x.shape[-1]
     d_x = _fresh(x) if want_x else None
-    d_weight = x.new_empty(d, dtype=kind) if want_weight else None
-    d_bias = x.new_empty(d, dtype=kind) if want_bias else None
+    like = weight if weight is not None else x.new_empty(d, dtype=kind) if want_weight or want_bias else None
+    d_weight = torch.empty_like(like) if want_weight else None
+    d_bias = torch.empty_like(like) if want_bias else None
     x, rows, stride = _rows(x)
     d_y, _, dy_stride = _rows(d_y)
     size = B.tcu_layer_norm_workspace_bytes(rows, d) if want_weight or want_bias else 0
-    ws = x.new_empty(size // 4, dtype=torch.float32) if size else None
-    B.check(B.tcu_layer_norm_backward(d_y, dy_stride, x, stride, rows, d, _FLOAT[x.dtype], weight, _FLOAT[kind], eps, d_x, d_weight, d_bias, ws, size, _stream(x.device)))
+    ws = torch.empty(size // 4, dtype=torch.float32, device=x.device) if size else None
+    B.check(B.tcu_layer_norm_backward(d_y.data_ptr(), dy_stride, x.data_ptr(), stride, rows, d, _FLOAT[x.dtype], _ptr(weight), _FLOAT[kind], eps, _ptr(d_x), _ptr(d_weight),
+                                      _ptr(d_bias), _ptr(ws), size, _stream(x.device)))
     return d_x, d_weight, d_bias
 
 

@@ -102,7 +102,6 @@ tcu_status_t check(const tcu_gated_t *a, Sizes &s) {
     return TCU_OK;
 }
 
-
 // Calls go(type, input gate) with these as types.
 template <typename F>
 void dispatch(const tcu_gated_t *a, F go) {
@@ -119,7 +118,7 @@ void dispatch(const tcu_gated_t *a, F go) {
 // Blocks of a cluster that walk a sequence together: as many as keep all blocks on the SMs at once, two an SM, and have a tile each.  16383 tokens of
 // 2048 channels, 32 walks: 8 blocks 61 us, 4 blocks 82; 8 x 4096 tokens, 256 walks: one block 84 us, two 111.  Packed sequences are of lengths
 // that the host does not know, and the longest alone may take most of the time: up to four times as many blocks (24 sequences of 1504 channels,
-// 16001 tokens: of 0 to 3972 each, one block 90 us, two 73; of 667 each 38 and 52).
+// 16001 tokens: of 0 to 3972 each, one block 61 us, two 53; of 667 each 38 and 54).
 uint32_t blocks_of_walk(uint64_t walks, const Sizes &s) {
     const uint64_t most = s.packed ? 4 * 2 * kSms : 2 * kSms, tiles = s.packed ? 4 * s.tokens / s.batch / 128 : (s.tokens + 127) / 128;
     uint32_t ranks = 1;
@@ -127,8 +126,14 @@ uint32_t blocks_of_walk(uint64_t walks, const Sizes &s) {
     return ranks;
 }
 
-tcu_status_t launch_walks(void (*kernel)(GatedParams), const GatedParams &p, uint64_t batch, uint32_t shared, cudaStream_t stream) {
-    if (!ok(cudaFuncSetAttribute(reinterpret_cast<const void *>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, int(shared)))) return TCU_ERR_CUDA;
+// (bytes: of shared memory, by the blocks of a cluster)
+template <auto kernel, auto bytes>
+tcu_status_t launch_walks(const GatedParams &p, uint64_t batch, cudaStream_t stream) {
+    if (!allow_shared<kernel>(bytes(kGatedMaxCluster))) return TCU_ERR_CUDA;
+    GatedParams q = p;
+    // Long packed sequences first, where not all blocks run at once: 24 sequences of 0 to 3972 tokens, 1504 channels, 73 -> 53 us.  Found by every block for
+    // itself: 200 sequences of 100 tokens would take 87 us instead of 54, and need it less.
+    if (p.offsets && batch > 1 && batch <= kGatedOrdered && batch * p.strips * p.ranks > 2 * kSms) q.ordered = int(batch);
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeClusterDimension;
     attr.val.clusterDim.x = p.ranks;
@@ -136,11 +141,11 @@ tcu_status_t launch_walks(void (*kernel)(GatedParams), const GatedParams &p, uin
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(uint32_t(batch * p.strips * p.ranks));
     cfg.blockDim = dim3(kGatedWarps * 32);
-    cfg.dynamicSmemBytes = shared;
+    cfg.dynamicSmemBytes = bytes(p.ranks);
     cfg.stream = stream;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
-    return ok(cudaLaunchKernelEx(&cfg, kernel, p)) ? TCU_OK : TCU_ERR_CUDA;
+    return ok(cudaLaunchKernelEx(&cfg, kernel, q)) ? TCU_OK : TCU_ERR_CUDA;
 }
 
 }  // namespace
@@ -177,9 +182,9 @@ tcu_status_t tcu_gated_forward(const tcu_gated_t *a, cudaStream_t stream) {
     dispatch(a, [&](auto t, auto in) {
         using T = decltype(t);
         constexpr int kInput = decltype(in)::value, kLast = sizeof(T) == 2 ? 2 : 4;
-        if (way == 0) st = launch_walks(tcu_gated_forward_kernel<T, kInput, 16, true>, p, a->batch, forward_bytes<T, 16>(p.ranks), stream);
-        else if (way == 1) st = launch_walks(tcu_gated_forward_kernel<T, kInput, 4, true>, p, a->batch, forward_bytes<T, 4>(p.ranks), stream);
-        else st = launch_walks(tcu_gated_forward_kernel<T, kInput, kLast, false>, p, a->batch, forward_bytes<T, kLast>(p.ranks), stream);
+        if (way == 0) st = launch_walks<tcu_gated_forward_kernel<T, kInput, 16, true>, forward_bytes<T, 16>>(p, a->batch, stream);
+        else if (way == 1) st = launch_walks<tcu_gated_forward_kernel<T, kInput, 4, true>, forward_bytes<T, 4>>(p, a->batch, stream);
+        else st = launch_walks<tcu_gated_forward_kernel<T, kInput, kLast, false>, forward_bytes<T, kLast>>(p, a->batch, stream);
     });
     return st;
 }
@@ -213,9 +218,9 @@ tcu_status_t tcu_gated_backward(const tcu_gated_t *a, cudaStream_t stream) {
     dispatch(a, [&](auto t, auto in) {
         using T = decltype(t);
         constexpr int kInput = decltype(in)::value, kLast = sizeof(T) == 2 ? 2 : 4;
-        if (way == 0) st = launch_walks(tcu_gated_backward_kernel<T, kInput, 16, true>, p, a->batch, backward_bytes<T, 16>(p.ranks), stream);
-        else if (way == 1) st = launch_walks(tcu_gated_backward_kernel<T, kInput, 4, true>, p, a->batch, backward_bytes<T, 4>(p.ranks), stream);
-        else st = launch_walks(tcu_gated_backward_kernel<T, kInput, kLast, false>, p, a->batch, backward_bytes<T, kLast>(p.ranks), stream);
+        if (way == 0) st = launch_walks<tcu_gated_backward_kernel<T, kInput, 16, true>, backward_bytes<T, 16>>(p, a->batch, stream);
+        else if (way == 1) st = launch_walks<tcu_gated_backward_kernel<T, kInput, 4, true>, backward_bytes<T, 4>>(p, a->batch, stream);
+        else st = launch_walks<tcu_gated_backward_kernel<T, kInput, kLast, false>, backward_bytes<T, kLast>>(p, a->batch, stream);
     });
     return st;
 }

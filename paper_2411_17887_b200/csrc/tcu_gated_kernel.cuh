@@ -27,6 +27,7 @@ constexpr int kGatedMark = 64;             // tokens between marks
 constexpr int kGatedWarps = 8;
 constexpr int kGatedChannels = 64;
 constexpr int kGatedMaxCluster = 8;
+constexpr int kGatedOrdered = 64;          // packed sequences that blocks order by length
 
 enum GatedInput { kInputComplement = 0, kInputOne = 1, kInputRoot = 2 };
 
@@ -46,6 +47,7 @@ struct GatedParams {
     uint64_t tokens;           // of each sequence (dense), of all together (packed)
     uint32_t channels, strips;
     uint32_t ranks;            // blocks of a cluster
+    int ordered;               // packed: so many sequences (at most kGatedOrdered) are walked in the order of their lengths; or 0
 };
 
 // Stores the two channels of a lane: in one access where they are aligned for it (PAIR), else one each.
@@ -137,19 +139,41 @@ struct GatedWalk {
     int64_t begin;             // of the sequence, in rows of the arrays (dense: 0)
     int len;
     uint64_t mark;             // row of its first mark
-    __device__ __forceinline__ GatedWalk(const GatedParams &p, uint32_t walk) {
+    // (shared: a number for each thread and one more, free again after the call)
+    __device__ __forceinline__ GatedWalk(const GatedParams &p, uint32_t walk, int *shared) {
         seq = walk / p.strips;
         c0 = (walk - seq * p.strips) * kGatedChannels;
-        if (p.offsets) {
-            // offsets that are not as they should be may give wrong results, but no access outside the arrays
-            begin = min(max(p.offsets[seq], int64_t(0)), int64_t(p.tokens));
-            len = int(min(max(p.offsets[seq + 1], begin), int64_t(p.tokens)) - begin);
-            mark = uint64_t(begin) / kGatedMark + seq;
-        } else {
+        if (!p.offsets) {
             begin = 0;
             len = int(p.tokens);
             mark = uint64_t(seq) * p.tokens / kGatedMark + seq;
+            return;
         }
+        if (p.ordered > 0) {           // long sequences first: the one with `seq` longer ones
+            const int t = int(threadIdx.x), n = t < p.ordered ? length(p, t) : -1;
+            shared[t] = n;
+            __syncthreads();
+            uint32_t longer = 0;
+            if (t < p.ordered) {
+                for (int k = 0; k < p.ordered; k += 4) {
+                    const int4 m = *reinterpret_cast<const int4 *>(shared + k);
+                    longer += (m.x > n || (m.x == n && k < t)) + (m.y > n || (m.y == n && k + 1 < t)) + (m.z > n || (m.z == n && k + 2 < t)) + (m.w > n || (m.w == n && k + 3 < t));
+                }
+            }
+            if (t < p.ordered && longer == seq) shared[kGatedWarps * 32] = t;
+            __syncthreads();
+            seq = uint32_t(shared[kGatedWarps * 32]);
+            __syncthreads();
+        }
+        begin = first(p, seq);
+        len = length(p, seq);
+        mark = uint64_t(begin) / kGatedMark + seq;
+    }
+    // offsets that are not as they should be may give wrong results, but no access outside the arrays
+    static __device__ __forceinline__ int64_t first(const GatedParams &p, uint32_t s) { return min(max(p.offsets[s], int64_t(0)), int64_t(p.tokens)); }
+    static __device__ __forceinline__ int length(const GatedParams &p, uint32_t s) {
+        const int64_t b = first(p, s);
+        return int(min(max(p.offsets[s + 1], b), int64_t(p.tokens)) - b);
     }
     template <typename T>
     __device__ __forceinline__ T *at(const GatedParams &p, const GatedRows &r, uint32_t c) const {
@@ -343,7 +367,7 @@ __global__ void __launch_bounds__(kGatedWarps * 32, sizeof(T) == 2 ? 2 : 3) tcu_
     GatedMeeting &meeting = *reinterpret_cast<GatedMeeting *>(gs + kForwardStages);
     const int warp = threadIdx.x >> 5;
     const uint32_t lane = threadIdx.x & 31, rank = blockIdx.x % p.ranks;
-    const GatedWalk w(p, blockIdx.x / p.ranks);
+    const GatedWalk w(p, blockIdx.x / p.ranks, reinterpret_cast<int *>(shared));
     const uint32_t c = w.c0 + 2 * lane;
     const int wide = int(min(p.channels - w.c0, uint32_t(kGatedChannels)));
     const bool c0 = c < p.channels, c1 = c + 1 < p.channels;
@@ -427,7 +451,7 @@ __global__ void __launch_bounds__(kGatedWarps * 32, 2) tcu_gated_backward_kernel
     GatedMeeting &meeting = *reinterpret_cast<GatedMeeting *>(ahead + 2);
     const int warp = threadIdx.x >> 5;
     const uint32_t lane = threadIdx.x & 31, rank = blockIdx.x % p.ranks;
-    const GatedWalk w(p, blockIdx.x / p.ranks);
+    const GatedWalk w(p, blockIdx.x / p.ranks, reinterpret_cast<int *>(shared));
     const uint32_t c = w.c0 + 2 * lane;
     const int wide = int(min(p.channels - w.c0, uint32_t(kGatedChannels)));
     const bool c0 = c < p.channels, c1 = c + 1 < p.channels;

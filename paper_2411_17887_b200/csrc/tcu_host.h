@@ -5,6 +5,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "tcu_lm.h"
 
 namespace {
@@ -23,6 +25,19 @@ inline bool ok(cudaError_t e) {
     return false;
 }
 inline tcu_status_t launched() { return cudaGetLastError() == cudaSuccess ? TCU_OK : TCU_ERR_CUDA; }
+
+// Lets a kernel have as much shared memory, on the current device, as any of its launches asks for; the devices that know are remembered.
+template <auto kernel>
+bool allow_shared(size_t most) {
+    static std::atomic<uint64_t> allowed{0};
+    int dev = 0;
+    if (!ok(cudaGetDevice(&dev))) return false;
+    const uint64_t bit = dev >= 0 && dev < 64 ? uint64_t(1) << dev : 0;
+    if (allowed.load(std::memory_order_relaxed) & bit) return true;
+    if (!ok(cudaFuncSetAttribute(reinterpret_cast<const void *>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, int(most)))) return false;
+    allowed.fetch_or(bit, std::memory_order_relaxed);
+    return true;
+}
 
 // A kernel that may be set up while the one ahead of it in the stream, of the same sequence, still runs.  A sequence ends at its
 // first launch that fails: the kernels behind it index memory by what the ones before have written.

@@ -66,11 +66,11 @@ int vector_of(size_t eb, size_t d, std::initializer_list<size_t> strides, std::i
 }
 
 // Launches a kernel with the rows that its threads have on their way, of `arrays` arrays, in shared memory.
-template <typename K>
-tcu_status_t launch(K kernel, const Shape &s, size_t eb, int arrays, const NormParams &p, cudaStream_t stream) {
-    const size_t shared = s.vec * eb == 16 ? size_t(arrays) * norm_ahead(int(s.held * eb)) * s.threads * s.held * eb : 0;
-    if (shared > 32768 && !ok(cudaFuncSetAttribute(reinterpret_cast<const void *>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, int(shared)))) return TCU_ERR_CUDA;
-    kernel<<<uint32_t(s.blocks), s.threads, shared, stream>>>(p);
+template <auto kernel>
+tcu_status_t launch(const Shape &s, size_t eb, int arrays, const NormParams &p, cudaStream_t stream) {
+    const size_t of_thread = s.vec * eb == 16 ? size_t(arrays) * norm_ahead(int(s.held * eb)) * s.held * eb : 0;
+    if (of_thread * kNormThreads > 32768 && !allow_shared<kernel>(of_thread * kNormThreads)) return TCU_ERR_CUDA;
+    kernel<<<uint32_t(s.blocks), s.threads, of_thread * s.threads, stream>>>(p);
     return launched();
 }
 
@@ -144,7 +144,7 @@ tcu_status_t tcu_layer_norm_forward(const void *d_x, size_t rows, size_t d, size
     with_type(type, [&](auto t) {
         using T = decltype(t);
         with_shape<T>(s, [&](auto v, auto e, auto lanes, auto full) {
-            st = launch(tcu_norm_forward_kernel<T, decltype(v)::value, decltype(e)::value, decltype(lanes)::value, decltype(full)::value>, s, eb, 1, p, stream);
+            st = launch<tcu_norm_forward_kernel<T, decltype(v)::value, decltype(e)::value, decltype(lanes)::value, decltype(full)::value>>(s, eb, 1, p, stream);
         });
     });
     return st;
@@ -196,7 +196,7 @@ tcu_status_t tcu_layer_norm_backward(const void *d_dy, size_t dy_stride, const v
     with_type(type, [&](auto t) {
         using T = decltype(t);
         with_shape<T>(s, [&](auto v, auto e, auto lanes, auto full) {
-            st = launch(tcu_norm_backward_kernel<T, decltype(v)::value, decltype(e)::value, decltype(lanes)::value, decltype(full)::value>, s, eb, 2, p, stream);
+            st = launch<tcu_norm_backward_kernel<T, decltype(v)::value, decltype(e)::value, decltype(lanes)::value, decltype(full)::value>>(s, eb, 2, p, stream);
         });
     });
     if (st != TCU_OK || !sums) return st;

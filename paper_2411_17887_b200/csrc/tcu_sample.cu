@@ -38,7 +38,8 @@ Division divide(uint64_t rows, uint32_t vocabulary, size_t eb) {
 template <typename T>
 tcu_status_t launch(const SampleParams &p, const Division &d, uint64_t rows, cudaStream_t stream) {
     const size_t shared = size_t(d.packs) * kSampleThreads * 16;
-    if (shared + sizeof(SampleShared) > 48000 && !ok(cudaFuncSetAttribute(tcu_sample_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, int(shared)))) return TCU_ERR_CUDA;
+    constexpr size_t kMostShared = kMostVocabulary / kSampleMaxCluster * sizeof(T) + kSampleThreads * 16;
+    if (shared + sizeof(SampleShared) > 48000 && !allow_shared<tcu_sample_kernel<T>>(kMostShared)) return TCU_ERR_CUDA;
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeClusterDimension;
     attr.val.clusterDim.x = d.blocks;

@@ -81,6 +81,30 @@ def test_packed(lens, d, dtype):
     check(x, gate, d_y, "root", None, None, lens)
 
 
+@pytest.mark.parametrize("batch,d,longest", [(30, 704, 400), (64, 330, 150), (65, 330, 150), (5, 4099, 300), (31, 650, 1)])
+def test_packed_in_the_order_of_lengths(batch, d, longest):
+    """More blocks than run at once: long sequences are walked first, whatever their place, and of equal ones each once."""
+    g = torch.Generator().manual_seed(batch)
+    lens = torch.randint(0, longest + 1, (batch,), generator=g).tolist()
+    lens[batch // 2] = lens[1]
+    x, gate, d_y = draw((sum(lens), d), torch.bfloat16, d)
+    check(x, gate, d_y, "complement", torch.randn((batch, d), device="cuda"), torch.randn((batch, d), device="cuda"), lens)
+
+
+def test_offsets_that_are_not_as_they_should_be():
+    """Wrong results, but nothing is read or written outside the arrays, and the call returns."""
+    x, gate, _ = draw((100, 64), torch.bfloat16, 6)
+    guard = torch.full((300, 64), 7.0, device="cuda", dtype=torch.bfloat16)
+    from paper_2411_17887_b200 import binding as B
+    row = lambda z: (z.data_ptr(), 0, 64)  # noqa: E731
+    for wrong in ([0, 50, 20, 1 << 40], [-5, 10, 90, 100], [100, 80, 60, 0], [1 << 62, -(1 << 62), 3, 500]):
+        offsets = torch.tensor(wrong, device="cuda")
+        args = B.tcu_gated_args(B.TCU_BF16, 0, 64, 3, 100, row(x), row(gate), row(guard[100:200]), d_offsets=offsets.data_ptr())
+        assert B.tcu_gated_forward(args, torch.cuda.current_stream().cuda_stream) == B.TCU_OK
+        torch.cuda.synchronize()
+        assert (guard[:100] == 7.0).all() and (guard[200:] == 7.0).all()
+
+
 def test_rows_behind_the_last_sequence():
     x, gate, d_y = draw((100, 24), torch.bfloat16, 5)
     x[70:] = gate[70:] = d_y[70:] = float("nan")
