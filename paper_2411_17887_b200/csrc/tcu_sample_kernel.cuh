@@ -170,7 +170,7 @@ struct Sampler {
     }
     __device__ __forceinline__ uint64_t fixed(float x) const { return uint64_t(__double2ll_rn(weight(x) * kSampleFixed)); }
     __device__ __forceinline__ void set_temperature(double temperature) {
-        inverse = 1.0 / temperature;
+        inverse = fmin(fmax(1.0 / temperature, 1e-300), 1e300);      // (0, or infinity, times nothing, or infinity, would be no number)
         parts = inverse * (32 * 1.4426950408889634074);
     }
 
@@ -352,7 +352,7 @@ struct Sampler {
 
     // The prefix of the tokens from `cut` on that reaches a number of them.  False: there are fewer.
     __device__ bool reach_number(float cut, double k, Prefix &out) {
-        const float scale = float(inverse * 64.0);
+        const float scale = float(fmin(inverse * 64.0, 1e37));
         const SampleFound f = histogram<1, kSampleBins>([&](float x) { return bin(x, cut, scale); }, [](float) { return 1u; }, k);
         if (f.bin < 0) return false;
         out = in_bin<false>(cut, scale, f.bin, k - double(f.before));
@@ -360,9 +360,9 @@ struct Sampler {
     }
     // The same for a weight, of `sum` of all that is looked at.
     __device__ bool reach_weight(float cut, double target, double sum, Prefix &out) {
-        const float scale = float(inverse * 64.0);
+        const float scale = float(fmin(inverse * 64.0, 1e37));
         // weights to about 2^-22, as parts of 2^30 of the sum
-        const float to_part = float(1073741824.0 / sum), octaves = float(inverse * 1.4426950408889634);
+        const float to_part = float(1073741824.0 / sum), octaves = float(fmin(inverse * 1.4426950408889634, 1e37));
         const SampleFound f = histogram<1, kSampleBins>(
             [&](float x) { return bin(x, cut, scale); },
             [&](float x) {
@@ -723,7 +723,7 @@ struct Sampler {
             } else {
                 // all tokens below (1 - top_p) of the mean weight together do not make up what may be left out
                 float cut = float(double(top) + log((1.0 - top_p) * sum / p.vocabulary) / inverse);
-                cut -= 1e-5f * fabsf(cut) + 1e-5f / float(inverse);                // (below it, whatever the rounding)
+                cut -= 1e-5f * fabsf(cut) + 1e-5f / float(fmin(inverse, 1e37));                // (below it, whatever the rounding)
                 cut = cut == cut ? fminf(fmaxf(cut, from), top) : from;
                 reach_weight(cut, target, sum, kept);
             }

@@ -136,6 +136,35 @@ def test_random_numbers_at_their_ends():
     assert api.sample(logits, u.double(), top_k=1).tolist() == logits.argmax(1).tolist()
 
 
+def test_temperatures_at_their_ends():
+    """So hot that all tokens are alike, so cold that only those with the largest logit are left; infinite ones from memory."""
+    logits, u = draw(20, 900, torch.float32, 11)
+    logits[:, ::7] = -math.inf
+    logits[:, 5] = logits[:, 700] = logits.amax(1) + 1.0
+    allowed = (logits > -math.inf).nonzero()[:, 1].view(20, -1)
+    for hot in (torch.full((20,), math.inf, device="cuda"), 1e299, torch.full((20,), 3e38, device="cuda")):
+        for limits in ({}, dict(top_k=allowed.shape[1])):
+            tokens = api.sample(logits, u, hot, **limits)
+            at = torch.floor(u.double() * allowed.shape[1]).long()
+            assert torch.equal(tokens, allowed.gather(1, at[:, None])[:, 0])
+        assert torch.isin(api.sample(logits, u, hot, top_p=0.5), allowed).all()
+    for cold in (1e-320, 1e-300, torch.full((20,), 1e-45, device="cuda"), 1e-20):
+        for limits in ({}, dict(top_k=100), dict(top_p=0.9), dict(min_p=0.1), dict(top_k=700, top_p=0.99)):
+            tokens = api.sample(logits, u, cold, **limits)
+            assert torch.equal(tokens, torch.where(u < 0.5, 5, 700)), (cold, limits)
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=["f32", "f16", "bf16"])
+@pytest.mark.parametrize("limits", [dict(top_k=150), dict(top_k=400), dict(top_k=3000), dict(top_k=3000, top_p=0.7), dict(top_p=0.995), dict(top_k=2000, min_p=1e-4),
+                                    dict(min_p=1e-5, top_p=0.99)], ids=str)
+def test_many_kept(limits, dtype):
+    """More tokens than are listed: histograms, with few and with many tokens in the bin that they name."""
+    for rows, v, spread in ((6, 30011, 1.0), (160, 9000, 2.0), (3, 200001, 0.5)):
+        logits, u = draw(rows, v, dtype, v, spread)
+        check(logits, u, 1.1, **limits)
+    check(logits.round(), u, 1.1, **limits)
+
+
 @pytest.mark.parametrize("dtype", TYPES, ids=["f32", "f16", "bf16"])
 def test_strides(dtype):
     wide, u = draw(20, 2100, dtype, 10)
