@@ -6,6 +6,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 namespace tcu {
 
 // ---- element types -------------------------------------------------------------------------------------------------
@@ -23,6 +25,32 @@ template <typename T, int VEC>
 struct alignas(sizeof(T) * VEC <= 16 ? sizeof(T) * VEC : 16) Pack {
     T v[VEC];
 };
+
+// Two elements at a time: a conversion of two 16-bit ones is one instruction, and so is that of either half of a word.
+template <typename T>
+__device__ __forceinline__ float2 two_f32(const Pack<T, 2> &p) {
+    if constexpr (sizeof(T) == 4) {
+        return make_float2(p.v[0], p.v[1]);
+    } else if constexpr (std::is_same_v<T, __half>) {
+        return __half22float2(*reinterpret_cast<const __half2 *>(p.v));
+    } else {
+        const uint32_t w = *reinterpret_cast<const uint32_t *>(p.v);
+        return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+    }
+}
+template <typename T>
+__device__ __forceinline__ Pack<T, 2> two_from_f32(float a, float b) {
+    Pack<T, 2> p;
+    if constexpr (sizeof(T) == 4) {
+        p.v[0] = a;
+        p.v[1] = b;
+    } else if constexpr (std::is_same_v<T, __half>) {
+        *reinterpret_cast<__half2 *>(p.v) = __floats2half2_rn(a, b);
+    } else {
+        *reinterpret_cast<__nv_bfloat162 *>(p.v) = __floats2bfloat162_rn(a, b);
+    }
+    return p;
+}
 
 // A kernel of a sequence lets the next one be set up while it runs, and touches no memory before the one ahead of it is
 // done with all of its own (which holds, in turn, for every one before).  What an earlier kernel writes is therefore not

@@ -54,7 +54,7 @@ struct GatedParams {
 template <typename T, bool PAIR>
 __device__ __forceinline__ void store_two(T *p, float a, float b, bool first, bool second) {
     if constexpr (PAIR) {
-        if (first) *reinterpret_cast<Pack<T, 2> *>(p) = Pack<T, 2>{{from_f32<T>(a), from_f32<T>(b)}};
+        if (first) *reinterpret_cast<Pack<T, 2> *>(p) = two_from_f32<T>(a, b);
     } else {
         if (first) p[0] = from_f32<T>(a);
         if (second) p[1] = from_f32<T>(b);
@@ -263,7 +263,7 @@ __device__ __forceinline__ float2 pair_of(const GatedRowsOf<T, STEPS, COPY> &row
     } else {
         v = *reinterpret_cast<const Pack<T, 2> *>(&rows.v[s][2 * lane]);
     }
-    return make_float2(to_f32<T>(v.v[0]), to_f32<T>(v.v[1]));
+    return two_f32<T>(v);
 }
 
 // Sets the rows from n on to a value.  What the tokens that are not there look like: a gate of infinity, f = 1, and zeros, nothing that comes in,

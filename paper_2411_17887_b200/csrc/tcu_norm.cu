@@ -17,7 +17,7 @@ using namespace tcu;
 constexpr uint64_t kMostRows = (uint64_t(1) << 31) - 1;
 constexpr uint64_t kMostStride = uint64_t(1) << 38;
 constexpr size_t kMostWidth = size_t(kNormThreads) * 32;
-constexpr uint32_t kSms = 148, kForwardThreads = 896, kBackwardThreads = 512;       // of an SM, by what registers allow
+constexpr uint32_t kSms = 148, kForwardThreads = 768, kForwardFull = 1024, kForwardNarrow = 512, kBackwardThreads = 512;       // of an SM, by what registers allow
 
 bool extent(size_t rows, size_t d, size_t stride, size_t eb, size_t &bytes) {
     const unsigned __int128 n = rows == 0 ? 0 : ((unsigned __int128)(rows - 1) * stride + d) * eb;
@@ -34,8 +34,9 @@ struct Shape {
     uint64_t blocks;
 };
 // (on_sm: threads that an SM holds at once)
-Shape shape_of(size_t rows, size_t d, int vec, uint32_t on_sm) {
+Shape shape_of(size_t rows, size_t d, int vec, size_t eb, uint32_t on_sm) {
     Shape s = {};
+    if (vec * eb < 16 && on_sm == kForwardThreads) on_sm = kForwardNarrow;
     s.vec = vec;
     s.held = 16;
     if (d <= 32 * 16) {
@@ -48,9 +49,10 @@ Shape shape_of(size_t rows, size_t d, int vec, uint32_t on_sm) {
     } else {
         s.held = d <= kNormThreads * 16 ? 16 : 32;
         s.threads = uint32_t((d + size_t(s.held) * 32 - 1) / (size_t(s.held) * 32)) * 32;
+        s.full = d == size_t(s.threads) * s.held;
+        if (s.full && on_sm == kForwardThreads) on_sm = kForwardFull;
         const uint64_t most = uint64_t(kSms) * (on_sm / s.threads);
         s.blocks = rows < most ? rows : most;
-        s.full = d == size_t(s.threads) * s.held;
     }
     return s;
 }
@@ -133,7 +135,7 @@ tcu_status_t tcu_layer_norm_forward(const void *d_x, size_t rows, size_t d, size
     if (!extent(rows, d, x_stride, eb, xb) || !extent(rows, d, d, eb, yb)) return TCU_ERR_INVALID_ARG;
     const bool in_place = d_x == d_y && (rows == 1 || x_stride == d);          // a row is read whole before it is written
     if ((!in_place && overlaps(d_y, yb, d_x, xb)) || overlaps(d_y, yb, d_weight, d * pb) || overlaps(d_y, yb, d_bias, d * pb)) return TCU_ERR_INVALID_ARG;
-    const Shape s = shape_of(rows, d, vector_of(eb, d, {rows > 1 ? x_stride : 0}, {d_x, d_y}), kForwardThreads);
+    const Shape s = shape_of(rows, d, vector_of(eb, d, {rows > 1 ? x_stride : 0}, {d_x, d_y}), eb, kForwardThreads);
     NormParams p = params(rows, d, param_type, eps);
     p.x = d_x;
     p.x_stride = x_stride;
@@ -152,7 +154,7 @@ tcu_status_t tcu_layer_norm_forward(const void *d_x, size_t rows, size_t d, size
 
 size_t tcu_layer_norm_workspace_bytes(size_t rows, size_t d) {
     if (d == 0 || d > kMostWidth || rows > kMostRows) return 0;
-    return shape_of(rows, d, 1, kBackwardThreads).blocks * 2 * d * 4 + 256;
+    return shape_of(rows, d, 1, 4, kBackwardThreads).blocks * 2 * d * 4 + 256;
 }
 
 tcu_status_t tcu_layer_norm_backward(const void *d_dy, size_t dy_stride, const void *d_x, size_t x_stride, size_t rows, size_t d, tcu_float_t type, const void *d_weight,
@@ -183,7 +185,7 @@ tcu_status_t tcu_layer_norm_backward(const void *d_dy, size_t dy_stride, const v
     for (const void *q : {static_cast<const void *>(d_dweight), static_cast<const void *>(d_dbias)})
         if (overlaps(d_dx, out, q, d * pb) || (sums && overlaps(d_ws, need, q, d * pb))) return TCU_ERR_INVALID_ARG;
     if (sums && overlaps(d_ws, need, d_dx, out)) return TCU_ERR_INVALID_ARG;
-    const Shape s = shape_of(rows, d, vector_of(eb, d, {rows > 1 ? x_stride : 0, rows > 1 ? dy_stride : 0}, {d_x, d_dy, d_dx}), kBackwardThreads);
+    const Shape s = shape_of(rows, d, vector_of(eb, d, {rows > 1 ? x_stride : 0, rows > 1 ? dy_stride : 0}, {d_x, d_dy, d_dx}), eb, kBackwardThreads);
     NormParams p = params(rows, d, param_type, eps);
     p.x = d_x;
     p.x_stride = x_stride;

@@ -89,7 +89,11 @@ template <typename T, int VEC, int E>
 struct NormPart {
     static constexpr int kPacks = E / VEC;
     Pack<T, VEC> raw[kPacks];
-    __device__ __forceinline__ float get(int j, int e) const { return to_f32<T>(raw[j].v[e]); }
+    __device__ __forceinline__ float get(int j, int e) const {
+        if constexpr (VEC == 1) return to_f32<T>(raw[j].v[e]);
+        const float2 two = two_f32<T>(*reinterpret_cast<const Pack<T, 2> *>(&raw[j].v[e & ~1]));
+        return e & 1 ? two.y : two.x;
+    }
 };
 
 // The row's thread, its number of threads, and the rows that it comes to.  (The groups of a warp go through as many rounds each, as they add
@@ -110,7 +114,7 @@ struct NormPlace {
 
 // The rows of an array that a thread comes to, some of them on their way to shared memory while it works on one: every thread copies, and reads,
 // its own elements, so that nobody waits for anybody.  Elements that cannot be copied 16 bytes at a time, or are too many, are read
-// when they are needed.  FULL: every thread has all its elements.
+// one row ahead into registers (forward), or when they are needed (backward, which has none left).  FULL: every thread has all its elements.
 template <typename T, int VEC, int E, bool FULL>
 struct NormAhead {
     static constexpr int kPacks = E / VEC;
@@ -151,6 +155,16 @@ struct NormAhead {
     }
 };
 
+template <typename T, int VEC>
+__device__ __forceinline__ void round_pack(Pack<T, VEC> &out, const float *v) {
+    if constexpr (VEC == 1) {
+        out.v[0] = from_f32<T>(v[0]);
+    } else {
+#pragma unroll
+        for (int e = 0; e < VEC; e += 2) *reinterpret_cast<Pack<T, 2> *>(&out.v[e]) = two_from_f32<T>(v[e], v[e + 1]);
+    }
+}
+
 template <typename T>
 __device__ __forceinline__ float param(const void *p, bool f32, uint32_t i) {
     return f32 ? static_cast<const float *>(p)[i] : to_f32<T>(static_cast<const T *>(p)[i]);
@@ -189,10 +203,18 @@ __global__ void __launch_bounds__(LANES ? kNormWarps * 32 : kNormThreads) tcu_no
         }
     };
     for (uint32_t k = 0; k + 1 < kRows; ++k) ask(k);
+    NormPart<T, VEC, E> next;              // without shared memory: on its way to registers
+    if (!Ahead::kShared && left > 0) next = x_ahead.take(0, at, step, p.d);
     T *y = static_cast<T *>(p.y) + uint64_t(place.row) * p.d + at;
     for (; left > 0; --left, row += place.step, y += uint64_t(place.step) * p.d) {
         if constexpr (Ahead::kShared) asm volatile("cp.async.wait_group %0;" ::"n"(int(kRows) - 2) : "memory");
-        const NormPart<T, VEC, E> x = x_ahead.take(stage, at, step, p.d);
+        NormPart<T, VEC, E> x;
+        if constexpr (Ahead::kShared) {
+            x = x_ahead.take(stage, at, step, p.d);
+        } else {
+            x = next;
+            if (left > 1) next = x_ahead.take(0, at, step, p.d);
+        }
         ask(stage == 0 ? kRows - 1 : stage - 1);
         stage = stage + 1 == kRows ? 0 : stage + 1;
         float sum[1] = {0.0f}, v[E];
@@ -228,7 +250,8 @@ __global__ void __launch_bounds__(LANES ? kNormWarps * 32 : kNormThreads) tcu_no
             if ((FULL || at + j * step < p.d) && (LANES % 32 == 0 || row < p.rows)) {
                 Pack<T, VEC> out;
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) out.v[e] = from_f32<T>(fmaf((v[j * VEC + e] - more) * r, weight[j * VEC + e], bias[j * VEC + e]));
+                for (int e = 0; e < VEC; ++e) v[j * VEC + e] = fmaf((v[j * VEC + e] - more) * r, weight[j * VEC + e], bias[j * VEC + e]);
+                round_pack(out, v + j * VEC);
                 *reinterpret_cast<Pack<T, VEC> *>(y + j * step) = out;
             }
     }
@@ -308,13 +331,15 @@ __global__ void __launch_bounds__(LANES ? kNormWarps * 32 : kNormThreads) tcu_no
         for (int j = 0; j < kPacks; ++j)
             if ((FULL || at + j * step < p.d) && (LANES % 32 == 0 || row < p.rows)) {
                 Pack<T, VEC> out;
+                float rounded[VEC];
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
                     const float dy = d_y.get(j, e), u = ((x.get(j, e) - mean) - more) * r;
-                    out.v[e] = from_f32<T>(r * fmaf(-u, mean_eu, fmaf(weight[j * VEC + e], dy, -mean_e)));
+                    rounded[e] = r * fmaf(-u, mean_eu, fmaf(weight[j * VEC + e], dy, -mean_e));
                     d_weight[j * VEC + e] = fmaf(dy, u, d_weight[j * VEC + e]);
                     d_bias[j * VEC + e] += dy;
                 }
+                round_pack(out, rounded);
                 if (p.d_x) *reinterpret_cast<Pack<T, VEC> *>(d_x + j * step) = out;
             }
     }
