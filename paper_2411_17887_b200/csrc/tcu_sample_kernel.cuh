@@ -80,6 +80,7 @@ struct SampleShared {
     uint32_t warp_u32[2][kSampleWarps], warp_ties[kSampleWarps];
     float warp_max[kSampleWarps];
     uint32_t count;                        // of this block's candidates
+    uint32_t counts[kSampleMaxCluster];    // of all blocks'
     uint2 list[kSampleList];               // their keys and tokens
     uint32_t ranges[kSampleRanges];        // keys of the largest logits of its ranges
     uint32_t all_ranges[kSampleMaxCluster * kSampleRanges];
@@ -224,6 +225,26 @@ struct Sampler {
         for (int k = 0; k < kSampleWarps; ++k) sum += s.warp_sum[k];
         return sum;
     }
+    // Two sums at once.
+    __device__ double2 block_sums(double x, double y) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) {
+            x += __shfl_xor_sync(~0u, x, o);
+            y += __shfl_xor_sync(~0u, y, o);
+        }
+        __syncthreads();
+        if (lane == 0) {
+            s.warp_sum[warp] = x;
+            s.warp_u64[warp] = uint64_t(__double_as_longlong(y));
+        }
+        __syncthreads();
+        double2 sum = make_double2(0.0, 0.0);
+        for (int k = 0; k < kSampleWarps; ++k) {
+            sum.x += s.warp_sum[k];
+            sum.y += __longlong_as_double(int64_t(s.warp_u64[k]));
+        }
+        return sum;
+    }
     template <typename Keep>
     __device__ double thread_sum(Keep keep) const {            // of the weights of the tokens that are kept
         double sum[4] = {0.0, 0.0, 0.0, 0.0};
@@ -301,16 +322,23 @@ struct Sampler {
         const bool some = threadIdx.x * each_thread < share;
         uint64_t mine[BINS / kSampleThreads], sum = 0;
 #pragma unroll
-        for (uint32_t j = 0; j < BINS / kSampleThreads; ++j) {
-            mine[j] = 0;
-            if (some && j < each_thread)
-                for (uint32_t k = 0; k < ranks; ++k) {
-                    const auto *h = cluster.map_shared_rank(s.hist, k) + own + j;
-                    mine[j] += h[0];
-                    if constexpr (LIMBS == 3) mine[j] += (uint64_t(h[BINS]) << kSampleLimb) + (uint64_t(h[2 * BINS]) << (2 * kSampleLimb));
+        for (uint32_t j = 0; j < BINS / kSampleThreads; ++j) mine[j] = 0;
+        if (some) {
+#pragma unroll
+            for (uint32_t k = 0; k < kSampleMaxCluster; ++k) {           // (unrolled: all blocks' bins are on their way at once)
+                if (k < ranks) {
+                    const auto *h = cluster.map_shared_rank(s.hist, k) + own;
+#pragma unroll
+                    for (uint32_t j = 0; j < BINS / kSampleThreads; ++j)
+                        if (j < each_thread) {
+                            mine[j] += h[j];
+                            if constexpr (LIMBS == 3) mine[j] += (uint64_t(h[BINS + j]) << kSampleLimb) + (uint64_t(h[2 * BINS + j]) << (2 * kSampleLimb));
+                        }
                 }
-            sum += mine[j];
+            }
         }
+#pragma unroll
+        for (uint32_t j = 0; j < BINS / kSampleThreads; ++j) sum += mine[j];
         uint64_t upto = sum;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -394,8 +422,8 @@ struct Sampler {
                     }
                 }
             }
-            const double in_here = block_sum(of_bin[0] + of_bin[1]), ahead_here = block_sum(ahead[0] + ahead[1]);
-            const SampleWord *w = exchange({ahead_here, uint32_t(__double2hiint(in_here)), uint32_t(__double2loint(in_here))});
+            const double2 here = block_sums(ahead[0] + ahead[1], of_bin[0] + of_bin[1]);
+            const SampleWord *w = exchange({here.x, uint32_t(__double2hiint(here.y)), uint32_t(__double2loint(here.y))});
             double before = 0.0, in = 0.0;
             for (uint32_t k = 0; k < ranks; ++k) {
                 before += w[k].a;
@@ -478,27 +506,31 @@ struct Sampler {
                 if (is(to_f32<T>(q.v[e]))) list_one(to_f32<T>(q.v[e]), at(j) + e);
         }
         __syncthreads();
-        return count_candidates(0.0, 0.0, nullptr, nullptr);
+        return count_candidates(0.0, 0.0f, nullptr, nullptr);
     }
     __device__ __forceinline__ void list_one(float x, int token) {
         if (*const_cast<volatile uint32_t *>(&s.count) > kSampleList) return;                // too many: no more need to be counted
         const uint32_t to = atomicAdd(&s.count, 1u);
         if (to < kSampleList) s.list[to] = make_uint2(sample_key(x), uint32_t(token));
     }
-    // The row's number of candidates, and its sums of two values.
-    __device__ uint32_t count_candidates(double a, double b, double *sum_a, double *sum_b) {
-        const SampleWord *w = exchange({a, s.count, 0});
+    // The row's number of candidates, and its sums of two values, the second to 2^-22.
+    __device__ uint32_t count_candidates(double a, float b, double *sum_a, float *sum_b) {
+        const SampleWord *w = exchange({a, s.count, __float_as_uint(b)});
+        if (threadIdx.x < ranks) s.counts[threadIdx.x] = w[threadIdx.x].b;
+        __syncthreads();
         uint32_t total = 0;
         for (uint32_t k = 0; k < ranks; ++k) total += w[k].b;
         if (sum_a) {
             *sum_a = 0.0;
-            for (uint32_t k = 0; k < ranks; ++k) *sum_a += w[k].a;
-            const SampleWord *q = exchange({b, 0, 0});
-            *sum_b = 0.0;
-            for (uint32_t k = 0; k < ranks; ++k) *sum_b += q[k].a;
+            *sum_b = 0.0f;
+            for (uint32_t k = 0; k < ranks; ++k) {
+                *sum_a += w[k].a;
+                *sum_b += __uint_as_float(w[k].c);
+            }
         }
         return total;
     }
+
     // A candidate as a number: in rising order the logits fall, the lower token first among equals.  Or, for the order of tokens, turned around.
     static __device__ __forceinline__ uint64_t candidate(uint32_t key, uint32_t token) { return uint64_t(~key) << 32 | token; }
     static __device__ __forceinline__ uint64_t turned(uint64_t v) { return v << 32 | v >> 32; }
@@ -547,10 +579,7 @@ struct Sampler {
     __device__ void sort_candidates(uint32_t total) {
         for (uint32_t i = threadIdx.x; i < total; i += kSampleThreads) {
             uint32_t k = 0, from = i;
-            for (uint32_t n = *cluster.map_shared_rank(&s.count, 0); from >= n; n = *cluster.map_shared_rank(&s.count, k)) {
-                from -= n;
-                ++k;
-            }
+            while (from >= s.counts[k]) from -= s.counts[k++];
             const uint2 q = cluster.map_shared_rank(s.list, k)[from];
             s.sorted[i] = candidate(q.x, q.y);
         }
@@ -694,7 +723,8 @@ struct Sampler {
             const float from = kept.whole ? kept.edge : sample_value(sample_key(kept.edge) + 1);
             // their weight, and that of the largest ones, which are listed
             const float cut_list = fmaxf(from, from_k);
-            double sums[2] = {0.0, 0.0}, large = 0.0, sum, sum_large;
+            double sums[2] = {0.0, 0.0}, large = 0.0, sum;
+            float sum_large;
             if (threadIdx.x == 0) s.count = 0;
             __syncthreads();
 #pragma unroll 1
@@ -713,12 +743,12 @@ struct Sampler {
                     }
                 }
             }
-            const double sum_here = block_sum(sums[0] + sums[1]), large_here = block_sum(large);
-            const uint32_t total = count_candidates(sum_here, large_here, &sum, &sum_large);
+            const double2 here = block_sums(sums[0] + sums[1], large);
+            const uint32_t total = count_candidates(here.x, float(here.y), &sum, &sum_large);
             const double at_edge = kept.whole ? 0.0 : weight(kept.edge), target = top_p * (sum + kept.ties * at_edge);
             if (!kept.whole && sum < target) {               // it ends within the edge
                 kept.ties = uint32_t(fewest(sum, at_edge, target, kept.ties));
-            } else if (total <= kSampleList && sum_large >= target * (1.0 + 1e-9)) {
+            } else if (total <= kSampleList && sum_large >= target * (1.0 + 1e-5)) {
                 return draw_listed(total, total, top_p, target);
             } else {
                 // all tokens below (1 - top_p) of the mean weight together do not make up what may be left out
