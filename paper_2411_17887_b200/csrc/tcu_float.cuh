@@ -52,6 +52,10 @@ __device__ __forceinline__ Pack<T, 2> two_from_f32(float a, float b) {
     return p;
 }
 
+// The blocks of a cluster may touch one another's shared memory once all of them run: each says so when it begins, and waits before it does.
+__device__ __forceinline__ void cluster_begin() { asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_begun() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
 // A kernel of a sequence lets the next one be set up while it runs, and touches no memory before the one ahead of it is
 // done with all of its own (which holds, in turn, for every one before).  What an earlier kernel writes is therefore not
 // read through pointers that promise the compiler that nobody writes it.

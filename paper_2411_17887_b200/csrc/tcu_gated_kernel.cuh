@@ -367,6 +367,7 @@ __global__ void __launch_bounds__(kGatedWarps * 32, sizeof(T) == 2 ? 2 : 3) tcu_
     GatedMeeting &meeting = *reinterpret_cast<GatedMeeting *>(gs + kForwardStages);
     const int warp = threadIdx.x >> 5;
     const uint32_t lane = threadIdx.x & 31, rank = blockIdx.x % p.ranks;
+    if (p.ranks > 1) cluster_begin();
     const GatedWalk w(p, blockIdx.x / p.ranks, reinterpret_cast<int *>(shared));
     const uint32_t c = w.c0 + 2 * lane;
     const int wide = int(min(p.channels - w.c0, uint32_t(kGatedChannels)));
@@ -390,6 +391,7 @@ __global__ void __launch_bounds__(kGatedWarps * 32, sizeof(T) == 2 ? 2 : 3) tcu_
     };
     fetch(0, t);
     fetch(1, t + stride);
+    if (p.ranks > 1) cluster_begun();
     T *py = w.at<T>(p, p.y, c) + t * p.y.token;
     uint32_t buf = 0, stage = 0;
     for (int done = 0; done < w.len; done += stride, t += stride, buf ^= 1) {
@@ -451,6 +453,7 @@ __global__ void __launch_bounds__(kGatedWarps * 32, 2) tcu_gated_backward_kernel
     GatedMeeting &meeting = *reinterpret_cast<GatedMeeting *>(ahead + 2);
     const int warp = threadIdx.x >> 5;
     const uint32_t lane = threadIdx.x & 31, rank = blockIdx.x % p.ranks;
+    if (p.ranks > 1) cluster_begin();
     const GatedWalk w(p, blockIdx.x / p.ranks, reinterpret_cast<int *>(shared));
     const uint32_t c = w.c0 + 2 * lane;
     const int wide = int(min(p.channels - w.c0, uint32_t(kGatedChannels)));
@@ -478,6 +481,7 @@ __global__ void __launch_bounds__(kGatedWarps * 32, 2) tcu_gated_backward_kernel
         commit_copies();
     };
     fetch(0, t);
+    if (p.ranks > 1) cluster_begun();
     T *pdx = w.at<T>(p, p.d_x, c) + t * p.d_x.token, *pdg = w.at<T>(p, p.d_gate, c) + t * p.d_gate.token;
     uint32_t buf = 0;
     for (int done = 0; done < tiles; done += int(p.ranks), t -= stride, buf ^= 1) {

@@ -685,8 +685,10 @@ struct Sampler {
     }
 
     __device__ void run() {
+        cluster_begin();
         const double temperature = p.temperature.at(row), min_p = p.min_p.at(row), top_p = p.top_p.at(row), k = p.top_k.at(row);
         const float of_block = block_max(load());
+        cluster_begun();
         const bool limited_k = k > 0.0 && k < double(p.vocabulary), limited_m = min_p > 0.0, limited_p = top_p < 1.0;
         if (!(temperature > 0.0) || k == 1.0 || min_p > 1.0 || top_p <= 0.0) return greedy(of_block);
         set_temperature(temperature);
@@ -711,8 +713,10 @@ struct Sampler {
         Prefix kept = {low, 0, true};
         if (limited_k) {
             const float cut = fmaxf(low, from_k);
-            const uint32_t total = list_candidates([&](float x) { return x >= cut; });
-            if (total <= kSampleList) return draw_listed(total, uint32_t(fmin(k, double(total))), top_p, -1.0);
+            if (limited_m || from_k > -INFINITY || p.vocabulary <= kSampleList) {          // (else they are too many)
+                const uint32_t total = list_candidates([&](float x) { return x >= cut; });
+                if (total <= kSampleList) return draw_listed(total, uint32_t(fmin(k, double(total))), top_p, -1.0);
+            }
             reach_number(cut, k, kept);                      // (or there are fewer than k from `low` on: all of them)
         } else if (limited_m) {
             const uint32_t total = list_candidates([&](float x) { return x >= low; });
@@ -722,7 +726,7 @@ struct Sampler {
             // what top_k and min_p leave: the tokens above the edge (from the edge on), and so many of it
             const float from = kept.whole ? kept.edge : sample_value(sample_key(kept.edge) + 1);
             // their weight, and that of the largest ones, which are listed
-            const float cut_list = fmaxf(from, from_k);
+            const float cut_list = from_k > -INFINITY || p.vocabulary <= kSampleList ? fmaxf(from, from_k) : INFINITY;
             double sums[2] = {0.0, 0.0}, large = 0.0, sum;
             float sum_large;
             if (threadIdx.x == 0) s.count = 0;
