@@ -732,7 +732,9 @@ def sample(logits, uniform, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, outp
     if vocabulary > 1 and logits.stride(1) != 1:
         logits = logits.contiguous()
     tokens = logits.new_empty(rows, dtype=torch.int64)
-    log_prob = logits.new_empty(rows, dtype=torch.float32) if output_log_prob else None
+    log_prob = None
+    if output_log_prob:
+        log_prob = torch.empty_like(uniform) if uniform.dtype == torch.float32 else logits.new_empty(rows, dtype=torch.float32)
     args = B.tcu_sample_args(_FLOAT[dtype], rows, vocabulary, logits.data_ptr(), logits.stride(0), uniform.data_ptr(), int(uniform.dtype == torch.float64), tokens.data_ptr(),
                              _ptr(log_prob), d_temperature=d_temperature, d_top_k=d_top_k, d_top_p=d_top_p, d_min_p=d_min_p, temperature=float(temperature),
                              top_k=min(max(int(top_k), 0), 1 << 40), top_p=float(top_p), min_p=float(min_p))
