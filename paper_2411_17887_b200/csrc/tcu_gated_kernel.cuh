@@ -181,15 +181,14 @@ struct GatedWalk {
     }
 };
 
-// Rows of the inputs on their way to shared memory.  A warp copies what it reads itself, so that no barrier of the block waits for data.
-// COPY bytes an access, 16 or 4 where all rows begin at multiples of them.  COPY 2: rows of 16-bit elements that begin anywhere are copied in the aligned
-// words that hold them (a word that holds an element lies in the same allocation), and shifted by one element, where a row begins in
-// the middle of a word, when they are read.
-__device__ __forceinline__ void copy_async4(void *to, const void *from) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(uint32_t(__cvta_generic_to_shared(to))), "l"(from) : "memory");
-}
+// Rows of the inputs on their way to shared memory, 16 bytes a piece.  A warp copies what it reads itself, so that no barrier of the block waits for data.
+// COPY 16: all rows begin at multiples of 16 bytes.  COPY 4, 2: at multiples of that many bytes; the pieces that hold a row are copied, the last one as far
+// as the row goes, and the row is read from behind what its first piece holds ahead of it (bytes of the same allocation: those begin at larger boundaries).
 __device__ __forceinline__ void copy_async16(void *to, const void *from) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(uint32_t(__cvta_generic_to_shared(to))), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copy_async16(void *to, const void *from, uint32_t bytes) {         // the rest is set to zero
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(uint32_t(__cvta_generic_to_shared(to))), "l"(from), "r"(bytes) : "memory");
 }
 template <int N>
 __device__ __forceinline__ void copies_but(void) {                  // waits for all but the last N commits of this thread
@@ -199,71 +198,67 @@ __device__ __forceinline__ void commit_copies() { asm volatile("cp.async.commit_
 
 template <typename T, int STEPS, int COPY>
 struct alignas(16) GatedRowsOf {           // of a warp
-    T v[STEPS][kGatedChannels + (COPY == 2 ? 2 : 0)];
+    static constexpr int kPieces = kGatedChannels * int(sizeof(T)) / 16 + (COPY == 16 ? 0 : 1);
+    T v[STEPS][kPieces * 16 / sizeof(T)];
 };
 
 // One array's rows, those of a tile after those of another.  Rows that are not there, and channels, are left as they are.
 template <typename T, int STEPS, int COPY>
 struct GatedSource {
-    static constexpr int kEach = COPY == 2 ? 2 : COPY / int(sizeof(T));        // elements of a piece
-    static constexpr int kRow = kGatedChannels / kEach;                        // pieces of a row
-    static constexpr int kRows = kRow < 32 ? 32 / kRow : 1, kCols = kRow < 32 ? 1 : kRow / 32;         // rows of an access, accesses of a row
-    const T *at;                           // row of this lane's first piece of the next tile
+    using Rows = GatedRowsOf<T, STEPS, COPY>;
+    static constexpr int kPieces = Rows::kPieces, kEach = 16 / int(sizeof(T)), kRows = 32 / kPieces;   // COPY 16: rows of an access
+    const T *at;                           // row (COPY 16: of this lane's first piece) of the next tile
     int64_t stride, step;                  // a row to the next one, a tile to the next one (in elements)
     __device__ __forceinline__ GatedSource(const T *array, int first, int64_t stride, int tokens_on) : stride(stride) {
-        at = array + (int64_t(first) + row()) * stride;
+        at = array + (int64_t(first) + (COPY == 16 ? int((threadIdx.x & 31) / kPieces) : 0)) * stride;
         step = tokens_on * stride;
     }
-    static __device__ __forceinline__ int row() { return kRows == 1 ? 0 : int((threadIdx.x & 31) / kRow); }
-    // How many elements the row of token s of a tile that begins with `row` lies behind the word that it begins in.
-    static __device__ __forceinline__ uint32_t shift(const T *row, int64_t stride, int s) {
-        return COPY == 2 ? uint32_t((reinterpret_cast<uintptr_t>(row) / sizeof(T) + uint64_t(stride) * s) & 1) : 0;
+    // How many bytes behind its first piece the row of token s of a tile begins, whose first row is `row`.
+    static __device__ __forceinline__ uint32_t behind(const T *row, int64_t stride, int s) {
+        return COPY == 16 ? 0 : (uint32_t(reinterpret_cast<uintptr_t>(row)) + uint32_t(stride) * uint32_t(sizeof(T)) * uint32_t(s)) & 15;
     }
     template <bool ALL>
-    __device__ __forceinline__ void copy(GatedRowsOf<T, STEPS, COPY> &rows, int n, int channels) {
+    __device__ __forceinline__ void copy(Rows &rows, int n, int channels) {
         const uint32_t lane = threadIdx.x & 31;
-        const T *src = at;
+        if constexpr (COPY == 16) {
+            const int row = int(lane / kPieces), c = int(lane % kPieces) * kEach;
+            const T *src = at + c;
 #pragma unroll
-        for (int k = 0; k < STEPS; k += kRows, src += stride * kRows) {
-            if constexpr (COPY == 2) {
-                const int off = int(shift(src, 0, 0));
-                if ((ALL || k < n) && 2 * int(lane) - off < channels) copy_async4(&rows.v[k][2 * lane], src + (2 * int(lane) - off));
-            } else {
+            for (int k = 0; k < STEPS; k += kRows, src += stride * kRows)
+                if ((ALL || row + k < n) && c < channels) copy_async16(&rows.v[row + k][c], src);
+        } else {
 #pragma unroll
-                for (int j = 0; j < kCols; ++j) {
-                    const int c = (lane % kRow + j * 32) * kEach;
-                    if ((ALL || row() + k < n) && c < channels) {
-                        if constexpr (COPY == 16) copy_async16(&rows.v[row() + k][c], src + c);
-                        else copy_async4(&rows.v[row() + k][c], src + c);
-                    }
-                }
+            for (uint32_t k = 0; k < STEPS * kPieces; k += 32) {
+                const uint32_t q = k + lane, row = q / kPieces, piece = q - row * kPieces;
+                const uintptr_t begin = reinterpret_cast<uintptr_t>(at + int64_t(row) * stride);
+                const int left = int(begin & 15) + channels * int(sizeof(T)) - 16 * int(piece);
+                if (int(row) < (ALL ? STEPS : n) && left > 0)
+                    copy_async16(&rows.v[row][piece * kEach], reinterpret_cast<const void *>((begin & ~uintptr_t(15)) + 16 * piece), uint32_t(min(left, 16)));
             }
-        }
-        if constexpr (COPY == 2) {         // the 33rd words, lane s that of row s
-            if (int(lane) < min(n, STEPS) && channels == kGatedChannels && shift(at, stride, lane)) copy_async4(&rows.v[lane][kGatedChannels], at + stride * lane + (kGatedChannels - 1));
         }
     }
     // the first n rows are there, and `channels`
-    __device__ __forceinline__ void load(GatedRowsOf<T, STEPS, COPY> &rows, int n, int channels) {
+    __device__ __forceinline__ void load(Rows &rows, int n, int channels) {
         if (n >= STEPS) copy<true>(rows, n, channels);
         else copy<false>(rows, n, channels);
         at += step;
     }
 };
 
-// Two channels of a token of a warp, whose row is `shift` elements behind a word.
+// Two channels of a token of a warp, whose row begins `behind` its first piece.
 template <typename T, int STEPS, int COPY>
-__device__ __forceinline__ float2 pair_of(const GatedRowsOf<T, STEPS, COPY> &rows, int s, uint32_t shift) {
+__device__ __forceinline__ float2 pair_of(const GatedRowsOf<T, STEPS, COPY> &rows, int s, uint32_t behind) {
     const uint32_t lane = threadIdx.x & 31;
-    Pack<T, 2> v;
-    if constexpr (COPY == 2) {
-        const uint32_t *words = reinterpret_cast<const uint32_t *>(&rows.v[s][2 * lane]);
-        const uint32_t both = __funnelshift_r(words[0], words[1], shift * 16);
-        v = *reinterpret_cast<const Pack<T, 2> *>(&both);
+    if constexpr (COPY == 16) {
+        return two_f32<T>(*reinterpret_cast<const Pack<T, 2> *>(&rows.v[s][2 * lane]));
+    } else if constexpr (sizeof(T) == 4) {
+        const T *at = &rows.v[s][2 * lane] + behind / 4;
+        return make_float2(at[0], at[1]);
     } else {
-        v = *reinterpret_cast<const Pack<T, 2> *>(&rows.v[s][2 * lane]);
+        const uint32_t *words = reinterpret_cast<const uint32_t *>(&rows.v[s][2 * lane]) + behind / 4;
+        const uint32_t two = COPY == 2 ? __funnelshift_r(words[0], words[1], (behind & 2) * 8) : words[0];
+        return two_f32<T>(*reinterpret_cast<const Pack<T, 2> *>(&two));
     }
-    return two_f32<T>(v);
 }
 
 // Sets the rows from n on to a value.  What the tokens that are not there look like: a gate of infinity, f = 1, and zeros, nothing that comes in,
@@ -342,13 +337,15 @@ __device__ __forceinline__ float2 meet(GatedMeeting &m, uint32_t buf, const floa
     return apply(m.warps[buf][place][lane], at_tile);
 }
 
-constexpr uint32_t kForwardStages = 3, kBackwardStages = 2;
+template <int COPY>
+constexpr uint32_t kForwardStages = COPY == 16 ? 3 : 2;                  // (longer rows: two blocks an SM have no room for three)
+constexpr uint32_t kBackwardStages = 2;
 template <typename T>
 constexpr int kForwardSteps = sizeof(T) == 2 ? 16 : 8;                  // tokens of a warp
 constexpr int kBackwardSteps = 8;
 template <typename T, int COPY>
 constexpr uint32_t forward_bytes(uint32_t ranks) {
-    return kForwardStages * 2 * kGatedWarps * sizeof(GatedRowsOf<T, kForwardSteps<T>, COPY>) + sizeof(float4) * 32 * (2 * kGatedWarps + (ranks > 1 ? 2 * ranks : 0));
+    return kForwardStages<COPY> * 2 * kGatedWarps * sizeof(GatedRowsOf<T, kForwardSteps<T>, COPY>) + sizeof(float4) * 32 * (2 * kGatedWarps + (ranks > 1 ? 2 * ranks : 0));
 }
 template <typename T, int COPY>
 constexpr uint32_t backward_bytes(uint32_t ranks) {
@@ -363,8 +360,8 @@ __global__ void __launch_bounds__(kGatedWarps * 32, sizeof(T) == 2 ? 2 : 3) tcu_
     extern __shared__ __align__(16) uint8_t shared[];
     using Stage = GatedRowsOf<T, STEPS, COPY>[kGatedWarps];
     using Source = GatedSource<T, STEPS, COPY>;
-    Stage *xs = reinterpret_cast<Stage *>(shared), *gs = xs + kForwardStages;
-    GatedMeeting &meeting = *reinterpret_cast<GatedMeeting *>(gs + kForwardStages);
+    Stage *xs = reinterpret_cast<Stage *>(shared), *gs = xs + kForwardStages<COPY>;
+    GatedMeeting &meeting = *reinterpret_cast<GatedMeeting *>(gs + kForwardStages<COPY>);
     const int warp = threadIdx.x >> 5;
     const uint32_t lane = threadIdx.x & 31, rank = blockIdx.x % p.ranks;
     if (p.ranks > 1) cluster_begin();
@@ -389,15 +386,15 @@ __global__ void __launch_bounds__(kGatedWarps * 32, sizeof(T) == 2 ? 2 : 3) tcu_
         }
         commit_copies();
     };
-    fetch(0, t);
-    fetch(1, t + stride);
+    constexpr uint32_t kStages = kForwardStages<COPY>;
+    for (uint32_t k = 0; k + 1 < kStages; ++k) fetch(k, t + int(k) * stride);
     if (p.ranks > 1) cluster_begun();
     T *py = w.at<T>(p, p.y, c) + t * p.y.token;
     uint32_t buf = 0, stage = 0;
     for (int done = 0; done < w.len; done += stride, t += stride, buf ^= 1) {
-        copies_but<1>();
+        copies_but<int(kStages) - 2>();
         __syncwarp();                                              // the rows are here, and the ones before have been read
-        fetch(stage == 0 ? 2 : stage - 1, t + 2 * stride);
+        fetch(stage == 0 ? kStages - 1 : stage - 1, t + (int(kStages) - 1) * stride);
         const int n = w.len - t;                                   // tokens of this warp, if it has so many
         const bool here = n > 0;
         float2 prod[STEPS], local[STEPS], a = both(1.0f), b = both(0.0f);
@@ -408,8 +405,8 @@ __global__ void __launch_bounds__(kGatedWarps * 32, sizeof(T) == 2 ? 2 : 3) tcu_
             }
 #pragma unroll
             for (int s = 0; s < STEPS; ++s) {
-                const float2 x = pair_of(xs[stage][warp], s, Source::shift(px + t * p.x.token, p.x.token, s));
-                const float2 g = pair_of(gs[stage][warp], s, Source::shift(pg + t * p.gate.token, p.gate.token, s));
+                const float2 x = pair_of(xs[stage][warp], s, Source::behind(px + t * p.x.token, p.x.token, s));
+                const float2 g = pair_of(gs[stage][warp], s, Source::behind(pg + t * p.gate.token, p.gate.token, s));
                 float2 f, rest;
                 sigmoids<sizeof(T) == 4>(g, f, rest);
                 a = mul2(a, f);
@@ -432,7 +429,7 @@ __global__ void __launch_bounds__(kGatedWarps * 32, sizeof(T) == 2 ? 2 : 3) tcu_
             }
         }
         py += stride * p.y.token;
-        stage = stage == 2 ? 0 : stage + 1;
+        stage = stage + 1 == kStages ? 0 : stage + 1;
     }
     if (p.ranks > 1) cooperative_groups::this_cluster().sync();           // (nobody leaves, or writes the state, before all have read)
     if (p.state_out && warp == 0 && rank == 0) {
@@ -500,11 +497,11 @@ __global__ void __launch_bounds__(kGatedWarps * 32, 2) tcu_gated_backward_kernel
             }
 #pragma unroll
             for (int s = 0; s < STEPS; ++s) {
-                sigmoids<sizeof(T) == 4>(pair_of(gs[buf][warp], s, Source::shift(pg + t * p.gate.token, p.gate.token, s)), f[s], rest[s]);
-                in[s] = taken_in<INPUT>(f[s], rest[s], pair_of(xs[buf][warp], s, Source::shift(px + t * p.x.token, p.x.token, s)));
+                sigmoids<sizeof(T) == 4>(pair_of(gs[buf][warp], s, Source::behind(pg + t * p.gate.token, p.gate.token, s)), f[s], rest[s]);
+                in[s] = taken_in<INPUT>(f[s], rest[s], pair_of(xs[buf][warp], s, Source::behind(px + t * p.x.token, p.x.token, s)));
                 a = mul2(a, f[s]);
                 b = fma2(f[s], b, in[s]);
-                r = fma2(a, pair_of(ds[buf][warp], s, Source::shift(pd + t * p.d_y.token, p.d_y.token, s)), r);       // of d_t flows back to the first token: d_t times all f up to its own
+                r = fma2(a, pair_of(ds[buf][warp], s, Source::behind(pd + t * p.d_y.token, p.d_y.token, s)), r);       // of d_t flows back to the first token: d_t times all f up to its own
             }
         }
         ahead[buf][warp][lane] = pairs_of(a, b);
@@ -521,7 +518,7 @@ __global__ void __launch_bounds__(kGatedWarps * 32, 2) tcu_gated_backward_kernel
             }
 #pragma unroll
             for (int s = STEPS - 1; s >= 0; --s) {
-                const float2 grad = add2(pair_of(ds[buf][warp], s, Source::shift(pd + t * p.d_y.token, p.d_y.token, s)), out);
+                const float2 grad = add2(pair_of(ds[buf][warp], s, Source::behind(pd + t * p.d_y.token, p.d_y.token, s)), out);
                 out = mul2(f[s], grad);
                 before[s] = mul2(grad, gate_slope<INPUT>(f[s], rest[s], before[s], in[s]));
                 rest[s] = taken_in<INPUT>(f[s], rest[s], grad);
