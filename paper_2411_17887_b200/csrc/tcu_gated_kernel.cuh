@@ -227,13 +227,19 @@ struct GatedSource {
             for (int k = 0; k < STEPS; k += kRows, src += stride * kRows)
                 if ((ALL || row + k < n) && c < channels) copy_async16(&rows.v[row + k][c], src);
         } else {
+            constexpr int kWhole = kPieces - 1, kAt = 32 / kWhole;             // the last piece of every row apart from the others
+            const int first = int(lane / kWhole), piece = int(lane % kWhole), bytes = channels * int(sizeof(T));
+            uintptr_t begin = reinterpret_cast<uintptr_t>(at + int64_t(first) * stride);
 #pragma unroll
-            for (uint32_t k = 0; k < STEPS * kPieces; k += 32) {
-                const uint32_t q = k + lane, row = q / kPieces, piece = q - row * kPieces;
-                const uintptr_t begin = reinterpret_cast<uintptr_t>(at + int64_t(row) * stride);
-                const int left = int(begin & 15) + channels * int(sizeof(T)) - 16 * int(piece);
-                if (int(row) < (ALL ? STEPS : n) && left > 0)
-                    copy_async16(&rows.v[row][piece * kEach], reinterpret_cast<const void *>((begin & ~uintptr_t(15)) + 16 * piece), uint32_t(min(left, 16)));
+            for (int k = 0; k < STEPS; k += kAt, begin += uint64_t(stride * kAt) * sizeof(T)) {
+                const int left = int(begin & 15) + bytes - 16 * piece;
+                if ((ALL || first + k < n) && left > 0)
+                    copy_async16(&rows.v[first + k][piece * kEach], reinterpret_cast<const void *>((begin & ~uintptr_t(15)) + 16 * piece), uint32_t(min(left, 16)));
+            }
+            if (int(lane) < (ALL ? STEPS : n)) {                                // (n: 0 or less, of a warp behind the end)
+                begin = reinterpret_cast<uintptr_t>(at + int64_t(lane) * stride);
+                const int left = int(begin & 15) + bytes - 16 * kWhole;
+                if (left > 0) copy_async16(&rows.v[lane][kWhole * kEach], reinterpret_cast<const void *>((begin & ~uintptr_t(15)) + 16 * kWhole), uint32_t(left));
             }
         }
     }
