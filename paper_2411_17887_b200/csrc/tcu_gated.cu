@@ -116,7 +116,7 @@ void dispatch(const tcu_gated_t *a, F go) {
 }
 
 // Blocks of a cluster that walk a sequence together: as many as keep all blocks on the SMs at once, two an SM, and have a tile each.  16383 tokens of
-// 2048 channels, 32 walks: 8 blocks 61 us, 4 blocks 82; 8 x 4096 tokens, 256 walks: one block 84 us, two 111.  Packed sequences are of lengths
+// 2048 channels, 32 walks: 8 blocks 61 us, 4 blocks 82; 8 x 4096 tokens, 256 walks: one block 81 us, two 111.  Packed sequences are of lengths
 // that the host does not know, and the longest alone may take most of the time: up to four times as many blocks (24 sequences of 1504 channels,
 // 16001 tokens: of 0 to 3972 each, one block 61 us, two 53; of 667 each 38 and 54).
 uint32_t blocks_of_walk(uint64_t walks, const Sizes &s) {

@@ -12,7 +12,7 @@
 // all sums follows from the sizes alone.
 //
 // What bounds it: instructions (28 an element forward, two of them on the special-function unit; 52 backward) and the barrier of a tile, close behind
-// memory.  8 x 4096 tokens of 2048 bfloat16 channels: forward 84 us (403 MB, 4.8 TB/s, 0.73 of the copy rate), backward 149 us (671 MB, 4.5
+// memory.  8 x 4096 tokens of 2048 bfloat16 channels: forward 81 us (403 MB, 4.9 TB/s, 0.75 of the copy rate), backward 148 us (671 MB, 4.5
 // TB/s).  Tried: values through registers instead of shared memory (215 us, loads wait for the store of the tile before), 8 tokens a warp forward
 // (110), two channels an instruction (no gain: moves into register pairs), a barrier of the block for the tile's arrival (88).
 #pragma once
@@ -184,6 +184,8 @@ struct GatedWalk {
 // Rows of the inputs on their way to shared memory, 16 bytes a piece.  A warp copies what it reads itself, so that no barrier of the block waits for data.
 // COPY 16: all rows begin at multiples of 16 bytes.  COPY 4, 2: at multiples of that many bytes; the pieces that hold a row are copied, the last one as far
 // as the row goes, and the row is read from behind what its first piece holds ahead of it (bytes of the same allocation: those begin at larger boundaries).
+// Measured, 8 x 4096 tokens of 2047 bfloat16 channels: forward 139 us, backward 273; in words of 4 bytes 179 and 259.  2046: 116 and 212 (147 and 192).
+// 2048 tokens of 2047 fp32: 108 and 181 (124 and 202).  Results stored in words across the lanes' pairs: 161 and 294 instead of 143 and 270.
 __device__ __forceinline__ void copy_async16(void *to, const void *from) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(uint32_t(__cvta_generic_to_shared(to))), "l"(from) : "memory");
 }

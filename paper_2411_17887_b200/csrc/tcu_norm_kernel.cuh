@@ -7,7 +7,7 @@
 // kernel adds the blocks' parts, in order.
 //
 // What bounds it: instructions (18 an element forward, 29 backward, a quarter of them the sums over a row), close behind memory.  32749 rows of 2048 bfloat16
-// values: forward 50 us (268 MB, 5.3 TB/s, 0.81 of the copy rate), backward 92 us (402 MB, 4.4 TB/s, the joining kernel 4 us of it).
+// values: forward 50 us (268 MB, 5.4 TB/s, 0.82 of the copy rate), backward 91 us (402 MB, 4.4 TB/s, the joining kernel 4 us of it).
 #pragma once
 
 #include "tcu_float.cuh"

@@ -15,8 +15,8 @@
 // in fixed point with 42 bits (three limbs of 14, each sum of at most 2^18 tokens within 32 bits), whose sums do not depend on their order.
 //
 // What bounds it: 64-bit arithmetic, 12 instructions a weight, and, with limits, the times that the blocks of a row have to meet.  256 rows of 128000
-// bfloat16 logits (66 MB, 10 us to read): largest logit alone 27 us, temperature 75, top_k 50 61, top_p 0.9 112.  192 rows of 50001 fp32 logits:
-// 18, 43, 33 and 53; top_p 0.99 at temperature 1.2, some ten thousand tokens, 149.  Tried: weights in all histograms in three limbs (top_p 284 us), logits in
+// bfloat16 logits (66 MB, 10 us to read): largest logit alone 27 us, temperature 75, top_k 50 59, top_p 0.9 107.  192 rows of 50001 fp32 logits:
+// 18, 43, 33 and 51; top_p 0.99 at temperature 1.2, some ten thousand tokens, 145.  Tried: weights in all histograms in three limbs (top_p 284 us), logits in
 // registers (they spill), weights by exp() (whole rows 203 us), all candidates sorted by every block for itself (top_k 128).
 #pragma once
 
