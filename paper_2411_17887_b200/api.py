@@ -511,7 +511,8 @@ def gated_recurrence_backward(d_y, x, gate, initial_state=None, offsets=None, d_
     m = _Gated(x, gate, offsets, input_gate, initial_state=initial_state, d_final_state=d_final_state, marks=marks)
     if marks is None:
         marks = _gated_forward(x, gate, initial_state, offsets, False, input_gate, True, output=False)[2]
-    d_x, d_gate = _fresh(x), _fresh(x)
+    fresh = _fresh if offsets is None else _zeros                # (nothing flows back to the rows behind the last sequence)
+    d_x, d_gate = fresh(x), fresh(x)
     d_first = torch.empty_like(initial_state) if initial_state is not None else None
     (x, xv), (gate, gv), (d_y, yv) = _channels(x), _channels(gate), _channels(d_y)
     m.call(B.tcu_gated_backward, xv, gv, marks=marks, d_y=yv, d_x=(d_x.data_ptr(), *m.strides), d_gate=(d_gate.data_ptr(), *m.strides), d_dstate_out=_ptr(d_final_state),
@@ -547,7 +548,7 @@ def gated_recurrence(x, gate, initial_state=None, offsets=None, output_final_sta
 
     x, gate (batch, tokens, channels), float32, float16 or bfloat16, any strides; or packed (tokens, channels) with `offsets`, an int64
     tensor of batch + 1 values on the GPU: sequence b is [offsets[b], offsets[b + 1]), rows behind the last one are left as they
-    are (of fresh memory).  States (batch, channels) float32."""
+    are (of fresh memory), and their gradients are zero.  States (batch, channels) float32."""
     if forward_ad._current_level >= 0 or (torch.is_grad_enabled() and (x.requires_grad or gate.requires_grad or
                                                                        (initial_state is not None and initial_state.requires_grad))):
         y, last, marks = _GatedRecurrence.apply(x, gate, initial_state, offsets, output_final_state, input_gate, output_marks)
@@ -597,6 +598,10 @@ def gated_recurrence_step(x, gate, state, slots=None, input_gate="complement"):
 def _fresh(x: torch.Tensor) -> torch.Tensor:
     """An empty tensor of x's shape and type, contiguous."""
     return torch.empty_like(x, memory_format=torch.contiguous_format)
+
+
+def _zeros(x: torch.Tensor) -> torch.Tensor:
+    return torch.zeros_like(x, memory_format=torch.contiguous_format)
 
 
 def _rows(x: torch.Tensor):

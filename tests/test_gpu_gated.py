@@ -136,6 +136,32 @@ def test_strides(dtype):
     check(x, gate, d_y[..., :36], "one", torch.randn((3, 36), device="cuda"))
 
 
+@pytest.mark.parametrize("dtype", TYPES, ids=["f32", "f16", "bf16"])
+@pytest.mark.parametrize("d", [57, 63, 64, 65, 130])
+@pytest.mark.parametrize("at", [0, 1, 2, 3, 5, 6, 7])
+def test_rows_off_every_boundary(at, d, dtype):
+    """Rows that begin `at` elements behind a boundary of 16 bytes, one stride odd and one even, among values that are not finite."""
+    for t, wide in ((1, d + 3), (7, d + 4), (9, d + 3), (100, d + 4), (143, d + 3)):
+        held = torch.full((3, 2 * t * wide + 16), float("nan"), device="cuda", dtype=dtype)
+        views = [h.as_strided((2, t, d), (t * wide, wide, 1), h.storage_offset() + o) for h, o in zip(held, (at, (at + 3) % 8, (3 * at) % 8))]
+        for view, values in zip(views, draw((2, t, d), dtype, t + d)):
+            view.copy_(values)
+        check(*views, "complement", torch.randn((2, d), device="cuda"), torch.randn((2, d), device="cuda"))
+
+
+def test_no_gradient_behind_the_last_sequence():
+    x, gate, d_y = draw((100, 24), torch.bfloat16, 5)
+    junk = [torch.full((100, 24), float("nan"), device="cuda", dtype=torch.bfloat16) for _ in range(4)]    # what fresh memory may hold
+    d_y[70:] = float("nan")
+    offsets = torch.tensor([0, 30, 70], device="cuda")
+    leaves = [z.clone().requires_grad_() for z in (x, gate)]
+    y, _ = api.gated_recurrence(*leaves, offsets=offsets)
+    del junk
+    y.backward(d_y)
+    for leaf, want in zip(leaves, api.gated_recurrence_backward(d_y[:70], x[:70], gate[:70], offsets=offsets)):
+        assert (leaf.grad[70:] == 0).all() and torch.equal(leaf.grad[:70], want)
+
+
 def test_no_tokens():
     first = torch.randn((2, 10), device="cuda")
     empty = torch.empty((2, 0, 10), device="cuda", dtype=torch.float16)
