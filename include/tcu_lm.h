@@ -242,8 +242,9 @@ typedef struct {
     float *d_log_probs;         /* NULL, or receives the log of its probability                                     */
 } tcu_sample_t;
 
-/* What is written must not overlap an input.  Weights and sums are 64-bit floating point, sums that top_p is compared with fixed point of 42 bits: the
- * token is that of exact arithmetic unless u or top_p lies within about 1e-12 (top_p: 1e-9) of the border between two.
+/* What is written must not overlap an input.  Weights and sums are 64-bit floating point; where top_p ends among more than 512 tokens of nearly one weight, these are
+ * added up in 42 bits of the largest of them.  The token is that of exact arithmetic unless u or top_p lies within 1e-11 of the border between two, or min_p
+ * within 1e-11 of itself of a weight.
  * TCU_ERR_UNSUPPORTED: more than 2^18 tokens, or 2^28 - 1 rows. */
 tcu_status_t tcu_sample(const tcu_sample_t *args, cudaStream_t stream);
 

@@ -11,8 +11,10 @@
 // of numbers names; for top_p the largest few hundred, found the same way, if they have the weight, or those in the bin that a histogram of weights names.  That one is of 32-bit weights, and sums of 64-bit ones say whether the
 // bin is right.  Where a bin has more tokens, exact histograms of the logit's bits as an integer follow, 9 bits a time.
 //
-// Sums that decide which token it is are exact enough that it is the token of the definition: weights in 64-bit floating point, in exact histograms
-// in fixed point with 42 bits (three limbs of 14, each sum of at most 2^18 tokens within 32 bits), whose sums do not depend on their order.
+// Sums that decide which token it is are exact enough that it is the token of the definition, off its borders: weights in 64-bit floating point, in exact
+// histograms in fixed point with 42 bits (three limbs of 14, each sum of at most 2^18 tokens within 32 bits), whose sums do not depend on their order.
+// A weight is off by 1.3e-12 of itself (what its series leaves out), in fixed point by 2^-43 of the largest one of a bin, whose weights are at least exp(-1/64)
+// of it (but in the last bin, 32 or more below the top: by less than 1e-21 in all): a quotient of two sums is off by less than 4e-12.
 //
 // What bounds it: 64-bit arithmetic, 12 instructions a weight, and, with limits, the times that the blocks of a row have to meet.  256 rows of 128000
 // bfloat16 logits (66 MB, 10 us to read): largest logit alone 27 us, temperature 75, top_k 50 59, top_p 0.9 107.  192 rows of 50001 fp32 logits:
@@ -442,7 +444,8 @@ struct Sampler {
             at += turn * int(by);
         }
     }
-    // The prefix that ends in a bin: with `left` of its tokens' number, or weight.
+    // The prefix that ends in a bin: with `left` of its tokens' number, or weight.  Weights that are too many to be sorted are added up as parts of the bin's largest
+    // one: 42 bits of the row's would leave a light token few (one of 1e-8, 15 of them, and of 2^18 equal ones an error of one sign: 3e-8 in all).
     template <bool WEIGHTS>
     __device__ Prefix in_bin(float cut, float scale, int which, double left) {
         const uint32_t total = list_candidates([&](float x) { return bin(x, cut, scale) == which; });
@@ -462,7 +465,13 @@ struct Sampler {
         const uint2 ends = cluster_min(lo, hi_not);
         lo = ends.x;
         uint32_t hi = ~ends.y;
-        double before = 0.0, one = WEIGHTS ? double(fixed(sample_value(hi))) : 1.0, target = WEIGHTS ? left * kSampleFixed : left, many = 1.0;
+        const float of_row = top;
+        double before = 0.0, one = 1.0, target = left, many = 1.0;
+        if (WEIGHTS) {
+            const double largest = weight(sample_value(hi));
+            top = sample_value(hi);
+            target = largest > 0.0 ? fmax(left / largest * kSampleFixed, 0.5) : 0.5;      // (less than any weight counts for: at least the first token)
+        }
         do {
             const int bits = 32 - __clz(int(hi - lo)), shift = bits > kSampleFineBits ? bits - kSampleFineBits : 0;
             auto bin_of = [&](float x) {
@@ -481,6 +490,7 @@ struct Sampler {
             one = WEIGHTS ? double(fixed(sample_value(hi))) : 1.0;
             many = one > 0.0 ? double(g.bin < 0 ? 1 : g.in) / one : 1.0;
         } while (lo < hi);
+        top = of_row;
         const uint32_t most = uint32_t(fmax(rint(many), 1.0)), ties = uint32_t(fewest(before, one, target, most));
         return {sample_value(hi), ties, ties >= most};
     }
