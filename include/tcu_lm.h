@@ -161,7 +161,7 @@ typedef struct {
     const int64_t *d_offsets;   /* NULL: dense.  Packed: batch + 1 values, sequence b holds tokens [offsets[b], offsets[b+1]);
                                    non-decreasing, from 0 to at most `tokens` (not checked: they live on the device; what leaves the
                                    range is taken as its end); empty sequences are allowed, rows behind the last one
-                                   are not touched                                                                  */
+                                   are not touched (backward: as clear_rows says)                                   */
     const int32_t *d_slots;     /* step only: NULL, or for each sequence its entry in the state pool; entries outside it mark a
                                    sequence to skip (its output is zero); no two sequences may share an entry       */
     uint64_t pool_slots;        /* step only: entries of the pool (at least `batch` when d_slots is NULL)           */
@@ -178,6 +178,9 @@ typedef struct {
     const float *d_dstate_out;  /* backward: NULL (zero), or the gradient with respect to the state after the last token */
     float *d_dstate_in;         /* backward: NULL, or receives the gradient with respect to the state before the first; may be
                                    d_dstate_out itself, but not overlap it otherwise                                */
+    uint64_t clear_rows;        /* backward, packed: 1: rows of d_x and d_gate that belong to no sequence (ahead of the first, behind the last) are
+                                   set to zero, if there is a sequence; 0: they are not touched.  (A structure that ends ahead of this field is
+                                   taken with 0)                                                                    */
 } tcu_gated_t;
 
 /* Bytes of d_marks for `tokens` tokens in all of `batch` sequences (dense: batch times those of one); 0 for sizes whose bytes

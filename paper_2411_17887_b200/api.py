@@ -511,12 +511,13 @@ def gated_recurrence_backward(d_y, x, gate, initial_state=None, offsets=None, d_
     m = _Gated(x, gate, offsets, input_gate, initial_state=initial_state, d_final_state=d_final_state, marks=marks)
     if marks is None:
         marks = _gated_forward(x, gate, initial_state, offsets, False, input_gate, True, output=False)[2]
-    fresh = _fresh if offsets is None else _zeros                # (nothing flows back to the rows behind the last sequence)
+    # (nothing flows back to the rows of no sequence: the kernel sets them to zero, if there is one)
+    fresh = _zeros if offsets is not None and m.state_shape[0] == 0 else _fresh
     d_x, d_gate = fresh(x), fresh(x)
     d_first = torch.empty_like(initial_state) if initial_state is not None else None
     (x, xv), (gate, gv), (d_y, yv) = _channels(x), _channels(gate), _channels(d_y)
     m.call(B.tcu_gated_backward, xv, gv, marks=marks, d_y=yv, d_x=(d_x.data_ptr(), *m.strides), d_gate=(d_gate.data_ptr(), *m.strides), d_dstate_out=_ptr(d_final_state),
-           d_dstate_in=_ptr(d_first))
+           d_dstate_in=_ptr(d_first), clear_rows=int(offsets is not None))
     return d_x, d_gate, d_first
 
 

@@ -299,17 +299,17 @@ def tcu_embedding_backward(d_out, dtype: int, d_ids, id_bytes: int, n: int, rows
 
 
 # tcu_gated_t, packed as bytes; an array of rows is (pointer, stride_batch, stride_token)
-_GATED = struct.Struct("=IIIIQQQQQ" + "Qqq" * 3 + "QQQQ" + "Qqq" * 3 + "QQ")
+_GATED = struct.Struct("=IIIIQQQQQ" + "Qqq" * 3 + "QQQQ" + "Qqq" * 3 + "QQQ")
 NO_ROWS = (0, 0, 0)
 INPUT_GATES = {"complement": 0, "one": 1, "root": 2}
 
 
 def tcu_gated_args(dtype: int, input_gate: int, channels: int, batch: int, tokens: int, x, gate, y=NO_ROWS, *, d_offsets: int = 0, d_slots: int = 0, pool_slots: int = 0,
                    d_state_in: int = 0, d_state_out: int = 0, d_marks: int = 0, marks_bytes: int = 0, d_y=NO_ROWS, d_x=NO_ROWS, d_gate=NO_ROWS, d_dstate_out: int = 0,
-                   d_dstate_in: int = 0) -> bytes:
+                   d_dstate_in: int = 0, clear_rows: int = 0) -> bytes:
     """The argument structure of the gated recurrence's calls; pointers are integers (0 for NULL)."""
     return _GATED.pack(_GATED.size, dtype, input_gate, channels, batch, tokens, d_offsets, d_slots, pool_slots, *x, *gate, *y, d_state_in, d_state_out, d_marks, marks_bytes,
-                       *d_y, *d_x, *d_gate, d_dstate_out, d_dstate_in)
+                       *d_y, *d_x, *d_gate, d_dstate_out, d_dstate_in, clear_rows)
 
 
 def tcu_gated_marks_bytes(batch: int, tokens: int, channels: int) -> int:

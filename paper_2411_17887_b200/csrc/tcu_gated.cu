@@ -2,6 +2,7 @@
 #include "tcu_lm.h"
 
 #include <cuda_runtime.h>
+#include <stddef.h>
 
 #include <initializer_list>
 #include <type_traits>
@@ -18,6 +19,7 @@ constexpr uint64_t kMostTokens = (uint64_t(1) << 31) - 8192;                // (
 constexpr uint32_t kMostChannels = uint32_t(1) << 30;
 constexpr uint64_t kSms = 148;
 constexpr int64_t kMostStride = int64_t(1) << 38;
+constexpr size_t kBytesBeforeClear = offsetof(tcu_gated_t, clear_rows);     // of the structure when it ended ahead of clear_rows, which is then 0
 
 // First and one-past-last byte that an array may touch; to the end of all addresses if it has no such last byte.
 struct Span {
@@ -89,7 +91,7 @@ GatedParams params(const tcu_gated_t *a) {
 }
 
 tcu_status_t check(const tcu_gated_t *a, Sizes &s) {
-    if (!a || a->struct_bytes != sizeof(tcu_gated_t)) return TCU_ERR_INVALID_ARG;
+    if (!a || (a->struct_bytes != sizeof(tcu_gated_t) && a->struct_bytes != kBytesBeforeClear)) return TCU_ERR_INVALID_ARG;
     if (!valid_float(int(a->type)) || a->input_gate > TCU_INPUT_ROOT || a->channels == 0) return TCU_ERR_INVALID_ARG;
     if (a->channels > kMostChannels || a->tokens > kMostTokens) return TCU_ERR_UNSUPPORTED;
     const uint64_t strips = (uint64_t(a->channels) + kGatedChannels - 1) / kGatedChannels;
@@ -200,6 +202,8 @@ tcu_status_t tcu_gated_backward(const tcu_gated_t *a, cudaStream_t stream) {
             if (!s.right(*r, true)) return TCU_ERR_INVALID_ARG;
         if (a->d_x.ptr == a->d_gate.ptr) return TCU_ERR_INVALID_ARG;
     }
+    const uint64_t clear = a->struct_bytes == kBytesBeforeClear ? 0 : a->clear_rows;
+    if (clear > 1) return TCU_ERR_INVALID_ARG;
     const size_t marks = tcu_gated_marks_bytes(a->batch, s.packed ? a->tokens : a->batch * a->tokens, a->channels);
     if (!a->d_marks || marks == 0 || a->marks_bytes < marks) return TCU_ERR_WORKSPACE;
     const Span kept = {reinterpret_cast<uintptr_t>(a->d_marks), reinterpret_cast<uintptr_t>(a->d_marks) + marks};
@@ -214,6 +218,7 @@ tcu_status_t tcu_gated_backward(const tcu_gated_t *a, cudaStream_t stream) {
     GatedParams p = params(a);
     tcu_status_t st = TCU_OK;
     p.ranks = blocks_of_walk(a->batch * p.strips, s);
+    p.clear = clear && s.packed && a->tokens > 0;
     const int way = s.way({&a->x, &a->gate, &a->d_y}, {&a->d_x, &a->d_gate});
     dispatch(a, [&](auto t, auto in) {
         using T = decltype(t);

@@ -48,6 +48,7 @@ struct GatedParams {
     uint32_t channels, strips;
     uint32_t ranks;            // blocks of a cluster
     int ordered;               // packed: so many sequences (at most kGatedOrdered) are walked in the order of their lengths; or 0
+    int clear;                 // packed, backward: rows that belong to no sequence are set to zero
 };
 
 // Stores the two channels of a lane: in one access where they are aligned for it (PAIR), else one each.
@@ -290,6 +291,20 @@ __device__ __forceinline__ void store_rows(T *at, int64_t stride, int n, bool c0
     }
 }
 
+// Sets the rows of d_x and d_gate that lie ahead of the first sequence and behind the last one to zero, in the channels of this block: the blocks of these channels
+// take turns.  24 sequences of 16001 tokens in all, 1504 bfloat16 channels, no such row: 91 us; with both arrays cleared whole ahead of the kernel 120.
+template <typename T, bool PAIR>
+__device__ __forceinline__ void clear_rows(const GatedParams &p, uint32_t c, bool c0, bool c1) {
+    const int64_t first = GatedWalk::first(p, 0), tokens = int64_t(p.tokens), batch = gridDim.x / (p.strips * p.ranks);
+    const int64_t last = max(GatedWalk::first(p, uint32_t(batch)), first), outside = first + tokens - last;
+    const int64_t place = int64_t(blockIdx.x / (p.strips * p.ranks)) * p.ranks + blockIdx.x % p.ranks;
+    for (int64_t k = place * kGatedWarps + (threadIdx.x >> 5); k < outside; k += batch * p.ranks * kGatedWarps) {
+        const int64_t row = k < first ? k : k - first + last;
+        store_two<T, PAIR>(static_cast<T *>(p.d_x.ptr) + row * p.d_x.token + c, 0.0f, 0.0f, c0, c1);
+        store_two<T, PAIR>(static_cast<T *>(p.d_gate.ptr) + row * p.d_gate.token + c, 0.0f, 0.0f, c0, c1);
+    }
+}
+
 // The pairs of a lane's two channels: (f, f', b, b').
 __device__ __forceinline__ float4 pairs_of(float2 f, float2 b) { return make_float4(f.x, f.y, b.x, b.y); }
 __device__ __forceinline__ float2 apply(const float4 &q, float2 h) { return fma2(make_float2(q.x, q.y), h, make_float2(q.z, q.w)); }
@@ -463,6 +478,7 @@ __global__ void __launch_bounds__(kGatedWarps * 32, 2) tcu_gated_backward_kernel
     const uint32_t c = w.c0 + 2 * lane;
     const int wide = int(min(p.channels - w.c0, uint32_t(kGatedChannels)));
     const bool c0 = c < p.channels, c1 = c + 1 < p.channels;
+    if (p.clear) clear_rows<T, PAIR>(p, c, c0, c1);
     const T *px = w.at<T>(p, p.x, w.c0), *pg = w.at<T>(p, p.gate, w.c0), *pd = w.at<T>(p, p.d_y, w.c0);
     float2 flow = make_float2(0.0f, 0.0f);                                 // C at the end of the blocks' tiles
     const uint64_t st = uint64_t(w.seq) * p.channels + c;
