@@ -17,7 +17,7 @@ using namespace tcu;
 constexpr uint64_t kMostWalks = (uint64_t(1) << 31) - 1;
 constexpr uint64_t kMostTokens = (uint64_t(1) << 31) - 8192;                // (positions ahead of the last tile are 32-bit integers too)
 constexpr uint32_t kMostChannels = uint32_t(1) << 30;
-constexpr uint64_t kSms = 148;
+constexpr uint64_t kSms = 148, kSharedOfSm = 228 * 1024, kSharedOfBlock = 1024;              // (shared memory of an SM, and what a block takes of it besides its own)
 constexpr int64_t kMostStride = int64_t(1) << 38;
 constexpr size_t kBytesBeforeClear = offsetof(tcu_gated_t, clear_rows);     // of the structure when it ended ahead of clear_rows, which is then 0
 
@@ -117,33 +117,41 @@ void dispatch(const tcu_gated_t *a, F go) {
     else input(__nv_bfloat16{});
 }
 
-// Blocks of a cluster that walk a sequence together: as many as keep all blocks on the SMs at once, two an SM, and have a tile each.  16383 tokens of
-// 2048 channels, 32 walks: 8 blocks 61 us, 4 blocks 82; 8 x 4096 tokens, 256 walks: one block 81 us, two 111.  Packed sequences are of lengths
+// Blocks that the SMs hold at once, two an SM by their registers, if their shared memory lets them.  (bytes: of it, by the blocks of a cluster)
+template <auto bytes>
+uint64_t blocks_at_once(uint32_t ranks) { return kSms * (2 * (bytes(ranks) + kSharedOfBlock) <= kSharedOfSm ? 2 : 1); }
+
+// Blocks of a cluster that walk a sequence together: as many as keep all blocks on the SMs at once and have a tile each.  16383 tokens of
+// 2048 channels, 32 walks: 8 blocks 61 us, 4 blocks 82; 8 x 4096 tokens, 256 walks: one block 81 us, two 111.  Gradients of 32-bit
+// elements have room for two blocks an SM only where a block walks alone (off 16 bytes not even there): 8 x 4096 tokens of 1024 channels, 128 walks, one block
+// 124 us, two 171; 32 walks of 16383 tokens, four blocks 175, eight 267.  Packed sequences are of lengths
 // that the host does not know, and the longest alone may take most of the time: up to four times as many blocks (24 sequences of 1504 channels,
 // 16001 tokens: of 0 to 3972 each, one block 61 us, two 53; of 667 each 38 and 54).
+template <auto bytes>
 uint32_t blocks_of_walk(uint64_t walks, const Sizes &s) {
-    const uint64_t most = s.packed ? 4 * 2 * kSms : 2 * kSms, tiles = s.packed ? 4 * s.tokens / s.batch / 128 : (s.tokens + 127) / 128;
+    const uint64_t tiles = s.packed ? 4 * s.tokens / s.batch / 128 : (s.tokens + 127) / 128;
     uint32_t ranks = 1;
-    while (ranks < kGatedMaxCluster && walks * ranks * 2 <= most && ranks * 2 <= tiles) ranks *= 2;
+    while (ranks < kGatedMaxCluster && walks * ranks * 2 <= (s.packed ? 4 : 1) * blocks_at_once<bytes>(ranks * 2) && ranks * 2 <= tiles) ranks *= 2;
     return ranks;
 }
 
-// (bytes: of shared memory, by the blocks of a cluster)
 template <auto kernel, auto bytes>
-tcu_status_t launch_walks(const GatedParams &p, uint64_t batch, cudaStream_t stream) {
+tcu_status_t launch_walks(const GatedParams &p, const Sizes &s, cudaStream_t stream) {
     if (!allow_shared<kernel>(bytes(kGatedMaxCluster))) return TCU_ERR_CUDA;
     GatedParams q = p;
+    const uint64_t batch = s.batch;
+    q.ranks = blocks_of_walk<bytes>(batch * p.strips, s);
     // Long packed sequences first, where not all blocks run at once: 24 sequences of 0 to 3972 tokens, 1504 channels, 73 -> 53 us.  Found by every block for
     // itself: 200 sequences of 100 tokens would take 87 us instead of 54, and need it less.
-    if (p.offsets && batch > 1 && batch <= kGatedOrdered && batch * p.strips * p.ranks > 2 * kSms) q.ordered = int(batch);
+    if (p.offsets && batch > 1 && batch <= kGatedOrdered && batch * p.strips * q.ranks > blocks_at_once<bytes>(q.ranks)) q.ordered = int(batch);
     cudaLaunchAttribute attr;
     attr.id = cudaLaunchAttributeClusterDimension;
-    attr.val.clusterDim.x = p.ranks;
+    attr.val.clusterDim.x = q.ranks;
     attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(uint32_t(batch * p.strips * p.ranks));
+    cfg.gridDim = dim3(uint32_t(batch * p.strips * q.ranks));
     cfg.blockDim = dim3(kGatedWarps * 32);
-    cfg.dynamicSmemBytes = bytes(p.ranks);
+    cfg.dynamicSmemBytes = bytes(q.ranks);
     cfg.stream = stream;
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
@@ -179,14 +187,13 @@ tcu_status_t tcu_gated_forward(const tcu_gated_t *a, cudaStream_t stream) {
     if (a->d_state_in != a->d_state_out && meet(in, out)) return TCU_ERR_INVALID_ARG;
     GatedParams p = params(a);
     tcu_status_t st = TCU_OK;
-    p.ranks = blocks_of_walk(a->batch * p.strips, s);
     const int way = s.way({&a->x, &a->gate}, {&a->y});
     dispatch(a, [&](auto t, auto in) {
         using T = decltype(t);
         constexpr int kInput = decltype(in)::value, kLast = sizeof(T) == 2 ? 2 : 4;
-        if (way == 0) st = launch_walks<tcu_gated_forward_kernel<T, kInput, 16, true>, forward_bytes<T, 16>>(p, a->batch, stream);
-        else if (way == 1) st = launch_walks<tcu_gated_forward_kernel<T, kInput, 4, true>, forward_bytes<T, 4>>(p, a->batch, stream);
-        else st = launch_walks<tcu_gated_forward_kernel<T, kInput, kLast, false>, forward_bytes<T, kLast>>(p, a->batch, stream);
+        if (way == 0) st = launch_walks<tcu_gated_forward_kernel<T, kInput, 16, true>, forward_bytes<T, 16>>(p, s, stream);
+        else if (way == 1) st = launch_walks<tcu_gated_forward_kernel<T, kInput, 4, true>, forward_bytes<T, 4>>(p, s, stream);
+        else st = launch_walks<tcu_gated_forward_kernel<T, kInput, kLast, false>, forward_bytes<T, kLast>>(p, s, stream);
     });
     return st;
 }
@@ -217,15 +224,14 @@ tcu_status_t tcu_gated_backward(const tcu_gated_t *a, cudaStream_t stream) {
     if (a->d_dstate_in != a->d_dstate_out && meet(in, out)) return TCU_ERR_INVALID_ARG;
     GatedParams p = params(a);
     tcu_status_t st = TCU_OK;
-    p.ranks = blocks_of_walk(a->batch * p.strips, s);
     p.clear = clear && s.packed && a->tokens > 0;
     const int way = s.way({&a->x, &a->gate, &a->d_y}, {&a->d_x, &a->d_gate});
     dispatch(a, [&](auto t, auto in) {
         using T = decltype(t);
         constexpr int kInput = decltype(in)::value, kLast = sizeof(T) == 2 ? 2 : 4;
-        if (way == 0) st = launch_walks<tcu_gated_backward_kernel<T, kInput, 16, true>, backward_bytes<T, 16>>(p, a->batch, stream);
-        else if (way == 1) st = launch_walks<tcu_gated_backward_kernel<T, kInput, 4, true>, backward_bytes<T, 4>>(p, a->batch, stream);
-        else st = launch_walks<tcu_gated_backward_kernel<T, kInput, kLast, false>, backward_bytes<T, kLast>>(p, a->batch, stream);
+        if (way == 0) st = launch_walks<tcu_gated_backward_kernel<T, kInput, 16, true>, backward_bytes<T, 16>>(p, s, stream);
+        else if (way == 1) st = launch_walks<tcu_gated_backward_kernel<T, kInput, 4, true>, backward_bytes<T, 4>>(p, s, stream);
+        else st = launch_walks<tcu_gated_backward_kernel<T, kInput, kLast, false>, backward_bytes<T, kLast>>(p, s, stream);
     });
     return st;
 }
