@@ -186,7 +186,7 @@ struct GatedWalk {
 // COPY 16: all rows begin at multiples of 16 bytes.  COPY 4, 2: at multiples of that many bytes; the pieces that hold a row are copied, the last one as far
 // as the row goes, and the row is read from behind what its first piece holds ahead of it (bytes of the same allocation: those begin at larger boundaries).
 // Measured, 8 x 4096 tokens of 2047 bfloat16 channels: forward 139 us, backward 273; in words of 4 bytes 179 and 259.  2046: 116 and 212 (147 and 192).
-// 2048 tokens of 2047 fp32: 108 and 181 (124 and 202).  Results stored in words across the lanes' pairs: 161 and 294 instead of 143 and 270.
+// 2048 tokens of 2047 fp32: 93 and 181 (124 and 202).  Results stored in words across the lanes' pairs: 161 and 294 instead of 143 and 270.
 __device__ __forceinline__ void copy_async16(void *to, const void *from) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(uint32_t(__cvta_generic_to_shared(to))), "l"(from) : "memory");
 }
@@ -376,8 +376,10 @@ constexpr uint32_t backward_bytes(uint32_t ranks) {
 }
 
 // Blocks of a cluster walk a sequence together, block r tile r of every `ranks` tiles.
+// Shared memory holds two blocks an SM.  The third one of the bound, of aligned 32-bit elements, stands for its 80 registers: 8 x 2048 tokens of 2048 channels 71.6 us, with
+// 126 registers 74.6.  Off 16 bytes 80 are too few (they spill): 2047 channels 107 us, with 127 registers 93.
 template <typename T, int INPUT, int COPY, bool PAIR>
-__global__ void __launch_bounds__(kGatedWarps * 32, sizeof(T) == 2 ? 2 : 3) tcu_gated_forward_kernel(const GatedParams p) {
+__global__ void __launch_bounds__(kGatedWarps * 32, sizeof(T) == 4 && COPY == 16 ? 3 : 2) tcu_gated_forward_kernel(const GatedParams p) {
     constexpr int STEPS = kForwardSteps<T>, TILE = STEPS * kGatedWarps;
     static_assert(TILE % kGatedMark == 0 && kGatedMark % STEPS == 0, "marks lie where a warp begins");
     extern __shared__ __align__(16) uint8_t shared[];
