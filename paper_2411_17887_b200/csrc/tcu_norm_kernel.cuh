@@ -3,7 +3,8 @@
 //     dx = r (e - mean(e) - u mean(e u))        dweight = sum over rows of dy u        dbias = sum over rows of dy
 // A row is held in registers, 16 elements a thread, by some lanes of a warp, a warp or a block, so that x (and dy) is read once; mean and
 // variance are those of the values less a first mean, which takes what rounding of the first mean leaves out again.  A block goes through rows
-// in steps of the grid, the next three on their way to shared memory, and adds up its part of the parameters' gradients in registers; a second
+// in steps of the grid - those of 16 bits, 16 elements a thread, with the next two on their way to shared memory, others with the next one on its way to registers forward and
+// none backward - and adds up its part of the parameters' gradients in registers; a second
 // kernel adds the blocks' parts, in order.
 //
 // What bounds it: instructions (18 an element forward, 29 backward, a quarter of them the sums over a row), close behind memory.  32749 rows of 2048 bfloat16
@@ -16,9 +17,9 @@ namespace tcu {
 
 constexpr int kNormWarps = 8;              // of a block, where a warp holds one row or several
 constexpr int kNormThreads = 512;          // at most, where a block holds a row: 128 registers each
-// Rows in shared memory of a thread, one that it works on and the others on their way, where it holds `bytes` of each (0: none, too many
-// for two rows of two arrays).
-__host__ __device__ constexpr int norm_ahead(int bytes) { return bytes <= 16 ? 4 : bytes <= 32 ? 3 : 0; }
+// Rows in shared memory of a thread, one that it works on and the others on their way, where it holds `bytes` of each: 16 elements of 16 bits (0: none, more are too many
+// for three rows of two arrays).
+__host__ __device__ constexpr int norm_ahead(int bytes) { return bytes <= 32 ? 3 : 0; }
 
 struct NormParams {
     const void *x, *d_y, *weight, *bias;
