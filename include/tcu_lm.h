@@ -200,7 +200,8 @@ tcu_status_t tcu_gated_forward(const tcu_gated_t *args, cudaStream_t stream);
  * y and the states themselves are not used: h is formed again from the marks, in 32 bits. */
 tcu_status_t tcu_gated_backward(const tcu_gated_t *args, cudaStream_t stream);
 
-/* One token for each of `batch` sequences: the state of each is updated in place, and y written (y may be x or gate, with its strides). */
+/* One token for each of `batch` sequences: the state of each is updated in place, and y written (y may be x or gate, with its strides).
+ * TCU_ERR_UNSUPPORTED: more than 2^31 - 1 blocks of 64 channels of a sequence. */
 tcu_status_t tcu_gated_step(const tcu_gated_t *args, cudaStream_t stream);
 
 /* ---- layer norm: y = weight * (x - mean) / sqrt(variance + eps) + bias over each row of d elements, the variance that of all d elements

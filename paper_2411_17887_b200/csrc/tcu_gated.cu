@@ -90,17 +90,17 @@ GatedParams params(const tcu_gated_t *a) {
     return p;
 }
 
-tcu_status_t check(const tcu_gated_t *a, Sizes &s) {
+tcu_status_t check(const tcu_gated_t *a, uint64_t tokens, Sizes &s) {
     if (!a || (a->struct_bytes != sizeof(tcu_gated_t) && a->struct_bytes != kBytesBeforeClear)) return TCU_ERR_INVALID_ARG;
     if (!valid_float(int(a->type)) || a->input_gate > TCU_INPUT_ROOT || a->channels == 0) return TCU_ERR_INVALID_ARG;
-    if (a->channels > kMostChannels || a->tokens > kMostTokens) return TCU_ERR_UNSUPPORTED;
+    if (a->channels > kMostChannels || tokens > kMostTokens) return TCU_ERR_UNSUPPORTED;
     const uint64_t strips = (uint64_t(a->channels) + kGatedChannels - 1) / kGatedChannels;
     if (a->batch > kMostWalks / strips) return TCU_ERR_UNSUPPORTED;
     if (!aligned(a->d_offsets, 8)) return TCU_ERR_INVALID_ARG;
     for (const void *q : {static_cast<const void *>(a->d_state_in), static_cast<const void *>(a->d_state_out), static_cast<const void *>(a->d_marks),
                           static_cast<const void *>(a->d_dstate_out), static_cast<const void *>(a->d_dstate_in)})
         if (!aligned(q, 4)) return TCU_ERR_INVALID_ARG;
-    s = {a->d_offsets != nullptr, a->batch, a->tokens, a->channels, float_bytes(tcu_float_t(a->type))};
+    s = {a->d_offsets != nullptr, a->batch, tokens, a->channels, float_bytes(tcu_float_t(a->type))};
     return TCU_OK;
 }
 
@@ -169,7 +169,7 @@ size_t tcu_gated_marks_bytes(uint64_t batch, uint64_t tokens, uint32_t channels)
 
 tcu_status_t tcu_gated_forward(const tcu_gated_t *a, cudaStream_t stream) {
     Sizes s;
-    if (tcu_status_t st = check(a, s)) return st;
+    if (tcu_status_t st = check(a, a ? a->tokens : 0, s)) return st;
     if (a->batch == 0) return TCU_OK;
     const bool tokens = a->tokens > 0;
     if (tokens && (!s.right(a->x, false) || !s.right(a->gate, false) || (a->y.ptr && !s.right(a->y, true)))) return TCU_ERR_INVALID_ARG;
@@ -200,7 +200,7 @@ tcu_status_t tcu_gated_forward(const tcu_gated_t *a, cudaStream_t stream) {
 
 tcu_status_t tcu_gated_backward(const tcu_gated_t *a, cudaStream_t stream) {
     Sizes s;
-    if (tcu_status_t st = check(a, s)) return st;
+    if (tcu_status_t st = check(a, a ? a->tokens : 0, s)) return st;
     if (a->batch == 0) return TCU_OK;
     if (a->tokens > 0) {
         for (const tcu_rows_t *r : {&a->x, &a->gate, &a->d_y})
@@ -238,10 +238,9 @@ tcu_status_t tcu_gated_backward(const tcu_gated_t *a, cudaStream_t stream) {
 
 tcu_status_t tcu_gated_step(const tcu_gated_t *a, cudaStream_t stream) {
     Sizes s;
-    if (tcu_status_t st = check(a, s)) return st;
+    if (tcu_status_t st = check(a, 1, s)) return st;
     if (a->d_offsets) return TCU_ERR_INVALID_ARG;
     if (a->batch == 0) return TCU_OK;
-    s.tokens = 1;
     if (!s.right(a->x, false) || !s.right(a->gate, false) || !s.right(a->y, true)) return TCU_ERR_INVALID_ARG;
     if (!a->d_state_out || !aligned(a->d_slots, 4) || (!a->d_slots && a->pool_slots < a->batch)) return TCU_ERR_INVALID_ARG;
     if (a->batch > (kMostWalks * 256) / a->channels) return TCU_ERR_UNSUPPORTED;
