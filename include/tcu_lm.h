@@ -188,7 +188,7 @@ typedef struct {
 size_t tcu_gated_marks_bytes(uint64_t batch, uint64_t tokens, uint32_t channels);
 
 /* y and, if asked for, the state after the last token (a sequence without tokens: the state before).  What is written must not
- * overlap an input, from the first byte of each to the last.  Gates of -inf (f = 0) and +inf (f = 1) are as any other; NaN and infinities stay in
+ * overlap an input, offsets among them, from the first byte of each to the last.  Gates of -inf (f = 0) and +inf (f = 1) are as any other; NaN and infinities stay in
  * their channel and sequence, from their token on.
  * Sums, states and marks are in 32 bits.  The smaller one of f and 1 - f is off by 10 * 2^-24 of itself, where x and gate have 16 bits by 1.3 |gate| * 2^-24 besides (a
  * step: not), the other one by that and its rounding: a prompt's state and that of its tokens one by one agree to this.
@@ -200,7 +200,8 @@ tcu_status_t tcu_gated_forward(const tcu_gated_t *args, cudaStream_t stream);
  * y and the states themselves are not used: h is formed again from the marks, in 32 bits. */
 tcu_status_t tcu_gated_backward(const tcu_gated_t *args, cudaStream_t stream);
 
-/* One token for each of `batch` sequences: the state of each is updated in place, and y written (y may be x or gate, with its strides).
+/* One token for each of `batch` sequences: the state of each is updated in place, and y written (y may be x or gate, with its strides;
+ * else what is written overlaps no input, slots among them).
  * TCU_ERR_UNSUPPORTED: more than 2^31 - 1 blocks of 64 channels of a sequence. */
 tcu_status_t tcu_gated_step(const tcu_gated_t *args, cudaStream_t stream);
 

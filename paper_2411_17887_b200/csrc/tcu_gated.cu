@@ -51,6 +51,12 @@ struct Sizes {
             if (s < 0 || s > kMostStride) return false;
         return !written || !((!packed && batch > 1 && r.stride_batch == 0) || (tokens > 1 && r.stride_token == 0));
     }
+    // `count` indices of `bytes` each, or none
+    static Span indices(const void *p, uint64_t count, size_t bytes) {
+        const auto lo = reinterpret_cast<uintptr_t>(p);
+        const unsigned __int128 end = (unsigned __int128)(lo) + (p ? (unsigned __int128)(count) * bytes : 0);
+        return {lo, end > ~uintptr_t(0) ? ~uintptr_t(0) : uintptr_t(end)};
+    }
     // whether all rows of an array begin at multiples of `bytes`, and have a number of them
     bool multiples(const tcu_rows_t &r, size_t bytes) const {
         const int64_t each = int64_t(bytes / element);
@@ -176,7 +182,7 @@ tcu_status_t tcu_gated_forward(const tcu_gated_t *a, cudaStream_t stream) {
     const uint64_t all = s.packed ? a->tokens : a->batch * a->tokens;
     const size_t marks = tcu_gated_marks_bytes(a->batch, all, a->channels);
     if (a->d_marks && (marks == 0 || a->marks_bytes < marks)) return TCU_ERR_WORKSPACE;
-    const Span inputs[] = {s.span(a->x), s.span(a->gate)};
+    const Span inputs[] = {s.span(a->x), s.span(a->gate), Sizes::indices(a->d_offsets, a->batch + 1, 8)};
     const Span y = a->y.ptr ? s.span(a->y) : Span{0, 0};
     const Span kept = a->d_marks ? Span{reinterpret_cast<uintptr_t>(a->d_marks), reinterpret_cast<uintptr_t>(a->d_marks) + marks} : Span{0, 0};
     const Span in = a->d_state_in ? s.states(a->d_state_in) : Span{0, 0}, out = a->d_state_out ? s.states(a->d_state_out) : Span{0, 0};
@@ -215,7 +221,7 @@ tcu_status_t tcu_gated_backward(const tcu_gated_t *a, cudaStream_t stream) {
     if (!a->d_marks || marks == 0 || a->marks_bytes < marks) return TCU_ERR_WORKSPACE;
     const Span kept = {reinterpret_cast<uintptr_t>(a->d_marks), reinterpret_cast<uintptr_t>(a->d_marks) + marks};
     const Span in = a->d_dstate_out ? s.states(a->d_dstate_out) : Span{0, 0}, out = a->d_dstate_in ? s.states(a->d_dstate_in) : Span{0, 0};
-    const Span inputs[] = {s.span(a->x), s.span(a->gate), s.span(a->d_y), kept};
+    const Span inputs[] = {s.span(a->x), s.span(a->gate), s.span(a->d_y), kept, Sizes::indices(a->d_offsets, a->batch + 1, 8)};
     const Span dx = s.span(a->d_x), dg = s.span(a->d_gate);
     for (const Span &w : {dx, dg, out})
         for (const Span &i : inputs)
@@ -246,7 +252,8 @@ tcu_status_t tcu_gated_step(const tcu_gated_t *a, cudaStream_t stream) {
     if (a->batch > (kMostWalks * 256) / a->channels) return TCU_ERR_UNSUPPORTED;
     Sizes pool = s;
     pool.batch = a->pool_slots;
-    const Span states = pool.states(a->d_state_out), y = s.span(a->y);
+    const Span states = pool.states(a->d_state_out), y = s.span(a->y), slots = Sizes::indices(a->d_slots, a->batch, 4);
+    if (meet(slots, states) || meet(slots, y)) return TCU_ERR_INVALID_ARG;
     if (meet(states, y) || meet(states, s.span(a->x)) || meet(states, s.span(a->gate))) return TCU_ERR_INVALID_ARG;
     for (const tcu_rows_t *r : {&a->x, &a->gate})
         if (meet(y, s.span(*r)) && !(r->ptr == a->y.ptr && (a->batch == 1 || r->stride_batch == a->y.stride_batch))) return TCU_ERR_INVALID_ARG;
