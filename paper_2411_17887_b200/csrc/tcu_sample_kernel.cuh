@@ -16,9 +16,10 @@
 // A weight is off by 1.3e-12 of itself (what its series leaves out), in fixed point by 2^-43 of the largest one of a bin, whose weights are at least exp(-1/64)
 // of it (but in the last bin, 32 or more below the top: by less than 1e-21 in all): a quotient of two sums is off by less than 4e-12.
 //
-// What bounds it: 64-bit arithmetic, 12 instructions a weight, and, with limits, the times that the blocks of a row have to meet.  256 rows of 128000
-// bfloat16 logits (66 MB, 10 us to read): largest logit alone 27 us, temperature 75, top_k 50 59, top_p 0.9 107.  192 rows of 50001 fp32 logits:
-// 18, 43, 33 and 51; top_p 0.99 at temperature 1.2, some ten thousand tokens, 145.  Tried: weights in all histograms in three limbs (top_p 284 us), logits in
+// What bounds it: instructions, 48 a token, 12 of them 64-bit arithmetic (issued in 73 % of the cycles of an SM with work; bank conflicts, those of the table, take 12 % of
+// them in a shared memory that is busy for 37 %), and, with limits, the times that the blocks of a row have to meet.  256 rows of 128000 bfloat16 logits, a few of them far above the others
+// (66 MB, 10 us to read): largest logit alone 28 us, temperature 75, top_k 50 58, top_p 0.9 107 (388 where it keeps 30000 tokens).  192 rows of 50001 fp32 logits:
+// 18, 44, 33 and 51; top_p 0.99 at temperature 1.2, some ten thousand tokens, 145.  Tried: weights in all histograms in three limbs (top_p 284 us), logits in
 // registers (they spill), weights by exp() (whole rows 203 us), all candidates sorted by every block for itself (top_k 128).
 #pragma once
 
