@@ -13,7 +13,7 @@ SMS, OF_SM, OF_BLOCK = 148, 228 * 1024, 1024
 @pytest.fixture(scope="module")
 def lib(tmp_path_factory):
     out = str(tmp_path_factory.mktemp("fake") / "libtcu_gated_fake.so")
-    subprocess.run(["nvcc", "-gencode", "arch=compute_100a,code=compute_100a", "-std=c++17", "-O0", "--cudart", "none", "-shared", "-Xcompiler", "-fPIC", "-Xlinker", "-Bsymbolic",
+    subprocess.run(["nvcc", "-gencode", "arch=compute_100a,code=compute_100a", "-std=c++17", "-O0", "-Xcicc", "-O0", "--cudart", "none", "-shared", "-Xcompiler", "-fPIC", "-Xlinker", "-Bsymbolic",
                     "-I", os.path.join(ROOT, "include"), "-o", out, os.path.join(ROOT, "paper_2411_17887_b200", "csrc", "tcu_gated.cu"), os.path.join(HERE, "fake_launches.cpp")], check=True)
     lib = ctypes.CDLL(out, mode=os.RTLD_LOCAL | os.RTLD_NOW)
     lib.fake_last_shared.restype = ctypes.c_size_t
